@@ -11,6 +11,8 @@
  *   5. statistical bias correction (Eq. 11-15)               aweq_bias_correct
  *   6. 8-bit quantisation of the equalised inputs (W8A8)     aweq_quant_act
  * aweq_layer_pass runs all six for one input and the matrices it feeds.
+ * A calibrated W8A8 layer is then run with aweq_linear_w8a8, and its attention with
+ * aweq_kv_append and aweq_prefix_attention (end of this header).
  * Around the pass: aweq_fold_scale folds diag(s)^-1 into the producer of an input
  * (Section 3.1); aweq_forward_check (W8A8) and aweq_forward_check_weights (weight-only)
  * measure what Eq. 11 names, E[y~ - y], for a calibrated layer on the tensor cores.
@@ -74,12 +76,13 @@ typedef enum { AWEQ_PER_TENSOR = 0, AWEQ_PER_ROW = 1, AWEQ_PER_GROUP = 2 } aweq_
 /* Device-side condition counters.  nonfinite: channels / vectors whose
  * statistics were Inf or NaN; zero_range: dead channels (factor forced to 1);
  * wait_timeout: a bounded wait inside a kernel gave up (results of that call
- * are invalid). */
+ * are invalid).  out_of_range: positions, lengths, sequence or page numbers that pointed outside
+ * their table or pool (aweq_kv_append, aweq_prefix_attention; nothing was read or written there). */
 typedef struct {
     unsigned long long nonfinite;
     unsigned long long zero_range;
     unsigned long long wait_timeout;
-    unsigned long long reserved;
+    unsigned long long out_of_range;
 } aweq_dev_status;
 
 typedef enum {
@@ -400,6 +403,108 @@ aweq_status aweq_forward_check_weights(const unsigned char *codes, const float *
                                        const void *X, const void *W, aweq_dtype dt, const void *bias,
                                        long long N, long long C_in, long long C_out, double *mean_err,
                                        double *sums, void *ws, size_t ws_bytes, void *stream);
+
+/* ==== Running a calibrated layer =============================================================
+ * aweq_linear_w8a8 multiplies the codes of steps 4 and 6; aweq_kv_append puts keys and values into
+ * a paged cache, rotating them (and the queries) on the way; aweq_prefix_attention attends over
+ * that cache for a batch whose sequences share a prefix. */
+
+/* Row sums of 8-bit codes, sums[r] = sum_j codes[r, j]: for a weight matrix they are formed once
+ * and passed to every aweq_linear_w8a8 call as w_sum.  codes: [rows x cols], row pitch ld bytes;
+ * base 16-byte aligned, ld and cols multiples of 16 (AWEQ_ERR_ALIGN / AWEQ_ERR_SHAPE), cols at most
+ * AWEQ_LINEAR_MAX_C_IN. */
+#define AWEQ_LINEAR_MAX_C_IN 65536
+aweq_status aweq_code_sums(const unsigned char *codes, long long rows, long long cols, long long ld, int *sums,
+                           void *stream);
+
+/* The calibrated W8A8 layer (Eq. 1-2 de-quantised on both sides, bias of Eq. 15):
+ *   out[n,o] = round16( Step^x_n Step^w_o sum_k (Xq[n,k] - Z^x_n)(Wq[o,k] - Z^w_o) + bias[o] ).
+ * The sum is formed in integers (tensor cores) and is exact as long as it fits 53 bits; the two
+ * Steps and the bias are applied in binary32 and the result is rounded once to the 16-bit type.
+ * Xq: step-6 codes [N x C_in], one per byte (any bit-width), row pitch ldx bytes; act_step / act_zp:
+ * one pair per token (act_gran AWEQ_PER_ROW) or a single pair (AWEQ_PER_TENSOR).
+ * Wq: 8-bit step-4 codes [C_out x C_in], row pitch ldw bytes; w_step / w_zp per output channel or a
+ * single pair (w_gran, as above); w_sum[C_out] from aweq_code_sums.  bias: float[C_out] or NULL.
+ * out: 16-bit [N x C_out], row pitch ldo elements.
+ * C_in: a multiple of 16, at most AWEQ_LINEAR_MAX_C_IN; C_out: any, at most 2^30; N: 0 (nothing is
+ * done) to 2^31 - 1.  Xq and Wq 16-byte aligned, ldx and ldw multiples of 16 and >= C_in; out 2-byte
+ * aligned, ldo >= C_out (16-byte aligned rows are written with wider stores).  No scratch. */
+aweq_status aweq_linear_w8a8(const unsigned char *Xq, long long ldx, const float *act_step, const int *act_zp,
+                             aweq_gran act_gran, const unsigned char *Wq, long long ldw, const float *w_step,
+                             const int *w_zp, const int *w_sum, aweq_gran w_gran, const float *bias, long long N,
+                             long long C_in, long long C_out, void *out, aweq_dtype dt, long long ldo,
+                             aweq_dev_status *st, void *stream);
+
+/* Rotary positions.  Pair i of a head (i < rotary_dim / 2) is turned by the angle p f_i at position
+ * p, f_i = theta^(-2i / rotary_dim), changed for contexts beyond the trained one:
+ *   AWEQ_ROPE_LINEAR  f_i / factor
+ *   AWEQ_ROPE_BASE    theta replaced by theta factor^(rotary_dim / (rotary_dim - 2))
+ *   AWEQ_ROPE_BANDS   g = clamp((r_i - low) / (high - low), 0, 1) with r_i = original_len f_i / 2 pi the
+ *                     turns within the trained length: f_i (g + (1 - g) / factor)
+ * attention multiplies every cos and sin (1 where no temperature is wanted). */
+typedef enum { AWEQ_ROPE_NONE = 0, AWEQ_ROPE_LINEAR = 1, AWEQ_ROPE_BASE = 2, AWEQ_ROPE_BANDS = 3 } aweq_rope_scaling;
+typedef struct {
+    int rotary_dim;                   /* even, 2 to 256 (AWEQ_ROPE_BASE: from 4) */
+    int scaling;                      /* aweq_rope_scaling */
+    double theta, factor;             /* > 0; factor is not read for AWEQ_ROPE_NONE */
+    double original_len, low, high;   /* AWEQ_ROPE_BANDS only; 0 <= low < high */
+    double attention;                 /* > 0 */
+} aweq_rope;
+/* table[p, 0 .. rotary_dim/2) = cos, table[p, rotary_dim/2 .. rotary_dim) = sin of position p < n_pos
+ * (binary64, rounded once to binary32).  spec is a HOST pointer.  Formed once per model. */
+aweq_status aweq_rope_table(const aweq_rope *spec, long long n_pos, float *table, void *stream);
+
+/* A paged cache: k and v are pools of n_pages pages of page_size tokens; element (page, token, head,
+ * d) of both lies at page * page_stride + token * token_stride + head * head_stride + d (in elements:
+ * heads inside tokens or tokens inside heads, as the strides say).  16-bit; bases 16-byte aligned,
+ * strides multiples of 8, head_dim a multiple of 8 up to 256.  This struct is a HOST argument. */
+typedef struct {
+    void *k, *v;
+    aweq_dtype dt;
+    int page_size, n_kv_heads, head_dim;
+    long long n_pages, page_stride, token_stride, head_stride;
+} aweq_kv_cache;
+
+/* Appends n_tokens keys and values.  Token t belongs to sequence s = seq[t] (seq NULL: s = t,
+ * n_tokens <= n_seq) and has position pos[t]; it is stored at index c = pos[t] - first of its sequence, that is in page
+ * page_table[s, c / page_size] (n_seq x pages_per_seq, row pitch ld_table) at row c % page_size.  first
+ * is the length of a prefix that is kept elsewhere; a token with c < 0 is not stored.
+ * k, v: [n_tokens x n_kv_heads * head_dim], row pitches ldk, ldv elements (slices of a joint q/k/v
+ * projection, say).  rope: the table of aweq_rope_table (n_pos rows) or NULL for no rotation; the first
+ * rotary_dim of every key head are turned by position pos[t], pairs (i, i + rotary_dim / 2) or, when
+ * interleaved != 0, (2i, 2i + 1); binary32, rounded once.  q: optional [n_tokens x n_heads * head_dim],
+ * turned the same way into q_out (which may be q).  Two tokens for the same place: either stays.
+ * A sequence, page or c outside the table or the pool, or (with rope) a position outside the
+ * table: the token is not stored, its q_out (position outside the table) becomes zero, and
+ * st->out_of_range counts the token.  k, v, q, q_out: 2-byte aligned, any pitch >= the row; 16-byte
+ * accesses are used where base, pitch and rotary_dim / 2 (interleaved: rotary_dim) allow them. */
+aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, long long n_seq, long long pages_per_seq,
+                           long long ld_table, const void *k, long long ldk, const void *v, long long ldv,
+                           const int *pos, const int *seq, long long first, long long n_tokens, const float *rope,
+                           long long n_pos, int rotary_dim, int interleaved, const void *q, long long ldq, int n_heads,
+                           void *q_out, long long ld_qout, aweq_dev_status *st, void *stream);
+
+/* Attention of n_q tokens of each of n_seq sequences over the prefix they share (prefix_len keys in
+ * prefix_pages, the same for all) and each sequence's own keys (own_len[b] keys in row b of page_table,
+ * the n_q tokens themselves included, appended before this call):
+ *   out[b n_q + i, h] = sum_j p_j v_j,  p = softmax_j(scale q . k_j)
+ * over all prefix keys and the own keys j < own_len[b] - (n_q - 1 - i); head h reads key head
+ * h / (n_heads / n_kv_heads).  A row without keys gives zeros.  The prefix is read once for all rows
+ * of the batch.  Scores, running maximum, sum and output are binary32; the probabilities are
+ * rounded to the 16-bit type for the product with v; one rounding at the end.
+ * q, out: 16-bit [n_seq * n_q x n_heads * head_dim], row pitches ldq, ldo elements, 16-byte aligned,
+ * pitches multiples of 8.  head_dim: a multiple of 8 up to 128.  own_len: device int[n_seq];
+ * max_own: HOST bound on it (a smaller one makes a smaller launch).  A length above max_own or
+ * pages_per_seq * page_size, or below zero, is clamped, a page outside the pool is replaced by page 0
+ * (the sequence's output is then meaningless); both are counted in st->out_of_range.
+ * ws: aweq_prefix_attention_workspace_bytes(...) bytes, 256-byte aligned. */
+size_t aweq_prefix_attention_workspace_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own,
+                                             long long n_seq, int n_q, int n_heads);
+aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages,
+                                  long long prefix_len, const int *page_table, long long pages_per_seq,
+                                  long long ld_table, const int *own_len, long long max_own, long long n_seq, int n_q,
+                                  int n_heads, float scale, void *out, long long ldo, void *ws, size_t ws_bytes,
+                                  aweq_dev_status *st, void *stream);
 
 #ifdef __cplusplus
 }

@@ -32,13 +32,14 @@ FLAG_NO_EQUALIZE, FLAG_NO_BIAS_CORRECT = 1, 2
 FLAG_PHASE_REDUCE, FLAG_PHASE_QUANT, FLAG_PHASE_ACT = 4, 8, 16
 FLAG_ABSMAX_CRITERION = 32
 FLAG_MERGED_STATS = 64
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
 
 _vp, _ll, _i, _sz = ctypes.c_void_p, ctypes.c_longlong, ctypes.c_int, ctypes.c_size_t
 
 
 class DevStatus(ctypes.Structure):
     _fields_ = [("nonfinite", ctypes.c_ulonglong), ("zero_range", ctypes.c_ulonglong),
-                ("wait_timeout", ctypes.c_ulonglong), ("reserved", ctypes.c_ulonglong)]
+                ("wait_timeout", ctypes.c_ulonglong), ("out_of_range", ctypes.c_ulonglong)]
 
 
 class LayerArgs(ctypes.Structure):
@@ -55,6 +56,17 @@ class LayerArgs(ctypes.Structure):
         ("ev_stats_begin", _vp), ("ev_stats_end", _vp), ("ev_act_begin", _vp), ("ev_act_end", _vp),
         ("stat_negmin_max", _vp), ("stat_sum_count", _vp),
     ]
+
+
+class RopeSpec(ctypes.Structure):
+    _fields_ = [("rotary_dim", _i), ("scaling", _i), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("attention", ctypes.c_double)]
+
+
+class KvCacheArgs(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("dt", _i), ("page_size", _i), ("n_kv_heads", _i), ("head_dim", _i),
+                ("n_pages", _ll), ("page_stride", _ll), ("token_stride", _ll), ("head_stride", _ll)]
 
 
 _lib.aweq_strerror.restype = ctypes.c_char_p
@@ -96,6 +108,21 @@ _lib.aweq_forward_check_weights_workspace_bytes.argtypes = [_ll, _ll, _ll]
 _lib.aweq_forward_check_weights.argtypes = [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _ll, _ll, _ll, _vp, _vp,
                                             _vp, _sz, _vp]
 _lib.aweq_forward_check_weights.restype = _i
+_lib.aweq_code_sums.argtypes = [_vp, _ll, _ll, _ll, _vp, _vp]
+_lib.aweq_code_sums.restype = _i
+_lib.aweq_linear_w8a8.argtypes = [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _vp, _vp, _i, _vp, _ll, _ll, _ll, _vp, _i, _ll, _vp,
+                                  _vp]
+_lib.aweq_linear_w8a8.restype = _i
+_lib.aweq_rope_table.argtypes = [ctypes.POINTER(RopeSpec), _ll, _vp, _vp]
+_lib.aweq_rope_table.restype = _i
+_lib.aweq_kv_append.argtypes = [ctypes.POINTER(KvCacheArgs), _vp, _ll, _ll, _ll, _vp, _ll, _vp, _ll, _vp, _vp, _ll, _ll, _vp,
+                                _ll, _i, _i, _vp, _ll, _i, _vp, _ll, _vp, _vp]
+_lib.aweq_kv_append.restype = _i
+_lib.aweq_prefix_attention_workspace_bytes.argtypes = [ctypes.POINTER(KvCacheArgs), _ll, _ll, _ll, _i, _i]
+_lib.aweq_prefix_attention_workspace_bytes.restype = _sz
+_lib.aweq_prefix_attention.argtypes = [_vp, _ll, ctypes.POINTER(KvCacheArgs), _vp, _ll, _vp, _ll, _ll, _vp, _ll, _ll, _i, _i,
+                                       ctypes.c_float, _vp, _ll, _vp, _sz, _vp, _vp]
+_lib.aweq_prefix_attention.restype = _i
 for _f in ("aweq_stats", "aweq_wrange", "aweq_factors", "aweq_equalize_quantize", "aweq_bias_correct",
            "aweq_quant_act", "aweq_layer_pass", "aweq_forward_check"):
     getattr(_lib, _f).restype = _i
@@ -170,6 +197,12 @@ def new_status(device="cuda") -> torch.Tensor:
 def read_status(st: torch.Tensor) -> dict:
     v = st.cpu().tolist()
     return {"nonfinite": v[0], "zero_range": v[1], "wait_timeout": v[2]}
+
+
+def read_out_of_range(st: torch.Tensor) -> int:
+    """The fourth counter of a status block: positions, lengths, sequence or page numbers that
+    pointed outside their table or pool (``aweq_kv_append``, ``aweq_prefix_attention``)."""
+    return int(st[3])
 
 
 def aweq_stats(X, xmin, xmax, xmean, xsum=None, count=None, accumulate=False, ws=None, st=None, N=None):
@@ -353,3 +386,202 @@ class LayerPass:
 
 def aweq_layer_pass(lp: LayerPass, ws: torch.Tensor, st: Optional[torch.Tensor] = None) -> None:
     lp(ws, st)
+
+
+# ---------------------------------------------------------------- running a calibrated layer
+def _want(t: Optional[torch.Tensor], dtype, n: int, what: str) -> None:
+    """The library cannot see a tensor's type or length: they are checked here."""
+    if t is not None and (t.dtype != dtype or t.numel() < n or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous %s tensor of at least %d elements" % (what, dtype, n))
+
+
+def _want_codes(t: torch.Tensor, what: str) -> None:
+    if t.dtype != torch.uint8:
+        raise TypeError("%s must be uint8 codes, got %s" % (what, t.dtype))
+
+
+def aweq_code_sums(codes, sums=None):
+    """Row sums of an 8-bit code matrix (int32)."""
+    _want_codes(codes, "codes")
+    if sums is None:
+        sums = torch.empty(codes.shape[0], dtype=torch.int32, device=codes.device)
+    _want(sums, torch.int32, codes.shape[0], "sums")
+    _check(_lib.aweq_code_sums(_ptr(codes), codes.shape[0], codes.shape[1], _ld(codes), _ptr(sums), _stream()))
+    return sums
+
+
+def aweq_linear_w8a8(Xq, act_step, act_zp, act_gran, Wq, w_step, w_zp, w_sum, w_gran, bias, out, st=None):
+    """The calibrated W8A8 layer on step-6 codes (argument marshalling only; see ``include/aweq.h``).
+    ``LinearW8A8`` marshals the weight's arguments once for repeated calls."""
+    N, C_in = Xq.shape
+    C_out = Wq.shape[0]
+    _want_codes(Xq, "Xq")
+    _want_codes(Wq, "Wq")
+    if Wq.shape[1] != C_in or out.shape[0] != N or out.shape[1] != C_out:
+        raise ValueError("shapes do not match: Xq %s, Wq %s, out %s" % (tuple(Xq.shape), tuple(Wq.shape), tuple(out.shape)))
+    pairs, w_pairs = (N if act_gran == PER_ROW else 1), (C_out if w_gran == PER_ROW else 1)
+    _want(act_step, torch.float32, pairs, "act_step")
+    _want(act_zp, torch.int32, pairs, "act_zp")
+    _want(w_step, torch.float32, w_pairs, "w_step")
+    _want(w_zp, torch.int32, w_pairs, "w_zp")
+    _want(w_sum, torch.int32, C_out, "w_sum")
+    _want(bias, torch.float32, C_out, "bias")
+    _check(_lib.aweq_linear_w8a8(_ptr(Xq), _ld(Xq), _ptr(act_step), _ptr(act_zp), act_gran, _ptr(Wq), _ld(Wq), _ptr(w_step),
+                                 _ptr(w_zp), _ptr(w_sum), w_gran, _ptr(bias), N, C_in, C_out, _ptr(out), dtype_tag(out),
+                                 _ld(out), _ptr(st), _stream()))
+    return out
+
+
+class LinearW8A8:
+    """A calibrated 8-bit linear layer ready to run: holds the step-4 codes (one pair per output channel,
+    or a single pair), the corrected binary32 bias and the codes' row sums (formed here, once), and
+    marshals them once.  Calling it with step-6 codes and their pairs (one per token, or a single
+    pair) writes the 16-bit output on the current stream."""
+
+    def __init__(self, codes, step, zp, bias=None):
+        _want_codes(codes, "codes")
+        self.C_out, self.C_in = codes.shape
+        gran = PER_TENSOR if step.numel() == 1 and self.C_out != 1 else PER_ROW
+        pairs = self.C_out if gran == PER_ROW else 1
+        _want(step, torch.float32, pairs, "step")
+        _want(zp, torch.int32, pairs, "zp")
+        _want(bias, torch.float32, self.C_out, "bias")
+        self.codes, self.step, self.zp, self.bias = codes, step, zp, bias
+        self.w_sum = aweq_code_sums(codes)
+        self._weight = (_ptr(codes), _ld(codes), _ptr(step), _ptr(zp), _ptr(self.w_sum), gran, _ptr(bias))
+
+    def __call__(self, Xq, act_step, act_zp, out=None, dtype=torch.float16, st=None):
+        N = Xq.shape[0]
+        if out is None:
+            out = torch.empty((N, self.C_out), dtype=dtype, device=Xq.device)
+        pairs = act_step.numel()
+        if (Xq.dtype != torch.uint8 or Xq.shape[1] != self.C_in or out.shape[0] != N or out.shape[1] != self.C_out
+                or act_step.dtype != torch.float32 or act_zp.dtype != torch.int32 or act_zp.numel() != pairs
+                or (pairs != N and pairs != 1) or not (act_step.is_contiguous() and act_zp.is_contiguous())):
+            raise ValueError("Xq [N x %d] uint8, act_step / act_zp float32 / int32 of N or one element, out [N x %d]"
+                             % (self.C_in, self.C_out))
+        _check(_lib.aweq_linear_w8a8(_ptr(Xq), _ld(Xq), _ptr(act_step), _ptr(act_zp), PER_ROW if pairs == N else PER_TENSOR,
+                                     *self._weight, N, self.C_in, self.C_out, _ptr(out), dtype_tag(out), _ld(out), _ptr(st),
+                                     _stream()))
+        return out
+
+
+def aweq_rope_table(rotary_dim, n_pos, theta=10000.0, scaling="none", factor=1.0, original_len=0.0, low=1.0, high=4.0,
+                    attention=1.0, table=None, device="cuda"):
+    """cos and sin of every position below ``n_pos``: float32 [n_pos x rotary_dim] for
+    ``aweq_kv_append``.  ``scaling``: "none", "linear", "base" or "bands" (see ``include/aweq.h``)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError("scaling must be one of %s" % sorted(ROPE_SCALINGS))
+    if table is None:
+        table = torch.empty((n_pos, rotary_dim), dtype=torch.float32, device=device)
+    _want(table, torch.float32, n_pos * rotary_dim, "table")
+    spec = RopeSpec(rotary_dim, ROPE_SCALINGS[scaling], theta, factor, original_len, low, high, attention)
+    _check(_lib.aweq_rope_table(ctypes.byref(spec), n_pos, _ptr(table), _stream()))
+    return table
+
+
+class KVCache:
+    """A paged cache: two pools [n_pages, page_size, n_kv_heads, head_dim] with the same strides and a
+    contiguous innermost dimension (a permuted view serves pools that keep tokens inside heads)."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(3) != 1:
+            raise ValueError("k and v must be alike: [n_pages, page_size, n_kv_heads, head_dim], innermost contiguous")
+        self.k, self.v = k, v
+        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = k.shape
+        self.dtype = k.dtype
+        # a dimension of one element has no stride of its own
+        stride = [max(k.stride(i), self.head_dim) if k.shape[i] == 1 else k.stride(i) for i in range(3)]
+        self.args = KvCacheArgs(_ptr(k), _ptr(v), dtype_tag(k), self.page_size, self.n_kv_heads, self.head_dim, self.n_pages,
+                                *stride)
+        self.ref = ctypes.byref(self.args)
+
+
+def _heads(t: torch.Tensor, n_heads: int, head_dim: int, dtype, what: str) -> int:
+    """Row pitch of [tokens, heads, head_dim] (or [tokens, heads * head_dim]) with contiguous rows."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        ok = shape[1] == n_heads and shape[2] == head_dim and stride[2] == 1 and (n_heads == 1 or stride[1] == head_dim)
+    else:
+        ok = len(shape) == 2 and shape[1] == n_heads * head_dim and stride[1] == 1
+    if not ok or t.dtype != dtype:
+        raise ValueError("%s must be %s [tokens, %d, %d] with contiguous rows" % (what, dtype, n_heads, head_dim))
+    return stride[0] if shape[0] > 1 else max(stride[0], n_heads * head_dim)
+
+
+def _int32_table(t: torch.Tensor, what: str) -> int:
+    if t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be int32 [sequences, pages] with contiguous rows" % what)
+    return max(t.stride(0), t.shape[1])
+
+
+def aweq_kv_append(cache, page_table, k, v, pos, seq=None, first=0, table=None, interleaved=False, q=None, q_out=None,
+                   st=None):
+    """Store keys and values of new tokens in their pages, keys (and ``q`` into ``q_out``) turned by
+    their positions on the way (argument marshalling only; see ``include/aweq.h``)."""
+    d, n = cache.head_dim, k.shape[0]
+    ldk, ldv = _heads(k, cache.n_kv_heads, d, cache.dtype, "k"), _heads(v, cache.n_kv_heads, d, cache.dtype, "v")
+    ld_table = _int32_table(page_table, "page_table")
+    if v.shape[0] != n or pos.dtype != torch.int32 or pos.numel() != n or not pos.is_contiguous():
+        raise ValueError("k, v and an int32 pos have one row per token")
+    if seq is None:
+        if page_table.shape[0] < n:
+            raise ValueError("without seq, page_table has a row per token")
+    elif seq.dtype != torch.int32 or seq.numel() != n or not seq.is_contiguous():
+        raise ValueError("seq must be int32, one per token")
+    n_pos = rd = 0
+    if table is not None:
+        n_pos, rd = table.shape
+        _want(table, torch.float32, n_pos * rd, "table")
+    ldq = ldo = heads = 0
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else q.shape[1] // d
+        q_out = q if q_out is None else q_out
+        ldq, ldo = _heads(q, heads, d, cache.dtype, "q"), _heads(q_out, heads, d, cache.dtype, "q_out")
+        if q.shape[0] != n or q_out.shape[0] != n:
+            raise ValueError("q and q_out have one row per token")
+    _check(_lib.aweq_kv_append(cache.ref, _ptr(page_table), page_table.shape[0], page_table.shape[1], ld_table, _ptr(k), ldk,
+                               _ptr(v), ldv, _ptr(pos), _ptr(seq), first, n, _ptr(table), n_pos, rd, int(interleaved),
+                               _ptr(q), ldq, heads, _ptr(q_out), ldo, _ptr(st), _stream()))
+    return q_out
+
+
+def aweq_prefix_attention_workspace_bytes(cache, prefix_len, max_own, n_seq, n_q, n_heads) -> int:
+    return int(_lib.aweq_prefix_attention_workspace_bytes(cache.ref, prefix_len, max_own, n_seq, n_q, n_heads))
+
+
+def aweq_prefix_attention(q, cache, prefix_pages, prefix_len, page_table, own_len, max_own, n_q, scale, out, ws, st=None):
+    """Attention over a shared prefix and each sequence's own keys (argument marshalling only; see
+    ``include/aweq.h``).  ``q``, ``out``: [n_seq * n_q, n_heads, head_dim]."""
+    n_seq, d = own_len.numel(), cache.head_dim
+    n_heads = q.shape[1] if q.dim() == 3 else q.shape[1] // d
+    ldq, ldo = _heads(q, n_heads, d, cache.dtype, "q"), _heads(out, n_heads, d, cache.dtype, "out")
+    ld_table = _int32_table(page_table, "page_table")
+    if q.shape[0] != n_seq * n_q or out.shape[0] != n_seq * n_q or page_table.shape[0] != n_seq:
+        raise ValueError("q and out have n_seq * n_q rows, page_table n_seq")
+    if own_len.dtype != torch.int32 or not own_len.is_contiguous():
+        raise ValueError("own_len must be int32")
+    if prefix_len:
+        _want(prefix_pages, torch.int32, -(-prefix_len // cache.page_size), "prefix_pages")
+    _check(_lib.aweq_prefix_attention(_ptr(q), ldq, cache.ref, _ptr(prefix_pages), prefix_len, _ptr(page_table),
+                                      page_table.shape[1], ld_table, _ptr(own_len), max_own, n_seq, n_q, n_heads, scale,
+                                      _ptr(out), ldo, _ptr(ws), ws.numel(), _ptr(st), _stream()))
+    return out
+
+
+class PrefixAttention:
+    """``aweq_prefix_attention`` for one batch shape: holds the prefix's page list and the scratch.  One
+    object serves one stream at a time (its calls share the scratch)."""
+
+    def __init__(self, cache, prefix_pages, prefix_len, n_heads, n_seq, n_q=1, max_own=None, scale=None):
+        self.cache, self.prefix_pages, self.prefix_len = cache, prefix_pages, int(prefix_len)
+        self.n_heads, self.n_seq, self.n_q = n_heads, n_seq, n_q
+        self.max_own = 0x7fffffff if max_own is None else int(max_own)
+        self.scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+        nbytes = aweq_prefix_attention_workspace_bytes(cache, self.prefix_len, self.max_own, n_seq, n_q, n_heads)
+        self.ws = workspace(nbytes, cache.k.device)
+
+    def __call__(self, q, page_table, own_len, out=None, st=None):
+        out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
+        return aweq_prefix_attention(q, self.cache, self.prefix_pages, self.prefix_len, page_table, own_len, self.max_own,
+                                     self.n_q, self.scale, out, self.ws, st)

@@ -8,6 +8,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "linear8.cuh"
 
 namespace aweq {
 
@@ -493,6 +494,166 @@ aweq_status aweq_forward_check_weights(const unsigned char *codes, const float *
               4.0 * N * C_in * C_out);
     return run_forward_check_weights(codes, step, zp, bits, gran, group, rinv, bias_q, X, W, dt, bias, N, C_in, C_out,
                                      mean_err, sums, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+// ------------------------------------------------------------------ running a calibrated layer
+static aweq_status check_codes(const void *Q, long long cols, long long ld)
+{
+    if (cols <= 0 || cols % 16 || cols > AWEQ_LINEAR_MAX_C_IN) return AWEQ_ERR_SHAPE;
+    if (!aligned(Q, 16) || ld < cols || ld % 16 || ld > (1ll << 40)) return AWEQ_ERR_ALIGN;
+    return AWEQ_OK;
+}
+
+aweq_status aweq_code_sums(const unsigned char *codes, long long rows, long long cols, long long ld, int *sums, void *stream)
+{
+    if (!codes || !sums) return AWEQ_ERR_NULL;
+    if (rows <= 0 || rows > (1ll << 30)) return AWEQ_ERR_SHAPE;
+    aweq_status rc = check_codes(codes, cols, ld);
+    if (rc != AWEQ_OK) return rc;
+    AWEQ_LOGF("aweq_code_sums rows=%lld cols=%lld bytes=%lld\n", rows, cols, rows * cols);
+    return run_code_sums(codes, rows, cols, ld, sums, (cudaStream_t)stream);
+}
+
+aweq_status aweq_linear_w8a8(const unsigned char *Xq, long long ldx, const float *act_step, const int *act_zp,
+                             aweq_gran act_gran, const unsigned char *Wq, long long ldw, const float *w_step,
+                             const int *w_zp, const int *w_sum, aweq_gran w_gran, const float *bias, long long N,
+                             long long C_in, long long C_out, void *out, aweq_dtype dt, long long ldo,
+                             aweq_dev_status *st, void *stream)
+{
+    if (dt != AWEQ_F16 && dt != AWEQ_BF16) return AWEQ_ERR_DTYPE;
+    if ((act_gran != AWEQ_PER_ROW && act_gran != AWEQ_PER_TENSOR) || (w_gran != AWEQ_PER_ROW && w_gran != AWEQ_PER_TENSOR))
+        return AWEQ_ERR_UNSUPPORTED;
+    if (N < 0 || N > 0x7fffffffll || C_out <= 0 || C_out > (1ll << 30)) return AWEQ_ERR_SHAPE;
+    if (!Wq || !w_step || !w_zp || !w_sum) return AWEQ_ERR_NULL;
+    if (N > 0 && (!Xq || !act_step || !act_zp || !out)) return AWEQ_ERR_NULL;
+    aweq_status rc = check_codes(Wq, C_in, ldw);
+    if (rc == AWEQ_OK) rc = check_codes(Xq, C_in, ldx);
+    if (rc != AWEQ_OK) return rc;
+    if (!aligned(out, 2) || ldo < C_out || !aligned(act_step, 4) || !aligned(act_zp, 4) || !aligned(w_step, 4) ||
+        !aligned(w_zp, 4) || !aligned(w_sum, 4) || (bias && !aligned(bias, 4)))
+        return AWEQ_ERR_ALIGN;
+    if (N == 0) return AWEQ_OK;
+    AWEQ_LOGF("aweq_linear_w8a8 N=%lld C_in=%lld C_out=%lld ops=%.3e\n", N, C_in, C_out, 2.0 * N * C_in * C_out);
+    Linear8Args a = {};
+    a.X = Xq; a.W = Wq; a.ldx = ldx; a.ldw = ldw; a.ldo = ldo; a.N = N;
+    a.x_step = act_step; a.w_step = w_step; a.bias = bias; a.x_zp = act_zp; a.w_zp = w_zp; a.w_sum = w_sum;
+    a.x_inc = act_gran == AWEQ_PER_ROW; a.w_inc = w_gran == AWEQ_PER_ROW;
+    a.K = (int)C_in; a.O = (int)C_out; a.out = reinterpret_cast<uint16_t *>(out); a.st = st;
+    return run_linear8_stream(a, dt, (cudaStream_t)stream);
+}
+
+aweq_status aweq_rope_table(const aweq_rope *r, long long n_pos, float *table, void *stream)
+{
+    if (!r || !table) return AWEQ_ERR_NULL;
+    if (r->rotary_dim < 2 || r->rotary_dim > 256 || r->rotary_dim % 2 || n_pos <= 0 || n_pos > (1ll << 31)) return AWEQ_ERR_SHAPE;
+    if (r->scaling < AWEQ_ROPE_NONE || r->scaling > AWEQ_ROPE_BANDS) return AWEQ_ERR_UNSUPPORTED;
+    if (!(r->theta > 0) || !(r->attention > 0) || (r->scaling != AWEQ_ROPE_NONE && !(r->factor > 0))) return AWEQ_ERR_UNSUPPORTED;
+    if (r->scaling == AWEQ_ROPE_BASE && r->rotary_dim < 4) return AWEQ_ERR_SHAPE;
+    if (r->scaling == AWEQ_ROPE_BANDS && !(r->original_len > 0 && r->low >= 0 && r->high > r->low)) return AWEQ_ERR_UNSUPPORTED;
+    if (!aligned(table, 4)) return AWEQ_ERR_ALIGN;
+    return run_rope_table(r, n_pos, table, (cudaStream_t)stream);
+}
+
+static aweq_status check_cache(const aweq_kv_cache *c, int most_dim)
+{
+    if (!c || !c->k || !c->v) return AWEQ_ERR_NULL;
+    if (c->dt != AWEQ_F16 && c->dt != AWEQ_BF16) return AWEQ_ERR_DTYPE;
+    if (c->page_size <= 0 || c->page_size > (1 << 20) || c->n_kv_heads <= 0 || c->n_kv_heads > 4096 || c->n_pages <= 0 ||
+        c->n_pages > 0x7fffffffll || c->head_dim <= 0 || c->head_dim % 8 || c->head_dim > most_dim)
+        return AWEQ_ERR_SHAPE;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || c->page_stride % 8 || c->token_stride % 8 || c->head_stride % 8 ||
+        c->page_stride < 0 || c->token_stride < c->head_dim || c->head_stride < c->head_dim)
+        return AWEQ_ERR_ALIGN;
+    return AWEQ_OK;
+}
+
+aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, long long n_seq, long long pages_per_seq,
+                           long long ld_table, const void *k, long long ldk, const void *v, long long ldv,
+                           const int *pos, const int *seq, long long first, long long n_tokens, const float *rope,
+                           long long n_pos, int rotary_dim, int interleaved, const void *q, long long ldq, int n_heads,
+                           void *q_out, long long ld_qout, aweq_dev_status *st, void *stream)
+{
+    aweq_status rc = check_cache(cache, 256);
+    if (rc != AWEQ_OK) return rc;
+    const long long row = (long long)cache->n_kv_heads * cache->head_dim;
+    if (n_tokens < 0 || n_tokens > 0x7fffffffll || n_seq <= 0 || n_seq > 0x7fffffffll || pages_per_seq <= 0 ||
+        pages_per_seq > 0x7fffffffll || first < 0)
+        return AWEQ_ERR_SHAPE;
+    if (rope && (rotary_dim < 2 || rotary_dim % 2 || rotary_dim > cache->head_dim || n_pos <= 0)) return AWEQ_ERR_SHAPE;
+    if ((q == nullptr) != (q_out == nullptr)) return AWEQ_ERR_NULL;
+    if (q && (n_heads <= 0 || n_heads > 65536)) return AWEQ_ERR_SHAPE;
+    if (!seq && n_tokens > n_seq) return AWEQ_ERR_SHAPE;
+    if (n_tokens == 0) return AWEQ_OK;
+    if (!page_table || !k || !v || !pos) return AWEQ_ERR_NULL;
+    if (ld_table < pages_per_seq || ldk < row || ldv < row || !aligned(k, 2) || !aligned(v, 2) || !aligned(pos, 4) ||
+        !aligned(seq, 4) || !aligned(page_table, 4) || !aligned(rope, 4))
+        return AWEQ_ERR_ALIGN;
+    if (q) {
+        const long long qrow = (long long)n_heads * cache->head_dim;
+        if (ldq < qrow || ld_qout < qrow || !aligned(q, 2) || !aligned(q_out, 2)) return AWEQ_ERR_ALIGN;
+    }
+    AWEQ_LOGF("aweq_kv_append tokens=%lld heads=%d kv_heads=%d head_dim=%d rotary_dim=%d bytes=%lld\n", n_tokens,
+              q ? n_heads : 0, cache->n_kv_heads, cache->head_dim, rope ? rotary_dim : 0,
+              n_tokens * ((q ? n_heads : 0) + 2 * cache->n_kv_heads) * cache->head_dim * 4);
+    KvAppendArgs a = {};
+    a.ck = reinterpret_cast<uint16_t *>(cache->k); a.cv = reinterpret_cast<uint16_t *>(cache->v);
+    a.n_pages = cache->n_pages; a.page_stride = cache->page_stride; a.token_stride = cache->token_stride;
+    a.head_stride = cache->head_stride; a.page_size = cache->page_size; a.n_kv = cache->n_kv_heads;
+    a.head_dim = cache->head_dim; a.page_table = page_table; a.n_seq = n_seq; a.pages_per_seq = pages_per_seq;
+    a.ld_table = ld_table; a.k = reinterpret_cast<const uint16_t *>(k); a.v = reinterpret_cast<const uint16_t *>(v);
+    a.q = reinterpret_cast<const uint16_t *>(q); a.q_out = reinterpret_cast<uint16_t *>(q_out);
+    a.ldk = ldk; a.ldv = ldv; a.ldq = ldq; a.ld_qout = ld_qout; a.n_heads = q ? n_heads : 0; a.pos = pos; a.seq = seq;
+    a.first = first; a.n_tokens = n_tokens; a.rope = rope; a.n_pos = n_pos; a.rd = rope ? rotary_dim : 0;
+    a.interleaved = interleaved; a.st = st;
+    return run_kv_append(a, cache->dt, (cudaStream_t)stream);
+}
+
+static aweq_status check_attention(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq, int n_q,
+                                   int n_heads)
+{
+    aweq_status rc = check_cache(cache, 128);
+    if (rc != AWEQ_OK) return rc;
+    if (prefix_len < 0 || prefix_len > 0x7fffffffll || max_own < 0 || max_own > 0x7fffffffll || n_seq < 0 || n_q <= 0 ||
+        n_heads <= 0 || n_heads % cache->n_kv_heads || n_heads > 65536 || n_q > 65536)
+        return AWEQ_ERR_SHAPE;
+    if (n_seq > 0x7fffffffll || (double)n_seq * n_q * n_heads > 2147483647.0) return AWEQ_ERR_SHAPE;
+    return AWEQ_OK;
+}
+
+size_t aweq_prefix_attention_workspace_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq,
+                                             int n_q, int n_heads)
+{
+    if (check_attention(cache, prefix_len, max_own, n_seq, n_q, n_heads) != AWEQ_OK || n_seq == 0) return 0;
+    return prefix_attention_ws_bytes(cache, prefix_len, max_own, n_seq, n_q, n_heads);
+}
+
+aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages,
+                                  long long prefix_len, const int *page_table, long long pages_per_seq, long long ld_table,
+                                  const int *own_len, long long max_own, long long n_seq, int n_q, int n_heads, float scale,
+                                  void *out, long long ldo, void *ws, size_t ws_bytes, aweq_dev_status *st, void *stream)
+{
+    aweq_status rc = check_attention(cache, prefix_len, max_own, n_seq, n_q, n_heads);
+    if (rc != AWEQ_OK) return rc;
+    if (pages_per_seq < 0 || pages_per_seq > 0x7fffffffll) return AWEQ_ERR_SHAPE;
+    if (n_seq == 0) return AWEQ_OK;
+    if (!q || !out || !own_len || (prefix_len && !prefix_pages) || (max_own && pages_per_seq && !page_table)) return AWEQ_ERR_NULL;
+    const long long row = (long long)n_heads * cache->head_dim;
+    if (!aligned(q, 16) || !aligned(out, 16) || ldq < row || ldo < row || ldq % 8 || ldo % 8 || ld_table < pages_per_seq ||
+        !aligned(prefix_pages, 4) || !aligned(page_table, 4) || !aligned(own_len, 4))
+        return AWEQ_ERR_ALIGN;
+    rc = check_ws(ws, ws_bytes, prefix_attention_ws_bytes(cache, prefix_len, max_own, n_seq, n_q, n_heads));
+    if (rc != AWEQ_OK) return rc;
+    AWEQ_LOGF("aweq_prefix_attention seqs=%lld n_q=%d heads=%d kv_heads=%d head_dim=%d prefix=%lld max_own=%lld\n", n_seq, n_q,
+              n_heads, cache->n_kv_heads, cache->head_dim, prefix_len, max_own);
+    AttentionArgs a = {};
+    a.q = reinterpret_cast<const uint16_t *>(q); a.ck = reinterpret_cast<const uint16_t *>(cache->k);
+    a.cv = reinterpret_cast<const uint16_t *>(cache->v); a.out = reinterpret_cast<uint16_t *>(out);
+    a.ldq = ldq; a.ldo = ldo; a.n_pages = cache->n_pages; a.page_stride = cache->page_stride;
+    a.token_stride = cache->token_stride; a.head_stride = cache->head_stride; a.page_size = cache->page_size;
+    a.n_kv = cache->n_kv_heads; a.head_dim = cache->head_dim; a.n_heads = n_heads; a.n_q = n_q;
+    a.prefix_pages = prefix_pages; a.page_table = page_table; a.own_len = own_len; a.prefix_len = prefix_len;
+    a.pages_per_seq = pages_per_seq; a.ld_table = ld_table; a.max_own = max_own; a.n_seq = n_seq; a.scale = scale; a.st = st;
+    return run_prefix_attention(a, cache->dt, ws, (cudaStream_t)stream);
 }
 
 }  // extern "C"

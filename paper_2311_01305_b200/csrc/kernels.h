@@ -82,4 +82,43 @@ aweq_status fc_gemm_f16(const void *A, const void *B, void *C, int M, int N, int
 aweq_status fc_gemm_bf16(const void *A, const void *B, void *C, int M, int N, int K, long long ld, void *scratch,
                          size_t scratch_bytes, cudaStream_t stream);
 
+// ------------------------------------------------------------------ running a calibrated layer
+aweq_status run_code_sums(const unsigned char *codes, long long rows, long long cols, long long ld, int *sums,
+                          cudaStream_t stream);
+
+aweq_status run_rope_table(const aweq_rope *spec, long long n_pos, float *table, cudaStream_t stream);
+
+struct KvAppendArgs {
+    uint16_t *ck, *cv;
+    long long n_pages, page_stride, token_stride, head_stride;
+    int page_size, n_kv, head_dim;
+    const int *page_table;
+    long long n_seq, pages_per_seq, ld_table;
+    const uint16_t *k, *v, *q;
+    uint16_t *q_out;
+    long long ldk, ldv, ldq, ld_qout;
+    int n_heads;                      // of q; 0 without q
+    const int *pos, *seq;
+    long long first, n_tokens;
+    const float *rope;
+    long long n_pos;
+    int rd, interleaved;
+    aweq_dev_status *st;
+};
+aweq_status run_kv_append(const KvAppendArgs &a, aweq_dtype dt, cudaStream_t stream);
+
+struct AttentionArgs {
+    const uint16_t *q, *ck, *cv;
+    uint16_t *out;
+    long long ldq, ldo, n_pages, page_stride, token_stride, head_stride;
+    int page_size, n_kv, head_dim, n_heads, n_q;
+    const int *prefix_pages, *page_table, *own_len;
+    long long prefix_len, pages_per_seq, ld_table, max_own, n_seq;
+    float scale;
+    aweq_dev_status *st;
+};
+size_t prefix_attention_ws_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq, int n_q,
+                                 int n_heads);
+aweq_status run_prefix_attention(const AttentionArgs &a, aweq_dtype dt, void *ws, cudaStream_t stream);
+
 }  // namespace aweq
