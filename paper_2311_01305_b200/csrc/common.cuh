@@ -106,6 +106,11 @@ struct F16 {
     }
     static __device__ __forceinline__ float one(uint16_t b) { return __half2float(__ushort_as_half(b)); }
     static __device__ __forceinline__ uint16_t encode(float f) { return __half_as_ushort(__float2half_rn(f)); }
+    static __device__ __forceinline__ uint32_t encode2(float lo, float hi)
+    {
+        const T2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
 };
 struct BF16 {
     using T2 = __nv_bfloat162;
@@ -119,6 +124,11 @@ struct BF16 {
     }
     static __device__ __forceinline__ float one(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
     static __device__ __forceinline__ uint16_t encode(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
+    static __device__ __forceinline__ uint32_t encode2(float lo, float hi)
+    {
+        const T2 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
 };
 
 // widen the 8 elements of a 16-byte vector
