@@ -35,6 +35,7 @@ struct Linear8Args {
 };
 
 aweq_status run_linear8_stream(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream);
+aweq_status run_linear8_split(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream);
 aweq_status run_linear8_big(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream);
 
 }  // namespace aweq

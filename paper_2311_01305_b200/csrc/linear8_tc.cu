@@ -32,16 +32,16 @@ constexpr int kL8Block = 128;                  // bytes of K per stage: one swiz
 // sum does not see; the lanes start at different pieces so that they spread over the banks.
 __device__ __forceinline__ uint32_t staged_row_sum(const unsigned char *row, int lane)
 {
-    uint32_t s = 0;
+    uint32_t s[4] = {};
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         const uint4 v = *reinterpret_cast<const uint4 *>(row + ((c + lane) & 7) * 16);
-        s = __dp4a(v.x, 0x01010101u, s);
-        s = __dp4a(v.y, 0x01010101u, s);
-        s = __dp4a(v.z, 0x01010101u, s);
-        s = __dp4a(v.w, 0x01010101u, s);
+        s[0] = __dp4a(v.x, 0x01010101u, s[0]);
+        s[1] = __dp4a(v.y, 0x01010101u, s[1]);
+        s[2] = __dp4a(v.z, 0x01010101u, s[2]);
+        s[3] = __dp4a(v.w, 0x01010101u, s[3]);
     }
-    return s;
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 struct alignas(16) Linear8Col {
@@ -315,6 +315,286 @@ static aweq_status big_launch(const Linear8Args &a, cudaStream_t stream)
 aweq_status run_linear8_big(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream)
 {
     return dt == AWEQ_F16 ? big_launch<F16>(a, stream) : big_launch<BF16>(a, stream);
+}
+
+// ------------------------------------------------------------------ a moderate number of tokens
+// The layer is bound by the weights here: what counts is that every SM has a deep queue of copies under
+// way and that they all end together.  A CTA per SM takes up to 256 tokens x bn channels, with bn chosen so that
+// the tiles fill one wave; where few channels leave SMs idle, K is cut over the CTAs of a cluster, whose integer
+// sums are added through distributed shared memory (exact in any order), each CTA finishing its share of the
+// rows.  A stage holds the tokens there are (rounded up to 8), not 128, so that few tokens leave the ring to the
+// weights; the product reads 128 rows all the same, those past the box belong to the weights behind them and
+// give sums that nobody reads.  Warps: 0 copies, 1 issues the products, 2-7 add up the tokens' codes.  The sums go
+// through shared memory (the stages) once so that the output is written along the channels.
+constexpr int kSplitRing = 200 * 1024, kSplitMaxStages = 16;
+struct SplitPlan {
+    int bn, slices;              // channels of a tile, slices of K
+    int box, mb;                 // token rows of a stage, 128-row blocks they make
+    int parts;                   // independent accumulators that the products of a block take in turn
+    int stages, kb_stage;        // ring, 128-byte blocks of K per stage
+    int rx_groups, rx_sets;      // 32-row groups of a stage; warps that share a group's stages
+};
+struct alignas(16) Linear8Row {
+    float step, reachK;
+    int zp;
+    uint32_t rx;
+};
+struct SplitShared {
+    uint64_t full[kSplitMaxStages], empty[kSplitMaxStages], acc_full;
+    uint32_t tmem, rx[256];
+    Linear8Row row[256];
+    Linear8Col col[256];
+};
+constexpr size_t kSplitSmem = 1024 + kSplitRing + sizeof(SplitShared);
+static_assert(kSplitSmem <= 227 * 1024, "shared memory of a CTA");
+
+template <class D>
+__global__ void __launch_bounds__(256, 1)
+linear8_split_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW,
+                     const SplitPlan plan, int vec_out)
+{
+    extern __shared__ unsigned char raw[];
+    unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    SplitShared &sh = *reinterpret_cast<SplitShared *>(stages + kSplitRing);
+    uint32_t *part = reinterpret_cast<uint32_t *>(stages);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int bn = plan.bn, pitch = bn + 4, x_bytes = plan.box * kL8Block, kb_bytes = x_bytes + bn * kL8Block;
+    const int slices = plan.slices, slice = blockIdx.x;
+    const int nkb = (p.K + kL8Block - 1) / kL8Block;
+    const int kb0 = (int)((long long)nkb * slice / slices), kb1 = (int)((long long)nkb * (slice + 1) / slices);
+    const long long row0 = (long long)blockIdx.z * 128 * plan.mb;
+    const int rows = (int)min(128ll * plan.mb, p.N - row0);
+    const int o0 = blockIdx.y * bn;
+    uint32_t cols = 32;
+    while ((int)cols < bn * plan.mb * plan.parts) cols *= 2;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < plan.stages; ++s) {
+            mbar_init(&sh.full[s], 1);
+            mbar_init(&sh.empty[s], 1 + min(plan.rx_groups, 6));
+        }
+        mbar_init(&sh.acc_full, 1);
+        mbar_init_fence();
+        tma_prefetch_map(&mapX);
+        tma_prefetch_map(&mapW);
+    }
+    sh.rx[threadIdx.x] = 0;
+    if (warp == 1) tc_alloc<1>(&sh.tmem, cols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    bool ok = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            for (int kb = kb0; kb < kb1; kb += plan.kb_stage) {
+                if (!mbar_wait(&sh.empty[s], ph ^ 1)) { ok = false; break; }
+                const int n = min(plan.kb_stage, kb1 - kb);
+                uint32_t dst = smem_u32(stages + s * plan.kb_stage * kb_bytes);
+                const uint32_t bar = smem_u32(&sh.full[s]);
+                mbar_arrive_expect_tx(&sh.full[s], (uint32_t)(n * kb_bytes));
+                for (int i = 0; i < n; ++i, dst += kb_bytes) {
+                    tma_load2<1>(dst + x_bytes, &mapW, (kb + i) * kL8Block, o0, bar);
+                    tma_load2<1>(dst, &mapX, (kb + i) * kL8Block, (int)row0, bar);
+                }
+                if (++s == plan.stages) { s = 0; ph ^= 1; }
+            }
+            if (!ok)                           // gave up: let what is under way land (bounded) before the memory goes
+                for (int i = 0; i < plan.stages; ++i) mbar_wait(&sh.full[i], ph ^ (i >= s ? 1u : 0u));
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            const uint32_t idesc = tc_idesc_u8(128, bn);
+            for (int kb = kb0; kb < kb1; kb += plan.kb_stage) {
+                if (!mbar_wait(&sh.full[s], ph)) { ok = false; break; }
+                tc_fence_after();
+                const int n = min(plan.kb_stage, kb1 - kb);
+                uint32_t a = smem_u32(stages + s * plan.kb_stage * kb_bytes);
+                for (int i = 0; i < n; ++i, a += kb_bytes) {
+                    const uint64_t da = tc_desc(a), db = tc_desc(a + x_bytes);
+                    for (int b = 0; b < plan.mb; ++b)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int at = k & (plan.parts - 1);
+                            tc_mma_u8<1>(tmem + (b * plan.parts + at) * bn, da + b * (128 * kL8Block / 16) + 2 * k, db + 2 * k, idesc,
+                                         kb + i > kb0 || k >= plan.parts);
+                        }
+                }
+                tc_commit<1>(&sh.empty[s]);
+                if (++s == plan.stages) { s = 0; ph ^= 1; }
+            }
+            if (ok) {
+                tc_commit<1>(&sh.acc_full);
+                ok = mbar_wait(&sh.acc_full, 0);
+            }
+        }
+    } else {
+        // the pairs of channels and tokens, while the first copies are under way
+        for (int i = threadIdx.x - 64; i < bn; i += 192) sh.col[i] = linear8_col(p, o0 + i);
+        for (int i = threadIdx.x - 64; i < rows; i += 192) {
+            const int z = __ldg(p.x_zp + (row0 + i) * p.x_inc);
+            sh.row[i] = {__ldg(p.x_step + (row0 + i) * p.x_inc), linear8_reach(z) * (float)p.K, z, 0u};
+        }
+        const int groups = min(plan.rx_groups, 6), group = (warp - 2) % groups, set = (warp - 2) / groups;
+        if (set < plan.rx_sets) {
+            // rows group * 32 + lane and, from 193 rows on, 192 further (boxes hold at most 256), in every rx_sets-th
+            // stage of the ring: a warp sees every phase of the barriers that it waits on
+            const int ra = group * 32 + lane, rb = ra + 192;
+            const bool two = group * 32 + 192 < plan.box;
+            int s = 0;
+            uint32_t ph = 0, a = 0, b = 0;
+            for (int kb = kb0; kb < kb1; kb += plan.kb_stage) {
+                if (s % plan.rx_sets == set) {
+                    ok = mbar_wait(&sh.full[s], ph);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    const unsigned char *x = stages + s * plan.kb_stage * kb_bytes;
+                    const int n = min(plan.kb_stage, kb1 - kb);
+                    for (int i = 0; i < n; ++i, x += kb_bytes) {
+                        a += staged_row_sum(x + ra * kL8Block, lane);
+                        if (two) b += staged_row_sum(x + rb * kL8Block, lane);
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.empty[s]);
+                }
+                if (++s == plan.stages) { s = 0; ph ^= 1; }
+            }
+            atomicAdd(&sh.rx[ra], a);
+            if (two) atomicAdd(&sh.rx[rb], b);
+        }
+    }
+    // every product, copy and row sum of this CTA is done (or has been given up)
+    if (!ok && p.st) atomicAdd(&p.st->wait_timeout, 1ull);
+    __syncthreads();
+    tc_fence_after();
+    {
+        // warps 0-3 and 4-7 take the blocks' four TMEM quarters in turn (a warp reads quarter warp % 4)
+        const int q = warp & 3;
+        const int b0 = plan.mb == 2 ? warp >> 2 : 0, c0 = plan.mb == 2 ? 0 : (warp >> 2) * 32, dc = plan.mb == 2 ? 32 : 64;
+        const int r = b0 * 128 + q * 32;
+        if (r < rows)
+            for (int c = c0; c < bn; c += dc) {
+                uint32_t S[32], T[32];
+                const uint32_t at = tmem + b0 * plan.parts * bn + c + ((uint32_t)(q * 32) << 16);
+                tc_ld32(at, S);
+                tc_wait_ld();
+                for (int i = 1; i < plan.parts; ++i) {
+                    tc_ld32(at + i * bn, T);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) S[j] += T[j];
+                }
+                if (r + lane < rows)
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4)
+                        *reinterpret_cast<uint4 *>(part + (r + lane) * pitch + c + j) = make_uint4(S[j], S[j + 1], S[j + 2], S[j + 3]);
+            }
+    }
+    tc_fence_before();
+    if (slices > 1) cluster_sync_all();
+    else __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tc_dealloc<1>(tmem, cols);
+    }
+    // rows slice, slice + slices, ... are this CTA's
+    for (int r = threadIdx.x; r < rows; r += 256)
+        if (r % slices == slice) {
+            uint32_t rx = sh.rx[r];
+            for (int k = 1; k < slices; ++k) {
+                uint32_t x;
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(cluster_map(sh.rx + r, (slice + k) % slices)) : "memory");
+                rx += x;
+            }
+            sh.row[r].rx = rx;
+        }
+    __syncthreads();
+    // a warp per row, a lane per pair of channels, four rows in flight
+    constexpr int U = 4;
+    for (int rb = slice + slices * warp; rb < rows; rb += slices * 8 * U)
+        for (int c = lane * 2; c < bn; c += 64) {
+            uint2 S[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                S[u] = *reinterpret_cast<const uint2 *>(part + min(rb + u * slices * 8, rows - 1) * pitch + c);
+            for (int k = 1; k < slices; ++k) {
+                const uint32_t peer = cluster_map(part + c, (slice + k) % slices);
+                uint2 v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    asm volatile("ld.shared::cluster.v2.u32 {%0,%1}, [%2];" : "=r"(v[u].x), "=r"(v[u].y)
+                                 : "r"(peer + min(rb + u * slices * 8, rows - 1) * pitch * 4) : "memory");
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    S[u].x += v[u].x;
+                    S[u].y += v[u].y;
+                }
+            }
+            const Linear8Col a = sh.col[c], b = sh.col[c + 1];
+            const float reach_a = linear8_reach(a.zp), reach_b = linear8_reach(b.zp);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int r = rb + u * slices * 8;
+                if (r >= rows) break;
+                const Linear8Row x = sh.row[r];
+                const float va = linear8_acc(S[u].x, x.zp, x.rx, a.zp, a.sum, (uint32_t)p.K, x.reachK, reach_a);
+                const float vb = linear8_acc(S[u].y, x.zp, x.rx, b.zp, b.sum, (uint32_t)p.K, x.reachK, reach_b);
+                const float ya = __fmaf_rn(va * x.step, a.step, a.bias), yb = __fmaf_rn(vb * x.step, b.step, b.bias);
+                uint16_t *dst = p.out + (row0 + r) * p.ldo + o0 + c;
+                if (vec_out && o0 + c + 2 <= p.O)
+                    *reinterpret_cast<uint32_t *>(dst) = D::encode2(ya, yb);
+                else {
+                    if (o0 + c < p.O) dst[0] = D::encode(ya);
+                    if (o0 + c + 1 < p.O) dst[1] = D::encode(yb);
+                }
+            }
+        }
+    if (slices > 1) cluster_sync_all();        // nobody leaves while its sums may still be read
+}
+
+template <class D>
+static aweq_status split_launch(const Linear8Args &a, SplitPlan plan, cudaStream_t stream)
+{
+    CUtensorMap mx, mw;
+    aweq_status rc = tma_bytes_map(&mx, a.X, a.N, a.K, a.ldx, plan.box);
+    if (rc == AWEQ_OK) rc = tma_bytes_map(&mw, a.W, a.O, a.K, a.ldw, plan.bn);
+    if (rc != AWEQ_OK) return rc;
+    AWEQ_CUDA_OK(cudaFuncSetAttribute(linear8_split_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSplitSmem));
+    const dim3 grid((unsigned)plan.slices, (unsigned)((a.O + plan.bn - 1) / plan.bn), (unsigned)((a.N + 128 * plan.mb - 1) / (128 * plan.mb)));
+    const int vec = (a.ldo % 2 == 0) && ((reinterpret_cast<uintptr_t>(a.out) & 3) == 0);
+    const cudaError_t e = launch_pdl_cluster(linear8_split_kernel<D>, grid, dim3(256), kSplitSmem, stream, (unsigned)plan.slices, a, mx,
+                                             mw, plan, vec);
+    note_launch();
+    if (e != cudaSuccess) return cuda_failed(e);
+    return AWEQ_OK;
+}
+
+aweq_status run_linear8_split(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream)
+{
+    SplitPlan s;
+    const int bn = 128, tiles = (a.O + bn - 1) / bn, slices = tiles * 4 <= kSmCount ? 4 : tiles * 3 <= kSmCount ? 3 : tiles * 2 <= kSmCount ? 2 : 1;
+    s.mb = a.N > 128 && bn <= 128 ? 2 : 1;
+    const long long rows = a.N < 128 * s.mb ? a.N : 128 * s.mb;
+    s.bn = bn;
+    s.box = (int)((rows + 7) / 8 * 8);
+    s.parts = bn * s.mb <= 128 ? 4 : bn * s.mb <= 256 ? 2 : 1;
+    const int nkb = (a.K + kL8Block - 1) / kL8Block;
+    s.slices = slices < nkb ? slices : nkb;                // no slice is empty
+    const int kb_bytes = (s.box + bn) * kL8Block, span = s.mb * 128 * kL8Block;
+    s.kb_stage = kb_bytes <= 20 * 1024 ? 2 : 1;
+    // the product's 128 rows per block stay inside the ring from the last block of K on too
+    const int blocks = (kSplitRing - (span > kb_bytes ? span : kb_bytes)) / kb_bytes + 1;
+    s.stages = blocks / s.kb_stage;
+    if (s.stages > kSplitMaxStages) s.stages = kSplitMaxStages;
+    s.rx_groups = (s.box + 31) / 32;
+    s.rx_sets = s.rx_groups <= 3 ? 6 / s.rx_groups : 1;
+    return dt == AWEQ_F16 ? split_launch<F16>(a, s, stream) : split_launch<BF16>(a, s, stream);
 }
 
 }  // namespace aweq
