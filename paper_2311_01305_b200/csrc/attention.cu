@@ -2,8 +2,14 @@
 //
 // All rows (token, head) that read one key head share the prefix, so the prefix is a dense product of a [rows x D]
 // matrix with K and V, read once per tile of rows; the own keys are a product of the n_q * G rows of one
-// sequence (G heads to a key head).  Both are cut along the keys into items, all items of both kinds run in
-// one launch, each leaving (maximum, sum, output) of its keys for its rows, and a second launch joins them:
+// sequence (G heads to a key head).  An item is a tile of rows with all its keys; its unit is a tile of 64 keys.
+// The units of all items in a row are dealt out evenly to a grid that fills the device once, so a CTA streams
+// through parts of one or several items without ever draining its copies, whatever the lengths are (they are known
+// on the device only).  Four warps walk the units, look up pages and copy the rows of K and V into a ring of stages
+// (cp.async: a bulk copy per row took 40 cycles each), 16 rows of a unit each; four other warps compute, with most of the
+// registers.  (With every warp doing its share of both, the lookups and copies, 1.8 us a unit, added to the 0.6 us of the
+// products; a single copying warp took 2.6 us a unit.)  Where a CTA leaves an item it writes a record (maximum m, sum l, output o of the keys it
+// has seen, for each row), and a second launch joins the records of a row:
 //   m = max m_i,  l = sum 2^(m_i - m) l_i,  out = sum 2^(m_i - m) o_i / l      (scores in units of log 2)
 #include <math_constants.h>
 
@@ -12,23 +18,27 @@
 
 namespace aweq {
 
-constexpr int kAtTile = 64;                 // keys of a tile
+constexpr int kAtTile = 64;                 // keys of a unit
 constexpr int kAtStages = 3;
-constexpr int kAtThreads = 128;
-constexpr int kAtMostPrefix = 64, kAtMostOwn = 16;      // splits of the prefix, of a sequence's own keys
+constexpr int kAtThreads = 256;             // four computing warps, four that copy
+// registers of a computing / copying thread: their mean is what the launch gives every thread (two CTAs of 256)
+constexpr int kAtComputeRegs = 200, kAtCopyRegs = 56;
 
 // How the work is cut (host; also sizes the scratch).
 struct AttentionPlan {
     int dp;                      // head_dim padded to 64, 96 or 128
-    int pre_wm, own_wm;          // warps along the rows of a prefix / own item (4 / wm along the keys)
+    int pre_wm, own_wm;          // warps along the rows of a prefix / own item (4 / wm share its keys)
     int pre_rt, own_rt;          // row tiles per key head / per sequence and key head
-    int pre_splits, own_splits;  // most items along the keys
-    int own_chunk;               // own keys (in tiles) that make another split worth while
-    long long pre_items, own_items, rows;
-    size_t off_ml, total;
+    int own_rec_rows;            // rows of an own record
+    int ctas;
+    long long pre_tiles, pre_units, rows;
+    // scratch: start of each sequence's units (long long[n_seq + 1], the total last), records
+    size_t off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
 };
 
 static int rows_warps(long long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+static size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
+constexpr int kAtCtasPerSm = 2;
 
 static AttentionPlan attention_plan(long long prefix_len, long long max_own, long long n_seq, int n_q, int n_heads, int n_kv,
                                     int head_dim)
@@ -41,33 +51,22 @@ static AttentionPlan attention_plan(long long prefix_len, long long max_own, lon
     p.own_wm = rows_warps(own_rows);
     p.pre_rt = (int)((pre_rows + 16 * p.pre_wm - 1) / (16 * p.pre_wm));
     p.own_rt = (int)((own_rows + 16 * p.own_wm - 1) / (16 * p.own_wm));
-    const long long pre_tiles = (prefix_len + kAtTile - 1) / kAtTile;
-    const long long own_tiles = (max_own + kAtTile - 1) / kAtTile;
-    // the chunk length (in tiles) whose items fill the SMs best: waves of two CTAs per SM, each costing its keys
-    // and about three tiles of filling, draining and joining
-    const long long slots = 2 * kSmCount, pre_base = (long long)n_kv * p.pre_rt, own_base = n_seq * n_kv * p.own_rt;
-    double best = 0;
-    p.pre_splits = p.own_splits = 0;
-    p.own_chunk = 1;
-    for (int t = 1; t <= 1024; t += t < 16 ? 1 : t < 128 ? 4 : 64) {
-        long long ps = (pre_tiles + t - 1) / t, os = (own_tiles + t - 1) / t;
-        if (ps > kAtMostPrefix) ps = kAtMostPrefix;
-        if (os > kAtMostOwn) os = kAtMostOwn;
-        const long long items = pre_base * ps + own_base * os;
-        const long long longest = ps ? (pre_tiles + ps - 1) / ps : 0;
-        const double cost = (double)((items + slots - 1) / slots) * ((longest > t ? longest : t) + 3.0);
-        if (p.pre_splits + p.own_splits == 0 || cost < best) {
-            best = cost;
-            p.pre_splits = (int)ps;
-            p.own_splits = (int)os;
-            p.own_chunk = t;
-        }
-    }
-    p.pre_items = pre_base * p.pre_splits;
-    p.own_items = own_base * p.own_splits;
-    const size_t slices = (size_t)(p.pre_splits + p.own_splits) * (size_t)p.rows;
-    p.off_ml = (slices * head_dim * 4 + 255) & ~(size_t)255;
-    p.total = p.off_ml + slices * 8 + 256;
+    p.own_rec_rows = (int)(own_rows < 16 * p.own_wm ? own_rows : 16 * p.own_wm);
+    p.pre_tiles = (prefix_len + kAtTile - 1) / kAtTile;
+    p.pre_units = p.pre_tiles * n_kv * p.pre_rt;
+    const long long own_items = n_seq * n_kv * p.own_rt;
+    const double most = (double)p.pre_units + (double)own_items * (double)((max_own + kAtTile - 1) / kAtTile);
+    p.ctas = kSmCount * kAtCtasPerSm;
+    if (most < p.ctas) p.ctas = most < 1 ? 1 : (int)most;
+    // an item makes a record, and one more for every CTA boundary inside it
+    const size_t pre_rows_kept = p.pre_tiles ? (size_t)((long long)n_kv * p.pre_rt + p.ctas) * 16 * p.pre_wm : 0;
+    const size_t own_rows_kept = (size_t)(own_items + p.ctas) * p.own_rec_rows;
+    size_t off = up256((size_t)(n_seq + 1) * 8);
+    p.off_pre_o = off; off += up256(pre_rows_kept * head_dim * 4);
+    p.off_pre_ml = off; off += up256(pre_rows_kept * 8);
+    p.off_own_o = off; off += up256(own_rows_kept * head_dim * 4);
+    p.off_own_ml = off; off += up256(own_rows_kept * 8);
+    p.total = off;
     return p;
 }
 
@@ -106,9 +105,6 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool i
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float r;
@@ -126,403 +122,580 @@ __device__ __forceinline__ float quad_sum(float v)
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
-// A clamped own length; every thread of every item computes the same.  `count`: the one caller that reports it.
-__device__ __forceinline__ long long own_length(const AttentionArgs &a, long long b, bool count)
+// A clamped own length.  `count`: the one caller that reports it.
+__device__ __forceinline__ int own_length(const AttentionArgs &a, long long b, bool count)
 {
-    long long len = __ldg(a.own_len + b);
-    const long long most = min(a.max_own, a.pages_per_seq * a.page_size);
+    const int len = __ldg(a.own_len + b);
+    const int most = (int)min(a.max_own, a.pages_per_seq * a.page_size);
     if (len < 0 || len > most) {
         if (count && a.st) atomicAdd(&a.st->out_of_range, 1ull);
-        len = len < 0 ? 0 : most;
+        return len < 0 ? 0 : most;
     }
     return len;
 }
-// own items along the keys of a sequence of `tiles` tiles
-__device__ __forceinline__ int own_splits_of(long long tiles, int most, int chunk)
+__device__ __forceinline__ int tiles_of(int len) { return (int)(((unsigned)len + kAtTile - 1) / kAtTile); }
+// The units are dealt out in order, total / ctas to a CTA and one more to the first total % ctas.  (Divisions of 64 bits
+// take hundreds of cycles: only where the numbers need them.)
+__device__ __forceinline__ long long div_units(long long a, int b)
 {
-    const long long n = (tiles + chunk - 1) / chunk;
-    return (int)(n < most ? n : most);
+    return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
-
-struct AttentionItem {
-    const int *pages;
-    long long k0, k1;            // keys [k0, k1)
-    long long limit0;            // own keys: token i of the sequence sees keys below limit0 + i; prefix: all
-    long long row0;              // first row (token * G + head in group) of this key head
-    int nrows, kh, slot;         // rows, key head, slice of the scratch
-    bool own;
+struct AttentionDeal {
+    long long each, more;        // units of a CTA, CTAs with one more
+    int ctas;                    // those that have any
+    __device__ __forceinline__ AttentionDeal(long long total, int most)
+    {
+        ctas = total < most ? (int)total : most;
+        each = ctas ? div_units(total, ctas) : 0;
+        more = total - each * ctas;
+    }
+    __device__ __forceinline__ long long first(int cta) const { return each * cta + (cta < more ? cta : more); }
+    __device__ __forceinline__ int cta_of(long long u) const
+    {
+        const long long big = more * (each + 1);
+        if ((each + 1) >> 31) return u < big ? (int)(u / (each + 1)) : (int)(more + (u - big) / each);
+        return u < big ? (int)div_units(u, (int)(each + 1)) : (int)more + (int)div_units(u - big, (int)each);
+    }
 };
 
+// What a unit is: the tile'th tile of the `len` keys of an item.
+struct alignas(16) AttentionUnit {
+    int own, kh, rt, b, tile, len;
+    int leave;                   // the CTA's last unit of this item
+    int stop;                    // 1: the CTA's last unit, 2: nothing to compute
+};
+// A staged row: its 16-byte pieces permuted by the row's number modulo 8, so that eight rows' like pieces lie in
+// different banks (rows of 12 pieces are kept in 16)
+__host__ __device__ constexpr int at_pitch(int dp) { return dp == 64 ? 128 : 256; }
+__device__ __forceinline__ uint32_t at_piece(int row, int piece) { return (uint32_t)((piece ^ (row & 7)) * 16); }
+
+struct AttentionState {          // of a warp's 16 rows: lanes hold rows g and g + 8
+    float m[2], l[2];
+};
+
+// One tile of keys for a warp's 16 rows.  WM warps of the CTA lie along the rows, 4 / WM share the keys of the tile.
 template <class D, int DP, int WM>
-__device__ __forceinline__ void attention_item(const AttentionArgs &a, const AttentionItem &it, float *o_part, float2 *ml_part,
-                                               long long rows_total, unsigned char *smem)
+__device__ __forceinline__ void attention_tile(const AttentionArgs &a, const AttentionUnit &it, uint32_t ks, const uint32_t (&q)[DP / 16][4],
+                                               const int (&own_i)[2], float scale, float (&o)[DP / 8][4], AttentionState &st)
 {
     constexpr int KW = 4 / WM, NT = kAtTile / 8 / KW;           // warps along the keys, 8-key groups of a warp
-    constexpr int PITCH = DP * 2 + 16;                          // bytes of a staged row: 16 more against bank conflicts
-    constexpr int STAGE = 2 * kAtTile * PITCH;
-    constexpr int CH = DP / 8;                                  // 16-byte pieces of a row
-    long long *const offs = reinterpret_cast<long long *>(smem + kAtStages * STAGE);          // [kAtStages + 1][kAtTile]
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int wm = warp % WM, wk = warp / WM;
-    const int G = a.n_heads / a.n_kv, hd = a.head_dim;
-    const int tiles = (int)((it.k1 - it.k0 + kAtTile - 1) / kAtTile);
-
-    // element offsets of a tile's keys (before the head), -1 past the end
-    auto find = [&](int tile) {
-        if (tile < tiles && tid < kAtTile) {
-            const long long c = it.k0 + (long long)tile * kAtTile + tid;
-            long long off = -1;
-            if (c < it.k1) {
-                long long page = __ldg(it.pages + (unsigned)c / (unsigned)a.page_size);
-                if (page < 0 || page >= a.n_pages) {
-                    if (a.st) atomicAdd(&a.st->out_of_range, 1ull);
-                    page = 0;
-                }
-                off = page * a.page_stride + (long long)((unsigned)c % (unsigned)a.page_size) * a.token_stride + it.kh * a.head_stride;
-            }
-            offs[(tile % (kAtStages + 1)) * kAtTile + tid] = off;
-        }
-    };
-    auto load = [&](int tile) {
-        if (tile < tiles) {
-            const uint32_t dst = smem_u32(smem + (tile % kAtStages) * STAGE);
-            const long long *of = offs + (tile % (kAtStages + 1)) * kAtTile;
+    constexpr int PITCH = at_pitch(DP);
+    const int lane = threadIdx.x & 31, t = lane & 3;
+    const uint32_t vs = ks + kAtTile * PITCH;
+    const int key0 = (int)(threadIdx.x >> 5) / WM * (NT * 8);   // this warp's keys of the tile
+    float s[NT][4] = {};
 #pragma unroll
-            for (int i = 0; i < kAtTile * CH / kAtThreads; ++i) {
-                const int idx = tid + i * kAtThreads, r = idx / CH, c = idx % CH;
-                const long long off = of[r];
-                const bool in = off >= 0 && c * 8 < hd;
-                const long long src = in ? off + c * 8 : 0;
-                cp_async16(dst + r * PITCH + c * 16, a.ck + src, in);
-                cp_async16(dst + (kAtTile + r) * PITCH + c * 16, a.cv + src, in);
-            }
+    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+        for (int n = 0; n < NT; n += 2) {
+            uint32_t b[4];          // keys n*8.. (k halves 0, 1), keys n*8 + 8.. (k halves 0, 1)
+            ldsm4(b, ks + (key0 + n * 8 + (lane & 7) + (lane >> 4) * 8) * PITCH + ((k * 2 + ((lane >> 3) & 1)) ^ (lane & 7)) * 16);
+            mma16<D>(s[n], q[k], b[0], b[1]);
+            mma16<D>(s[n + 1], q[k], b[2], b[3]);
         }
-        cp_async_commit();
-    };
-    for (int i = 0; i < kAtStages; ++i) find(i);
-    __syncthreads();
-    for (int i = 0; i < kAtStages - 1; ++i) load(i);
-
-    // this warp's 16 rows of q, as A fragments: rows g and g + 8
-    uint32_t q[DP / 16][4];
-    long long tok[2];
-    int rloc[2];
+    // keys of this warp's share that a row sees: token i of a sequence leaves out the last n_q - 1 - i
+    const int there = it.len - (it.tile * kAtTile + key0), first = it.own ? there - (a.n_q - 1) : there;
+    const bool edge = first < NT * 8;
+    float top[2] = {st.m[0], st.m[1]};
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            s[n][e] *= scale;
+            if (edge && n * 8 + 2 * t + (e & 1) >= first + own_i[e >> 1]) s[n][e] = -CUDART_INF_F;
+            top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
+        }
+    float base[2], f[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        rloc[h] = wm * 16 + g + h * 8;
-        const long long r = it.row0 + min(rloc[h], it.nrows - 1);
-        tok[h] = r / G;
-        const uint16_t *src = a.q + tok[h] * a.ldq + (long long)(it.kh * G + (int)(r % G)) * hd;
-#pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int d = k * 16 + e * 8 + 2 * t;
-                q[k][h + 2 * e] = d < hd && rloc[h] < it.nrows ? *reinterpret_cast<const uint32_t *>(src + d) : 0u;
-            }
+        top[h] = quad_max(top[h]);
+        base[h] = top[h] == -CUDART_INF_F ? 0.0f : top[h];      // a row that has seen no key yet
+        f[h] = exp2_fast(st.m[h] - base[h]);
+        st.m[h] = top[h];
+        st.l[h] *= f[h];
     }
-    // keys that rows g and g + 8 see
-    long long lim[2];
+    // The probabilities are rounded to the 16-bit type for the product with v (at most half a unit of it each, as the
+    // output's own rounding); their sum is not.
+    uint32_t p[NT / 2][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) lim[h] = it.own ? it.limit0 + tok[h] % a.n_q : it.k1;
-    const long long lim_min = it.own ? it.limit0 : it.k1;       // a tile below it needs no comparison
-
-    float o[DP / 8][4] = {}, m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.0f, 0.0f};
-    const float scale = a.scale * 1.4426950408889634f;
-    for (int tile = 0; tile < tiles; ++tile) {
-        cp_async_wait<kAtStages - 2>();
-        __syncthreads();
-        load(tile + kAtStages - 1);
-        find(tile + kAtStages);
-        const uint32_t ks = smem_u32(smem + (tile % kAtStages) * STAGE), vs = ks + kAtTile * PITCH;
-        const int key0 = wk * (NT * 8);                          // this warp's keys of the tile
-        float s[NT][4] = {};
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-                uint32_t b[4];          // keys n*8.. (k halves 0, 1), keys n*8 + 8.. (k halves 0, 1)
-                ldsm4(b, ks + (key0 + n * 8 + (lane & 7) + (lane >> 4) * 8) * PITCH + k * 32 + ((lane >> 3) & 1) * 16);
-                mma16<D>(s[n], q[k], b[0], b[1]);
-                mma16<D>(s[n + 1], q[k], b[2], b[3]);
-            }
-        const long long c0 = it.k0 + (long long)tile * kAtTile + key0;
-        const bool edge = c0 + NT * 8 > lim_min;
-        float top[2] = {m[0], m[1]};
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[n][e] *= scale;
-                if (edge && c0 + n * 8 + 2 * t + (e & 1) >= lim[e >> 1]) s[n][e] = -CUDART_INF_F;
-                top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
-            }
-        float base[2], f[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            top[h] = quad_max(top[h]);
-            base[h] = top[h] == -CUDART_INF_F ? 0.0f : top[h];  // a row that has seen no key yet
-            f[h] = exp2_fast(m[h] - base[h]);
-            m[h] = top[h];
-            l[h] *= f[h];
+        for (int e = 0; e < 4; ++e) {
+            s[n][e] = exp2_fast(s[n][e] - base[e >> 1]);
+            st.l[e >> 1] += s[n][e];
         }
-        uint32_t p[NT / 2][4];          // probabilities as A fragments, rounded to the 16-bit type
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[n][e] = exp2_fast(s[n][e] - base[e >> 1]);
-                l[e >> 1] += s[n][e];
-            }
-            p[n / 2][(n & 1) * 2] = D::encode2(s[n][0], s[n][1]);
-            p[n / 2][(n & 1) * 2 + 1] = D::encode2(s[n][2], s[n][3]);
-        }
+        p[n / 2][(n & 1) * 2] = D::encode2(s[n][0], s[n][1]);
+        p[n / 2][(n & 1) * 2 + 1] = D::encode2(s[n][2], s[n][3]);
+    }
+    if (__any_sync(0xffffffffu, f[0] != 1.0f || f[1] != 1.0f))   // the maxima soon stay what they are
 #pragma unroll
         for (int n = 0; n < DP / 8; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[n][e] *= f[e >> 1];
-        if (!(it.own && edge && a.n_q > 1)) {
+    // Among the last keys are some that only a sequence's later tokens see.  Zero times their values is zero unless a value is
+    // infinite or NaN, which is looked for.
+    bool apart = false;
+    if (it.own && edge && a.n_q > 1) {
+        const int from = max(first, 0), to = min(there, NT * 8);
+        for (int i = lane; i < (to - from) * (DP / 8); i += 32) {
+            const int r = key0 + from + i / (DP / 8);
+            uint4 v;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                         : "r"(vs + r * PITCH + at_piece(r, i % (DP / 8))) : "memory");
+            apart |= D::any_nonfinite(v);
+        }
+        apart = __any_sync(0xffffffffu, apart);
+    }
+    if (!apart) {
+#pragma unroll
+        for (int k = 0; k < NT / 2; ++k)
+#pragma unroll
+            for (int n = 0; n < DP / 8; n += 2) {
+                uint32_t b[4];
+                ldsm4t(b, vs + (key0 + k * 16 + (lane & 15)) * PITCH + ((n + (lane >> 4)) ^ (lane & 7)) * 16);
+                mma16<D>(o[n], p[k], b[0], b[1]);
+                mma16<D>(o[n + 1], p[k], b[2], b[3]);
+            }
+    } else {
+        // one token's rows at a time, with the values beyond its limit replaced by zero
+        const int lo = __reduce_min_sync(0xffffffffu, min(own_i[0], own_i[1])), hi = __reduce_max_sync(0xffffffffu, max(own_i[0], own_i[1]));
+        for (int i = lo; i <= hi; ++i) {
 #pragma unroll
             for (int k = 0; k < NT / 2; ++k)
 #pragma unroll
                 for (int n = 0; n < DP / 8; n += 2) {
                     uint32_t b[4];
-                    ldsm4t(b, vs + (key0 + k * 16 + (lane & 15)) * PITCH + n * 16 + (lane >> 4) * 16);
-                    mma16<D>(o[n], p[k], b[0], b[1]);
-                    mma16<D>(o[n + 1], p[k], b[2], b[3]);
-                }
-        } else {
-            // The last keys: a key may be one that only the later tokens see, and 0 * Inf of its value must not reach the
-            // earlier ones.  One token's rows at a time, with the values beyond its limit replaced by zero.
-            long long i0 = tok[0] % a.n_q, i1 = tok[1] % a.n_q;
-            long long lo = min(i0, i1), hi = max(i0, i1);
-            for (int x = 16; x > 0; x >>= 1) {
-                lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, x));
-                hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, x));
-            }
-            for (long long i = lo; i <= hi; ++i) {
-                const long long left = it.limit0 + i - c0;       // keys of this warp's share that token i sees
+                    ldsm4t(b, vs + (key0 + k * 16 + (lane & 15)) * PITCH + ((n + (lane >> 4)) ^ (lane & 7)) * 16);
 #pragma unroll
-                for (int k = 0; k < NT / 2; ++k)
-#pragma unroll
-                    for (int n = 0; n < DP / 8; n += 2) {
-                        uint32_t b[4];
-                        ldsm4t(b, vs + (key0 + k * 16 + (lane & 15)) * PITCH + n * 16 + (lane >> 4) * 16);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const long long key = k * 16 + (e & 1) * 8 + 2 * t;
-                            if (key >= left) b[e] = 0u;
-                            else if (key + 1 >= left) b[e] &= 0xffffu;
-                        }
-                        float c[4] = {}, d[4] = {};
-                        mma16<D>(c, p[k], b[0], b[1]);
-                        mma16<D>(d, p[k], b[2], b[3]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if ((e >> 1 ? i1 : i0) == i) {
-                                o[n][e] += c[e];
-                                o[n + 1][e] += d[e];
-                            }
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = k * 16 + (e & 1) * 8 + 2 * t;
+                        if (key >= first + i) b[e] = 0u;
+                        else if (key + 1 >= first + i) b[e] &= 0xffffu;
                     }
-            }
-        }
-    }
-    cp_async_wait<0>();
+                    float c[4] = {}, d[4] = {};
+                    mma16<D>(c, p[k], b[0], b[1]);
+                    mma16<D>(d, p[k], b[2], b[3]);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) l[h] = quad_sum(l[h]);
-
-    if (KW > 1) {
-        // join the warps that shared the rows: maxima and factors first, then the outputs through shared memory
-        __syncthreads();
-        float *const ex = reinterpret_cast<float *>(smem);       // [4 warps][16 rows] x {m, l}, then outputs
-        float *const eo = ex + 4 * 16 * 2;
-        if (t == 0)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                ex[(warp * 16 + g + h * 8) * 2] = m[h];
-                ex[(warp * 16 + g + h * 8) * 2 + 1] = l[h];
-            }
-        __syncthreads();
-        float all_m[2], all_l[2], mine[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            all_m[h] = -CUDART_INF_F;
-#pragma unroll
-            for (int k = 0; k < KW; ++k) all_m[h] = fmaxf(all_m[h], ex[((k * WM + wm) * 16 + g + h * 8) * 2]);
-            const float b = all_m[h] == -CUDART_INF_F ? 0.0f : all_m[h];
-            all_l[h] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < KW; ++k) {
-                const float *x = ex + ((k * WM + wm) * 16 + g + h * 8) * 2;
-                all_l[h] += x[1] * exp2_fast(x[0] - b);
-            }
-            mine[h] = exp2_fast(m[h] - b);
-            m[h] = all_m[h];
-            l[h] = all_l[h];
-        }
-#pragma unroll
-        for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                *reinterpret_cast<float2 *>(eo + (warp * 16 + g + h * 8) * (DP + 8) + n * 8 + 2 * t) =
-                    make_float2(o[n][2 * h] * mine[h], o[n][2 * h + 1] * mine[h]);
-        __syncthreads();
-        // every thread adds a share of the columns
-        for (int i = tid; i < WM * 16 * (DP / 4); i += kAtThreads) {
-            const int r = i / (DP / 4), c = i % (DP / 4) * 4;
-            if (r >= it.nrows || c >= hd) continue;
-            float4 v = make_float4(0, 0, 0, 0);
-#pragma unroll
-            for (int k = 0; k < KW; ++k) {
-                const float4 x = *reinterpret_cast<const float4 *>(eo + ((k * WM + r / 16) * 16 + r % 16) * (DP + 8) + c);
-                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-            }
-            const long long row = it.row0 + r, out_row = (row / G) * a.n_heads + it.kh * G + row % G;
-            *reinterpret_cast<float4 *>(o_part + ((long long)it.slot * rows_total + out_row) * hd + c) = v;
-        }
-        if (wk == 0 && t == 0)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (rloc[h] < it.nrows) {
-                    const long long row = it.row0 + rloc[h], out_row = (row / G) * a.n_heads + it.kh * G + row % G;
-                    ml_part[(long long)it.slot * rows_total + out_row] = make_float2(m[h], l[h]);
+                    for (int e = 0; e < 4; ++e)
+                        if (own_i[e >> 1] == i) {
+                            o[n][e] += c[e];
+                            o[n + 1][e] += d[e];
+                        }
                 }
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (rloc[h] >= it.nrows) continue;
-            const long long row = it.row0 + rloc[h], out_row = (row / G) * a.n_heads + it.kh * G + row % G;
-            float *dst = o_part + ((long long)it.slot * rows_total + out_row) * hd;
-#pragma unroll
-            for (int n = 0; n < DP / 8; ++n)
-                if (n * 8 < hd) *reinterpret_cast<float2 *>(dst + n * 8 + 2 * t) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
-            if (t == 0) ml_part[(long long)it.slot * rows_total + out_row] = make_float2(m[h], l[h]);
         }
     }
 }
 
 template <int DP>
-constexpr size_t attention_smem() { return (size_t)kAtStages * 2 * kAtTile * (DP * 2 + 16) + (kAtStages + 1) * kAtTile * 8; }
+__host__ __device__ constexpr int attention_stage_bytes() { return (2 * kAtTile + 16) * at_pitch(DP); }     // K, V, 16 rows of q
 
-template <class D, int DP>
-__global__ void __launch_bounds__(kAtThreads, 2)
-attention_items_kernel(const AttentionArgs a, const AttentionPlan p, float *o_part, float2 *ml_part)
-{
-    extern __shared__ __align__(16) unsigned char smem[];
-    pdl_begin();
-    const int G = a.n_heads / a.n_kv;
-    AttentionItem it;
-    int wm;
-    long long x = blockIdx.x;
-    if (x < p.pre_items) {
-        // row tiles of the same keys are neighbours: they find them in the L2
-        const long long rows = a.n_seq * a.n_q * G;
-        const int rt = (int)(x % p.pre_rt);
-        x /= p.pre_rt;
-        const int s = (int)(x % p.pre_splits);
-        it.kh = (int)(x / p.pre_splits);
-        const long long tiles = (a.prefix_len + kAtTile - 1) / kAtTile;
-        it.pages = a.prefix_pages;
-        it.k0 = tiles * s / p.pre_splits * kAtTile;
-        it.k1 = min(a.prefix_len, tiles * (s + 1) / p.pre_splits * kAtTile);
-        it.limit0 = 0;
-        it.row0 = (long long)rt * 16 * p.pre_wm;
-        it.nrows = (int)min(rows - it.row0, 16ll * p.pre_wm);
-        it.slot = s;
-        it.own = false;
-        wm = p.pre_wm;
-    } else {
-        x -= p.pre_items;
-        const int s = (int)(x % p.own_splits);
-        x /= p.own_splits;
-        const int rt = (int)(x % p.own_rt);
-        x /= p.own_rt;
-        it.kh = (int)(x % a.n_kv);
-        const long long b = x / a.n_kv;
-        const long long len = own_length(a, b, threadIdx.x == 0 && s == 0 && rt == 0 && it.kh == 0);
-        const long long tiles = (len + kAtTile - 1) / kAtTile;
-        const int splits = own_splits_of(tiles, p.own_splits, p.own_chunk);
-        if (s >= splits) return;
-        it.pages = a.page_table + b * a.ld_table;
-        it.k0 = tiles * s / splits * kAtTile;
-        it.k1 = min(len, tiles * (s + 1) / splits * kAtTile);
-        it.limit0 = len - (a.n_q - 1);
-        it.row0 = b * a.n_q * G + (long long)rt * 16 * p.own_wm;
-        it.nrows = (int)min((long long)a.n_q * G - (long long)rt * 16 * p.own_wm, 16ll * p.own_wm);
-        it.slot = p.pre_splits + s;
-        it.own = true;
-        wm = p.own_wm;
-    }
-    if (wm == 1) attention_item<D, DP, 1>(a, it, o_part, ml_part, p.rows, smem);
-    else if (wm == 2) attention_item<D, DP, 2>(a, it, o_part, ml_part, p.rows, smem);
-    else attention_item<D, DP, 4>(a, it, o_part, ml_part, p.rows, smem);
-}
-
-// One warp per row (token, head): the slices' maxima and sums, then the weighted outputs.
-template <class D>
-__global__ void __launch_bounds__(128)
-attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const float *__restrict__ o_part, const float2 *__restrict__ ml_part)
-{
-    pdl_begin();
-    const int lane = threadIdx.x & 31;
-    const long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (r >= p.rows) return;
-    const long long tok = r / a.n_heads, len = own_length(a, tok / a.n_q, false);
-    const int n = p.pre_splits + own_splits_of((len + kAtTile - 1) / kAtTile, p.own_splits, p.own_chunk);
-    float m = -CUDART_INF_F, l = 0.0f;
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, ml_part[(long long)i * p.rows + r].x);
-    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    const float base = m == -CUDART_INF_F ? 0.0f : m;
-    float4 o = make_float4(0, 0, 0, 0);
-    const bool in = lane * 4 < a.head_dim;
-    for (int i = 0; i < n; ++i) {
-        const float2 x = ml_part[(long long)i * p.rows + r];
-        const float w = exp2_fast(x.x - base);
-        l += w * x.y;
-        if (in) {
-            const float4 v = *reinterpret_cast<const float4 *>(o_part + ((long long)i * p.rows + r) * a.head_dim + lane * 4);
-            o.x += w * v.x; o.y += w * v.y; o.z += w * v.z; o.w += w * v.w;
+// The walk over a CTA's units by a warp: every lane knows the unit and looks up the page of a key.
+struct AttentionWalk {
+    AttentionUnit at;
+    int tiles, next_len;         // of the item; length of the sequence after this one (its load is long under way when needed)
+    __device__ __forceinline__ void advance(const AttentionArgs &a, const AttentionPlan &p)
+    {
+        if (++at.tile < tiles) return;
+        at.tile = 0;
+        if (++at.rt < (at.own ? p.own_rt : p.pre_rt)) return;
+        at.rt = 0;
+        if (++at.kh < a.n_kv) return;
+        at.kh = 0;
+        const int n_seq = (int)a.n_seq;
+        if (at.own) ++at.b;
+        at.own = 1;
+        for (;;) {                                              // sequences without keys have no units
+            at.len = next_len;
+            tiles = tiles_of(at.len);
+            next_len = at.b + 1 < n_seq ? own_length(a, at.b + 1, false) : 0;
+            if (tiles > 0 || at.b + 1 >= n_seq) return;
+            ++at.b;
         }
     }
-    if (in) {
+    // page of the lane's r'th key of the unit; -1: no such key, -2: a page outside the pool
+    __device__ __forceinline__ int page(const AttentionArgs &a, int r) const
+    {
+        const int c = at.tile * kAtTile + r;
+        if (c >= at.len) return -1;
+        const int *pages = at.own ? a.page_table + (long long)at.b * a.ld_table : a.prefix_pages;
+        const int page = __ldg(pages + (unsigned)c / (unsigned)a.page_size);
+        return page < 0 || page >= a.n_pages ? -2 : page;
+    }
+};
+
+template <class D, int DP>
+__global__ void __launch_bounds__(kAtThreads, kAtCtasPerSm)
+attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned char *ws)
+{
+    constexpr int PITCH = at_pitch(DP), STAGE = attention_stage_bytes<DP>();
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ uint64_t full[kAtStages], empty[kAtStages];
+    __shared__ AttentionUnit unit[kAtStages];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int hd = a.head_dim, cta = blockIdx.x;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (tid == 0) {
+        for (int s = 0; s < kAtStages; ++s) {
+            mbar_init(&full[s], 129);                           // every copying lane, and the unit itself
+            mbar_init(&empty[s], 4);
+        }
+        mbar_init_fence();
+    }
+    if (hd < DP)                                                // what no copy writes: columns past head_dim
+        for (int i = tid; i < kAtStages * (2 * kAtTile + 16) * ((DP - hd) / 8); i += kAtThreads) {
+            const int r = i / ((DP - hd) / 8);                  // a stage is a multiple of eight rows
+            *reinterpret_cast<uint4 *>(smem + r * PITCH + at_piece(r, hd / 8 + i % ((DP - hd) / 8))) = make_uint4(0, 0, 0, 0);
+        }
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    if (warp >= 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAtCopyRegs));
+        const int cw = warp - 4;
+        const bool lead = cta == 0 && cw == 0;                  // reports lengths, leaves the starts for the join
+        const int n_seq = (int)a.n_seq, per_seq = a.n_kv * p.own_rt;
+        // the number of units, and where this CTA's first one lies
+        auto scan = [&](int b, bool count, int *n) {            // tiles of 32 sequences: own, before it
+            *n = b < n_seq ? tiles_of(own_length(a, b, count)) : 0;
+            int sum = *n;                                       // 32 lengths of at most 2^31 keys: below 2^31 tiles
+#pragma unroll
+            for (int x = 1; x < 32; x <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, sum, x);
+                if (lane >= x) sum += y;
+            }
+            return (long long)(sum - *n);
+        };
+        long long *const start = reinterpret_cast<long long *>(ws);
+        long long total = 0;
+        int n;
+        for (int b0 = 0; b0 < n_seq; b0 += 32) {
+            const long long before = scan(b0 + lane, lead, &n);
+            if (lead && b0 + lane < n_seq) start[b0 + lane] = p.pre_units + (total + before) * per_seq;
+            total += __shfl_sync(0xffffffffu, before + n, 31);
+        }
+        total = p.pre_units + total * per_seq;
+        if (lead && lane == 0) start[n_seq] = total;
+        const AttentionDeal deal(total, p.ctas);
+        if (cta >= deal.ctas) {
+            if (cw == 0 && lane == 0) {
+                unit[0].stop = 2;
+                mbar_arrive(&full[0]);
+            }
+            mbar_arrive(&full[0]);
+            return;
+        }
+        const long long u0 = deal.first(cta);
+        int left = (int)(deal.first(cta + 1) - u0);
+        AttentionWalk w;
+        w.at = {};
+        if (u0 < p.pre_units) {
+            const int item = (int)div_units(u0, (int)p.pre_tiles);
+            w.at.kh = item / p.pre_rt;
+            w.at.rt = item % p.pre_rt;
+            w.at.tile = (int)(u0 - item * p.pre_tiles);
+            w.at.len = (int)a.prefix_len;
+            w.tiles = (int)p.pre_tiles;
+            w.next_len = n_seq ? own_length(a, 0, false) : 0;
+        } else {
+            long long passed = p.pre_units;
+            for (int b0 = 0;; b0 += 32) {
+                const long long mine = passed + scan(b0 + lane, false, &n) * per_seq;
+                const uint32_t here = __ballot_sync(0xffffffffu, u0 >= mine && u0 < mine + (long long)n * per_seq);
+                if (here) {
+                    const int src = __ffs(here) - 1, within = (int)(u0 - __shfl_sync(0xffffffffu, mine, src));
+                    w.tiles = __shfl_sync(0xffffffffu, n, src);
+                    w.at.own = 1;
+                    w.at.b = b0 + src;
+                    w.at.kh = within / w.tiles / p.own_rt;
+                    w.at.rt = within / w.tiles % p.own_rt;
+                    w.at.tile = within % w.tiles;
+                    break;
+                }
+                passed = __shfl_sync(0xffffffffu, mine + (long long)n * per_seq, 31);
+            }
+            w.at.len = own_length(a, w.at.b, false);
+            w.next_len = w.at.b + 1 < n_seq ? own_length(a, w.at.b + 1, false) : 0;
+        }
+        // lanes 0-15 know this warp's 16 rows of a unit; a lane copies the same 16-byte piece of every (32 / CH)-th
+        constexpr int CH = DP / 8 == 12 ? 16 : DP / 8, R = 32 / CH;
+        const int mine = cw * 16 + (lane & 15), piece = lane % CH * 8;
+        const uint32_t dst0 = smem_u32(smem) + cw * 16 * PITCH;
+        const int G = a.n_heads / a.n_kv;
+        const uint16_t *const kp = a.ck + piece, *const vp = a.cv + piece;
+        int page = w.page(a, mine);
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true, fresh = true;
+        for (; left > 0; --left) {
+            const AttentionUnit now = w.at;
+            const bool leave = now.tile + 1 == w.tiles || left == 1;
+            const int pg = page;
+            w.advance(a, p);
+            if (left > 1) page = w.page(a, mine);               // the next unit's page, while this one's stage empties
+            if (pg == -2 && lane < 16 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+            // element offset of the row, -1: no such key
+            const long long off = pg == -1 ? -1
+                                           : (long long)max(pg, 0) * a.page_stride +
+                                                 (long long)((unsigned)(now.tile * kAtTile + mine) % (unsigned)a.page_size) * a.token_stride +
+                                                 now.kh * a.head_stride;
+            ok = mbar_wait(&empty[s], ph ^ 1);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            if (cw == 0 && lane == 0) {
+                unit[s] = now;
+                unit[s].leave = leave;
+                unit[s].stop = left == 1;
+                mbar_arrive(&full[s]);
+            }
+            // missing rows become zeros, so that a zero probability times what lies there is zero
+            const uint32_t dst = dst0 + s * STAGE;
+#pragma unroll
+            for (int i = 0; i < 16 / R; ++i) {
+                const long long o = __shfl_sync(0xffffffffu, off, i * R + lane / CH);
+                const long long at = o < 0 ? 0 : o;
+                const int r = i * R + lane / CH;
+                if (piece < hd) {
+                    cp_async16(dst + r * PITCH + at_piece(r, lane % CH), kp + at, o >= 0);
+                    cp_async16(dst + (kAtTile + r) * PITCH + at_piece(r, lane % CH), vp + at, o >= 0);
+                }
+            }
+            if (now.own && p.own_wm == 1 && fresh) {
+                // the item's rows of q come with its first unit (four a warp)
+                for (int r = cw * 4 + lane / CH; r < min(cw * 4 + 4, p.own_rec_rows); r += R) {
+                    const unsigned tok = now.b * a.n_q + (unsigned)r / (unsigned)G, head = now.kh * G + (unsigned)r % (unsigned)G;
+                    if (piece < hd)
+                        cp_async16(smem_u32(smem) + s * STAGE + (2 * kAtTile + r) * PITCH + at_piece(r, lane % CH),
+                                   a.q + (long long)tok * a.ldq + (long long)head * hd + piece, true);
+                }
+            }
+            fresh = leave;
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
+            if (++s == kAtStages) { s = 0; ph ^= 1; }
+        }
+        if (!ok) {                                              // gave up: let what is under way land (bounded) before the memory goes
+            for (int i = 0; i < kAtStages; ++i) mbar_wait(&full[i], ph ^ (i >= s ? 1u : 0u));
+            if (lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
+        }
+        return;
+    }
+
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kAtComputeRegs));
+    const int g = lane >> 2, t = lane & 3, G = a.n_heads / a.n_kv;
+    uint32_t q[DP / 16][4];
+    float o[DP / 8][4];
+    AttentionState st;
+    int own_i[2];
+    bool fresh = true;
+    const float scale = a.scale * 1.4426950408889634f;
+    int s = 0;
+    uint32_t ph = 0;
+    for (;;) {
+        const bool ok = mbar_wait(&full[s], ph);
+        if (!__all_sync(0xffffffffu, ok)) {
+            if (lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
+            return;
+        }
+        const AttentionUnit it = unit[s];
+        if (it.stop == 2) return;
+        const int wm = it.own ? p.own_wm : p.pre_wm, wrow = (wm == 1 ? 0 : wm == 2 ? warp & 1 : warp) * 16;
+        const int base_row = it.own ? it.b * a.n_q * G : 0;     // rows of a key head: token * G + head in group
+        const int row0 = it.rt * 16 * wm, rows = (it.own ? 1 : (int)a.n_seq) * a.n_q * G - row0;
+        const int nrows = rows < 16 * wm ? rows : 16 * wm;
+        const uint32_t ks = smem_u32(smem + s * STAGE);
+        if (fresh) {
+            // q as A fragments, rows g and g + 8 (rows past nrows: whatever, nobody reads what they give)
+            const int r0 = wrow + g, r1 = r0 + 8;
+            const unsigned row_a = base_row + row0 + min(r0, nrows - 1), row_b = base_row + row0 + min(r1, nrows - 1);
+            const unsigned tok_a = row_a / (unsigned)G, tok_b = row_b / (unsigned)G;
+            own_i[0] = it.own ? (int)tok_a - it.b * a.n_q : 0;
+            own_i[1] = it.own ? (int)tok_b - it.b * a.n_q : 0;
+            if (it.own && p.own_wm == 1) {
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k)
+                    ldsm4(q[k], ks + (2 * kAtTile + (lane & 15)) * PITCH + ((k * 2 + (lane >> 4)) ^ (lane & 7)) * 16);
+            } else {
+                const uint16_t *const sa = a.q + (long long)tok_a * a.ldq + (long long)(it.kh * G + (int)(row_a % (unsigned)G)) * hd + 2 * t;
+                const uint16_t *const sb = a.q + (long long)tok_b * a.ldq + (long long)(it.kh * G + (int)(row_b % (unsigned)G)) * hd + 2 * t;
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int d = k * 16 + e * 8;
+                        q[k][2 * e] = d < hd ? *reinterpret_cast<const uint32_t *>(sa + d) : 0u;
+                        q[k][2 * e + 1] = d < hd ? *reinterpret_cast<const uint32_t *>(sb + d) : 0u;
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                st.m[h] = -CUDART_INF_F;
+                st.l[h] = 0.0f;
+            }
+#pragma unroll
+            for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
+        }
+        fresh = it.leave;
+        if (wm == 1) attention_tile<D, DP, 1>(a, it, ks, q, own_i, scale, o, st);
+        else if (wm == 2) attention_tile<D, DP, 2>(a, it, ks, q, own_i, scale, o, st);
+        else attention_tile<D, DP, 4>(a, it, ks, q, own_i, scale, o, st);
+        if (it.leave) {
+            // the CTA's record of the item
+            const int item = it.own ? (it.b * a.n_kv + it.kh) * p.own_rt + it.rt : it.kh * p.pre_rt + it.rt;
+            const long long rec = (long long)(item + cta) * (it.own ? p.own_rec_rows : 16 * wm);
+            float *const ro = reinterpret_cast<float *>(ws + (it.own ? p.off_own_o : p.off_pre_o));
+            float2 *const rml = reinterpret_cast<float2 *>(ws + (it.own ? p.off_own_ml : p.off_pre_ml));
+            float *const ex = reinterpret_cast<float *>(smem + s * STAGE);      // the stage just used: [warp][16][DP]
+            float2 *const exml = reinterpret_cast<float2 *>(ex + 4 * 16 * DP);
+            if (wm < 4) named_bar_sync(1, 128);                 // the warps that share rows have all read the stage
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                st.l[h] = quad_sum(st.l[h]);
+                const int r = wrow + g + h * 8;
+                if (r >= nrows) continue;
+                float *const dst = (wm < 4 ? ex + (warp * 16 + g + h * 8) * DP : ro + (rec + r) * hd) + 2 * t;
+#pragma unroll
+                for (int n = 0; n < DP / 8; ++n)
+                    if (n * 8 < hd) *reinterpret_cast<float2 *>(dst + n * 8) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+                if (t == 0) (wm < 4 ? exml[warp * 16 + g + h * 8] : rml[rec + r]) = make_float2(st.m[h], st.l[h]);
+            }
+            if (wm < 4) {
+                named_bar_sync(1, 128);
+                for (int i = tid; i < nrows * (hd / 4); i += 128) {
+                    const int r = i / (hd / 4), c = i % (hd / 4) * 4;
+                    float m = -CUDART_INF_F, l = 0.0f;
+                    for (int k = r / 16; k < 4; k += wm) m = fmaxf(m, exml[k * 16 + r % 16].x);
+                    const float base = m == -CUDART_INF_F ? 0.0f : m;
+                    float4 v = make_float4(0, 0, 0, 0);
+                    for (int k = r / 16; k < 4; k += wm) {
+                        const float2 x = exml[k * 16 + r % 16];
+                        const float w = exp2_fast(x.x - base);
+                        const float4 y = *reinterpret_cast<const float4 *>(ex + (k * 16 + r % 16) * DP + c);
+                        l += w * x.y;
+                        v.x += w * y.x; v.y += w * y.y; v.z += w * y.z; v.w += w * y.w;
+                    }
+                    *reinterpret_cast<float4 *>(ro + (rec + r) * hd + c) = v;
+                    if (c == 0) rml[rec + r] = make_float2(m, l);
+                }
+            }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[s]);
+        if (++s == kAtStages) { s = 0; ph ^= 1; }
+        if (it.stop) return;
+    }
+}
+
+// One CTA per row (token, head).  A row has a handful of records in the usual case and some hundreds when one key head's
+// keys are spread over the whole device, so all warps look at all (m, l), then share the outputs, eight loads under way.
+template <class D>
+__global__ void __launch_bounds__(128)
+attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsigned char *__restrict__ ws)
+{
+    __shared__ float part[4][128], part_l[4];
+    pdl_begin();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.n_heads / a.n_kv, hd = a.head_dim;
+    const unsigned r = blockIdx.x, tok = r / (unsigned)a.n_heads, h = r % (unsigned)a.n_heads, kh = h / (unsigned)G, b = tok / (unsigned)a.n_q;
+    const long long *start = reinterpret_cast<const long long *>(ws);
+    const long long total = start[a.n_seq], own0 = start[b], own1 = start[b + 1];
+    const AttentionDeal deal(total, p.ctas);
+    const int tiles = (int)div_units(own1 - own0, a.n_kv * p.own_rt);
+    // the rows of this one's records: the prefix item's, then the own item's
+    long long pre0 = 0, rec0 = 0;
+    int n_pre = 0, n_all = 0;
+    const int pre_step = 16 * p.pre_wm, own_step = p.own_rec_rows;
+    if (p.pre_tiles) {
+        const unsigned row = tok * G + h % (unsigned)G, in = row % (unsigned)pre_step;
+        const long long item = (long long)kh * p.pre_rt + row / (unsigned)pre_step;
+        const int c0 = deal.cta_of(item * p.pre_tiles);
+        n_pre = deal.cta_of((item + 1) * p.pre_tiles - 1) - c0 + 1;
+        pre0 = (item + c0) * pre_step + in;
+    }
+    n_all = n_pre;
+    if (tiles) {
+        const unsigned row = tok % (unsigned)a.n_q * G + h % (unsigned)G, step = 16 * p.own_wm;
+        const int within = kh * p.own_rt + row / step;
+        const long long u = own0 + (long long)within * tiles;
+        const int c0 = deal.cta_of(u);
+        n_all += deal.cta_of(u + tiles - 1) - c0 + 1;
+        rec0 = ((long long)b * a.n_kv * p.own_rt + within + c0) * own_step + row % step;
+    }
+    const float *const pre_o = reinterpret_cast<const float *>(ws + p.off_pre_o), *const own_o = reinterpret_cast<const float *>(ws + p.off_own_o);
+    const float2 *const pre_ml = reinterpret_cast<const float2 *>(ws + p.off_pre_ml), *const own_ml = reinterpret_cast<const float2 *>(ws + p.off_own_ml);
+    auto ml = [&](int i) { return i < n_pre ? pre_ml[pre0 + (long long)i * pre_step] : own_ml[rec0 + (long long)(i - n_pre) * own_step]; };
+    auto out = [&](int i) { return i < n_pre ? pre_o + (pre0 + (long long)i * pre_step) * hd : own_o + (rec0 + (long long)(i - n_pre) * own_step) * hd; };
+    float m = -CUDART_INF_F;
+    for (int i = lane; i < n_all; i += 32) m = fmaxf(m, ml(i).x);
+    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+    const float base = m == -CUDART_INF_F ? 0.0f : m;
+    constexpr int U = 8;
+    float l = 0.0f;
+    float4 o = make_float4(0, 0, 0, 0);
+    const bool in = lane * 4 < hd;
+    for (int i0 = warp * U; i0 < n_all; i0 += 4 * U) {
+        float4 v[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            v[j] = in && i0 + j < n_all ? *reinterpret_cast<const float4 *>(out(i0 + j) + lane * 4) : make_float4(0, 0, 0, 0);
+        float w = 0.0f, wl = 0.0f;
+        if (lane < U && i0 + lane < n_all) {
+            const float2 x = ml(i0 + lane);
+            w = exp2_fast(x.x - base);
+            wl = w * x.y;
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const float f = __shfl_sync(0xffffffffu, w, j);
+            l += __shfl_sync(0xffffffffu, wl, j);
+            if (i0 + j < n_all) { o.x += f * v[j].x; o.y += f * v[j].y; o.z += f * v[j].z; o.w += f * v[j].w; }
+        }
+    }
+    if (n_all > U) {
+        if (in) *reinterpret_cast<float4 *>(&part[warp][lane * 4]) = o;
+        if (lane == 0) part_l[warp] = l;
+        __syncthreads();
+        l = 0.0f;
+        o = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            l += part_l[k];
+            if (in) {
+                const float4 v = *reinterpret_cast<const float4 *>(&part[k][lane * 4]);
+                o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+            }
+        }
+    }
+    if (warp == 0 && in) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;          // no key at all: zeros
-        *reinterpret_cast<uint2 *>(a.out + tok * a.ldo + (r % a.n_heads) * a.head_dim + lane * 4) =
+        *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.ldo + (long long)h * hd + lane * 4) =
             make_uint2(D::encode2(o.x * inv, o.y * inv), D::encode2(o.z * inv, o.w * inv));
     }
 }
 
 template <class D, int DP>
-static aweq_status items_launch(const AttentionArgs &a, const AttentionPlan &p, float *o_part, float2 *ml_part, cudaStream_t stream)
+static aweq_status units_launch(const AttentionArgs &a, const AttentionPlan &p, unsigned char *ws, cudaStream_t stream)
 {
-    constexpr size_t smem = attention_smem<DP>();
-    static_assert(4 * 16 * 2 * 4 + 4 * 16 * (DP + 8) * 4 <= smem, "the join reuses the stages");
-    AWEQ_CUDA_OK(cudaFuncSetAttribute(attention_items_kernel<D, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    AWEQ_LAUNCH((attention_items_kernel<D, DP>), dim3((unsigned)(p.pre_items + p.own_items)), dim3(kAtThreads), smem, stream, a, p,
-                o_part, ml_part);
+    constexpr int smem = kAtStages * attention_stage_bytes<DP>();
+    AWEQ_CUDA_OK(cudaFuncSetAttribute(attention_units_kernel<D, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    AWEQ_LAUNCH((attention_units_kernel<D, DP>), dim3((unsigned)p.ctas), dim3(kAtThreads), smem, stream, a, p, ws);
     return AWEQ_OK;
 }
 
 template <class D>
-static aweq_status attention_launch(const AttentionArgs &a, void *ws, cudaStream_t stream)
+static aweq_status attention_launch(const AttentionArgs &a, unsigned char *ws, cudaStream_t stream)
 {
     const AttentionPlan p = attention_plan(a.prefix_len, a.max_own, a.n_seq, a.n_q, a.n_heads, a.n_kv, a.head_dim);
-    if (p.pre_items + p.own_items > 0x7fffffffll) return AWEQ_ERR_SHAPE;
-    float *o_part = reinterpret_cast<float *>(ws);
-    float2 *ml_part = reinterpret_cast<float2 *>(reinterpret_cast<char *>(ws) + p.off_ml);
-    if (p.pre_items + p.own_items > 0) {
-        const aweq_status rc = p.dp == 64 ? items_launch<D, 64>(a, p, o_part, ml_part, stream)
-                               : p.dp == 96 ? items_launch<D, 96>(a, p, o_part, ml_part, stream)
-                                            : items_launch<D, 128>(a, p, o_part, ml_part, stream);
-        if (rc != AWEQ_OK) return rc;
-    }
-    AWEQ_LAUNCH(attention_join_kernel<D>, dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, stream, a, p, (const float *)o_part,
-                (const float2 *)ml_part);
+    const aweq_status rc = p.dp == 64   ? units_launch<D, 64>(a, p, ws, stream)
+                           : p.dp == 96 ? units_launch<D, 96>(a, p, ws, stream)
+                                        : units_launch<D, 128>(a, p, ws, stream);
+    if (rc != AWEQ_OK) return rc;
+    AWEQ_LAUNCH(attention_join_kernel<D>, dim3((unsigned)p.rows), dim3(128), 0, stream, a, p, (const unsigned char *)ws);
     return AWEQ_OK;
 }
 
 aweq_status run_prefix_attention(const AttentionArgs &a, aweq_dtype dt, void *ws, cudaStream_t stream)
 {
-    return dt == AWEQ_F16 ? attention_launch<F16>(a, ws, stream) : attention_launch<BF16>(a, ws, stream);
+    unsigned char *const w = reinterpret_cast<unsigned char *>(ws);
+    return dt == AWEQ_F16 ? attention_launch<F16>(a, w, stream) : attention_launch<BF16>(a, w, stream);
 }
 
 }  // namespace aweq

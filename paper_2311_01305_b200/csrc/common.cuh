@@ -88,6 +88,15 @@ __device__ __forceinline__ void pdl_begin()
 }
 
 // ------------------------------------------------------------------ 16-bit traits
+// whether one of eight 16-bit elements has all exponent bits (of `mask`) set
+__device__ __forceinline__ bool has_exponent(const uint4 &v, uint32_t mask)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) any |= (w[i] & mask) == mask || (w[i] >> 16 & mask) == mask;
+    return any;
+}
 struct F16 {
     using T2 = __half2;
     static __device__ __forceinline__ T2 from_bits(uint32_t u) { return *reinterpret_cast<T2 *>(&u); }
@@ -105,6 +114,7 @@ struct F16 {
         return r;
     }
     static __device__ __forceinline__ float one(uint16_t b) { return __half2float(__ushort_as_half(b)); }
+    static __device__ __forceinline__ bool any_nonfinite(const uint4 &v) { return has_exponent(v, 0x7C00u); }
     static __device__ __forceinline__ uint16_t encode(float f) { return __half_as_ushort(__float2half_rn(f)); }
     static __device__ __forceinline__ uint32_t encode2(float lo, float hi)
     {
@@ -123,6 +133,7 @@ struct BF16 {
         return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
     }
     static __device__ __forceinline__ float one(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+    static __device__ __forceinline__ bool any_nonfinite(const uint4 &v) { return has_exponent(v, 0x7F80u); }
     static __device__ __forceinline__ uint16_t encode(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
     static __device__ __forceinline__ uint32_t encode2(float lo, float hi)
     {
