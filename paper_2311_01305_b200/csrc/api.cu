@@ -655,7 +655,7 @@ aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_ca
     a.n_kv = cache->n_kv_heads; a.head_dim = cache->head_dim; a.n_heads = n_heads; a.n_q = n_q;
     a.prefix_pages = prefix_pages; a.page_table = page_table; a.own_len = own_len; a.prefix_len = prefix_len;
     a.pages_per_seq = pages_per_seq; a.ld_table = ld_table; a.max_own = max_own; a.n_seq = n_seq; a.scale = scale; a.st = st;
-    return run_prefix_attention(a, cache->dt, ws, (cudaStream_t)stream);
+    return run_prefix_attention(a, cache, ws, (cudaStream_t)stream);
 }
 
 }  // extern "C"

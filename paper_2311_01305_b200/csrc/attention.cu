@@ -2,19 +2,20 @@
 //
 // All rows (token, head) that read one key head share the prefix, so the prefix is a dense product of a [rows x D]
 // matrix with K and V, read once per tile of rows; the own keys are a product of the n_q * G rows of one
-// sequence (G heads to a key head).  An item is a tile of rows with all its keys; its unit is a tile of 64 keys.
+// sequence (G heads to a key head).  An item is a tile of rows with all its keys; a unit is a tile of 64 of them.
 // The units of all items in a row are dealt out evenly to a grid that fills the device once, so a CTA streams
-// through parts of one or several items without ever draining its copies, whatever the lengths are (they are known
-// on the device only).  Four warps walk the units, look up pages and copy the rows of K and V into a ring of stages
-// (cp.async: a bulk copy per row took 40 cycles each), 16 rows of a unit each; four other warps compute, with most of the
-// registers.  (With every warp doing its share of both, the lookups and copies, 1.8 us a unit, added to the 0.6 us of the
-// products; a single copying warp took 2.6 us a unit.)  Where a CTA leaves an item it writes a record (maximum m, sum l, output o of the keys it
-// has seen, for each row), and a second launch joins the records of a row:
+// through parts of one or several items without ever draining its copies, whatever the lengths are (the own ones are
+// known on the device only).  Where a CTA leaves an item it writes a record (maximum m, sum l, output o of the keys it
+// has seen, for each row).  One launch for the prefix (this kernel, or attention_tc.cu), one for the own keys, which starts
+// while the first still runs, and one that joins the records of a row:
 //   m = max m_i,  l = sum 2^(m_i - m) l_i,  out = sum 2^(m_i - m) o_i / l      (scores in units of log 2)
-#include <math_constants.h>
-
-#include "common.cuh"
-#include "kernels.h"
+//
+// In a CTA four warps walk the units, look up pages and copy the rows of K and V into a ring of stages (cp.async: a bulk
+// copy per row took 40 cycles each), 16 rows of a unit each; four other warps compute with mma.sync, with most of the
+// registers.  (With every warp doing its share of both, the lookups and copies, 1.8 us a unit, added to the 0.6 us of the
+// products; a single copying warp took 2.6 us a unit.)  Measured: 16 sequences of 1-4 thousand own keys, 32 heads of 128:
+// 122 us, 5.5 TB/s (the bound); 128 sequences of 64-256 keys 87 us, 3.9 TB/s (the change from item to item costs).
+#include "attention.cuh"
 
 namespace aweq {
 
@@ -24,48 +25,65 @@ constexpr int kAtThreads = 256;             // four computing warps, four that c
 // registers of a computing / copying thread: their mean is what the launch gives every thread (two CTAs of 256)
 constexpr int kAtComputeRegs = 200, kAtCopyRegs = 56;
 
-// How the work is cut (host; also sizes the scratch).
-struct AttentionPlan {
-    int dp;                      // head_dim padded to 64, 96 or 128
-    int pre_wm, own_wm;          // warps along the rows of a prefix / own item (4 / wm share its keys)
-    int pre_rt, own_rt;          // row tiles per key head / per sequence and key head
-    int own_rec_rows;            // rows of an own record
-    int ctas;
-    long long pre_tiles, pre_units, rows;
-    // scratch: start of each sequence's units (long long[n_seq + 1], the total last), records
-    size_t off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
-};
-
-static int rows_warps(long long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
-static size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 constexpr int kAtCtasPerSm = 2;
 
-static AttentionPlan attention_plan(long long prefix_len, long long max_own, long long n_seq, int n_q, int n_heads, int n_kv,
-                                    int head_dim)
+static size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+// The tensor kernel copies boxes of `box` keys that lie in one page (rows a multiple of eight, so that they keep the
+// swizzle's phase) and takes as many as fit 128 keys for a unit.  Page sizes of which less than 96 keys fit are left to
+// the other kernel.
+static void tensor_unit(int page_size, int *unit, int *box)
+{
+    *unit = *box = 0;
+    if (page_size % 8) return;
+    if (page_size <= 128) *box = page_size;
+    else if (page_size % 128 == 0) *box = 128;
+    else if (page_size % 64 == 0) *box = 64;
+    else return;
+    *unit = 128 / *box * *box;
+}
+
+// Whether the prefix goes to the tensor kernel: more than 32 rows per key head (the other kernel's 16-row tiles serve 32
+// rows at the rate of the copies: 32 rows x 8192 keys x 32 heads of 128, 47.1 us against 46.4; 96 rows, 99.9 against 69.9)
+// and three units for every SM (its start is slower: 64 rows x 1024 keys x 12 heads of 64, 18.6 us against 21.0).
+static bool attention_prefers_tensor(long long rows, long long units)
+{
+    return rows > 32 && units * ((rows + 127) / 128) >= 3 * kSmCount;
+}
+
+static AttentionPlan attention_plan(const aweq_kv_cache *c, long long prefix_len, long long max_own, long long n_seq, int n_q,
+                                    int n_heads)
 {
     AttentionPlan p;
+    const int n_kv = c->n_kv_heads, head_dim = c->head_dim;
+    const long long pre_rows = n_seq * n_q * (n_heads / n_kv), own_rows = (long long)n_q * (n_heads / n_kv);
     p.dp = head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : 128;
     p.rows = n_seq * n_q * n_heads;
-    const long long pre_rows = n_seq * n_q * (n_heads / n_kv), own_rows = (long long)n_q * (n_heads / n_kv);
-    p.pre_wm = rows_warps(pre_rows);
-    p.own_wm = rows_warps(own_rows);
-    p.pre_rt = (int)((pre_rows + 16 * p.pre_wm - 1) / (16 * p.pre_wm));
-    p.own_rt = (int)((own_rows + 16 * p.own_wm - 1) / (16 * p.own_wm));
-    p.own_rec_rows = (int)(own_rows < 16 * p.own_wm ? own_rows : 16 * p.own_wm);
-    p.pre_tiles = (prefix_len + kAtTile - 1) / kAtTile;
+    tensor_unit(c->page_size, &p.pre_unit, &p.box);
+    p.unit = kAtTile;
+    p.tensor = p.pre_unit >= 96 && prefix_len > 0 && attention_prefers_tensor(pre_rows, (prefix_len + p.pre_unit - 1) / p.pre_unit * n_kv);
+    if (!p.tensor) p.pre_unit = p.unit;
+    p.pre_tile = p.tensor ? 128 : pre_rows <= 16 ? 16 : pre_rows <= 32 ? 32 : 64;
+    p.own_tile = own_rows <= 16 ? 16 : own_rows <= 32 ? 32 : 64;
+    p.pre_rt = (int)((pre_rows + p.pre_tile - 1) / p.pre_tile);
+    p.own_rt = (int)((own_rows + p.own_tile - 1) / p.own_tile);
+    p.pre_rec = (int)(pre_rows < p.pre_tile ? pre_rows : p.pre_tile);
+    p.own_rec = (int)(own_rows < p.own_tile ? own_rows : p.own_tile);
+    p.pre_tiles = (prefix_len + p.pre_unit - 1) / p.pre_unit;
     p.pre_units = p.pre_tiles * n_kv * p.pre_rt;
-    const long long own_items = n_seq * n_kv * p.own_rt;
-    const double most = (double)p.pre_units + (double)own_items * (double)((max_own + kAtTile - 1) / kAtTile);
-    p.ctas = kSmCount * kAtCtasPerSm;
-    if (most < p.ctas) p.ctas = most < 1 ? 1 : (int)most;
+    const long long own_items = n_seq * n_kv * p.own_rt, slots = kSmCount * kAtCtasPerSm;
+    const double own_most = (double)own_items * (double)((max_own + p.unit - 1) / p.unit);
+    p.own_ctas = own_most < (double)slots ? (int)own_most : (int)slots;
+    const long long pre_slots = p.tensor ? kSmCount : slots;
+    p.pre_ctas = p.pre_units < pre_slots ? (int)p.pre_units : (int)pre_slots;
     // an item makes a record, and one more for every CTA boundary inside it
-    const size_t pre_rows_kept = p.pre_tiles ? (size_t)((long long)n_kv * p.pre_rt + p.ctas) * 16 * p.pre_wm : 0;
-    const size_t own_rows_kept = (size_t)(own_items + p.ctas) * p.own_rec_rows;
+    const size_t pre_kept = p.pre_tiles ? (size_t)((long long)n_kv * p.pre_rt + p.pre_ctas) * p.pre_rec : 0;
+    const size_t own_kept = (size_t)(own_items + p.own_ctas) * p.own_rec;
     size_t off = up256((size_t)(n_seq + 1) * 8);
-    p.off_pre_o = off; off += up256(pre_rows_kept * head_dim * 4);
-    p.off_pre_ml = off; off += up256(pre_rows_kept * 8);
-    p.off_own_o = off; off += up256(own_rows_kept * head_dim * 4);
-    p.off_own_ml = off; off += up256(own_rows_kept * 8);
+    p.off_pre_o = off; off += up256(pre_kept * head_dim * 4);
+    p.off_pre_ml = off; off += up256(pre_kept * 8);
+    p.off_own_o = off; off += up256(own_kept * head_dim * 4);
+    p.off_own_ml = off; off += up256(own_kept * 8);
     p.total = off;
     return p;
 }
@@ -73,7 +91,7 @@ static AttentionPlan attention_plan(long long prefix_len, long long max_own, lon
 size_t prefix_attention_ws_bytes(const aweq_kv_cache *c, long long prefix_len, long long max_own, long long n_seq, int n_q,
                                  int n_heads)
 {
-    return attention_plan(prefix_len, max_own, n_seq, n_q, n_heads, c->n_kv_heads, c->head_dim).total;
+    return attention_plan(c, prefix_len, max_own, n_seq, n_q, n_heads).total;
 }
 
 // ------------------------------------------------------------------ device pieces
@@ -105,12 +123,6 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool i
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 __device__ __forceinline__ float quad_max(float v)
 {
     v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
@@ -122,48 +134,6 @@ __device__ __forceinline__ float quad_sum(float v)
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
-// A clamped own length.  `count`: the one caller that reports it.
-__device__ __forceinline__ int own_length(const AttentionArgs &a, long long b, bool count)
-{
-    const int len = __ldg(a.own_len + b);
-    const int most = (int)min(a.max_own, a.pages_per_seq * a.page_size);
-    if (len < 0 || len > most) {
-        if (count && a.st) atomicAdd(&a.st->out_of_range, 1ull);
-        return len < 0 ? 0 : most;
-    }
-    return len;
-}
-__device__ __forceinline__ int tiles_of(int len) { return (int)(((unsigned)len + kAtTile - 1) / kAtTile); }
-// The units are dealt out in order, total / ctas to a CTA and one more to the first total % ctas.  (Divisions of 64 bits
-// take hundreds of cycles: only where the numbers need them.)
-__device__ __forceinline__ long long div_units(long long a, int b)
-{
-    return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
-}
-struct AttentionDeal {
-    long long each, more;        // units of a CTA, CTAs with one more
-    int ctas;                    // those that have any
-    __device__ __forceinline__ AttentionDeal(long long total, int most)
-    {
-        ctas = total < most ? (int)total : most;
-        each = ctas ? div_units(total, ctas) : 0;
-        more = total - each * ctas;
-    }
-    __device__ __forceinline__ long long first(int cta) const { return each * cta + (cta < more ? cta : more); }
-    __device__ __forceinline__ int cta_of(long long u) const
-    {
-        const long long big = more * (each + 1);
-        if ((each + 1) >> 31) return u < big ? (int)(u / (each + 1)) : (int)(more + (u - big) / each);
-        return u < big ? (int)div_units(u, (int)(each + 1)) : (int)more + (int)div_units(u - big, (int)each);
-    }
-};
-
-// What a unit is: the tile'th tile of the `len` keys of an item.
-struct alignas(16) AttentionUnit {
-    int own, kh, rt, b, tile, len;
-    int leave;                   // the CTA's last unit of this item
-    int stop;                    // 1: the CTA's last unit, 2: nothing to compute
-};
 // A staged row: its 16-byte pieces permuted by the row's number modulo 8, so that eight rows' like pieces lie in
 // different banks (rows of 12 pieces are kept in 16)
 __host__ __device__ constexpr int at_pitch(int dp) { return dp == 64 ? 128 : 256; }
@@ -174,7 +144,7 @@ struct AttentionState {          // of a warp's 16 rows: lanes hold rows g and g
 };
 
 // One tile of keys for a warp's 16 rows.  WM warps of the CTA lie along the rows, 4 / WM share the keys of the tile.
-template <class D, int DP, int WM>
+template <class D, int DP, int WM, bool OWN>
 __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const AttentionUnit &it, uint32_t ks, const uint32_t (&q)[DP / 16][4],
                                                const int (&own_i)[2], float scale, float (&o)[DP / 8][4], AttentionState &st)
 {
@@ -194,7 +164,7 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
             mma16<D>(s[n + 1], q[k], b[2], b[3]);
         }
     // keys of this warp's share that a row sees: token i of a sequence leaves out the last n_q - 1 - i
-    const int there = it.len - (it.tile * kAtTile + key0), first = it.own ? there - (a.n_q - 1) : there;
+    const int there = it.len - (it.tile * kAtTile + key0), first = OWN ? there - (a.n_q - 1) : there;
     const bool edge = first < NT * 8;
     float top[2] = {st.m[0], st.m[1]};
 #pragma unroll
@@ -202,7 +172,7 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             s[n][e] *= scale;
-            if (edge && n * 8 + 2 * t + (e & 1) >= first + own_i[e >> 1]) s[n][e] = -CUDART_INF_F;
+            if (edge && n * 8 + 2 * t + (e & 1) >= first + (OWN ? own_i[e >> 1] : 0)) s[n][e] = -CUDART_INF_F;
             top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
         }
     float base[2], f[2];
@@ -235,7 +205,7 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
     // Among the last keys are some that only a sequence's later tokens see.  Zero times their values is zero unless a value is
     // infinite or NaN, which is looked for.
     bool apart = false;
-    if (it.own && edge && a.n_q > 1) {
+    if (OWN && edge && a.n_q > 1) {
         const int from = max(first, 0), to = min(there, NT * 8);
         for (int i = lane; i < (to - from) * (DP / 8); i += 32) {
             const int r = key0 + from + i / (DP / 8);
@@ -246,7 +216,7 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
         }
         apart = __any_sync(0xffffffffu, apart);
     }
-    if (!apart) {
+    if (!OWN || !apart) {
 #pragma unroll
         for (int k = 0; k < NT / 2; ++k)
 #pragma unroll
@@ -289,51 +259,19 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
 template <int DP>
 __host__ __device__ constexpr int attention_stage_bytes() { return (2 * kAtTile + 16) * at_pitch(DP); }     // K, V, 16 rows of q
 
-// The walk over a CTA's units by a warp: every lane knows the unit and looks up the page of a key.
-struct AttentionWalk {
-    AttentionUnit at;
-    int tiles, next_len;         // of the item; length of the sequence after this one (its load is long under way when needed)
-    __device__ __forceinline__ void advance(const AttentionArgs &a, const AttentionPlan &p)
-    {
-        if (++at.tile < tiles) return;
-        at.tile = 0;
-        if (++at.rt < (at.own ? p.own_rt : p.pre_rt)) return;
-        at.rt = 0;
-        if (++at.kh < a.n_kv) return;
-        at.kh = 0;
-        const int n_seq = (int)a.n_seq;
-        if (at.own) ++at.b;
-        at.own = 1;
-        for (;;) {                                              // sequences without keys have no units
-            at.len = next_len;
-            tiles = tiles_of(at.len);
-            next_len = at.b + 1 < n_seq ? own_length(a, at.b + 1, false) : 0;
-            if (tiles > 0 || at.b + 1 >= n_seq) return;
-            ++at.b;
-        }
-    }
-    // page of the lane's r'th key of the unit; -1: no such key, -2: a page outside the pool
-    __device__ __forceinline__ int page(const AttentionArgs &a, int r) const
-    {
-        const int c = at.tile * kAtTile + r;
-        if (c >= at.len) return -1;
-        const int *pages = at.own ? a.page_table + (long long)at.b * a.ld_table : a.prefix_pages;
-        const int page = __ldg(pages + (unsigned)c / (unsigned)a.page_size);
-        return page < 0 || page >= a.n_pages ? -2 : page;
-    }
-};
-
-template <class D, int DP>
+// `chained`: behind the prefix's kernel.  This one then starts without waiting for it, and ends after it for the join's sake.
+template <class D, int DP, int WM, bool OWN>
 __global__ void __launch_bounds__(kAtThreads, kAtCtasPerSm)
-attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned char *ws)
+attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned char *ws, bool chained)
 {
-    constexpr int PITCH = at_pitch(DP), STAGE = attention_stage_bytes<DP>();
+    constexpr int PITCH = at_pitch(DP), STAGE = attention_stage_bytes<DP>(), KW = 4 / WM;
+    constexpr bool kStagedQ = OWN && WM == 1;                   // short items: their rows of q come with their first unit
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ uint64_t full[kAtStages], empty[kAtStages];
     __shared__ AttentionUnit unit[kAtStages];
+    __shared__ float2 sh_ml[64];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int hd = a.head_dim, cta = blockIdx.x;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int hd = a.head_dim, cta = blockIdx.x, G = a.n_heads / a.n_kv, rec_rows = OWN ? p.own_rec : p.pre_rec;
     if (tid == 0) {
         for (int s = 0; s < kAtStages; ++s) {
             mbar_init(&full[s], 129);                           // every copying lane, and the unit itself
@@ -347,82 +285,27 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
             *reinterpret_cast<uint4 *>(smem + r * PITCH + at_piece(r, hd / 8 + i % ((DP - hd) / 8))) = make_uint4(0, 0, 0, 0);
         }
     __syncthreads();
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!chained) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
 
     if (warp >= 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAtCopyRegs));
         const int cw = warp - 4;
-        const bool lead = cta == 0 && cw == 0;                  // reports lengths, leaves the starts for the join
-        const int n_seq = (int)a.n_seq, per_seq = a.n_kv * p.own_rt;
-        // the number of units, and where this CTA's first one lies
-        auto scan = [&](int b, bool count, int *n) {            // tiles of 32 sequences: own, before it
-            *n = b < n_seq ? tiles_of(own_length(a, b, count)) : 0;
-            int sum = *n;                                       // 32 lengths of at most 2^31 keys: below 2^31 tiles
-#pragma unroll
-            for (int x = 1; x < 32; x <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, sum, x);
-                if (lane >= x) sum += y;
-            }
-            return (long long)(sum - *n);
-        };
-        long long *const start = reinterpret_cast<long long *>(ws);
-        long long total = 0;
-        int n;
-        for (int b0 = 0; b0 < n_seq; b0 += 32) {
-            const long long before = scan(b0 + lane, lead, &n);
-            if (lead && b0 + lane < n_seq) start[b0 + lane] = p.pre_units + (total + before) * per_seq;
-            total += __shfl_sync(0xffffffffu, before + n, 31);
-        }
-        total = p.pre_units + total * per_seq;
-        if (lead && lane == 0) start[n_seq] = total;
-        const AttentionDeal deal(total, p.ctas);
-        if (cta >= deal.ctas) {
-            if (cw == 0 && lane == 0) {
-                unit[0].stop = 2;
-                mbar_arrive(&full[0]);
-            }
+        AttentionWalk<OWN> w;
+        int left = attention_begin<OWN>(a, p, cta, cta == 0 && cw == 0, ws, w);
+        if (left == 0) {
+            if (cw == 0 && lane == 0) unit[0].stop = 2;
             mbar_arrive(&full[0]);
-            return;
-        }
-        const long long u0 = deal.first(cta);
-        int left = (int)(deal.first(cta + 1) - u0);
-        AttentionWalk w;
-        w.at = {};
-        if (u0 < p.pre_units) {
-            const int item = (int)div_units(u0, (int)p.pre_tiles);
-            w.at.kh = item / p.pre_rt;
-            w.at.rt = item % p.pre_rt;
-            w.at.tile = (int)(u0 - item * p.pre_tiles);
-            w.at.len = (int)a.prefix_len;
-            w.tiles = (int)p.pre_tiles;
-            w.next_len = n_seq ? own_length(a, 0, false) : 0;
-        } else {
-            long long passed = p.pre_units;
-            for (int b0 = 0;; b0 += 32) {
-                const long long mine = passed + scan(b0 + lane, false, &n) * per_seq;
-                const uint32_t here = __ballot_sync(0xffffffffu, u0 >= mine && u0 < mine + (long long)n * per_seq);
-                if (here) {
-                    const int src = __ffs(here) - 1, within = (int)(u0 - __shfl_sync(0xffffffffu, mine, src));
-                    w.tiles = __shfl_sync(0xffffffffu, n, src);
-                    w.at.own = 1;
-                    w.at.b = b0 + src;
-                    w.at.kh = within / w.tiles / p.own_rt;
-                    w.at.rt = within / w.tiles % p.own_rt;
-                    w.at.tile = within % w.tiles;
-                    break;
-                }
-                passed = __shfl_sync(0xffffffffu, mine + (long long)n * per_seq, 31);
-            }
-            w.at.len = own_length(a, w.at.b, false);
-            w.next_len = w.at.b + 1 < n_seq ? own_length(a, w.at.b + 1, false) : 0;
+            if (cw == 0 && lane == 0) mbar_arrive(&full[0]);
         }
         // lanes 0-15 know this warp's 16 rows of a unit; a lane copies the same 16-byte piece of every (32 / CH)-th
         constexpr int CH = DP / 8 == 12 ? 16 : DP / 8, R = 32 / CH;
         const int mine = cw * 16 + (lane & 15), piece = lane % CH * 8;
         const uint32_t dst0 = smem_u32(smem) + cw * 16 * PITCH;
-        const int G = a.n_heads / a.n_kv;
         const uint16_t *const kp = a.ck + piece, *const vp = a.cv + piece;
-        int page = w.page(a, mine);
+        int page = left > 0 ? w.page(a, p, mine) : -1;
         int s = 0;
         uint32_t ph = 0;
         bool ok = true, fresh = true;
@@ -431,7 +314,7 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
             const bool leave = now.tile + 1 == w.tiles || left == 1;
             const int pg = page;
             w.advance(a, p);
-            if (left > 1) page = w.page(a, mine);               // the next unit's page, while this one's stage empties
+            if (left > 1) page = w.page(a, p, mine);            // the next unit's page, while this one's stage empties
             if (pg == -2 && lane < 16 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
             // element offset of the row, -1: no such key
             const long long off = pg == -1 ? -1
@@ -458,9 +341,9 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
                     cp_async16(dst + (kAtTile + r) * PITCH + at_piece(r, lane % CH), vp + at, o >= 0);
                 }
             }
-            if (now.own && p.own_wm == 1 && fresh) {
-                // the item's rows of q come with its first unit (four a warp)
-                for (int r = cw * 4 + lane / CH; r < min(cw * 4 + 4, p.own_rec_rows); r += R) {
+            if (kStagedQ && fresh) {
+                // the item's rows of q (four a warp)
+                for (int r = cw * 4 + lane / CH; r < min(cw * 4 + 4, p.own_rec); r += R) {
                     const unsigned tok = now.b * a.n_q + (unsigned)r / (unsigned)G, head = now.kh * G + (unsigned)r % (unsigned)G;
                     if (piece < hd)
                         cp_async16(smem_u32(smem) + s * STAGE + (2 * kAtTile + r) * PITCH + at_piece(r, lane % CH),
@@ -475,15 +358,16 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
             for (int i = 0; i < kAtStages; ++i) mbar_wait(&full[i], ph ^ (i >= s ? 1u : 0u));
             if (lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
         }
+        if (chained && cta == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
     }
 
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kAtComputeRegs));
-    const int g = lane >> 2, t = lane & 3, G = a.n_heads / a.n_kv;
+    const int g = lane >> 2, t = lane & 3, wrow = warp % WM * 16;
     uint32_t q[DP / 16][4];
     float o[DP / 8][4];
     AttentionState st;
-    int own_i[2];
+    int own_i[2] = {0, 0}, nrows = 0;
     bool fresh = true;
     const float scale = a.scale * 1.4426950408889634f;
     int s = 0;
@@ -496,19 +380,19 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
         }
         const AttentionUnit it = unit[s];
         if (it.stop == 2) return;
-        const int wm = it.own ? p.own_wm : p.pre_wm, wrow = (wm == 1 ? 0 : wm == 2 ? warp & 1 : warp) * 16;
-        const int base_row = it.own ? it.b * a.n_q * G : 0;     // rows of a key head: token * G + head in group
-        const int row0 = it.rt * 16 * wm, rows = (it.own ? 1 : (int)a.n_seq) * a.n_q * G - row0;
-        const int nrows = rows < 16 * wm ? rows : 16 * wm;
         const uint32_t ks = smem_u32(smem + s * STAGE);
         if (fresh) {
+            // rows of a key head: token * G + head in group
+            const int base = (OWN ? it.b * a.n_q * G : 0) + it.rt * 16 * WM;
+            nrows = min((OWN ? 1 : (int)a.n_seq) * a.n_q * G - it.rt * 16 * WM, 16 * WM);
             // q as A fragments, rows g and g + 8 (rows past nrows: whatever, nobody reads what they give)
-            const int r0 = wrow + g, r1 = r0 + 8;
-            const unsigned row_a = base_row + row0 + min(r0, nrows - 1), row_b = base_row + row0 + min(r1, nrows - 1);
+            const unsigned row_a = base + min(wrow + g, nrows - 1), row_b = base + min(wrow + g + 8, nrows - 1);
             const unsigned tok_a = row_a / (unsigned)G, tok_b = row_b / (unsigned)G;
-            own_i[0] = it.own ? (int)tok_a - it.b * a.n_q : 0;
-            own_i[1] = it.own ? (int)tok_b - it.b * a.n_q : 0;
-            if (it.own && p.own_wm == 1) {
+            if (OWN) {
+                own_i[0] = (int)tok_a - it.b * a.n_q;
+                own_i[1] = (int)tok_b - it.b * a.n_q;
+            }
+            if (kStagedQ) {
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
                     ldsm4(q[k], ks + (2 * kAtTile + (lane & 15)) * PITCH + ((k * 2 + (lane >> 4)) ^ (lane & 7)) * 16);
@@ -535,46 +419,65 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
         }
         fresh = it.leave;
-        if (wm == 1) attention_tile<D, DP, 1>(a, it, ks, q, own_i, scale, o, st);
-        else if (wm == 2) attention_tile<D, DP, 2>(a, it, ks, q, own_i, scale, o, st);
-        else attention_tile<D, DP, 4>(a, it, ks, q, own_i, scale, o, st);
+        attention_tile<D, DP, WM, OWN>(a, it, ks, q, own_i, scale, o, st);
         if (it.leave) {
             // the CTA's record of the item
-            const int item = it.own ? (it.b * a.n_kv + it.kh) * p.own_rt + it.rt : it.kh * p.pre_rt + it.rt;
-            const long long rec = (long long)(item + cta) * (it.own ? p.own_rec_rows : 16 * wm);
-            float *const ro = reinterpret_cast<float *>(ws + (it.own ? p.off_own_o : p.off_pre_o));
-            float2 *const rml = reinterpret_cast<float2 *>(ws + (it.own ? p.off_own_ml : p.off_pre_ml));
-            float *const ex = reinterpret_cast<float *>(smem + s * STAGE);      // the stage just used: [warp][16][DP]
-            float2 *const exml = reinterpret_cast<float2 *>(ex + 4 * 16 * DP);
-            if (wm < 4) named_bar_sync(1, 128);                 // the warps that share rows have all read the stage
+            const int item = OWN ? (it.b * a.n_kv + it.kh) * p.own_rt + it.rt : it.kh * p.pre_rt + it.rt;
+            const long long rec = (long long)(item + cta) * rec_rows;
+            float *const ro = reinterpret_cast<float *>(ws + (OWN ? p.off_own_o : p.off_pre_o)) + rec * hd;
+            float2 *const rml = reinterpret_cast<float2 *>(ws + (OWN ? p.off_own_ml : p.off_pre_ml)) + rec;
+            if (KW > 1) {
+                // The warps that share rows: each scales its output to their common maximum and leaves it in the stage just used
+                // ([warp][16][DP]), then the sums are shared out over the threads.
+                float *const ex = reinterpret_cast<float *>(smem + s * STAGE);
+                const int gw = warp * 16 + g;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                st.l[h] = quad_sum(st.l[h]);
-                const int r = wrow + g + h * 8;
-                if (r >= nrows) continue;
-                float *const dst = (wm < 4 ? ex + (warp * 16 + g + h * 8) * DP : ro + (rec + r) * hd) + 2 * t;
+                for (int h = 0; h < 2; ++h) {
+                    st.l[h] = quad_sum(st.l[h]);
+                    if (t == 0) sh_ml[gw + 8 * h] = make_float2(st.m[h], st.l[h]);
+                }
+                named_bar_sync(1, 128);                         // all have read the stage, and all (m, l) are there
 #pragma unroll
-                for (int n = 0; n < DP / 8; ++n)
-                    if (n * 8 < hd) *reinterpret_cast<float2 *>(dst + n * 8) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
-                if (t == 0) (wm < 4 ? exml[warp * 16 + g + h * 8] : rml[rec + r]) = make_float2(st.m[h], st.l[h]);
-            }
-            if (wm < 4) {
-                named_bar_sync(1, 128);
-                for (int i = tid; i < nrows * (hd / 4); i += 128) {
-                    const int r = i / (hd / 4), c = i % (hd / 4) * 4;
+                for (int h = 0; h < 2; ++h) {
+                    const int r = wrow + g + 8 * h;
+                    if (r >= nrows) continue;
+                    float2 x[KW];
                     float m = -CUDART_INF_F, l = 0.0f;
-                    for (int k = r / 16; k < 4; k += wm) m = fmaxf(m, exml[k * 16 + r % 16].x);
-                    const float base = m == -CUDART_INF_F ? 0.0f : m;
-                    float4 v = make_float4(0, 0, 0, 0);
-                    for (int k = r / 16; k < 4; k += wm) {
-                        const float2 x = exml[k * 16 + r % 16];
-                        const float w = exp2_fast(x.x - base);
-                        const float4 y = *reinterpret_cast<const float4 *>(ex + (k * 16 + r % 16) * DP + c);
-                        l += w * x.y;
-                        v.x += w * y.x; v.y += w * y.y; v.z += w * y.z; v.w += w * y.w;
+#pragma unroll
+                    for (int k = 0; k < KW; ++k) {
+                        x[k] = sh_ml[(k * WM + warp % WM) * 16 + g + 8 * h];
+                        m = fmaxf(m, x[k].x);
                     }
-                    *reinterpret_cast<float4 *>(ro + (rec + r) * hd + c) = v;
-                    if (c == 0) rml[rec + r] = make_float2(m, l);
+                    const float base = m == -CUDART_INF_F ? 0.0f : m, mine = exp2_fast(st.m[h] - base);
+#pragma unroll
+                    for (int k = 0; k < KW; ++k) l += exp2_fast(x[k].x - base) * x[k].y;
+                    if (t == 0 && warp < WM) rml[r] = make_float2(m, l);
+#pragma unroll
+                    for (int n = 0; n < DP / 8; ++n)
+                        *reinterpret_cast<float2 *>(ex + (gw + 8 * h) * DP + n * 8 + 2 * t) = make_float2(o[n][2 * h] * mine, o[n][2 * h + 1] * mine);
+                }
+                named_bar_sync(1, 128);
+                for (int i = tid; i < nrows * (DP / 4); i += 128) {
+                    const int r = i / (DP / 4), c = i % (DP / 4) * 4;
+                    float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll
+                    for (int k = 0; k < KW; ++k) {
+                        const float4 y = *reinterpret_cast<const float4 *>(ex + (k * WM * 16 + r) * DP + c);
+                        v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w;
+                    }
+                    if (c < hd) *reinterpret_cast<float4 *>(ro + (long long)r * hd + c) = v;
+                }
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    st.l[h] = quad_sum(st.l[h]);
+                    const int r = wrow + g + 8 * h;
+                    if (r >= nrows) continue;
+                    float *const dst = ro + (long long)r * hd + 2 * t;
+#pragma unroll
+                    for (int n = 0; n < DP / 8; ++n)
+                        if (n * 8 < hd) *reinterpret_cast<float2 *>(dst + n * 8) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+                    if (t == 0) rml[r] = make_float2(st.m[h], st.l[h]);
                 }
             }
         }
@@ -596,23 +499,23 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.n_heads / a.n_kv, hd = a.head_dim;
     const unsigned r = blockIdx.x, tok = r / (unsigned)a.n_heads, h = r % (unsigned)a.n_heads, kh = h / (unsigned)G, b = tok / (unsigned)a.n_q;
     const long long *start = reinterpret_cast<const long long *>(ws);
-    const long long total = start[a.n_seq], own0 = start[b], own1 = start[b + 1];
-    const AttentionDeal deal(total, p.ctas);
+    const long long total = p.own_ctas ? start[a.n_seq] : 0, own0 = p.own_ctas ? start[b] : 0, own1 = p.own_ctas ? start[b + 1] : 0;
+    const AttentionDeal deal(total, p.own_ctas), pre_deal(p.pre_units, p.pre_ctas);
     const int tiles = (int)div_units(own1 - own0, a.n_kv * p.own_rt);
     // the rows of this one's records: the prefix item's, then the own item's
     long long pre0 = 0, rec0 = 0;
     int n_pre = 0, n_all = 0;
-    const int pre_step = 16 * p.pre_wm, own_step = p.own_rec_rows;
+    const int pre_step = p.pre_rec, own_step = p.own_rec;
     if (p.pre_tiles) {
-        const unsigned row = tok * G + h % (unsigned)G, in = row % (unsigned)pre_step;
-        const long long item = (long long)kh * p.pre_rt + row / (unsigned)pre_step;
-        const int c0 = deal.cta_of(item * p.pre_tiles);
-        n_pre = deal.cta_of((item + 1) * p.pre_tiles - 1) - c0 + 1;
+        const unsigned row = tok * G + h % (unsigned)G, in = row % (unsigned)p.pre_tile;
+        const long long item = (long long)kh * p.pre_rt + row / (unsigned)p.pre_tile;
+        const int c0 = pre_deal.cta_of(item * p.pre_tiles);
+        n_pre = pre_deal.cta_of((item + 1) * p.pre_tiles - 1) - c0 + 1;
         pre0 = (item + c0) * pre_step + in;
     }
     n_all = n_pre;
     if (tiles) {
-        const unsigned row = tok % (unsigned)a.n_q * G + h % (unsigned)G, step = 16 * p.own_wm;
+        const unsigned row = tok % (unsigned)a.n_q * G + h % (unsigned)G, step = p.own_tile;
         const int within = kh * p.own_rt + row / step;
         const long long u = own0 + (long long)within * tiles;
         const int c0 = deal.cta_of(u);
@@ -671,31 +574,42 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
     }
 }
 
-template <class D, int DP>
+template <class D, int DP, int WM, bool OWN>
 static aweq_status units_launch(const AttentionArgs &a, const AttentionPlan &p, unsigned char *ws, cudaStream_t stream)
 {
     constexpr int smem = kAtStages * attention_stage_bytes<DP>();
-    AWEQ_CUDA_OK(cudaFuncSetAttribute(attention_units_kernel<D, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    AWEQ_LAUNCH((attention_units_kernel<D, DP>), dim3((unsigned)p.ctas), dim3(kAtThreads), smem, stream, a, p, ws);
+    AWEQ_CUDA_OK(cudaFuncSetAttribute(attention_units_kernel<D, DP, WM, OWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    AWEQ_LAUNCH((attention_units_kernel<D, DP, WM, OWN>), dim3((unsigned)(OWN ? p.own_ctas : p.pre_ctas)), dim3(kAtThreads), smem, stream,
+                a, p, ws, OWN && p.pre_ctas > 0);
     return AWEQ_OK;
 }
 
-template <class D>
-static aweq_status attention_launch(const AttentionArgs &a, unsigned char *ws, cudaStream_t stream)
+template <class D, bool OWN>
+static aweq_status units_dispatch(const AttentionArgs &a, const AttentionPlan &p, unsigned char *ws, cudaStream_t stream)
 {
-    const AttentionPlan p = attention_plan(a.prefix_len, a.max_own, a.n_seq, a.n_q, a.n_heads, a.n_kv, a.head_dim);
-    const aweq_status rc = p.dp == 64   ? units_launch<D, 64>(a, p, ws, stream)
-                           : p.dp == 96 ? units_launch<D, 96>(a, p, ws, stream)
-                                        : units_launch<D, 128>(a, p, ws, stream);
+    const int wm = (OWN ? p.own_tile : p.pre_tile) / 16;
+#define AWEQ_UNITS(DP) \
+    (wm == 1 ? units_launch<D, DP, 1, OWN>(a, p, ws, stream) : wm == 2 ? units_launch<D, DP, 2, OWN>(a, p, ws, stream) : units_launch<D, DP, 4, OWN>(a, p, ws, stream))
+    return p.dp == 64 ? AWEQ_UNITS(64) : p.dp == 96 ? AWEQ_UNITS(96) : AWEQ_UNITS(128);
+#undef AWEQ_UNITS
+}
+
+template <class D>
+static aweq_status attention_launch(const AttentionArgs &a, const AttentionPlan &p, aweq_dtype dt, unsigned char *ws, cudaStream_t stream)
+{
+    aweq_status rc = AWEQ_OK;
+    if (p.pre_ctas) rc = p.tensor ? run_attention_tc(a, p, dt, ws, stream) : units_dispatch<D, false>(a, p, ws, stream);
+    if (rc == AWEQ_OK && p.own_ctas) rc = units_dispatch<D, true>(a, p, ws, stream);
     if (rc != AWEQ_OK) return rc;
     AWEQ_LAUNCH(attention_join_kernel<D>, dim3((unsigned)p.rows), dim3(128), 0, stream, a, p, (const unsigned char *)ws);
     return AWEQ_OK;
 }
 
-aweq_status run_prefix_attention(const AttentionArgs &a, aweq_dtype dt, void *ws, cudaStream_t stream)
+aweq_status run_prefix_attention(const AttentionArgs &a, const aweq_kv_cache *cache, void *ws, cudaStream_t stream)
 {
+    const AttentionPlan p = attention_plan(cache, a.prefix_len, a.max_own, a.n_seq, a.n_q, a.n_heads);
     unsigned char *const w = reinterpret_cast<unsigned char *>(ws);
-    return dt == AWEQ_F16 ? attention_launch<F16>(a, w, stream) : attention_launch<BF16>(a, w, stream);
+    return cache->dt == AWEQ_F16 ? attention_launch<F16>(a, p, cache->dt, w, stream) : attention_launch<BF16>(a, p, cache->dt, w, stream);
 }
 
 }  // namespace aweq

@@ -97,8 +97,20 @@ __device__ __forceinline__ bool has_exponent(const uint4 &v, uint32_t mask)
     for (int i = 0; i < 4; ++i) any |= (w[i] & mask) == mask || (w[i] >> 16 & mask) == mask;
     return any;
 }
+// ... and those elements set to zero
+__device__ __forceinline__ void drop_exponent(uint4 &v, uint32_t mask)
+{
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((w[i] & mask) == mask) w[i] &= 0xffff0000u;
+        if ((w[i] >> 16 & mask) == mask) w[i] &= 0x0000ffffu;
+    }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+}
 struct F16 {
     using T2 = __half2;
+    static constexpr bool kBf16 = false;
     static __device__ __forceinline__ T2 from_bits(uint32_t u) { return *reinterpret_cast<T2 *>(&u); }
     static __device__ __forceinline__ uint32_t pos_inf2() { return 0x7C007C00u; }
     static __device__ __forceinline__ uint32_t neg_inf2() { return 0xFC00FC00u; }
@@ -115,6 +127,7 @@ struct F16 {
     }
     static __device__ __forceinline__ float one(uint16_t b) { return __half2float(__ushort_as_half(b)); }
     static __device__ __forceinline__ bool any_nonfinite(const uint4 &v) { return has_exponent(v, 0x7C00u); }
+    static __device__ __forceinline__ void drop_nonfinite(uint4 &v) { drop_exponent(v, 0x7C00u); }
     static __device__ __forceinline__ uint16_t encode(float f) { return __half_as_ushort(__float2half_rn(f)); }
     static __device__ __forceinline__ uint32_t encode2(float lo, float hi)
     {
@@ -124,6 +137,7 @@ struct F16 {
 };
 struct BF16 {
     using T2 = __nv_bfloat162;
+    static constexpr bool kBf16 = true;
     static __device__ __forceinline__ T2 from_bits(uint32_t u) { return *reinterpret_cast<T2 *>(&u); }
     static __device__ __forceinline__ uint32_t pos_inf2() { return 0x7F807F80u; }
     static __device__ __forceinline__ uint32_t neg_inf2() { return 0xFF80FF80u; }
@@ -134,6 +148,7 @@ struct BF16 {
     }
     static __device__ __forceinline__ float one(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
     static __device__ __forceinline__ bool any_nonfinite(const uint4 &v) { return has_exponent(v, 0x7F80u); }
+    static __device__ __forceinline__ void drop_nonfinite(uint4 &v) { drop_exponent(v, 0x7F80u); }
     static __device__ __forceinline__ uint16_t encode(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
     static __device__ __forceinline__ uint32_t encode2(float lo, float hi)
     {

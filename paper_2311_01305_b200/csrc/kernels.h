@@ -119,6 +119,6 @@ struct AttentionArgs {
 };
 size_t prefix_attention_ws_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq, int n_q,
                                  int n_heads);
-aweq_status run_prefix_attention(const AttentionArgs &a, aweq_dtype dt, void *ws, cudaStream_t stream);
+aweq_status run_prefix_attention(const AttentionArgs &a, const aweq_kv_cache *cache, void *ws, cudaStream_t stream);
 
 }  // namespace aweq

@@ -4,28 +4,6 @@
 
 namespace aweq {
 
-aweq_status tma_bytes_map(CUtensorMap *map, const void *base, long long rows, long long cols, long long ld, int box_rows)
-{
-    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const Encode encode = [] {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            f = nullptr;
-        return reinterpret_cast<Encode>(f);
-    }();
-    if (!encode) return AWEQ_ERR_UNSUPPORTED;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)ld};
-    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, step[2] = {1, 1};
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, pitch, box, step,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? AWEQ_OK : cuda_failed(cudaErrorInvalidValue);
-}
-
 constexpr int kL8Block = 128;                  // bytes of K per stage: one swizzled row
 
 // sum of the 128 code bytes of a staged row.  A row's 16-byte pieces are permuted by the swizzle, which a
@@ -149,7 +127,8 @@ linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX
                 for (int i = 0; i < kBigStages; ++i) mbar_wait(&sh.full[i], ph ^ (i >= s ? 1u : 0u));
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
+            const bool lead = tc_elect();
             int s = 0, it = 0;
             uint32_t ph = 0;
             const uint32_t idesc = tc_idesc_u8(256, 256);
@@ -161,14 +140,14 @@ linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX
                     if (!mbar_wait_cluster(&sh.full[s], ph)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t a = smem_u32(stages + s * kBigStageBytes);
-                    const uint64_t da = tc_desc(a), db = tc_desc(a + 128 * kL8Block);
+                    const uint32_t da = tc_desc(a), db = tc_desc(a + 128 * kL8Block);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        tc_mma_u8<2>(tmem + acc * 256, da + 2 * k, db + 2 * k, idesc, (kb | k) != 0);
-                    tc_commit<2>(&sh.done[s]);
+                        tc_mma_u8<2>(tmem + acc * 256, da + 2 * k, db + 2 * k, idesc, (kb | k) != 0, lead);
+                    tc_commit<2>(&sh.done[s], lead);
                     if (++s == kBigStages) { s = 0; ph ^= 1; }
                 }
-                if (ok) tc_commit<2>(&sh.acc_full[acc]);
+                if (ok) tc_commit<2>(&sh.acc_full[acc], lead);
             }
         }
     } else if (warp < 4) {
@@ -407,7 +386,8 @@ linear8_split_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap ma
                 for (int i = 0; i < plan.stages; ++i) mbar_wait(&sh.full[i], ph ^ (i >= s ? 1u : 0u));
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        {
+            const bool lead = tc_elect();
             int s = 0;
             uint32_t ph = 0;
             const uint32_t idesc = tc_idesc_u8(128, bn);
@@ -417,20 +397,20 @@ linear8_split_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap ma
                 const int n = min(plan.kb_stage, kb1 - kb);
                 uint32_t a = smem_u32(stages + s * plan.kb_stage * kb_bytes);
                 for (int i = 0; i < n; ++i, a += kb_bytes) {
-                    const uint64_t da = tc_desc(a), db = tc_desc(a + x_bytes);
+                    const uint32_t da = tc_desc(a), db = tc_desc(a + x_bytes);
                     for (int b = 0; b < plan.mb; ++b)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int at = k & (plan.parts - 1);
                             tc_mma_u8<1>(tmem + (b * plan.parts + at) * bn, da + b * (128 * kL8Block / 16) + 2 * k, db + 2 * k, idesc,
-                                         kb + i > kb0 || k >= plan.parts);
+                                         kb + i > kb0 || k >= plan.parts, lead);
                         }
                 }
-                tc_commit<1>(&sh.empty[s]);
+                tc_commit<1>(&sh.empty[s], lead);
                 if (++s == plan.stages) { s = 0; ph ^= 1; }
             }
             if (ok) {
-                tc_commit<1>(&sh.acc_full);
+                tc_commit<1>(&sh.acc_full, lead);
                 ok = mbar_wait(&sh.acc_full, 0);
             }
         }
