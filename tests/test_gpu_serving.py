@@ -549,6 +549,85 @@ def test_attention_many_rows():
     attention_check(70, 2, 16, 2, 128, 640, [(11 * b) % 60 + 2 for b in range(70)], 16, torch.bfloat16)
 
 
+# A prefix of more than 32 rows per key head and three 128-key units for every SM goes to a kernel of its own.
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n_seq,n_q,h,kv,d,prefix,page", [
+    (40, 1, 16, 16, 128, 4100, 16),     # one row tile, 40 of its 128 rows
+    (33, 1, 16, 16, 64, 3585, 32),      # one row more than the other kernel takes; one key in the last unit
+    (9, 2, 32, 4, 128, 7000, 16),       # 144 rows: two row tiles, the second of 16
+    (130, 1, 8, 4, 128, 3700, 64),      # 260 rows: three tiles
+    (35, 1, 15, 15, 72, 4000, 8),       # a head that is no multiple of 16
+    (40, 1, 16, 16, 80, 3710, 24),      # 120 keys to a unit
+    (50, 1, 12, 12, 96, 5000, 128),     # a page to a unit
+    (36, 1, 14, 14, 8, 4096, 256),      # half a page to a unit, the smallest head
+    (34, 1, 16, 16, 64, 4000, 192)])    # copies of 64 keys, units across pages
+def test_attention_long_prefix(n_seq, n_q, h, kv, d, prefix, page, dtype):
+    attention_check(n_seq, n_q, h, kv, d, prefix, [(7 * b) % 40 + n_q for b in range(n_seq)], page, dtype)
+
+
+@pytest.mark.parametrize("layout", ["heads", "joint"])
+def test_attention_long_prefix_layouts(layout):
+    attention_check(40, 1, 16, 16, 128, 4100, [1 + b for b in range(40)], 16, torch.bfloat16, layout)
+
+
+@pytest.mark.parametrize("page", [1, 12, 72, 136])
+def test_attention_long_prefix_of_other_pages(page):
+    """Page sizes that the tiled copies do not fit."""
+    attention_check(40, 1, 16, 16, 64, 3000, [1 + b for b in range(40)], page, torch.float16)
+
+
+@pytest.mark.parametrize("kw", [dict(spread=25.0), dict(spread=25.0, scale=-0.4), dict(scale=0.0), dict(spread=0.01)])
+def test_attention_long_prefix_scores(kw):
+    """Scores that climb far beyond a row's first maximum, a negative and a zero scale, no spread at all."""
+    attention_check(40, 1, 16, 16, 128, 4100, [5] * 40, 16, torch.float16, **kw)
+
+
+def test_attention_long_prefix_rising_maximum():
+    """Keys that grow along the prefix: the reference maximum has to move many times."""
+    q, cache, prefix_pages, pages, lens = attention_case(40, 1, 16, 16, 64, 4096, [3] * 40, 16, torch.bfloat16)
+    grow = torch.linspace(0.05, 6.0, 4096, device="cuda").view(256, 16, 1, 1)
+    cache.k[prefix_pages.long()] = (cache.k[prefix_pages.long()].float() * grow).to(torch.bfloat16)
+    attend = aweq.PrefixAttention(cache, prefix_pages, 4096, 16, 40)
+    attention_close(attend(q, pages, lens), *attention_reference(q, cache, prefix_pages, 4096, pages, lens, 1, attend.scale), 4100,
+                    64, torch.bfloat16)
+
+
+def test_attention_long_prefix_rows_are_independent():
+    q, cache, prefix_pages, pages, lens = attention_case(40, 1, 16, 16, 64, 4100, [9] * 40, 16, torch.float16)
+    attend = aweq.PrefixAttention(cache, prefix_pages, 4100, 16, 40)
+    clean = attend(q, pages, lens)
+    assert torch.equal(clean, attend(q, pages, lens))
+    q[7, 3] = math.nan
+    out = attend(q, pages, lens)
+    assert torch.isnan(out[7, 3]).all()
+    keep = torch.ones(40, 16, dtype=torch.bool, device="cuda")
+    keep[7, 3] = False
+    assert torch.equal(out[keep], clean[keep])
+    # an infinite value reaches every row of its key head and no other
+    cache.v[prefix_pages[100].long(), 3, 5, 11] = math.inf
+    out = attend(q, pages, lens)
+    assert torch.isinf(out[keep[:, 5].nonzero()[:, 0], 5, 11]).all()
+    keep[:, 5] = False
+    assert torch.equal(out[keep], clean[keep])
+
+
+def test_attention_long_prefix_pages_out_of_range_are_counted():
+    q, cache, prefix_pages, pages, lens = attention_case(40, 1, 16, 16, 64, 4100, [9] * 40, 16, torch.float16, stale=False)
+    attend = aweq.PrefixAttention(cache, prefix_pages, 4100, 16, 40)
+    attend.prefix_pages[3], attend.prefix_pages[200] = cache.n_pages, -1
+    st = aweq.new_status()
+    attend(q, pages, lens, st=st)
+    assert aweq.read_out_of_range(st) >= 2 and aweq.read_status(st)["wait_timeout"] == 0
+
+
+def test_attention_many_short_sequences():
+    """Many items of one or two units to a CTA, some sequences without keys, with and without a prefix."""
+    lens = [(37 * b) % 200 for b in range(200)]
+    attention_check(200, 1, 16, 16, 64, 0, lens, 16, torch.bfloat16)
+    attention_check(200, 1, 16, 4, 128, 40, lens, 32, torch.float16)
+    attention_check(200, 1, 8, 8, 128, 2500, lens, 16, torch.float16)
+
+
 def test_attention_values_of_later_tokens_stay_out():
     """Infinities and NaN in the key and value of the last token: the earlier tokens do not see them."""
     q, cache, prefix_pages, pages, lens = attention_case(2, 4, 4, 2, 64, 33, [20, 65], 16, torch.float16)
