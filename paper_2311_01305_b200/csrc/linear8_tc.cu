@@ -40,24 +40,27 @@ __device__ __forceinline__ Linear8Col linear8_col(const Linear8Args &p, long lon
 }
 
 // ------------------------------------------------------------------ many tokens
-// 256 x 256 output tiles, each by a pair of CTAs (cta_group::2): a CTA stages its 128 tokens and half of
-// the 256 channels, and holds the 128 x 256 sums of its tokens in TMEM, twice, so that the
-// epilogue of one tile runs under the products of the next.  Persistent: a pair takes every
-// (pairs)-th tile.  Warps: 0 copies, 1 issues the products (in the pair's even CTA), 2-3 add up the
-// tokens' codes from the stages (after the products have used them: that completion is the one
-// signal both CTAs get), 4-7 write the output.
-constexpr int kBigStages = 6;
+// Output tiles of 256 tokens x 248 channels, each by a pair of CTAs (cta_group::2): a CTA stages its 128 tokens and half of
+// the weights, and holds the sums of its tokens in TMEM, twice, so that the epilogue of one tile runs under the
+// products of the next.  Persistent: a pair takes every (pairs)-th tile.  Warps: 0 copies, 1 issues the products (in the
+// pair's even CTA), 4-11 write the output, two to a quarter of the TMEM lanes.
+//
+// The tokens' code sums rx come out of the same products: the last eight of the 256 rows of the weight tile are ones, laid
+// down once per stage where the copies do not reach.  Summing the staged codes with other warps instead cost 14 % at 2048 x 4096
+// x 11008 (the products read and the copies write 32 KB a stage each, which is all that shared memory moves in that
+// time); the eight rows cost 3 %.
+constexpr int kBigStages = 6, kBigThreads = 384, kBigCols = 248;
 constexpr int kBigStageBytes = 2 * 128 * kL8Block;
-constexpr int kBigOutPitch = 144;              // bytes of a staged output row: 64 columns and 16 bytes against bank conflicts
+constexpr int kBigOutPitch = 80;               // bytes of a staged output row: 32 columns and 16 bytes against bank conflicts
 struct BigShared {
-    uint64_t full[kBigStages], done[kBigStages], empty[kBigStages], acc_full[2], acc_empty[2], rx_full[2], rx_empty[2];
+    uint64_t full[kBigStages], empty[kBigStages], acc_full[2], acc_empty[2];
     uint32_t tmem;
-    float reach[4];
-    uint32_t rx[2][128];
+    float reach[8];
     Linear8Col col[256];
-    alignas(16) unsigned char out[4][32 * kBigOutPitch];
+    alignas(16) unsigned char out[8][32 * kBigOutPitch];
 };
 constexpr size_t kBigSmem = 1024 + (size_t)kBigStages * kBigStageBytes + sizeof(BigShared);
+static_assert(kBigSmem <= 227 * 1024, "shared memory of a CTA");
 
 __device__ __forceinline__ void big_tile(long long t, int mt, int nt, int *m, int *n)
 {
@@ -69,9 +72,9 @@ __device__ __forceinline__ void big_tile(long long t, int mt, int nt, int *m, in
 }
 
 template <class D>
-__global__ void __launch_bounds__(256, 1)
-linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW,
-                   int mt, int nt, int vec_out)
+__global__ void __launch_bounds__(kBigThreads, 1)
+linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW0,
+                   const __grid_constant__ CUtensorMap mapW1, int mt, int nt, int vec_out)
 {
     extern __shared__ unsigned char raw[];
     unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -84,18 +87,21 @@ linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX
     if (threadIdx.x == 0) {
         for (int s = 0; s < kBigStages; ++s) {
             mbar_init(&sh.full[s], 1);
-            mbar_init(&sh.done[s], 1);
-            mbar_init(&sh.empty[s], 2);
+            mbar_init(&sh.empty[s], 1);
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(&sh.acc_full[a], 1);
-            mbar_init(&sh.acc_empty[a], 8);
-            mbar_init(&sh.rx_full[a], 2);
-            mbar_init(&sh.rx_empty[a], 4);
+            mbar_init(&sh.acc_empty[a], 16);
         }
         mbar_init_fence();
         tma_prefetch_map(&mapX);
-        tma_prefetch_map(&mapW);
+        tma_prefetch_map(rank ? &mapW1 : &mapW0);
+    }
+    if (rank == 1) {                               // rows 120-127 of this CTA's half of the weight tile: ones
+        for (int i = threadIdx.x; i < kBigStages * 64; i += kBigThreads)
+            *reinterpret_cast<uint4 *>(stages + (i >> 6) * kBigStageBytes + (128 + 120) * kL8Block + (i & 63) * 16) =
+                make_uint4(0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 1) tc_alloc<2>(&sh.tmem, 512);
     tc_fence_before();
@@ -108,18 +114,19 @@ linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX
     bool ok = true;
     if (warp == 0) {
         if (lane == 0) {
+            const CUtensorMap *const mapW = rank ? &mapW1 : &mapW0;
             int s = 0;
             uint32_t ph = 0;
             for (long long t = blockIdx.x / 2; ok && t < tiles; t += step) {
                 int m, n;
                 big_tile(t, mt, nt, &m, &n);
-                const int row = m * 256 + (int)rank * 128, col = n * 256 + (int)rank * 128;
+                const int row = m * 256 + (int)rank * 128, col = n * kBigCols + (int)rank * 128;
                 for (int kb = 0; kb < nkb; ++kb) {
-                    if (!mbar_wait(&sh.empty[s], ph ^ 1)) { ok = false; break; }
+                    if (!mbar_wait_cluster(&sh.empty[s], ph ^ 1)) { ok = false; break; }
                     const uint32_t bar = cluster_map(&sh.full[s], 0), dst = smem_u32(stages + s * kBigStageBytes);
-                    if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2 * kBigStageBytes);
+                    if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2 * kBigStageBytes - 8 * kL8Block);
                     tma_load2<2>(dst, &mapX, kb * kL8Block, row, bar);
-                    tma_load2<2>(dst + 128 * kL8Block, &mapW, kb * kL8Block, col, bar);
+                    tma_load2<2>(dst + 128 * kL8Block, mapW, kb * kL8Block, col, bar);
                     if (++s == kBigStages) { s = 0; ph ^= 1; }
                 }
             }
@@ -144,118 +151,83 @@ linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         tc_mma_u8<2>(tmem + acc * 256, da + 2 * k, db + 2 * k, idesc, (kb | k) != 0, lead);
-                    tc_commit<2>(&sh.done[s], lead);
+                    tc_commit<2>(&sh.empty[s], lead);
                     if (++s == kBigStages) { s = 0; ph ^= 1; }
                 }
                 if (ok) tc_commit<2>(&sh.acc_full[acc], lead);
             }
         }
-    } else if (warp < 4) {
-        int s = 0, it = 0;
-        uint32_t ph = 0;
-        const int r0 = (warp - 2) * 64 + lane;
-        for (long long t = blockIdx.x / 2; ok && t < tiles; t += step, ++it) {
-            const int acc = it & 1;
-            uint32_t a = 0, b = 0;
-            for (int kb = 0; kb < nkb; ++kb) {
-                ok = mbar_wait_cluster(&sh.done[s], ph);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                const unsigned char *x = stages + s * kBigStageBytes + r0 * kL8Block;
-                a += staged_row_sum(x, lane);
-                b += staged_row_sum(x + 32 * kL8Block, lane);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.empty[s]);
-                if (++s == kBigStages) { s = 0; ph ^= 1; }
-            }
-            if (!ok) break;
-            ok = mbar_wait(&sh.rx_empty[acc], ((it >> 1) & 1) ^ 1);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-            sh.rx[acc][r0] = a;
-            sh.rx[acc][r0 + 32] = b;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.rx_full[acc]);
-        }
-    } else {
-        const int q = warp - 4, tid = threadIdx.x - 128;
-        unsigned char *buf = sh.out[q];
+    } else if (warp >= 4) {
+        const int q = warp & 3, half = (warp - 4) >> 2, tid = threadIdx.x - 128;
+        unsigned char *buf = sh.out[warp - 4];
         int it = 0;
         for (long long t = blockIdx.x / 2; t < tiles; t += step, ++it) {
             const int acc = it & 1;
             int m, n;
             big_tile(t, mt, nt, &m, &n);
-            const long long row0 = (long long)m * 256 + rank * 128 + q * 32, row = row0 + lane, o0 = (long long)n * 256;
+            const long long row0 = (long long)m * 256 + rank * 128 + q * 32, row = row0 + lane, o0 = (long long)n * kBigCols;
             // the channels' pairs, and the largest reach of their zero-points
-            named_bar_sync(1, 128);
-            float reach = 0.0f;
-            for (int i = tid; i < 256; i += 128) {
-                const Linear8Col c = linear8_col(p, o0 + i);
-                sh.col[i] = c;
-                reach = fmaxf(reach, linear8_reach(c.zp));
-            }
-            reach = redux_max(reach, 0xffffffffu);
-            if (lane == 0) sh.reach[q] = reach;
+            named_bar_sync(1, 256);
+            const Linear8Col mine = linear8_col(p, tid < kBigCols ? o0 + tid : p.O);
+            sh.col[tid] = mine;
+            float reach = redux_max(linear8_reach(mine.zp), 0xffffffffu);
+            if (lane == 0) sh.reach[warp - 4] = reach;
             const bool live = row < p.N;
             const int zx = live ? __ldg(p.x_zp + row * p.x_inc) : 0;
             const float sx = live ? __ldg(p.x_step + row * p.x_inc) : 0.0f;
-            named_bar_sync(1, 128);
-            reach = fmaxf(fmaxf(sh.reach[0], sh.reach[1]), fmaxf(sh.reach[2], sh.reach[3]));
-            bool got = mbar_wait(&sh.rx_full[acc], (it >> 1) & 1) && mbar_wait_cluster(&sh.acc_full[acc], (it >> 1) & 1);
-            if (!named_bar_and(2, 128, got)) { ok = false; break; }
+            named_bar_sync(1, 256);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) reach = fmaxf(reach, sh.reach[i]);
+            const bool got = mbar_wait_cluster(&sh.acc_full[acc], (it >> 1) & 1);
+            if (!named_bar_and(2, 256, got)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t rx = sh.rx[acc][q * 32 + lane];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.rx_empty[acc]);
-            const float reachK = linear8_reach(zx) * (float)p.K;
-            const bool all_small = __all_sync(0xffffffffu, reachK * reach < 2.147e9f);      // see linear8_acc
-            const uint32_t u = rx - (uint32_t)p.K * (uint32_t)zx;
+            const uint32_t at = tmem + acc * 256 + ((uint32_t)(q * 32) << 16);
+            if (row0 < p.N) {
+                const uint32_t rx = tc_ld1(at + kBigCols);
+                const float reachK = linear8_reach(zx) * (float)p.K;
+                const bool all_small = __all_sync(0xffffffffu, reachK * reach < 2.147e9f);      // see linear8_acc
+                const uint32_t u = rx - (uint32_t)p.K * (uint32_t)zx;
+                const int c1 = half ? kBigCols : 128;
 #pragma unroll 1
-            for (int c0 = 0; c0 < 256; c0 += 64) {
-                if (row0 < p.N && o0 + c0 < p.O) {
+                for (int c0 = half * 128; c0 < c1 && o0 + c0 < p.O; c0 += 32) {
+                    uint32_t S[32], packed[16];
+                    tc_ld32(at + c0, S);
+                    tc_wait_ld();
+                    if (all_small) {
 #pragma unroll
-                    for (int h = 0; h < 64; h += 32) {
-                        uint32_t S[32];
-                        tc_ld32(tmem + acc * 256 + c0 + h + ((uint32_t)(q * 32) << 16), S);
-                        tc_wait_ld();
-                        uint32_t packed[16];
-                        if (all_small) {
-#pragma unroll
-                            for (int j = 0; j < 32; j += 2) {
-                                const Linear8Col c = sh.col[c0 + h + j], d = sh.col[c0 + h + j + 1];
-                                const float v = (float)(int)(S[j] - (uint32_t)zx * c.sum - (uint32_t)c.zp * u);
-                                const float w = (float)(int)(S[j + 1] - (uint32_t)zx * d.sum - (uint32_t)d.zp * u);
-                                packed[j / 2] = D::encode2(__fmaf_rn(v * sx, c.step, c.bias), __fmaf_rn(w * sx, d.step, d.bias));
-                            }
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                const Linear8Col c = sh.col[c0 + h + j];
-                                const float v = linear8_acc(S[j], zx, rx, c.zp, c.sum, (uint32_t)p.K, reachK, reach);
-                                const uint32_t y = D::encode(__fmaf_rn(v * sx, c.step, c.bias));
-                                packed[j / 2] = j & 1 ? packed[j / 2] | y << 16 : y;
-                            }
+                        for (int j = 0; j < 32; j += 2) {
+                            const Linear8Col c = sh.col[c0 + j], d = sh.col[c0 + j + 1];
+                            const float v = (float)(int)(S[j] - (uint32_t)zx * c.sum - (uint32_t)c.zp * u);
+                            const float w = (float)(int)(S[j + 1] - (uint32_t)zx * d.sum - (uint32_t)d.zp * u);
+                            packed[j / 2] = D::encode2(__fmaf_rn(v * sx, c.step, c.bias), __fmaf_rn(w * sx, d.step, d.bias));
                         }
+                    } else {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            *reinterpret_cast<uint4 *>(buf + lane * kBigOutPitch + h * 2 + j * 16) =
-                                make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
+                        for (int j = 0; j < 32; ++j) {
+                            const Linear8Col c = sh.col[c0 + j];
+                            const float v = linear8_acc(S[j], zx, rx, c.zp, c.sum, (uint32_t)p.K, reachK, reach);
+                            const uint32_t y = D::encode(__fmaf_rn(v * sx, c.step, c.bias));
+                            packed[j / 2] = j & 1 ? packed[j / 2] | y << 16 : y;
+                        }
                     }
-                    __syncwarp();
-                    if (vec_out && o0 + c0 + 64 <= p.O) {
-                        // four rows of 128 bytes per store
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int r = i * 4 + (lane >> 3);
-                            if (row0 + r < p.N)
-                                *reinterpret_cast<uint4 *>(p.out + (row0 + r) * p.ldo + o0 + c0 + (lane & 7) * 8) =
-                                    *reinterpret_cast<const uint4 *>(buf + r * kBigOutPitch + (lane & 7) * 16);
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<uint4 *>(buf + lane * kBigOutPitch + j * 16) =
+                            make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
+                    __syncwarp();
+                    const int cols = (int)min((long long)min(32, c1 - c0), p.O - (o0 + c0));
+                    if (vec_out && cols % 8 == 0) {
+                        // eight rows of 64 bytes per store
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = i * 8 + (lane >> 2), c = (lane & 3) * 8;
+                            if (row0 + r < p.N && c < cols)
+                                *reinterpret_cast<uint4 *>(p.out + (row0 + r) * p.ldo + o0 + c0 + c) =
+                                    *reinterpret_cast<const uint4 *>(buf + r * kBigOutPitch + c * 2);
                         }
                     } else {
                         for (int r = 0; r < 32 && row0 + r < p.N; ++r)
-#pragma unroll
-                            for (int e = 0; e < 64; e += 32)
-                                if (o0 + c0 + e + lane < p.O)
-                                    p.out[(row0 + r) * p.ldo + o0 + c0 + e + lane] =
-                                        *reinterpret_cast<const uint16_t *>(buf + r * kBigOutPitch + (e + lane) * 2);
+                            if (lane < cols) p.out[(row0 + r) * p.ldo + o0 + c0 + lane] = *reinterpret_cast<const uint16_t *>(buf + r * kBigOutPitch + lane * 2);
                     }
                     __syncwarp();
                 }
@@ -275,17 +247,18 @@ linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX
 template <class D>
 static aweq_status big_launch(const Linear8Args &a, cudaStream_t stream)
 {
-    CUtensorMap mx, mw;
+    CUtensorMap mx, w0, w1;
     aweq_status rc = tma_bytes_map(&mx, a.X, a.N, a.K, a.ldx, 128);
-    if (rc == AWEQ_OK) rc = tma_bytes_map(&mw, a.W, a.O, a.K, a.ldw, 128);
+    if (rc == AWEQ_OK) rc = tma_bytes_map(&w0, a.W, a.O, a.K, a.ldw, 128);
+    if (rc == AWEQ_OK) rc = tma_bytes_map(&w1, a.W, a.O, a.K, a.ldw, 120);
     if (rc != AWEQ_OK) return rc;
     AWEQ_CUDA_OK(cudaFuncSetAttribute(linear8_big_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBigSmem));
-    const int mt = (int)((a.N + 255) / 256), nt = (a.O + 255) / 256;
+    const int mt = (int)((a.N + 255) / 256), nt = (a.O + kBigCols - 1) / kBigCols;
     const long long tiles = (long long)mt * nt;
     const unsigned pairs = (unsigned)(tiles < kSmCount / 2 ? tiles : kSmCount / 2);
     const int vec = (a.ldo % 8 == 0) && ((reinterpret_cast<uintptr_t>(a.out) & 15) == 0);
-    const cudaError_t e = launch_pdl_cluster(linear8_big_kernel<D>, dim3(pairs * 2), dim3(256), kBigSmem, stream, 2, a, mx, mw, mt,
-                                             nt, vec);
+    const cudaError_t e = launch_pdl_cluster(linear8_big_kernel<D>, dim3(pairs * 2), dim3(kBigThreads), kBigSmem, stream, 2, a, mx, w0, w1,
+                                             mt, nt, vec);
     note_launch();
     if (e != cudaSuccess) return cuda_failed(e);
     return AWEQ_OK;

@@ -98,6 +98,14 @@ __device__ __forceinline__ void tc_ld32(uint32_t tmem, uint32_t (&r)[32])
         : "r"(tmem));
 }
 
+__device__ __forceinline__ uint32_t tc_ld1(uint32_t tmem)
+{
+    uint32_t r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(tmem));
+    tc_wait_ld();
+    return r;
+}
+
 // 2-D box global -> this CTA's shared memory.  CG 2: the barrier may be the pair's other CTA's
 // (bar is a shared::cluster address either way).
 template <int CG>
