@@ -539,9 +539,7 @@ aweq_status aweq_linear_w8a8(const unsigned char *Xq, long long ldx, const float
     a.x_step = act_step; a.w_step = w_step; a.bias = bias; a.x_zp = act_zp; a.w_zp = w_zp; a.w_sum = w_sum;
     a.x_inc = act_gran == AWEQ_PER_ROW; a.w_inc = w_gran == AWEQ_PER_ROW;
     a.K = (int)C_in; a.O = (int)C_out; a.out = reinterpret_cast<uint16_t *>(out); a.st = st;
-    if (N > 128) return run_linear8_big(a, dt, (cudaStream_t)stream);
-    if (N > 16) return run_linear8_split(a, dt, (cudaStream_t)stream);
-    return run_linear8_stream(a, dt, (cudaStream_t)stream);
+    return run_linear8(a, dt, (cudaStream_t)stream);
 }
 
 aweq_status aweq_rope_table(const aweq_rope *r, long long n_pos, float *table, void *stream)

@@ -34,8 +34,7 @@ struct Linear8Args {
     aweq_dev_status *st;
 };
 
-aweq_status run_linear8_stream(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream);
-aweq_status run_linear8_split(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream);
-aweq_status run_linear8_big(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream);
+aweq_status run_linear8_stream(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream);       // linear8.cu
+aweq_status run_linear8(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream);              // linear8_tc.cu: any of them
 
 }  // namespace aweq

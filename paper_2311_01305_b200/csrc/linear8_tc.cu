@@ -1,4 +1,6 @@
 // aweq_linear_w8a8 on the tensor cores: tcgen05.mma kind::i8 over TMA-fed tiles.
+#include <math.h>
+
 #include "linear8.cuh"
 #include "tensorcore.cuh"
 
@@ -264,7 +266,7 @@ static aweq_status big_launch(const Linear8Args &a, cudaStream_t stream)
     return AWEQ_OK;
 }
 
-aweq_status run_linear8_big(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream)
+static aweq_status run_linear8_big(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream)
 {
     return dt == AWEQ_F16 ? big_launch<F16>(a, stream) : big_launch<BF16>(a, stream);
 }
@@ -282,7 +284,6 @@ constexpr int kSplitRing = 200 * 1024, kSplitMaxStages = 16;
 struct SplitPlan {
     int bn, slices;              // channels of a tile, slices of K
     int box, mb;                 // token rows of a stage, 128-row blocks they make
-    int parts;                   // independent accumulators that the products of a block take in turn
     int stages, kb_stage;        // ring, 128-byte blocks of K per stage
     int rx_groups, rx_sets;      // 32-row groups of a stage; warps that share a group's stages
 };
@@ -318,7 +319,7 @@ linear8_split_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap ma
     const int rows = (int)min(128ll * plan.mb, p.N - row0);
     const int o0 = blockIdx.y * bn;
     uint32_t cols = 32;
-    while ((int)cols < bn * plan.mb * plan.parts) cols *= 2;
+    while ((int)cols < bn * plan.mb) cols *= 2;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < plan.stages; ++s) {
@@ -359,33 +360,28 @@ linear8_split_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap ma
                 for (int i = 0; i < plan.stages; ++i) mbar_wait(&sh.full[i], ph ^ (i >= s ? 1u : 0u));
         }
     } else if (warp == 1) {
-        {
-            const bool lead = tc_elect();
-            int s = 0;
-            uint32_t ph = 0;
-            const uint32_t idesc = tc_idesc_u8(128, bn);
-            for (int kb = kb0; kb < kb1; kb += plan.kb_stage) {
-                if (!mbar_wait(&sh.full[s], ph)) { ok = false; break; }
-                tc_fence_after();
-                const int n = min(plan.kb_stage, kb1 - kb);
-                uint32_t a = smem_u32(stages + s * plan.kb_stage * kb_bytes);
-                for (int i = 0; i < n; ++i, a += kb_bytes) {
-                    const uint32_t da = tc_desc(a), db = tc_desc(a + x_bytes);
-                    for (int b = 0; b < plan.mb; ++b)
+        const bool lead = tc_elect();
+        int s = 0;
+        uint32_t ph = 0;
+        const uint32_t idesc = tc_idesc_u8(128, bn);
+        for (int kb = kb0; kb < kb1; kb += plan.kb_stage) {
+            if (!mbar_wait(&sh.full[s], ph)) { ok = false; break; }
+            tc_fence_after();
+            const int n = min(plan.kb_stage, kb1 - kb);
+            uint32_t a = smem_u32(stages + s * plan.kb_stage * kb_bytes);
+            for (int i = 0; i < n; ++i, a += kb_bytes) {
+                const uint32_t da = tc_desc(a), db = tc_desc(a + x_bytes);
+                for (int b = 0; b < plan.mb; ++b)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int at = k & (plan.parts - 1);
-                            tc_mma_u8<1>(tmem + (b * plan.parts + at) * bn, da + b * (128 * kL8Block / 16) + 2 * k, db + 2 * k, idesc,
-                                         kb + i > kb0 || k >= plan.parts, lead);
-                        }
-                }
-                tc_commit<1>(&sh.empty[s], lead);
-                if (++s == plan.stages) { s = 0; ph ^= 1; }
+                    for (int k = 0; k < 4; ++k)
+                        tc_mma_u8<1>(tmem + b * bn, da + b * (128 * kL8Block / 16) + 2 * k, db + 2 * k, idesc, kb + i > kb0 || k > 0, lead);
             }
-            if (ok) {
-                tc_commit<1>(&sh.acc_full, lead);
-                ok = mbar_wait(&sh.acc_full, 0);
-            }
+            tc_commit<1>(&sh.empty[s], lead);
+            if (++s == plan.stages) { s = 0; ph ^= 1; }
+        }
+        if (ok) {
+            tc_commit<1>(&sh.acc_full, lead);
+            ok = mbar_wait(&sh.acc_full, 0);
         }
     } else {
         // the pairs of channels and tokens, while the first copies are under way
@@ -432,16 +428,9 @@ linear8_split_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap ma
         const int r = b0 * 128 + q * 32;
         if (r < rows)
             for (int c = c0; c < bn; c += dc) {
-                uint32_t S[32], T[32];
-                const uint32_t at = tmem + b0 * plan.parts * bn + c + ((uint32_t)(q * 32) << 16);
-                tc_ld32(at, S);
+                uint32_t S[32];
+                tc_ld32(tmem + b0 * bn + c + ((uint32_t)(q * 32) << 16), S);
                 tc_wait_ld();
-                for (int i = 1; i < plan.parts; ++i) {
-                    tc_ld32(at + i * bn, T);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) S[j] += T[j];
-                }
                 if (r + lane < rows)
 #pragma unroll
                     for (int j = 0; j < 32; j += 4)
@@ -528,17 +517,55 @@ static aweq_status split_launch(const Linear8Args &a, SplitPlan plan, cudaStream
     return AWEQ_OK;
 }
 
-aweq_status run_linear8_split(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream)
+// Which kernel, and how it cuts the layer.
+//
+// The plain-load kernel (linear8.cu) reads the weights once for up to 32 tokens and the tokens once for every 16 channels: it wins
+// while that is little (1 x 4096 x 4096: 6.8 us against 7.7; 64 x 768 x 768: 3.6 against 5.5; 16 x 4096 x 12288: 19.1 against 12.7).
+// For the other two the estimate below is within about 10 % of 70 measured (shape, cut) pairs between 16 x 4096 x 4096
+// and 256 x 4096 x 4096, in microseconds: a start, then per 128-byte block of K the slowest of an issue limit, what an SM
+// can take in and what the memory gives.  A K slice costs an exchange; clusters of three and four do not fill the device.
+struct Linear8Choice {
+    int kernel;                  // 0: plain loads, 1: K slices on single CTAs, 2: pairs of CTAs
+    int bn, slices;
+};
+static Linear8Choice linear8_choose(long long N, int K, int O)
+{
+    if (N <= 64 && (double)K * O * (double)(N > 16 ? N : 16) <= 2.7e8) return {0, 0, 0};
+    const int nkb = (K + kL8Block - 1) / kL8Block;
+    const double tiles = (double)((N + 255) / 256) * ((O + kBigCols - 1) / kBigCols), waves = ceil(tiles / (kSmCount / 2));
+    Linear8Choice best = {2, 0, 0};
+    double cost = 6.0 + waves * nkb * (0.3 + 0.1 * (tiles < 60 ? tiles / 60 : 1.0));
+    static const int bns[5] = {32, 64, 96, 128, 256}, most[5] = {0, kSmCount, kSmCount, 120, 128};
+    if (N <= 256)
+        for (int bn : bns)
+            for (int slices = 1; slices <= 4 && slices <= nkb; ++slices) {
+                const int mb = N > 128 && bn <= 128 ? 2 : 1;
+                const double rows = N < 128 * mb ? (double)N : 128.0 * mb, box = rows + 7;
+                const double ctas = (double)((O + bn - 1) / bn) * (double)((N + 128 * mb - 1) / (128 * mb)) * slices;
+                if (slices > 1 && ctas > most[slices]) continue;
+                const double live = ctas < kSmCount ? ctas : kSmCount;
+                double t = 0.16;
+                t = fmax(t, (bn + box) * 128 / 75e3);
+                t = fmax(t, bn * 128 * live / 6.6e6);
+                if (bn >= 128) t = fmax(t, 0.13 * mb * bn / 128);
+                const double c = 4.6 + ceil(ctas / kSmCount) * ((nkb + slices - 1) / slices * t + 0.00012 * rows * bn / slices) +
+                                 (slices > 1 ? 0.9 + 0.009 * rows : 0.0);
+                if (c < cost) {
+                    cost = c;
+                    best = {1, bn, slices};
+                }
+            }
+    return best;
+}
+
+static aweq_status run_linear8_split(const Linear8Args &a, aweq_dtype dt, int bn, int slices, cudaStream_t stream)
 {
     SplitPlan s;
-    const int bn = 128, tiles = (a.O + bn - 1) / bn, slices = tiles * 4 <= kSmCount ? 4 : tiles * 3 <= kSmCount ? 3 : tiles * 2 <= kSmCount ? 2 : 1;
     s.mb = a.N > 128 && bn <= 128 ? 2 : 1;
     const long long rows = a.N < 128 * s.mb ? a.N : 128 * s.mb;
     s.bn = bn;
+    s.slices = slices;
     s.box = (int)((rows + 7) / 8 * 8);
-    s.parts = bn * s.mb <= 128 ? 4 : bn * s.mb <= 256 ? 2 : 1;
-    const int nkb = (a.K + kL8Block - 1) / kL8Block;
-    s.slices = slices < nkb ? slices : nkb;                // no slice is empty
     const int kb_bytes = (s.box + bn) * kL8Block, span = s.mb * 128 * kL8Block;
     s.kb_stage = kb_bytes <= 20 * 1024 ? 2 : 1;
     // the product's 128 rows per block stay inside the ring from the last block of K on too
@@ -548,6 +575,14 @@ aweq_status run_linear8_split(const Linear8Args &a, aweq_dtype dt, cudaStream_t 
     s.rx_groups = (s.box + 31) / 32;
     s.rx_sets = s.rx_groups <= 3 ? 6 / s.rx_groups : 1;
     return dt == AWEQ_F16 ? split_launch<F16>(a, s, stream) : split_launch<BF16>(a, s, stream);
+}
+
+aweq_status run_linear8(const Linear8Args &a, aweq_dtype dt, cudaStream_t stream)
+{
+    const Linear8Choice c = linear8_choose(a.N, a.K, a.O);
+    if (c.kernel == 0) return run_linear8_stream(a, dt, stream);
+    if (c.kernel == 1) return run_linear8_split(a, dt, c.bn, c.slices, stream);
+    return run_linear8_big(a, dt, stream);
 }
 
 }  // namespace aweq
