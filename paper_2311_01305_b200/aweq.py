@@ -151,7 +151,12 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the raw handle of the current stream (torch.cuda.current_stream() builds an object: 3 us a call)
+    return _raw_stream(_current_device())
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch.cuda.current_device
 
 
 def dtype_tag(t: torch.Tensor) -> int:
@@ -451,18 +456,25 @@ class LinearW8A8:
         self._weight = (_ptr(codes), _ld(codes), _ptr(step), _ptr(zp), _ptr(self.w_sum), gran, _ptr(bias))
 
     def __call__(self, Xq, act_step, act_zp, out=None, dtype=torch.float16, st=None):
-        N = Xq.shape[0]
+        n, c = Xq.shape
         if out is None:
-            out = torch.empty((N, self.C_out), dtype=dtype, device=Xq.device)
+            out = torch.empty((n, self.C_out), dtype=dtype, device=Xq.device)
+        ldx, one = Xq.stride()
+        ldo, out_one = out.stride()
         pairs = act_step.numel()
-        if (Xq.dtype != torch.uint8 or Xq.shape[1] != self.C_in or out.shape[0] != N or out.shape[1] != self.C_out
-                or act_step.dtype != torch.float32 or act_zp.dtype != torch.int32 or act_zp.numel() != pairs
-                or (pairs != N and pairs != 1) or not (act_step.is_contiguous() and act_zp.is_contiguous())):
-            raise ValueError("Xq [N x %d] uint8, act_step / act_zp float32 / int32 of N or one element, out [N x %d]"
-                             % (self.C_in, self.C_out))
-        _check(_lib.aweq_linear_w8a8(_ptr(Xq), _ld(Xq), _ptr(act_step), _ptr(act_zp), PER_ROW if pairs == N else PER_TENSOR,
-                                     *self._weight, N, self.C_in, self.C_out, _ptr(out), dtype_tag(out), _ld(out), _ptr(st),
-                                     _stream()))
+        # every check a few tenths of a microsecond: a decoding step calls this once per projection
+        if (c != self.C_in or Xq.dtype is not torch.uint8 or one != 1 or out_one != 1 or out.shape != (n, self.C_out)
+                or act_step.dtype is not torch.float32 or act_zp.dtype is not torch.int32 or act_zp.numel() != pairs
+                or (pairs != n and pairs != 1) or not (act_step.is_contiguous() and act_zp.is_contiguous())
+                or not (Xq.is_cuda and out.is_cuda and act_step.is_cuda and act_zp.is_cuda)):
+            raise ValueError("device tensors: Xq [N x %d] uint8, act_step / act_zp float32 / int32 of N or one element, "
+                             "out [N x %d], rows contiguous" % (self.C_in, self.C_out))
+        if n == 1:                                                      # one row has no pitch of its own
+            ldx, ldo = max(ldx, c), max(ldo, self.C_out)
+        rc = _lib.aweq_linear_w8a8(Xq.data_ptr(), ldx, act_step.data_ptr(), act_zp.data_ptr(), PER_ROW if pairs == n else PER_TENSOR,
+                                   *self._weight, n, c, self.C_out, out.data_ptr(), dtype_tag(out), ldo, _ptr(st), _stream())
+        if rc:
+            raise AweqError(rc)
         return out
 
 
@@ -497,52 +509,59 @@ class KVCache:
         self.ref = ctypes.byref(self.args)
 
 
-def _heads(t: torch.Tensor, n_heads: int, head_dim: int, dtype, what: str) -> int:
-    """Row pitch of [tokens, heads, head_dim] (or [tokens, heads * head_dim]) with contiguous rows."""
+def _heads(t: torch.Tensor, n: int, n_heads: int, head_dim: int, dtype, what: str) -> int:
+    """Row pitch of [n, heads, head_dim] (or [n, heads * head_dim]) on the device with contiguous rows."""
     shape, stride = t.shape, t.stride()
     if len(shape) == 3:
         ok = shape[1] == n_heads and shape[2] == head_dim and stride[2] == 1 and (n_heads == 1 or stride[1] == head_dim)
     else:
         ok = len(shape) == 2 and shape[1] == n_heads * head_dim and stride[1] == 1
-    if not ok or t.dtype != dtype:
-        raise ValueError("%s must be %s [tokens, %d, %d] with contiguous rows" % (what, dtype, n_heads, head_dim))
-    return stride[0] if shape[0] > 1 else max(stride[0], n_heads * head_dim)
+    if not ok or shape[0] != n or t.dtype is not dtype or not t.is_cuda:
+        raise ValueError("%s must be a %s device tensor [%d, %d, %d] with contiguous rows" % (what, dtype, n, n_heads, head_dim))
+    return stride[0] if n > 1 else max(stride[0], n_heads * head_dim)
 
 
-def _int32_table(t: torch.Tensor, what: str) -> int:
-    if t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be int32 [sequences, pages] with contiguous rows" % what)
-    return max(t.stride(0), t.shape[1])
+def _int32_rows(t: torch.Tensor, n: int, what: str) -> int:
+    """Pointer of a contiguous int32 device tensor of n elements."""
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s must be a contiguous int32 device tensor of %d elements" % (what, n))
+    return t.data_ptr()
+
+
+def _int32_table(t: torch.Tensor, what: str):
+    """(pointer, rows, columns, pitch) of an int32 device matrix with contiguous rows."""
+    if t.dtype is not torch.int32 or t.dim() != 2 or not t.is_cuda:
+        raise ValueError("%s must be an int32 device matrix" % what)
+    (rows, cols), (ld, one) = t.shape, t.stride()
+    if cols > 1 and one != 1:
+        raise ValueError("%s must have contiguous rows" % what)
+    return t.data_ptr(), rows, cols, max(ld, cols)
 
 
 def aweq_kv_append(cache, page_table, k, v, pos, seq=None, first=0, table=None, interleaved=False, q=None, q_out=None,
                    st=None):
     """Store keys and values of new tokens in their pages, keys (and ``q`` into ``q_out``) turned by
     their positions on the way (argument marshalling only; see ``include/aweq.h``)."""
-    d, n = cache.head_dim, k.shape[0]
-    ldk, ldv = _heads(k, cache.n_kv_heads, d, cache.dtype, "k"), _heads(v, cache.n_kv_heads, d, cache.dtype, "v")
-    ld_table = _int32_table(page_table, "page_table")
-    if v.shape[0] != n or pos.dtype != torch.int32 or pos.numel() != n or not pos.is_contiguous():
-        raise ValueError("k, v and an int32 pos have one row per token")
-    if seq is None:
-        if page_table.shape[0] < n:
-            raise ValueError("without seq, page_table has a row per token")
-    elif seq.dtype != torch.int32 or seq.numel() != n or not seq.is_contiguous():
-        raise ValueError("seq must be int32, one per token")
+    d, kv, dt, n = cache.head_dim, cache.n_kv_heads, cache.dtype, k.shape[0]
+    ldk, ldv = _heads(k, n, kv, d, dt, "k"), _heads(v, n, kv, d, dt, "v")
+    pages, n_seq, per_seq, ld_table = _int32_table(page_table, "page_table")
+    if seq is None and n_seq < n:
+        raise ValueError("without seq, page_table has a row per token")
     n_pos = rd = 0
     if table is not None:
         n_pos, rd = table.shape
-        _want(table, torch.float32, n_pos * rd, "table")
+        if table.dtype is not torch.float32 or not table.is_contiguous():
+            raise ValueError("table must be contiguous float32 [positions, rotary_dim]")
     ldq = ldo = heads = 0
     if q is not None:
         heads = q.shape[1] if q.dim() == 3 else q.shape[1] // d
         q_out = q if q_out is None else q_out
-        ldq, ldo = _heads(q, heads, d, cache.dtype, "q"), _heads(q_out, heads, d, cache.dtype, "q_out")
-        if q.shape[0] != n or q_out.shape[0] != n:
-            raise ValueError("q and q_out have one row per token")
-    _check(_lib.aweq_kv_append(cache.ref, _ptr(page_table), page_table.shape[0], page_table.shape[1], ld_table, _ptr(k), ldk,
-                               _ptr(v), ldv, _ptr(pos), _ptr(seq), first, n, _ptr(table), n_pos, rd, int(interleaved),
-                               _ptr(q), ldq, heads, _ptr(q_out), ldo, _ptr(st), _stream()))
+        ldq, ldo = _heads(q, n, heads, d, dt, "q"), _heads(q_out, n, heads, d, dt, "q_out")
+    rc = _lib.aweq_kv_append(cache.ref, pages, n_seq, per_seq, ld_table, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                             _int32_rows(pos, n, "pos"), None if seq is None else _int32_rows(seq, n, "seq"), first, n, _ptr(table),
+                             n_pos, rd, 1 if interleaved else 0, _ptr(q), ldq, heads, _ptr(q_out), ldo, _ptr(st), _stream())
+    if rc:
+        raise AweqError(rc)
     return q_out
 
 
@@ -553,19 +572,19 @@ def aweq_prefix_attention_workspace_bytes(cache, prefix_len, max_own, n_seq, n_q
 def aweq_prefix_attention(q, cache, prefix_pages, prefix_len, page_table, own_len, max_own, n_q, scale, out, ws, st=None):
     """Attention over a shared prefix and each sequence's own keys (argument marshalling only; see
     ``include/aweq.h``).  ``q``, ``out``: [n_seq * n_q, n_heads, head_dim]."""
-    n_seq, d = own_len.numel(), cache.head_dim
+    n_seq, d, dt = own_len.numel(), cache.head_dim, cache.dtype
     n_heads = q.shape[1] if q.dim() == 3 else q.shape[1] // d
-    ldq, ldo = _heads(q, n_heads, d, cache.dtype, "q"), _heads(out, n_heads, d, cache.dtype, "out")
-    ld_table = _int32_table(page_table, "page_table")
-    if q.shape[0] != n_seq * n_q or out.shape[0] != n_seq * n_q or page_table.shape[0] != n_seq:
-        raise ValueError("q and out have n_seq * n_q rows, page_table n_seq")
-    if own_len.dtype != torch.int32 or not own_len.is_contiguous():
-        raise ValueError("own_len must be int32")
+    ldq, ldo = _heads(q, n_seq * n_q, n_heads, d, dt, "q"), _heads(out, n_seq * n_q, n_heads, d, dt, "out")
+    pages, rows, per_seq, ld_table = _int32_table(page_table, "page_table")
+    if rows != n_seq:
+        raise ValueError("page_table has a row per sequence")
     if prefix_len:
         _want(prefix_pages, torch.int32, -(-prefix_len // cache.page_size), "prefix_pages")
-    _check(_lib.aweq_prefix_attention(_ptr(q), ldq, cache.ref, _ptr(prefix_pages), prefix_len, _ptr(page_table),
-                                      page_table.shape[1], ld_table, _ptr(own_len), max_own, n_seq, n_q, n_heads, scale,
-                                      _ptr(out), ldo, _ptr(ws), ws.numel(), _ptr(st), _stream()))
+    rc = _lib.aweq_prefix_attention(q.data_ptr(), ldq, cache.ref, _ptr(prefix_pages), prefix_len, pages, per_seq, ld_table,
+                                    _int32_rows(own_len, n_seq, "own_len"), max_own, n_seq, n_q, n_heads, scale, out.data_ptr(), ldo,
+                                    _ptr(ws), ws.numel(), _ptr(st), _stream())
+    if rc:
+        raise AweqError(rc)
     return out
 
 

@@ -578,7 +578,8 @@ template <class D, int DP, int WM, bool OWN>
 static aweq_status units_launch(const AttentionArgs &a, const AttentionPlan &p, unsigned char *ws, cudaStream_t stream)
 {
     constexpr int smem = kAtStages * attention_stage_bytes<DP>();
-    AWEQ_CUDA_OK(cudaFuncSetAttribute(attention_units_kernel<D, DP, WM, OWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static std::atomic<unsigned long long> allowed{0};
+    AWEQ_CUDA_OK(allow_smem(attention_units_kernel<D, DP, WM, OWN>, smem, allowed));
     AWEQ_LAUNCH((attention_units_kernel<D, DP, WM, OWN>), dim3((unsigned)(OWN ? p.own_ctas : p.pre_ctas)), dim3(kAtThreads), smem, stream,
                 a, p, ws, OWN && p.pre_ctas > 0);
     return AWEQ_OK;

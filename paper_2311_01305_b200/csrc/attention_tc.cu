@@ -374,7 +374,8 @@ static aweq_status tc_launch(const AttentionArgs &a, const AttentionPlan &p, uns
     if (rc == AWEQ_OK)
         rc = tma_pool_map(&mv, a.cv, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, p.box);
     if (rc != AWEQ_OK) return rc;
-    AWEQ_CUDA_OK(cudaFuncSetAttribute(attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTcSmem));
+    static std::atomic<unsigned long long> allowed{0};
+    AWEQ_CUDA_OK(allow_smem(attention_tc_kernel<D>, kTcSmem, allowed));
     AWEQ_LAUNCH(attention_tc_kernel<D>, dim3((unsigned)p.pre_ctas), dim3(kTcThreads), kTcSmem, stream, a, p, mk, mv, ws);
     return AWEQ_OK;
 }

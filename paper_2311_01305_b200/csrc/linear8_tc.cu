@@ -254,7 +254,8 @@ static aweq_status big_launch(const Linear8Args &a, cudaStream_t stream)
     if (rc == AWEQ_OK) rc = tma_bytes_map(&w0, a.W, a.O, a.K, a.ldw, 128);
     if (rc == AWEQ_OK) rc = tma_bytes_map(&w1, a.W, a.O, a.K, a.ldw, 120);
     if (rc != AWEQ_OK) return rc;
-    AWEQ_CUDA_OK(cudaFuncSetAttribute(linear8_big_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBigSmem));
+    static std::atomic<unsigned long long> allowed{0};
+    AWEQ_CUDA_OK(allow_smem(linear8_big_kernel<D>, kBigSmem, allowed));
     const int mt = (int)((a.N + 255) / 256), nt = (a.O + kBigCols - 1) / kBigCols;
     const long long tiles = (long long)mt * nt;
     const unsigned pairs = (unsigned)(tiles < kSmCount / 2 ? tiles : kSmCount / 2);
@@ -507,7 +508,8 @@ static aweq_status split_launch(const Linear8Args &a, SplitPlan plan, cudaStream
     aweq_status rc = tma_bytes_map(&mx, a.X, a.N, a.K, a.ldx, plan.box);
     if (rc == AWEQ_OK) rc = tma_bytes_map(&mw, a.W, a.O, a.K, a.ldw, plan.bn);
     if (rc != AWEQ_OK) return rc;
-    AWEQ_CUDA_OK(cudaFuncSetAttribute(linear8_split_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSplitSmem));
+    static std::atomic<unsigned long long> allowed{0};
+    AWEQ_CUDA_OK(allow_smem(linear8_split_kernel<D>, kSplitSmem, allowed));
     const dim3 grid((unsigned)plan.slices, (unsigned)((a.O + plan.bn - 1) / plan.bn), (unsigned)((a.N + 128 * plan.mb - 1) / (128 * plan.mb)));
     const int vec = (a.ldo % 2 == 0) && ((reinterpret_cast<uintptr_t>(a.out) & 3) == 0);
     const cudaError_t e = launch_pdl_cluster(linear8_split_kernel<D>, grid, dim3(256), kSplitSmem, stream, (unsigned)plan.slices, a, mx,
