@@ -5,9 +5,10 @@
 // sequence (G heads to a key head).  An item is a tile of rows with all its keys; a unit is a tile of 64 of them.
 // The units of all items in a row are dealt out evenly to a grid that fills the device once, so a CTA streams
 // through parts of one or several items without ever draining its copies, whatever the lengths are (the own ones are
-// known on the device only).  Where a CTA leaves an item it writes a record (maximum m, sum l, output o of the keys it
-// has seen, for each row).  One launch for the prefix (this kernel, or attention_tc.cu), one for the own keys, which starts
-// while the first still runs, and one that joins the records of a row:
+// known on the device only): so many CTAs take the prefix and so many the own keys as their units ask for.  Where a CTA
+// leaves an item it writes a record (maximum m, sum l, output o of the keys it has seen, for each row).  A prefix with many
+// rows goes to a launch of its own (attention_tc.cu), which the own keys' CTAs follow as it ends.  The last launch joins the
+// records of a row:
 //   m = max m_i,  l = sum 2^(m_i - m) l_i,  out = sum 2^(m_i - m) o_i / l      (scores in units of log 2)
 //
 // In a CTA four warps walk the units, look up pages and copy the rows of K and V into a ring of stages (cp.async: a bulk
@@ -71,15 +72,15 @@ static AttentionPlan attention_plan(const aweq_kv_cache *c, long long prefix_len
     p.own_rec = (int)(own_rows < p.own_tile ? own_rows : p.own_tile);
     p.pre_tiles = (prefix_len + p.pre_unit - 1) / p.pre_unit;
     p.pre_units = p.pre_tiles * n_kv * p.pre_rt;
-    const long long own_items = n_seq * n_kv * p.own_rt, slots = kSmCount * kAtCtasPerSm;
-    const double own_most = (double)own_items * (double)((max_own + p.unit - 1) / p.unit);
-    p.own_ctas = own_most < (double)slots ? (int)own_most : (int)slots;
-    const long long pre_slots = p.tensor ? kSmCount : slots;
-    p.pre_ctas = p.pre_units < pre_slots ? (int)p.pre_units : (int)pre_slots;
+    const long long own_items = n_seq * n_kv * p.own_rt;
+    const double most = (p.tensor ? 0.0 : (double)p.pre_units) + (double)own_items * (double)((max_own + p.unit - 1) / p.unit);
+    p.ctas = kSmCount * kAtCtasPerSm;
+    if (most < p.ctas) p.ctas = (int)most;
+    p.tc_ctas = !p.tensor ? 0 : p.pre_units < kSmCount ? (int)p.pre_units : kSmCount;
     // an item makes a record, and one more for every CTA boundary inside it
-    const size_t pre_kept = p.pre_tiles ? (size_t)((long long)n_kv * p.pre_rt + p.pre_ctas) * p.pre_rec : 0;
-    const size_t own_kept = (size_t)(own_items + p.own_ctas) * p.own_rec;
-    size_t off = up256((size_t)(n_seq + 1) * 8);
+    const size_t pre_kept = p.pre_tiles ? (size_t)((long long)n_kv * p.pre_rt + (p.tensor ? p.tc_ctas : p.ctas)) * p.pre_rec : 0;
+    const size_t own_kept = (size_t)(own_items + p.ctas) * p.own_rec;
+    size_t off = up256((size_t)(n_seq + 2) * 8);
     p.off_pre_o = off; off += up256(pre_kept * head_dim * 4);
     p.off_pre_ml = off; off += up256(pre_kept * 8);
     p.off_own_o = off; off += up256(own_kept * head_dim * 4);
@@ -259,42 +260,30 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
 template <int DP>
 __host__ __device__ constexpr int attention_stage_bytes() { return (2 * kAtTile + 16) * at_pitch(DP); }     // K, V, 16 rows of q
 
-// `chained`: behind the prefix's kernel.  This one then starts without waiting for it, and ends after it for the join's sake.
+struct AttentionRing {
+    uint64_t full[kAtStages], empty[kAtStages];
+    AttentionUnit unit[kAtStages];
+    float2 ml[64];
+};
+
+// CTA `cta` of the `ctas` that have the prefix / the own keys.
 template <class D, int DP, int WM, bool OWN>
-__global__ void __launch_bounds__(kAtThreads, kAtCtasPerSm)
-attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned char *ws, bool chained)
+__device__ __forceinline__ void attention_part(const AttentionArgs &a, const AttentionPlan &p, int cta, int ctas, long long total,
+                                               unsigned char *ws, unsigned char *smem, AttentionRing &ring)
 {
     constexpr int PITCH = at_pitch(DP), STAGE = attention_stage_bytes<DP>(), KW = 4 / WM;
     constexpr bool kStagedQ = OWN && WM == 1;                   // short items: their rows of q come with their first unit
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ uint64_t full[kAtStages], empty[kAtStages];
-    __shared__ AttentionUnit unit[kAtStages];
-    __shared__ float2 sh_ml[64];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int hd = a.head_dim, cta = blockIdx.x, G = a.n_heads / a.n_kv, rec_rows = OWN ? p.own_rec : p.pre_rec;
-    if (tid == 0) {
-        for (int s = 0; s < kAtStages; ++s) {
-            mbar_init(&full[s], 129);                           // every copying lane, and the unit itself
-            mbar_init(&empty[s], 4);
-        }
-        mbar_init_fence();
-    }
-    if (hd < DP)                                                // what no copy writes: columns past head_dim
-        for (int i = tid; i < kAtStages * (2 * kAtTile + 16) * ((DP - hd) / 8); i += kAtThreads) {
-            const int r = i / ((DP - hd) / 8);                  // a stage is a multiple of eight rows
-            *reinterpret_cast<uint4 *>(smem + r * PITCH + at_piece(r, hd / 8 + i % ((DP - hd) / 8))) = make_uint4(0, 0, 0, 0);
-        }
-    __syncthreads();
-    if (!chained) {
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    }
+    const int hd = a.head_dim, G = a.n_heads / a.n_kv, rec_rows = OWN ? p.own_rec : p.pre_rec;
+    uint64_t *const full = ring.full, *const empty = ring.empty;
+    AttentionUnit *const unit = ring.unit;
+    float2 *const sh_ml = ring.ml;
 
     if (warp >= 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAtCopyRegs));
         const int cw = warp - 4;
         AttentionWalk<OWN> w;
-        int left = attention_begin<OWN>(a, p, cta, cta == 0 && cw == 0, ws, w);
+        int left = attention_begin<OWN>(a, p, cta, ctas, total, w);
         if (left == 0) {
             if (cw == 0 && lane == 0) unit[0].stop = 2;
             mbar_arrive(&full[0]);
@@ -358,7 +347,6 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
             for (int i = 0; i < kAtStages; ++i) mbar_wait(&full[i], ph ^ (i >= s ? 1u : 0u));
             if (lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
         }
-        if (chained && cta == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
     }
 
@@ -488,19 +476,72 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
     }
 }
 
-// One CTA per row (token, head).  A row has a handful of records in the usual case and some hundreds when one key head's
-// keys are spread over the whole device, so all warps look at all (m, l), then share the outputs, eight loads under way.
-template <class D>
+// `chained`: behind the prefix's tensor kernel.  This one then starts without waiting for it, and ends after it for the
+// join's sake.
+template <class D, int DP, int WMP, int WMO>
+__global__ void __launch_bounds__(kAtThreads, kAtCtasPerSm)
+attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned char *ws, bool chained)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ AttentionRing ring;
+    const int tid = threadIdx.x, hd = a.head_dim, cta = blockIdx.x;
+    if (tid == 0) {
+        for (int s = 0; s < kAtStages; ++s) {
+            mbar_init(&ring.full[s], 129);                      // every copying lane, and the unit itself
+            mbar_init(&ring.empty[s], 4);
+        }
+        mbar_init_fence();
+    }
+    if (hd < DP)                                                // what no copy writes: columns past head_dim
+        for (int i = tid; i < kAtStages * (2 * kAtTile + 16) * ((DP - hd) / 8); i += kAtThreads) {
+            const int r = i / ((DP - hd) / 8);                  // a stage is a multiple of eight rows
+            *reinterpret_cast<uint4 *>(smem + r * at_pitch(DP) + at_piece(r, hd / 8 + i % ((DP - hd) / 8))) = make_uint4(0, 0, 0, 0);
+        }
+    __syncthreads();
+    if (!chained) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
+    // CTAs for the prefix, by the time its units take (units of 16, 32 and 64 rows: as 4 to 5 to 8) and the changes from own
+    // item to own item (as much as a unit each: 16 x 8192 shared keys and 512 items of one unit, 43 us without them, 37 with)
+    const bool lead = cta == 0 && tid < 32;
+    long long *const start = reinterpret_cast<long long *>(ws);
+    const long long own = own_units(a, p, lead, start), pre = p.tensor ? 0 : p.pre_units;
+    const float pre_cost = (float)pre * (WMP == 1 ? 4 : WMP == 2 ? 5 : 8);
+    const float own_cost = ((float)own + fminf((float)own, (float)a.n_seq * (float)(a.n_kv * p.own_rt))) * (WMO == 1 ? 4 : WMO == 2 ? 5 : 8);
+    int split = pre == 0 ? 0 : own == 0 ? p.ctas : min(max((int)(p.ctas * (pre_cost / (pre_cost + own_cost)) + 0.5f), 1), p.ctas - 1);
+    if (split > pre) split = (int)pre;
+    if (lead && tid == 0) {
+        start[a.n_seq] = own;
+        start[a.n_seq + 1] = split;
+    }
+    if (cta < split) attention_part<D, DP, WMP, false>(a, p, cta, split, pre, ws, smem, ring);
+    else attention_part<D, DP, WMO, true>(a, p, cta - split, p.ctas - split, own, ws, smem, ring);
+    if (chained && cta == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// WARPS warps per row (token, head), each with eight records' outputs under way.  A row has a handful of records in the usual
+// case and some hundreds when one key head's keys are spread over the whole device; then there are few rows.
+template <class D, int WARPS>
 __global__ void __launch_bounds__(128)
 attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsigned char *__restrict__ ws)
 {
     __shared__ float part[4][128], part_l[4];
     pdl_begin();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.n_heads / a.n_kv, hd = a.head_dim;
-    const unsigned r = blockIdx.x, tok = r / (unsigned)a.n_heads, h = r % (unsigned)a.n_heads, kh = h / (unsigned)G, b = tok / (unsigned)a.n_q;
+    const int lane = threadIdx.x & 31, warp = (int)(threadIdx.x >> 5) % WARPS, G = a.n_heads / a.n_kv, hd = a.head_dim;
+    const unsigned r = blockIdx.x * (4 / WARPS) + (threadIdx.x >> 5) / WARPS;
+    if (WARPS == 1 && r >= p.rows) return;
+    const unsigned tok = r / (unsigned)a.n_heads, h = r % (unsigned)a.n_heads, kh = h / (unsigned)G, b = tok / (unsigned)a.n_q;
     const long long *start = reinterpret_cast<const long long *>(ws);
-    const long long total = p.own_ctas ? start[a.n_seq] : 0, own0 = p.own_ctas ? start[b] : 0, own1 = p.own_ctas ? start[b + 1] : 0;
-    const AttentionDeal deal(total, p.own_ctas), pre_deal(p.pre_units, p.pre_ctas);
+    long long total = 0, own0 = 0, own1 = 0;
+    int split = p.tc_ctas;
+    if (p.ctas) {
+        total = start[a.n_seq];
+        own0 = start[b];
+        own1 = b + 1 < a.n_seq ? start[b + 1] : total;
+        if (!p.tensor) split = (int)start[a.n_seq + 1];
+    }
+    const AttentionDeal deal(total, p.tensor ? p.ctas : p.ctas - split), pre_deal(p.pre_units, split);
     const int tiles = (int)div_units(own1 - own0, a.n_kv * p.own_rt);
     // the rows of this one's records: the prefix item's, then the own item's
     long long pre0 = 0, rec0 = 0;
@@ -525,20 +566,26 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
     const float *const pre_o = reinterpret_cast<const float *>(ws + p.off_pre_o), *const own_o = reinterpret_cast<const float *>(ws + p.off_own_o);
     const float2 *const pre_ml = reinterpret_cast<const float2 *>(ws + p.off_pre_ml), *const own_ml = reinterpret_cast<const float2 *>(ws + p.off_own_ml);
     auto ml = [&](int i) { return i < n_pre ? pre_ml[pre0 + (long long)i * pre_step] : own_ml[rec0 + (long long)(i - n_pre) * own_step]; };
-    auto out = [&](int i) { return i < n_pre ? pre_o + (pre0 + (long long)i * pre_step) * hd : own_o + (rec0 + (long long)(i - n_pre) * own_step) * hd; };
+    constexpr int U = 8;
+    const bool in = lane * 4 < hd;
+    float4 v[U];
+    auto fetch = [&](int i0) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int i = i0 + j;
+            const float *src = i < n_pre ? pre_o + (pre0 + (long long)i * pre_step) * hd : own_o + (rec0 + (long long)(i - n_pre) * own_step) * hd;
+            v[j] = in && i < n_all ? *reinterpret_cast<const float4 *>(src + lane * 4) : make_float4(0, 0, 0, 0);
+        }
+    };
+    fetch(warp * U);                                            // under way while the maximum is found
     float m = -CUDART_INF_F;
     for (int i = lane; i < n_all; i += 32) m = fmaxf(m, ml(i).x);
     for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
     const float base = m == -CUDART_INF_F ? 0.0f : m;
-    constexpr int U = 8;
     float l = 0.0f;
     float4 o = make_float4(0, 0, 0, 0);
-    const bool in = lane * 4 < hd;
-    for (int i0 = warp * U; i0 < n_all; i0 += 4 * U) {
-        float4 v[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j)
-            v[j] = in && i0 + j < n_all ? *reinterpret_cast<const float4 *>(out(i0 + j) + lane * 4) : make_float4(0, 0, 0, 0);
+    for (int i0 = warp * U; i0 < n_all; i0 += WARPS * U) {
+        if (i0 != warp * U) fetch(i0);
         float w = 0.0f, wl = 0.0f;
         if (lane < U && i0 + lane < n_all) {
             const float2 x = ml(i0 + lane);
@@ -552,57 +599,63 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
             if (i0 + j < n_all) { o.x += f * v[j].x; o.y += f * v[j].y; o.z += f * v[j].z; o.w += f * v[j].w; }
         }
     }
-    if (n_all > U) {
+    if (WARPS > 1) {
         if (in) *reinterpret_cast<float4 *>(&part[warp][lane * 4]) = o;
         if (lane == 0) part_l[warp] = l;
         __syncthreads();
+        if (warp) return;
         l = 0.0f;
         o = make_float4(0, 0, 0, 0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < WARPS; ++k) {
             l += part_l[k];
             if (in) {
-                const float4 v = *reinterpret_cast<const float4 *>(&part[k][lane * 4]);
-                o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+                const float4 x = *reinterpret_cast<const float4 *>(&part[k][lane * 4]);
+                o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
             }
         }
     }
-    if (warp == 0 && in) {
+    if (in) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;          // no key at all: zeros
         *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.ldo + (long long)h * hd + lane * 4) =
             make_uint2(D::encode2(o.x * inv, o.y * inv), D::encode2(o.z * inv, o.w * inv));
     }
 }
 
-template <class D, int DP, int WM, bool OWN>
+template <class D, int DP, int WMP, int WMO>
 static aweq_status units_launch(const AttentionArgs &a, const AttentionPlan &p, unsigned char *ws, cudaStream_t stream)
 {
     constexpr int smem = kAtStages * attention_stage_bytes<DP>();
     static std::atomic<unsigned long long> allowed{0};
-    AWEQ_CUDA_OK(allow_smem(attention_units_kernel<D, DP, WM, OWN>, smem, allowed));
-    AWEQ_LAUNCH((attention_units_kernel<D, DP, WM, OWN>), dim3((unsigned)(OWN ? p.own_ctas : p.pre_ctas)), dim3(kAtThreads), smem, stream,
-                a, p, ws, OWN && p.pre_ctas > 0);
+    AWEQ_CUDA_OK(allow_smem(attention_units_kernel<D, DP, WMP, WMO>, smem, allowed));
+    AWEQ_LAUNCH((attention_units_kernel<D, DP, WMP, WMO>), dim3((unsigned)p.ctas), dim3(kAtThreads), smem, stream, a, p, ws, p.tensor != 0);
     return AWEQ_OK;
 }
 
-template <class D, bool OWN>
+template <class D, int DP>
 static aweq_status units_dispatch(const AttentionArgs &a, const AttentionPlan &p, unsigned char *ws, cudaStream_t stream)
 {
-    const int wm = (OWN ? p.own_tile : p.pre_tile) / 16;
-#define AWEQ_UNITS(DP) \
-    (wm == 1 ? units_launch<D, DP, 1, OWN>(a, p, ws, stream) : wm == 2 ? units_launch<D, DP, 2, OWN>(a, p, ws, stream) : units_launch<D, DP, 4, OWN>(a, p, ws, stream))
-    return p.dp == 64 ? AWEQ_UNITS(64) : p.dp == 96 ? AWEQ_UNITS(96) : AWEQ_UNITS(128);
-#undef AWEQ_UNITS
+    // without a prefix here its side is what the own keys have; a prefix has at least the rows of a sequence
+    const int wmo = p.own_tile / 16, wmp = p.tensor || !p.pre_tiles ? wmo : p.pre_tile / 16;
+    if (wmo == 1) {
+        if (wmp == 1) return units_launch<D, DP, 1, 1>(a, p, ws, stream);
+        return wmp == 2 ? units_launch<D, DP, 2, 1>(a, p, ws, stream) : units_launch<D, DP, 4, 1>(a, p, ws, stream);
+    }
+    if (wmo == 2) return wmp == 2 ? units_launch<D, DP, 2, 2>(a, p, ws, stream) : units_launch<D, DP, 4, 2>(a, p, ws, stream);
+    return units_launch<D, DP, 4, 4>(a, p, ws, stream);
 }
 
 template <class D>
 static aweq_status attention_launch(const AttentionArgs &a, const AttentionPlan &p, aweq_dtype dt, unsigned char *ws, cudaStream_t stream)
 {
-    aweq_status rc = AWEQ_OK;
-    if (p.pre_ctas) rc = p.tensor ? run_attention_tc(a, p, dt, ws, stream) : units_dispatch<D, false>(a, p, ws, stream);
-    if (rc == AWEQ_OK && p.own_ctas) rc = units_dispatch<D, true>(a, p, ws, stream);
+    aweq_status rc = p.tensor ? run_attention_tc(a, p, dt, ws, stream) : AWEQ_OK;
+    if (rc == AWEQ_OK && p.ctas)
+        rc = p.dp == 64 ? units_dispatch<D, 64>(a, p, ws, stream) : p.dp == 96 ? units_dispatch<D, 96>(a, p, ws, stream) : units_dispatch<D, 128>(a, p, ws, stream);
     if (rc != AWEQ_OK) return rc;
-    AWEQ_LAUNCH(attention_join_kernel<D>, dim3((unsigned)p.rows), dim3(128), 0, stream, a, p, (const unsigned char *)ws);
+    if (p.rows >= 4 * kSmCount)
+        AWEQ_LAUNCH((attention_join_kernel<D, 1>), dim3((unsigned)((p.rows + 3) / 4)), dim3(128), 0, stream, a, p, (const unsigned char *)ws);
+    else
+        AWEQ_LAUNCH((attention_join_kernel<D, 4>), dim3((unsigned)p.rows), dim3(128), 0, stream, a, p, (const unsigned char *)ws);
     return AWEQ_OK;
 }
 

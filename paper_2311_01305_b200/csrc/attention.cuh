@@ -17,9 +17,10 @@ struct AttentionPlan {
     int pre_tile, own_tile;      // rows of a prefix / own item
     int pre_rt, own_rt;          // row tiles per key head / per sequence and key head
     int pre_rec, own_rec;        // rows of a record
-    int pre_ctas, own_ctas;      // the two grids; 0: no prefix / no own keys
+    int ctas;                    // grid of attention.cu's kernel
+    int tc_ctas;                 // tensor: grid of attention_tc.cu's
     long long pre_tiles, pre_units, rows;
-    // scratch: start of each sequence's units (long long[n_seq + 1], the total last), records
+    // scratch: start of each sequence's own units, their number, the CTAs of the prefix (long long[n_seq + 2]); records
     size_t off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
 };
 
@@ -105,16 +106,44 @@ struct AttentionWalk {
     }
 };
 
-// A warp finds its CTA's first unit (every lane gets the same) and the number of its units.  `lead`: the one warp of the
-// grid that counts bad lengths and leaves the starts of the sequences for the join.
+// Tiles of 32 sequences: the lane's own length and tiles, and the tiles before it.
+__device__ __forceinline__ long long scan_tiles(const AttentionArgs &a, const AttentionPlan &p, int b, bool count, int *len, int *n)
+{
+    *len = b < (int)a.n_seq ? own_length(a, b, count) : 0;
+    *n = tiles_of(*len, p.unit);
+    int sum = *n;                                               // 32 lengths of at most 2^31 keys: below 2^31 tiles
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, sum, x);
+        if ((int)(threadIdx.x & 31) >= x) sum += y;
+    }
+    return (long long)(sum - *n);
+}
+// The number of own units; every warp computes it.  `lead`: the one warp of the grid that counts bad lengths and leaves the
+// starts of the sequences for the join.
+__device__ __forceinline__ long long own_units(const AttentionArgs &a, const AttentionPlan &p, bool lead, long long *start)
+{
+    const int lane = threadIdx.x & 31, n_seq = (int)a.n_seq, per_seq = a.n_kv * p.own_rt;
+    long long total = 0;
+    for (int b0 = 0; b0 < n_seq; b0 += 32) {
+        int len, n;
+        const long long before = scan_tiles(a, p, b0 + lane, lead, &len, &n);
+        if (lead && b0 + lane < n_seq) start[b0 + lane] = (total + before) * per_seq;
+        total += __shfl_sync(0xffffffffu, before + n, 31);
+    }
+    return total * per_seq;
+}
+
+// A warp finds the first unit of CTA `cta` of `ctas` (every lane gets the same) and the number of its units.
 template <bool OWN>
-__device__ __forceinline__ int attention_begin(const AttentionArgs &a, const AttentionPlan &p, int cta, bool lead, unsigned char *ws,
+__device__ __forceinline__ int attention_begin(const AttentionArgs &a, const AttentionPlan &p, int cta, int ctas, long long total,
                                                AttentionWalk<OWN> &w)
 {
     w.at = {};
+    const AttentionDeal deal(total, ctas);
+    if (cta >= deal.ctas) return 0;
+    const long long u0 = deal.first(cta);
     if (!OWN) {
-        const AttentionDeal deal(p.pre_units, p.pre_ctas);
-        const long long u0 = deal.first(cta);
         const int item = (int)div_units(u0, (int)p.pre_tiles);
         w.at.kh = item / p.pre_rt;
         w.at.rt = item % p.pre_rt;
@@ -124,35 +153,10 @@ __device__ __forceinline__ int attention_begin(const AttentionArgs &a, const Att
         return (int)(deal.first(cta + 1) - u0);
     }
     const int lane = threadIdx.x & 31, n_seq = (int)a.n_seq, per_seq = a.n_kv * p.own_rt;
-    long long *const start = reinterpret_cast<long long *>(ws);
-    // tiles of 32 sequences, the lane's own and those before it
-    int len = 0, n = 0;
-    auto scan = [&](int b, bool count) {
-        len = b < n_seq ? own_length(a, b, count) : 0;
-        n = tiles_of(len, p.unit);
-        int sum = n;                                            // 32 lengths of at most 2^31 keys: below 2^31 tiles
-#pragma unroll
-        for (int x = 1; x < 32; x <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, sum, x);
-            if (lane >= x) sum += y;
-        }
-        return (long long)(sum - n);
-    };
-    long long total = 0, before = 0;
-    for (int b0 = 0; b0 < n_seq; b0 += 32) {
-        before = scan(b0 + lane, lead);
-        if (lead && b0 + lane < n_seq) start[b0 + lane] = (total + before) * per_seq;
-        total += __shfl_sync(0xffffffffu, before + n, 31);
-    }
-    total *= per_seq;
-    if (lead && lane == 0) start[n_seq] = total;
-    const AttentionDeal deal(total, p.own_ctas);
-    if (cta >= deal.ctas) return 0;
-    const long long u0 = deal.first(cta);
     long long passed = 0;
     for (int b0 = 0;; b0 += 32) {
-        if (n_seq > 32) before = scan(b0 + lane, false);        // else still in the registers
-        const long long mine = passed + before * per_seq;
+        int len, n;
+        const long long mine = passed + scan_tiles(a, p, b0 + lane, false, &len, &n) * per_seq;
         const uint32_t here = __ballot_sync(0xffffffffu, u0 >= mine && u0 < mine + (long long)n * per_seq);
         if (here) {
             const int src = __ffs(here) - 1, within = (int)(u0 - __shfl_sync(0xffffffffu, mine, src));

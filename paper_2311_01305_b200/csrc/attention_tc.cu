@@ -80,7 +80,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
     // the kernel of the own keys may start as soon as what came before this one is done: it does not wait for this one
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const AttentionDeal deal(p.pre_units, p.pre_ctas);
+    const AttentionDeal deal(p.pre_units, p.tc_ctas);
     const long long u0 = deal.first(cta);
     const int units = (int)(deal.first(cta + 1) - u0), item0 = (int)div_units(u0, (int)p.pre_tiles), tile0 = (int)(u0 - item0 * p.pre_tiles);
     // the CTA's items are item0, item0 + 1, ...: key head item / pre_rt, row tile item % pre_rt
@@ -376,7 +376,7 @@ static aweq_status tc_launch(const AttentionArgs &a, const AttentionPlan &p, uns
     if (rc != AWEQ_OK) return rc;
     static std::atomic<unsigned long long> allowed{0};
     AWEQ_CUDA_OK(allow_smem(attention_tc_kernel<D>, kTcSmem, allowed));
-    AWEQ_LAUNCH(attention_tc_kernel<D>, dim3((unsigned)p.pre_ctas), dim3(kTcThreads), kTcSmem, stream, a, p, mk, mv, ws);
+    AWEQ_LAUNCH(attention_tc_kernel<D>, dim3((unsigned)p.tc_ctas), dim3(kTcThreads), kTcSmem, stream, a, p, mk, mv, ws);
     return AWEQ_OK;
 }
 
