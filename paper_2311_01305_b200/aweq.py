@@ -511,12 +511,12 @@ class KVCache:
 
 def _heads(t: torch.Tensor, n: int, n_heads: int, head_dim: int, dtype, what: str) -> int:
     """Row pitch of [n, heads, head_dim] (or [n, heads * head_dim]) on the device with contiguous rows."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 3:
-        ok = shape[1] == n_heads and shape[2] == head_dim and stride[2] == 1 and (n_heads == 1 or stride[1] == head_dim)
+    stride = t.stride()
+    if t.shape == (n, n_heads, head_dim):
+        ok = stride[2] == 1 and (n_heads == 1 or stride[1] == head_dim)
     else:
-        ok = len(shape) == 2 and shape[1] == n_heads * head_dim and stride[1] == 1
-    if not ok or shape[0] != n or t.dtype is not dtype or not t.is_cuda:
+        ok = t.shape == (n, n_heads * head_dim) and stride[1] == 1
+    if not ok or t.dtype is not dtype or not t.is_cuda:
         raise ValueError("%s must be a %s device tensor [%d, %d, %d] with contiguous rows" % (what, dtype, n, n_heads, head_dim))
     return stride[0] if n > 1 else max(stride[0], n_heads * head_dim)
 
@@ -597,10 +597,24 @@ class PrefixAttention:
         self.n_heads, self.n_seq, self.n_q = n_heads, n_seq, n_q
         self.max_own = 0x7fffffff if max_own is None else int(max_own)
         self.scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+        if self.prefix_len:
+            _want(prefix_pages, torch.int32, -(-self.prefix_len // cache.page_size), "prefix_pages")
         nbytes = aweq_prefix_attention_workspace_bytes(cache, self.prefix_len, self.max_own, n_seq, n_q, n_heads)
         self.ws = workspace(nbytes, cache.k.device)
+        self._fixed = (cache.ref, _ptr(prefix_pages) if self.prefix_len else None, self.prefix_len)
+        self._batch = (self.max_own, n_seq, n_q, n_heads, self.scale)
+        self._scratch = (self.ws.data_ptr(), self.ws.numel())
 
     def __call__(self, q, page_table, own_len, out=None, st=None):
         out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
-        return aweq_prefix_attention(q, self.cache, self.prefix_pages, self.prefix_len, page_table, own_len, self.max_own,
-                                     self.n_q, self.scale, out, self.ws, st)
+        n, h, c = self.n_seq * self.n_q, self.n_heads, self.cache
+        ldq, ldo = _heads(q, n, h, c.head_dim, c.dtype, "q"), _heads(out, n, h, c.head_dim, c.dtype, "out")
+        pages, rows, per_seq, ld_table = _int32_table(page_table, "page_table")
+        if rows != self.n_seq:
+            raise ValueError("page_table has a row per sequence")
+        rc = _lib.aweq_prefix_attention(q.data_ptr(), ldq, *self._fixed, pages, per_seq, ld_table,
+                                        _int32_rows(own_len, self.n_seq, "own_len"), *self._batch, out.data_ptr(), ldo, *self._scratch,
+                                        _ptr(st), _stream())
+        if rc:
+            raise AweqError(rc)
+        return out
