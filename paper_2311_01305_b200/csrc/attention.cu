@@ -264,6 +264,7 @@ struct AttentionRing {
     uint64_t full[kAtStages], empty[kAtStages];
     AttentionUnit unit[kAtStages];
     float2 ml[64];
+    volatile int gave_up;        // a computing warp has
 };
 
 // CTA `cta` of the `ctas` that have the prefix / the own keys.
@@ -360,10 +361,20 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
     const float scale = a.scale * 1.4426950408889634f;
     int s = 0;
     uint32_t ph = 0;
+    // The four warps wait for one another where they share rows; one that gives up says so and arrives for the others.
+    auto meet = [&] {
+        named_bar_sync(1, 128);
+        return !ring.gave_up;
+    };
     for (;;) {
         const bool ok = mbar_wait(&full[s], ph);
         if (!__all_sync(0xffffffffu, ok)) {
-            if (lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
+            if (lane == 0) {
+                if (a.st) atomicAdd(&a.st->wait_timeout, 1ull);
+                ring.gave_up = 1;
+            }
+            __syncwarp();
+            named_bar_arrive(1, 128);
             return;
         }
         const AttentionUnit it = unit[s];
@@ -424,7 +435,7 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
                     st.l[h] = quad_sum(st.l[h]);
                     if (t == 0) sh_ml[gw + 8 * h] = make_float2(st.m[h], st.l[h]);
                 }
-                named_bar_sync(1, 128);                         // all have read the stage, and all (m, l) are there
+                if (!meet()) return;                            // all have read the stage, and all (m, l) are there
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int r = wrow + g + 8 * h;
@@ -444,7 +455,7 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
                     for (int n = 0; n < DP / 8; ++n)
                         *reinterpret_cast<float2 *>(ex + (gw + 8 * h) * DP + n * 8 + 2 * t) = make_float2(o[n][2 * h] * mine, o[n][2 * h + 1] * mine);
                 }
-                named_bar_sync(1, 128);
+                if (!meet()) return;
                 for (int i = tid; i < nrows * (DP / 4); i += 128) {
                     const int r = i / (DP / 4), c = i % (DP / 4) * 4;
                     float4 v = make_float4(0, 0, 0, 0);
@@ -490,6 +501,7 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
             mbar_init(&ring.full[s], 129);                      // every copying lane, and the unit itself
             mbar_init(&ring.empty[s], 4);
         }
+        ring.gave_up = 0;
         mbar_init_fence();
     }
     if (hd < DP)                                                // what no copy writes: columns past head_dim

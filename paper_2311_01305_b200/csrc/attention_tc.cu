@@ -40,6 +40,7 @@ struct TcShared {
     uint64_t full[kTcMaxStages], empty[kTcMaxStages], s_full[2], p_ready[2], pv_done[2], q_ready[2], item_done[4], o_full, o_free;
     TcUnit unit[kTcMaxStages];
     uint32_t tmem;
+    volatile int gave_up[4];             // by TMEM quarter: a softmax warp has
     float top[2][2][128], sum[128];      // the halves' maxima (by unit parity), one half's sum
 };
 constexpr size_t kTcSmem = 1024 + kTcStageBytes + sizeof(TcShared);
@@ -67,7 +68,10 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
         }
         mbar_init(&sh.o_full, 1);
         mbar_init(&sh.o_free, 4);
-        for (int i = 0; i < 4; ++i) mbar_init(&sh.item_done[i], 8);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&sh.item_done[i], 8);
+            sh.gave_up[i] = 0;
+        }
         mbar_init_fence();
         tma_prefetch_map(&mapK);
         tma_prefetch_map(&mapV);
@@ -196,6 +200,11 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
         int s = 0, u = 0, nrows = 0;
         uint32_t ph = 0;
         long long rec = 0;
+        // The two warps that share 32 rows wait for one another; one that gives up says so and arrives for the other.
+        auto meet = [&] {
+            named_bar_sync(2 + q4, 64);
+            return !sh.gave_up[q4];
+        };
         for (;; ++u) {
             ok = mbar_wait(&sh.full[s], ph);
             if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
@@ -246,7 +255,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                 // the other half's maximum; past this barrier both have their scores in registers, so that P may overwrite them
                 float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 sh.top[u & 1][half][r] = t;
-                named_bar_sync(2 + q4, 64);
+                if (!(ok = meet())) break;
                 t = fmaxf(t, sh.top[u & 1][half ^ 1][r]) * scale;
                 if (it.fresh) m = t;
                 else if (__any_sync(0xffffffffu, t > m + kTcSlack)) {
@@ -292,7 +301,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
             if (it.leave) {
                 if (live) {
                     if (half) sh.sum[r] = l;
-                    named_bar_sync(2 + q4, 64);
+                    if (!(ok = meet())) break;
                     if (!half && r < nrows)
                         reinterpret_cast<float2 *>(ws + p.off_pre_ml)[rec + r] = make_float2(m, l + sh.sum[r]);
                 }
@@ -301,6 +310,11 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
             }
             if (it.stop) break;
             if (++s == nstages) { s = 0; ph ^= 1; }
+        }
+        if (!ok) {
+            if (lane == 0) sh.gave_up[q4] = 1;
+            __syncwarp();
+            named_bar_arrive(2 + q4, 64);
         }
     } else {
         // -------------------------------------------------------------- Q in, O out: a thread per row

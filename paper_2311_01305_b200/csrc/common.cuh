@@ -112,17 +112,6 @@ __device__ __forceinline__ bool has_exponent(const uint4 &v, uint32_t mask)
     for (int i = 0; i < 4; ++i) any |= (w[i] & mask) == mask || (w[i] >> 16 & mask) == mask;
     return any;
 }
-// ... and those elements set to zero
-__device__ __forceinline__ void drop_exponent(uint4 &v, uint32_t mask)
-{
-    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if ((w[i] & mask) == mask) w[i] &= 0xffff0000u;
-        if ((w[i] >> 16 & mask) == mask) w[i] &= 0x0000ffffu;
-    }
-    v = make_uint4(w[0], w[1], w[2], w[3]);
-}
 struct F16 {
     using T2 = __half2;
     static constexpr bool kBf16 = false;
@@ -142,7 +131,6 @@ struct F16 {
     }
     static __device__ __forceinline__ float one(uint16_t b) { return __half2float(__ushort_as_half(b)); }
     static __device__ __forceinline__ bool any_nonfinite(const uint4 &v) { return has_exponent(v, 0x7C00u); }
-    static __device__ __forceinline__ void drop_nonfinite(uint4 &v) { drop_exponent(v, 0x7C00u); }
     static __device__ __forceinline__ uint16_t encode(float f) { return __half_as_ushort(__float2half_rn(f)); }
     static __device__ __forceinline__ uint32_t encode2(float lo, float hi)
     {
@@ -163,7 +151,6 @@ struct BF16 {
     }
     static __device__ __forceinline__ float one(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
     static __device__ __forceinline__ bool any_nonfinite(const uint4 &v) { return has_exponent(v, 0x7F80u); }
-    static __device__ __forceinline__ void drop_nonfinite(uint4 &v) { drop_exponent(v, 0x7F80u); }
     static __device__ __forceinline__ uint16_t encode(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
     static __device__ __forceinline__ uint32_t encode2(float lo, float hi)
     {
@@ -304,6 +291,11 @@ __device__ __forceinline__ void named_bar_sync(int id, int threads)
 }
 
 // barrier over `threads` threads that also ANDs a predicate (all arrive, all get the same answer)
+// Arrives without waiting: for a warp that gives up where others will come to the barrier.
+__device__ __forceinline__ void named_bar_arrive(int id, int threads)
+{
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
 __device__ __forceinline__ bool named_bar_and(int id, int threads, bool pred)
 {
     uint32_t r;

@@ -116,25 +116,16 @@ __global__ void __launch_bounds__(256) linear8_stream_kernel(const Linear8Args p
 }
 
 template <class D>
-static aweq_status stream_launch(Linear8Args a, cudaStream_t stream)
+static aweq_status stream_launch(const Linear8Args &a, cudaStream_t stream)
 {
     const int nt = a.N <= 8 ? 1 : a.N <= 16 ? 2 : 4;
-    const long long most = 65535ll * 8 * nt, N = a.N;        // tokens of one launch (grid.y)
-    for (long long n0 = 0; n0 < N; n0 += most) {
-        Linear8Args b = a;
-        b.N = N - n0 < most ? N - n0 : most;
-        b.X += n0 * a.ldx;
-        b.out += n0 * a.ldo;
-        b.x_step += n0 * a.x_inc;
-        b.x_zp += n0 * a.x_inc;
-        const dim3 grid((unsigned)((a.O + 15) / 16), (unsigned)((b.N + 8 * nt - 1) / (8 * nt)));
-        if (nt == 1)
-            AWEQ_LAUNCH((linear8_stream_kernel<1, D>), grid, dim3(256), 0, stream, b);
-        else if (nt == 2)
-            AWEQ_LAUNCH((linear8_stream_kernel<2, D>), grid, dim3(256), 0, stream, b);
-        else
-            AWEQ_LAUNCH((linear8_stream_kernel<4, D>), grid, dim3(256), 0, stream, b);
-    }
+    const dim3 grid((unsigned)((a.O + 15) / 16), (unsigned)((a.N + 8 * nt - 1) / (8 * nt)));     // (few tokens: two rows at most)
+    if (nt == 1)
+        AWEQ_LAUNCH((linear8_stream_kernel<1, D>), grid, dim3(256), 0, stream, a);
+    else if (nt == 2)
+        AWEQ_LAUNCH((linear8_stream_kernel<2, D>), grid, dim3(256), 0, stream, a);
+    else
+        AWEQ_LAUNCH((linear8_stream_kernel<4, D>), grid, dim3(256), 0, stream, a);
     return AWEQ_OK;
 }
 
