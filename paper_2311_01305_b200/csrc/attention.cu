@@ -294,7 +294,7 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
         constexpr int CH = DP / 8 == 12 ? 16 : DP / 8, R = 32 / CH;
         const int mine = cw * 16 + (lane & 15), piece = lane % CH * 8;
         const uint32_t dst0 = smem_u32(smem) + cw * 16 * PITCH;
-        const uint16_t *const kp = a.ck + piece, *const vp = a.cv + piece;
+        const uint16_t *const kp = a.ck + (piece < hd ? piece : 0), *const vp = a.cv + (piece < hd ? piece : 0);
         int page = left > 0 ? w.page(a, p, mine) : -1;
         int s = 0;
         uint32_t ph = 0;
@@ -326,18 +326,17 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
                 const long long o = __shfl_sync(0xffffffffu, off, i * R + lane / CH);
                 const long long at = o < 0 ? 0 : o;
                 const int r = i * R + lane / CH;
-                if (piece < hd) {
-                    cp_async16(dst + r * PITCH + at_piece(r, lane % CH), kp + at, o >= 0);
-                    cp_async16(dst + (kAtTile + r) * PITCH + at_piece(r, lane % CH), vp + at, o >= 0);
-                }
+                // (zeros in the columns past head_dim too: an item's sums may have lain there since)
+                cp_async16(dst + r * PITCH + at_piece(r, lane % CH), kp + at, o >= 0 && piece < hd);
+                cp_async16(dst + (kAtTile + r) * PITCH + at_piece(r, lane % CH), vp + at, o >= 0 && piece < hd);
             }
             if (kStagedQ && fresh) {
                 // the item's rows of q (four a warp)
                 for (int r = cw * 4 + lane / CH; r < min(cw * 4 + 4, p.own_rec); r += R) {
                     const unsigned tok = now.b * a.n_q + (unsigned)r / (unsigned)G, head = now.kh * G + (unsigned)r % (unsigned)G;
-                    if (piece < hd)
-                        cp_async16(smem_u32(smem) + s * STAGE + (2 * kAtTile + r) * PITCH + at_piece(r, lane % CH),
-                                   a.q + (long long)tok * a.ldq + (long long)head * hd + piece, true);
+                    const uint16_t *const src = a.q + (long long)tok * a.ldq + (long long)head * hd;
+                    cp_async16(smem_u32(smem) + s * STAGE + (2 * kAtTile + r) * PITCH + at_piece(r, lane % CH),
+                               piece < hd ? src + piece : src, piece < hd);
                 }
             }
             fresh = leave;
@@ -495,7 +494,7 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ AttentionRing ring;
-    const int tid = threadIdx.x, hd = a.head_dim, cta = blockIdx.x;
+    const int tid = threadIdx.x, cta = blockIdx.x;
     if (tid == 0) {
         for (int s = 0; s < kAtStages; ++s) {
             mbar_init(&ring.full[s], 129);                      // every copying lane, and the unit itself
@@ -504,11 +503,6 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
         ring.gave_up = 0;
         mbar_init_fence();
     }
-    if (hd < DP)                                                // what no copy writes: columns past head_dim
-        for (int i = tid; i < kAtStages * (2 * kAtTile + 16) * ((DP - hd) / 8); i += kAtThreads) {
-            const int r = i / ((DP - hd) / 8);                  // a stage is a multiple of eight rows
-            *reinterpret_cast<uint4 *>(smem + r * at_pitch(DP) + at_piece(r, hd / 8 + i % ((DP - hd) / 8))) = make_uint4(0, 0, 0, 0);
-        }
     __syncthreads();
     if (!chained) {
         asm volatile("griddepcontrol.wait;" ::: "memory");

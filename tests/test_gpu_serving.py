@@ -620,6 +620,14 @@ def test_attention_long_prefix_pages_out_of_range_are_counted():
     assert aweq.read_out_of_range(st) >= 2 and aweq.read_status(st)["wait_timeout"] == 0
 
 
+@pytest.mark.parametrize("d", [8, 40, 72, 80, 88, 104, 120])
+def test_attention_many_items_of_odd_heads(d):
+    """Many items to a CTA with heads that its tiles pad: what an item leaves behind must not reach the next one's padding."""
+    lens = [(37 * b) % 150 for b in range(300)]
+    attention_check(300, 1, 16, 16, d, 0, lens, 16, torch.bfloat16)
+    attention_check(300, 1, 8, 8, d, 100, lens, 8, torch.float16)
+
+
 def test_attention_many_short_sequences():
     """Many items of one or two units to a CTA, some sequences without keys, with and without a prefix."""
     lens = [(37 * b) % 200 for b in range(200)]
