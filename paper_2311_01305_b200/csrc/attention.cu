@@ -11,12 +11,16 @@
 // records of a row:
 //   m = max m_i,  l = sum 2^(m_i - m) l_i,  out = sum 2^(m_i - m) o_i / l      (scores in units of log 2)
 //
-// In a CTA four warps walk the units, look up pages and copy the rows of K and V into a ring of stages (cp.async: a bulk
-// copy per row took 40 cycles each), 16 rows of a unit each; four other warps compute with mma.sync, with most of the
-// registers.  (With every warp doing its share of both, the lookups and copies, 1.8 us a unit, added to the 0.6 us of the
-// products; a single copying warp took 2.6 us a unit.)  Measured: 16 sequences of 1-4 thousand own keys, 32 heads of 128:
-// 122 us, 5.5 TB/s (the bound); 128 sequences of 64-256 keys 87 us, 3.9 TB/s (the change from item to item costs).
+// In a CTA four warps copy into a ring of stages and four compute with mma.sync, with most of the registers.  Units of the
+// prefix come as tiled copies of one warp; own keys, whose pages, lengths and rows of q change from item to item, as
+// 16-byte copies, 16 rows of a unit to a warp (96 sequences of 350 own keys: 43.5 us against 46 with tiled copies; 32 rows x
+// 2048 shared keys and 4800 own ones: 41.9 against 45 with 16-byte copies throughout; a bulk copy per row: 40 cycles each).
+// What bounds it: memory where the keys are many (16 sequences of 1-4 thousand own keys, 32 heads of 128: 111 us, 6.05 TB/s, 94 % of
+// a copy's rate), the changes from item to item where they are few (128 sequences of 64-256 keys: 78 us, 4.3 TB/s), and
+// the start: the code itself comes from memory, 1 us a stretch, which is why the copying loop has one place for each step
+// and the computing warps run through theirs once before the first keys are there.
 #include "attention.cuh"
+#include "tensorcore.cuh"
 
 namespace aweq {
 
@@ -135,10 +139,15 @@ __device__ __forceinline__ float quad_sum(float v)
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
-// A staged row: its 16-byte pieces permuted by the row's number modulo 8, so that eight rows' like pieces lie in
-// different banks (rows of 12 pieces are kept in 16)
+// A stage: 64 rows of K and of V in halves of 64 columns (128 bytes; one half up to a head of 64), each row's 16-byte pieces
+// permuted by the row's number modulo 8, as the tiled copies leave them, so that eight rows' like pieces lie in different banks;
+// then 16 rows of q with 16 bytes between them to the same end.
 __host__ __device__ constexpr int at_pitch(int dp) { return dp == 64 ? 128 : 256; }
-__device__ __forceinline__ uint32_t at_piece(int row, int piece) { return (uint32_t)((piece ^ (row & 7)) * 16); }
+__device__ __forceinline__ uint32_t at_kv(int row, int piece) { return (uint32_t)((piece >> 3) * (kAtTile * 128) + row * 128 + ((piece ^ row) & 7) * 16); }
+template <int DP>
+__host__ __device__ constexpr int at_q_pitch() { return DP * 2 + 16; }
+template <int DP>
+__host__ __device__ constexpr int attention_stage_bytes() { return (2 * kAtTile * at_pitch(DP) + 16 * at_q_pitch<DP>() + 1023) / 1024 * 1024; }
 
 struct AttentionState {          // of a warp's 16 rows: lanes hold rows g and g + 8
     float m[2], l[2];
@@ -147,12 +156,11 @@ struct AttentionState {          // of a warp's 16 rows: lanes hold rows g and g
 // One tile of keys for a warp's 16 rows.  WM warps of the CTA lie along the rows, 4 / WM share the keys of the tile.
 template <class D, int DP, int WM, bool OWN>
 __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const AttentionUnit &it, uint32_t ks, const uint32_t (&q)[DP / 16][4],
-                                               const int (&own_i)[2], float scale, float (&o)[DP / 8][4], AttentionState &st)
+                                               const int (&own_i)[2], float scale, float (&o)[DP / 8][4], AttentionState &st, bool boxes)
 {
     constexpr int KW = 4 / WM, NT = kAtTile / 8 / KW;           // warps along the keys, 8-key groups of a warp
-    constexpr int PITCH = at_pitch(DP);
     const int lane = threadIdx.x & 31, t = lane & 3;
-    const uint32_t vs = ks + kAtTile * PITCH;
+    const uint32_t vs = ks + kAtTile * at_pitch(DP);
     const int key0 = (int)(threadIdx.x >> 5) / WM * (NT * 8);   // this warp's keys of the tile
     float s[NT][4] = {};
 #pragma unroll
@@ -160,13 +168,20 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
 #pragma unroll
         for (int n = 0; n < NT; n += 2) {
             uint32_t b[4];          // keys n*8.. (k halves 0, 1), keys n*8 + 8.. (k halves 0, 1)
-            ldsm4(b, ks + (key0 + n * 8 + (lane & 7) + (lane >> 4) * 8) * PITCH + ((k * 2 + ((lane >> 3) & 1)) ^ (lane & 7)) * 16);
+            ldsm4(b, ks + at_kv(key0 + n * 8 + (lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1)));
             mma16<D>(s[n], q[k], b[0], b[1]);
             mma16<D>(s[n + 1], q[k], b[2], b[3]);
         }
     // keys of this warp's share that a row sees: token i of a sequence leaves out the last n_q - 1 - i
     const int there = it.len - (it.tile * kAtTile + key0), first = OWN ? there - (a.n_q - 1) : there;
     const bool edge = first < NT * 8;
+    if (boxes && there < NT * 8) {
+        // values past the last key: zero, because a zero probability times whatever a page holds there (NaN, say) would not be
+        const int from = max(there, 0);
+        for (int i = lane; i < (NT * 8 - from) * (DP / 8); i += 32)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vs + at_kv(key0 + from + i / (DP / 8), i % (DP / 8))), "r"(0) : "memory");
+        __syncwarp();
+    }
     float top[2] = {st.m[0], st.m[1]};
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -212,7 +227,7 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
             const int r = key0 + from + i / (DP / 8);
             uint4 v;
             asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                         : "r"(vs + r * PITCH + at_piece(r, i % (DP / 8))) : "memory");
+                         : "r"(vs + at_kv(r, i % (DP / 8))) : "memory");
             apart |= D::any_nonfinite(v);
         }
         apart = __any_sync(0xffffffffu, apart);
@@ -223,7 +238,7 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
 #pragma unroll
             for (int n = 0; n < DP / 8; n += 2) {
                 uint32_t b[4];
-                ldsm4t(b, vs + (key0 + k * 16 + (lane & 15)) * PITCH + ((n + (lane >> 4)) ^ (lane & 7)) * 16);
+                ldsm4t(b, vs + at_kv(key0 + k * 16 + (lane & 15), n + (lane >> 4)));
                 mma16<D>(o[n], p[k], b[0], b[1]);
                 mma16<D>(o[n + 1], p[k], b[2], b[3]);
             }
@@ -236,7 +251,7 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
 #pragma unroll
                 for (int n = 0; n < DP / 8; n += 2) {
                     uint32_t b[4];
-                    ldsm4t(b, vs + (key0 + k * 16 + (lane & 15)) * PITCH + ((n + (lane >> 4)) ^ (lane & 7)) * 16);
+                    ldsm4t(b, vs + at_kv(key0 + k * 16 + (lane & 15), n + (lane >> 4)));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = k * 16 + (e & 1) * 8 + 2 * t;
@@ -257,26 +272,81 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
     }
 }
 
-template <int DP>
-__host__ __device__ constexpr int attention_stage_bytes() { return (2 * kAtTile + 16) * at_pitch(DP); }     // K, V, 16 rows of q
-
 struct AttentionRing {
-    uint64_t full[kAtStages], empty[kAtStages];
+    uint64_t full[kAtStages], landed[kAtStages], empty[kAtStages];      // (full: by the lanes' copies, landed: by boxes)
     AttentionUnit unit[kAtStages];
     float2 ml[64];
     volatile int gave_up;        // a computing warp has
 };
 
+// The copies of a CTA's units of the prefix by one warp, as boxes of `box` keys of a page (a lane each).  What a box brings
+// beyond the last key is masked, and its values are zeroed, by those who compute.  Pages are looked up a unit ahead.
+template <int DP>
+__device__ __forceinline__ void attention_boxes(const AttentionArgs &a, const AttentionPlan &p, AttentionWalk<false> &w, int left,
+                                                unsigned char *smem, AttentionRing &ring, const CUtensorMap &mapK, const CUtensorMap &mapV,
+                                                int box)
+{
+    constexpr int STAGE = attention_stage_bytes<DP>(), HALVES = DP > 64 ? 2 : 1;
+    const int lane = threadIdx.x & 31, boxes = kAtTile / box;
+    // One place for each step (the first pass only looks up a page): at the start each line of code comes from memory as well.
+    AttentionUnit now = {};
+    int s = 0, page = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (int step = 0; left > 0 && step <= left; ++step) {
+        AttentionUnit next = w.at;
+        int entry = 0;
+        if (step < left) {
+            entry = lane < boxes ? w.entry(a, p, lane * box) : 0;
+            next.stop = step + 1 == left;
+            next.leave = next.tile + 1 == w.tiles || next.stop;
+            w.advance(a, p);
+        }
+        if (step > 0) {
+            ok = mbar_wait(&ring.empty[s], ph ^ 1);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            const int keys = now.len - now.tile * kAtTile - lane * box;
+            const bool has = lane < boxes && keys > 0, bad = bad_page(a, page);
+            const int n = __popc(__ballot_sync(0xffffffffu, has));
+            if (has && bad && a.st) atomicAdd(&a.st->out_of_range, (unsigned long long)min(box, keys));
+            if (lane == 0) {
+                ring.unit[s] = now;
+                mbar_arrive_expect_tx(&ring.landed[s], (uint32_t)(n * box * 256 * HALVES));
+            }
+            __syncwarp();
+            if (has) {
+                const uint32_t dst = smem_u32(smem) + s * STAGE + lane * box * 128, bar = smem_u32(&ring.landed[s]);
+                const int row = (now.tile * kAtTile + lane * box) % (unsigned)a.page_size, pid = bad ? 0 : page;
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) {
+                    tma_load4(dst + h * (kAtTile * 128), &mapK, h * 64, now.kh, row, pid, bar);
+                    tma_load4(dst + (HALVES + h) * (kAtTile * 128), &mapV, h * 64, now.kh, row, pid, bar);
+                }
+            }
+            if (++s == kAtStages) { s = 0; ph ^= 1; }
+        }
+        now = next;
+        page = entry;
+    }
+    if (!ok) {                                                  // gave up: let what is under way land (bounded) before the memory goes
+        for (int i = 0; i < kAtStages; ++i) mbar_wait(&ring.landed[i], ph ^ (i >= s ? 1u : 0u));
+        if (lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
+    }
+}
+
 // CTA `cta` of the `ctas` that have the prefix / the own keys.
 template <class D, int DP, int WM, bool OWN>
 __device__ __forceinline__ void attention_part(const AttentionArgs &a, const AttentionPlan &p, int cta, int ctas, long long total,
-                                               unsigned char *ws, unsigned char *smem, AttentionRing &ring)
+                                               unsigned char *ws, unsigned char *smem, AttentionRing &ring, const CUtensorMap &mapK,
+                                               const CUtensorMap &mapV, int box)
 {
-    constexpr int PITCH = at_pitch(DP), STAGE = attention_stage_bytes<DP>(), KW = 4 / WM;
+    constexpr int PITCH = at_pitch(DP), QP = at_q_pitch<DP>(), STAGE = attention_stage_bytes<DP>(), KW = 4 / WM;
     constexpr bool kStagedQ = OWN && WM == 1;                   // short items: their rows of q come with their first unit
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int hd = a.head_dim, G = a.n_heads / a.n_kv, rec_rows = OWN ? p.own_rec : p.pre_rec;
-    uint64_t *const full = ring.full, *const empty = ring.empty;
+    const bool boxes = !OWN && box;
+    uint64_t *const full = boxes ? ring.landed : ring.full, *const empty = ring.empty;
     AttentionUnit *const unit = ring.unit;
     float2 *const sh_ml = ring.ml;
 
@@ -290,25 +360,30 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
             mbar_arrive(&full[0]);
             if (cw == 0 && lane == 0) mbar_arrive(&full[0]);
         }
+        if constexpr (!OWN)
+            if (box) {
+                if (cw == 0) attention_boxes<DP>(a, p, w, left, smem, ring, mapK, mapV, box);
+                return;
+            }
         // lanes 0-15 know this warp's 16 rows of a unit; a lane copies the same 16-byte piece of every (32 / CH)-th
         constexpr int CH = DP / 8 == 12 ? 16 : DP / 8, R = 32 / CH;
         const int mine = cw * 16 + (lane & 15), piece = lane % CH * 8;
-        const uint32_t dst0 = smem_u32(smem) + cw * 16 * PITCH;
         const uint16_t *const kp = a.ck + (piece < hd ? piece : 0), *const vp = a.cv + (piece < hd ? piece : 0);
-        int page = left > 0 ? w.page(a, p, mine) : -1;
+        int page = left > 0 ? w.entry(a, p, mine) : 0;
         int s = 0;
         uint32_t ph = 0;
         bool ok = true, fresh = true;
         for (; left > 0; --left) {
             const AttentionUnit now = w.at;
             const bool leave = now.tile + 1 == w.tiles || left == 1;
-            const int pg = page;
+            const bool has = w.has(p, mine), bad = bad_page(a, page);
+            const int pg = bad ? 0 : page;
             w.advance(a, p);
-            if (left > 1) page = w.page(a, p, mine);            // the next unit's page, while this one's stage empties
-            if (pg == -2 && lane < 16 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+            if (left > 1) page = w.entry(a, p, mine);           // the next unit's page, while this one's stage empties
+            if (has && bad && lane < 16 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
             // element offset of the row, -1: no such key
-            const long long off = pg == -1 ? -1
-                                           : (long long)max(pg, 0) * a.page_stride +
+            const long long off = !has ? -1
+                                           : (long long)pg * a.page_stride +
                                                  (long long)((unsigned)(now.tile * kAtTile + mine) % (unsigned)a.page_size) * a.token_stride +
                                                  now.kh * a.head_stride;
             ok = mbar_wait(&empty[s], ph ^ 1);
@@ -320,23 +395,22 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
                 mbar_arrive(&full[s]);
             }
             // missing rows become zeros, so that a zero probability times what lies there is zero
-            const uint32_t dst = dst0 + s * STAGE;
+            const uint32_t dst = smem_u32(smem) + s * STAGE;
 #pragma unroll
             for (int i = 0; i < 16 / R; ++i) {
                 const long long o = __shfl_sync(0xffffffffu, off, i * R + lane / CH);
                 const long long at = o < 0 ? 0 : o;
-                const int r = i * R + lane / CH;
+                const uint32_t to = dst + at_kv(cw * 16 + i * R + lane / CH, lane % CH);
                 // (zeros in the columns past head_dim too: an item's sums may have lain there since)
-                cp_async16(dst + r * PITCH + at_piece(r, lane % CH), kp + at, o >= 0 && piece < hd);
-                cp_async16(dst + (kAtTile + r) * PITCH + at_piece(r, lane % CH), vp + at, o >= 0 && piece < hd);
+                cp_async16(to, kp + at, o >= 0 && piece < hd);
+                cp_async16(to + kAtTile * PITCH, vp + at, o >= 0 && piece < hd);
             }
             if (kStagedQ && fresh) {
                 // the item's rows of q (four a warp)
                 for (int r = cw * 4 + lane / CH; r < min(cw * 4 + 4, p.own_rec); r += R) {
                     const unsigned tok = now.b * a.n_q + (unsigned)r / (unsigned)G, head = now.kh * G + (unsigned)r % (unsigned)G;
-                    const uint16_t *const src = a.q + (long long)tok * a.ldq + (long long)head * hd;
-                    cp_async16(smem_u32(smem) + s * STAGE + (2 * kAtTile + r) * PITCH + at_piece(r, lane % CH),
-                               piece < hd ? src + piece : src, piece < hd);
+                    if (piece < hd)
+                        cp_async16(dst + 2 * kAtTile * PITCH + r * QP + piece * 2, a.q + (long long)tok * a.ldq + (long long)head * hd + piece, true);
                 }
             }
             fresh = leave;
@@ -365,46 +439,65 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
         named_bar_sync(1, 128);
         return !ring.gave_up;
     };
+    // The first pass computes nothing that is kept: it brings the code of the loop in, and the first rows of a prefix item's q,
+    // while the first copies are under way.
+    bool warm = true, q_there = false;
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[k][e] = 0u;
+    AttentionUnit it = {};
+    it.len = 0x40000000;
+    if (!OWN) {
+        const AttentionDeal deal(total, ctas);
+        const int item = cta < deal.ctas ? (int)div_units(deal.first(cta), (int)p.pre_tiles) : 0;
+        it.kh = item / p.pre_rt;
+        it.rt = item % p.pre_rt;
+    }
     for (;;) {
-        const bool ok = mbar_wait(&full[s], ph);
-        if (!__all_sync(0xffffffffu, ok)) {
-            if (lane == 0) {
-                if (a.st) atomicAdd(&a.st->wait_timeout, 1ull);
-                ring.gave_up = 1;
+        if (!warm) {
+            const bool ok = mbar_wait(&full[s], ph);
+            if (!__all_sync(0xffffffffu, ok)) {
+                if (lane == 0) {
+                    if (a.st) atomicAdd(&a.st->wait_timeout, 1ull);
+                    ring.gave_up = 1;
+                }
+                __syncwarp();
+                named_bar_arrive(1, 128);
+                return;
             }
-            __syncwarp();
-            named_bar_arrive(1, 128);
-            return;
+            it = unit[s];
+            if (it.stop == 2) return;
         }
-        const AttentionUnit it = unit[s];
-        if (it.stop == 2) return;
         const uint32_t ks = smem_u32(smem + s * STAGE);
         if (fresh) {
-            // rows of a key head: token * G + head in group
-            const int base = (OWN ? it.b * a.n_q * G : 0) + it.rt * 16 * WM;
-            nrows = min((OWN ? 1 : (int)a.n_seq) * a.n_q * G - it.rt * 16 * WM, 16 * WM);
-            // q as A fragments, rows g and g + 8 (rows past nrows: whatever, nobody reads what they give)
-            const unsigned row_a = base + min(wrow + g, nrows - 1), row_b = base + min(wrow + g + 8, nrows - 1);
-            const unsigned tok_a = row_a / (unsigned)G, tok_b = row_b / (unsigned)G;
-            if (OWN) {
-                own_i[0] = (int)tok_a - it.b * a.n_q;
-                own_i[1] = (int)tok_b - it.b * a.n_q;
-            }
-            if (kStagedQ) {
+            if (OWN ? !warm : !q_there) {
+                // rows of a key head: token * G + head in group
+                const int base = (OWN ? it.b * a.n_q * G : 0) + it.rt * 16 * WM;
+                nrows = min((OWN ? 1 : (int)a.n_seq) * a.n_q * G - it.rt * 16 * WM, 16 * WM);
+                // q as A fragments, rows g and g + 8 (rows past nrows: whatever, nobody reads what they give)
+                const unsigned row_a = base + min(wrow + g, nrows - 1), row_b = base + min(wrow + g + 8, nrows - 1);
+                const unsigned tok_a = row_a / (unsigned)G, tok_b = row_b / (unsigned)G;
+                if (OWN) {
+                    own_i[0] = (int)tok_a - it.b * a.n_q;
+                    own_i[1] = (int)tok_b - it.b * a.n_q;
+                }
+                if (kStagedQ) {
 #pragma unroll
-                for (int k = 0; k < DP / 16; ++k)
-                    ldsm4(q[k], ks + (2 * kAtTile + (lane & 15)) * PITCH + ((k * 2 + (lane >> 4)) ^ (lane & 7)) * 16);
-            } else {
-                const uint16_t *const sa = a.q + (long long)tok_a * a.ldq + (long long)(it.kh * G + (int)(row_a % (unsigned)G)) * hd + 2 * t;
-                const uint16_t *const sb = a.q + (long long)tok_b * a.ldq + (long long)(it.kh * G + (int)(row_b % (unsigned)G)) * hd + 2 * t;
+                    for (int k = 0; k < DP / 16; ++k)
+                        ldsm4(q[k], ks + 2 * kAtTile * PITCH + (lane & 15) * QP + (k * 2 + (lane >> 4)) * 16);
+                } else {
+                    const uint16_t *const sa = a.q + (long long)tok_a * a.ldq + (long long)(it.kh * G + (int)(row_a % (unsigned)G)) * hd + 2 * t;
+                    const uint16_t *const sb = a.q + (long long)tok_b * a.ldq + (long long)(it.kh * G + (int)(row_b % (unsigned)G)) * hd + 2 * t;
 #pragma unroll
-                for (int k = 0; k < DP / 16; ++k)
+                    for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int d = k * 16 + e * 8;
-                        q[k][2 * e] = d < hd ? *reinterpret_cast<const uint32_t *>(sa + d) : 0u;
-                        q[k][2 * e + 1] = d < hd ? *reinterpret_cast<const uint32_t *>(sb + d) : 0u;
-                    }
+                        for (int e = 0; e < 2; ++e) {
+                            const int d = k * 16 + e * 8;
+                            q[k][2 * e] = d < hd ? *reinterpret_cast<const uint32_t *>(sa + d) : 0u;
+                            q[k][2 * e + 1] = d < hd ? *reinterpret_cast<const uint32_t *>(sb + d) : 0u;
+                        }
+                }
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -417,7 +510,13 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.0f;
         }
         fresh = it.leave;
-        attention_tile<D, DP, WM, OWN>(a, it, ks, q, own_i, scale, o, st);
+        q_there = false;
+        attention_tile<D, DP, WM, OWN>(a, it, ks, q, own_i, scale, o, st, boxes);
+        if (warm) {
+            warm = false;
+            fresh = q_there = true;
+            continue;
+        }
         if (it.leave) {
             // the CTA's record of the item
             const int item = OWN ? (it.b * a.n_kv + it.kh) * p.own_rt + it.rt : it.kh * p.pre_rt + it.rt;
@@ -479,6 +578,7 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
                 }
             }
         }
+        if (boxes && it.leave) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // what was written here, before the next copies
         __syncwarp();
         if (lane == 0) mbar_arrive(&empty[s]);
         if (++s == kAtStages) { s = 0; ph ^= 1; }
@@ -490,18 +590,31 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
 // join's sake.
 template <class D, int DP, int WMP, int WMO>
 __global__ void __launch_bounds__(kAtThreads, kAtCtasPerSm)
-attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned char *ws, bool chained)
+attention_units_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_constant__ CUtensorMap mapK,
+                       const __grid_constant__ CUtensorMap mapV, unsigned char *ws, int box, bool chained)
 {
-    extern __shared__ __align__(16) unsigned char smem[];
+    extern __shared__ unsigned char raw[];
+    unsigned char *const smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     __shared__ AttentionRing ring;
     const int tid = threadIdx.x, cta = blockIdx.x;
     if (tid == 0) {
         for (int s = 0; s < kAtStages; ++s) {
             mbar_init(&ring.full[s], 129);                      // every copying lane, and the unit itself
+            mbar_init(&ring.landed[s], 1);
             mbar_init(&ring.empty[s], 4);
         }
         ring.gave_up = 0;
         mbar_init_fence();
+        if (box) {
+            tma_prefetch_map(&mapK);
+            tma_prefetch_map(&mapV);
+        }
+    }
+    if (a.head_dim < DP) {                                      // columns of q past head_dim: no copy writes them
+        const int pieces = (DP - a.head_dim) / 8;
+        for (int i = tid; i < kAtStages * 16 * pieces; i += kAtThreads)
+            *reinterpret_cast<uint4 *>(smem + i / pieces / 16 * attention_stage_bytes<DP>() + 2 * kAtTile * at_pitch(DP) +
+                                       i / pieces % 16 * at_q_pitch<DP>() + a.head_dim * 2 + i % pieces * 16) = make_uint4(0, 0, 0, 0);
     }
     __syncthreads();
     if (!chained) {
@@ -521,8 +634,8 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, unsigned ch
         start[a.n_seq] = own;
         start[a.n_seq + 1] = split;
     }
-    if (cta < split) attention_part<D, DP, WMP, false>(a, p, cta, split, pre, ws, smem, ring);
-    else attention_part<D, DP, WMO, true>(a, p, cta - split, p.ctas - split, own, ws, smem, ring);
+    if (cta < split) attention_part<D, DP, WMP, false>(a, p, cta, split, pre, ws, smem, ring, mapK, mapV, box);
+    else attention_part<D, DP, WMO, true>(a, p, cta - split, p.ctas - split, own, ws, smem, ring, mapK, mapV, box);
     if (chained && cta == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
@@ -628,13 +741,28 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
     }
 }
 
+// Keys of a tiled copy: a box lies in one page, on a row of the stage that keeps the swizzle's phase (a multiple of eight).
+// 0: the four warps' 16-byte copies, for other page sizes, and where the units do not even fill the device once.
+static int units_box(const AttentionArgs &a, const AttentionPlan &p)
+{
+    if (p.tensor || !p.pre_tiles || a.page_size % 8 || p.ctas < kSmCount * kAtCtasPerSm) return 0;
+    int box = 8;
+    while (box < kAtTile && a.page_size % (2 * box) == 0) box *= 2;
+    return box;
+}
+
 template <class D, int DP, int WMP, int WMO>
 static aweq_status units_launch(const AttentionArgs &a, const AttentionPlan &p, unsigned char *ws, cudaStream_t stream)
 {
-    constexpr int smem = kAtStages * attention_stage_bytes<DP>();
+    constexpr int smem = kAtStages * attention_stage_bytes<DP>() + 1024;
+    CUtensorMap mk = {}, mv = {};
+    int box = units_box(a, p);
+    if (box && (tma_pool_map(&mk, a.ck, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, box) != AWEQ_OK ||
+                tma_pool_map(&mv, a.cv, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, box) != AWEQ_OK))
+        box = 0;                                                // strides that a tensor map cannot hold
     static std::atomic<unsigned long long> allowed{0};
     AWEQ_CUDA_OK(allow_smem(attention_units_kernel<D, DP, WMP, WMO>, smem, allowed));
-    AWEQ_LAUNCH((attention_units_kernel<D, DP, WMP, WMO>), dim3((unsigned)p.ctas), dim3(kAtThreads), smem, stream, a, p, ws, p.tensor != 0);
+    AWEQ_LAUNCH((attention_units_kernel<D, DP, WMP, WMO>), dim3((unsigned)p.ctas), dim3(kAtThreads), smem, stream, a, p, mk, mv, ws, box, p.tensor != 0);
     return AWEQ_OK;
 }
 

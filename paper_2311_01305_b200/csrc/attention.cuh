@@ -30,17 +30,14 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// A clamped own length.  `count`: the one caller that reports it.
-__device__ __forceinline__ int own_length(const AttentionArgs &a, long long b, bool count)
+// An own length, clamped.  `count`: the one caller that reports it.
+__device__ __forceinline__ int clamp_length(const AttentionArgs &a, int len, bool count)
 {
-    const int len = __ldg(a.own_len + b);
     const int most = (int)min(a.max_own, a.pages_per_seq * a.page_size);
-    if (len < 0 || len > most) {
-        if (count && a.st) atomicAdd(&a.st->out_of_range, 1ull);
-        return len < 0 ? 0 : most;
-    }
-    return len;
+    if (count && a.st && (len < 0 || len > most)) atomicAdd(&a.st->out_of_range, 1ull);
+    return len < 0 ? 0 : min(len, most);
 }
+__device__ __forceinline__ int own_length(const AttentionArgs &a, long long b) { return clamp_length(a, __ldg(a.own_len + b), false); }
 __device__ __forceinline__ int tiles_of(int len, int unit) { return (int)(((unsigned)len + (unsigned)unit - 1) / (unsigned)unit); }
 
 // The units are dealt out in order, total / ctas to a CTA and one more to the first total % ctas.  (Divisions of 64 bits
@@ -92,24 +89,22 @@ struct AttentionWalk {
             ++at.b;
             at.len = next_len;
             tiles = tiles_of(at.len, p.unit);
-            next_len = at.b + 1 < n_seq ? own_length(a, at.b + 1, false) : 0;
+            next_len = at.b + 1 < n_seq ? own_length(a, at.b + 1) : 0;
         } while (tiles == 0 && at.b + 1 < n_seq);
     }
-    // page of the unit's r'th key; -1: no such key, -2: a page outside the pool
-    __device__ __forceinline__ int page(const AttentionArgs &a, const AttentionPlan &p, int r) const
+    __device__ __forceinline__ bool has(const AttentionPlan &p, int r) const { return at.tile * (OWN ? p.unit : p.pre_unit) + r < at.len; }
+    // entry of the page list for the unit's r'th key, if there is such a key; not looked at here, so that the load can fly
+    __device__ __forceinline__ int entry(const AttentionArgs &a, const AttentionPlan &p, int r) const
     {
-        const int c = at.tile * (OWN ? p.unit : p.pre_unit) + r;
-        if (c >= at.len) return -1;
         const int *pages = OWN ? a.page_table + (long long)at.b * a.ld_table : a.prefix_pages;
-        const int page = __ldg(pages + (unsigned)c / (unsigned)a.page_size);
-        return page < 0 || page >= a.n_pages ? -2 : page;
+        return has(p, r) ? __ldg(pages + (unsigned)(at.tile * (OWN ? p.unit : p.pre_unit) + r) / (unsigned)a.page_size) : 0;
     }
 };
 
 // Tiles of 32 sequences: the lane's own length and tiles, and the tiles before it.
 __device__ __forceinline__ long long scan_tiles(const AttentionArgs &a, const AttentionPlan &p, int b, bool count, int *len, int *n)
 {
-    *len = b < (int)a.n_seq ? own_length(a, b, count) : 0;
+    *len = clamp_length(a, b < (int)a.n_seq ? __ldg(a.own_len + b) : 0, count);
     *n = tiles_of(*len, p.unit);
     int sum = *n;                                               // 32 lengths of at most 2^31 keys: below 2^31 tiles
 #pragma unroll
@@ -133,6 +128,8 @@ __device__ __forceinline__ long long own_units(const AttentionArgs &a, const Att
     }
     return total * per_seq;
 }
+
+__device__ __forceinline__ bool bad_page(const AttentionArgs &a, int page) { return page < 0 || page >= a.n_pages; }
 
 // A warp finds the first unit of CTA `cta` of `ctas` (every lane gets the same) and the number of its units.
 template <bool OWN>
@@ -167,7 +164,7 @@ __device__ __forceinline__ int attention_begin(const AttentionArgs &a, const Att
             w.at.rt = item % p.own_rt;
             w.at.tile = within - item * w.tiles;
             w.at.len = __shfl_sync(0xffffffffu, len, src);
-            w.next_len = src < 31 ? __shfl_sync(0xffffffffu, len, src + 1) : w.at.b + 1 < n_seq ? own_length(a, w.at.b + 1, false) : 0;
+            w.next_len = src < 31 ? __shfl_sync(0xffffffffu, len, src + 1) : w.at.b + 1 < n_seq ? own_length(a, w.at.b + 1) : 0;
             break;
         }
         passed = __shfl_sync(0xffffffffu, mine + (long long)n * per_seq, 31);

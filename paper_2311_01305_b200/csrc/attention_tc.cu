@@ -96,11 +96,9 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
             const bool lead = warp == 0;
             const CUtensorMap *const map = lead ? &mapK : &mapV;
             const int boxes = p.pre_unit / p.box;
-            auto look_up = [&](int tile) {                                  // page of the lane's box; -1: none, -2: outside the pool
-                const int c = tile * p.pre_unit + lane * p.box;
-                if (lane >= boxes || c >= a.prefix_len) return -1;
-                const int page = __ldg(a.prefix_pages + (unsigned)c / (unsigned)a.page_size);
-                return page < 0 || page >= a.n_pages ? -2 : page;
+            auto has = [&](int tile) { return lane < boxes && tile * p.pre_unit + lane * p.box < a.prefix_len; };
+            auto look_up = [&](int tile) {                                  // entry of the lane's box (not looked at here: the load flies)
+                return has(tile) ? __ldg(a.prefix_pages + (unsigned)(tile * p.pre_unit + lane * p.box) / (unsigned)a.page_size) : 0;
             };
             int tile = tile0, kh = item0 / p.pre_rt, rt = item0 % p.pre_rt, page = look_up(tile), s = 0, items = 0;
             uint32_t ph = 0;
@@ -115,24 +113,25 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                 u.leave = tile + 1 == p.pre_tiles || u.stop;
                 u.item = items;
                 u.fresh = fresh;
-                const int pg = page;
+                const bool there = has(u.tile), bad = bad_page(a, page);
+                const int pid = bad ? 0 : page;
                 if (++tile == p.pre_tiles) {
                     tile = 0;
                     if (++rt == p.pre_rt) { rt = 0; ++kh; }
                 }
                 if (left > 1) page = look_up(tile);                         // the next unit's, while this stage empties
-                if (lead && pg == -2 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+                if (lead && there && bad && a.st) atomicAdd(&a.st->out_of_range, 1ull);
                 ok = mbar_wait(&sh.empty[s], ph ^ 1);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                const int n = __popc(__ballot_sync(0xffffffffu, pg != -1));
+                const int n = __popc(__ballot_sync(0xffffffffu, there));
                 if (lane == 0) {
                     if (lead) sh.unit[s] = u;
                     mbar_arrive_expect_tx(&sh.full[s], (uint32_t)(n * p.box * 128 * halves));
                 }
                 __syncwarp();
-                if (pg != -1) {
+                if (there) {
                     const uint32_t dst = smem_u32(stages + s * stage_bytes + (lead ? 0 : v_at)) + lane * p.box * 128, bar = smem_u32(&sh.full[s]);
-                    const int row = (unsigned)(u.tile * p.pre_unit + lane * p.box) % (unsigned)a.page_size, pid = max(pg, 0);
+                    const int row = (unsigned)(u.tile * p.pre_unit + lane * p.box) % (unsigned)a.page_size;
                     for (int h = 0; h < halves; ++h) tma_load4(dst + h * 16384, map, h * 64, u.kh, row, pid, bar);
                 }
                 fresh = u.leave;
