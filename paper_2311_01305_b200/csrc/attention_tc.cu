@@ -8,6 +8,8 @@
 // Each row's reference maximum m moves only when a new maximum exceeds it by more than 8 (a factor of 256, which
 // neither the 16-bit P nor the binary32 sums mind), so O is hardly ever rescaled: only then do the softmax threads
 // wait for the product under way, scale O and go on.
+// What bounds it: the exponentials, 128 x 128 of a unit in some 1450 of its 2900 cycles, and the hand-over of S and P (384 rows x 32779
+// keys x 8 heads of 128: 66 us, 0.78 PFLOP/s).
 // Warps: 0 and 2 look up pages and issue the copies of K and V, 1 issues the products (S of a unit before O of the one
 // before it), 4-11 softmax (two threads to a row, half of the keys each), 12-15 bring the next item's rows of Q and take
 // the finished item's O to its record.

@@ -91,7 +91,8 @@ __device__ __forceinline__ bool append_head(const KvAppendArgs &a, const AppendP
 // 16-byte accesses.  The pass is a copy: what bounds it is memory, and before that the loads under way.  A warp
 // takes one token and a run of its heads, a lane the same two 16-byte pieces of every head it gets (the two
 // halves of eight pairs, or 16 neighbouring elements when interleaved), so cos and sin are read once per
-// token and stay in registers, and four heads' loads are issued before the first is used.
+// token and stay in registers, and four heads' loads are issued before the first is used.  Measured: 26624 tokens of 40 + 2 x 8 heads of
+// 128, 138 us, 5.64 TB/s (a copy: 6.46); 64 tokens 3.7 us, three dependent loads (sequence, page, row) after the start.
 template <class D, bool INTER>
 __global__ void __launch_bounds__(256)
 kv_append_kernel(const KvAppendArgs a, int segments)
@@ -179,7 +180,8 @@ kv_append_kernel(const KvAppendArgs a, int segments)
     }
 }
 
-// Element by element, for rows or rotations that 16-byte pieces do not fit.
+// Element by element, for rows or rotations that 16-byte pieces do not fit: the same formulas, several times slower (the first of the
+// two cases above took 657 us in this form).
 template <class D>
 __global__ void __launch_bounds__(256) kv_append_elements_kernel(const KvAppendArgs a)
 {
