@@ -491,7 +491,8 @@ aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, lo
  * over all prefix keys and the own keys j < own_len[b] - (n_q - 1 - i); head h reads key head
  * h / (n_heads / n_kv_heads).  A row without keys gives zeros.  The prefix is read once for all rows
  * of the batch.  Scores, running maximum, sum and output are binary32; the probabilities are
- * rounded to the 16-bit type for the product with v; one rounding at the end.
+ * rounded to the 16-bit type for the product with v (fp16: to 2^-32 of a row's largest at worst, however
+ * small they are); one rounding at the end.
  * q, out: 16-bit [n_seq * n_q x n_heads * head_dim], row pitches ldq, ldo elements, 16-byte aligned,
  * pitches multiples of 8.  head_dim: a multiple of 8 up to 128.  own_len: device int[n_seq];
  * max_own: HOST bound on it (a smaller one makes a smaller launch).  A length above max_own or

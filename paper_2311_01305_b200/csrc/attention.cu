@@ -6,7 +6,7 @@
 // The units of all items in a row are dealt out evenly to a grid that fills the device once, so a CTA streams
 // through parts of one or several items without ever draining its copies, whatever the lengths are (the own ones are
 // known on the device only): so many CTAs take the prefix and so many the own keys as their units ask for.  Where a CTA
-// leaves an item it writes a record (maximum m, sum l, output o of the keys it has seen, for each row).  A prefix with many
+// leaves an item it writes a record (base m near the maximum, sum l, output o of the keys it has seen, for each row).  A prefix with many
 // rows goes to a launch of its own (attention_tc.cu), which the own keys' CTAs follow as it ends.  The last launch joins the
 // records of a row:
 //   m = max m_i,  l = sum 2^(m_i - m) l_i,  out = sum 2^(m_i - m) o_i / l      (scores in units of log 2)
@@ -195,13 +195,12 @@ __device__ __forceinline__ void attention_tile(const AttentionArgs &a, const Att
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         top[h] = quad_max(top[h]);
-        base[h] = top[h] == -CUDART_INF_F ? 0.0f : top[h];      // a row that has seen no key yet
-        f[h] = exp2_fast(st.m[h] - base[h]);
+        base[h] = top[h] == -CUDART_INF_F ? 0.0f : probability_base<D>(top[h]);      // (a row that has seen no key yet)
+        f[h] = exp2_fast(probability_base<D>(st.m[h]) - base[h]);
         st.m[h] = top[h];
         st.l[h] *= f[h];
     }
-    // The probabilities are rounded to the 16-bit type for the product with v (at most half a unit of it each, as the
-    // output's own rounding); their sum is not.
+    // rounded to the 16-bit type for the product with v, unrounded in their sum (see probability_base)
     uint32_t p[NT / 2][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -531,7 +530,7 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     st.l[h] = quad_sum(st.l[h]);
-                    if (t == 0) sh_ml[gw + 8 * h] = make_float2(st.m[h], st.l[h]);
+                    if (t == 0) sh_ml[gw + 8 * h] = make_float2(probability_base<D>(st.m[h]), st.l[h]);
                 }
                 if (!meet()) return;                            // all have read the stage, and all (m, l) are there
 #pragma unroll
@@ -545,7 +544,7 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
                         x[k] = sh_ml[(k * WM + warp % WM) * 16 + g + 8 * h];
                         m = fmaxf(m, x[k].x);
                     }
-                    const float base = m == -CUDART_INF_F ? 0.0f : m, mine = exp2_fast(st.m[h] - base);
+                    const float base = m == -CUDART_INF_F ? 0.0f : m, mine = exp2_fast(probability_base<D>(st.m[h]) - base);
 #pragma unroll
                     for (int k = 0; k < KW; ++k) l += exp2_fast(x[k].x - base) * x[k].y;
                     if (t == 0 && warp < WM) rml[r] = make_float2(m, l);
@@ -574,7 +573,7 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
 #pragma unroll
                     for (int n = 0; n < DP / 8; ++n)
                         if (n * 8 < hd) *reinterpret_cast<float2 *>(dst + n * 8) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
-                    if (t == 0) rml[r] = make_float2(st.m[h], st.l[h]);
+                    if (t == 0) rml[r] = make_float2(probability_base<D>(st.m[h]), st.l[h]);
                 }
             }
         }

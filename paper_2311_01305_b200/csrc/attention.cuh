@@ -30,6 +30,15 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// What a row's probabilities 2^(score - base) are relative to; m is its maximum so far, or lies a little below it.
+//
+// They are rounded to the 16-bit type for the product with v (their sum takes them unrounded), which leaves each within
+// u = 2^-11 (fp16) or 2^-8 (bf16) of itself, as the output's own rounding does, as long as it is a normal number.  fp16 has
+// those down to 2^-14 and nothing below 2^-25, and a million keys beside one large one may all lie there.  So fp16 ones
+// are held 2^7 times as large; below 2^-21 of 2^m they are off by at most 2^-32 of it each.  (In binary32 m - 7 is m - 8 at
+// the lowest, wherever m lies.)
+template <class D>
+__device__ __forceinline__ float probability_base(float m) { return D::kBf16 ? m : m - 7.0f; }
 // An own length, clamped.  `count`: the one caller that reports it.
 __device__ __forceinline__ int clamp_length(const AttentionArgs &a, int len, bool count)
 {

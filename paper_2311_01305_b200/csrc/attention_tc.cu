@@ -3,10 +3,10 @@
 //
 // An item is up to 128 rows (TMEM lanes) against the prefix, 128 keys (or the whole pages that fit) to a unit:
 //   S = Q K^T   A = Q in TMEM, B = the staged keys            -> S in TMEM (two buffers)
-//   P = 2^(S scale - m)  by two threads per row, 16-bit, in TMEM over the S it came from
+//   P = 2^(S scale - base(m))  by two threads per row, 16-bit, in TMEM over the S it came from
 //   O += P V    A = P in TMEM, B = the staged values (N contiguous)  -> O in TMEM
-// Each row's reference maximum m moves only when a new maximum exceeds it by more than 8 (a factor of 256, which
-// neither the 16-bit P nor the binary32 sums mind), so O is hardly ever rescaled: only then do the softmax threads
+// Each row's reference maximum m moves only when a new maximum exceeds it by more than 8 (a factor of 256, for which
+// the 16-bit P and the binary32 sums have room), so O is hardly ever rescaled: only then do the softmax threads
 // wait for the product under way, scale O and go on.
 // What bounds it: the exponentials, 128 x 128 of a unit in some 1450 of its 2900 cycles, and the hand-over of S and P (384 rows x 32779
 // keys x 8 heads of 128: 66 us, 0.78 PFLOP/s).
@@ -21,6 +21,9 @@ namespace aweq {
 constexpr int kTcThreads = 512, kTcStageBytes = 192 * 1024, kTcMaxStages = 6;
 constexpr uint32_t kTcO = 256, kTcQ = 384;      // TMEM columns: S at 0 and 128, O, two of Q (64 columns each)
 constexpr float kTcSlack = 8.0f;
+// up to 2^8 of slack and 2^7 of fp16's head room; no head room where m is so large that the slack is rounded
+template <class D>
+__device__ __forceinline__ float tc_base(float m) { return fabsf(m) <= 1048576.0f ? probability_base<D>(m) : m; }
 
 // A unit: the tile'th tile of the prefix for row tile rt of key head kh.
 struct alignas(16) TcUnit {
@@ -264,7 +267,8 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                     ok = mbar_wait(&sh.pv_done[(u - 1) & 1], ((u - 1) >> 1) & 1);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                     tc_fence_after();
-                    const float to = t > m + kTcSlack ? t : m, f = to == -CUDART_INF_F ? 1.0f : exp2_fast(m - to);
+                    const float to = t > m + kTcSlack ? t : m, move = tc_base<D>(m) - tc_base<D>(to);
+                    const float f = to == -CUDART_INF_F ? 1.0f : exp2_fast(move);
                     m = to;
                     l *= f;
 #pragma unroll 1
@@ -278,7 +282,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                     }
                     tc_wait_st();
                 }
-                const float base = m == -CUDART_INF_F ? 0.0f : m;
+                const float base = m == -CUDART_INF_F ? 0.0f : tc_base<D>(m);
                 float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
@@ -288,8 +292,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                         const float f = exp2_fast(__fmaf_rn(__uint_as_float(x[c][j + 1]), scale, -base));
                         sum[j & 2] += e;
                         sum[(j & 2) + 1] += f;
-                        // Rounded to the 16-bit type for the product with v (at most half a unit of it each, as the output's
-                        // own rounding); the sum takes the unrounded ones.
+                        // rounded to the 16-bit type for the product with v; the sum takes the unrounded ones (see probability_base)
                         x[0][c * 16 + j / 2] = D::encode2(e, f);
                     }
                 tc_st32(at + half * 32, x[0]);
@@ -304,7 +307,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                     if (half) sh.sum[r] = l;
                     if (!(ok = meet())) break;
                     if (!half && r < nrows)
-                        reinterpret_cast<float2 *>(ws + p.off_pre_ml)[rec + r] = make_float2(m, l + sh.sum[r]);
+                        reinterpret_cast<float2 *>(ws + p.off_pre_ml)[rec + r] = make_float2(tc_base<D>(m), l + sh.sum[r]);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.item_done[it.item & 3]);

@@ -1,0 +1,55 @@
+"""Where the operators that run a calibrated layer could go wrong quietly: weights far below the row's largest,
+channels beyond a grid's limit, codes that change after the layer was made, pools whose strides no tiled copy can
+hold, scores of minus infinity, counts of bad entries, rows without a pitch, zero-points of 31 bits.  Tolerances
+are those of ``test_gpu_serving`` (derived there); what a test adds to them is derived beside it."""
+import math
+
+import pytest
+import torch
+
+from paper_2311_01305_b200 import aweq
+
+from .test_gpu_serving import (DTYPES, TINY, U16, attention_case, attention_reference, gen, linear_check, linear_inputs, make_cache)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------- weights far below the largest
+# Rows and keys of a prefix for the kernel of few rows (page sizes that no tiled copy fits go there, whatever the rows) and
+# for the tensor kernel; own keys of many sequences.
+FEW, MANY, OWN = (dict(n_seq=50, heads=64, keys=4096, page=12), dict(n_seq=40, heads=16, keys=4100, page=16),
+                  dict(n_seq=80, heads=16, keys=600, page=16, own=True))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("place", [0, 77, -1])
+@pytest.mark.parametrize("log2_weight", [-12.3, -18.6, -23.5, -25])
+@pytest.mark.parametrize("shape", [FEW, MANY, OWN], ids=["few", "many", "own"])
+def test_attention_many_small_weights_beside_one_large(shape, log2_weight, place, dtype):
+    """One key of weight 1 whose value is zero, hundreds to thousands of weight 2^-12 to 2^-25: the output is made of the small ones.
+
+    The header allows fp16 probabilities to be off by 2^-32 of the largest each (beside u of themselves); values are below 2."""
+    n_seq, h, n, page, own, d = shape["n_seq"], shape["heads"], shape["keys"], shape["page"], shape.get("own"), 64
+    g = gen(31)
+    each = -(-n // page)
+    cache = make_cache(n_seq * each if own else each, page, h, d, dtype)
+    listed = torch.arange(cache.n_pages, dtype=torch.int32, device="cuda").view(-1, each)
+    k = torch.zeros(listed.shape + (page, h, d), device="cuda")
+    v = 1.0 + torch.rand(k.shape, generator=g, device="cuda")
+    k[..., 0] = log2_weight
+    sink = place % n
+    k[:, sink // page, sink % page], v[:, sink // page, sink % page] = 0.0, 0.0
+    cache.k.copy_(k.view_as(cache.k))
+    cache.v.copy_(v.view_as(cache.v))
+    q = torch.zeros((n_seq, h, d), dtype=dtype, device="cuda")
+    q[:, :, 0] = 1.0
+    prefix, lens = (0, n) if own else (n, 0)
+    pages = listed if own else torch.zeros((n_seq, 1), dtype=torch.int32, device="cuda")
+    lens = torch.full((n_seq,), lens, dtype=torch.int32, device="cuda")
+    attend = aweq.PrefixAttention(cache, listed[0], prefix, h, n_seq, 1, n, scale=math.log(2.0))
+    out = attend(q, pages, lens)
+    want, mag, reach = attention_reference(q, cache, listed[0], prefix, pages, lens, 1, attend.scale)
+    off = (reach * d * 2.0 ** -23 + 2.0 ** -20 + (n / 16 + 64) * 2.0 ** -23)[..., None]
+    tol = U16[dtype] * 1.001 * want.abs() + (U16[dtype] + 2 * off) * 1.01 * mag + TINY[dtype] + (n * 2.0 ** -32 * 2 if dtype is torch.float16 else 0)
+    err = (out.double() - want).abs()
+    assert (err <= tol).all(), "off by %.3g of the output" % (err / want.abs()).max().item()
