@@ -21,9 +21,13 @@ namespace aweq {
 constexpr int kTcThreads = 512, kTcStageBytes = 192 * 1024, kTcMaxStages = 6;
 constexpr uint32_t kTcO = 256, kTcQ = 384;      // TMEM columns: S at 0 and 128, O, two of Q (64 columns each)
 constexpr float kTcSlack = 8.0f;
-// up to 2^8 of slack and 2^7 of fp16's head room; no head room where m is so large that the slack is rounded
+// Where a reference is so large that binary32 keeps less than an eighth behind the point, neither the slack nor fp16's head room
+// (2^8 and 2^7 of fp16's 2^16) can be told from rounding: the reference is the maximum itself there, the base is the reference,
+// and scores are scaled, and rounded, before it is taken off, as the maximum was.
+__device__ __forceinline__ bool tc_far(float m) { return fabsf(m) > 1048576.0f && m != -CUDART_INF_F; }
 template <class D>
-__device__ __forceinline__ float tc_base(float m) { return fabsf(m) <= 1048576.0f ? probability_base<D>(m) : m; }
+__device__ __forceinline__ float tc_base(float m) { return tc_far(m) ? m : probability_base<D>(m); }
+__device__ __forceinline__ float tc_limit(float m) { return tc_far(m) ? m : m + kTcSlack; }
 
 // A unit: the tile'th tile of the prefix for row tile rt of key head kh.
 struct alignas(16) TcUnit {
@@ -200,7 +204,9 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
         const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
         // a negative scale turned q's signs; a zero one must leave -inf where a key is not seen
         const float scale = fmaxf(fabsf(a.scale), 1.17549435e-38f) * 1.4426950408889634f;
-        float m = -CUDART_INF_F, l = 0.0f;
+        // of the row: reference maximum, what moves it, what the exponents are relative to, sum; whether a row of the warp is far
+        float m = -CUDART_INF_F, limit = m, base = 0.0f, l = 0.0f;
+        bool far = false;
         int s = 0, u = 0, nrows = 0;
         uint32_t ph = 0;
         long long rec = 0;
@@ -217,7 +223,6 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                 const TcItem x = tc_item(a, p, it.kh, it.rt, cta);
                 nrows = x.nrows;
                 rec = x.rec;
-                m = -CUDART_INF_F;
                 l = 0.0f;
             }
             const bool live = q4 * 32 < nrows;                              // of the warp
@@ -261,15 +266,21 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                 sh.top[u & 1][half][r] = t;
                 if (!(ok = meet())) break;
                 t = fmaxf(t, sh.top[u & 1][half ^ 1][r]) * scale;
-                if (it.fresh) m = t;
-                else if (__any_sync(0xffffffffu, t > m + kTcSlack)) {
+                auto refer = [&](float to) {
+                    m = to;
+                    limit = tc_limit(m);
+                    base = m == -CUDART_INF_F ? 0.0f : tc_base<D>(m);
+                    far = __any_sync(0xffffffffu, tc_far(m));
+                };
+                if (it.fresh) refer(t);
+                else if (__any_sync(0xffffffffu, t > limit)) {
                     // a maximum well above the reference: O (half of it here) and l move to it
                     ok = mbar_wait(&sh.pv_done[(u - 1) & 1], ((u - 1) >> 1) & 1);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                     tc_fence_after();
-                    const float to = t > m + kTcSlack ? t : m, move = tc_base<D>(m) - tc_base<D>(to);
+                    const float to = t > limit ? t : m, move = tc_base<D>(m) - tc_base<D>(to);
                     const float f = to == -CUDART_INF_F ? 1.0f : exp2_fast(move);
-                    m = to;
+                    refer(to);
                     l *= f;
 #pragma unroll 1
                     for (int c = half * 64; c < min(hd, half * 64 + 64); c += 32) {
@@ -282,21 +293,32 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                     }
                     tc_wait_st();
                 }
-                const float base = m == -CUDART_INF_F ? 0.0f : tc_base<D>(m);
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                auto weigh = [&](float times) {
+                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                    for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const float e = exp2_fast(__fmaf_rn(__uint_as_float(x[c][j]), scale, -base));
-                        const float f = exp2_fast(__fmaf_rn(__uint_as_float(x[c][j + 1]), scale, -base));
-                        sum[j & 2] += e;
-                        sum[(j & 2) + 1] += f;
-                        // rounded to the 16-bit type for the product with v; the sum takes the unrounded ones (see probability_base)
-                        x[0][c * 16 + j / 2] = D::encode2(e, f);
-                    }
-                tc_st32(at + half * 32, x[0]);
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                        for (int j = 0; j < 32; j += 2) {
+                            const float e = exp2_fast(__fmaf_rn(__uint_as_float(x[c][j]), times, -base));
+                            const float f = exp2_fast(__fmaf_rn(__uint_as_float(x[c][j + 1]), times, -base));
+                            sum[j & 2] += e;
+                            sum[(j & 2) + 1] += f;
+                            // rounded to the 16-bit type for the product with v; the sum takes the unrounded ones (see probability_base)
+                            x[0][c * 16 + j / 2] = D::encode2(e, f);
+                        }
+                    tc_st32(at + half * 32, x[0]);
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                };
+                if (!far)
+                    weigh(scale);
+                else {                      // (code of its own: the test costs 384 rows x 32779 keys 2 us; one loop for both, 4)
+                    const float first = tc_far(m) ? scale : 1.0f;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[c][j] = __float_as_uint(__fmul_rn(__uint_as_float(x[c][j]), first));
+                    weigh(tc_far(m) ? 1.0f : scale);
+                }
                 tc_wait_st();
             }
             tc_fence_before();

@@ -53,3 +53,22 @@ def test_attention_many_small_weights_beside_one_large(shape, log2_weight, place
     tol = U16[dtype] * 1.001 * want.abs() + (U16[dtype] + 2 * off) * 1.01 * mag + TINY[dtype] + (n * 2.0 ** -32 * 2 if dtype is torch.float16 else 0)
     err = (out.double() - want).abs()
     assert (err <= tol).all(), "off by %.3g of the output" % (err / want.abs()).max().item()
+
+
+# ---------------------------------------------------------------------------- large scores
+@pytest.mark.parametrize("n_seq,heads", [(3, 4), (40, 16)])
+@pytest.mark.parametrize("dtype,log2_size", [(torch.float16, e) for e in (8, 9, 12, 13, 15)] + [(torch.bfloat16, e) for e in (8, 9, 13, 16, 20, 24)])
+def test_attention_of_scores_far_beyond_the_exponents_resolution(n_seq, heads, dtype, log2_size):
+    """Queries and keys of plus and minus 2^e: scores are exact multiples of 2^(2e), and each row's own key leads by so much
+    that the softmax has nothing else: the output is that key's value."""
+    g, n, d, page = gen(17), 4100, 64, 16
+    cache = make_cache(-(-n // page) + n_seq, page, heads, d, dtype)
+    sign = lambda *s: torch.randint(0, 2, s, generator=g, device="cuda").mul_(2).sub_(1).to(dtype) * 2.0 ** log2_size  # noqa: E731
+    cache.k.copy_(sign(*cache.k.shape))
+    q = sign(n_seq, heads, d)
+    pages = torch.arange(cache.n_pages, dtype=torch.int32, device="cuda")
+    at = (torch.arange(n_seq, device="cuda") * 997 + 65) % n         # where each sequence's key lies in the prefix
+    cache.k[at // page, at % page] = q
+    attend = aweq.PrefixAttention(cache, pages[:-n_seq], n, heads, n_seq, 1, page)
+    out = attend(q, pages[-n_seq:].view(-1, 1), torch.full((n_seq,), 5, dtype=torch.int32, device="cuda"))
+    assert torch.equal(out, cache.v[at // page, at % page])
