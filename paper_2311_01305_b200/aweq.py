@@ -441,16 +441,23 @@ class LinearW8A8:
     """A calibrated 8-bit linear layer ready to run: holds the step-4 codes (one pair per output channel,
     or a single pair), the corrected binary32 bias and the codes' row sums (formed here, once), and
     marshals them once.  Calling it with step-6 codes and their pairs (one per token, or a single
-    pair) writes the 16-bit output on the current stream."""
+    pair) writes the 16-bit output on the current stream.
 
-    def __init__(self, codes, step, zp, bias=None):
+    The layer is what its arguments are now: it copies them, so that a calibration that runs again into the
+    same tensors changes the next layer and not this one.  ``copy=False`` keeps the tensors themselves, for a
+    caller that writes none of them as long as the layer lives (new codes would meet old row sums)."""
+
+    def __init__(self, codes, step, zp, bias=None, copy=True):
         _want_codes(codes, "codes")
+        _ld(codes)
         self.C_out, self.C_in = codes.shape
         gran = PER_TENSOR if step.numel() == 1 and self.C_out != 1 else PER_ROW
         pairs = self.C_out if gran == PER_ROW else 1
         _want(step, torch.float32, pairs, "step")
         _want(zp, torch.int32, pairs, "zp")
         _want(bias, torch.float32, self.C_out, "bias")
+        if copy:
+            codes, step, zp, bias = (None if t is None else t.clone(memory_format=torch.contiguous_format) for t in (codes, step, zp, bias))
         self.codes, self.step, self.zp, self.bias = codes, step, zp, bias
         self.w_sum = aweq_code_sums(codes)
         self._weight = (_ptr(codes), _ld(codes), _ptr(step), _ptr(zp), _ptr(self.w_sum), gran, _ptr(bias))

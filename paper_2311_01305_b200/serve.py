@@ -24,7 +24,7 @@ def joint_linear(cal: calibrate.LayerCalibrator, names: Sequence[str]) -> aweq.L
     """The calibrated linears ``names``, which share an input, as one product (channels one after the other)."""
     outs = [cal.out[n] for n in names]
     return aweq.LinearW8A8(torch.cat([o["codes"] for o in outs]), torch.cat([o["step"] for o in outs]),
-                           torch.cat([o["zp"] for o in outs]), torch.cat([o["bias_f32"] for o in outs]))
+                           torch.cat([o["zp"] for o in outs]), torch.cat([o["bias_f32"] for o in outs]), copy=False)
 
 
 class AttentionBlock:

@@ -72,3 +72,18 @@ def test_attention_of_scores_far_beyond_the_exponents_resolution(n_seq, heads, d
     attend = aweq.PrefixAttention(cache, pages[:-n_seq], n, heads, n_seq, 1, page)
     out = attend(q, pages[-n_seq:].view(-1, 1), torch.full((n_seq,), 5, dtype=torch.int32, device="cuda"))
     assert torch.equal(out, cache.v[at // page, at % page])
+
+
+# ---------------------------------------------------------------------------- a layer is what it was made of
+@pytest.mark.parametrize("n", [3, 300])
+def test_linear_layer_keeps_its_weights_when_the_callers_change(n):
+    """A calibrator that runs again writes its codes, Steps and zero-points in place."""
+    i = linear_inputs(n, 256, 72, 15)
+    layer = aweq.LinearW8A8(i["w"], i["ws"], i["wz"], i["b"])
+    want = layer(i["x"], i["xs"], i["xz"])
+    i["w"].copy_(255 - i["w"])
+    i["ws"].mul_(3.0)
+    i["wz"].add_(5)
+    i["b"].add_(1.0)
+    assert torch.equal(layer(i["x"], i["xs"], i["xz"]), want)
+    linear_check(i, torch.float16)                                 # a layer made of them now
