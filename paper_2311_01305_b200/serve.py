@@ -29,7 +29,7 @@ def joint_linear(cal: calibrate.LayerCalibrator, names: Sequence[str]) -> aweq.L
 
 class AttentionBlock:
     """``cal``: a calibrator that has run, of a workload with 8-bit row-wise weights and activation
-    quantisation.  ``pages`` / ``page_size``: the cache it makes (16-bit, in the workload's type)."""
+    quantisation; what it left is copied.  ``pages`` / ``page_size``: the cache it makes (16-bit, in the workload's type)."""
 
     def __init__(self, cal: calibrate.LayerCalibrator, n_heads: int, pages: int, page_size: int = 16, rope: Optional[torch.Tensor] = None,
                  interleaved: bool = False):
@@ -41,7 +41,7 @@ class AttentionBlock:
         self.n_kv = width["k"] // self.head_dim
         self.dtype, dev = synth.torch_dtype(wl.dtype), cal.ws.device
         self.qkv, self.o = joint_linear(cal, ("q", "k", "v")), joint_linear(cal, ("o",))
-        self.rinv = {i: cal.out[i]["rinv"] if cal.equalized else None for i in ("attn_in", "o_in")}
+        self.rinv = {i: cal.out[i]["rinv"].clone() if cal.equalized else None for i in ("attn_in", "o_in")}
         shape = (pages, page_size, self.n_kv, self.head_dim)
         self.cache = aweq.KVCache(torch.zeros(shape, dtype=self.dtype, device=dev), torch.zeros(shape, dtype=self.dtype, device=dev))
         self.rope, self.interleaved = rope, interleaved
