@@ -71,6 +71,8 @@ class AttentionBlock:
                  seq: torch.Tensor, st: Optional[torch.Tensor] = None) -> torch.Tensor:
         """``x`` [n_seq * n_q, C_in], the block's input of every new token, sequence by sequence; ``pos`` their positions
         (a shared prefix counts), ``seq`` their sequences, ``own_len`` each sequence's own keys, these included."""
+        if x.dim() != 2 or x.shape != (attend.n_seq * attend.n_q, self.qkv.C_in) or attend.cache is not self.cache:
+            raise ValueError("x must be [%d x %d], with an attention of this block" % (attend.n_seq * attend.n_q, self.qkv.C_in))
         n, b = x.shape[0], self._buffer(x.shape[0])
         self.qkv(*self._quantised(x, self.rinv["attn_in"], b["x"]), b["qkv"], st=st)
         h, kv, d = self.n_heads, self.n_kv, self.head_dim

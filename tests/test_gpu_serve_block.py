@@ -37,3 +37,16 @@ def test_block_keeps_what_it_was_made_of():
             if isinstance(t, torch.Tensor) and t.is_floating_point():
                 t.mul_(1.5)
     assert torch.equal(step(), want)
+
+
+def test_block_refuses_inputs_of_another_shape():
+    """The codes of an input wider than the layer's would not fit the buffers made for them."""
+    cal, x = calibrated()
+    block, other = (serve.AttentionBlock(cal, 12, 4) for _ in range(2))
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2)
+    for bad in (torch.cat([x[:10], x[:10, :16]], 1), x[:10, :752].contiguous(), x[:9].contiguous(), x[:11].contiguous(), x[0]):
+        with pytest.raises(ValueError):
+            chunk(block, bad, 2, 5, 32, table)()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        block(x[:2].contiguous(), other.attention(2, 1, max_own=16), table, torch.ones(2, **i32), torch.zeros(2, **i32), torch.arange(2, **i32))
