@@ -13,7 +13,7 @@ from the 16-bit layer and what a step takes.
 """
 from __future__ import annotations
 
-from typing import Dict, Optional, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import torch
 
@@ -27,9 +27,34 @@ def joint_linear(cal: calibrate.LayerCalibrator, names: Sequence[str]) -> aweq.L
                            torch.cat([o["zp"] for o in outs]), torch.cat([o["bias_f32"] for o in outs]), copy=False)
 
 
+class _Scratch:
+    """What lies between the calls of a block, for up to ``rows`` tokens; ``of(n)``: its first n rows."""
+
+    def __init__(self, block: "AttentionBlock", rows: int):
+        dev, self.rows, self.n = block.cache.k.device, rows, -1
+        u8 = lambda c: (torch.empty((rows, c), dtype=torch.uint8, device=dev), torch.empty(rows, device=dev),  # noqa: E731
+                        torch.empty(rows, dtype=torch.int32, device=dev))
+        self.x, self.o = u8(block.qkv.C_in), u8(block.o.C_in)
+        h, kv, d = block.n_heads, block.n_kv, block.head_dim
+        self.widths, self.d = [h * d, kv * d, kv * d], d
+        self.qkv = torch.empty((rows, block.qkv.C_out), dtype=block.dtype, device=dev)
+        self.q, self.attended = (torch.empty((rows, h, d), dtype=block.dtype, device=dev) for _ in range(2))
+
+    def of(self, n: int):
+        if n != self.n:
+            x, o = (tuple(t[:n] for t in u) for u in (self.x, self.o))
+            qkv, q, attended = self.qkv[:n], self.q[:n], self.attended[:n]
+            self.views = x, o, qkv, [t.unflatten(1, (-1, self.d)) for t in qkv.split(self.widths, 1)], q, attended, attended.flatten(1)
+            self.n = n
+        return self.views
+
+
 class AttentionBlock:
     """``cal``: a calibrator that has run, of a workload with 8-bit row-wise weights and activation
-    quantisation; what it left is copied.  ``pages`` / ``page_size``: the cache it makes (16-bit, in the workload's type)."""
+    quantisation; what it left is copied.  ``pages`` / ``page_size``: the cache it makes (16-bit, in the workload's type).
+
+    Several streams or threads may call a block at a time, each with an attention of its own (``attention``) and pages that the
+    others do not write.  The block keeps one set of buffers for each that did, for the most tokens it had."""
 
     def __init__(self, cal: calibrate.LayerCalibrator, n_heads: int, pages: int, page_size: int = 16, rope: Optional[torch.Tensor] = None,
                  interleaved: bool = False):
@@ -45,22 +70,11 @@ class AttentionBlock:
         shape = (pages, page_size, self.n_kv, self.head_dim)
         self.cache = aweq.KVCache(torch.zeros(shape, dtype=self.dtype, device=dev), torch.zeros(shape, dtype=self.dtype, device=dev))
         self.rope, self.interleaved = rope, interleaved
-        self._buffers: Dict[int, dict] = {}
+        self._idle: Dict[int, List[_Scratch]] = {}          # by stream
 
-    def _quantised(self, x: torch.Tensor, rinv, b: dict):
-        aweq.aweq_quant_act(x, rinv, 8, aweq.PER_ROW, None, b["codes"], b["step"], b["zp"])
-        return b["codes"], b["step"], b["zp"]
-
-    def _buffer(self, n: int) -> dict:
-        if n not in self._buffers:
-            dev, h = self.cache.k.device, self.n_heads * self.head_dim
-            u8 = lambda c: dict(codes=torch.empty((n, c), dtype=torch.uint8, device=dev), step=torch.empty(n, device=dev),  # noqa: E731
-                                zp=torch.empty(n, dtype=torch.int32, device=dev))
-            self._buffers[n] = dict(x=u8(self.qkv.C_in), o=u8(self.o.C_in),
-                                    qkv=torch.empty((n, self.qkv.C_out), dtype=self.dtype, device=dev),
-                                    q=torch.empty((n, self.n_heads, self.head_dim), dtype=self.dtype, device=dev),
-                                    attended=torch.empty((n, h), dtype=self.dtype, device=dev))
-        return self._buffers[n]
+    def _quantised(self, x: torch.Tensor, rinv, into):
+        aweq.aweq_quant_act(x, rinv, 8, aweq.PER_ROW, None, *into)
+        return into
 
     def attention(self, n_seq: int, n_q: int = 1, prefix_pages: Optional[torch.Tensor] = None, prefix_len: int = 0,
                   max_own: Optional[int] = None) -> aweq.PrefixAttention:
@@ -73,15 +87,25 @@ class AttentionBlock:
         (a shared prefix counts), ``seq`` their sequences, ``own_len`` each sequence's own keys, these included."""
         if x.dim() != 2 or x.shape != (attend.n_seq * attend.n_q, self.qkv.C_in) or attend.cache is not self.cache:
             raise ValueError("x must be [%d x %d], with an attention of this block" % (attend.n_seq * attend.n_q, self.qkv.C_in))
-        n, b = x.shape[0], self._buffer(x.shape[0])
-        self.qkv(*self._quantised(x, self.rinv["attn_in"], b["x"]), b["qkv"], st=st)
-        h, kv, d = self.n_heads, self.n_kv, self.head_dim
-        q, k, v = (t.unflatten(1, (-1, d)) for t in b["qkv"].split([h * d, kv * d, kv * d], 1))
+        # A set of the current stream that no other thread is using, or a new one; a call's work is in the stream when it gives its
+        # set back.  A graph that is being captured keeps its own.
+        capturing = torch.cuda.is_current_stream_capturing()
+        idle = self._idle.setdefault(torch.cuda.current_stream(x.device).cuda_stream, [])
+        try:
+            scratch = None if capturing else idle.pop()
+        except IndexError:
+            scratch = None
+        if scratch is None or scratch.rows < x.shape[0]:
+            scratch = _Scratch(self, x.shape[0])
+        for_x, for_o, qkv, (q, k, v), q_turned, attended, attended_rows = scratch.of(x.shape[0])
+        self.qkv(*self._quantised(x, self.rinv["attn_in"], for_x), qkv, st=st)
         aweq.aweq_kv_append(self.cache, page_table, k, v, pos, seq=seq, first=attend.prefix_len, table=self.rope,
-                            interleaved=self.interleaved, q=q, q_out=b["q"], st=st)
-        attend(b["q"], page_table, own_len, b["attended"].unflatten(1, (h, d)), st=st)
-        out = torch.empty((n, self.o.C_out), dtype=self.dtype, device=x.device)
-        return self.o(*self._quantised(b["attended"], self.rinv["o_in"], b["o"]), out, st=st)
+                            interleaved=self.interleaved, q=q, q_out=q_turned, st=st)
+        attend(q_turned, page_table, own_len, attended, st=st)
+        out = self.o(*self._quantised(attended_rows, self.rinv["o_in"], for_o), dtype=self.dtype, st=st)
+        if not capturing:
+            idle.append(scratch)
+        return out
 
 
 def main(n_seq: int = 16, prefix: int = 500, steps: int = 8) -> None:
