@@ -541,7 +541,8 @@ static Linear8Choice linear8_choose(long long N, int K, int O)
     double cost = 6.0 + waves * nkb * (0.3 + 0.1 * (tiles < 60 ? tiles / 60 : 1.0));
     static const int bns[5] = {32, 64, 96, 128, 256}, most[5] = {0, kSmCount, kSmCount, 120, 128};
     if (N <= 256)
-        for (int bn : bns)
+        for (int bn : bns) {
+            if ((O + bn - 1) / bn > 65535) continue;             // channels lie on the grid's second dimension
             for (int slices = 1; slices <= 4 && slices <= nkb; ++slices) {
                 const int mb = N > 128 && bn <= 128 ? 2 : 1;
                 const double rows = N < 128 * mb ? (double)N : 128.0 * mb, box = rows + 7;
@@ -559,6 +560,7 @@ static Linear8Choice linear8_choose(long long N, int K, int O)
                     best = {1, bn, slices};
                 }
             }
+        }
     return best;
 }
 

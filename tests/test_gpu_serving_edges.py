@@ -87,3 +87,9 @@ def test_linear_layer_keeps_its_weights_when_the_callers_change(n):
     i["b"].add_(1.0)
     assert torch.equal(layer(i["x"], i["xs"], i["xz"]), want)
     linear_check(i, torch.float16)                                 # a layer made of them now
+
+
+# ---------------------------------------------------------------------------- channels beyond a grid's limit
+@pytest.mark.parametrize("n,k,o", [(1, 64, 65535 * 64 + 65), (17, 16, 65535 * 64 + 1), (3, 64, 65535 * 256 + 300)])
+def test_linear_millions_of_channels(n, k, o):
+    linear_check(linear_inputs(n, k, o, 6), torch.float16)
