@@ -66,7 +66,8 @@ static AttentionPlan attention_plan(const aweq_kv_cache *c, long long prefix_len
     p.rows = n_seq * n_q * n_heads;
     tensor_unit(c->page_size, &p.pre_unit, &p.box);
     p.unit = kAtTile;
-    p.tensor = p.pre_unit >= 96 && prefix_len > 0 && attention_prefers_tensor(pre_rows, (prefix_len + p.pre_unit - 1) / p.pre_unit * n_kv);
+    p.tensor = p.pre_unit >= 96 && prefix_len > 0 && tma_pool_fits(c->page_stride, c->token_stride, c->head_stride) &&
+               attention_prefers_tensor(pre_rows, (prefix_len + p.pre_unit - 1) / p.pre_unit * n_kv);
     if (!p.tensor) p.pre_unit = p.unit;
     p.pre_tile = p.tensor ? 128 : pre_rows <= 16 ? 16 : pre_rows <= 32 ? 32 : 64;
     p.own_tile = own_rows <= 16 ? 16 : own_rows <= 32 ? 32 : 64;
@@ -742,10 +743,11 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
 }
 
 // Keys of a tiled copy: a box lies in one page, on a row of the stage that keeps the swizzle's phase (a multiple of eight).
-// 0: the four warps' 16-byte copies, for other page sizes, and where the units do not even fill the device once.
+// 0: the four warps' 16-byte copies, for other page sizes and strides, and where the units do not even fill the device once.
 static int units_box(const AttentionArgs &a, const AttentionPlan &p)
 {
     if (p.tensor || !p.pre_tiles || a.page_size % 8 || p.ctas < kSmCount * kAtCtasPerSm) return 0;
+    if (!tma_pool_fits(a.page_stride, a.token_stride, a.head_stride)) return 0;
     int box = 8;
     while (box < kAtTile && a.page_size % (2 * box) == 0) box *= 2;
     return box;
@@ -756,10 +758,13 @@ static aweq_status units_launch(const AttentionArgs &a, const AttentionPlan &p, 
 {
     constexpr int smem = kAtStages * attention_stage_bytes<DP>() + 1024;
     CUtensorMap mk = {}, mv = {};
-    int box = units_box(a, p);
-    if (box && (tma_pool_map(&mk, a.ck, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, box) != AWEQ_OK ||
-                tma_pool_map(&mv, a.cv, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, box) != AWEQ_OK))
-        box = 0;                                                // strides that a tensor map cannot hold
+    const int box = units_box(a, p);
+    if (box) {
+        aweq_status rc = tma_pool_map(&mk, a.ck, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, box);
+        if (rc == AWEQ_OK)
+            rc = tma_pool_map(&mv, a.cv, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, box);
+        if (rc != AWEQ_OK) return rc;
+    }
     static std::atomic<unsigned long long> allowed{0};
     AWEQ_CUDA_OK(allow_smem(attention_units_kernel<D, DP, WMP, WMO>, smem, allowed));
     AWEQ_LAUNCH((attention_units_kernel<D, DP, WMP, WMO>), dim3((unsigned)p.ctas), dim3(kAtThreads), smem, stream, a, p, mk, mv, ws, box, p.tensor != 0);

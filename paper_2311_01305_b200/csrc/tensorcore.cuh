@@ -13,6 +13,11 @@ namespace aweq {
 aweq_status tma_bytes_map(CUtensorMap *map, const void *base, long long rows, long long cols, long long ld, int box_rows);
 // A pool of 16-bit pages [pages x tokens x heads x dim] with any strides (elements, multiples of 8), read in boxes of
 // box_tokens tokens x 64 elements of one head, rows swizzled by 128 bytes; elements past head_dim read as zero.
+// Strides of 2^40 bytes and more do not fit a tensor map.
+inline bool tma_pool_fits(long long page_stride, long long token_stride, long long head_stride)
+{
+    return page_stride < 1ll << 39 && token_stride < 1ll << 39 && head_stride < 1ll << 39;
+}
 aweq_status tma_pool_map(CUtensorMap *map, const void *base, long long pages, int tokens, int heads, int dim, long long page_stride,
                          long long token_stride, long long head_stride, int box_tokens);
 

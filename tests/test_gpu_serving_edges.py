@@ -93,3 +93,26 @@ def test_linear_layer_keeps_its_weights_when_the_callers_change(n):
 @pytest.mark.parametrize("n,k,o", [(1, 64, 65535 * 64 + 65), (17, 16, 65535 * 64 + 1), (3, 64, 65535 * 256 + 300)])
 def test_linear_millions_of_channels(n, k, o):
     linear_check(linear_inputs(n, k, o, 6), torch.float16)
+
+
+# ---------------------------------------------------------------------------- strides that no tiled copy can hold
+@pytest.mark.parametrize("page_stride", [0, 1 << 40])
+@pytest.mark.parametrize("n_seq", [2, 20, 40])
+def test_attention_over_one_page_of_any_stride(n_seq, page_stride):
+    """Everything in one page: its stride is never used, and may be more than a tiled copy can hold, or nothing.  Few rows and many
+    rows take different kernels; both answer."""
+    h, d, n = 16, 64, 4096
+    cache = make_cache(1, n, h, d, torch.float16)
+    cache.args.page_stride = page_stride
+    zero = torch.zeros((n_seq, 1), dtype=torch.int32, device="cuda")
+    lens = torch.full((n_seq,), 30, dtype=torch.int32, device="cuda")
+    q = (2.0 * torch.randn((n_seq, h, d), generator=gen(9), device="cuda")).to(torch.float16)
+    out = aweq.PrefixAttention(cache, zero[0], n - 7, h, n_seq, 1, 64)(q, zero, lens)
+    cache.args.page_stride = n * h * d
+    assert torch.isfinite(out).all()
+    plain = aweq.PrefixAttention(cache, zero[0], n - 7, h, n_seq, 1, 64)(q, zero, lens)
+    want, mag, reach = attention_reference(q, cache, zero[0], n - 7, zero, lens, 1, d ** -0.5)
+    off = (reach * d * 2.0 ** -23 + 2.0 ** -20 + (n / 16 + 64) * 2.0 ** -23)[..., None]
+    tol = U16[torch.float16] * 1.001 * want.abs() + (U16[torch.float16] + 2 * off) * 1.01 * mag + TINY[torch.float16]
+    for got in (out, plain):
+        assert ((got.double() - want).abs() <= tol).all()
