@@ -489,7 +489,8 @@ aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, lo
  * the n_q tokens themselves included, appended before this call):
  *   out[b n_q + i, h] = sum_j p_j v_j,  p = softmax_j(scale q . k_j)
  * over all prefix keys and the own keys j < own_len[b] - (n_q - 1 - i); head h reads key head
- * h / (n_heads / n_kv_heads).  A row without keys gives zeros.  The prefix is read once for all rows
+ * h / (n_heads / n_kv_heads).  A row without keys gives zeros, one whose
+ * scores are all minus infinity NaN.  The prefix is read once for all rows
  * of the batch.  Scores, running maximum, sum and output are binary32; the probabilities are
  * rounded to the 16-bit type for the product with v (fp16: to 2^-32 of a row's largest at worst, however
  * small they are); one rounding at the end.

@@ -736,7 +736,9 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
         }
     }
     if (in) {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;          // no key at all: zeros
+        // no key at all: zeros (keys whose scores are all minus infinity: 0 / 0, as the softmax of them is)
+        const bool none = l == 0.0f && a.prefix_len == 0 && own_length(a, b) < a.n_q - (int)(tok % (unsigned)a.n_q);
+        const float inv = none ? 0.0f : 1.0f / l;
         *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.ldo + (long long)h * hd + lane * 4) =
             make_uint2(D::encode2(o.x * inv, o.y * inv), D::encode2(o.z * inv, o.w * inv));
     }

@@ -116,3 +116,22 @@ def test_attention_over_one_page_of_any_stride(n_seq, page_stride):
     tol = U16[torch.float16] * 1.001 * want.abs() + (U16[torch.float16] + 2 * off) * 1.01 * mag + TINY[torch.float16]
     for got in (out, plain):
         assert ((got.double() - want).abs() <= tol).all()
+
+
+# ---------------------------------------------------------------------------- scores of minus infinity
+@pytest.mark.parametrize("n_seq,heads,prefix", [(3, 4, 70), (3, 4, 0), (40, 16, 4100)])
+def test_attention_of_scores_that_are_all_minus_infinity(n_seq, heads, prefix):
+    """The softmax of such a row is 0 / 0.  A row that sees no key stays zero."""
+    q, cache, prefix_pages, pages, lens = attention_case(n_seq, 2, heads, heads, 64, prefix, [5] * n_seq, 16, torch.float16, stale=False)
+    cache.k[..., 3] = -math.inf
+    q[..., 3] = 1.0
+    q[2, :, 3] = -1.0
+    attend = aweq.PrefixAttention(cache, prefix_pages, prefix, heads, n_seq, 2)
+    if prefix == 0:
+        lens[2] = 1                                                # its first token sees nothing
+    out = attend(q, pages, lens)
+    nothing = torch.zeros(2 * n_seq, dtype=torch.bool, device="cuda")
+    if prefix == 0:
+        nothing[4] = True
+    assert (out[nothing] == 0).all()
+    assert torch.isnan(out[~nothing]).all()
