@@ -105,7 +105,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
             const bool lead = warp == 0;
             const CUtensorMap *const map = lead ? &mapK : &mapV;
             const int boxes = p.pre_unit / p.box;
-            auto has = [&](int tile) { return lane < boxes && tile * p.pre_unit + lane * p.box < a.prefix_len; };
+            auto has = [&](int tile) { return lane < boxes && (long long)tile * p.pre_unit + lane * p.box < a.prefix_len; };
             auto look_up = [&](int tile) {                                  // entry of the lane's box (not looked at here: the load flies)
                 return has(tile) ? __ldg(a.prefix_pages + (unsigned)(tile * p.pre_unit + lane * p.box) / (unsigned)a.page_size) : 0;
             };

@@ -135,3 +135,25 @@ def test_attention_of_scores_that_are_all_minus_infinity(n_seq, heads, prefix):
         nothing[4] = True
     assert (out[nothing] == 0).all()
     assert torch.isnan(out[~nothing]).all()
+
+
+# ---------------------------------------------------------------------------- the longest prefix
+def test_attention_of_the_longest_prefix():
+    """2^31 - 1 keys, most of them the same page: 24 keys to a page, five pages to a unit, so the last unit reaches past what 31 bits
+    count.  The last seven keys outweigh all others; what lies behind them in their page is not a number."""
+    n, page, d, n_seq = 2 ** 31 - 1, 24, 8, 33
+    cache = make_cache(2, page, 1, d, torch.float16)
+    cache.k.zero_()
+    cache.k[1, :n % page, 0, 0], cache.k[1, n % page:], cache.v[1, n % page:] = 60.0, math.nan, math.nan
+    pages = torch.zeros(-(-n // page), dtype=torch.int32, device="cuda")
+    pages[-1] = 1
+    q = torch.zeros((n_seq, 1, d), dtype=torch.float16, device="cuda")
+    q[:, 0, 0] = 1.0
+    lens = torch.zeros(n_seq, dtype=torch.int32, device="cuda")
+    st = aweq.new_status()
+    out = aweq.PrefixAttention(cache, pages, n, 1, n_seq, 1, 0, scale=1.0)(q, torch.zeros((n_seq, 1), dtype=torch.int32, device="cuda"), lens, st=st)
+    assert aweq.read_out_of_range(st) == 0 and aweq.read_status(st)["wait_timeout"] == 0
+    # exp(60) seven times beside 2^31 ones; the other keys' share is below 2^-55
+    want = cache.v[1, :n % page, 0].double().mean(0)
+    tol = U16[torch.float16] * (1.001 * want.abs() + 1.02 * cache.v[1, :n % page, 0].double().abs().mean(0)) + TINY[torch.float16]
+    assert ((out[:, 0].double() - want).abs() <= tol + 2.0 ** -18).all()
