@@ -419,7 +419,8 @@ aweq_status aweq_code_sums(const unsigned char *codes, long long rows, long long
 
 /* The calibrated W8A8 layer (Eq. 1-2 de-quantised on both sides, bias of Eq. 15):
  *   out[n,o] = round16( Step^x_n Step^w_o sum_k (Xq[n,k] - Z^x_n)(Wq[o,k] - Z^w_o) + bias[o] ).
- * The sum is formed in integers (tensor cores) and is exact as long as it fits 53 bits; the two
+ * The sum is formed in integers (tensor cores) and is exact as long as C_in times the largest |Xq - Z^x| and
+ * |Wq - Z^w| that 8-bit codes can make is below 2^62 (beyond, its parts are joined in binary64); the two
  * Steps and the bias are applied in binary32 and the result is rounded once to the 16-bit type.
  * Xq: step-6 codes [N x C_in], one per byte (any bit-width), row pitch ldx bytes; act_step / act_zp:
  * one pair per token (act_gran AWEQ_PER_ROW) or a single pair (AWEQ_PER_TENSOR).

@@ -11,13 +11,18 @@ namespace aweq {
 // acc from its parts.  With bx = max(|Z^x|, |255 - Z^x|) no |xq - Z^x| is larger than bx, likewise
 // for w, so |acc| <= K bx bw.  Where that is below 2^31 (every pair of zero-points inside the code
 // range up to K = 33025, and far beyond for zero-points near the middle) the parts may wrap and
-// acc is still exact modulo 2^32, hence exact.  Otherwise the parts are joined in binary64: S itself
-// is below 2^32 for K <= 65536, and every sum is exact while it stays below 2^53.
+// acc is still exact modulo 2^32, hence exact; below 2^62 the same holds of 64 bits.  Beyond, the parts are joined in
+// binary64 (S itself is below 2^32 for K <= 65536), rounded where they pass 2^53.
 __device__ __forceinline__ float linear8_acc(uint32_t S, int zx, uint32_t rx, int zw, uint32_t cw, uint32_t K, float bxK,
                                              float bw)
 {
     if (bxK * bw < 2.147e9f)
         return (float)(int)(S - (uint32_t)zx * cw - (uint32_t)zw * (rx - K * (uint32_t)zx));
+    if (bxK * bw < 4.6e18f) {
+        const long long x = zx, w = zw;
+        const unsigned long long u = rx - K * (unsigned long long)x;
+        return (float)(long long)(S - (unsigned long long)x * cw - (unsigned long long)w * u);
+    }
     const double u = (double)rx - (double)K * (double)zx;
     return (float)((double)S - (double)zx * (double)cw - (double)zw * u);
 }

@@ -157,3 +157,22 @@ def test_attention_of_the_longest_prefix():
     want = cache.v[1, :n % page, 0].double().mean(0)
     tol = U16[torch.float16] * (1.001 * want.abs() + 1.02 * cache.v[1, :n % page, 0].double().abs().mean(0)) + TINY[torch.float16]
     assert ((out[:, 0].double() - want).abs() <= tol + 2.0 ** -18).all()
+
+
+# ---------------------------------------------------------------------------- zero-points of 31 bits
+@pytest.mark.parametrize("n", [2, 100, 300])
+@pytest.mark.parametrize("side", ["x", "w"])
+def test_linear_sums_that_cancel_behind_large_zero_points(n, side):
+    """One side's codes are all its zero-point, so the sum is zero whatever the other side's zero-point: the output is the
+    bias, rounded once.  The parts of the sum reach 2^55 here, the sum's bound K reach(Zx) reach(Zw) stays below 2^62."""
+    k, o = 65536, 40
+    i = linear_inputs(n, k, o, 8)
+    far = torch.tensor([2147483647, -2147483648, 2147483629, -2147483587], dtype=torch.int32, device="cuda")
+    xz, wz = (i["xz"], i["wz"]) if side == "w" else (i["wz"], i["xz"])
+    codes, steps = (i["w"], i["ws"]) if side == "w" else (i["x"], i["xs"])
+    xz.copy_(far.repeat(xz.numel() // 4 + 1)[:xz.numel()])
+    codes.fill_(255)
+    wz.fill_(255)
+    layer = aweq.LinearW8A8(i["w"], i["ws"], i["wz"], i["b"])
+    out = layer(i["x"], i["xs"], i["xz"])
+    assert torch.equal(out, i["b"].to(torch.float16).expand_as(out))
