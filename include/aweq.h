@@ -77,7 +77,8 @@ typedef enum { AWEQ_PER_TENSOR = 0, AWEQ_PER_ROW = 1, AWEQ_PER_GROUP = 2 } aweq_
  * statistics were Inf or NaN; zero_range: dead channels (factor forced to 1);
  * wait_timeout: a bounded wait inside a kernel gave up (results of that call
  * are invalid).  out_of_range: positions, lengths, sequence or page numbers that pointed outside
- * their table or pool (aweq_kv_append, aweq_prefix_attention; nothing was read or written there). */
+ * their table or pool (aweq_kv_append: tokens with one; aweq_prefix_attention: each once; nothing was read or
+ * written there). */
 typedef struct {
     unsigned long long nonfinite;
     unsigned long long zero_range;
@@ -499,7 +500,8 @@ aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, lo
  * pitches multiples of 8.  head_dim: a multiple of 8 up to 128.  own_len: device int[n_seq];
  * max_own: HOST bound on it (a smaller one makes a smaller launch).  A length above max_own or
  * pages_per_seq * page_size, or below zero, is clamped, a page outside the pool is replaced by page 0
- * (the sequence's output is then meaningless); both are counted in st->out_of_range.
+ * (the output of those that read it is then meaningless); st->out_of_range counts every such length, and every such
+ * entry of prefix_pages and of a sequence's row of page_table that holds keys, once.
  * ws: aweq_prefix_attention_workspace_bytes(...) bytes, 256-byte aligned. */
 size_t aweq_prefix_attention_workspace_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own,
                                              long long n_seq, int n_q, int n_heads);

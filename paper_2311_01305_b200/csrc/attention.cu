@@ -309,7 +309,7 @@ __device__ __forceinline__ void attention_boxes(const AttentionArgs &a, const At
             const int keys = now.len - now.tile * kAtTile - lane * box;
             const bool has = lane < boxes && keys > 0, bad = bad_page(a, page);
             const int n = __popc(__ballot_sync(0xffffffffu, has));
-            if (has && bad && a.st) atomicAdd(&a.st->out_of_range, (unsigned long long)min(box, keys));
+            if (has && bad) count_bad_page(a, now.kh, now.rt, now.tile * kAtTile + lane * box);
             if (lane == 0) {
                 ring.unit[s] = now;
                 mbar_arrive_expect_tx(&ring.landed[s], (uint32_t)(n * box * 256 * HALVES));
@@ -380,7 +380,7 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
             const int pg = bad ? 0 : page;
             w.advance(a, p);
             if (left > 1) page = w.entry(a, p, mine);           // the next unit's page, while this one's stage empties
-            if (has && bad && lane < 16 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+            if (has && bad && lane < 16) count_bad_page(a, now.kh, now.rt, now.tile * kAtTile + mine);
             // element offset of the row, -1: no such key
             const long long off = !has ? -1
                                            : (long long)pg * a.page_stride +

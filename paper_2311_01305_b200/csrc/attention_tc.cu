@@ -129,7 +129,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                     if (++rt == p.pre_rt) { rt = 0; ++kh; }
                 }
                 if (left > 1) page = look_up(tile);                         // the next unit's, while this stage empties
-                if (lead && there && bad && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+                if (lead && there && bad) count_bad_page(a, u.kh, u.rt, u.tile * p.pre_unit + lane * p.box);
                 ok = mbar_wait(&sh.empty[s], ph ^ 1);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 const int n = __popc(__ballot_sync(0xffffffffu, there));

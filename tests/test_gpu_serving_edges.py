@@ -176,3 +176,32 @@ def test_linear_sums_that_cancel_behind_large_zero_points(n, side):
     layer = aweq.LinearW8A8(i["w"], i["ws"], i["wz"], i["b"])
     out = layer(i["x"], i["xs"], i["xz"])
     assert torch.equal(out, i["b"].to(torch.float16).expand_as(out))
+
+
+# ---------------------------------------------------------------------------- counts
+def counted(attend, q, pages, lens):
+    st = aweq.new_status()
+    attend(q, pages, lens, st=st)
+    assert aweq.read_status(st)["wait_timeout"] == 0
+    return aweq.read_out_of_range(st)
+
+
+@pytest.mark.parametrize("n_seq,h,kv,page,prefix", [(5, 4, 2, 16, 200), (5, 4, 2, 7, 200), (16, 16, 16, 16, 4100), (70, 4, 1, 12, 400),
+                                                    (40, 16, 16, 16, 4100), (260, 16, 8, 128, 3700), (40, 14, 14, 256, 4096)])
+def test_attention_counts_every_bad_entry_once(n_seq, h, kv, page, prefix):
+    """A bad entry of the prefix's page list counts once, one of a sequence's pages once, a bad length once, whatever kernel meets it
+    and however many heads, rows and keys lie behind it; entries behind the last key are not looked at."""
+    q, cache, prefix_pages, pages, lens = attention_case(n_seq, 1, h, kv, 64, prefix, [(13 * b) % 60 + 1 for b in range(n_seq)], page,
+                                                         torch.float16, stale=False)
+    attend = aweq.PrefixAttention(cache, prefix_pages, prefix, h, n_seq, 1, 60)
+    assert counted(attend, q, pages, lens) == 0
+    for b in range(n_seq):
+        pages[b, -(-int(lens[b]) // page):] = -1
+    assert counted(attend, q, pages, lens) == 0
+    attend.prefix_pages[0], attend.prefix_pages[-1] = -5, cache.n_pages
+    assert counted(attend, q, pages, lens) == 2
+    pages[3, 0], pages[4, 0] = cache.n_pages + 3, -2
+    assert counted(attend, q, pages, lens) == 4
+    lens[0], lens[1] = 61, -1
+    # (the first sequence, of one key before, now reaches entries that were never given out)
+    assert counted(attend, q, pages, lens) == 6 + -(-60 // page) - 1
