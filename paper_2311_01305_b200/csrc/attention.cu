@@ -648,6 +648,9 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
 {
     __shared__ float part[4][128], part_l[4];
     pdl_begin();
+    // without own keys no other kernel looks at the lengths
+    if (!p.ctas && blockIdx.x == 0)
+        for (int b = threadIdx.x; b < (int)a.n_seq; b += 128) clamp_length(a, __ldg(a.own_len + b), true);
     const int lane = threadIdx.x & 31, warp = (int)(threadIdx.x >> 5) % WARPS, G = a.n_heads / a.n_kv, hd = a.head_dim;
     const unsigned r = blockIdx.x * (4 / WARPS) + (threadIdx.x >> 5) / WARPS;
     if (WARPS == 1 && r >= p.rows) return;

@@ -205,3 +205,11 @@ def test_attention_counts_every_bad_entry_once(n_seq, h, kv, page, prefix):
     lens[0], lens[1] = 61, -1
     # (the first sequence, of one key before, now reaches entries that were never given out)
     assert counted(attend, q, pages, lens) == 6 + -(-60 // page) - 1
+
+
+@pytest.mark.parametrize("n_seq,prefix", [(3, 0), (3, 50), (40, 4100)])
+def test_attention_counts_lengths_where_no_own_keys_are_allowed(n_seq, prefix):
+    q, cache, prefix_pages, pages, lens = attention_case(n_seq, 1, 16, 16, 64, prefix, [3] * n_seq, 16, torch.float16, stale=False)
+    attend = aweq.PrefixAttention(cache, prefix_pages, prefix, 16, n_seq, 1, max_own=0)
+    assert counted(attend, q, pages, lens) == n_seq
+    assert counted(attend, q, pages, torch.zeros_like(lens)) == 0
