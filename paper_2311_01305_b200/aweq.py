@@ -400,6 +400,12 @@ def _want(t: Optional[torch.Tensor], dtype, n: int, what: str) -> None:
         raise ValueError("%s must be a contiguous %s tensor of at least %d elements" % (what, dtype, n))
 
 
+def _pitch(t: torch.Tensor) -> int:
+    """Row pitch of a matrix; one row has none of its own (its stride may be anything)."""
+    _ld(t)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
 def _want_codes(t: torch.Tensor, what: str) -> None:
     if t.dtype != torch.uint8:
         raise TypeError("%s must be uint8 codes, got %s" % (what, t.dtype))
@@ -411,7 +417,7 @@ def aweq_code_sums(codes, sums=None):
     if sums is None:
         sums = torch.empty(codes.shape[0], dtype=torch.int32, device=codes.device)
     _want(sums, torch.int32, codes.shape[0], "sums")
-    _check(_lib.aweq_code_sums(_ptr(codes), codes.shape[0], codes.shape[1], _ld(codes), _ptr(sums), _stream()))
+    _check(_lib.aweq_code_sums(_ptr(codes), codes.shape[0], codes.shape[1], _pitch(codes), _ptr(sums), _stream()))
     return sums
 
 
@@ -431,9 +437,9 @@ def aweq_linear_w8a8(Xq, act_step, act_zp, act_gran, Wq, w_step, w_zp, w_sum, w_
     _want(w_zp, torch.int32, w_pairs, "w_zp")
     _want(w_sum, torch.int32, C_out, "w_sum")
     _want(bias, torch.float32, C_out, "bias")
-    _check(_lib.aweq_linear_w8a8(_ptr(Xq), _ld(Xq), _ptr(act_step), _ptr(act_zp), act_gran, _ptr(Wq), _ld(Wq), _ptr(w_step),
+    _check(_lib.aweq_linear_w8a8(_ptr(Xq), _pitch(Xq), _ptr(act_step), _ptr(act_zp), act_gran, _ptr(Wq), _pitch(Wq), _ptr(w_step),
                                  _ptr(w_zp), _ptr(w_sum), w_gran, _ptr(bias), N, C_in, C_out, _ptr(out), dtype_tag(out),
-                                 _ld(out), _ptr(st), _stream()))
+                                 _pitch(out), _ptr(st), _stream()))
     return out
 
 
@@ -449,7 +455,7 @@ class LinearW8A8:
 
     def __init__(self, codes, step, zp, bias=None, copy=True):
         _want_codes(codes, "codes")
-        _ld(codes)
+        ld = _pitch(codes)
         self.C_out, self.C_in = codes.shape
         gran = PER_TENSOR if step.numel() == 1 and self.C_out != 1 else PER_ROW
         pairs = self.C_out if gran == PER_ROW else 1
@@ -457,10 +463,11 @@ class LinearW8A8:
         _want(zp, torch.int32, pairs, "zp")
         _want(bias, torch.float32, self.C_out, "bias")
         if copy:
+            ld = self.C_in
             codes, step, zp, bias = (None if t is None else t.clone(memory_format=torch.contiguous_format) for t in (codes, step, zp, bias))
         self.codes, self.step, self.zp, self.bias = codes, step, zp, bias
         self.w_sum = aweq_code_sums(codes)
-        self._weight = (_ptr(codes), _ld(codes), _ptr(step), _ptr(zp), _ptr(self.w_sum), gran, _ptr(bias))
+        self._weight = (_ptr(codes), ld, _ptr(step), _ptr(zp), _ptr(self.w_sum), gran, _ptr(bias))
 
     def __call__(self, Xq, act_step, act_zp, out=None, dtype=torch.float16, st=None):
         n, c = Xq.shape
@@ -476,8 +483,8 @@ class LinearW8A8:
                 or not (Xq.is_cuda and out.is_cuda and act_step.is_cuda and act_zp.is_cuda)):
             raise ValueError("device tensors: Xq [N x %d] uint8, act_step / act_zp float32 / int32 of N or one element, "
                              "out [N x %d], rows contiguous" % (self.C_in, self.C_out))
-        if n == 1:                                                      # one row has no pitch of its own
-            ldx, ldo = max(ldx, c), max(ldo, self.C_out)
+        if n == 1:                                                      # (see _pitch)
+            ldx, ldo = c, self.C_out
         rc = _lib.aweq_linear_w8a8(Xq.data_ptr(), ldx, act_step.data_ptr(), act_zp.data_ptr(), PER_ROW if pairs == n else PER_TENSOR,
                                    *self._weight, n, c, self.C_out, out.data_ptr(), dtype_tag(out), ldo, _ptr(st), _stream())
         if rc:
@@ -510,7 +517,7 @@ class KVCache:
         self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = k.shape
         self.dtype = k.dtype
         # a dimension of one element has no stride of its own
-        stride = [max(k.stride(i), self.head_dim) if k.shape[i] == 1 else k.stride(i) for i in range(3)]
+        stride = [self.head_dim if k.shape[i] == 1 else k.stride(i) for i in range(3)]
         self.args = KvCacheArgs(_ptr(k), _ptr(v), dtype_tag(k), self.page_size, self.n_kv_heads, self.head_dim, self.n_pages,
                                 *stride)
         self.ref = ctypes.byref(self.args)
@@ -525,7 +532,7 @@ def _heads(t: torch.Tensor, n: int, n_heads: int, head_dim: int, dtype, what: st
         ok = t.shape == (n, n_heads * head_dim) and stride[1] == 1
     if not ok or t.dtype is not dtype or not t.is_cuda:
         raise ValueError("%s must be a %s device tensor [%d, %d, %d] with contiguous rows" % (what, dtype, n, n_heads, head_dim))
-    return stride[0] if n > 1 else max(stride[0], n_heads * head_dim)
+    return stride[0] if n > 1 else n_heads * head_dim
 
 
 def _int32_rows(t: torch.Tensor, n: int, what: str) -> int:

@@ -213,3 +213,34 @@ def test_attention_counts_lengths_where_no_own_keys_are_allowed(n_seq, prefix):
     attend = aweq.PrefixAttention(cache, prefix_pages, prefix, 16, n_seq, 1, max_own=0)
     assert counted(attend, q, pages, lens) == n_seq
     assert counted(attend, q, pages, torch.zeros_like(lens)) == 0
+
+
+# ---------------------------------------------------------------------------- rows without a pitch
+def test_one_row_has_no_pitch():
+    """A single row cut from a matrix of any width."""
+    i = linear_inputs(1, 64, 24, 2)
+    layer = aweq.LinearW8A8(i["w"], i["ws"], i["wz"], i["b"])
+    want = layer(i["x"], i["xs"], i["xz"])
+    wide = torch.zeros((3, 101), dtype=torch.uint8, device="cuda")
+    wide[:1, :64] = i["x"]
+    assert torch.equal(layer(wide[:1, :64], i["xs"], i["xz"]), want)
+    out = torch.empty_like(want)
+    aweq.aweq_linear_w8a8(wide[:1, :64], i["xs"], i["xz"], aweq.PER_ROW, i["w"], i["ws"], i["wz"], layer.w_sum, aweq.PER_ROW, i["b"], out)
+    assert torch.equal(out, want)
+    q, cache, prefix_pages, pages, lens = attention_case(1, 1, 4, 2, 64, 40, [20], 16, torch.float16)
+    attend = aweq.PrefixAttention(cache, prefix_pages, 40, 4, 1)
+    want = attend(q, pages, lens)
+    row, row_out = torch.zeros((2, 301), dtype=torch.float16, device="cuda"), torch.zeros((2, 259), dtype=torch.float16, device="cuda")
+    row[:1, :256] = q.flatten(1)
+    attend(row[:1, :256], pages, lens, row_out[:1, :256])
+    assert torch.equal(row_out[:1, :256], want.flatten(1))
+    # a pool of one page, of one token a page, of one head
+    buf = torch.randn((1 << 16,), generator=gen(3), device="cuda").to(torch.float16)
+    for shape, stride in [((1, 8, 2, 64), (1027, 128, 64, 1)), ((8, 1, 2, 64), (128, 3, 64, 1)), ((4, 8, 1, 64), (512, 64, 77, 1))]:
+        odd = aweq.KVCache(buf.as_strided(shape, stride), buf.as_strided(shape, stride, 4096))
+        even = aweq.KVCache(*(torch.empty(shape, dtype=torch.float16, device="cuda").copy_(t) for t in (odd.k, odd.v)))
+        qq = torch.randn((1, 2, 64), generator=gen(4), device="cuda").to(torch.float16)
+        table = torch.zeros((1, 8), dtype=torch.int32, device="cuda")
+        one = torch.ones(1, dtype=torch.int32, device="cuda")
+        outs = [aweq.PrefixAttention(c, None, 0, 2, 1)(qq, table, one) for c in (odd, even)]
+        assert torch.equal(*outs)
