@@ -549,7 +549,7 @@ def _int32_table(t: torch.Tensor, what: str):
     (rows, cols), (ld, one) = t.shape, t.stride()
     if cols > 1 and one != 1:
         raise ValueError("%s must have contiguous rows" % what)
-    return t.data_ptr(), rows, cols, max(ld, cols)
+    return t.data_ptr(), rows, cols, ld if rows > 1 else cols
 
 
 def aweq_kv_append(cache, page_table, k, v, pos, seq=None, first=0, table=None, interleaved=False, q=None, q_out=None,

@@ -244,3 +244,15 @@ def test_one_row_has_no_pitch():
         one = torch.ones(1, dtype=torch.int32, device="cuda")
         outs = [aweq.PrefixAttention(c, None, 0, 2, 1)(qq, table, one) for c in (odd, even)]
         assert torch.equal(*outs)
+
+
+def test_page_tables_of_overlapping_rows_are_refused():
+    """One row for all sequences by a stride of zero: a table has a row for each."""
+    q, cache, prefix_pages, pages, lens = attention_case(3, 1, 4, 2, 64, 0, [20, 20, 20], 16, torch.float16, stale=False)
+    for table in (pages[:1].expand(3, -1), pages.flatten().as_strided((3, 3), (1, 1))):
+        with pytest.raises(aweq.AweqError) as e:
+            aweq.PrefixAttention(cache, None, 0, 4, 3)(q, table, lens)
+        assert e.value.code == 3
+        with pytest.raises(aweq.AweqError) as e:
+            aweq.aweq_kv_append(cache, table, q[:, :2], q[:, :2], lens)
+        assert e.value.code == 3
