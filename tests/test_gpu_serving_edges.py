@@ -9,7 +9,8 @@ import torch
 
 from paper_2311_01305_b200 import aweq
 
-from .test_gpu_serving import (DTYPES, TINY, U16, attention_case, attention_reference, gen, linear_check, linear_inputs, make_cache)
+from .test_gpu_serving import (DTYPES, TINY, U16, attention_case, attention_check, attention_close, attention_reference, gen, linear_check,
+                               linear_inputs, make_cache)
 
 pytestmark = pytest.mark.gpu
 
@@ -256,3 +257,67 @@ def test_page_tables_of_overlapping_rows_are_refused():
         with pytest.raises(aweq.AweqError) as e:
             aweq.aweq_kv_append(cache, table, q[:, :2], q[:, :2], lens)
         assert e.value.code == 3
+
+
+# ---------------------------------------------------------------------------- launches that follow one another
+def test_attention_long_prefix_on_another_stream_and_in_a_graph():
+    """The kernel of the own keys starts before the prefix's has ended: lengths, queries and pages that change from call to call, and
+    calls that replay from a graph."""
+    q, cache, prefix_pages, pages, lens = attention_case(40, 2, 16, 16, 64, 4100, [20 + b for b in range(40)], 16, torch.float16, stale=False)
+    attend = aweq.PrefixAttention(cache, prefix_pages, 4100, 16, 40, 2)
+    want = attend(q, pages, lens)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = attend(q, pages, lens)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want)
+    out, graph = torch.zeros_like(want), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attend(q, pages, lens, out)
+    for step in range(5):
+        lens.sub_(3)
+        q.copy_(q.flip(0))
+        pages.copy_(pages.flip(0))
+        graph.replay()
+        assert torch.equal(out, attend(q, pages, lens))
+
+
+@pytest.mark.parametrize("n_seq,prefix", [(40, 4100), (20, 4100), (5, 100)])
+def test_append_and_attention_in_a_row(n_seq, prefix):
+    """Steps that are issued without waiting for one another give what the same steps give one by one: each reads the keys that
+    the call before it has just stored, and queries that have just been turned."""
+    h, d, page, steps = 16, 64, 16, 24
+    q, cache, prefix_pages, pages, lens = attention_case(n_seq, 1, h, h, d, prefix, [steps] * n_seq, page, torch.float16, stale=False)
+    table = aweq.aweq_rope_table(d, prefix + steps)
+    attend = aweq.PrefixAttention(cache, prefix_pages, prefix, h, n_seq)
+    g = gen(23)
+    tokens = torch.randn((steps, 3, n_seq, h, d), generator=g, device="cuda").to(torch.float16)
+    pos = [torch.full((n_seq,), prefix + t, dtype=torch.int32, device="cuda") for t in range(steps)]
+    own = [torch.full((n_seq,), t + 1, dtype=torch.int32, device="cuda") for t in range(steps)]
+    blank = cache.k.clone(), cache.v.clone()
+    turned, runs = torch.empty_like(q), []
+    for wait in (True, False):
+        cache.k.copy_(blank[0])
+        cache.v.copy_(blank[1])
+        outs = [torch.empty_like(q) for _ in range(steps)]
+        torch.cuda.synchronize()
+        for t in range(steps):
+            aweq.aweq_kv_append(cache, pages, tokens[t, 1], tokens[t, 2], pos[t], first=prefix, table=table, q=tokens[t, 0], q_out=turned)
+            if wait:
+                torch.cuda.synchronize()
+            attend(turned, pages, own[t], outs[t])
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        runs.append(torch.stack(outs))
+    assert torch.equal(*runs)
+    want, mag, reach = attention_reference(turned, cache, prefix_pages, prefix, pages, own[-1], 1, d ** -0.5)
+    attention_close(runs[1][-1], want, mag, reach, prefix + steps, d, torch.float16)
+
+
+@pytest.mark.parametrize("n_q", [128, 257, 500])
+@pytest.mark.parametrize("h,kv,prefix", [(4, 4, 0), (8, 2, 130), (16, 16, 4100)])
+def test_attention_of_prompts(n_q, h, kv, prefix):
+    """All of a prompt's tokens at once, with and without something before them."""
+    attention_check(2, n_q, h, kv, 64, prefix, [n_q, n_q + 19], 16, torch.float16)
