@@ -155,7 +155,8 @@ def _stream() -> int:
     return _raw_stream(_current_device())
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# (not a public name: a torch without it serves the slow way)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 _current_device = torch.cuda.current_device
 
 
@@ -200,6 +201,7 @@ def new_status(device="cuda") -> torch.Tensor:
 
 
 def read_status(st: torch.Tensor) -> dict:
+    """The three counters that the calibration calls write (``read_out_of_range`` has the fourth)."""
     v = st.cpu().tolist()
     return {"nonfinite": v[0], "zero_range": v[1], "wait_timeout": v[2]}
 
@@ -555,7 +557,8 @@ def _int32_table(t: torch.Tensor, what: str):
 def aweq_kv_append(cache, page_table, k, v, pos, seq=None, first=0, table=None, interleaved=False, q=None, q_out=None,
                    st=None):
     """Store keys and values of new tokens in their pages, keys (and ``q`` into ``q_out``) turned by
-    their positions on the way (argument marshalling only; see ``include/aweq.h``)."""
+    their positions on the way (argument marshalling only; see ``include/aweq.h``).  Without ``q_out`` the
+    queries are turned in place.  Returns where they are."""
     d, kv, dt, n = cache.head_dim, cache.n_kv_heads, cache.dtype, k.shape[0]
     ldk, ldv = _heads(k, n, kv, d, dt, "k"), _heads(v, n, kv, d, dt, "v")
     pages, n_seq, per_seq, ld_table = _int32_table(page_table, "page_table")
