@@ -475,7 +475,8 @@ typedef struct {
  * projection, say).  rope: the table of aweq_rope_table (n_pos rows) or NULL for no rotation; the first
  * rotary_dim of every key head are turned by position pos[t], pairs (i, i + rotary_dim / 2) or, when
  * interleaved != 0, (2i, 2i + 1); binary32, rounded once.  q: optional [n_tokens x n_heads * head_dim],
- * turned the same way into q_out (which may be q).  Two tokens for the same place: either stays.
+ * turned the same way into q_out (which may be q).  Two tokens for the same place: each element of it is
+ * one's or the other's.
  * A sequence, page or c outside the table or the pool, or (with rope) a position outside the
  * table: the token is not stored, its q_out (position outside the table) becomes zero, and
  * st->out_of_range counts the token.  k, v, q, q_out: 2-byte aligned, any pitch >= the row; 16-byte
@@ -492,8 +493,8 @@ aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, lo
  *   out[b n_q + i, h] = sum_j p_j v_j,  p = softmax_j(scale q . k_j)
  * over all prefix keys and the own keys j < own_len[b] - (n_q - 1 - i); head h reads key head
  * h / (n_heads / n_kv_heads).  A row without keys gives zeros, one whose
- * scores are all minus infinity NaN.  The prefix is read once for all rows
- * of the batch.  Scores, running maximum, sum and output are binary32; the probabilities are
+ * scores are all minus infinity NaN.  The prefix is read once for every 16, 32, 64 or 128 of the rows (tokens and
+ * heads of the whole batch) that share a key head.  Scores, running maximum, sum and output are binary32; the probabilities are
  * rounded to the 16-bit type for the product with v (fp16: to 2^-32 of a row's largest at worst, however
  * small they are); one rounding at the end.
  * q, out: 16-bit [n_seq * n_q x n_heads * head_dim], row pitches ldq, ldo elements, 16-byte aligned,

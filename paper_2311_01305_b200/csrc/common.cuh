@@ -290,12 +290,12 @@ __device__ __forceinline__ void named_bar_sync(int id, int threads)
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
-// barrier over `threads` threads that also ANDs a predicate (all arrive, all get the same answer)
 // Arrives without waiting: for a warp that gives up where others will come to the barrier.
 __device__ __forceinline__ void named_bar_arrive(int id, int threads)
 {
     asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
+// barrier over `threads` threads that also ANDs a predicate (all arrive, all get the same answer)
 __device__ __forceinline__ bool named_bar_and(int id, int threads, bool pred)
 {
     uint32_t r;

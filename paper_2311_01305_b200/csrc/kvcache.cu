@@ -109,7 +109,7 @@ kv_append_kernel(const KvAppendArgs a, int segments)
     if (sub >= per) return;
     const int rd = a.rd;
     // the lane's two pieces, in elements of the head
-    const bool turn0 = INTER ? u * 16 < rd : u * 16 < rd, turn1 = INTER ? u * 16 + 8 < rd : turn0;
+    const bool turn0 = u * 16 < rd, turn1 = INTER ? u * 16 + 8 < rd : turn0;
     const int e0 = !INTER && turn0 ? u * 8 : u * 16, e1 = !INTER && turn0 ? u * 8 + rd / 2 : u * 16 + 8;
     float co[8], si[8];
     if (turn0 && place.turn_ok) {
