@@ -309,7 +309,6 @@ __device__ __forceinline__ void attention_boxes(const AttentionArgs &a, const At
             const int keys = now.len - now.tile * kAtTile - lane * box;
             const bool has = lane < boxes && keys > 0, bad = bad_page(a, page);
             const int n = __popc(__ballot_sync(0xffffffffu, has));
-            if (has && bad) count_bad_page(a, now.kh, now.rt, now.tile * kAtTile + lane * box);
             if (lane == 0) {
                 ring.unit[s] = now;
                 mbar_arrive_expect_tx(&ring.landed[s], (uint32_t)(n * box * 256 * HALVES));
@@ -318,6 +317,7 @@ __device__ __forceinline__ void attention_boxes(const AttentionArgs &a, const At
             if (has) {
                 const uint32_t dst = smem_u32(smem) + s * STAGE + lane * box * 128, bar = smem_u32(&ring.landed[s]);
                 const int row = (now.tile * kAtTile + lane * box) % (unsigned)a.page_size, pid = bad ? 0 : page;
+                if (bad) count_bad_page(a, now.kh, now.rt, row);
 #pragma unroll
                 for (int h = 0; h < HALVES; ++h) {
                     tma_load4(dst + h * (kAtTile * 128), &mapK, h * 64, now.kh, row, pid, bar);
@@ -380,12 +380,10 @@ __device__ __forceinline__ void attention_part(const AttentionArgs &a, const Att
             const int pg = bad ? 0 : page;
             w.advance(a, p);
             if (left > 1) page = w.entry(a, p, mine);           // the next unit's page, while this one's stage empties
-            if (has && bad && lane < 16) count_bad_page(a, now.kh, now.rt, now.tile * kAtTile + mine);
+            const unsigned row = (unsigned)(now.tile * kAtTile + mine) % (unsigned)a.page_size;
+            if (has && bad && lane < 16) count_bad_page(a, now.kh, now.rt, row);
             // element offset of the row, -1: no such key
-            const long long off = !has ? -1
-                                           : (long long)pg * a.page_stride +
-                                                 (long long)((unsigned)(now.tile * kAtTile + mine) % (unsigned)a.page_size) * a.token_stride +
-                                                 now.kh * a.head_stride;
+            const long long off = !has ? -1 : (long long)pg * a.page_stride + (long long)row * a.token_stride + now.kh * a.head_stride;
             ok = mbar_wait(&empty[s], ph ^ 1);
             if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
             if (cw == 0 && lane == 0) {
@@ -648,9 +646,6 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
 {
     __shared__ float part[4][128], part_l[4];
     pdl_begin();
-    // without own keys no other kernel looks at the lengths
-    if (!p.ctas && blockIdx.x == 0)
-        for (int b = threadIdx.x; b < (int)a.n_seq; b += 128) clamp_length(a, __ldg(a.own_len + b), true);
     const int lane = threadIdx.x & 31, warp = (int)(threadIdx.x >> 5) % WARPS, G = a.n_heads / a.n_kv, hd = a.head_dim;
     const unsigned r = blockIdx.x * (4 / WARPS) + (threadIdx.x >> 5) / WARPS;
     if (WARPS == 1 && r >= p.rows) return;
@@ -745,6 +740,9 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
         *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.ldo + (long long)h * hd + lane * 4) =
             make_uint2(D::encode2(o.x * inv, o.y * inv), D::encode2(o.z * inv, o.w * inv));
     }
+    // without own keys no other kernel looks at the lengths
+    if (!p.ctas && blockIdx.x == 0 && threadIdx.x < 32)
+        for (int i = lane; i < (int)a.n_seq; i += 32) clamp_length(a, __ldg(a.own_len + i), true);
 }
 
 // Keys of a tiled copy: a box lies in one page, on a row of the stage that keeps the swizzle's phase (a multiple of eight).

@@ -139,10 +139,11 @@ __device__ __forceinline__ long long own_units(const AttentionArgs &a, const Att
 }
 
 __device__ __forceinline__ bool bad_page(const AttentionArgs &a, int page) { return page < 0 || page >= a.n_pages; }
-// A bad entry of a page list counts once: where its first key is met by the first row tile of the first key head.
-__device__ __forceinline__ void count_bad_page(const AttentionArgs &a, int kh, int rt, int key)
+// A bad entry of a page list counts once: where its first key (row 0 of the page) is met by the first row tile of the first key
+// head.  (The row is at hand: another division there cost 1 us at 32 x (2048 + 300) keys.)
+__device__ __forceinline__ void count_bad_page(const AttentionArgs &a, int kh, int rt, unsigned row)
 {
-    if (a.st && kh == 0 && rt == 0 && (unsigned)key % (unsigned)a.page_size == 0) atomicAdd(&a.st->out_of_range, 1ull);
+    if (((unsigned)(kh | rt) | row) == 0 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
 }
 
 // A warp finds the first unit of CTA `cta` of `ctas` (every lane gets the same) and the number of its units.

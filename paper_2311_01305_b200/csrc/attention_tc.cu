@@ -129,7 +129,6 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                     if (++rt == p.pre_rt) { rt = 0; ++kh; }
                 }
                 if (left > 1) page = look_up(tile);                         // the next unit's, while this stage empties
-                if (lead && there && bad) count_bad_page(a, u.kh, u.rt, u.tile * p.pre_unit + lane * p.box);
                 ok = mbar_wait(&sh.empty[s], ph ^ 1);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 const int n = __popc(__ballot_sync(0xffffffffu, there));
@@ -141,6 +140,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                 if (there) {
                     const uint32_t dst = smem_u32(stages + s * stage_bytes + (lead ? 0 : v_at)) + lane * p.box * 128, bar = smem_u32(&sh.full[s]);
                     const int row = (unsigned)(u.tile * p.pre_unit + lane * p.box) % (unsigned)a.page_size;
+                    if (lead && bad) count_bad_page(a, u.kh, u.rt, row);
                     for (int h = 0; h < halves; ++h) tma_load4(dst + h * 16384, map, h * 64, u.kh, row, pid, bar);
                 }
                 fresh = u.leave;
