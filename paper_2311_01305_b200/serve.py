@@ -108,7 +108,7 @@ class AttentionBlock:
         return out
 
 
-def main(n_seq: int = 16, prefix: int = 500, steps: int = 8) -> None:
+def main(n_seq: int = 16, prefix: int = 500, steps: int = 8) -> float:
     from torch.nn.functional import linear
     wl = synth.workloads(1.0 / 128)["opt125m_model_w8a8"]
     X, W = synth.generate(wl, "cuda")
@@ -154,6 +154,7 @@ def main(n_seq: int = 16, prefix: int = 500, steps: int = 8) -> None:
         worst = max(worst, ((got - y).norm() / y.norm()).item())
     print("%d sequences after a prefix of %d tokens, %d steps: at most %.3f off the 16-bit layer (2-norm), %.0f us a step" % (
         n_seq, prefix, steps, worst, begin.elapsed_time(end) * 1e3 / (steps - 1)))
+    return worst
 
 
 if __name__ == "__main__":
