@@ -203,7 +203,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
         const int q4 = warp & 3, half = (warp - 4) >> 2, r = q4 * 32 + lane, st = tid - 128;
         const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
         // a negative scale turned q's signs; a zero one must leave -inf where a key is not seen
-        const float scale = fmaxf(fabsf(a.scale), 1.17549435e-38f) * 1.4426950408889634f;
+        const float scale = (a.scale == 0.0f ? 1.17549435e-38f : fabsf(a.scale)) * 1.4426950408889634f;
         // of the row: reference maximum, what moves it, what the exponents are relative to, sum; whether a row of the warp is far
         float m = -CUDART_INF_F, limit = m, base = 0.0f, l = 0.0f;
         bool far = false;

@@ -179,6 +179,14 @@ def test_linear_sums_that_cancel_behind_large_zero_points(n, side):
     assert torch.equal(out, i["b"].to(torch.float16).expand_as(out))
 
 
+@pytest.mark.parametrize("n_seq,heads,prefix", [(3, 4, 70), (40, 16, 4100)])
+def test_attention_with_a_scale_that_is_no_number(n_seq, heads, prefix):
+    q, cache, prefix_pages, pages, lens = attention_case(n_seq, 1, heads, heads, 64, prefix, [5] * n_seq, 16, torch.float16)
+    assert torch.isnan(aweq.PrefixAttention(cache, prefix_pages, prefix, heads, n_seq, scale=math.nan)(q, pages, lens)).all()
+    lens.zero_()                                                   # by the prefix alone
+    assert torch.isnan(aweq.PrefixAttention(cache, prefix_pages, prefix, heads, n_seq, scale=math.nan)(q, pages, lens)).all()
+
+
 # ---------------------------------------------------------------------------- counts
 def counted(attend, q, pages, lens):
     st = aweq.new_status()
