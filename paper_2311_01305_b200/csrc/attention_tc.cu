@@ -8,8 +8,8 @@
 // Each row's reference maximum m moves only when a new maximum exceeds it by more than 8 (a factor of 256, for which
 // the 16-bit P and the binary32 sums have room), so O is hardly ever rescaled: only then do the softmax threads
 // wait for the product under way, scale O and go on.
-// What bounds it: the exponentials, 128 x 128 of a unit in some 1450 of its 2900 cycles, and the hand-over of S and P (384 rows x 32779
-// keys x 8 heads of 128: 66 us, 0.78 PFLOP/s).
+// What bounds it: one unit's chain of load, maximum, meeting, exponentials and store, 2900 cycles, in which neither the exponentials'
+// pipe (1060 cycles) nor the tensor pipe (35 %) is full (384 rows x 32779 keys x 8 heads of 128: 76 us by itself, 0.68 PFLOP/s).
 // Warps: 0 and 2 look up pages and issue the copies of K and V, 1 issues the products (S of a unit before O of the one
 // before it), 4-11 softmax (two threads to a row, half of the keys each), 12-15 bring the next item's rows of Q and take
 // the finished item's O to its record.
@@ -311,7 +311,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                 };
                 if (!far)
                     weigh(scale);
-                else {                      // (code of its own: the test costs 384 rows x 32779 keys 2 us; one loop for both, 4)
+                else {                      // (code of its own: its being there costs 384 rows x 32779 keys 3 us of 76; one loop for both, 5, a call, 6)
                     const float first = tc_far(m) ? scale : 1.0f;
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
