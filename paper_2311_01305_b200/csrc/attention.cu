@@ -15,7 +15,7 @@
 // prefix come as tiled copies of one warp; own keys, whose pages, lengths and rows of q change from item to item, as
 // 16-byte copies, 16 rows of a unit to a warp (96 sequences of 350 own keys: 43.5 us against 46 with tiled copies; 32 rows x
 // 2048 shared keys and 4800 own ones: 41.9 against 45 with 16-byte copies throughout; a bulk copy per row: 40 cycles each).
-// What bounds it: memory where the keys are many (16 sequences of 1-4 thousand own keys, 32 heads of 128: 111 us, 6.05 TB/s, 94 % of
+// What bounds it (times on the device, replayed from a graph): memory where the keys are many (16 sequences of 1-4 thousand own keys, 32 heads of 128: 111 us, 6.05 TB/s, 94 % of
 // a copy's rate), the changes from item to item where they are few (128 sequences of 64-256 keys: 78 us, 4.3 TB/s), and
 // the start: the code itself comes from memory, 1 us a stretch, which is why the copying loop has one place for each step
 // and the computing warps run through theirs once before the first keys are there.
@@ -639,7 +639,7 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, const __gri
 
 // WARPS warps per row (token, head), each with eight records' outputs under way.  A row has a handful of records in the usual
 // case and some hundreds when one key head's keys are spread over the whole device; then there are few rows.  Bound by latency: lengths and
-// cut, then (m, l) and the outputs, which fly together (1024 rows 5 us).
+// cut, then (m, l) and the outputs, which fly together (1024 rows 5-6 us; 8 by itself, its start included, which nothing hides).
 template <class D, int WARPS>
 __global__ void __launch_bounds__(128)
 attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsigned char *__restrict__ ws)

@@ -92,7 +92,8 @@ __device__ __forceinline__ bool append_head(const KvAppendArgs &a, const AppendP
 // takes one token and a run of its heads, a lane the same two 16-byte pieces of every head it gets (the two
 // halves of eight pairs, or 16 neighbouring elements when interleaved), so cos and sin are read once per
 // token and stay in registers, and four heads' loads are issued before the first is used.  Measured: 26624 tokens of 40 + 2 x 8 heads of
-// 128, 138 us, 5.64 TB/s (a copy: 6.46); 64 tokens 3.7 us, three dependent loads (sequence, page, row) after the start.
+// 128, 138 us, 5.64 TB/s (a copy: 6.46); 64 tokens 3.8 us on the device (a call of the binding 10.5), three dependent loads (position and
+// sequence, page, row) after the start, of which only the stores need the first two.
 template <class D, bool INTER>
 __global__ void __launch_bounds__(256)
 kv_append_kernel(const KvAppendArgs a, int segments)

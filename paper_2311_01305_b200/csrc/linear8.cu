@@ -44,7 +44,7 @@ __device__ __forceinline__ void mma_u8(uint32_t (&c)[4], uint32_t a0, uint32_t a
 // same under any order of k that both operands share, so a lane loads 16 consecutive bytes of its
 // two rows (lane % 4 picks the quarter of the segment) straight into the registers of two instructions
 // and the same bytes of its token: no shared memory, no barrier until the warps' sums are added.  Bound by the start of a launch and the
-// latency of the loads (1 x 768 x 768: 2.3 us), then by memory (1 x 4096 x 4096: 6.8 us).
+// latency of the loads (1 x 768 x 768: 2.4 us on the device, a call of the binding 7.6), then by memory (1 x 4096 x 4096: 6.8 us).
 template <int NT, class D>
 __global__ void __launch_bounds__(256) linear8_stream_kernel(const Linear8Args p)
 {

@@ -44,8 +44,9 @@ __device__ __forceinline__ Linear8Col linear8_col(const Linear8Args &p, long lon
 // ------------------------------------------------------------------ many tokens
 // Output tiles of 256 tokens x 248 channels, each by a pair of CTAs (cta_group::2): a CTA stages its 128 tokens and half of
 // the weights, and holds the sums of its tokens in TMEM, twice, so that the epilogue of one tile runs under the
-// products of the next.  Persistent: a pair takes every (pairs)-th tile.  Bound by the tensor pipe: 2048 x 4096 x 11008 62.5 us (2953
-// TOP/s), 16384 x 5120 x 13824 711 us (3261 TOP/s); what the first loses is its last wave.  Warps: 0 copies, 1 issues the products (in the
+// products of the next.  Persistent: a pair takes every (pairs)-th tile.  Bound by the tensor pipe: 2048 x 4096 x 11008 63.5 us (2909
+// TOP/s, the pipe busy 83 % of the time; calls in a row 75, at the power cap), 16384 x 5120 x 13824 711 us (3261 TOP/s); what the first
+// loses is its last wave.  Warps: 0 copies, 1 issues the products (in the
 // pair's even CTA), 4-11 write the output, two to a quarter of the TMEM lanes.
 //
 // The tokens' code sums rx come out of the same products: the last eight of the 256 rows of the weight tile are ones, laid
@@ -281,7 +282,7 @@ static aweq_status run_linear8_big(const Linear8Args &a, aweq_dtype dt, cudaStre
 // rows.  A stage holds the tokens there are (rounded up to 8), not 128, so that few tokens leave the ring to the
 // weights; the product reads 128 rows all the same, those past the box belong to the weights behind them and
 // give sums that nobody reads.  Warps: 0 copies, 1 issues the products, 2-7 add up the tokens' codes.  The sums go
-// through shared memory (the stages) once so that the output is written along the channels.  Measured: 16 x 4096 x 12288 12.3 us;
+// through shared memory (the stages) once so that the output is written along the channels.  Measured on the device: 16 x 4096 x 12288 12.5 us;
 // 16 x 9216 x 36864 56 us, 6.1 TB/s; 64 x 4096 x 4096 10.9 us (its start and its end).
 constexpr int kSplitRing = 200 * 1024, kSplitMaxStages = 16;
 struct SplitPlan {
