@@ -37,8 +37,9 @@ __device__ __forceinline__ float exp2_fast(float x)
 // those down to 2^-14 and nothing below 2^-25, and a million keys beside one large one may all lie there.  So fp16 ones
 // are held 2^7 times as large; below 2^-21 of 2^m they are off by at most 2^-32 of it each.  (In binary32 m - 7 is m - 8 at
 // the lowest, wherever m lies.)
+constexpr float kProbabilityShift = 7.0f;
 template <class D>
-__device__ __forceinline__ float probability_base(float m) { return D::kBf16 ? m : m - 7.0f; }
+__device__ __forceinline__ float probability_base(float m) { return D::kBf16 ? m : m - kProbabilityShift; }
 // An own length, clamped.  `count`: the one caller that reports it.
 __device__ __forceinline__ int clamp_length(const AttentionArgs &a, int len, bool count)
 {

@@ -3,13 +3,13 @@
 //
 // An item is up to 128 rows (TMEM lanes) against the prefix, 128 keys (or the whole pages that fit) to a unit:
 //   S = Q K^T   A = Q in TMEM, B = the staged keys            -> S in TMEM (two buffers)
-//   P = 2^(S scale - base(m))  by two threads per row, 16-bit, in TMEM over the S it came from
+//   P = 2^((S - m) scale)  by two threads per row, 16-bit, in TMEM over the S it came from
 //   O += P V    A = P in TMEM, B = the staged values (N contiguous)  -> O in TMEM
 // Each row's reference maximum m moves only when a new maximum exceeds it by more than 8 (a factor of 256, for which
 // the 16-bit P and the binary32 sums have room), so O is hardly ever rescaled: only then do the softmax threads
 // wait for the product under way, scale O and go on.
-// What bounds it: one unit's chain of load, maximum, meeting, exponentials and store, 2900 cycles, in which neither the exponentials'
-// pipe (1060 cycles) nor the tensor pipe (35 %) is full (384 rows x 32779 keys x 8 heads of 128: 76 us by itself, 0.68 PFLOP/s).
+// What bounds it: one unit's chain of load, maximum, meeting, exponentials and store, 2800 cycles, in which neither the exponentials'
+// pipe (1060 cycles) nor the tensor pipe (37 %) is full (384 rows x 32779 keys x 8 heads of 128: 73 us by itself, 0.71 PFLOP/s).
 // Warps: 0 and 2 look up pages and issue the copies of K and V, 1 issues the products (S of a unit before O of the one
 // before it), 4-11 softmax (two threads to a row, half of the keys each), 12-15 bring the next item's rows of Q and take
 // the finished item's O to its record.
@@ -21,13 +21,6 @@ namespace aweq {
 constexpr int kTcThreads = 512, kTcStageBytes = 192 * 1024, kTcMaxStages = 6;
 constexpr uint32_t kTcO = 256, kTcQ = 384;      // TMEM columns: S at 0 and 128, O, two of Q (64 columns each)
 constexpr float kTcSlack = 8.0f;
-// Where a reference is so large that binary32 keeps less than an eighth behind the point, neither the slack nor fp16's head room
-// (2^8 and 2^7 of fp16's 2^16) can be told from rounding: the reference is the maximum itself there, the base is the reference,
-// and scores are scaled, and rounded, before it is taken off, as the maximum was.
-__device__ __forceinline__ bool tc_far(float m) { return fabsf(m) > 1048576.0f && m != -CUDART_INF_F; }
-template <class D>
-__device__ __forceinline__ float tc_base(float m) { return tc_far(m) ? m : probability_base<D>(m); }
-__device__ __forceinline__ float tc_limit(float m) { return tc_far(m) ? m : m + kTcSlack; }
 
 // A unit: the tile'th tile of the prefix for row tile rt of key head kh.
 struct alignas(16) TcUnit {
@@ -204,9 +197,11 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
         const uint32_t lanes = (uint32_t)(q4 * 32) << 16;
         // a negative scale turned q's signs; a zero one must leave -inf where a key is not seen
         const float scale = (a.scale == 0.0f ? 1.17549435e-38f : fabsf(a.scale)) * 1.4426950408889634f;
-        // of the row: reference maximum, what moves it, what the exponents are relative to, sum; whether a row of the warp is far
-        float m = -CUDART_INF_F, limit = m, base = 0.0f, l = 0.0f;
-        bool far = false;
+        // The row's reference is a score before scaling: the difference to it is taken first and scaled then, which is as good as the
+        // scores are, however large.  (One step, the rounded scaled maximum taken off an unrounded product, gives infinity or zero
+        // from 2^28 on.  Two steps on pairs of scores cost 384 rows x 32779 keys 1 us, on single ones 2.5.)
+        constexpr float kShift = D::kBf16 ? 0.0f : kProbabilityShift;
+        float m = -CUDART_INF_F, l = 0.0f;
         int s = 0, u = 0, nrows = 0;
         uint32_t ph = 0;
         long long rec = 0;
@@ -265,22 +260,16 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                 float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 sh.top[u & 1][half][r] = t;
                 if (!(ok = meet())) break;
-                t = fmaxf(t, sh.top[u & 1][half ^ 1][r]) * scale;
-                auto refer = [&](float to) {
-                    m = to;
-                    limit = tc_limit(m);
-                    base = m == -CUDART_INF_F ? 0.0f : tc_base<D>(m);
-                    far = __any_sync(0xffffffffu, tc_far(m));
-                };
-                if (it.fresh) refer(t);
-                else if (__any_sync(0xffffffffu, t > limit)) {
+                t = fmaxf(t, sh.top[u & 1][half ^ 1][r]);
+                const bool above = (t - m) * scale > kTcSlack;
+                if (it.fresh) m = t;
+                else if (__any_sync(0xffffffffu, above)) {
                     // a maximum well above the reference: O (half of it here) and l move to it
                     ok = mbar_wait(&sh.pv_done[(u - 1) & 1], ((u - 1) >> 1) & 1);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                     tc_fence_after();
-                    const float to = t > limit ? t : m, move = tc_base<D>(m) - tc_base<D>(to);
-                    const float f = to == -CUDART_INF_F ? 1.0f : exp2_fast(move);
-                    refer(to);
+                    const float to = above ? t : m, f = to == -CUDART_INF_F ? 1.0f : exp2_fast((m - to) * scale);
+                    m = to;
                     l *= f;
 #pragma unroll 1
                     for (int c = half * 64; c < min(hd, half * 64 + 64); c += 32) {
@@ -293,32 +282,22 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                     }
                     tc_wait_st();
                 }
-                auto weigh = [&](float times) {
-                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const float from = m == -CUDART_INF_F ? 0.0f : m;
+                const float2 from2 = make_float2(-from, -from), scale2 = make_float2(scale, scale), shift2 = make_float2(kShift, kShift);
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            const float e = exp2_fast(__fmaf_rn(__uint_as_float(x[c][j]), times, -base));
-                            const float f = exp2_fast(__fmaf_rn(__uint_as_float(x[c][j + 1]), times, -base));
-                            sum[j & 2] += e;
-                            sum[(j & 2) + 1] += f;
-                            // rounded to the 16-bit type for the product with v; the sum takes the unrounded ones (see probability_base)
-                            x[0][c * 16 + j / 2] = D::encode2(e, f);
-                        }
-                    tc_st32(at + half * 32, x[0]);
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                };
-                if (!far)
-                    weigh(scale);
-                else {                      // (code of its own: its being there costs 384 rows x 32779 keys 3 us of 76; one loop for both, 5, a call, 6)
-                    const float first = tc_far(m) ? scale : 1.0f;
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) x[c][j] = __float_as_uint(__fmul_rn(__uint_as_float(x[c][j]), first));
-                    weigh(tc_far(m) ? 1.0f : scale);
-                }
+                    for (int j = 0; j < 32; j += 2) {
+                        const float2 d = __ffma2_rn(__fadd2_rn(make_float2(__uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1])), from2), scale2, shift2);
+                        const float e = exp2_fast(d.x), f = exp2_fast(d.y);
+                        sum[j & 2] += e;
+                        sum[(j & 2) + 1] += f;
+                        // rounded to the 16-bit type for the product with v; the sum takes the unrounded ones (see probability_base)
+                        x[0][c * 16 + j / 2] = D::encode2(e, f);
+                    }
+                tc_st32(at + half * 32, x[0]);
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 tc_wait_st();
             }
             tc_fence_before();
@@ -329,7 +308,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
                     if (half) sh.sum[r] = l;
                     if (!(ok = meet())) break;
                     if (!half && r < nrows)
-                        reinterpret_cast<float2 *>(ws + p.off_pre_ml)[rec + r] = make_float2(tc_base<D>(m), l + sh.sum[r]);
+                        reinterpret_cast<float2 *>(ws + p.off_pre_ml)[rec + r] = make_float2(__fmul_rn(m, scale) - kShift, l + sh.sum[r]);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.item_done[it.item & 3]);
