@@ -32,7 +32,7 @@ class _Scratch:
 
     def __init__(self, block: "AttentionBlock", rows: int):
         dev, self.rows, self.n = block.cache.k.device, rows, -1
-        u8 = lambda c: (torch.empty((rows, c), dtype=torch.uint8, device=dev), torch.empty(rows, device=dev),  # noqa: E731
+        u8 = lambda c: (torch.empty((rows, c), dtype=torch.uint8, device=dev), torch.empty(rows, dtype=torch.float32, device=dev),  # noqa: E731
                         torch.empty(rows, dtype=torch.int32, device=dev))
         self.x, self.o = u8(block.qkv.C_in), u8(block.o.C_in)
         h, kv, d = block.n_heads, block.n_kv, block.head_dim

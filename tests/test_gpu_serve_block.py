@@ -117,3 +117,17 @@ def test_block_in_graphs_that_replay_side_by_side():
                 graphs[w].replay()
     torch.cuda.synchronize()
     assert all(torch.equal(o, t) for o, t in zip(outs, want))
+
+
+def test_block_under_another_default_type():
+    """A program that sets torch's default type to a 16-bit one: Steps are binary32 all the same."""
+    cal, x = calibrated()
+    block = serve.AttentionBlock(cal, 12, 4)
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2)
+    want = chunk(block, x[:10].contiguous(), 2, 5, 32, table)()
+    torch.set_default_dtype(torch.bfloat16)
+    try:
+        got = chunk(serve.AttentionBlock(cal, 12, 4), x[:10].contiguous(), 2, 5, 32, table)()
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert torch.equal(got, want)
