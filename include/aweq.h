@@ -437,6 +437,44 @@ aweq_status aweq_linear_w8a8(const unsigned char *Xq, long long ldx, const float
                              long long C_in, long long C_out, void *out, aweq_dtype dt, long long ldo,
                              aweq_dev_status *st, void *stream);
 
+/* Microscaled 4-bit floating point: elements e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), a scale for every
+ * block of a row's columns.  With v[n,j] = X[n,j] scale[j] (binary32; scale NULL: X itself; 1/s for activations, s for weights),
+ * top its largest magnitude in the block, and rn(.) rounding to the nearest value of a type, ties to the even code:
+ *   AWEQ_MX4_E8M0  blocks of 32, step = 2^e, e = clamp(floor(log2 top) - 2, -127, 127); the scale byte is e + 127
+ *   AWEQ_MX4_E4M3  blocks of 16, row_step = (largest of the row) (1 / 2688), the scale is b = rn_e4m3(top / (6 row_step)),
+ *                  step = b row_step (a block whose step is below 2^-126 becomes zeros)
+ *   element = rn_e2m1(v (1 / step)), saturating at 6; it stands for element * step.
+ * A block (E8M0) or row (E4M3) with an infinity or a NaN stands for NaN throughout; st->nonfinite counts it.
+ * X: 16-bit [rows x cols], row pitch ld; cols a multiple of 32, at most AWEQ_LINEAR_MAX_C_IN.
+ * codes: [rows x cols / 2], two elements to a byte, the even column in the low half, contiguous, 16-byte aligned.
+ * scales: aweq_mx4_scale_bytes(rows, cols, fmt) bytes, 16-byte aligned, in tiles of 128 rows x 4 blocks: the scale of block k of
+ * row r is byte 16 (r % 32) + 4 (r % 128 / 32) + k % 4 of tile (r / 128) G + k / 4, G = the tiles of whole groups of 256
+ * columns (2 to a group for E8M0, 4 for E4M3).  Bytes of rows that there are not are left as they were.
+ * row_step: float[rows] (E4M3; not read for E8M0).
+ * mu, epsmu: both or neither; epsmu[n] = sum_j (element step - v)[n,j] mu[j], the row sums of the bias correction (Eq. 15),
+ * in binary32. */
+typedef enum { AWEQ_MX4_E8M0 = 0, AWEQ_MX4_E4M3 = 1 } aweq_mx4_format;
+size_t aweq_mx4_scale_bytes(long long rows, long long cols, aweq_mx4_format fmt);
+aweq_status aweq_quant_mx4(const void *X, aweq_dtype dt, long long rows, long long cols, long long ld, const float *scale,
+                           aweq_mx4_format fmt, unsigned char *codes, unsigned char *scales, float *row_step,
+                           const float *mu, float *epsmu, aweq_dev_status *st, void *stream);
+/* What codes and scales stand for, out[n,j] = round16(element scale row_step): 16-bit [rows x cols], row pitch ldo (a
+ * multiple of 8), 16-byte aligned. */
+aweq_status aweq_dequant_mx4(const unsigned char *codes, const unsigned char *scales, const float *row_step,
+                             aweq_mx4_format fmt, long long rows, long long cols, void *out, aweq_dtype dt, long long ldo,
+                             void *stream);
+/* The layer on such codes:
+ *   out[n,o] = round16( x_step[n] w_step[o] sum_blocks bx bw sum_block ex ew + bias[o] )
+ * with products and sums in binary32 on the tensor cores (in an order of their own), steps (E4M3 only) and bias in binary32 and one rounding.
+ * Xq [N x C_in] and Wq [C_out x C_in] as aweq_quant_mx4 wrote them, of one format; bias: float[C_out] or NULL.
+ * out: 16-bit [N x C_out], row pitch ldo elements, 2-byte aligned (16-byte aligned rows are written with wider stores).
+ * C_in: a multiple of 32, at most AWEQ_LINEAR_MAX_C_IN; C_out: any, at most 2^30; N: 0 (nothing is done) to 2^31 - 1; neither
+ * matrix has more than 2^31 - 1 tiles of scales.  No scratch. */
+aweq_status aweq_linear_mx4(const unsigned char *Xq, const unsigned char *x_scales, const float *x_step,
+                            const unsigned char *Wq, const unsigned char *w_scales, const float *w_step,
+                            aweq_mx4_format fmt, const float *bias, long long N, long long C_in, long long C_out, void *out,
+                            aweq_dtype dt, long long ldo, aweq_dev_status *st, void *stream);
+
 /* Rotary positions.  Pair i of a head (i < rotary_dim / 2) is turned by the angle p f_i at position
  * p, f_i = theta^(-2i / rotary_dim), changed for contexts beyond the trained one:
  *   AWEQ_ROPE_LINEAR  f_i / factor

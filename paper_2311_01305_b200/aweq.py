@@ -32,6 +32,7 @@ FLAG_NO_EQUALIZE, FLAG_NO_BIAS_CORRECT = 1, 2
 FLAG_PHASE_REDUCE, FLAG_PHASE_QUANT, FLAG_PHASE_ACT = 4, 8, 16
 FLAG_ABSMAX_CRITERION = 32
 FLAG_MERGED_STATS = 64
+MX4_FORMATS = {"e8m0": 0, "e4m3": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
 
 _vp, _ll, _i, _sz = ctypes.c_void_p, ctypes.c_longlong, ctypes.c_int, ctypes.c_size_t
@@ -113,6 +114,14 @@ _lib.aweq_code_sums.restype = _i
 _lib.aweq_linear_w8a8.argtypes = [_vp, _ll, _vp, _vp, _i, _vp, _ll, _vp, _vp, _vp, _i, _vp, _ll, _ll, _ll, _vp, _i, _ll, _vp,
                                   _vp]
 _lib.aweq_linear_w8a8.restype = _i
+_lib.aweq_mx4_scale_bytes.argtypes = [_ll, _ll, _i]
+_lib.aweq_mx4_scale_bytes.restype = _sz
+_lib.aweq_quant_mx4.argtypes = [_vp, _i, _ll, _ll, _ll, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.aweq_quant_mx4.restype = _i
+_lib.aweq_dequant_mx4.argtypes = [_vp, _vp, _vp, _i, _ll, _ll, _vp, _i, _ll, _vp]
+_lib.aweq_dequant_mx4.restype = _i
+_lib.aweq_linear_mx4.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _ll, _ll, _ll, _vp, _i, _ll, _vp, _vp]
+_lib.aweq_linear_mx4.restype = _i
 _lib.aweq_rope_table.argtypes = [ctypes.POINTER(RopeSpec), _ll, _vp, _vp]
 _lib.aweq_rope_table.restype = _i
 _lib.aweq_kv_append.argtypes = [ctypes.POINTER(KvCacheArgs), _vp, _ll, _ll, _ll, _vp, _ll, _vp, _ll, _vp, _vp, _ll, _ll, _vp,
@@ -489,6 +498,122 @@ class LinearW8A8:
             ldx, ldo = c, self.C_out
         rc = _lib.aweq_linear_w8a8(Xq.data_ptr(), ldx, act_step.data_ptr(), act_zp.data_ptr(), PER_ROW if pairs == n else PER_TENSOR,
                                    *self._weight, n, c, self.C_out, out.data_ptr(), dtype_tag(out), ldo, _ptr(st), _stream())
+        if rc:
+            raise AweqError(rc)
+        return out
+
+
+# ---- microscaled 4-bit floating point
+def aweq_mx4_scale_bytes(rows, cols, fmt) -> int:
+    return int(_lib.aweq_mx4_scale_bytes(rows, cols, MX4_FORMATS[fmt]))
+
+
+def aweq_quant_mx4(X, scale, fmt, codes, scales, row_step=None, mu=None, epsmu=None, st=None):
+    """16-bit rows to 4-bit codes and block scales (argument marshalling only; see ``include/aweq.h``).  ``MX4`` holds the
+    buffers of one shape."""
+    rows, cols = X.shape
+    _want(scale, torch.float32, cols, "scale")
+    _want(codes, torch.uint8, rows * cols // 2, "codes")
+    _want(scales, torch.uint8, aweq_mx4_scale_bytes(rows, cols, fmt), "scales")
+    _want(row_step, torch.float32, rows, "row_step")
+    _want(mu, torch.float32, cols, "mu")
+    _want(epsmu, torch.float32, rows, "epsmu")
+    _check(_lib.aweq_quant_mx4(_ptr(X), dtype_tag(X), rows, cols, _pitch(X), _ptr(scale), MX4_FORMATS[fmt], _ptr(codes), _ptr(scales),
+                               _ptr(row_step), _ptr(mu), _ptr(epsmu), _ptr(st), _stream()))
+
+
+def aweq_dequant_mx4(codes, scales, row_step, fmt, out):
+    """What codes and scales stand for, rounded once to the type of ``out`` [rows x cols]."""
+    rows, cols = out.shape
+    _want(codes, torch.uint8, rows * cols // 2, "codes")
+    _want(scales, torch.uint8, aweq_mx4_scale_bytes(rows, cols, fmt), "scales")
+    _want(row_step, torch.float32, rows, "row_step")
+    _check(_lib.aweq_dequant_mx4(_ptr(codes), _ptr(scales), _ptr(row_step), MX4_FORMATS[fmt], rows, cols, _ptr(out), dtype_tag(out),
+                                 _pitch(out), _stream()))
+    return out
+
+
+def aweq_linear_mx4(Xq, x_scales, x_step, Wq, w_scales, w_step, fmt, bias, out, st=None):
+    """The 4-bit layer on what ``aweq_quant_mx4`` wrote (argument marshalling only; see ``include/aweq.h``).
+    ``LinearMX4`` marshals the weight's arguments once for repeated calls."""
+    (N, half), C_out = Xq.shape, Wq.shape[0]
+    _want_codes(Xq, "Xq")
+    _want_codes(Wq, "Wq")
+    if Wq.shape[1] != half or out.shape != (N, C_out) or not (Xq.is_contiguous() and Wq.is_contiguous()):
+        raise ValueError("shapes do not match: Xq %s, Wq %s, out %s" % (tuple(Xq.shape), tuple(Wq.shape), tuple(out.shape)))
+    for t, rows, what in ((x_scales, N, "x_scales"), (w_scales, C_out, "w_scales")):
+        _want(t, torch.uint8, aweq_mx4_scale_bytes(rows, 2 * half, fmt), what)
+    _want(x_step, torch.float32, N, "x_step")
+    _want(w_step, torch.float32, C_out, "w_step")
+    _want(bias, torch.float32, C_out, "bias")
+    _check(_lib.aweq_linear_mx4(_ptr(Xq), _ptr(x_scales), _ptr(x_step), _ptr(Wq), _ptr(w_scales), _ptr(w_step), MX4_FORMATS[fmt],
+                                _ptr(bias), N, 2 * half, C_out, _ptr(out), dtype_tag(out), _pitch(out), _ptr(st), _stream()))
+    return out
+
+
+class MX4:
+    """Buffers for a [rows x cols] matrix in microscaled 4-bit floating point: ``codes``, ``scales`` and, for "e4m3",
+    ``row_step``.  ``quantise`` fills them from 16-bit rows, ``values`` gives back what they stand for."""
+
+    def __init__(self, rows, cols, fmt="e8m0", device="cuda"):
+        if fmt not in MX4_FORMATS:
+            raise ValueError("fmt must be one of %s" % sorted(MX4_FORMATS))
+        if rows < 0 or cols <= 0 or cols % 32:
+            raise ValueError("cols must be a positive multiple of 32")
+        self.rows, self.cols, self.fmt = rows, cols, fmt
+        self.codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=device)
+        self.scales = torch.empty(aweq_mx4_scale_bytes(rows, cols, fmt), dtype=torch.uint8, device=device)
+        self.row_step = torch.empty(rows, dtype=torch.float32, device=device) if fmt == "e4m3" else None
+        self.args = (_ptr(self.codes), _ptr(self.scales), _ptr(self.row_step))
+        self.tag = MX4_FORMATS[fmt]
+
+    def quantise(self, X, scale=None, mu=None, epsmu=None, st=None):
+        """Codes of X times ``scale`` (float32 per column); ``epsmu`` gets the row sums of (value - X scale) mu."""
+        shape, (ld, one) = X.shape, X.stride()
+        if shape != (self.rows, self.cols) or one != 1 or not X.is_cuda:
+            raise ValueError("X must be a 16-bit device matrix [%d x %d] with contiguous rows" % (self.rows, self.cols))
+        for t, n, what in ((scale, self.cols, "scale"), (mu, self.cols, "mu"), (epsmu, self.rows, "epsmu")):
+            _want(t, torch.float32, n, what)
+        rc = _lib.aweq_quant_mx4(X.data_ptr(), dtype_tag(X), self.rows, self.cols, ld if self.rows > 1 else self.cols, _ptr(scale), self.tag,
+                                 *self.args, _ptr(mu), _ptr(epsmu), _ptr(st), _stream())
+        if rc:
+            raise AweqError(rc)
+        return self
+
+    def values(self, out=None, dtype=torch.bfloat16):
+        out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.codes.device) if out is None else out
+        if out.shape != (self.rows, self.cols):
+            raise ValueError("out must be [%d x %d]" % (self.rows, self.cols))
+        return aweq_dequant_mx4(self.codes, self.scales, self.row_step, self.fmt, out)
+
+
+class LinearMX4:
+    """A linear layer in microscaled 4-bit floating point: quantises the 16-bit weights [C_out x C_in] times ``scale`` (the
+    equalisation factors s) once and keeps codes, scales and a copy of the binary32 bias.  Called with the activations'
+    ``MX4`` (quantised with 1/s) it writes the 16-bit output on the current stream.  ``mu``: E[x/s] of the calibration; the
+    bias is then corrected for the mean of the weights' rounding (Eq. 15)."""
+
+    def __init__(self, W, fmt="e8m0", scale=None, bias=None, mu=None, st=None):
+        self.C_out, self.C_in = W.shape
+        self.fmt = fmt
+        _want(bias, torch.float32, self.C_out, "bias")
+        self.weight = MX4(self.C_out, self.C_in, fmt, W.device)
+        epsmu = None if mu is None else torch.empty(self.C_out, dtype=torch.float32, device=W.device)
+        self.weight.quantise(W, scale, mu, epsmu, st)
+        self.bias = None if bias is None else bias.clone()
+        if mu is not None:
+            self.bias = -epsmu if bias is None else bias - epsmu
+        self._args = (*self.weight.args, self.weight.tag, _ptr(self.bias))
+
+    def __call__(self, xq, out=None, dtype=torch.float16, st=None):
+        n = xq.rows
+        if out is None:
+            out = torch.empty((n, self.C_out), dtype=dtype, device=xq.codes.device)
+        ldo, one = out.stride()
+        if xq.cols != self.C_in or xq.fmt != self.fmt or out.shape != (n, self.C_out) or one != 1 or not out.is_cuda:
+            raise ValueError("xq must be an MX4 [N x %d] of format %s, out [N x %d] with contiguous rows" % (self.C_in, self.fmt, self.C_out))
+        rc = _lib.aweq_linear_mx4(*xq.args, *self._args, n, self.C_in, self.C_out, out.data_ptr(), dtype_tag(out),
+                                  ldo if n > 1 else self.C_out, _ptr(st), _stream())
         if rc:
             raise AweqError(rc)
         return out

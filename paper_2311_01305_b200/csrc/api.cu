@@ -9,6 +9,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "linear8.cuh"
+#include "mx4.cuh"
 
 namespace aweq {
 
@@ -540,6 +541,72 @@ aweq_status aweq_linear_w8a8(const unsigned char *Xq, long long ldx, const float
     a.x_inc = act_gran == AWEQ_PER_ROW; a.w_inc = w_gran == AWEQ_PER_ROW;
     a.K = (int)C_in; a.O = (int)C_out; a.out = reinterpret_cast<uint16_t *>(out); a.st = st;
     return run_linear8(a, dt, (cudaStream_t)stream);
+}
+
+static aweq_status check_mx4(int fmt, long long rows, long long cols)
+{
+    if (fmt != AWEQ_MX4_E8M0 && fmt != AWEQ_MX4_E4M3) return AWEQ_ERR_UNSUPPORTED;
+    if (rows < 0 || rows > 0x7fffffffll || cols <= 0 || cols % 32 || cols > AWEQ_LINEAR_MAX_C_IN) return AWEQ_ERR_SHAPE;
+    if ((rows + 127) / 128 * mx4_row_tiles(cols, fmt) > 0x7fffffffll) return AWEQ_ERR_SHAPE;
+    return AWEQ_OK;
+}
+
+size_t aweq_mx4_scale_bytes(long long rows, long long cols, aweq_mx4_format fmt)
+{
+    if (check_mx4(fmt, rows, cols) != AWEQ_OK) return 0;
+    return (size_t)((rows + 127) / 128 * mx4_row_tiles(cols, fmt)) * kMx4Tile;
+}
+
+aweq_status aweq_quant_mx4(const void *X, aweq_dtype dt, long long rows, long long cols, long long ld, const float *scale,
+                           aweq_mx4_format fmt, unsigned char *codes, unsigned char *scales, float *row_step, const float *mu,
+                           float *epsmu, aweq_dev_status *st, void *stream)
+{
+    if (dt != AWEQ_F16 && dt != AWEQ_BF16) return AWEQ_ERR_DTYPE;
+    aweq_status rc = check_mx4(fmt, rows, cols);
+    if (rc != AWEQ_OK) return rc;
+    if ((mu == nullptr) != (epsmu == nullptr)) return AWEQ_ERR_NULL;
+    if (rows == 0) return AWEQ_OK;
+    if (!X || !codes || !scales || (fmt == AWEQ_MX4_E4M3 && !row_step)) return AWEQ_ERR_NULL;
+    if (!aligned(X, 16) || ld < cols || ld % 8 || !aligned(codes, 16) || !aligned(scales, 16) || !aligned(scale, 16) || !aligned(mu, 16) ||
+        !aligned(row_step, 4) || !aligned(epsmu, 4))
+        return AWEQ_ERR_ALIGN;
+    AWEQ_LOGF("aweq_quant_mx4 rows=%lld cols=%lld fmt=%d bytes=%lld\n", rows, cols, (int)fmt, rows * cols * 5 / 2);
+    return run_quant_mx4(X, dt, rows, cols, ld, scale, fmt, codes, scales, row_step, mu, epsmu, st, (cudaStream_t)stream);
+}
+
+aweq_status aweq_dequant_mx4(const unsigned char *codes, const unsigned char *scales, const float *row_step, aweq_mx4_format fmt,
+                             long long rows, long long cols, void *out, aweq_dtype dt, long long ldo, void *stream)
+{
+    if (dt != AWEQ_F16 && dt != AWEQ_BF16) return AWEQ_ERR_DTYPE;
+    aweq_status rc = check_mx4(fmt, rows, cols);
+    if (rc != AWEQ_OK || rows == 0) return rc;
+    if (!out || !codes || !scales || (fmt == AWEQ_MX4_E4M3 && !row_step)) return AWEQ_ERR_NULL;
+    if (!aligned(out, 16) || ldo < cols || ldo % 8 || !aligned(codes, 16) || !aligned(scales, 16) || !aligned(row_step, 4)) return AWEQ_ERR_ALIGN;
+    return run_dequant_mx4(codes, scales, row_step, fmt, rows, cols, out, dt, ldo, (cudaStream_t)stream);
+}
+
+aweq_status aweq_linear_mx4(const unsigned char *Xq, const unsigned char *x_scales, const float *x_step, const unsigned char *Wq,
+                            const unsigned char *w_scales, const float *w_step, aweq_mx4_format fmt, const float *bias, long long N,
+                            long long C_in, long long C_out, void *out, aweq_dtype dt, long long ldo, aweq_dev_status *st, void *stream)
+{
+    if (dt != AWEQ_F16 && dt != AWEQ_BF16) return AWEQ_ERR_DTYPE;
+    aweq_status rc = check_mx4(fmt, N, C_in);
+    if (rc == AWEQ_OK) rc = check_mx4(fmt, C_out, C_in);
+    if (rc != AWEQ_OK) return rc;
+    if (C_out <= 0 || C_out > (1ll << 30)) return AWEQ_ERR_SHAPE;
+    const bool steps = fmt == AWEQ_MX4_E4M3;
+    if (!Wq || !w_scales || (steps && !w_step)) return AWEQ_ERR_NULL;
+    if (N > 0 && (!Xq || !x_scales || !out || (steps && !x_step))) return AWEQ_ERR_NULL;
+    if (!aligned(Xq, 16) || !aligned(Wq, 16) || !aligned(x_scales, 16) || !aligned(w_scales, 16) || !aligned(x_step, 4) || !aligned(w_step, 4) ||
+        !aligned(bias, 4) || !aligned(out, 2) || ldo < C_out)
+        return AWEQ_ERR_ALIGN;
+    if (N == 0) return AWEQ_OK;
+    AWEQ_LOGF("aweq_linear_mx4 N=%lld C_in=%lld C_out=%lld fmt=%d ops=%.3e\n", N, C_in, C_out, (int)fmt, 2.0 * N * C_in * C_out);
+    Mx4LinearArgs a = {};
+    a.X = Xq; a.W = Wq; a.x_scales = x_scales; a.w_scales = w_scales; a.bias = bias; a.N = N; a.ldo = ldo;
+    a.x_step = steps ? x_step : nullptr; a.w_step = steps ? w_step : nullptr;
+    a.K = (int)C_in; a.O = (int)C_out; a.fmt = fmt; a.out = reinterpret_cast<uint16_t *>(out); a.st = st;
+    return run_linear_mx4(a, dt, (cudaStream_t)stream);
 }
 
 aweq_status aweq_rope_table(const aweq_rope *r, long long n_pos, float *table, void *stream)

@@ -86,6 +86,14 @@ aweq_status fc_gemm_bf16(const void *A, const void *B, void *C, int M, int N, in
 aweq_status run_code_sums(const unsigned char *codes, long long rows, long long cols, long long ld, int *sums,
                           cudaStream_t stream);
 
+aweq_status run_quant_mx4(const void *X, aweq_dtype dt, long long rows, long long cols, long long ld, const float *scale, int fmt,
+                          unsigned char *codes, unsigned char *scales, float *row_step, const float *mu, float *epsmu,
+                          aweq_dev_status *st, cudaStream_t stream);
+aweq_status run_dequant_mx4(const unsigned char *codes, const unsigned char *scales, const float *row_step, int fmt, long long rows,
+                            long long cols, void *out, aweq_dtype dt, long long ldo, cudaStream_t stream);
+struct Mx4LinearArgs;
+aweq_status run_linear_mx4(const Mx4LinearArgs &a, aweq_dtype dt, cudaStream_t stream);
+
 aweq_status run_rope_table(const aweq_rope *spec, long long n_pos, float *table, cudaStream_t stream);
 
 struct KvAppendArgs {

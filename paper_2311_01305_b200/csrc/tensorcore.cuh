@@ -18,6 +18,8 @@ inline bool tma_pool_fits(long long page_stride, long long token_stride, long lo
 {
     return page_stride < 1ll << 39 && token_stride < 1ll << 39 && head_stride < 1ll << 39;
 }
+// `tiles` tiles of 512 bytes in a row, read `box` at a time into consecutive shared memory
+aweq_status tma_tiles_map(CUtensorMap *map, const void *base, long long tiles, int box);
 aweq_status tma_pool_map(CUtensorMap *map, const void *base, long long pages, int tokens, int heads, int dim, long long page_stride,
                          long long token_stride, long long head_stride, int box_tokens);
 
@@ -72,6 +74,46 @@ __device__ __forceinline__ void tc_mma_u8(uint32_t d, uint32_t a, uint32_t b, ui
                      "@q tcgen05.mma.cta_group::2.kind::i8 [%0], da, db, %3, p;\n\t}"
                      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kTcDescHi), "r"((uint32_t)lead) : "memory");
 }
+// ------------------------------------------------------------------ 4-bit operands with block scales
+// e2m1 x e2m1 -> binary32, both K-major, 64 elements of K (32 bytes of a row) an instruction.  `e8m0`: blocks of 32 with
+// power-of-two scales, of which a word of TMEM holds those of two instructions; else blocks of 16 with e4m3 scales, a word
+// for one.  `half`: which two of the four scales (e8m0).
+__host__ __device__ constexpr uint32_t tc_idesc_mx4(bool e8m0, int m, int n)
+{
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((e8m0 ? 1u : 0u) << 23) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t tc_idesc_mx4_half(uint32_t idesc, int half) { return idesc | ((uint32_t)half << 5) | ((uint32_t)half << 30); }
+template <int CG, bool E8M0>
+__device__ __forceinline__ void tc_mma_mx4(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool add, bool lead)
+{
+#define AWEQ_MMA_MX4(CG_, KIND_)                                                                                              \
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %6, 0;\n\t"           \
+                 "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"                                                        \
+                 "@q tcgen05.mma.cta_group::" CG_ "." KIND_ " [%0], da, db, %3, [%7], [%8], p;\n\t}"                          \
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kTcDescHi), "r"((uint32_t)lead), "r"(sa), "r"(sb) : "memory")
+    if (CG == 1) {
+        if (E8M0) AWEQ_MMA_MX4("1", "kind::mxf4.block_scale.scale_vec::2X");
+        else AWEQ_MMA_MX4("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+    } else {
+        if (E8M0) AWEQ_MMA_MX4("2", "kind::mxf4.block_scale.scale_vec::2X");
+        else AWEQ_MMA_MX4("2", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+    }
+#undef AWEQ_MMA_MX4
+}
+// A tile of scales (32 rows of 16 bytes, without swizzle) to four columns of TMEM, the same in every quarter of the lanes.  In order
+// with the products that this thread issues later; not with those before it.
+constexpr uint32_t kTcScaleDescHi = 8u | (1u << 14);
+template <int CG>
+__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint32_t smem, bool lead)
+{
+    const uint32_t lo = (smem >> 4) & 0x3fff;
+    if (CG == 1)
+        asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 d;\n\tsetp.ne.u32 q, %3, 0;\n\tmov.b64 d, {%1, %2};\n\t"
+                     "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}" ::"r"(tmem), "r"(lo), "r"(kTcScaleDescHi), "r"((uint32_t)lead) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\t.reg .b64 d;\n\tsetp.ne.u32 q, %3, 0;\n\tmov.b64 d, {%1, %2};\n\t"
+                     "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], d;\n\t}" ::"r"(tmem), "r"(lo), "r"(kTcScaleDescHi), "r"((uint32_t)lead) : "memory");
+}
 // one arrival on the barrier (cta_group::2: on that barrier of both CTAs of the pair) when every
 // tcgen05.mma issued so far by this thread has completed
 template <int CG>
@@ -103,6 +145,14 @@ __device__ __forceinline__ void tc_ld32(uint32_t tmem, uint32_t (&r)[32])
         : "r"(tmem));
 }
 
+__device__ __forceinline__ void tc_ld16(uint32_t tmem, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(tmem));
+}
 __device__ __forceinline__ uint32_t tc_ld1(uint32_t tmem)
 {
     uint32_t r;

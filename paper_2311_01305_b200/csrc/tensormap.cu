@@ -8,7 +8,8 @@ using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void
                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 static aweq_status encode_map(CUtensorMap *map, CUtensorMapDataType type, int rank, const void *base, const cuuint64_t *dims,
-                              const cuuint64_t *strides, const cuuint32_t *box)
+                              const cuuint64_t *strides, const cuuint32_t *box,
+                              CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B)
 {
     static const Encode encode = [] {
         void *f = nullptr;
@@ -21,7 +22,7 @@ static aweq_status encode_map(CUtensorMap *map, CUtensorMapDataType type, int ra
     if (!encode) return AWEQ_ERR_UNSUPPORTED;
     const cuuint32_t step[4] = {1, 1, 1, 1};
     const CUresult r = encode(map, type, (cuuint32_t)rank, const_cast<void *>(base), dims, strides, box, step,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? AWEQ_OK : cuda_failed(cudaErrorInvalidValue);
 }
@@ -31,6 +32,13 @@ aweq_status tma_bytes_map(CUtensorMap *map, const void *base, long long rows, lo
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)ld};
     const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
     return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, pitch, box);
+}
+
+aweq_status tma_tiles_map(CUtensorMap *map, const void *base, long long tiles, int box_tiles)
+{
+    const cuuint64_t dims[2] = {128, (cuuint64_t)tiles}, pitch[1] = {512};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_tiles};
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, base, dims, pitch, box, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 aweq_status tma_pool_map(CUtensorMap *map, const void *base, long long pages, int tokens, int heads, int dim, long long page_stride,
