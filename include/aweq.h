@@ -525,6 +525,48 @@ aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, lo
                            long long n_pos, int rotary_dim, int interleaved, const void *q, long long ldq, int n_heads,
                            void *q_out, long long ld_qout, aweq_dev_status *st, void *stream);
 
+/* The same with the places given one by one: token t is stored at slot[t] = page * page_size + row of the pool and turned by
+ * pos[t] (which is not a place: the drafted children of one token have one position and a slot each).  A slot below zero says that
+ * there is no such token: nothing is stored, its q_out becomes zero, nothing is counted.  A slot outside the pool or (with
+ * rope) a position outside the table is treated and counted as above. */
+aweq_status aweq_kv_append_slots(const aweq_kv_cache *cache, const long long *slot, const void *k, long long ldk, const void *v,
+                                 long long ldv, const int *pos, long long n_tokens, const float *rope, long long n_pos,
+                                 int rotary_dim, int interleaved, const void *q, long long ldq, int n_heads, void *q_out,
+                                 long long ld_qout, aweq_dev_status *st, void *stream);
+
+/* Lengths, pages, slots, positions and tree masks of a step, from the sequences' lengths, on the device.
+ * Sequence b holds held[b] keys and changes by change[b]: new tokens, or, below zero, keys given up at its end.  Then
+ *   own_len[b] = held[b] + change[b]; start[b] = its first new token (start[n_seq]: all of them);
+ *   pages ceil(own_len / page_size) - ceil(held / page_size) are taken from or put to the ring of free pages, in the order of the
+ *   sequences, and row b of page_table gets them (its row keeps a -1 for a page put back).
+ * New token t, the i'th of sequence b (t = start[b] + i): seq[t] = b, pos[t] = first + held[b] + i, slot[t] = page * page_size +
+ * row of key held[b] + i.  Rows from start[n_seq] to max_tokens get seq, pos and slot -1 (and mask 0).
+ * parent: NULL, or for every new token the number within its sequence of the node above it, a smaller one than its own, -1 for
+ * none (drafted trees): then pos[t] = first + held[b] + its depth, and mask[t] (words 64-bit words, node j in bit j % 64 of word
+ * j / 64) has the bits of the node itself and of those above it.  At most 64 * words nodes to a sequence; words 1 to 4.
+ * ring: int[n_pages], state: {taken, given}: the free pages are ring[i % n_pages], taken <= i < given; taken pages come from the one end,
+ * pages put back go to the other (this call takes none of those that it puts back).  n_pages at most 2^22.
+ * Where something does not fit, it is counted in st->out_of_range, once for each sequence: a length or change beyond 0 ..
+ * pages_per_seq * page_size or the max_tokens rows is clamped, a sequence that finds no free pages keeps own_len within what it
+ * has, and its tokens without a page get slot -1, pages put back beyond n_pages are lost.  Also counted: each page number outside
+ * 0 .. n_pages in the ring that is taken, each parent that is none of the nodes before (the node then has none), each node
+ * beyond 64 * words (mask 0, depth 0), and a state that cannot be, which is taken as an empty ring.
+ * own_len must not be held or change.  seq, pos, slot, mask and ws 16-byte aligned (not read for max_tokens = 0).
+ * ws: aweq_kv_plan_workspace_bytes(n_seq) bytes, 256-byte aligned, zero before its first call, for one stream at a time. */
+size_t aweq_kv_plan_workspace_bytes(long long n_seq);
+aweq_status aweq_kv_plan(int *page_table, long long n_seq, long long pages_per_seq, long long ld_table, int page_size, int *ring,
+                         long long *state, long long n_pages, const int *held, const int *change, long long first,
+                         long long max_tokens, int *own_len, int *start, int *seq, int *pos, long long *slot, const int *parent,
+                         long long *mask, int words, void *ws, size_t ws_bytes, aweq_dev_status *st, void *stream);
+
+/* Moves the keys and values of accepted drafts together: key base[b] + path[b, i] of sequence b goes to base[b] + i, i <
+ * n_path[b] <= max_path (row pitch ld_path).  A path ascends.  Keys lie where row b of page_table says; no page belongs
+ * to two sequences here.  A sequence with a base, a count, a page or a node out of range or order is counted in st->out_of_range once;
+ * what comes before such a node is moved, the rest stays. */
+aweq_status aweq_kv_accept(const aweq_kv_cache *cache, const int *page_table, long long n_seq, long long pages_per_seq,
+                           long long ld_table, const int *base, const int *path, long long ld_path, int max_path,
+                           const int *n_path, aweq_dev_status *st, void *stream);
+
 /* Attention of n_q tokens of each of n_seq sequences over the prefix they share (prefix_len keys in
  * prefix_pages, the same for all) and each sequence's own keys (own_len[b] keys in row b of page_table,
  * the n_q tokens themselves included, appended before this call):

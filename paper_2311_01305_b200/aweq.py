@@ -127,6 +127,16 @@ _lib.aweq_rope_table.restype = _i
 _lib.aweq_kv_append.argtypes = [ctypes.POINTER(KvCacheArgs), _vp, _ll, _ll, _ll, _vp, _ll, _vp, _ll, _vp, _vp, _ll, _ll, _vp,
                                 _ll, _i, _i, _vp, _ll, _i, _vp, _ll, _vp, _vp]
 _lib.aweq_kv_append.restype = _i
+_lib.aweq_kv_append_slots.argtypes = [ctypes.POINTER(KvCacheArgs), _vp, _vp, _ll, _vp, _ll, _vp, _ll, _vp, _ll, _i, _i, _vp, _ll, _i,
+                                      _vp, _ll, _vp, _vp]
+_lib.aweq_kv_append_slots.restype = _i
+_lib.aweq_kv_plan_workspace_bytes.argtypes = [_ll]
+_lib.aweq_kv_plan_workspace_bytes.restype = _sz
+_lib.aweq_kv_plan.argtypes = [_vp, _ll, _ll, _ll, _i, _vp, _vp, _ll, _vp, _vp, _ll, _ll, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz,
+                              _vp, _vp]
+_lib.aweq_kv_plan.restype = _i
+_lib.aweq_kv_accept.argtypes = [ctypes.POINTER(KvCacheArgs), _vp, _ll, _ll, _ll, _vp, _vp, _ll, _i, _vp, _vp, _vp]
+_lib.aweq_kv_accept.restype = _i
 _lib.aweq_prefix_attention_workspace_bytes.argtypes = [ctypes.POINTER(KvCacheArgs), _ll, _ll, _ll, _i, _i]
 _lib.aweq_prefix_attention_workspace_bytes.restype = _sz
 _lib.aweq_prefix_attention.argtypes = [_vp, _ll, ctypes.POINTER(KvCacheArgs), _vp, _ll, _vp, _ll, _ll, _vp, _ll, _ll, _i, _i,
@@ -705,6 +715,112 @@ def aweq_kv_append(cache, page_table, k, v, pos, seq=None, first=0, table=None, 
     if rc:
         raise AweqError(rc)
     return q_out
+
+
+def aweq_kv_append_slots(cache, slot, k, v, pos, table=None, interleaved=False, q=None, q_out=None, st=None):
+    """``aweq_kv_append`` with the place of every token in ``slot`` (int64: page * page_size + row, below zero for rows that are no
+    tokens); ``pos`` turns only (argument marshalling only; see ``include/aweq.h``)."""
+    d, kv, dt, n = cache.head_dim, cache.n_kv_heads, cache.dtype, k.shape[0]
+    ldk, ldv = _heads(k, n, kv, d, dt, "k"), _heads(v, n, kv, d, dt, "v")
+    if slot.dtype is not torch.int64 or slot.numel() != n or not slot.is_contiguous() or not slot.is_cuda:
+        raise ValueError("slot must be a contiguous int64 device tensor of %d elements" % n)
+    n_pos = rd = 0
+    if table is not None:
+        n_pos, rd = table.shape
+        if table.dtype is not torch.float32 or not table.is_contiguous():
+            raise ValueError("table must be contiguous float32 [positions, rotary_dim]")
+    ldq = ldo = heads = 0
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else q.shape[1] // d
+        q_out = q if q_out is None else q_out
+        ldq, ldo = _heads(q, n, heads, d, dt, "q"), _heads(q_out, n, heads, d, dt, "q_out")
+    rc = _lib.aweq_kv_append_slots(cache.ref, slot.data_ptr(), k.data_ptr(), ldk, v.data_ptr(), ldv, _int32_rows(pos, n, "pos"), n,
+                                   _ptr(table), n_pos, rd, 1 if interleaved else 0, _ptr(q), ldq, heads, _ptr(q_out), ldo, _ptr(st),
+                                   _stream())
+    if rc:
+        raise AweqError(rc)
+    return q_out
+
+
+def aweq_kv_plan_workspace_bytes(n_seq) -> int:
+    return int(_lib.aweq_kv_plan_workspace_bytes(n_seq))
+
+
+def aweq_kv_plan(page_table, page_size, ring, state, held, change, own_len, start, ws, max_tokens=0, seq=None, pos=None, slot=None, first=0,
+                 parent=None, mask=None, st=None):
+    """Lengths, pages, slots, positions and tree masks of a step (argument marshalling only; see ``include/aweq.h``).  ``PagePool``
+    and ``StepPlan`` hold what it reads and writes."""
+    pages, n_seq, per_seq, ld_table = _int32_table(page_table, "page_table")
+    n_pages = ring.numel()
+    if state.dtype is not torch.int64 or state.numel() != 2 or not state.is_contiguous() or not state.is_cuda:
+        raise ValueError("state must be a contiguous int64 device tensor of two elements")
+    if max_tokens:
+        if slot is None or slot.dtype is not torch.int64 or slot.numel() != max_tokens or not slot.is_contiguous():
+            raise ValueError("slot must be a contiguous int64 device tensor of %d elements" % max_tokens)
+        rows = (_int32_rows(seq, max_tokens, "seq"), _int32_rows(pos, max_tokens, "pos"), _ptr(slot))
+    else:
+        rows = (None, None, None)
+    up = bits = None
+    words = 0
+    if parent is not None and max_tokens:
+        if mask is None or mask.dtype is not torch.int64 or mask.dim() != 2 or mask.shape[0] != max_tokens or not mask.is_contiguous():
+            raise ValueError("with parent, mask must be a contiguous int64 device matrix with a row per token")
+        words = mask.shape[1]
+        up, bits = _int32_rows(parent, max_tokens, "parent"), _ptr(mask)
+    rc = _lib.aweq_kv_plan(pages, n_seq, per_seq, ld_table, page_size, _int32_rows(ring, n_pages, "ring"), state.data_ptr(), n_pages,
+                           _int32_rows(held, n_seq, "held"), _int32_rows(change, n_seq, "change"), first, max_tokens,
+                           _int32_rows(own_len, n_seq, "own_len"), _int32_rows(start, n_seq + 1, "start"), *rows, up, bits, words,
+                           _ptr(ws), ws.numel(), _ptr(st), _stream())
+    if rc:
+        raise AweqError(rc)
+
+
+class StepPlan:
+    """What ``PagePool.plan`` writes for ``n_seq`` sequences and up to ``max_tokens`` new tokens: ``own_len``, ``start``, ``seq``,
+    ``pos``, ``slot`` and, for drafted trees of up to ``max_nodes`` nodes a sequence, ``mask``.  Serves one stream at a time."""
+
+    def __init__(self, n_seq, max_tokens, max_nodes=0, device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.n_seq, self.max_tokens = n_seq, max_tokens
+        self.own_len, self.start = torch.empty(n_seq, **i32), torch.empty(n_seq + 1, **i32)
+        self.seq, self.pos = torch.empty(max_tokens, **i32), torch.empty(max_tokens, **i32)
+        self.slot = torch.empty(max_tokens, dtype=torch.int64, device=device)
+        self.mask = torch.empty((max_tokens, -(-max_nodes // 64)), dtype=torch.int64, device=device) if max_nodes else None
+        self.ws = workspace(aweq_kv_plan_workspace_bytes(n_seq), device).zero_()
+
+
+class PagePool:
+    """The free pages of a cache, as a ring in device memory: all of them at first, or ``ring`` (int32, one place for every page of the
+    cache) and ``state`` (int64: taken, given) as they are."""
+
+    def __init__(self, n_pages, page_size, device="cuda", ring=None, state=None):
+        self.n_pages, self.page_size = n_pages, page_size
+        self.ring = torch.arange(n_pages, dtype=torch.int32, device=device) if ring is None else ring
+        self.state = torch.tensor([0, n_pages], dtype=torch.int64, device=device) if state is None else state
+        if self.ring.numel() != n_pages:
+            raise ValueError("ring has a place for every page")
+
+    def plan(self, page_table, held, change, into, first=0, parent=None, st=None):
+        """Sequence b of ``page_table`` holds ``held[b]`` keys and gets ``change[b]`` new tokens (below zero: gives up that many): its
+        pages come from or go to the ring, lengths, slots and positions are written into the ``StepPlan`` ``into``."""
+        if parent is not None and into.mask is None:
+            raise ValueError("trees need a StepPlan with max_nodes")
+        aweq_kv_plan(page_table, self.page_size, self.ring, self.state, held, change, into.own_len, into.start, into.ws, into.max_tokens,
+                     into.seq, into.pos, into.slot, first, parent, into.mask, st)
+        return into
+
+
+def aweq_kv_accept(cache, page_table, base, path, n_path, st=None):
+    """Key ``base[b] + path[b, i]`` of sequence b goes to ``base[b] + i``, i < ``n_path[b]`` (argument marshalling only; see
+    ``include/aweq.h``)."""
+    pages, n_seq, per_seq, ld_table = _int32_table(page_table, "page_table")
+    paths, rows, most, ld_path = _int32_table(path, "path")
+    if rows != n_seq:
+        raise ValueError("path has a row per sequence")
+    rc = _lib.aweq_kv_accept(cache.ref, pages, n_seq, per_seq, ld_table, _int32_rows(base, n_seq, "base"), paths, ld_path, most,
+                             _int32_rows(n_path, n_seq, "n_path"), _ptr(st), _stream())
+    if rc:
+        raise AweqError(rc)
 
 
 def aweq_prefix_attention_workspace_bytes(cache, prefix_len, max_own, n_seq, n_q, n_heads) -> int:

@@ -634,6 +634,21 @@ static aweq_status check_cache(const aweq_kv_cache *c, int most_dim)
     return AWEQ_OK;
 }
 
+static KvAppendArgs append_args(const aweq_kv_cache *cache, const void *k, long long ldk, const void *v, long long ldv, const int *pos,
+                                long long n_tokens, const float *rope, long long n_pos, int rotary_dim, int interleaved, const void *q,
+                                long long ldq, int n_heads, void *q_out, long long ld_qout, aweq_dev_status *st)
+{
+    KvAppendArgs a = {};
+    a.ck = reinterpret_cast<uint16_t *>(cache->k); a.cv = reinterpret_cast<uint16_t *>(cache->v);
+    a.n_pages = cache->n_pages; a.page_stride = cache->page_stride; a.token_stride = cache->token_stride;
+    a.head_stride = cache->head_stride; a.page_size = cache->page_size; a.n_kv = cache->n_kv_heads;
+    a.head_dim = cache->head_dim; a.k = reinterpret_cast<const uint16_t *>(k); a.v = reinterpret_cast<const uint16_t *>(v);
+    a.q = reinterpret_cast<const uint16_t *>(q); a.q_out = reinterpret_cast<uint16_t *>(q_out);
+    a.ldk = ldk; a.ldv = ldv; a.ldq = ldq; a.ld_qout = ld_qout; a.n_heads = q ? n_heads : 0; a.pos = pos; a.n_tokens = n_tokens;
+    a.rope = rope; a.n_pos = n_pos; a.rd = rope ? rotary_dim : 0; a.interleaved = interleaved; a.st = st;
+    return a;
+}
+
 aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, long long n_seq, long long pages_per_seq,
                            long long ld_table, const void *k, long long ldk, const void *v, long long ldv,
                            const int *pos, const int *seq, long long first, long long n_tokens, const float *rope,
@@ -662,17 +677,89 @@ aweq_status aweq_kv_append(const aweq_kv_cache *cache, const int *page_table, lo
     AWEQ_LOGF("aweq_kv_append tokens=%lld heads=%d kv_heads=%d head_dim=%d rotary_dim=%d bytes=%lld\n", n_tokens,
               q ? n_heads : 0, cache->n_kv_heads, cache->head_dim, rope ? rotary_dim : 0,
               n_tokens * ((q ? n_heads : 0) + 2 * cache->n_kv_heads) * cache->head_dim * 4);
-    KvAppendArgs a = {};
+    KvAppendArgs a = append_args(cache, k, ldk, v, ldv, pos, n_tokens, rope, n_pos, rotary_dim, interleaved, q, ldq, n_heads, q_out, ld_qout, st);
+    a.page_table = page_table; a.n_seq = n_seq; a.pages_per_seq = pages_per_seq; a.ld_table = ld_table; a.seq = seq; a.first = first;
+    return run_kv_append(a, cache->dt, (cudaStream_t)stream);
+}
+
+aweq_status aweq_kv_append_slots(const aweq_kv_cache *cache, const long long *slot, const void *k, long long ldk, const void *v,
+                                 long long ldv, const int *pos, long long n_tokens, const float *rope, long long n_pos, int rotary_dim,
+                                 int interleaved, const void *q, long long ldq, int n_heads, void *q_out, long long ld_qout,
+                                 aweq_dev_status *st, void *stream)
+{
+    aweq_status rc = check_cache(cache, 256);
+    if (rc != AWEQ_OK) return rc;
+    const long long row = (long long)cache->n_kv_heads * cache->head_dim;
+    if (n_tokens < 0 || n_tokens > 0x7fffffffll) return AWEQ_ERR_SHAPE;
+    if (rope && (rotary_dim < 2 || rotary_dim % 2 || rotary_dim > cache->head_dim || n_pos <= 0)) return AWEQ_ERR_SHAPE;
+    if ((q == nullptr) != (q_out == nullptr)) return AWEQ_ERR_NULL;
+    if (q && (n_heads <= 0 || n_heads > 65536)) return AWEQ_ERR_SHAPE;
+    if (n_tokens == 0) return AWEQ_OK;
+    if (!slot || !k || !v || !pos) return AWEQ_ERR_NULL;
+    if (ldk < row || ldv < row || !aligned(k, 2) || !aligned(v, 2) || !aligned(pos, 4) || !aligned(slot, 8) || !aligned(rope, 4)) return AWEQ_ERR_ALIGN;
+    if (q) {
+        const long long qrow = (long long)n_heads * cache->head_dim;
+        if (ldq < qrow || ld_qout < qrow || !aligned(q, 2) || !aligned(q_out, 2)) return AWEQ_ERR_ALIGN;
+    }
+    KvAppendArgs a = append_args(cache, k, ldk, v, ldv, pos, n_tokens, rope, n_pos, rotary_dim, interleaved, q, ldq, n_heads, q_out, ld_qout, st);
+    a.slot = slot;
+    return run_kv_append(a, cache->dt, (cudaStream_t)stream);
+}
+
+constexpr long long kMostPages = 1ll << 22;
+
+size_t aweq_kv_plan_workspace_bytes(long long n_seq)
+{
+    return n_seq < 0 || n_seq > 0x7fffffffll ? 0 : kv_plan_ws_bytes(n_seq);
+}
+
+aweq_status aweq_kv_plan(int *page_table, long long n_seq, long long pages_per_seq, long long ld_table, int page_size, int *ring,
+                         long long *state, long long n_pages, const int *held, const int *change, long long first,
+                         long long max_tokens, int *own_len, int *start, int *seq, int *pos, long long *slot, const int *parent,
+                         long long *mask, int words, void *ws, size_t ws_bytes, aweq_dev_status *st, void *stream)
+{
+    if (n_seq <= 0 || n_seq > 0x7fffffffll || pages_per_seq <= 0 || pages_per_seq > 0x7fffffffll || page_size <= 0 || page_size > (1 << 20) ||
+        n_pages <= 0 || n_pages > kMostPages || max_tokens < 0 || max_tokens > 0x7fffffffll - 2048 || first < 0)
+        return AWEQ_ERR_SHAPE;
+    if (first + (double)pages_per_seq * page_size > 2147483647.0) return AWEQ_ERR_SHAPE;
+    if (!page_table || !ring || !state || !held || !change || !own_len || !start) return AWEQ_ERR_NULL;
+    if (max_tokens && (!seq || !pos || !slot)) return AWEQ_ERR_NULL;
+    if ((parent == nullptr) != (mask == nullptr)) return AWEQ_ERR_NULL;
+    if (parent && (words < 1 || words > kPlanMaxWords)) return AWEQ_ERR_SHAPE;
+    if (ld_table < pages_per_seq || !aligned(page_table, 4) || !aligned(ring, 4) || !aligned(state, 8) || !aligned(held, 4) || !aligned(change, 4) ||
+        !aligned(own_len, 4) || !aligned(start, 4) || !aligned(parent, 4) || own_len == held || own_len == change)
+        return AWEQ_ERR_ALIGN;
+    if (max_tokens && (!aligned(seq, 16) || !aligned(pos, 16) || !aligned(slot, 16) || !aligned(mask, 16))) return AWEQ_ERR_ALIGN;
+    aweq_status rc = check_ws(ws, ws_bytes, kv_plan_ws_bytes(n_seq));
+    if (rc != AWEQ_OK) return rc;
+    AWEQ_LOGF("aweq_kv_plan seqs=%lld tokens=%lld page=%d words=%d\n", n_seq, max_tokens, page_size, parent ? words : 0);
+    KvPlanArgs a = {};
+    a.page_table = page_table; a.n_seq = n_seq; a.pages_per_seq = pages_per_seq; a.ld_table = ld_table; a.page_size = page_size;
+    a.words = words; a.ring = ring; a.state = state; a.n_pages = n_pages; a.held = held; a.change = change; a.parent = parent;
+    a.first = first; a.max_tokens = max_tokens; a.own_len = own_len; a.start = start; a.seq = seq; a.pos = pos; a.slot = slot;
+    a.mask = mask; a.st = st;
+    return run_kv_plan(a, ws, (cudaStream_t)stream);
+}
+
+aweq_status aweq_kv_accept(const aweq_kv_cache *cache, const int *page_table, long long n_seq, long long pages_per_seq,
+                           long long ld_table, const int *base, const int *path, long long ld_path, int max_path, const int *n_path,
+                           aweq_dev_status *st, void *stream)
+{
+    aweq_status rc = check_cache(cache, 256);
+    if (rc != AWEQ_OK) return rc;
+    const long long blocks = ((long long)cache->n_kv_heads * cache->head_dim / 4 + 127) / 128;
+    if (n_seq < 0 || n_seq > 0x7fffffffll / blocks || pages_per_seq <= 0 || pages_per_seq > 0x7fffffffll || max_path < 0) return AWEQ_ERR_SHAPE;
+    if (n_seq == 0 || max_path == 0) return AWEQ_OK;
+    if (!page_table || !base || !path || !n_path) return AWEQ_ERR_NULL;
+    if (ld_table < pages_per_seq || ld_path < max_path || !aligned(page_table, 4) || !aligned(base, 4) || !aligned(path, 4) || !aligned(n_path, 4))
+        return AWEQ_ERR_ALIGN;
+    KvAcceptArgs a = {};
     a.ck = reinterpret_cast<uint16_t *>(cache->k); a.cv = reinterpret_cast<uint16_t *>(cache->v);
     a.n_pages = cache->n_pages; a.page_stride = cache->page_stride; a.token_stride = cache->token_stride;
-    a.head_stride = cache->head_stride; a.page_size = cache->page_size; a.n_kv = cache->n_kv_heads;
-    a.head_dim = cache->head_dim; a.page_table = page_table; a.n_seq = n_seq; a.pages_per_seq = pages_per_seq;
-    a.ld_table = ld_table; a.k = reinterpret_cast<const uint16_t *>(k); a.v = reinterpret_cast<const uint16_t *>(v);
-    a.q = reinterpret_cast<const uint16_t *>(q); a.q_out = reinterpret_cast<uint16_t *>(q_out);
-    a.ldk = ldk; a.ldv = ldv; a.ldq = ldq; a.ld_qout = ld_qout; a.n_heads = q ? n_heads : 0; a.pos = pos; a.seq = seq;
-    a.first = first; a.n_tokens = n_tokens; a.rope = rope; a.n_pos = n_pos; a.rd = rope ? rotary_dim : 0;
-    a.interleaved = interleaved; a.st = st;
-    return run_kv_append(a, cache->dt, (cudaStream_t)stream);
+    a.head_stride = cache->head_stride; a.page_size = cache->page_size; a.n_kv = cache->n_kv_heads; a.head_dim = cache->head_dim;
+    a.max_path = max_path; a.page_table = page_table; a.base = base; a.path = path; a.n_path = n_path; a.n_seq = n_seq;
+    a.pages_per_seq = pages_per_seq; a.ld_table = ld_table; a.ld_path = ld_path; a.st = st;
+    return run_kv_accept(a, (cudaStream_t)stream);
 }
 
 static aweq_status check_attention(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq, int n_q,

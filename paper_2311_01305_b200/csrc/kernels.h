@@ -107,6 +107,7 @@ struct KvAppendArgs {
     long long ldk, ldv, ldq, ld_qout;
     int n_heads;                      // of q; 0 without q
     const int *pos, *seq;
+    const long long *slot;            // places given one by one, in the place of page_table and seq
     long long first, n_tokens;
     const float *rope;
     long long n_pos;
@@ -114,6 +115,32 @@ struct KvAppendArgs {
     aweq_dev_status *st;
 };
 aweq_status run_kv_append(const KvAppendArgs &a, aweq_dtype dt, cudaStream_t stream);
+
+constexpr int kPlanMaxWords = 4;
+struct KvPlanArgs {
+    int *page_table;
+    long long n_seq, pages_per_seq, ld_table;
+    int page_size, words;
+    int *ring;
+    long long *state, n_pages;
+    const int *held, *change, *parent;
+    long long first, max_tokens;
+    int *own_len, *start, *seq, *pos;
+    long long *slot, *mask;
+    aweq_dev_status *st;
+};
+size_t kv_plan_ws_bytes(long long n_seq);
+aweq_status run_kv_plan(const KvPlanArgs &a, void *ws, cudaStream_t stream);
+
+struct KvAcceptArgs {
+    uint16_t *ck, *cv;
+    long long n_pages, page_stride, token_stride, head_stride;
+    int page_size, n_kv, head_dim, max_path;
+    const int *page_table, *base, *path, *n_path;
+    long long n_seq, pages_per_seq, ld_table, ld_path;
+    aweq_dev_status *st;
+};
+aweq_status run_kv_accept(const KvAcceptArgs &a, cudaStream_t stream);
 
 struct AttentionArgs {
     const uint16_t *q, *ck, *cv;

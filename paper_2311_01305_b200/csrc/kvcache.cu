@@ -58,6 +58,20 @@ __device__ __forceinline__ AppendPlace append_place(const KvAppendArgs &a, long 
     w.pos = __ldg(a.pos + t);
     w.turn_ok = !a.rope || (w.pos >= 0 && w.pos < a.n_pos);
     w.at = -1;
+    if (a.slot) {
+        const long long slot = __ldg(a.slot + t);
+        if (slot < 0) {                                         // no token
+            w.turn_ok = false;
+            return w;
+        }
+        const bool out = !w.turn_ok || slot >= a.n_pages * a.page_size;
+        if (out && count && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+        if (!out) {
+            const long long page = slot >> 32 ? slot / a.page_size : (long long)((uint32_t)slot / (uint32_t)a.page_size);
+            w.at = page * a.page_stride + (slot - page * a.page_size) * a.token_stride;
+        }
+        return w;
+    }
     const long long s = a.seq ? __ldg(a.seq + t) : t, c = (long long)w.pos - a.first;
     bool bad = !w.turn_ok || s < 0 || s >= a.n_seq;
     if (!bad && c >= 0) {
