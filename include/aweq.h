@@ -592,6 +592,30 @@ aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_ca
                                   int n_heads, float scale, void *out, long long ldo, void *ws, size_t ws_bytes,
                                   aweq_dev_status *st, void *stream);
 
+/* Attention of drafted trees over the prefix the sequences share, each sequence's own keys and the trees themselves.  Sequence b
+ * brings the tokens (nodes) t = start[b] .. start[b+1] - 1; own_len[b] own keys lie where row b of page_table says, the last of
+ * which are the nodes' (appended before this call), as aweq_kv_plan and aweq_kv_append_slots leave them.
+ *   out[t, h] = sum_j p_j v_j,  p = softmax_j(scale q . k_j)
+ * over all prefix keys, all own keys before the nodes', and the key of the sequence's node j where bit j % 64 of
+ * mask[t, j / 64] is set (its own only if its bit is); head h reads key head h / (n_heads / n_kv_heads).  A key or value that a token does not
+ * see has no part in its output, whatever it is.  A row without keys gives zeros, one whose scores are all minus infinity NaN.
+ * Scores, running maximum, sum and output are binary32; the probabilities of prefix and own keys before the nodes' are rounded to the 16-bit
+ * type for the product with v, as in aweq_prefix_attention; one rounding at the end.
+ * q, out: 16-bit [max_tokens x n_heads * head_dim], row pitches ldq, ldo elements, 16-byte aligned, pitches multiples of 8; rows of out from
+ * start[n_seq] on stay as they were.  start: device int[n_seq + 1], ascending from 0; mask: device [max_tokens x words] 64-bit words,
+ * words >= ceil(max_nodes / 64).  max_nodes (to 256), max_own: HOST bounds on a sequence's nodes and own keys.
+ * Lengths and starts out of range are clamped, nodes beyond max_nodes are not computed, a page outside the pool is replaced by
+ * page 0; st->out_of_range counts each sequence with such a length or start, and each such entry of prefix_pages and page_table that holds
+ * keys, once.  max_tokens * n_heads at most 2^31 - 1.
+ * ws: aweq_tree_attention_workspace_bytes(...) bytes, 256-byte aligned. */
+size_t aweq_tree_attention_workspace_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq,
+                                           long long max_tokens, int max_nodes, int n_heads);
+aweq_status aweq_tree_attention(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages,
+                                long long prefix_len, const int *page_table, long long pages_per_seq, long long ld_table,
+                                const int *own_len, const int *start, const long long *mask, int words, long long max_own,
+                                long long n_seq, long long max_tokens, int max_nodes, int n_heads, float scale, void *out,
+                                long long ldo, void *ws, size_t ws_bytes, aweq_dev_status *st, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

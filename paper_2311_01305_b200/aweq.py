@@ -142,6 +142,11 @@ _lib.aweq_prefix_attention_workspace_bytes.restype = _sz
 _lib.aweq_prefix_attention.argtypes = [_vp, _ll, ctypes.POINTER(KvCacheArgs), _vp, _ll, _vp, _ll, _ll, _vp, _ll, _ll, _i, _i,
                                        ctypes.c_float, _vp, _ll, _vp, _sz, _vp, _vp]
 _lib.aweq_prefix_attention.restype = _i
+_lib.aweq_tree_attention_workspace_bytes.argtypes = [ctypes.POINTER(KvCacheArgs), _ll, _ll, _ll, _ll, _i, _i]
+_lib.aweq_tree_attention_workspace_bytes.restype = _sz
+_lib.aweq_tree_attention.argtypes = [_vp, _ll, ctypes.POINTER(KvCacheArgs), _vp, _ll, _vp, _ll, _ll, _vp, _vp, _vp, _i, _ll, _ll, _ll, _i,
+                                     _i, ctypes.c_float, _vp, _ll, _vp, _sz, _vp, _vp]
+_lib.aweq_tree_attention.restype = _i
 for _f in ("aweq_stats", "aweq_wrange", "aweq_factors", "aweq_equalize_quantize", "aweq_bias_correct",
            "aweq_quant_act", "aweq_layer_pass", "aweq_forward_check"):
     getattr(_lib, _f).restype = _i
@@ -876,3 +881,54 @@ class PrefixAttention:
         if rc:
             raise AweqError(rc)
         return out
+
+
+def aweq_tree_attention_workspace_bytes(cache, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads) -> int:
+    return int(_lib.aweq_tree_attention_workspace_bytes(cache.ref, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads))
+
+
+def aweq_tree_attention(q, cache, prefix_pages, prefix_len, page_table, own_len, start, mask, max_own, max_nodes, scale, out, ws, st=None):
+    """Attention of drafted trees over a shared prefix, each sequence's own keys and the trees (argument marshalling only; see
+    ``include/aweq.h``).  ``TreeAttention`` holds the scratch of one batch shape."""
+    return TreeAttention._call(q, page_table, own_len, start, mask, out, cache, prefix_pages, prefix_len, own_len.numel(), q.shape[0], max_nodes,
+                               q.shape[1] if q.dim() == 3 else q.shape[1] // cache.head_dim, max_own, scale, ws, st)
+
+
+class TreeAttention:
+    """``aweq_tree_attention`` for one batch shape: up to ``max_nodes`` tokens of each of ``n_seq`` sequences, ``max_tokens`` rows in
+    all.  Holds the prefix's page list and the scratch; one object serves one stream at a time (its calls share the scratch)."""
+
+    def __init__(self, cache, prefix_pages, prefix_len, n_heads, n_seq, max_tokens, max_nodes, max_own=None, scale=None):
+        self.cache, self.prefix_pages, self.prefix_len = cache, prefix_pages, int(prefix_len)
+        self.n_heads, self.n_seq, self.max_tokens, self.max_nodes = n_heads, n_seq, max_tokens, max_nodes
+        self.max_own = 0x7fffffff if max_own is None else int(max_own)
+        self.scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+        if self.prefix_len:
+            _want(prefix_pages, torch.int32, -(-self.prefix_len // cache.page_size), "prefix_pages")
+        self.ws = workspace(aweq_tree_attention_workspace_bytes(cache, self.prefix_len, self.max_own, n_seq, max_tokens, max_nodes, n_heads),
+                            cache.k.device)
+
+    @staticmethod
+    def _call(q, page_table, own_len, start, mask, out, cache, prefix_pages, prefix_len, n_seq, n, max_nodes, h, max_own, scale, ws, st):
+        ldq, ldo = _heads(q, n, h, cache.head_dim, cache.dtype, "q"), _heads(out, n, h, cache.head_dim, cache.dtype, "out")
+        pages, rows, per_seq, ld_table = _int32_table(page_table, "page_table")
+        if rows != n_seq:
+            raise ValueError("page_table has a row per sequence")
+        if mask.dtype is not torch.int64 or mask.dim() != 2 or mask.shape[0] != n or not mask.is_contiguous() or not mask.is_cuda:
+            raise ValueError("mask must be a contiguous int64 device matrix with a row for each of %d tokens" % n)
+        if prefix_len:
+            _want(prefix_pages, torch.int32, -(-prefix_len // cache.page_size), "prefix_pages")
+        rc = _lib.aweq_tree_attention(q.data_ptr(), ldq, cache.ref, _ptr(prefix_pages) if prefix_len else None, prefix_len, pages, per_seq, ld_table,
+                                      _int32_rows(own_len, n_seq, "own_len"), _int32_rows(start, n_seq + 1, "start"), mask.data_ptr(),
+                                      mask.shape[1], max_own, n_seq, n, max_nodes, h, scale, out.data_ptr(), ldo, ws.data_ptr(), ws.numel(),
+                                      _ptr(st), _stream())
+        if rc:
+            raise AweqError(rc)
+        return out
+
+    def __call__(self, q, page_table, own_len, start, mask, out=None, st=None):
+        """``q``, ``out``: [max_tokens, n_heads, head_dim]; ``start``: the sequences' first rows and the number of all; ``mask``: a
+        row of 64-bit words for every token, bit j for its sequence's node j."""
+        out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
+        return self._call(q, page_table, own_len, start, mask, out, self.cache, self.prefix_pages, self.prefix_len, self.n_seq, self.max_tokens,
+                          self.max_nodes, self.n_heads, self.max_own, self.scale, self.ws, st)

@@ -90,7 +90,7 @@ def _build_locked(force: bool, verbose: bool) -> str:
         deps = [src, os.path.abspath(__file__)]
         for h in headers:
             name = os.path.basename(h)
-            if name in ("common.cuh", "kernels.h", "aweq.h", "tensorcore.cuh", "attention.cuh") or ('"%s"' % name) in text:
+            if name in ("common.cuh", "kernels.h", "aweq.h", "tensorcore.cuh", "attention.cuh", "mx4.cuh") or ('"%s"' % name) in text:
                 deps.append(h)
         return os.path.getmtime(obj) < _newest(deps)
     todo = [(s, o) for s, o in zip(srcs, objs) if stale(s, o)]

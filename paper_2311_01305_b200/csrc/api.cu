@@ -810,4 +810,54 @@ aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_ca
     return run_prefix_attention(a, cache, ws, (cudaStream_t)stream);
 }
 
+static aweq_status check_tree(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq, long long max_tokens,
+                              int max_nodes, int n_heads)
+{
+    aweq_status rc = check_cache(cache, 128);
+    if (rc != AWEQ_OK) return rc;
+    if (prefix_len < 0 || prefix_len > 0x7fffffffll || max_own < 0 || max_own > 0x7fffffffll || n_seq < 0 || n_seq > (1ll << 24) || max_tokens < 0 ||
+        max_tokens > 0x7fffffffll || max_nodes <= 0 || max_nodes > 64 * kPlanMaxWords || n_heads <= 0 || n_heads % cache->n_kv_heads || n_heads > 65536)
+        return AWEQ_ERR_SHAPE;
+    if ((double)max_tokens * n_heads > 2147483647.0 || (double)n_seq * 64 * kPlanMaxWords * n_heads > 2e12) return AWEQ_ERR_SHAPE;
+    return AWEQ_OK;
+}
+
+size_t aweq_tree_attention_workspace_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq,
+                                           long long max_tokens, int max_nodes, int n_heads)
+{
+    if (check_tree(cache, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads) != AWEQ_OK || n_seq == 0 || max_tokens == 0) return 0;
+    return tree_attention_ws_bytes(cache, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads);
+}
+
+aweq_status aweq_tree_attention(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages, long long prefix_len,
+                                const int *page_table, long long pages_per_seq, long long ld_table, const int *own_len, const int *start,
+                                const long long *mask, int words, long long max_own, long long n_seq, long long max_tokens, int max_nodes,
+                                int n_heads, float scale, void *out, long long ldo, void *ws, size_t ws_bytes, aweq_dev_status *st,
+                                void *stream)
+{
+    aweq_status rc = check_tree(cache, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads);
+    if (rc != AWEQ_OK) return rc;
+    if (pages_per_seq <= 0 || pages_per_seq > 0x7fffffffll || words < (max_nodes + 63) / 64 || words > kPlanMaxWords) return AWEQ_ERR_SHAPE;
+    if (n_seq == 0 || max_tokens == 0) return AWEQ_OK;
+    if (!q || !out || !own_len || !start || !mask || !page_table || (prefix_len && !prefix_pages)) return AWEQ_ERR_NULL;
+    const long long row = (long long)n_heads * cache->head_dim;
+    if (!aligned(q, 16) || !aligned(out, 16) || ldq < row || ldo < row || ldq % 8 || ldo % 8 || ld_table < pages_per_seq ||
+        !aligned(prefix_pages, 4) || !aligned(page_table, 4) || !aligned(own_len, 4) || !aligned(start, 4) || !aligned(mask, 8))
+        return AWEQ_ERR_ALIGN;
+    rc = check_ws(ws, ws_bytes, tree_attention_ws_bytes(cache, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads));
+    if (rc != AWEQ_OK) return rc;
+    AWEQ_LOGF("aweq_tree_attention seqs=%lld tokens=%lld heads=%d kv_heads=%d head_dim=%d prefix=%lld max_own=%lld\n", n_seq, max_tokens, n_heads,
+              cache->n_kv_heads, cache->head_dim, prefix_len, max_own);
+    TreeArgs a = {};
+    a.q = reinterpret_cast<const uint16_t *>(q); a.ck = reinterpret_cast<const uint16_t *>(cache->k);
+    a.cv = reinterpret_cast<const uint16_t *>(cache->v); a.out = reinterpret_cast<uint16_t *>(out);
+    a.ldq = ldq; a.ldo = ldo; a.n_pages = cache->n_pages; a.page_stride = cache->page_stride;
+    a.token_stride = cache->token_stride; a.head_stride = cache->head_stride; a.page_size = cache->page_size;
+    a.n_kv = cache->n_kv_heads; a.head_dim = cache->head_dim; a.n_heads = n_heads; a.words = words; a.max_nodes = max_nodes;
+    a.max_tokens = (int)max_tokens; a.n_seq = (int)n_seq; a.prefix_pages = prefix_pages; a.page_table = page_table;
+    a.own_len = own_len; a.start = start; a.mask = mask; a.prefix_len = prefix_len; a.pages_per_seq = pages_per_seq;
+    a.ld_table = ld_table; a.max_own = max_own; a.scale = scale; a.st = st;
+    return run_tree_attention(a, cache, ws, (cudaStream_t)stream);
+}
+
 }  // extern "C"

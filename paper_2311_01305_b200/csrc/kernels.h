@@ -152,6 +152,21 @@ struct AttentionArgs {
     float scale;
     aweq_dev_status *st;
 };
+struct TreeArgs {
+    const uint16_t *q, *ck, *cv;
+    uint16_t *out;
+    long long ldq, ldo, n_pages, page_stride, token_stride, head_stride;
+    int page_size, n_kv, head_dim, n_heads, words, max_nodes, max_tokens, n_seq;
+    const int *prefix_pages, *page_table, *own_len, *start;
+    const long long *mask;
+    long long prefix_len, pages_per_seq, ld_table, max_own;
+    float scale;
+    aweq_dev_status *st;
+};
+size_t tree_attention_ws_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq, long long max_tokens,
+                               int max_nodes, int n_heads);
+aweq_status run_tree_attention(const TreeArgs &a, const aweq_kv_cache *cache, void *ws, cudaStream_t stream);
+
 size_t prefix_attention_ws_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq, int n_q,
                                  int n_heads);
 aweq_status run_prefix_attention(const AttentionArgs &a, const aweq_kv_cache *cache, void *ws, cudaStream_t stream);

@@ -1,0 +1,175 @@
+// Shared pieces of the attention of drafted trees (tree.cu has the overview): how the work is cut and walked.
+#pragma once
+#include <math_constants.h>
+
+#include "attention.cuh"
+#include "common.cuh"
+#include "kernels.h"
+
+namespace aweq {
+
+struct TreePlan {
+    int two;                     // 1: an item has two tiles of 128 rows on the same keys; 0: one, whose units alternate between two sums
+    int rows;                    // rows of an item: 256 or 128
+    int unit, box;               // keys of a unit, of one tiled copy (0: 16-byte copies)
+    int ctas, pre_rt, pre_tiles; // grid; most row tiles of the prefix; units of a prefix item
+    int pre_rec, own_rec;        // rows of a record, of one sum each
+    // scratch: per sequence the first own unit and item (TreeFirst[n_seq]), the totals; records
+    size_t off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
+};
+struct TreeFirst { long long unit; int item, tiles; };
+struct TreeTotals { long long pre, own; int tokens, pad; };
+
+// A sequence's new tokens and the keys before them, clamped.
+struct TreeSeq { int t0, nodes, ctx, base; bool bad; };      // base: key of node 0
+__device__ __forceinline__ TreeSeq tree_seq(const TreeArgs &a, int s0, int s1, int len)
+{
+    const int cap = (int)min(a.max_own, a.pages_per_seq * a.page_size);
+    TreeSeq s;
+    s.t0 = min(max(s0, 0), a.max_tokens);
+    const int t1 = min(max(s1, s.t0), a.max_tokens), l = min(max(len, 0), cap);
+    s.nodes = min(t1 - s.t0, a.max_nodes);
+    s.base = l - s.nodes;
+    s.ctx = max(s.base, 0);
+    s.bad = s.t0 != s0 || t1 != s1 || s.nodes != t1 - s.t0 || l != len || l < s.nodes;
+    return s;
+}
+__device__ __forceinline__ TreeSeq tree_load(const TreeArgs &a, int b)
+{
+    return b < a.n_seq ? tree_seq(a, __ldg(a.start + b), __ldg(a.start + b + 1), __ldg(a.own_len + b)) : TreeSeq{0, 0, 0, 0, false};
+}
+__device__ __forceinline__ int tree_tokens(const TreeArgs &a) { return min(max(__ldg(a.start + a.n_seq), 0), a.max_tokens); }
+__device__ __forceinline__ int tree_tiles(int n, int of) { return (int)(((unsigned)n + (unsigned)of - 1) / (unsigned)of); }
+
+// own units and items of 32 sequences: the lane's, and those before it
+struct TreeScan { long long units, unit0; int items, item0; };
+__device__ __forceinline__ TreeScan tree_scan(const TreeArgs &a, const TreePlan &p, const TreeSeq &s)
+{
+    const int lane = threadIdx.x & 31, G = a.n_heads / a.n_kv;
+    TreeScan r;
+    r.items = a.n_kv * tree_tiles(s.nodes * G, p.rows);
+    r.units = (long long)r.items * tree_tiles(s.ctx, p.unit);
+    long long u = r.units;
+    int i = r.items;
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, u, x);
+        const int w = __shfl_up_sync(0xffffffffu, i, x);
+        if (lane >= x) { u += v; i += w; }
+    }
+    r.unit0 = u - r.units;
+    r.item0 = i - r.items;
+    return r;
+}
+// All units; every warp computes them.  `lead`: the one warp that counts what is out of range and leaves the sequences' firsts.
+__device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreePlan &p, unsigned char *ws, bool lead)
+{
+    const int lane = threadIdx.x & 31;
+    TreeTotals t = {0, 0, tree_tokens(a), 0};
+    t.pre = (long long)a.n_kv * tree_tiles(t.tokens * (a.n_heads / a.n_kv), p.rows) * p.pre_tiles;
+    int items = 0;
+    for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
+        const TreeSeq s = tree_load(a, b0 + lane);
+        const TreeScan c = tree_scan(a, p, s);
+        if (lead && b0 + lane < a.n_seq) {
+            reinterpret_cast<TreeFirst *>(ws)[b0 + lane] = {t.own + c.unit0, items + c.item0, tree_tiles(s.ctx, p.unit)};
+            if (s.bad && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+        }
+        t.own += __shfl_sync(0xffffffffu, c.unit0 + c.units, 31);
+        items += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
+    }
+    return t;
+}
+
+// The walk over a CTA's units by a warp (every lane knows the unit): prefix items first, then each sequence's, tiles of keys
+// inside row tiles inside key heads.
+struct TreeWalk {
+    int own, b, kh, rt, tile, tiles, n_rt, len, t0, n_tok, item;     // len: keys of the segment; t0, n_tok: the tokens whose rows they are
+    __device__ __forceinline__ void enter(const TreeArgs &a, const TreePlan &p, int to)        // the next sequence with units
+    {
+        own = 1;
+        for (int b0 = to;; b0 += 32) {
+            const TreeSeq s = tree_load(a, b0 + (int)(threadIdx.x & 31));
+            const TreeScan c = tree_scan(a, p, s);
+            const uint32_t here = __ballot_sync(0xffffffffu, c.units > 0);
+            if (here || b0 + 32 >= a.n_seq) {
+                const int src = here ? __ffs(here) - 1 : 0;
+                b = b0 + src;
+                t0 = __shfl_sync(0xffffffffu, s.t0, src);
+                n_tok = __shfl_sync(0xffffffffu, s.nodes, src);
+                len = __shfl_sync(0xffffffffu, s.ctx, src);
+                item += __shfl_sync(0xffffffffu, c.item0, src);
+                tiles = tree_tiles(len, p.unit);
+                n_rt = tree_tiles(n_tok * (a.n_heads / a.n_kv), p.rows);
+                return;
+            }
+            item += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
+        }
+    }
+    __device__ __forceinline__ void begin(const TreeArgs &a, const TreePlan &p, const TreeTotals &t, long long u0)
+    {
+        own = b = kh = rt = tile = tiles = n_rt = len = t0 = n_tok = item = 0;
+        const int lane = threadIdx.x & 31;
+        if (u0 < t.pre) {
+            tiles = p.pre_tiles;
+            len = (int)a.prefix_len;
+            n_tok = t.tokens;
+            n_rt = tree_tiles(n_tok * (a.n_heads / a.n_kv), p.rows);
+            item = (int)(u0 / tiles);
+            tile = (int)(u0 - (long long)item * tiles);
+            kh = item / n_rt;
+            rt = item - kh * n_rt;
+            return;
+        }
+        const long long u = u0 - t.pre;
+        long long passed = 0;
+        int items = 0;
+        for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
+            const TreeSeq s = tree_load(a, b0 + lane);
+            const TreeScan c = tree_scan(a, p, s);
+            const uint32_t here = __ballot_sync(0xffffffffu, u >= passed + c.unit0 && u < passed + c.unit0 + c.units);
+            if (here) {
+                const int src = __ffs(here) - 1;
+                own = 1;
+                b = b0 + src;
+                const long long within = u - passed - __shfl_sync(0xffffffffu, c.unit0, src);
+                t0 = __shfl_sync(0xffffffffu, s.t0, src);
+                n_tok = __shfl_sync(0xffffffffu, s.nodes, src);
+                len = __shfl_sync(0xffffffffu, s.ctx, src);
+                tiles = tree_tiles(len, p.unit);
+                n_rt = tree_tiles(n_tok * (a.n_heads / a.n_kv), p.rows);
+                const int i = (int)(within / tiles);
+                tile = (int)(within - (long long)i * tiles);
+                kh = i / n_rt;
+                rt = i - kh * n_rt;
+                item = items + __shfl_sync(0xffffffffu, c.item0, src) + i;
+                return;
+            }
+            passed += __shfl_sync(0xffffffffu, c.unit0 + c.units, 31);
+            items += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
+        }
+    }
+    __device__ __forceinline__ void advance(const TreeArgs &a, const TreePlan &p)
+    {
+        if (++tile < tiles) return;
+        tile = 0;
+        ++item;
+        if (++rt < n_rt) return;
+        rt = 0;
+        if (++kh < a.n_kv) return;
+        kh = 0;
+        if (!own) item = 0;
+        enter(a, p, own ? b + 1 : 0);
+    }
+    __device__ __forceinline__ int keys(const TreePlan &p) const { return min(p.unit, len - tile * p.unit); }
+    __device__ __forceinline__ int rows(const TreeArgs &a, const TreePlan &p) const { return min(p.rows, n_tok * (a.n_heads / a.n_kv) - rt * p.rows); }
+    // entry of the page list for the unit's r'th key, if there is such a key
+    __device__ __forceinline__ int entry(const TreeArgs &a, const TreePlan &p, int r) const
+    {
+        const int key = tile * p.unit + r;
+        if (key >= len) return 0;
+        return __ldg((own ? a.page_table + (long long)b * a.ld_table : a.prefix_pages) + (unsigned)key / (unsigned)a.page_size);
+    }
+};
+
+}  // namespace aweq
