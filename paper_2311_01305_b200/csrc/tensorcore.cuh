@@ -20,6 +20,9 @@ inline bool tma_pool_fits(long long page_stride, long long token_stride, long lo
 }
 // `tiles` tiles of 512 bytes in a row, read `box` at a time into consecutive shared memory
 aweq_status tma_tiles_map(CUtensorMap *map, const void *base, long long tiles, int box);
+// 16-bit rows [tokens x heads x dim], pitch ld elements (heads side by side), read in boxes of box_tokens tokens x box_heads heads x
+// 64 elements, swizzled by 128 bytes; elements past dim and tokens past the last read as zero
+aweq_status tma_heads_map(CUtensorMap *map, const void *base, long long tokens, int heads, int dim, long long ld, int box_heads, int box_tokens);
 aweq_status tma_pool_map(CUtensorMap *map, const void *base, long long pages, int tokens, int heads, int dim, long long page_stride,
                          long long token_stride, long long head_stride, int box_tokens);
 
@@ -221,6 +224,12 @@ __device__ __forceinline__ void tc_st16(uint32_t tmem, const uint32_t *r)
           "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(tmem) : "memory");
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 3-D box global -> shared memory of this CTA
+__device__ __forceinline__ void tma_load3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
 // 4-D box global -> shared memory of this CTA
 __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar)
 {

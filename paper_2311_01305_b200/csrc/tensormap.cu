@@ -41,6 +41,13 @@ aweq_status tma_tiles_map(CUtensorMap *map, const void *base, long long tiles, i
     return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, base, dims, pitch, box, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
+aweq_status tma_heads_map(CUtensorMap *map, const void *base, long long tokens, int heads, int dim, long long ld, int box_heads, int box_tokens)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)tokens}, strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)ld * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+    return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, base, dims, strides, box);
+}
+
 aweq_status tma_pool_map(CUtensorMap *map, const void *base, long long pages, int tokens, int heads, int dim, long long page_stride,
                          long long token_stride, long long head_stride, int box_tokens)
 {

@@ -12,19 +12,24 @@
 // the same keys where a sequence has more than 128 rows to a key head, else the same rows on every other unit of keys.
 // A unit is 128 keys (or the whole pages that fit).  The units of all (segment, key head, row tile) items in a row are dealt out evenly
 // to a CTA per SM; where a CTA leaves an item it writes a record (m, sum, O of the keys it has seen) for each row and sum.
-// Warps: 0 copies keys and values, 1 issues the products, 2 and 3 bring the rows of Q, 4-7 and 8-11 the softmax of the two sums.
+// Warps: 0 copies keys and values, 1 issues the products, 2 brings the rows of Q, 3 says which items come, 4-7 and 8-11 the
+// softmax of the two sums.
+#include <type_traits>
+
 #include "tree.cuh"
 #include "tensorcore.cuh"
 
 namespace aweq {
 
-constexpr int kTrThreads = 384, kTrQBytes = 64 * 1024, kTrRing = 160 * 1024, kTrMaxTiles = 10;
+constexpr int kTrThreads = 384, kTrQBytes = 64 * 1024, kTrRing = 160 * 1024, kTrMaxTiles = 10, kTrItems = 4;
 // registers of a softmax thread and of the others: together no more than the launch gives
 constexpr int kTrSoftRegs = 208, kTrOtherRegs = 80;
 constexpr float kTrSlack = 8.0f;
 
 struct TreeShared {
     uint64_t full[kTrMaxTiles], empty[kTrMaxTiles], q_ready[2], q_free[2], s_full[2], p_ready[2], pv_done[2], o_free[2];
+    uint64_t item_full[kTrItems], item_empty[kTrItems];
+    TreeItem item[kTrItems];
     uint32_t tmem;
 };
 constexpr size_t kTrSmem = 1024 + kTrQBytes + kTrRing + sizeof(TreeShared);
@@ -38,7 +43,9 @@ static TreePlan tree_plan(const aweq_kv_cache *c, long long prefix_len, long lon
     const int G = n_heads / c->n_kv_heads;
     const long long own_rows = (long long)(max_nodes < max_tokens ? max_nodes : max_tokens) * G, pre_rows = max_tokens * G;
     p.two = own_rows > 128;
-    p.rows = p.two ? 256 : 128;
+    p.group = G;
+    p.part = G <= 128 ? 128 / G * G : 128;
+    p.rows = p.two ? 2 * p.part : p.part;
     // tiled copies of `box` keys that lie in one page (rows a multiple of eight keep the swizzle's phase)
     p.box = 0;
     if (c->page_size % 8 == 0 && tma_pool_fits(c->page_stride, c->token_stride, c->head_stride)) {
@@ -79,23 +86,41 @@ size_t tree_attention_ws_bytes(const aweq_kv_cache *cache, long long prefix_len,
     return tree_plan(cache, prefix_len, n_seq, max_tokens, max_nodes, n_heads).total;
 }
 
+// Where row `row` of all records has its dims d, d + 1, ..., d + 7 (d a multiple of eight): a record of n rows is [dims / 8][n][8].
+__device__ __forceinline__ long long tree_record(const TreePlan &p, bool own, long long row, int d, int hd)
+{
+    const int n = own ? p.own_rec : p.pre_rec;
+    const long long rec = row >> 32 ? row / n : (long long)((uint32_t)row / (uint32_t)n), in = row - rec * n;
+    return rec * n * hd + (long long)(d >> 3) * n * 8 + in * 8;
+}
 __device__ __forceinline__ AttentionDeal tree_deal(const TreePlan &p, const TreeTotals &t) { return AttentionDeal(t.pre + t.own, p.ctas); }
 
-// A step of one of the two sums: a unit of keys on a row tile.
-struct TreeStep {
-    int live, fresh, keys;       // rows there; first of its item for this sum in this CTA
+// The items of a CTA in turn, by a warp that works on them.
+struct TreeItems {
+    int n = 0;
+    __device__ __forceinline__ bool next(TreeShared &sh, TreeItem &it)
+    {
+        const int i = n & (kTrItems - 1);
+        const bool ok = __all_sync(0xffffffffu, mbar_wait(&sh.item_full[i], (n / kTrItems) & 1));
+        if (ok) it = sh.item[i];
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.item_empty[i]);
+        ++n;
+        return ok;
+    }
 };
 
-template <class D>
+template <class D, bool TWO>
 __global__ void __launch_bounds__(kTrThreads, 1)
 tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
-                  unsigned char *ws)
+                  const __grid_constant__ CUtensorMap mapQ, unsigned char *ws)
 {
     extern __shared__ unsigned char raw[];
     unsigned char *const qs = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     unsigned char *const tiles = qs + kTrQBytes;
     TreeShared &sh = *reinterpret_cast<TreeShared *>(tiles + kTrRing);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, hd = a.head_dim;
+    // (the warp's number by a shuffle, so that the compiler knows that a warp has one: the products' operands live in uniform registers)
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), cta = blockIdx.x, hd = a.head_dim;
     const int halves = hd > 64 ? 2 : 1, tile_bytes = halves * 16384, n_tiles = kTrRing / tile_bytes;
     if (tid == 0) {
         for (int i = 0; i < n_tiles; ++i) {
@@ -103,65 +128,119 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             mbar_init(&sh.empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sh.q_ready[i], 2);
+            mbar_init(&sh.q_ready[i], 1);
             mbar_init(&sh.q_free[i], 1);
             mbar_init(&sh.s_full[i], 1);
             mbar_init(&sh.p_ready[i], 4);
             mbar_init(&sh.pv_done[i], 1);
             mbar_init(&sh.o_free[i], 4);
         }
+        for (int i = 0; i < kTrItems; ++i) {
+            mbar_init(&sh.item_full[i], 1);
+            mbar_init(&sh.item_empty[i], 11);
+        }
         mbar_init_fence();
         if (p.box) {
             tma_prefetch_map(&mapK);
             tma_prefetch_map(&mapV);
         }
+        if (p.group <= 128) tma_prefetch_map(&mapQ);
     }
     if (warp == 1) tc_alloc<1>(&sh.tmem, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const TreeTotals totals = tree_totals(a, p, ws, cta == 0 && warp == 0);
-    if (cta == 0 && tid == 0) *reinterpret_cast<TreeTotals *>(ws + (size_t)a.n_seq * sizeof(TreeFirst)) = totals;
-    const AttentionDeal deal = tree_deal(p, totals);
-    const long long u0 = cta < deal.ctas ? deal.first(cta) : 0;
-    const int units = cta < deal.ctas ? (int)(deal.first(cta + 1) - u0) : 0;
-    TreeWalk w;
-    if (units) w.begin(a, p, totals, u0);
 
     bool ok = true;
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTrOtherRegs));
-        if (warp == 0) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (warp == 3) {
+            // ---------------------------------------------------------- the CTA's items, a few ahead of those who work on them
+            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+            TreeSeq s0 = {};
+            TreeScan c0 = {};
+            const TreeTotals totals = tree_totals(a, p, ws, cta == 0, s0, c0);
+            if (cta == 0 && lane == 0) *reinterpret_cast<TreeTotals *>(ws + (size_t)a.n_seq * sizeof(TreeFirst)) = totals;
+            const AttentionDeal deal = tree_deal(p, totals);
+            long long u0 = 0;
+            int left = 0;
+            TreeWalk w;
+            if (cta < deal.ctas) {
+                u0 = deal.first(cta);
+                left = (int)(deal.first(cta + 1) - u0);
+                w.begin(a, p, totals, u0, s0, c0);
+            }
+            for (int n = 0;; ++n) {
+                const int i = n & (kTrItems - 1);
+                TreeItem it = {};
+                it.stop = 1;
+                if (left) {
+                    const int rec = w.own ? p.own_rec : p.pre_rec;
+                    it.own = w.own;
+                    it.b = w.b;
+                    it.kh = w.kh;
+                    it.rt = w.rt;
+                    it.tile = w.tile;
+                    it.count = min(w.tiles - w.tile, left);
+                    it.len = w.len;
+                    it.rows = w.rows(p);
+                    it.t0 = w.t0;
+                    it.rec = (long long)(w.item + cta) * (TWO ? rec : 2 * rec);
+                    left -= it.count;
+                    it.stop = left == 0;
+                }
+                ok = __all_sync(0xffffffffu, mbar_wait(&sh.item_empty[i], ((n / kTrItems) & 1) ^ 1));
+                if (!ok) break;
+                if (lane == 0) {
+                    sh.item[i] = it;
+                    mbar_arrive(&sh.item_full[i]);
+                }
+                __syncwarp();
+                if (it.stop) break;
+                w.next_item(a, p);
+            }
+        } else if (warp == 0) {
             // ---------------------------------------------------------- copies: a unit's keys, then its values
-            int s = 0;
+            TreeItems items;
+            TreeItem it, next;
+            ok = items.next(sh, it);
+            int s = 0, tile = it.tile, left = it.count;
             uint32_t ph = 0;
+            auto entry = [&](const TreeItem &x, int t, int r) {     // entry of the page list for the unit's r'th key, if there is such a key
+                const int key = t * p.unit + r;
+                if (key >= x.len) return 0;
+                return __ldg((x.own ? a.page_table + (long long)x.b * a.ld_table : a.prefix_pages) + (unsigned)key / (unsigned)a.page_size);
+            };
             if (p.box) {
-                const int boxes = p.unit / p.box;
-                int page = units && lane < boxes ? w.entry(a, p, lane * p.box) : 0;
-                for (int left = units; left > 0; --left) {
-                    const int keys = w.keys(p), kh = w.kh, row = (unsigned)(w.tile * p.unit + lane * p.box) % (unsigned)a.page_size;
-                    const bool there = lane < boxes && lane * p.box < keys, bad = there && (page < 0 || page >= a.n_pages);
+                const int boxes = p.unit / p.box, at = lane * p.box;
+                int page = ok && left && lane < boxes ? entry(it, tile, at) : 0;
+                while (ok && left > 0) {
+                    const int keys = min(p.unit, it.len - tile * p.unit), kh = it.kh, row = (unsigned)(tile * p.unit + at) % (unsigned)a.page_size;
+                    const bool there = lane < boxes && at < keys, bad = there && (page < 0 || page >= a.n_pages);
                     const int pid = bad ? 0 : page, n = __popc(__ballot_sync(0xffffffffu, there));
-                    if (bad && (w.kh | w.rt | row) == 0 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
-                    if (left > 1) {
-                        w.advance(a, p);
-                        page = lane < boxes ? w.entry(a, p, lane * p.box) : 0;      // the next unit's, while these stages empty
+                    if (bad && (kh | it.rt | row) == 0 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+                    // the next unit's page, while these stages empty
+                    ++tile;
+                    if (--left == 0 && !it.stop) {
+                        if (!(ok = items.next(sh, next))) break;
+                        it = next;
+                        tile = it.tile;
+                        left = it.count;
                     }
+                    if (left) page = lane < boxes ? entry(it, tile, at) : 0;
+#pragma unroll 1
                     for (int v = 0; v < 2; ++v) {
-                        ok = mbar_wait(&sh.empty[s], ph ^ 1);
-                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        ok = __all_sync(0xffffffffu, mbar_wait(&sh.empty[s], ph ^ 1));
+                        if (!ok) break;
                         if (lane == 0) mbar_arrive_expect_tx(&sh.full[s], (uint32_t)(n * p.box * 128 * halves));
                         __syncwarp();
                         if (there)
                             for (int h = 0; h < halves; ++h)
-                                tma_load4(smem_u32(tiles + s * tile_bytes + h * 16384) + lane * p.box * 128, v ? &mapV : &mapK, h * 64, kh, row, pid,
-                                          smem_u32(&sh.full[s]));
+                                tma_load4(smem_u32(tiles + s * tile_bytes + h * 16384) + at * 128, v ? &mapV : &mapK, h * 64, kh, row, pid, smem_u32(&sh.full[s]));
                         if (++s == n_tiles) { s = 0; ph ^= 1; }
                     }
-                    if (!ok) break;
                 }
             } else {
                 // pages and strides that tiled copies do not serve: 16 bytes at a time, a tile's under way while the one before lands
@@ -172,27 +251,34 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.full[stage]);
                 };
-                for (int left = units; left > 0; --left) {
-                    const int keys = w.keys(p);
+                while (ok && left > 0) {
+                    const int keys = min(p.unit, it.len - tile * p.unit);
                     long long off[4];                           // element of the pool of keys lane, lane + 32, ...; -1: none
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = i * 32 + lane;
-                        const int page = w.entry(a, p, r);
-                        const unsigned row = (unsigned)(w.tile * p.unit + r) % (unsigned)a.page_size;
+                        const int page = entry(it, tile, r);
+                        const unsigned row = (unsigned)(tile * p.unit + r) % (unsigned)a.page_size;
                         const bool bad = r < keys && (page < 0 || page >= a.n_pages);
-                        if (bad && (w.kh | w.rt) == 0 && (row == 0) && a.st) atomicAdd(&a.st->out_of_range, 1ull);
-                        off[i] = r < keys ? (long long)(bad ? 0 : page) * a.page_stride + (long long)row * a.token_stride + w.kh * a.head_stride : -1;
+                        if (bad && (it.kh | it.rt) == 0 && row == 0 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+                        off[i] = r < keys ? (long long)(bad ? 0 : page) * a.page_stride + (long long)row * a.token_stride + it.kh * a.head_stride : -1;
                     }
-                    if (left > 1) w.advance(a, p);
+                    ++tile;
+                    if (--left == 0 && !it.stop) {
+                        if (!(ok = items.next(sh, next))) break;
+                        it = next;
+                        tile = it.tile;
+                        left = it.count;
+                    }
+#pragma unroll 1
                     for (int v = 0; v < 2; ++v) {
                         if (pending >= 0 && !__all_sync(0xffffffffu, mbar_try_wait(&sh.empty[s], ph ^ 1))) {
                             asm volatile("cp.async.wait_group 0;" ::: "memory");
                             landed(pending);
                             pending = -1;
                         }
-                        ok = mbar_wait(&sh.empty[s], ph ^ 1);
-                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        ok = __all_sync(0xffffffffu, mbar_wait(&sh.empty[s], ph ^ 1));
+                        if (!ok) break;
                         const uint16_t *const pool = v ? a.cv : a.ck;
                         const uint32_t dst = smem_u32(tiles + s * tile_bytes);
 #pragma unroll
@@ -211,259 +297,334 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                         pending = s;
                         if (++s == n_tiles) { s = 0; ph ^= 1; }
                     }
-                    if (!ok) break;
                 }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
                 if (pending >= 0) landed(pending);
             }
             if (!ok)                                            // gave up: let what is under way land (bounded) before the memory goes
                 for (int i = 0; i < n_tiles; ++i) mbar_wait(&sh.full[i], ph ^ (i >= s ? 1u : 0u));
-        } else if (warp == 1) {
+        } else if (warp == 2) {
+            // ---------------------------------------------------------- the rows of Q: one buffer for two tiles, or two for one each
+            TreeItems items;
+            TreeItem it;
+            constexpr int kBufs = TWO ? 1 : 2;
+            for (int n = 0;; ++n) {
+                if (!(ok = items.next(sh, it)) || it.count == 0) break;
+                const int buf = n % kBufs;
+                if (n >= kBufs && !(ok = __all_sync(0xffffffffu, mbar_wait(&sh.q_free[buf], (n / kBufs - 1) & 1)))) break;
+                const int parts = TWO && it.rows > p.part ? 2 : 1;
+                if (p.group <= 128) {
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(&sh.q_ready[buf], (uint32_t)(parts * halves * p.part * 128));
+                        const int tok = it.t0 + it.rt * (p.rows / p.group);
+                        for (int i = 0; i < parts; ++i)
+                            for (int h = 0; h < halves; ++h)
+                                tma_load3(smem_u32(qs + (TWO ? i : buf) * 32768 + h * 16384), &mapQ, h * 64, it.kh * p.group, tok + i * (p.part / p.group),
+                                          smem_u32(&sh.q_ready[buf]));
+                    }
+                } else {
+                    // more heads to a key head than a tile has rows: row by row
+                    for (int i = lane; i < it.rows * halves * 8; i += 32) {
+                        const int r = i / (halves * 8), c = i % (halves * 8);
+                        const unsigned row = (unsigned)(it.rt * p.rows + r);
+                        const uint16_t *src = a.q + (long long)(it.t0 + (int)(row / (unsigned)p.group)) * a.ldq +
+                                              (long long)(it.kh * p.group + (int)(row % (unsigned)p.group)) * hd;
+                        *reinterpret_cast<uint4 *>(qs + (TWO ? r >> 7 : buf) * 32768 + (c >> 3) * 16384 + (r & 127) * 128 + (((c ^ r) & 7) << 4)) =
+                            c * 8 < hd ? *reinterpret_cast<const uint4 *>(src + c * 8) : make_uint4(0, 0, 0, 0);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.q_ready[buf]);
+                }
+                __syncwarp();
+                if (it.stop) break;
+            }
+            if (!ok && p.group <= 128)                          // (copies of Q that are under way)
+                for (int i = 0; i < kBufs; ++i) mbar_wait(&sh.q_ready[i], 0);
+        } else {
             // ---------------------------------------------------------- products
             const bool lead = tc_elect();
             const uint32_t idesc_s = tc_idesc_f16(D::kBf16, 128, 128, false), idesc_o = tc_idesc_f16(D::kBf16, 128, (hd + 15) / 16 * 16, true);
-            const int ksteps = (hd + 15) / 16, steps = units << p.two;
+            const int ksteps = (hd + 15) / 16;
+            const uint32_t q0 = tc_desc(smem_u32(qs)), kv0 = tc_desc(smem_u32(tiles)), v0 = tc_desc_mn(smem_u32(tiles), 16384);
+            TreeItems items;
+            TreeItem it;
+            // the units as the scores meet them: those left of the item, keys from the current one on, number of the item, units of it so far
+            int left = 0, rest = 0, n_item = -1, of = 0, stop = 0, rows = 0;
             // the stages of the next K and V tiles (every other one)
-            int ks = 0, vs = 1, item = 0, of_item = 0, unit = 0;     // item: its number here; of_item: units of it so far
-            uint32_t kph = 0, vph = 0, cnt[2] = {0, 0}, outs[2] = {0, 0};
-            TreeStep st[2];
-            bool have_unit = false;
-            // S of step j; the walk goes on with the last step of a unit
-            auto scores = [&](int j) {
-                TreeStep &x = st[j & 1];
-                x.live = p.two ? w.rows(a, p) > (j & 1) * 128 : 1;
-                x.fresh = p.two ? of_item == 0 : of_item < 2;
-                x.keys = w.keys(p);
-                const int buf = p.two ? 0 : item & 1;
-                if (of_item == 0 && !have_unit) {
-                    if (!mbar_wait(&sh.q_ready[buf], (p.two ? item : item >> 1) & 1)) return false;
+            int ks = 0, vs = 1;
+            uint32_t kph = 0, vph = 0;
+            struct Unit { int live1, fresh, steps, last; } nu;
+            auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+            // the next unit: 1, none left: 0, gave up: -1
+            auto next_unit = [&]() -> int {
+                if (left == 0) {
+                    if (stop) return 0;
+                    if (!items.next(sh, it)) return -1;
+                    left = uniform(it.count);
+                    stop = uniform(it.stop);
+                    rows = uniform(it.rows);
+                    rest = uniform(it.len - it.tile * p.unit);
+                    of = 0;
+                    ++n_item;
+                    if (left == 0) return 0;
                 }
-                if (!have_unit && !mbar_wait(&sh.full[ks], kph)) return false;
-                have_unit = true;
-                const bool last = !p.two || (j & 1);
-                if (x.live) {
-                    tc_fence_after();
-                    const uint32_t q = tc_desc(smem_u32(qs) + (p.two ? j & 1 : buf) * 32768), k = tc_desc(smem_u32(tiles) + ks * tile_bytes);
+                nu.live1 = rows > p.part;
+                nu.fresh = TWO ? of == 0 : of < 2;
+                nu.steps = (min(p.unit, rest) + 15) >> 4;
+                nu.last = left == 1;
+                rest -= p.unit;
+                --left;
+                ++of;
+                return 1;
+            };
+            auto scores = [&](auto S) {                         // S = Q K^T into sum S
+                constexpr int s = decltype(S)::value;
+                const uint32_t q = q0 + (TWO ? s : n_item & 1) * 2048, k = kv0 + ks * (tile_bytes >> 4);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i < ksteps)
-                            tc_mma_f16_ss(tmem + (j & 1) * 128, q + (i >> 2) * 1024 + 2 * (i & 3), k + (i >> 2) * 1024 + 2 * (i & 3), idesc_s, i > 0, lead);
-                    tc_commit<1>(&sh.s_full[j & 1], lead);
+                for (int i = 0; i < 8; ++i)
+                    if (i < ksteps) tc_mma_f16_ss(tmem + s * 128, q + (i >> 2) * 1024 + 2 * (i & 3), k + (i >> 2) * 1024 + 2 * (i & 3), idesc_s, i > 0, lead);
+                tc_commit<1>(&sh.s_full[s], lead);
+            };
+            auto keys_done = [&] {
+                tc_commit<1>(&sh.empty[ks], lead);
+                if (nu.last) tc_commit<1>(&sh.q_free[TWO ? 0 : n_item & 1], lead);
+                ks += 2;
+                if (ks >= n_tiles) { ks -= n_tiles; kph ^= 1; }
+            };
+            auto keys_there = [&] {
+                if (of == 1 && !__all_sync(0xffffffffu, mbar_wait(&sh.q_ready[TWO ? 0 : n_item & 1], (TWO ? n_item : n_item >> 1) & 1))) return false;
+                const bool r = __all_sync(0xffffffffu, mbar_wait(&sh.full[ks], kph));
+                tc_fence_after();
+                return r;
+            };
+            // O += P V of sum S; cnt: its products so far, outs: its items
+            auto values = [&](auto S, const Unit &u, uint32_t &cnt, uint32_t &outs, bool wait_v) {
+                constexpr int s = decltype(S)::value;
+                if (wait_v && !__all_sync(0xffffffffu, mbar_wait(&sh.full[vs], vph))) return false;
+                if (!__all_sync(0xffffffffu, mbar_wait(&sh.p_ready[s], cnt & 1))) return false;
+                ++cnt;
+                if (u.fresh) {
+                    if (outs > 0 && !__all_sync(0xffffffffu, mbar_wait(&sh.o_free[s], (outs - 1) & 1))) return false;
+                    ++outs;
                 }
-                if (last) {
-                    tc_commit<1>(&sh.empty[ks], lead);
-                    ks += 2;
-                    if (ks >= n_tiles) { ks -= n_tiles; kph ^= 1; }
-                    have_unit = false;
-                    ++unit;
-                    ++of_item;
-                    if (unit == units || w.tile + 1 == w.tiles) {
-                        tc_commit<1>(&sh.q_free[buf], lead);
-                        ++item;
-                        of_item = 0;
-                    }
-                    if (unit < units) w.advance(a, p);
-                }
+                tc_fence_after();
+                const uint32_t v = v0 + vs * (tile_bytes >> 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < u.steps) tc_mma_f16_ta(tmem + 256 + s * 128, tmem + s * 128 + i * 8, v + i * 128, idesc_o, !u.fresh || i > 0, lead);
+                tc_commit<1>(&sh.pv_done[s], lead);
                 return true;
             };
-            for (int j = 0; ok && j < 2 && j < steps; ++j) ok = scores(j);
-            for (int j = 0; ok && j < steps; ++j) {
-                const int s = j & 1;
-                const TreeStep x = st[s];
-                if (x.live) {
-                    if (!(ok = mbar_wait(&sh.full[vs], vph) && mbar_wait(&sh.p_ready[s], cnt[s] & 1))) break;
-                    ++cnt[s];
-                    if (x.fresh && outs[s]++ > 0 && !(ok = mbar_wait(&sh.o_free[s], outs[s] & 1))) break;
-                    tc_fence_after();
-                    const uint32_t v = tc_desc_mn(smem_u32(tiles) + vs * tile_bytes, 16384);
-                    const int n = (x.keys + 15) / 16;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i < n) tc_mma_f16_ta(tmem + 256 + s * 128, tmem + s * 128 + i * 8, v + i * 128, idesc_o, !x.fresh || i > 0, lead);
-                    tc_commit<1>(&sh.pv_done[s], lead);
-                }
-                if (!p.two || s) {
-                    tc_commit<1>(&sh.empty[vs], lead);
-                    vs += 2;
-                    if (vs >= n_tiles) { vs -= n_tiles; vph ^= 1; }
-                }
-                if (j + 2 < steps) ok = scores(j + 2);
-            }
-        } else {
-            // ---------------------------------------------------------- the rows of Q, half of them to a warp
-            const int G = a.n_heads / a.n_kv, bufs = p.two ? 1 : 2, per = p.rows / 2;
-            const uint32_t turn = a.scale < 0.0f ? 0x80008000u : 0u;
-            int item = 0;
-            for (int u = 0; u < units; ++item) {
-                const int buf = item % bufs;
-                if (item >= bufs) ok = mbar_wait(&sh.q_free[buf], (item / bufs - 1) & 1);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                const int rows = w.rows(a, p), r0 = (warp - 2) * per;
-                // a lane takes a 16-byte piece of every other row
-                const int c = lane & 15;
-                if (c < halves * 8)
-                    for (int r = r0 + (lane >> 4); r < min(r0 + per, (rows + 31) & ~31); r += 16) {
-                        uint4 v[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int rr = r + 2 * i;
-                            v[i] = make_uint4(0, 0, 0, 0);
-                            if (rr < rows && rr < r0 + per && c * 8 < hd) {
-                                const unsigned row = (unsigned)(w.rt * p.rows + rr);
-                                const uint16_t *src = a.q + (long long)(w.t0 + (int)(row / (unsigned)G)) * a.ldq + (long long)(w.kh * G + (int)(row % (unsigned)G)) * hd;
-                                v[i] = *reinterpret_cast<const uint4 *>(src + c * 8);
-                            }
+            auto values_done = [&] {
+                tc_commit<1>(&sh.empty[vs], lead);
+                vs += 2;
+                if (vs >= n_tiles) { vs -= n_tiles; vph ^= 1; }
+            };
+            constexpr std::integral_constant<int, 0> S0{};
+            constexpr std::integral_constant<int, 1> S1{};
+            uint32_t cnt0 = 1, cnt1 = 1, outs0 = 0, outs1 = 0;
+            int more = next_unit();
+            // (the softmax's first pass writes where S will be)
+            if (more > 0 && !(__all_sync(0xffffffffu, mbar_wait(&sh.p_ready[0], 0)) && __all_sync(0xffffffffu, mbar_wait(&sh.p_ready[1], 0)))) more = -1;
+            tc_fence_after();
+            if (TWO) {
+                // both sums on a unit: each's scores of the next unit behind its values of this one
+                if (more > 0 && (ok = keys_there())) {
+                    scores(S0);
+                    if (nu.live1) scores(S1);
+                    keys_done();
+                    for (;;) {
+                        const Unit u = nu;
+                        more = next_unit();
+                        if (more < 0 || !(ok = values(S0, u, cnt0, outs0, true))) break;
+                        if (more) {
+                            if (!(ok = keys_there())) break;
+                            scores(S0);
                         }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int rr = r + 2 * i;
-                            if (rr < r0 + per)
-                                *reinterpret_cast<uint4 *>(qs + (p.two ? rr >> 7 : buf) * 32768 + (c >> 3) * 16384 + (rr & 127) * 128 + (((c ^ rr) & 7) << 4)) =
-                                    make_uint4(v[i].x ^ turn, v[i].y ^ turn, v[i].z ^ turn, v[i].w ^ turn);
-                        }
+                        if (u.live1 && !(ok = values(S1, u, cnt1, outs1, false))) break;
+                        values_done();
+                        if (!more) break;
+                        if (nu.live1) scores(S1);
+                        keys_done();
                     }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.q_ready[buf]);
-                // on to the next item
-                const int rest = min(w.tiles - w.tile, units - u);
-                u += rest;
-                if (u < units) {
-                    w.tile = w.tiles - 1;
-                    w.advance(a, p);
+                }
+            } else {
+                // units in turn: each sum's scores of the unit after next behind its values of this one
+                Unit u0 = {}, u1 = {};
+                bool on0 = false, on1 = false;
+                auto ahead = [&](auto S, Unit &u, bool &on) {
+                    on = more > 0;
+                    if (!on) return true;
+                    u = nu;
+                    if (!keys_there()) return false;
+                    scores(S);
+                    keys_done();
+                    more = next_unit();
+                    return more >= 0;
+                };
+                ok = ahead(S0, u0, on0) && ahead(S1, u1, on1);
+                while (ok) {
+                    if (!on0 || !(ok = values(S0, u0, cnt0, outs0, true))) break;
+                    values_done();
+                    if (!(ok = ahead(S0, u0, on0))) break;
+                    if (!on1 || !(ok = values(S1, u1, cnt1, outs1, true))) break;
+                    values_done();
+                    if (!(ok = ahead(S1, u1, on1))) break;
                 }
             }
+            ok = ok && more >= 0;
         }
     } else {
         // -------------------------------------------------------------- softmax: a thread to a row
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTrSoftRegs));
         const int sum = (warp - 4) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
         const uint32_t at = tmem + sum * 128 + ((uint32_t)(q4 * 32) << 16), acc = at + 256;
-        // a negative scale turned q's signs; a zero one must leave -inf where a key is not seen
+        const bool turn = a.scale < 0.0f;                       // a negative scale turns the scores' signs; a zero one must leave -inf as it is
         const float scale = (a.scale == 0.0f ? 1.17549435e-38f : fabsf(a.scale)) * 1.4426950408889634f;
         constexpr float kShift = D::kBf16 ? 0.0f : kProbabilityShift;
+        TreeItems items;
+        // The first pass, on a unit that there is not, keeps nothing: it brings the code in while the first keys are under way (the
+        // products wait for its P).  cnt: passes; the products of the first do not exist.
+        TreeItem it = {};
+        it.count = 1;
+        it.len = it.rows = 256;
+        bool warm = true;
         uint32_t cnt = 0;
-        int of_item = 0, taken = 0;                             // units of the item so far, and those of this sum
-        float m = -CUDART_INF_F, l = 0.0f;
-        for (int u = 0; u < units; ++u) {
-            const int rows = w.rows(a, p), mine = rows - (p.two ? sum * 128 : 0), keys = w.keys(p);
-            const bool leave = u + 1 == units || w.tile + 1 == w.tiles;
-            if (mine > 0 && (p.two || (u & 1) == sum)) {
-                const bool fresh = taken == 0, live = q4 * 32 < mine;
-                ++taken;
-                // values past the last key, up to the product's step of 16: zero, because a zero probability times whatever lay
-                // there (NaN, say) would not be
-                const int zeros = (keys + 15) / 16 * 16 - keys;
-                if (zeros && (!p.two || sum == 0)) {
-                    const int t = 2 * u + 1, stage = t % n_tiles;
-                    ok = mbar_wait(&sh.full[stage], (t / n_tiles) & 1);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                    unsigned char *const vt = tiles + stage * tile_bytes;
-                    for (int i = r; i < zeros * halves * 8; i += 128) {
-                        const int piece = i % (halves * 8);
-                        *reinterpret_cast<uint4 *>(vt + (piece >> 3) * 16384 + (keys + i / (halves * 8)) * 128 + ((piece & 7) << 4)) = make_uint4(0, 0, 0, 0);
+        int done = 0;                                           // units of the items before
+        do {
+            if (!warm && !(ok = items.next(sh, it))) break;
+            const int mine = min(it.rows - (TWO ? sum * p.part : 0), p.part);
+            const bool live = q4 * 32 < mine;
+            float m = -CUDART_INF_F, l = 0.0f;
+            bool fresh = true;
+            if (mine > 0)
+                for (int u = 0; u < it.count; ++u) {
+                    if (!TWO && !warm && ((done + u) & 1) != sum) continue;
+                    const int keys = min(p.unit, it.len - (it.tile + u) * p.unit);
+                    // values past the last key, up to the product's step of 16: zero, because a zero probability times whatever lay
+                    // there (NaN, say) would not be
+                    const int zeros = (keys + 15) / 16 * 16 - keys;
+                    if (zeros && (!TWO || sum == 0) && !warm) {
+                        const int t = 2 * (done + u) + 1, stage = t % n_tiles;
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.full[stage], (t / n_tiles) & 1)))) break;
+                        unsigned char *const vt = tiles + stage * tile_bytes;
+                        for (int i = r; i < zeros * halves * 8; i += 128) {
+                            const int piece = i % (halves * 8);
+                            *reinterpret_cast<uint4 *>(vt + (piece >> 3) * 16384 + (keys + i / (halves * 8)) * 128 + ((piece & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
-                ok = mbar_wait(&sh.s_full[sum], cnt & 1);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                tc_fence_after();
-                if (live) {
-                    uint32_t x[4][32];
+                    if (!warm && !(ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[sum], (cnt - 1) & 1)))) break;
+                    tc_fence_after();
+                    if (live) {
+                        uint32_t x[4][32];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tc_ld32(at + c * 32, x[c]);
-                    tc_wait_ld();
-                    if (keys < 128)
+                        for (int c = 0; c < 4; ++c) tc_ld32(at + c * 32, x[c]);
+                        tc_wait_ld();
+                        if (turn)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) x[c][j] ^= 0x80000000u;
+                        if (keys < 128)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (c * 32 + j >= keys) x[c][j] = 0xff800000u;
+                        float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (c * 32 + j >= keys) x[c][j] = 0xff800000u;
-                    float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) top[(j >> 1) & 3] = fmax3(top[(j >> 1) & 3], __uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1]));
-                    const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                    const bool above = (t - m) * scale > kTrSlack;
-                    if (fresh) {
-                        m = t;
-                        l = 0.0f;
-                    } else if (__any_sync(0xffffffffu, above)) {
-                        // a maximum well above the reference: O and l move to it
-                        ok = mbar_wait(&sh.pv_done[sum], (cnt - 1) & 1);
-                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                        tc_fence_after();
-                        const float to = above ? t : m, f = to == -CUDART_INF_F ? 1.0f : exp2_fast((m - to) * scale);
-                        m = to;
-                        l *= f;
+                            for (int j = 0; j < 32; j += 2) top[(j >> 1) & 3] = fmax3(top[(j >> 1) & 3], __uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1]));
+                        const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                        const bool above = (t - m) * scale > kTrSlack;
+                        if (fresh) m = t;
+                        else if (__any_sync(0xffffffffu, above && r < mine)) {
+                            // a maximum well above the reference: O and l move to it
+                            if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.pv_done[sum], cnt & 1)))) break;       // (pass cnt - 1)
+                            tc_fence_after();
+                            const float to = above ? t : m, f = to == -CUDART_INF_F ? 1.0f : exp2_fast((m - to) * scale);
+                            m = to;
+                            l *= f;
 #pragma unroll 1
-                        for (int c = 0; c < hd; c += 16) {
-                            uint32_t o[16];
-                            tc_ld16(acc + c, o);
-                            tc_wait_ld();
+                            for (int c = 0; c < hd; c += 16) {
+                                uint32_t o[16];
+                                tc_ld16(acc + c, o);
+                                tc_wait_ld();
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                            tc_st16(acc + c, o);
+                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                tc_st16(acc + c, o);
+                            }
+                            tc_wait_st();
                         }
+                        const float from = m == -CUDART_INF_F ? 0.0f : m;
+                        const float2 from2 = make_float2(-from, -from), scale2 = make_float2(scale, scale), shift2 = make_float2(kShift, kShift);
+                        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int j = 0; j < 32; j += 2) {
+                                const float2 d = __ffma2_rn(__fadd2_rn(make_float2(__uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1])), from2), scale2, shift2);
+                                const float e = exp2_fast(d.x), f = exp2_fast(d.y);
+                                part[j & 2] += e;
+                                part[(j & 2) + 1] += f;
+                                // rounded to the 16-bit type for the product with v; the sum takes the unrounded ones (see probability_base)
+                                x[c >> 1][(c & 1) * 16 + j / 2] = D::encode2(e, f);
+                            }
+                        l += (part[0] + part[1]) + (part[2] + part[3]);
+                        tc_st32(at, x[0]);
+                        tc_st32(at + 32, x[1]);
                         tc_wait_st();
-                    }
-                    const float from = m == -CUDART_INF_F ? 0.0f : m;
-                    const float2 from2 = make_float2(-from, -from), scale2 = make_float2(scale, scale), shift2 = make_float2(kShift, kShift);
-                    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            const float2 d = __ffma2_rn(__fadd2_rn(make_float2(__uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1])), from2), scale2, shift2);
-                            const float e = exp2_fast(d.x), f = exp2_fast(d.y);
-                            part[j & 2] += e;
-                            part[(j & 2) + 1] += f;
-                            // rounded to the 16-bit type for the product with v; the sum takes the unrounded ones (see probability_base)
-                            x[c >> 1][(c & 1) * 16 + j / 2] = D::encode2(e, f);
-                        }
-                    tc_st32(at, x[0]);
-                    tc_st32(at + 32, x[1]);
-                    l += (part[0] + part[1]) + (part[2] + part[3]);
-                    tc_wait_st();
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.p_ready[sum]);
-                ++cnt;
-            }
-            ++of_item;
-            if (leave) {
-                const int own_rec = w.own ? p.own_rec : p.pre_rec, stride = p.two ? own_rec : 2 * own_rec;
-                const long long rec = (long long)(w.item + cta) * stride + (p.two ? sum * 128 : sum * own_rec) + r;
-                float2 *const ml = reinterpret_cast<float2 *>(ws + (w.own ? p.off_own_ml : p.off_pre_ml));
-                if (taken) {
-                    ok = mbar_wait(&sh.pv_done[sum], (cnt - 1) & 1);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                    tc_fence_after();
-                    if (q4 * 32 < mine) {
-                        float *const dst = reinterpret_cast<float *>(ws + (w.own ? p.off_own_o : p.off_pre_o)) + rec * hd;
-#pragma unroll 1
-                        for (int c = 0; c < hd; c += 32) {
-                            uint32_t o[32];
-                            tc_ld32(acc + c, o);
-                            tc_wait_ld();
-                            if (r < mine)
-#pragma unroll
-                                for (int j = 0; j < 32; j += 4)
-                                    if (c + j < hd) *reinterpret_cast<uint4 *>(dst + c + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-                        }
-                        if (r < mine) ml[rec] = make_float2(m == -CUDART_INF_F ? m : __fmul_rn(m, scale) - kShift, l);
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.o_free[sum]);
-                } else if (!p.two && r < mine)
-                    ml[rec] = make_float2(-CUDART_INF_F, 0.0f);         // the item had no unit for this sum
-                of_item = taken = 0;
+                    if (lane == 0) mbar_arrive(&sh.p_ready[sum]);
+                    ++cnt;
+                    fresh = false;
+                }
+            if (!ok) break;
+            if (warm) {
+                warm = false;
+                asm volatile("griddepcontrol.wait;" ::: "memory");
+                continue;
             }
-            if (u + 1 < units) w.advance(a, p);
-        }
+            done += it.count;
+            if (mine <= 0 || it.count == 0) continue;
+            const long long rec = it.rec + (TWO ? sum * p.part : sum * (it.own ? p.own_rec : p.pre_rec)) + r;       // (its number among all rows)
+            float2 *const ml = reinterpret_cast<float2 *>(ws + (it.own ? p.off_own_ml : p.off_pre_ml));
+            if (fresh) {
+                if (r < mine) ml[rec] = make_float2(-CUDART_INF_F, 0.0f);       // the item had no unit for this sum
+                continue;
+            }
+            if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.pv_done[sum], cnt & 1)))) break;                      // (pass cnt - 1)
+            tc_fence_after();
+            if (live) {
+                // (eight dims of every row side by side, so that a warp's stores lie together)
+                float *const dst = reinterpret_cast<float *>(ws + (it.own ? p.off_own_o : p.off_pre_o)) + tree_record(p, it.own, rec, 0, hd);
+                const int step = (it.own ? p.own_rec : p.pre_rec) * 8;
+#pragma unroll 1
+                for (int c = 0; c < hd; c += 32) {
+                    uint32_t o[32];
+                    tc_ld32(acc + c, o);
+                    tc_wait_ld();
+                    if (r < mine)
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8)
+                            if (c + j < hd) {
+                                uint4 *const to = reinterpret_cast<uint4 *>(dst + ((c + j) >> 3) * step);
+                                to[0] = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                                to[1] = make_uint4(o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
+                            }
+                    __syncwarp();
+                }
+                if (r < mine) ml[rec] = make_float2(m == -CUDART_INF_F ? m : __fmul_rn(m, scale) - kShift, l);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.o_free[sum]);
+        } while (!it.stop);
     }
     if (!ok && lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
     tc_fence_before();
@@ -476,18 +637,25 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
 }
 
 // ------------------------------------------------------------------ the tree itself, and the join
-// A warp per row.  Its halves take turns at the visible nodes and the records, 16 lanes with eight dims each; binary32 throughout.
+// A CTA per token and eight heads, a warp to a head.  Which nodes the token sees and where their keys lie is looked up once, the nodes
+// are taken before the launch with the records has to have ended.  A warp's halves take turns at nodes and records, 16 lanes with eight
+// dims each, four nodes of a half under way; binary32 throughout.
+constexpr int kTjHeads = 8, kTjUnroll = 4;
 template <class D>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(kTjHeads * 32, 4)
 tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *__restrict__ ws)
 {
-    pdl_begin();
-    const int lane = threadIdx.x & 31, half = lane >> 4, d0 = (lane & 15) * 8, hd = a.head_dim, G = a.n_heads / a.n_kv;
-    const unsigned row = blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int tok = (int)(row / (unsigned)a.n_heads), h = (int)(row % (unsigned)a.n_heads), kh = h / G;
-    const TreeTotals totals = *reinterpret_cast<const TreeTotals *>(ws + (size_t)a.n_seq * sizeof(TreeFirst));
-    if (tok >= totals.tokens) return;
+    __shared__ long long place[64 * kPlanMaxWords];             // element of the pools (before the head) of each visible node
+    __shared__ int counts[8];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, half = lane >> 4, d0 = (lane & 15) * 8, hd = a.head_dim, G = p.group;
+    const int parts = (a.n_heads + kTjHeads - 1) / kTjHeads, tok = (int)(blockIdx.x / (unsigned)parts), h = (int)(blockIdx.x % (unsigned)parts) * kTjHeads + warp;
+    const bool on = h < a.n_heads, in = d0 < hd;
+    const int kh = on ? h / G : 0, g = h - kh * G;
     // the last sequence that starts at or before the token (32 at a time)
+    const int tokens = tree_tokens(a);
+    uint4 q16 = make_uint4(0, 0, 0, 0);
+    if (on && in && tok < tokens) q16 = *reinterpret_cast<const uint4 *>(a.q + (long long)tok * a.ldq + (long long)h * hd + d0);
     int b = 0;
     for (int n = a.n_seq; n > 1;) {
         const int step = (n + 31) / 32, at = b + lane * step;
@@ -498,123 +666,166 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *__rest
     }
     const TreeSeq s = tree_load(a, b);
     const int node = tok - s.t0;
-    if (node < 0 || node >= s.nodes) return;                    // (more nodes than there may be: counted, not computed)
-    const float scale = a.scale * 1.4426950408889634f;
-    const bool in = d0 < hd;
+    if (tok >= tokens || node < 0 || node >= s.nodes) return;   // (more nodes than there may be: counted, not computed)
+    // the nodes that this one sees; a thread per bit, a warp per half word
+    bool sees = false;
+    const int key = s.base + tid;
+    if (tid >> 6 < a.words && tid < s.nodes && key >= 0) {      // (a length below the number of nodes: the first have no key)
+        const unsigned long long bits = (unsigned long long)__ldg(a.mask + (long long)tok * a.words + (tid >> 6));
+        sees = bits >> (tid & 63) & 1;
+    }
+    const uint32_t seen = __ballot_sync(0xffffffffu, sees);
+    if (lane == 0) counts[warp] = __popc(seen);
+    long long at = 0;
+    if (sees || (tid == node && key >= 0)) {
+        const unsigned pg = (unsigned)key / (unsigned)a.page_size, row = (unsigned)key - pg * (unsigned)a.page_size;
+        int page = __ldg(a.page_table + (long long)b * a.ld_table + pg);
+        const bool bad = page < 0 || page >= a.n_pages;
+        // a page that is none counts where its first key is
+        if (bad && tid == node && row == 0 && h == warp && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+        if (bad) page = 0;
+        at = (long long)page * a.page_stride + (long long)row * a.token_stride;
+    }
+    __syncthreads();
+    int nodes = 0, before = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i < warp) before += counts[i];
+        nodes += counts[i];
+    }
+    if (sees) place[before + __popc(seen & ((1u << lane) - 1))] = at;
+    __syncthreads();
     float m = -CUDART_INF_F, l = 0.0f, o[8] = {};
-    // ---- records
-    const AttentionDeal deal = tree_deal(p, totals);
-    auto records = [&](const float *ro, const float2 *rml, long long first, int rec_rows, int in_rec, long long unit0, int n_units) {
-        const int c0 = deal.cta_of(unit0), c1 = deal.cta_of(unit0 + n_units - 1), sums = p.two ? 1 : 2;
-        for (int i = half; i < (c1 - c0 + 1) * sums; i += 2) {
-            const long long rec = ((first + c0 + i / sums) * sums + i % sums) * rec_rows + in_rec;
-            const float2 x = rml[rec];
-            if (x.x == -CUDART_INF_F && x.y == 0.0f) continue;  // (its output may be anything)
-            float4 v0 = make_float4(0, 0, 0, 0), v1 = v0;
-            if (in) {
-                v0 = *reinterpret_cast<const float4 *>(ro + rec * hd + d0);
-                v1 = *reinterpret_cast<const float4 *>(ro + rec * hd + d0 + 4);
-            }
-            const float to = fmaxf(m, x.x), f = m == -CUDART_INF_F ? 0.0f : exp2_fast(m - to), g = exp2_fast(x.x - to);
-            m = to;
-            l = l * f + x.y * g;
-            const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+    const float scale = a.scale * 1.4426950408889634f;
+    if (on) {
+        float q[8];
+        widen8<D>(q16, q);
+        for (int i0 = 0; i0 < nodes; i0 += 2 * kTjUnroll) {
+            uint4 k[kTjUnroll], v[kTjUnroll];
+            float sc[kTjUnroll];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = o[j] * f + v[j] * g;
-        }
-    };
-    if (p.pre_tiles) {
-        const unsigned in_all = (unsigned)(tok * G + h % G), rt = in_all / (unsigned)p.rows;
-        const long long item = (long long)kh * tree_tiles(totals.tokens * G, p.rows) + rt;
-        records(reinterpret_cast<const float *>(ws + p.off_pre_o), reinterpret_cast<const float2 *>(ws + p.off_pre_ml), item, p.pre_rec,
-                (int)(in_all - rt * p.rows), item * p.pre_tiles, p.pre_tiles);
-    }
-    if (s.ctx) {
-        const TreeFirst f = reinterpret_cast<const TreeFirst *>(ws)[b];
-        const unsigned in_seq = (unsigned)(node * G + h % G), rt = in_seq / (unsigned)p.rows;
-        const int within = kh * tree_tiles(s.nodes * G, p.rows) + (int)rt;
-        records(reinterpret_cast<const float *>(ws + p.off_own_o), reinterpret_cast<const float2 *>(ws + p.off_own_ml), f.item + within, p.own_rec,
-                (int)(in_seq - rt * p.rows), totals.pre + f.unit + (long long)within * f.tiles, f.tiles);
-    }
-    // ---- the nodes that this one sees
-    float q[8] = {};
-    if (in) widen8<D>(*reinterpret_cast<const uint4 *>(a.q + (long long)tok * a.ldq + (long long)h * hd + d0), q);
-    // a page that is none counts where its first key is
-    if (h == 0 && lane == 0 && s.base + node >= 0 && (unsigned)(s.base + node) % (unsigned)a.page_size == 0 && a.st) {
-        const int page = __ldg(a.page_table + (long long)b * a.ld_table + (unsigned)(s.base + node) / (unsigned)a.page_size);
-        if (page < 0 || page >= a.n_pages) atomicAdd(&a.st->out_of_range, 1ull);
-    }
-    bool any = false;
-    for (int word = 0; word < a.words; ++word) {
-        unsigned long long bits = (unsigned long long)__ldg(a.mask + (long long)tok * a.words + word);
-        const int left = s.nodes - word * 64;
-        if (left <= 0) break;
-        if (left < 64) bits &= (1ull << left) - 1;
-        // (a length below the number of nodes: the first have no key)
-        const int gone = -s.base - word * 64;
-        if (gone > 0) bits &= gone < 64 ? ~0ull << gone : 0ull;
-        any |= bits != 0;
-        while (bits) {
-            // two nodes, one to each half
-            const int n0 = __ffsll((long long)bits) - 1;
-            bits &= bits - 1;
-            const int n1 = bits ? __ffsll((long long)bits) - 1 : -1;
-            bits &= bits ? bits - 1 : 0;
-            const int n = half ? n1 : n0, key = s.base + word * 64 + n;
-            float sc = 0.0f, v[8] = {};
-            if (n >= 0) {
-                const unsigned pg = (unsigned)key / (unsigned)a.page_size;
-                int page = __ldg(a.page_table + (long long)b * a.ld_table + pg);
-                if (page < 0 || page >= a.n_pages) page = 0;
-                const long long at = (long long)page * a.page_stride + (long long)(key - (int)pg * a.page_size) * a.token_stride + kh * a.head_stride + d0;
-                if (in) {
-                    float k[8];
-                    widen8<D>(*reinterpret_cast<const uint4 *>(a.ck + at), k);
-                    widen8<D>(*reinterpret_cast<const uint4 *>(a.cv + at), v);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) sc = __fmaf_rn(q[j], k[j], sc);
+            for (int i = 0; i < kTjUnroll; ++i) {
+                const int n = i0 + 2 * i + half;
+                k[i] = v[i] = make_uint4(0, 0, 0, 0);
+                if (n < nodes && in) {
+                    const long long x = place[n] + kh * a.head_stride + d0;
+                    k[i] = *reinterpret_cast<const uint4 *>(a.ck + x);
+                    v[i] = *reinterpret_cast<const uint4 *>(a.cv + x);
                 }
             }
 #pragma unroll
-            for (int x = 8; x > 0; x >>= 1) sc += __shfl_xor_sync(0xffffffffu, sc, x);
-            sc = n >= 0 ? sc * scale : -CUDART_INF_F;
-            if (n < 0) continue;
-            const float to = sc != sc ? sc : fmaxf(m, sc), base = to == -CUDART_INF_F ? 0.0f : to;
-            const float f = exp2_fast(m - base), g = exp2_fast(sc - base);
-            m = to;
-            l = l * f + g;
+            for (int i = 0; i < kTjUnroll; ++i) {
+                float f[8];
+                widen8<D>(k[i], f);
+                sc[i] = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = o[j] * f + v[j] * g;
+                for (int j = 0; j < 8; ++j) sc[i] = __fmaf_rn(q[j], f[j], sc[i]);
+            }
+#pragma unroll
+            for (int y = 8; y > 0; y >>= 1)
+#pragma unroll
+                for (int i = 0; i < kTjUnroll; ++i) sc[i] += __shfl_xor_sync(0xffffffffu, sc[i], y);
+            float to = m;
+#pragma unroll
+            for (int i = 0; i < kTjUnroll; ++i) {
+                sc[i] = i0 + 2 * i + half < nodes ? sc[i] * scale : -CUDART_INF_F;
+                to = fmaxf(to, sc[i]);
+            }
+            const float base = to == -CUDART_INF_F ? 0.0f : to, f = exp2_fast(m - base);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] *= f;
+#pragma unroll
+            for (int i = 0; i < kTjUnroll; ++i) {
+                if (i0 + 2 * i + half >= nodes) break;
+                const float e = exp2_fast(sc[i] - base);
+                float w[8];
+                widen8<D>(v[i], w);
+                l += e;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = __fmaf_rn(w[j], e, o[j]);
+            }
         }
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!on) return;
+    // ---- records: of the CTAs that had units of the head's items
+    const TreeTotals totals = *reinterpret_cast<const TreeTotals *>(ws + (size_t)a.n_seq * sizeof(TreeFirst));
+    const AttentionDeal deal = tree_deal(p, totals);
+    const int sums = p.two ? 1 : 2;
+    auto records = [&](bool own, long long item, int in_rec, long long unit0, int n_units) {
+        const float *const ro = reinterpret_cast<const float *>(ws + (own ? p.off_own_o : p.off_pre_o));
+        const float2 *const rml = reinterpret_cast<const float2 *>(ws + (own ? p.off_own_ml : p.off_pre_ml));
+        const int n = own ? p.own_rec : p.pre_rec, c0 = deal.cta_of(unit0), c1 = n_units > 1 ? deal.cta_of(unit0 + n_units - 1) : c0;
+        const int records = (c1 - c0 + 1) * sums;
+        const long long rec0 = (item + c0) * sums;              // the first record; the others follow
+        for (int i = half; i < records; i += 2) {
+            const long long rec = rec0 + i;
+            const float2 y = rml[rec * n + in_rec];
+            float4 v0 = make_float4(0, 0, 0, 0), v1 = v0;
+            if (in) {
+                const float *src = ro + rec * n * hd + (long long)d0 * n + in_rec * 8;
+                v0 = *reinterpret_cast<const float4 *>(src);
+                v1 = *reinterpret_cast<const float4 *>(src + 4);
+            }
+            if (y.x == -CUDART_INF_F && y.y == 0.0f) continue;  // (its output may be anything)
+            const float to = fmaxf(m, y.x), f = m == -CUDART_INF_F ? 0.0f : exp2_fast(m - to), e = exp2_fast(y.x - to);
+            l = l * f + y.y * e;                                // (a sum that is no number stays one)
+            m = to;
+            const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = o[j] * f + v[j] * e;
+        }
+    };
+    if (p.pre_tiles) {
+        const unsigned in_all = (unsigned)(tok * G + g), rt = in_all / (unsigned)p.rows;
+        const long long item = (long long)kh * tree_tiles(tokens * G, p.rows) + rt;
+        records(false, item, (int)(in_all - rt * p.rows), item * p.pre_tiles, p.pre_tiles);
+    }
+    if (s.ctx) {
+        const TreeFirst first = reinterpret_cast<const TreeFirst *>(ws)[b];
+        const unsigned in_seq = (unsigned)(node * G + g), rt = in_seq / (unsigned)p.rows;
+        const int within = kh * tree_tiles(s.nodes * G, p.rows) + (int)rt;
+        records(true, first.item + within, (int)(in_seq - rt * p.rows), totals.pre + first.unit + (long long)within * first.tiles, first.tiles);
     }
     // ---- the halves together
     const float m1 = __shfl_xor_sync(0xffffffffu, m, 16), l1 = __shfl_xor_sync(0xffffffffu, l, 16);
-    const float to = fmaxf(m, m1), base = to == -CUDART_INF_F ? 0.0f : to, f = exp2_fast(m - base), g = exp2_fast(m1 - base);
-    l = l * f + l1 * g;
-    const bool none = !any && s.ctx == 0 && a.prefix_len == 0;
-    const float inv = none ? 0.0f : 1.0f / l;
+    const float to = fmaxf(m, m1), base = to == -CUDART_INF_F ? 0.0f : to, f = exp2_fast(m - base), e = exp2_fast(m1 - base);
+    const float inv = 1.0f / (l * f + l1 * e);
+    const bool none = nodes == 0 && s.ctx == 0 && a.prefix_len == 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = none ? 0.0f : (o[j] * f + __shfl_xor_sync(0xffffffffu, o[j], 16) * g) * inv;
+    for (int j = 0; j < 8; ++j) o[j] = none ? 0.0f : (o[j] * f + __shfl_xor_sync(0xffffffffu, o[j], 16) * e) * inv;
     if (in && half == 0)
         *reinterpret_cast<uint4 *>(a.out + (long long)tok * a.ldo + (long long)h * hd + d0) =
             make_uint4(D::encode2(o[0], o[1]), D::encode2(o[2], o[3]), D::encode2(o[4], o[5]), D::encode2(o[6], o[7]));
 }
 
+template <class D, bool TWO>
+static aweq_status tree_units(const TreeArgs &a, const TreePlan &p, unsigned char *ws, cudaStream_t stream)
+{
+    CUtensorMap mk = {}, mv = {}, mq = {};
+    aweq_status rc = AWEQ_OK;
+    if (p.box) {
+        rc = tma_pool_map(&mk, a.ck, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, p.box);
+        if (rc == AWEQ_OK)
+            rc = tma_pool_map(&mv, a.cv, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, p.box);
+    }
+    if (rc == AWEQ_OK && p.group <= 128) rc = tma_heads_map(&mq, a.q, a.max_tokens, a.n_heads, a.head_dim, a.ldq, p.group, p.part / p.group);
+    if (rc != AWEQ_OK) return rc;
+    static std::atomic<unsigned long long> allowed{0};
+    AWEQ_CUDA_OK(allow_smem(tree_units_kernel<D, TWO>, kTrSmem, allowed));
+    AWEQ_LAUNCH((tree_units_kernel<D, TWO>), dim3((unsigned)p.ctas), dim3(kTrThreads), kTrSmem, stream, a, p, mk, mv, mq, ws);
+    return AWEQ_OK;
+}
+
 template <class D>
 static aweq_status tree_launch(const TreeArgs &a, const TreePlan &p, unsigned char *ws, cudaStream_t stream)
 {
-    CUtensorMap mk = {}, mv = {};
-    if (p.box) {
-        aweq_status rc = tma_pool_map(&mk, a.ck, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, p.box);
-        if (rc == AWEQ_OK)
-            rc = tma_pool_map(&mv, a.cv, a.n_pages, a.page_size, a.n_kv, a.head_dim, a.page_stride, a.token_stride, a.head_stride, p.box);
-        if (rc != AWEQ_OK) return rc;
-    }
-    static std::atomic<unsigned long long> allowed{0};
-    AWEQ_CUDA_OK(allow_smem(tree_units_kernel<D>, kTrSmem, allowed));
-    AWEQ_LAUNCH(tree_units_kernel<D>, dim3((unsigned)p.ctas), dim3(kTrThreads), kTrSmem, stream, a, p, mk, mv, ws);
-    const long long rows = (long long)a.max_tokens * a.n_heads;
-    AWEQ_LAUNCH(tree_join_kernel<D>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, stream, a, p, (const unsigned char *)ws);
+    const aweq_status rc = p.two ? tree_units<D, true>(a, p, ws, stream) : tree_units<D, false>(a, p, ws, stream);
+    if (rc != AWEQ_OK) return rc;
+    AWEQ_LAUNCH(tree_join_kernel<D>, dim3((unsigned)a.max_tokens * (unsigned)((a.n_heads + kTjHeads - 1) / kTjHeads)), dim3(kTjHeads * 32), 0,
+                stream, a, p, (const unsigned char *)ws);
     return AWEQ_OK;
 }
 

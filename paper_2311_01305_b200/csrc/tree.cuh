@@ -9,8 +9,8 @@
 namespace aweq {
 
 struct TreePlan {
-    int two;                     // 1: an item has two tiles of 128 rows on the same keys; 0: one, whose units alternate between two sums
-    int rows;                    // rows of an item: 256 or 128
+    int two;                     // 1: an item has two tiles of rows on the same keys; 0: one, whose units alternate between two sums
+    int group, part, rows;       // heads to a key head; rows of a tile: whole tokens, up to 128; rows of an item: one tile or two
     int unit, box;               // keys of a unit, of one tiled copy (0: 16-byte copies)
     int ctas, pre_rt, pre_tiles; // grid; most row tiles of the prefix; units of a prefix item
     int pre_rec, own_rec;        // rows of a record, of one sum each
@@ -45,9 +45,9 @@ __device__ __forceinline__ int tree_tiles(int n, int of) { return (int)(((unsign
 struct TreeScan { long long units, unit0; int items, item0; };
 __device__ __forceinline__ TreeScan tree_scan(const TreeArgs &a, const TreePlan &p, const TreeSeq &s)
 {
-    const int lane = threadIdx.x & 31, G = a.n_heads / a.n_kv;
+    const int lane = threadIdx.x & 31;
     TreeScan r;
-    r.items = a.n_kv * tree_tiles(s.nodes * G, p.rows);
+    r.items = a.n_kv * tree_tiles(s.nodes * p.group, p.rows);
     r.units = (long long)r.items * tree_tiles(s.ctx, p.unit);
     long long u = r.units;
     int i = r.items;
@@ -62,15 +62,20 @@ __device__ __forceinline__ TreeScan tree_scan(const TreeArgs &a, const TreePlan 
     return r;
 }
 // All units; every warp computes them.  `lead`: the one warp that counts what is out of range and leaves the sequences' firsts.
-__device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreePlan &p, unsigned char *ws, bool lead)
+// s0, c0: what the lane has of the first 32 sequences.
+__device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreePlan &p, unsigned char *ws, bool lead, TreeSeq &s0, TreeScan &c0)
 {
     const int lane = threadIdx.x & 31;
     TreeTotals t = {0, 0, tree_tokens(a), 0};
-    t.pre = (long long)a.n_kv * tree_tiles(t.tokens * (a.n_heads / a.n_kv), p.rows) * p.pre_tiles;
+    t.pre = (long long)a.n_kv * tree_tiles(t.tokens * p.group, p.rows) * p.pre_tiles;
     int items = 0;
     for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
         const TreeSeq s = tree_load(a, b0 + lane);
         const TreeScan c = tree_scan(a, p, s);
+        if (b0 == 0) {
+            s0 = s;
+            c0 = c;
+        }
         if (lead && b0 + lane < a.n_seq) {
             reinterpret_cast<TreeFirst *>(ws)[b0 + lane] = {t.own + c.unit0, items + c.item0, tree_tiles(s.ctx, p.unit)};
             if (s.bad && a.st) atomicAdd(&a.st->out_of_range, 1ull);
@@ -81,10 +86,26 @@ __device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreeP
     return t;
 }
 
-// The walk over a CTA's units by a warp (every lane knows the unit): prefix items first, then each sequence's, tiles of keys
-// inside row tiles inside key heads.
+// What a CTA has of an item: units tile .. tile + count - 1 of a segment's keys on one row tile of one key head.
+struct alignas(16) TreeItem {
+    int own, b, kh, rt;          // b: the sequence (own)
+    int tile, count, len, rows;  // len: keys of the segment
+    int t0, stop;                // first token of the rows; the CTA's last item
+    long long rec;               // first row of its record
+};
+
+// The walk over a CTA's items by a warp (every lane knows the item): prefix items first, then each sequence's, row tiles inside
+// key heads.
 struct TreeWalk {
-    int own, b, kh, rt, tile, tiles, n_rt, len, t0, n_tok, item;     // len: keys of the segment; t0, n_tok: the tokens whose rows they are
+    int own, b, kh, rt, tile, tiles, n_rt, len, t0, n_tok, item;     // t0, n_tok: the tokens whose rows they are
+    __device__ __forceinline__ void take(const TreePlan &p, const TreeSeq &s, int src)
+    {
+        t0 = __shfl_sync(0xffffffffu, s.t0, src);
+        n_tok = __shfl_sync(0xffffffffu, s.nodes, src);
+        len = __shfl_sync(0xffffffffu, s.ctx, src);
+        tiles = tree_tiles(len, p.unit);
+        n_rt = tree_tiles(n_tok * p.group, p.rows);
+    }
     __device__ __forceinline__ void enter(const TreeArgs &a, const TreePlan &p, int to)        // the next sequence with units
     {
         own = 1;
@@ -95,18 +116,14 @@ struct TreeWalk {
             if (here || b0 + 32 >= a.n_seq) {
                 const int src = here ? __ffs(here) - 1 : 0;
                 b = b0 + src;
-                t0 = __shfl_sync(0xffffffffu, s.t0, src);
-                n_tok = __shfl_sync(0xffffffffu, s.nodes, src);
-                len = __shfl_sync(0xffffffffu, s.ctx, src);
                 item += __shfl_sync(0xffffffffu, c.item0, src);
-                tiles = tree_tiles(len, p.unit);
-                n_rt = tree_tiles(n_tok * (a.n_heads / a.n_kv), p.rows);
+                take(p, s, src);
                 return;
             }
             item += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
         }
     }
-    __device__ __forceinline__ void begin(const TreeArgs &a, const TreePlan &p, const TreeTotals &t, long long u0)
+    __device__ __forceinline__ void begin(const TreeArgs &a, const TreePlan &p, const TreeTotals &t, long long u0, const TreeSeq &s0, const TreeScan &c0)
     {
         own = b = kh = rt = tile = tiles = n_rt = len = t0 = n_tok = item = 0;
         const int lane = threadIdx.x & 31;
@@ -114,8 +131,8 @@ struct TreeWalk {
             tiles = p.pre_tiles;
             len = (int)a.prefix_len;
             n_tok = t.tokens;
-            n_rt = tree_tiles(n_tok * (a.n_heads / a.n_kv), p.rows);
-            item = (int)(u0 / tiles);
+            n_rt = tree_tiles(n_tok * p.group, p.rows);
+            item = (int)div_units(u0, tiles);
             tile = (int)(u0 - (long long)item * tiles);
             kh = item / n_rt;
             rt = item - kh * n_rt;
@@ -125,20 +142,16 @@ struct TreeWalk {
         long long passed = 0;
         int items = 0;
         for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
-            const TreeSeq s = tree_load(a, b0 + lane);
-            const TreeScan c = tree_scan(a, p, s);
+            const TreeSeq s = b0 ? tree_load(a, b0 + lane) : s0;
+            const TreeScan c = b0 ? tree_scan(a, p, s) : c0;
             const uint32_t here = __ballot_sync(0xffffffffu, u >= passed + c.unit0 && u < passed + c.unit0 + c.units);
             if (here) {
                 const int src = __ffs(here) - 1;
                 own = 1;
                 b = b0 + src;
                 const long long within = u - passed - __shfl_sync(0xffffffffu, c.unit0, src);
-                t0 = __shfl_sync(0xffffffffu, s.t0, src);
-                n_tok = __shfl_sync(0xffffffffu, s.nodes, src);
-                len = __shfl_sync(0xffffffffu, s.ctx, src);
-                tiles = tree_tiles(len, p.unit);
-                n_rt = tree_tiles(n_tok * (a.n_heads / a.n_kv), p.rows);
-                const int i = (int)(within / tiles);
+                take(p, s, src);
+                const int i = (int)div_units(within, tiles);
                 tile = (int)(within - (long long)i * tiles);
                 kh = i / n_rt;
                 rt = i - kh * n_rt;
@@ -149,9 +162,8 @@ struct TreeWalk {
             items += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
         }
     }
-    __device__ __forceinline__ void advance(const TreeArgs &a, const TreePlan &p)
+    __device__ __forceinline__ void next_item(const TreeArgs &a, const TreePlan &p)
     {
-        if (++tile < tiles) return;
         tile = 0;
         ++item;
         if (++rt < n_rt) return;
@@ -161,15 +173,7 @@ struct TreeWalk {
         if (!own) item = 0;
         enter(a, p, own ? b + 1 : 0);
     }
-    __device__ __forceinline__ int keys(const TreePlan &p) const { return min(p.unit, len - tile * p.unit); }
-    __device__ __forceinline__ int rows(const TreeArgs &a, const TreePlan &p) const { return min(p.rows, n_tok * (a.n_heads / a.n_kv) - rt * p.rows); }
-    // entry of the page list for the unit's r'th key, if there is such a key
-    __device__ __forceinline__ int entry(const TreeArgs &a, const TreePlan &p, int r) const
-    {
-        const int key = tile * p.unit + r;
-        if (key >= len) return 0;
-        return __ldg((own ? a.page_table + (long long)b * a.ld_table : a.prefix_pages) + (unsigned)key / (unsigned)a.page_size);
-    }
+    __device__ __forceinline__ int rows(const TreePlan &p) const { return min(p.rows, n_tok * p.group - rt * p.rows); }
 };
 
 }  // namespace aweq
