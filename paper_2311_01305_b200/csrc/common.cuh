@@ -96,6 +96,8 @@ inline cudaError_t allow_smem(void (*kern)(KArgs...), size_t bytes, std::atomic<
     if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_release);
     return e;
 }
+// (What an earlier launch may have written is not read through __ldg or a const __restrict__ pointer behind a wait that other
+// loads stand before: such loads count as invariant, and nothing keeps them behind it.)
 __device__ __forceinline__ void pdl_begin()
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

@@ -59,7 +59,7 @@ __device__ __forceinline__ AppendPlace append_place(const KvAppendArgs &a, long 
     w.turn_ok = !a.rope || (w.pos >= 0 && w.pos < a.n_pos);
     w.at = -1;
     if (a.slot) {
-        const long long slot = __ldg(a.slot + t);
+        const long long slot = a.slot[t];
         if (slot < 0) {                                         // no token
             w.turn_ok = false;
             return w;

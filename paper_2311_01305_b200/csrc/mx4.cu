@@ -69,7 +69,7 @@ __device__ __forceinline__ void mx4_values(const Mx4Chunk &c, const float *scale
     if (scale && in)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const float4 s = ldg_f4(scale + chunk * 16 + i);
+            const float4 s = *reinterpret_cast<const float4 *>(scale + chunk * 16 + i);
             v[i] *= s.x; v[i + 1] *= s.y; v[i + 2] *= s.z; v[i + 3] *= s.w;
         }
 }
@@ -176,7 +176,7 @@ mx4_quant_kernel(const Mx4QuantArgs a)
                 e2m1_decode8(codes.y, q + 8);
 #pragma unroll
                 for (int j = 0; j < 16; j += 4) {
-                    const float4 m = ldg_f4(a.mu + chunk * 16 + j);
+                    const float4 m = *reinterpret_cast<const float4 *>(a.mu + chunk * 16 + j);
                     eps = __fmaf_rn(__fmaf_rn(q[j], step, -v[j]), m.x, eps);
                     eps = __fmaf_rn(__fmaf_rn(q[j + 1], step, -v[j + 1]), m.y, eps);
                     eps = __fmaf_rn(__fmaf_rn(q[j + 2], step, -v[j + 2]), m.z, eps);
@@ -237,21 +237,21 @@ aweq_status run_quant_mx4(const void *X, aweq_dtype dt, long long rows, long lon
 // ------------------------------------------------------------------ back
 template <class D, int FMT>
 __global__ void __launch_bounds__(256)
-mx4_dequant_kernel(const unsigned char *__restrict__ codes, const unsigned char *__restrict__ scales, const float *__restrict__ row_step,
-                   long long rows, int chunks, long long row_tiles, uint16_t *__restrict__ out, long long ldo)
+mx4_dequant_kernel(const unsigned char *codes, const unsigned char *scales, const float *row_step, long long rows, int chunks,
+                   long long row_tiles, uint16_t *out, long long ldo)
 {
     pdl_begin();
     const long long total = rows * chunks;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
         const long long row = i / chunks;
         const int chunk = (int)(i - row * chunks);
-        const uint2 c = __ldg(reinterpret_cast<const uint2 *>(codes + i * 8));
-        const uint32_t byte = __ldg(scales + mx4_scale_at(row, FMT == AWEQ_MX4_E8M0 ? chunk >> 1 : chunk, row_tiles));
+        const uint2 c = *reinterpret_cast<const uint2 *>(codes + i * 8);
+        const uint32_t byte = scales[mx4_scale_at(row, FMT == AWEQ_MX4_E8M0 ? chunk >> 1 : chunk, row_tiles)];
         float v[16], s, r = 1.0f;
         if (FMT == AWEQ_MX4_E8M0) s = byte == 0xffu ? __uint_as_float(0x7fffffffu) : byte ? __uint_as_float(byte << 23) : 5.877471754111438e-39f;
         else {
             s = e4m3_decode(byte);
-            r = __ldg(row_step + row);
+            r = row_step[row];
         }
         e2m1_decode8(c.x, v);
         e2m1_decode8(c.y, v + 8);

@@ -15,8 +15,8 @@ __device__ __forceinline__ Mx4Col mx4_col(const Mx4LinearArgs &p, long long o)
 {
     Mx4Col c = {0.0f, 0.0f};
     if (o < p.O) {
-        c.step = p.w_step ? __ldg(p.w_step + o) : 1.0f;
-        if (p.bias) c.bias = __ldg(p.bias + o);
+        c.step = p.w_step ? p.w_step[o] : 1.0f;
+        if (p.bias) c.bias = p.bias[o];
     }
     return c;
 }
@@ -161,7 +161,7 @@ mx4_big_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX, 
             const long long row0 = (long long)m * 256 + rank * 128 + q * 32, row = row0 + lane, o0 = (long long)n * 256;
             named_bar_sync(1, 256);
             sh.col[tid] = mx4_col(p, o0 + tid);
-            const float sx = row < p.N && p.x_step ? __ldg(p.x_step + row) : 1.0f;
+            const float sx = row < p.N && p.x_step ? p.x_step[row] : 1.0f;
             named_bar_sync(1, 256);
             const bool got = mbar_wait_cluster(&sh.acc_full[it & 1], (it >> 1) & 1);
             if (!named_bar_and(2, 256, got)) { ok = false; break; }
@@ -397,7 +397,7 @@ mx4_split_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX
                              : "r"(cluster_map(part + r * pitch + c, k)) : "memory");
             v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
         }
-        const float sx = p.x_step ? __ldg(p.x_step + row0 + r) : 1.0f;
+        const float sx = p.x_step ? p.x_step[row0 + r] : 1.0f;
         const float y[4] = {__fmaf_rn(v.x * sx, col[0].step, col[0].bias), __fmaf_rn(v.y * sx, col[1].step, col[1].bias),
                             __fmaf_rn(v.z * sx, col[2].step, col[2].bias), __fmaf_rn(v.w * sx, col[3].step, col[3].bias)};
         uint16_t *dst = p.out + (row0 + r) * p.ldo + o0 + c;

@@ -56,7 +56,7 @@ __device__ __forceinline__ PlanTotals plan_sequences(const KvPlanArgs &a, long l
     for (int b0 = 0; b0 < (int)a.n_seq; b0 += kPlanThreads) {
         const int b = b0 + (int)threadIdx.x;
         const bool in = b < (int)a.n_seq;
-        const int asked_held = in ? __ldg(a.held + b) : 0, asked = in ? __ldg(a.change + b) : 0;
+        const int asked_held = in ? a.held[b] : 0, asked = in ? a.change[b] : 0;
         const int held = (int)(asked_held < 0 ? 0 : min((long long)asked_held, cap));
         int fresh = asked > 0 ? (int)min((long long)asked, cap - held) : 0;
         const int drop = asked < 0 ? (int)min(-(long long)asked, (long long)held) : 0;
@@ -169,7 +169,7 @@ __device__ __forceinline__ void plan_fill(const KvPlanArgs &a, long long taken, 
 #pragma unroll
                     for (int w = 0; w < kPlanMaxWords; ++w)
                         if (at >> 6 == w) bits[w] |= 1ull << (at & 63);
-                    const int up = __ldg(a.parent + s.start + at);
+                    const int up = a.parent[s.start + at];
                     const bool bad = up < -1 || up >= at;
                     if (bad && at == node && a.st) atomicAdd(&a.st->out_of_range, 1ull);
                     if (bad || up < 0) break;
@@ -276,8 +276,8 @@ __global__ void __launch_bounds__(128) kv_accept_kernel(const KvAcceptArgs a, in
     const int b = blockIdx.x / blocks, i = (blockIdx.x - b * blocks) * 128 + threadIdx.x;
     const bool lead = i == 0;
     if (i >= 2 * pieces) return;
-    const long long base = __ldg(a.base + b), cap = a.pages_per_seq * a.page_size;
-    const int asked = __ldg(a.n_path + b);
+    const long long base = a.base[b], cap = a.pages_per_seq * a.page_size;
+    const int asked = a.n_path[b];
     int n = min(max(asked, 0), a.max_path);
     bool bad = n != asked;
     if (base < 0 || base > cap) {
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(128) kv_accept_kernel(const KvAcceptArgs a, in
     auto place = [&](long long key) -> long long {
         if (key >= cap) return -1;
         const unsigned p = (unsigned)((unsigned long long)key / (unsigned)a.page_size);
-        const int page = __ldg(row + p);
+        const int page = row[p];
         return page < 0 || page >= a.n_pages ? -1 : page * a.page_stride + (key - (long long)p * a.page_size) * a.token_stride;
     };
     constexpr int U = 8;
@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(128) kv_accept_kernel(const KvAcceptArgs a, in
         long long to[U];
         int node[U];
 #pragma unroll
-        for (int j = 0; j < U; ++j) node[j] = i0 + j < n ? __ldg(path + i0 + j) : -1;
+        for (int j = 0; j < U; ++j) node[j] = i0 + j < n ? path[i0 + j] : -1;
 #pragma unroll
         for (int j = 0; j < U; ++j) {
             to[j] = -1;

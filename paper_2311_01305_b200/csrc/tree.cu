@@ -70,7 +70,8 @@ static TreePlan tree_plan(const aweq_kv_cache *c, long long prefix_len, long lon
     if (rt > pre_rows / p.rows + n_seq) rt = pre_rows / p.rows + n_seq;
     const size_t pre_kept = p.pre_tiles ? (size_t)(pre_items + p.ctas) * p.pre_rec * sums : 0;
     const size_t own_kept = (size_t)(rt * c->n_kv_heads + p.ctas) * p.own_rec * sums;
-    size_t off = up256((size_t)n_seq * sizeof(TreeFirst) + sizeof(TreeTotals));
+    size_t off = up256(sizeof(TreeTotals) + (size_t)n_seq * sizeof(TreeFirst));
+    p.off_seq = off; off += up256((size_t)max_tokens * 4);
     p.off_pre_o = off; off += up256(pre_kept * c->head_dim * 4);
     p.off_pre_ml = off; off += up256(pre_kept * 8);
     p.off_own_o = off; off += up256(own_kept * c->head_dim * 4);
@@ -161,8 +162,8 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
             TreeSeq s0 = {};
             TreeScan c0 = {};
-            const TreeTotals totals = tree_totals(a, p, ws, cta == 0, s0, c0);
-            if (cta == 0 && lane == 0) *reinterpret_cast<TreeTotals *>(ws + (size_t)a.n_seq * sizeof(TreeFirst)) = totals;
+            const TreeTotals totals = tree_totals(a, p, s0, c0);
+            if (cta == 0 && lane == 0) *reinterpret_cast<TreeTotals *>(ws) = totals;
             const AttentionDeal deal = tree_deal(p, totals);
             long long u0 = 0;
             int left = 0;
@@ -201,6 +202,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                 if (it.stop) break;
                 w.next_item(a, p);
             }
+            tree_leave(a, p, ws, cta);
         } else if (warp == 0) {
             // ---------------------------------------------------------- copies: a unit's keys, then its values
             TreeItems items;
@@ -211,7 +213,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             auto entry = [&](const TreeItem &x, int t, int r) {     // entry of the page list for the unit's r'th key, if there is such a key
                 const int key = t * p.unit + r;
                 if (key >= x.len) return 0;
-                return __ldg((x.own ? a.page_table + (long long)x.b * a.ld_table : a.prefix_pages) + (unsigned)key / (unsigned)a.page_size);
+                return (x.own ? a.page_table + (long long)x.b * a.ld_table : a.prefix_pages)[(unsigned)key / (unsigned)a.page_size];
             };
             if (p.box) {
                 const int boxes = p.unit / p.box, at = lane * p.box;
@@ -637,13 +639,13 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
 }
 
 // ------------------------------------------------------------------ the tree itself, and the join
-// A CTA per token and eight heads, a warp to a head.  Which nodes the token sees and where their keys lie is looked up once, the nodes
-// are taken before the launch with the records has to have ended.  A warp's halves take turns at nodes and records, 16 lanes with eight
-// dims each, four nodes of a half under way; binary32 throughout.
+// A CTA per token and eight heads, a warp to a head.  Which nodes the token sees and where their keys lie is looked up once, and
+// the records of the units' launch are joined by the same warp: its halves take turns at nodes and records, 16 lanes with eight dims
+// each, four nodes of a half under way; binary32 throughout.
 constexpr int kTjHeads = 8, kTjUnroll = 4;
 template <class D>
 __global__ void __launch_bounds__(kTjHeads * 32, 4)
-tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *__restrict__ ws)
+tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *ws)
 {
     __shared__ long long place[64 * kPlanMaxWords];             // element of the pools (before the head) of each visible node
     __shared__ int counts[8];
@@ -652,34 +654,26 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *__rest
     const int parts = (a.n_heads + kTjHeads - 1) / kTjHeads, tok = (int)(blockIdx.x / (unsigned)parts), h = (int)(blockIdx.x % (unsigned)parts) * kTjHeads + warp;
     const bool on = h < a.n_heads, in = d0 < hd;
     const int kh = on ? h / G : 0, g = h - kh * G;
-    // the last sequence that starts at or before the token (32 at a time)
-    const int tokens = tree_tokens(a);
+    // what does not depend on the launch before this one
     uint4 q16 = make_uint4(0, 0, 0, 0);
-    if (on && in && tok < tokens) q16 = *reinterpret_cast<const uint4 *>(a.q + (long long)tok * a.ldq + (long long)h * hd + d0);
-    int b = 0;
-    for (int n = a.n_seq; n > 1;) {
-        const int step = (n + 31) / 32, at = b + lane * step;
-        const bool before = lane * step < n && __ldg(a.start + at) <= tok;
-        const int k = 31 - __clz(__ballot_sync(0xffffffffu, before) | 1u);
-        b += k * step;
-        n = min(step, n - k * step);
-    }
-    const TreeSeq s = tree_load(a, b);
+    if (on && in) q16 = *reinterpret_cast<const uint4 *>(a.q + (long long)tok * a.ldq + (long long)h * hd + d0);
+    const unsigned long long bits = tid >> 6 < a.words ? (unsigned long long)a.mask[(long long)tok * a.words + (tid >> 6)] : 0ull;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const TreeTotals totals = *reinterpret_cast<const TreeTotals *>(ws);
+    const int b = reinterpret_cast<const int *>(ws + p.off_seq)[tok];
+    if (tok >= totals.tokens || b < 0 || b >= a.n_seq) return;
+    const TreeFirst s = reinterpret_cast<const TreeFirst *>(ws + sizeof(TreeTotals))[b];
     const int node = tok - s.t0;
-    if (tok >= tokens || node < 0 || node >= s.nodes) return;   // (more nodes than there may be: counted, not computed)
-    // the nodes that this one sees; a thread per bit, a warp per half word
-    bool sees = false;
+    if (node < 0 || node >= s.nodes) return;                    // (more nodes than there may be: counted, not computed)
+    // the nodes that this one sees; a thread per bit, a warp per half word (a length below the number of nodes: the first have no key)
     const int key = s.base + tid;
-    if (tid >> 6 < a.words && tid < s.nodes && key >= 0) {      // (a length below the number of nodes: the first have no key)
-        const unsigned long long bits = (unsigned long long)__ldg(a.mask + (long long)tok * a.words + (tid >> 6));
-        sees = bits >> (tid & 63) & 1;
-    }
+    const bool sees = (bits >> (tid & 63) & 1) && tid < s.nodes && key >= 0;
     const uint32_t seen = __ballot_sync(0xffffffffu, sees);
     if (lane == 0) counts[warp] = __popc(seen);
     long long at = 0;
     if (sees || (tid == node && key >= 0)) {
         const unsigned pg = (unsigned)key / (unsigned)a.page_size, row = (unsigned)key - pg * (unsigned)a.page_size;
-        int page = __ldg(a.page_table + (long long)b * a.ld_table + pg);
+        int page = a.page_table[(long long)b * a.ld_table + pg];
         const bool bad = page < 0 || page >= a.n_pages;
         // a page that is none counts where its first key is
         if (bad && tid == node && row == 0 && h == warp && a.st) atomicAdd(&a.st->out_of_range, 1ull);
@@ -748,10 +742,8 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *__rest
             }
         }
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (!on) return;
     // ---- records: of the CTAs that had units of the head's items
-    const TreeTotals totals = *reinterpret_cast<const TreeTotals *>(ws + (size_t)a.n_seq * sizeof(TreeFirst));
     const AttentionDeal deal = tree_deal(p, totals);
     const int sums = p.two ? 1 : 2;
     auto records = [&](bool own, long long item, int in_rec, long long unit0, int n_units) {
@@ -780,20 +772,19 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *__rest
     };
     if (p.pre_tiles) {
         const unsigned in_all = (unsigned)(tok * G + g), rt = in_all / (unsigned)p.rows;
-        const long long item = (long long)kh * tree_tiles(tokens * G, p.rows) + rt;
+        const long long item = (long long)kh * totals.pre_rt + rt;
         records(false, item, (int)(in_all - rt * p.rows), item * p.pre_tiles, p.pre_tiles);
     }
-    if (s.ctx) {
-        const TreeFirst first = reinterpret_cast<const TreeFirst *>(ws)[b];
+    if (s.base > 0) {
         const unsigned in_seq = (unsigned)(node * G + g), rt = in_seq / (unsigned)p.rows;
-        const int within = kh * tree_tiles(s.nodes * G, p.rows) + (int)rt;
-        records(true, first.item + within, (int)(in_seq - rt * p.rows), totals.pre + first.unit + (long long)within * first.tiles, first.tiles);
+        const int within = kh * s.n_rt + (int)rt;
+        records(true, s.item + within, (int)(in_seq - rt * p.rows), totals.pre + s.unit + (long long)within * s.tiles, s.tiles);
     }
     // ---- the halves together
     const float m1 = __shfl_xor_sync(0xffffffffu, m, 16), l1 = __shfl_xor_sync(0xffffffffu, l, 16);
     const float to = fmaxf(m, m1), base = to == -CUDART_INF_F ? 0.0f : to, f = exp2_fast(m - base), e = exp2_fast(m1 - base);
     const float inv = 1.0f / (l * f + l1 * e);
-    const bool none = nodes == 0 && s.ctx == 0 && a.prefix_len == 0;
+    const bool none = nodes == 0 && s.base <= 0 && a.prefix_len == 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = none ? 0.0f : (o[j] * f + __shfl_xor_sync(0xffffffffu, o[j], 16) * e) * inv;
     if (in && half == 0)

@@ -14,31 +14,32 @@ struct TreePlan {
     int unit, box;               // keys of a unit, of one tiled copy (0: 16-byte copies)
     int ctas, pre_rt, pre_tiles; // grid; most row tiles of the prefix; units of a prefix item
     int pre_rec, own_rec;        // rows of a record, of one sum each
-    // scratch: per sequence the first own unit and item (TreeFirst[n_seq]), the totals; records
-    size_t off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
+    // scratch: the totals, per sequence its first own unit and item (TreeFirst[n_seq]), every token's sequence; records
+    size_t off_seq, off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
 };
-struct TreeFirst { long long unit; int item, tiles; };
-struct TreeTotals { long long pre, own; int tokens, pad; };
+struct alignas(16) TreeFirst { long long unit; int item, tiles, t0, nodes, base, n_rt; };
+struct alignas(16) TreeTotals { long long pre, own; int tokens, pre_rt; };
 
 // A sequence's new tokens and the keys before them, clamped.
-struct TreeSeq { int t0, nodes, ctx, base; bool bad; };      // base: key of node 0
+struct TreeSeq { int t0, t1, nodes, ctx, base; bool bad; };  // base: key of node 0
 __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs &a, int s0, int s1, int len)
 {
     const int cap = (int)min(a.max_own, a.pages_per_seq * a.page_size);
     TreeSeq s;
     s.t0 = min(max(s0, 0), a.max_tokens);
-    const int t1 = min(max(s1, s.t0), a.max_tokens), l = min(max(len, 0), cap);
-    s.nodes = min(t1 - s.t0, a.max_nodes);
+    s.t1 = min(max(s1, s.t0), a.max_tokens);
+    const int l = min(max(len, 0), cap);
+    s.nodes = min(s.t1 - s.t0, a.max_nodes);
     s.base = l - s.nodes;
     s.ctx = max(s.base, 0);
-    s.bad = s.t0 != s0 || t1 != s1 || s.nodes != t1 - s.t0 || l != len || l < s.nodes;
+    s.bad = s.t0 != s0 || s.t1 != s1 || s.nodes != s.t1 - s.t0 || l != len || l < s.nodes;
     return s;
 }
 __device__ __forceinline__ TreeSeq tree_load(const TreeArgs &a, int b)
 {
-    return b < a.n_seq ? tree_seq(a, __ldg(a.start + b), __ldg(a.start + b + 1), __ldg(a.own_len + b)) : TreeSeq{0, 0, 0, 0, false};
+    return b < a.n_seq ? tree_seq(a, a.start[b], a.start[b + 1], a.own_len[b]) : TreeSeq{0, 0, 0, 0, 0, false};
 }
-__device__ __forceinline__ int tree_tokens(const TreeArgs &a) { return min(max(__ldg(a.start + a.n_seq), 0), a.max_tokens); }
+__device__ __forceinline__ int tree_tokens(const TreeArgs &a) { return min(max(a.start[a.n_seq], 0), a.max_tokens); }
 __device__ __forceinline__ int tree_tiles(int n, int of) { return (int)(((unsigned)n + (unsigned)of - 1) / (unsigned)of); }
 
 // own units and items of 32 sequences: the lane's, and those before it
@@ -51,7 +52,7 @@ __device__ __forceinline__ TreeScan tree_scan(const TreeArgs &a, const TreePlan 
     r.units = (long long)r.items * tree_tiles(s.ctx, p.unit);
     long long u = r.units;
     int i = r.items;
-#pragma unroll
+#pragma unroll 1
     for (int x = 1; x < 32; x <<= 1) {
         const long long v = __shfl_up_sync(0xffffffffu, u, x);
         const int w = __shfl_up_sync(0xffffffffu, i, x);
@@ -61,29 +62,51 @@ __device__ __forceinline__ TreeScan tree_scan(const TreeArgs &a, const TreePlan 
     r.item0 = i - r.items;
     return r;
 }
-// All units; every warp computes them.  `lead`: the one warp that counts what is out of range and leaves the sequences' firsts.
-// s0, c0: what the lane has of the first 32 sequences.
-__device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreePlan &p, unsigned char *ws, bool lead, TreeSeq &s0, TreeScan &c0)
+// All units; every CTA computes them for itself.  s0, c0: what the lane has of the first 32 sequences.
+__device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreePlan &p, TreeSeq &s0, TreeScan &c0)
 {
-    const int lane = threadIdx.x & 31;
-    TreeTotals t = {0, 0, tree_tokens(a), 0};
-    t.pre = (long long)a.n_kv * tree_tiles(t.tokens * p.group, p.rows) * p.pre_tiles;
-    int items = 0;
+    TreeTotals t;
+    t.tokens = tree_tokens(a);
+    t.own = 0;
     for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
-        const TreeSeq s = tree_load(a, b0 + lane);
+        const TreeSeq s = tree_load(a, b0 + (int)(threadIdx.x & 31));
         const TreeScan c = tree_scan(a, p, s);
         if (b0 == 0) {
             s0 = s;
             c0 = c;
         }
-        if (lead && b0 + lane < a.n_seq) {
-            reinterpret_cast<TreeFirst *>(ws)[b0 + lane] = {t.own + c.unit0, items + c.item0, tree_tiles(s.ctx, p.unit)};
+        t.own += __shfl_sync(0xffffffffu, c.unit0 + c.units, 31);
+    }
+    t.pre_rt = tree_tiles(t.tokens * p.group, p.rows);
+    t.pre = (long long)a.n_kv * t.pre_rt * p.pre_tiles;
+    return t;
+}
+// What the join needs, in scratch: every ctas'th sequence's first unit and item, and the sequence of its tokens.  Lengths and starts out
+// of range are counted here, once.
+__device__ __forceinline__ void tree_leave(const TreeArgs &a, const TreePlan &p, unsigned char *ws, int cta)
+{
+    const int lane = threadIdx.x & 31;
+    TreeFirst *const first = reinterpret_cast<TreeFirst *>(ws + sizeof(TreeTotals));
+    int *const seq_of = reinterpret_cast<int *>(ws + p.off_seq);
+    long long units = 0;
+    int items = 0;
+    for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
+        const TreeSeq s = tree_load(a, b0 + lane);
+        const TreeScan c = tree_scan(a, p, s);
+        const bool mine = b0 + lane < a.n_seq && (unsigned)(b0 + lane) % (unsigned)p.ctas == (unsigned)cta;
+        if (mine) {
+            first[b0 + lane] = {units + c.unit0, items + c.item0, tree_tiles(s.ctx, p.unit), s.t0, s.nodes, s.base, tree_tiles(s.nodes * p.group, p.rows)};
             if (s.bad && a.st) atomicAdd(&a.st->out_of_range, 1ull);
         }
-        t.own += __shfl_sync(0xffffffffu, c.unit0 + c.units, 31);
+        for (uint32_t left = __ballot_sync(0xffffffffu, mine); left; left &= left - 1) {
+            const int src = __ffs(left) - 1, b = b0 + src, t0 = __shfl_sync(0xffffffffu, s.t0, src), t1 = __shfl_sync(0xffffffffu, s.t1, src);
+            for (int t = t0 + lane; t < t1; t += 32) seq_of[t] = b;
+            if (b == 0)
+                for (int t = lane; t < t0; t += 32) seq_of[t] = -1;         // (starts that do not begin at zero)
+        }
+        units += __shfl_sync(0xffffffffu, c.unit0 + c.units, 31);
         items += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
     }
-    return t;
 }
 
 // What a CTA has of an item: units tile .. tile + count - 1 of a segment's keys on one row tile of one key head.
