@@ -5,14 +5,14 @@
 // keys are taken one by one by the launch that joins the parts, which so never touches a key or value that its row does not see.
 //
 //   S = Q K^T   Q and K in shared memory          -> S in TMEM
-//   P = 2^((S - m) scale), a thread to a row, 16-bit, in TMEM over the S it came from
+//   P = 2^((S - m) scale), two threads to a row, 16-bit, in TMEM over the S it came from
 //   O += P V    P in TMEM, V in shared memory     -> O in TMEM
 // with the maximum m of a row moving only when a new one exceeds it by more than 8 (a factor of 256), so that O is hardly ever
 // rescaled.  Two such sums are under way in a CTA, so that one's products run under the other's exponentials: two row tiles on
 // the same keys where a sequence has more than 128 rows to a key head, else the same rows on every other unit of keys.
 // A unit is 128 keys (or the whole pages that fit).  The units of all (segment, key head, row tile) items in a row are dealt out evenly
 // to a CTA per SM; where a CTA leaves an item it writes a record (m, sum, O of the keys it has seen) for each row and sum.
-// Warps: 0 copies keys and values, 1 issues the products, 2 brings the rows of Q, 3 says which items come, 4-7 and 8-11 the
+// Warps: 0 copies keys and values, 1 issues the products, 2 brings the rows of Q, 3 says which items come, 4-11 and 12-19 the
 // softmax of the two sums.
 #include <type_traits>
 
@@ -21,9 +21,9 @@
 
 namespace aweq {
 
-constexpr int kTrThreads = 384, kTrQBytes = 64 * 1024, kTrRing = 160 * 1024, kTrMaxTiles = 10, kTrItems = 4;
+constexpr int kTrThreads = 640, kTrQBytes = 64 * 1024, kTrRing = 160 * 1024, kTrMaxTiles = 10, kTrItems = 4;
 // registers of a softmax thread and of the others: together no more than the launch gives
-constexpr int kTrSoftRegs = 208, kTrOtherRegs = 80;
+constexpr int kTrSoftRegs = 104, kTrOtherRegs = 64;
 constexpr float kTrSlack = 8.0f;
 
 struct TreeShared {
@@ -31,8 +31,10 @@ struct TreeShared {
     uint64_t item_full[kTrItems], item_empty[kTrItems];
     TreeItem item[kTrItems];
     uint32_t tmem;
+    volatile int gave_up[8];             // by sum and TMEM quarter: a softmax warp has
+    float top[2][2][128];                // the halves' maxima, by sum and half; at the end of an item one half's l
 };
-constexpr size_t kTrSmem = 1024 + kTrQBytes + kTrRing + sizeof(TreeShared);
+constexpr size_t kTrSmem = kTrQBytes + kTrRing + sizeof(TreeShared);
 static_assert(kTrSmem <= 227 * 1024, "shared memory of a CTA");
 
 static size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -94,8 +96,6 @@ __device__ __forceinline__ long long tree_record(const TreePlan &p, bool own, lo
     const long long rec = row >> 32 ? row / n : (long long)((uint32_t)row / (uint32_t)n), in = row - rec * n;
     return rec * n * hd + (long long)(d >> 3) * n * 8 + in * 8;
 }
-__device__ __forceinline__ AttentionDeal tree_deal(const TreePlan &p, const TreeTotals &t) { return AttentionDeal(t.pre + t.own, p.ctas); }
-
 // The items of a CTA in turn, by a warp that works on them.
 struct TreeItems {
     int n = 0;
@@ -116,8 +116,7 @@ __global__ void __launch_bounds__(kTrThreads, 1)
 tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
                   const __grid_constant__ CUtensorMap mapQ, unsigned char *ws)
 {
-    extern __shared__ unsigned char raw[];
-    unsigned char *const qs = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) unsigned char qs[];       // (there is no room to round an address up)
     unsigned char *const tiles = qs + kTrQBytes;
     TreeShared &sh = *reinterpret_cast<TreeShared *>(tiles + kTrRing);
     // (the warp's number by a shuffle, so that the compiler knows that a warp has one: the products' operands live in uniform registers)
@@ -132,14 +131,15 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             mbar_init(&sh.q_ready[i], 1);
             mbar_init(&sh.q_free[i], 1);
             mbar_init(&sh.s_full[i], 1);
-            mbar_init(&sh.p_ready[i], 4);
+            mbar_init(&sh.p_ready[i], 8);
             mbar_init(&sh.pv_done[i], 1);
-            mbar_init(&sh.o_free[i], 4);
+            mbar_init(&sh.o_free[i], 8);
         }
         for (int i = 0; i < kTrItems; ++i) {
             mbar_init(&sh.item_full[i], 1);
-            mbar_init(&sh.item_empty[i], 11);
+            mbar_init(&sh.item_empty[i], 19);
         }
+        for (int i = 0; i < 8; ++i) sh.gave_up[i] = 0;
         mbar_init_fence();
         if (p.box) {
             tma_prefetch_map(&mapK);
@@ -162,9 +162,12 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
             TreeSeq s0 = {};
             TreeScan c0 = {};
-            const TreeTotals totals = tree_totals(a, p, s0, c0);
+            TreeTotals totals = tree_totals(a, p, s0, c0);
+            const AttentionDeal deal(totals.pre + totals.own, p.ctas);
+            totals.each = deal.each;
+            totals.more = deal.more;
+            totals.ctas = deal.ctas;
             if (cta == 0 && lane == 0) *reinterpret_cast<TreeTotals *>(ws) = totals;
-            const AttentionDeal deal = tree_deal(p, totals);
             long long u0 = 0;
             int left = 0;
             TreeWalk w;
@@ -478,13 +481,18 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             ok = ok && more >= 0;
         }
     } else {
-        // -------------------------------------------------------------- softmax: a thread to a row
+        // -------------------------------------------------------------- softmax: two threads to a row, half of a unit's keys each
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTrSoftRegs));
-        const int sum = (warp - 4) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
+        const int sum = (warp - 4) >> 3, half = (warp - 4) >> 2 & 1, q4 = warp & 3, r = q4 * 32 + lane, pair = sum * 4 + q4;
         const uint32_t at = tmem + sum * 128 + ((uint32_t)(q4 * 32) << 16), acc = at + 256;
         const bool turn = a.scale < 0.0f;                       // a negative scale turns the scores' signs; a zero one must leave -inf as it is
         const float scale = (a.scale == 0.0f ? 1.17549435e-38f : fabsf(a.scale)) * 1.4426950408889634f;
         constexpr float kShift = D::kBf16 ? 0.0f : kProbabilityShift;
+        // The two warps that share 32 rows wait for one another; one that gives up says so and arrives for the other.
+        auto meet = [&] {
+            named_bar_sync(1 + pair, 64);
+            return !sh.gave_up[pair];
+        };
         TreeItems items;
         // The first pass, on a unit that there is not, keeps nothing: it brings the code in while the first keys are under way (the
         // products wait for its P).  cnt: passes; the products of the first do not exist.
@@ -511,7 +519,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                         const int t = 2 * (done + u) + 1, stage = t % n_tiles;
                         if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.full[stage], (t / n_tiles) & 1)))) break;
                         unsigned char *const vt = tiles + stage * tile_bytes;
-                        for (int i = r; i < zeros * halves * 8; i += 128) {
+                        for (int i = half * 128 + r; i < zeros * halves * 8; i += 256) {
                             const int piece = i % (halves * 8);
                             *reinterpret_cast<uint4 *>(vt + (piece >> 3) * 16384 + (keys + i / (halves * 8)) * 128 + ((piece & 7) << 4)) = make_uint4(0, 0, 0, 0);
                         }
@@ -520,38 +528,43 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     if (!warm && !(ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[sum], (cnt - 1) & 1)))) break;
                     tc_fence_after();
                     if (live) {
-                        uint32_t x[4][32];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) tc_ld32(at + c * 32, x[c]);
+                        uint32_t x[2][32];
+                        tc_ld32(at + half * 64, x[0]);
+                        tc_ld32(at + half * 64 + 32, x[1]);
                         tc_wait_ld();
                         if (turn)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c)
+                            for (int c = 0; c < 2; ++c)
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) x[c][j] ^= 0x80000000u;
-                        if (keys < 128)
+                        if (keys < half * 64 + 64)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c)
+                            for (int c = 0; c < 2; ++c)
 #pragma unroll
                                 for (int j = 0; j < 32; ++j)
-                                    if (c * 32 + j >= keys) x[c][j] = 0xff800000u;
+                                    if (half * 64 + c * 32 + j >= keys) x[c][j] = 0xff800000u;
                         float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
+                        for (int c = 0; c < 2; ++c)
 #pragma unroll
                             for (int j = 0; j < 32; j += 2) top[(j >> 1) & 3] = fmax3(top[(j >> 1) & 3], __uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1]));
-                        const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                        // the other half's maximum; past this barrier both have their scores in registers, so that P may overwrite them
+                        // (and the next pass's maxima come when both have said that P is there)
+                        float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                        sh.top[sum][half][r] = t;
+                        if (!(ok = meet())) break;
+                        t = fmaxf(t, sh.top[sum][half ^ 1][r]);
                         const bool above = (t - m) * scale > kTrSlack;
                         if (fresh) m = t;
                         else if (__any_sync(0xffffffffu, above && r < mine)) {
-                            // a maximum well above the reference: O and l move to it
+                            // a maximum well above the reference: O (half of it here) and l move to it
                             if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.pv_done[sum], cnt & 1)))) break;       // (pass cnt - 1)
                             tc_fence_after();
                             const float to = above ? t : m, f = to == -CUDART_INF_F ? 1.0f : exp2_fast((m - to) * scale);
                             m = to;
                             l *= f;
 #pragma unroll 1
-                            for (int c = 0; c < hd; c += 16) {
+                            for (int c = half * 64; c < min(hd, half * 64 + 64); c += 16) {
                                 uint32_t o[16];
                                 tc_ld16(acc + c, o);
                                 tc_wait_ld();
@@ -565,7 +578,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                         const float2 from2 = make_float2(-from, -from), scale2 = make_float2(scale, scale), shift2 = make_float2(kShift, kShift);
                         float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
+                        for (int c = 0; c < 2; ++c)
 #pragma unroll
                             for (int j = 0; j < 32; j += 2) {
                                 const float2 d = __ffma2_rn(__fadd2_rn(make_float2(__uint_as_float(x[c][j]), __uint_as_float(x[c][j + 1])), from2), scale2, shift2);
@@ -573,11 +586,10 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                                 part[j & 2] += e;
                                 part[(j & 2) + 1] += f;
                                 // rounded to the 16-bit type for the product with v; the sum takes the unrounded ones (see probability_base)
-                                x[c >> 1][(c & 1) * 16 + j / 2] = D::encode2(e, f);
+                                x[0][c * 16 + j / 2] = D::encode2(e, f);
                             }
+                        tc_st32(at + half * 32, x[0]);
                         l += (part[0] + part[1]) + (part[2] + part[3]);
-                        tc_st32(at, x[0]);
-                        tc_st32(at + 32, x[1]);
                         tc_wait_st();
                     }
                     tc_fence_before();
@@ -597,18 +609,22 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             const long long rec = it.rec + (TWO ? sum * p.part : sum * (it.own ? p.own_rec : p.pre_rec)) + r;       // (its number among all rows)
             float2 *const ml = reinterpret_cast<float2 *>(ws + (it.own ? p.off_own_ml : p.off_pre_ml));
             if (fresh) {
-                if (r < mine) ml[rec] = make_float2(-CUDART_INF_F, 0.0f);       // the item had no unit for this sum
+                if (r < mine && !half) ml[rec] = make_float2(-CUDART_INF_F, 0.0f);      // the item had no unit for this sum
                 continue;
             }
             if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.pv_done[sum], cnt & 1)))) break;                      // (pass cnt - 1)
             tc_fence_after();
             if (live) {
+                if (half) sh.top[sum][1][r] = l;
+                if (!(ok = meet())) break;
+                if (r < mine && !half) ml[rec] = make_float2(m == -CUDART_INF_F ? m : __fmul_rn(m, scale) - kShift, l + sh.top[sum][1][r]);
                 // (eight dims of every row side by side, so that a warp's stores lie together)
                 float *const dst = reinterpret_cast<float *>(ws + (it.own ? p.off_own_o : p.off_pre_o)) + tree_record(p, it.own, rec, 0, hd);
                 const int step = (it.own ? p.own_rec : p.pre_rec) * 8;
 #pragma unroll 1
-                for (int c = 0; c < hd; c += 32) {
+                for (int c = half * 64; c < min(hd, half * 64 + 64); c += 32) {
                     uint32_t o[32];
+                    __syncwarp();
                     tc_ld32(acc + c, o);
                     tc_wait_ld();
                     if (r < mine)
@@ -619,14 +635,17 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                                 to[0] = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
                                 to[1] = make_uint4(o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
                             }
-                    __syncwarp();
                 }
-                if (r < mine) ml[rec] = make_float2(m == -CUDART_INF_F ? m : __fmul_rn(m, scale) - kShift, l);
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.o_free[sum]);
         } while (!it.stop);
+        if (!ok) {
+            if (lane == 0) sh.gave_up[pair] = 1;
+            __syncwarp();
+            named_bar_arrive(1 + pair, 64);
+        }
     }
     if (!ok && lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
     tc_fence_before();
@@ -743,42 +762,54 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *ws)
         }
     }
     if (!on) return;
-    // ---- records: of the CTAs that had units of the head's items
-    const AttentionDeal deal = tree_deal(p, totals);
+    // ---- records: of the CTAs that had units of the head's items, on the prefix and on the sequence's own keys.  Four lanes find the first
+    // and the last CTA of the two.
     const int sums = p.two ? 1 : 2;
-    auto records = [&](bool own, long long item, int in_rec, long long unit0, int n_units) {
-        const float *const ro = reinterpret_cast<const float *>(ws + (own ? p.off_own_o : p.off_pre_o));
-        const float2 *const rml = reinterpret_cast<const float2 *>(ws + (own ? p.off_own_ml : p.off_pre_ml));
-        const int n = own ? p.own_rec : p.pre_rec, c0 = deal.cta_of(unit0), c1 = n_units > 1 ? deal.cta_of(unit0 + n_units - 1) : c0;
-        const int records = (c1 - c0 + 1) * sums;
-        const long long rec0 = (item + c0) * sums;              // the first record; the others follow
-        for (int i = half; i < records; i += 2) {
-            const long long rec = rec0 + i;
-            const float2 y = rml[rec * n + in_rec];
-            float4 v0 = make_float4(0, 0, 0, 0), v1 = v0;
-            if (in) {
-                const float *src = ro + rec * n * hd + (long long)d0 * n + in_rec * 8;
-                v0 = *reinterpret_cast<const float4 *>(src);
-                v1 = *reinterpret_cast<const float4 *>(src + 4);
-            }
-            if (y.x == -CUDART_INF_F && y.y == 0.0f) continue;  // (its output may be anything)
-            const float to = fmaxf(m, y.x), f = m == -CUDART_INF_F ? 0.0f : exp2_fast(m - to), e = exp2_fast(y.x - to);
-            l = l * f + y.y * e;                                // (a sum that is no number stays one)
-            m = to;
-            const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+    const unsigned in_all = (unsigned)(tok * G + g), in_seq = (unsigned)(node * G + g), rt0 = in_all / (unsigned)p.rows, rt1 = in_seq / (unsigned)p.rows;
+    const long long item0 = (long long)kh * totals.pre_rt + rt0;
+    const int within = kh * s.n_rt + (int)rt1, item1 = s.item + within;
+    const long long u = lane & 2 ? totals.pre + s.unit + (long long)within * s.tiles + (lane & 1 ? s.tiles - 1 : 0)
+                                 : item0 * p.pre_tiles + (lane & 1 ? p.pre_tiles - 1 : 0);
+    AttentionDeal deal(0, 1);
+    deal.each = totals.each;
+    deal.more = totals.more;
+    const bool there = lane & 2 ? s.base > 0 : p.pre_tiles > 0;
+    const int c = there ? deal.cta_of(u) : lane & 1 ? -1 : 0;
+    const int c0 = __shfl_sync(0xffffffffu, c, 0), n0 = (__shfl_sync(0xffffffffu, c, 1) - c0 + 1) * sums;
+    const int c2 = __shfl_sync(0xffffffffu, c, 2), n1 = (__shfl_sync(0xffffffffu, c, 3) - c2 + 1) * sums;
+    const long long rec0 = (item0 + c0) * sums, rec1 = (long long)(item1 + c2) * sums - n0;
+    const int in0 = (int)(in_all - rt0 * (unsigned)p.rows), in1 = (int)(in_seq - rt1 * (unsigned)p.rows);
+    constexpr int U = 2;
+    for (int i0 = half; i0 < n0 + n1; i0 += 2 * U) {
+        float2 y[U];
+        float4 v[U][2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = o[j] * f + v[j] * e;
+        for (int i = 0; i < U; ++i) {
+            const int k = i0 + 2 * i;
+            const bool own = k >= n0;
+            const int n = own ? p.own_rec : p.pre_rec, row = own ? in1 : in0;
+            const long long rec = (own ? rec1 : rec0) + k;
+            y[i] = make_float2(-CUDART_INF_F, 0.0f);
+            v[i][0] = v[i][1] = make_float4(0, 0, 0, 0);
+            if (k < n0 + n1) {
+                y[i] = reinterpret_cast<const float2 *>(ws + (own ? p.off_own_ml : p.off_pre_ml))[rec * n + row];
+                const float *src = reinterpret_cast<const float *>(ws + (own ? p.off_own_o : p.off_pre_o)) + rec * n * hd + d0 * n + row * 8;
+                if (in) {
+                    v[i][0] = *reinterpret_cast<const float4 *>(src);
+                    v[i][1] = *reinterpret_cast<const float4 *>(src + 4);
+                }
+            }
         }
-    };
-    if (p.pre_tiles) {
-        const unsigned in_all = (unsigned)(tok * G + g), rt = in_all / (unsigned)p.rows;
-        const long long item = (long long)kh * totals.pre_rt + rt;
-        records(false, item, (int)(in_all - rt * p.rows), item * p.pre_tiles, p.pre_tiles);
-    }
-    if (s.base > 0) {
-        const unsigned in_seq = (unsigned)(node * G + g), rt = in_seq / (unsigned)p.rows;
-        const int within = kh * s.n_rt + (int)rt;
-        records(true, s.item + within, (int)(in_seq - rt * p.rows), totals.pre + s.unit + (long long)within * s.tiles, s.tiles);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (y[i].x == -CUDART_INF_F && y[i].y == 0.0f) continue;    // (its output may be anything)
+            const float to = fmaxf(m, y[i].x), f = m == -CUDART_INF_F ? 0.0f : exp2_fast(m - to), e = exp2_fast(y[i].x - to);
+            l = l * f + y[i].y * e;                             // (a sum that is no number stays one)
+            m = to;
+            const float w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = o[j] * f + w[j] * e;
+        }
     }
     // ---- the halves together
     const float m1 = __shfl_xor_sync(0xffffffffu, m, 16), l1 = __shfl_xor_sync(0xffffffffu, l, 16);

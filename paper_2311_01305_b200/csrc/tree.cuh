@@ -18,7 +18,7 @@ struct TreePlan {
     size_t off_seq, off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
 };
 struct alignas(16) TreeFirst { long long unit; int item, tiles, t0, nodes, base, n_rt; };
-struct alignas(16) TreeTotals { long long pre, own; int tokens, pre_rt; };
+struct alignas(16) TreeTotals { long long pre, own, each, more; int tokens, pre_rt, ctas; };     // each, more, ctas: how the units are dealt
 
 // A sequence's new tokens and the keys before them, clamped.
 struct TreeSeq { int t0, t1, nodes, ctx, base; bool bad; };  // base: key of node 0
