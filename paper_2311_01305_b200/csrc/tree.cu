@@ -658,24 +658,23 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
 }
 
 // ------------------------------------------------------------------ the tree itself, and the join
-// A CTA per token and eight heads, a warp to a head.  Which nodes the token sees and where their keys lie is looked up once, and
-// the records of the units' launch are joined by the same warp: its halves take turns at nodes and records, 16 lanes with eight dims
-// each, four nodes of a half under way; binary32 throughout.
-constexpr int kTjHeads = 8, kTjUnroll = 4;
-template <class D>
-__global__ void __launch_bounds__(kTjHeads * 32, 4)
-tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *ws)
+// A CTA per token and run of its heads.  Which nodes the token sees and where their keys lie is looked up once; a warp takes HB heads of
+// one key head at a time, for which it reads a node's key and value once, joins the nodes with the records of the units' launch, and
+// writes the heads.  Its halves take turns at nodes and records, 16 lanes with eight dims each; binary32 throughout.  Bound by its
+// instructions: with a warp to a single head 990 of them a row and 67 us for 1548 tokens of 32 heads.
+constexpr int kTjWarps = 8;
+template <class D, int HB>
+__global__ void __launch_bounds__(kTjWarps * 32, HB == 4 ? 2 : 3)
+tree_join_kernel(const TreeArgs a, const TreePlan p, int parts, const unsigned char *ws)
 {
+    constexpr int U = HB == 4 ? 2 : 4;                          // nodes of a half under way
     __shared__ long long place[64 * kPlanMaxWords];             // element of the pools (before the head) of each visible node
-    __shared__ int counts[8];
+    __shared__ int counts[kTjWarps];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, half = lane >> 4, d0 = (lane & 15) * 8, hd = a.head_dim, G = p.group;
-    const int parts = (a.n_heads + kTjHeads - 1) / kTjHeads, tok = (int)(blockIdx.x / (unsigned)parts), h = (int)(blockIdx.x % (unsigned)parts) * kTjHeads + warp;
-    const bool on = h < a.n_heads, in = d0 < hd;
-    const int kh = on ? h / G : 0, g = h - kh * G;
-    // what does not depend on the launch before this one
-    uint4 q16 = make_uint4(0, 0, 0, 0);
-    if (on && in) q16 = *reinterpret_cast<const uint4 *>(a.q + (long long)tok * a.ldq + (long long)h * hd + d0);
+    const int tok = (int)(blockIdx.x / (unsigned)parts), part = (int)(blockIdx.x - (unsigned)tok * (unsigned)parts), blocks = a.n_heads / HB;
+    const bool in = d0 < hd;
+    // (does not depend on the launch before this one)
     const unsigned long long bits = tid >> 6 < a.words ? (unsigned long long)a.mask[(long long)tok * a.words + (tid >> 6)] : 0ull;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const TreeTotals totals = *reinterpret_cast<const TreeTotals *>(ws);
@@ -695,132 +694,162 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, const unsigned char *ws)
         int page = a.page_table[(long long)b * a.ld_table + pg];
         const bool bad = page < 0 || page >= a.n_pages;
         // a page that is none counts where its first key is
-        if (bad && tid == node && row == 0 && h == warp && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+        if (bad && tid == node && row == 0 && part == 0 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
         if (bad) page = 0;
         at = (long long)page * a.page_stride + (long long)row * a.token_stride;
     }
     __syncthreads();
     int nodes = 0, before = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kTjWarps; ++i) {
         if (i < warp) before += counts[i];
         nodes += counts[i];
     }
     if (sees) place[before + __popc(seen & ((1u << lane) - 1))] = at;
     __syncthreads();
-    float m = -CUDART_INF_F, l = 0.0f, o[8] = {};
     const float scale = a.scale * 1.4426950408889634f;
-    if (on) {
-        float q[8];
-        widen8<D>(q16, q);
-        for (int i0 = 0; i0 < nodes; i0 += 2 * kTjUnroll) {
-            uint4 k[kTjUnroll], v[kTjUnroll];
-            float sc[kTjUnroll];
+    const int sums = p.two ? 1 : 2;
+    const bool none = nodes == 0 && s.base <= 0 && a.prefix_len == 0;
+    for (int block = part * kTjWarps + warp; block < blocks; block += parts * kTjWarps) {
+        const int h = block * HB, kh = h / G, g = h - kh * G;
+        const long long kv = kh * a.head_stride + d0;
+        float q[HB][8], m[HB], l[HB], o[HB][8];
 #pragma unroll
-            for (int i = 0; i < kTjUnroll; ++i) {
-                const int n = i0 + 2 * i + half;
+        for (int i = 0; i < HB; ++i) {
+            m[i] = -CUDART_INF_F;
+            l[i] = 0.0f;
+            widen8<D>(in ? *reinterpret_cast<const uint4 *>(a.q + (long long)tok * a.ldq + (long long)(h + i) * hd + d0) : make_uint4(0, 0, 0, 0), q[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[i][j] = 0.0f;
+        }
+        // ---- nodes
+        for (int i0 = half; i0 < nodes + half; i0 += 2 * U) {   // (both halves make the same steps)
+            uint4 k[U], v[U];
+            float sc[U][HB];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int n = i0 + 2 * i;
                 k[i] = v[i] = make_uint4(0, 0, 0, 0);
                 if (n < nodes && in) {
-                    const long long x = place[n] + kh * a.head_stride + d0;
+                    const long long x = place[n] + kv;
                     k[i] = *reinterpret_cast<const uint4 *>(a.ck + x);
                     v[i] = *reinterpret_cast<const uint4 *>(a.cv + x);
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kTjUnroll; ++i) {
+            for (int i = 0; i < U; ++i) {
                 float f[8];
                 widen8<D>(k[i], f);
-                sc[i] = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sc[i] = __fmaf_rn(q[j], f[j], sc[i]);
+                for (int c = 0; c < HB; ++c) {
+                    sc[i][c] = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sc[i][c] = __fmaf_rn(q[c][j], f[j], sc[i][c]);
+                }
             }
 #pragma unroll
             for (int y = 8; y > 0; y >>= 1)
 #pragma unroll
-                for (int i = 0; i < kTjUnroll; ++i) sc[i] += __shfl_xor_sync(0xffffffffu, sc[i], y);
-            float to = m;
+                for (int i = 0; i < U; ++i)
 #pragma unroll
-            for (int i = 0; i < kTjUnroll; ++i) {
-                sc[i] = i0 + 2 * i + half < nodes ? sc[i] * scale : -CUDART_INF_F;
-                to = fmaxf(to, sc[i]);
+                    for (int c = 0; c < HB; ++c) sc[i][c] += __shfl_xor_sync(0xffffffffu, sc[i][c], y);
+#pragma unroll
+            for (int c = 0; c < HB; ++c) {
+                float to = m[c];
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    sc[i][c] = i0 + 2 * i < nodes ? sc[i][c] * scale : -CUDART_INF_F;
+                    to = fmaxf(to, sc[i][c]);
+                }
+                const float base = to == -CUDART_INF_F ? 0.0f : to, f = exp2_fast(m[c] - base);
+                m[c] = to;
+                l[c] *= f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[c][j] *= f;
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    // (a node that there is not has the value zero, and no part in the sum)
+                    sc[i][c] = i0 + 2 * i < nodes ? exp2_fast(sc[i][c] - base) : 0.0f;
+                    l[c] += sc[i][c];
+                }
             }
-            const float base = to == -CUDART_INF_F ? 0.0f : to, f = exp2_fast(m - base);
-            m = to;
-            l *= f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] *= f;
-#pragma unroll
-            for (int i = 0; i < kTjUnroll; ++i) {
-                if (i0 + 2 * i + half >= nodes) break;
-                const float e = exp2_fast(sc[i] - base);
+            for (int i = 0; i < U; ++i) {
                 float w[8];
                 widen8<D>(v[i], w);
-                l += e;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = __fmaf_rn(w[j], e, o[j]);
+                for (int c = 0; c < HB; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) o[c][j] = __fmaf_rn(w[j], sc[i][c], o[c][j]);
             }
         }
-    }
-    if (!on) return;
-    // ---- records: of the CTAs that had units of the head's items, on the prefix and on the sequence's own keys.  Four lanes find the first
-    // and the last CTA of the two.
-    const int sums = p.two ? 1 : 2;
-    const unsigned in_all = (unsigned)(tok * G + g), in_seq = (unsigned)(node * G + g), rt0 = in_all / (unsigned)p.rows, rt1 = in_seq / (unsigned)p.rows;
-    const long long item0 = (long long)kh * totals.pre_rt + rt0;
-    const int within = kh * s.n_rt + (int)rt1, item1 = s.item + within;
-    const long long u = lane & 2 ? totals.pre + s.unit + (long long)within * s.tiles + (lane & 1 ? s.tiles - 1 : 0)
-                                 : item0 * p.pre_tiles + (lane & 1 ? p.pre_tiles - 1 : 0);
-    AttentionDeal deal(0, 1);
-    deal.each = totals.each;
-    deal.more = totals.more;
-    const bool there = lane & 2 ? s.base > 0 : p.pre_tiles > 0;
-    const int c = there ? deal.cta_of(u) : lane & 1 ? -1 : 0;
-    const int c0 = __shfl_sync(0xffffffffu, c, 0), n0 = (__shfl_sync(0xffffffffu, c, 1) - c0 + 1) * sums;
-    const int c2 = __shfl_sync(0xffffffffu, c, 2), n1 = (__shfl_sync(0xffffffffu, c, 3) - c2 + 1) * sums;
-    const long long rec0 = (item0 + c0) * sums, rec1 = (long long)(item1 + c2) * sums - n0;
-    const int in0 = (int)(in_all - rt0 * (unsigned)p.rows), in1 = (int)(in_seq - rt1 * (unsigned)p.rows);
-    constexpr int U = 2;
-    for (int i0 = half; i0 < n0 + n1; i0 += 2 * U) {
-        float2 y[U];
-        float4 v[U][2];
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int k = i0 + 2 * i;
+        // ---- records: of the CTAs that had units of the key head's items, on the prefix and on the sequence's own keys.  Four lanes find
+        // the first and the last CTA of the two.  (The heads' rows follow one another, in one tile: tiles hold whole tokens, or one
+        // head at a time comes here.)
+        const unsigned in_all = (unsigned)(tok * G + g), in_seq = (unsigned)(node * G + g), rt0 = in_all / (unsigned)p.rows, rt1 = in_seq / (unsigned)p.rows;
+        const long long item0 = (long long)kh * totals.pre_rt + rt0;
+        const int within = kh * s.n_rt + (int)rt1;
+        const long long u = lane & 2 ? totals.pre + s.unit + (long long)within * s.tiles + (lane & 1 ? s.tiles - 1 : 0)
+                                     : item0 * p.pre_tiles + (lane & 1 ? p.pre_tiles - 1 : 0);
+        AttentionDeal deal(0, 1);
+        deal.each = totals.each;
+        deal.more = totals.more;
+        const bool there = lane & 2 ? s.base > 0 : p.pre_tiles > 0;
+        const int c = there ? deal.cta_of(u) : lane & 1 ? -1 : 0;
+        const int c0 = __shfl_sync(0xffffffffu, c, 0), n0 = (__shfl_sync(0xffffffffu, c, 1) - c0 + 1) * sums;
+        const int c2 = __shfl_sync(0xffffffffu, c, 2), n1 = (__shfl_sync(0xffffffffu, c, 3) - c2 + 1) * sums;
+        const long long rec0 = (item0 + c0) * sums, rec1 = (long long)(s.item + within + c2) * sums - n0;
+        const int in0 = (int)(in_all - rt0 * (unsigned)p.rows), in1 = (int)(in_seq - rt1 * (unsigned)p.rows);
+        for (int k = half; k < n0 + n1; k += 2) {
             const bool own = k >= n0;
             const int n = own ? p.own_rec : p.pre_rec, row = own ? in1 : in0;
             const long long rec = (own ? rec1 : rec0) + k;
-            y[i] = make_float2(-CUDART_INF_F, 0.0f);
-            v[i][0] = v[i][1] = make_float4(0, 0, 0, 0);
-            if (k < n0 + n1) {
-                y[i] = reinterpret_cast<const float2 *>(ws + (own ? p.off_own_ml : p.off_pre_ml))[rec * n + row];
-                const float *src = reinterpret_cast<const float *>(ws + (own ? p.off_own_o : p.off_pre_o)) + rec * n * hd + d0 * n + row * 8;
-                if (in) {
-                    v[i][0] = *reinterpret_cast<const float4 *>(src);
-                    v[i][1] = *reinterpret_cast<const float4 *>(src + 4);
-                }
+            const float2 *const ml = reinterpret_cast<const float2 *>(ws + (own ? p.off_own_ml : p.off_pre_ml)) + rec * n + row;
+            const float *const src = reinterpret_cast<const float *>(ws + (own ? p.off_own_o : p.off_pre_o)) + rec * n * hd + d0 * n + row * 8;
+            float2 y[HB];
+            float4 v[HB][2];
+#pragma unroll
+            for (int i = 0; i < HB; ++i) {
+                y[i] = ml[i];
+                v[i][0] = in ? *reinterpret_cast<const float4 *>(src + i * 8) : make_float4(0, 0, 0, 0);
+                v[i][1] = in ? *reinterpret_cast<const float4 *>(src + i * 8 + 4) : make_float4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < HB; ++i) {
+                if (y[i].x == -CUDART_INF_F && y[i].y == 0.0f) continue;        // (its output may be anything)
+                const float to = fmaxf(m[i], y[i].x), f = m[i] == -CUDART_INF_F ? 0.0f : exp2_fast(m[i] - to), e = exp2_fast(y[i].x - to);
+                l[i] = l[i] * f + y[i].y * e;                   // (a sum that is no number stays one)
+                m[i] = to;
+                const float w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[i][j] = o[i][j] * f + w[j] * e;
             }
         }
+        // ---- the halves together
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            if (y[i].x == -CUDART_INF_F && y[i].y == 0.0f) continue;    // (its output may be anything)
-            const float to = fmaxf(m, y[i].x), f = m == -CUDART_INF_F ? 0.0f : exp2_fast(m - to), e = exp2_fast(y[i].x - to);
-            l = l * f + y[i].y * e;                             // (a sum that is no number stays one)
-            m = to;
-            const float w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
+        for (int i = 0; i < HB; ++i) {
+            const float m1 = __shfl_xor_sync(0xffffffffu, m[i], 16), l1 = __shfl_xor_sync(0xffffffffu, l[i], 16);
+            const float to = fmaxf(m[i], m1), base = to == -CUDART_INF_F ? 0.0f : to, f = exp2_fast(m[i] - base), e = exp2_fast(m1 - base);
+            const float inv = 1.0f / (l[i] * f + l1 * e), f1 = f * inv, e1 = e * inv;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = o[j] * f + w[j] * e;
+            for (int j = 0; j < 8; ++j) o[i][j] = none ? 0.0f : o[i][j] * f1 + __shfl_xor_sync(0xffffffffu, o[i][j], 16) * e1;
+            if (in && half == 0)
+                *reinterpret_cast<uint4 *>(a.out + (long long)tok * a.ldo + (long long)(h + i) * hd + d0) =
+                    make_uint4(D::encode2(o[i][0], o[i][1]), D::encode2(o[i][2], o[i][3]), D::encode2(o[i][4], o[i][5]), D::encode2(o[i][6], o[i][7]));
         }
     }
-    // ---- the halves together
-    const float m1 = __shfl_xor_sync(0xffffffffu, m, 16), l1 = __shfl_xor_sync(0xffffffffu, l, 16);
-    const float to = fmaxf(m, m1), base = to == -CUDART_INF_F ? 0.0f : to, f = exp2_fast(m - base), e = exp2_fast(m1 - base);
-    const float inv = 1.0f / (l * f + l1 * e);
-    const bool none = nodes == 0 && s.base <= 0 && a.prefix_len == 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = none ? 0.0f : (o[j] * f + __shfl_xor_sync(0xffffffffu, o[j], 16) * e) * inv;
-    if (in && half == 0)
-        *reinterpret_cast<uint4 *>(a.out + (long long)tok * a.ldo + (long long)h * hd + d0) =
-            make_uint4(D::encode2(o[0], o[1]), D::encode2(o[2], o[3]), D::encode2(o[4], o[5]), D::encode2(o[6], o[7]));
+}
+
+template <class D, int HB>
+static aweq_status tree_join(const TreeArgs &a, const TreePlan &p, unsigned char *ws, cudaStream_t stream)
+{
+    // a token's heads over several CTAs while the tokens alone do not give every SM two
+    const int most = (a.n_heads / HB + kTjWarps - 1) / kTjWarps;
+    int parts = (2 * kSmCount + a.max_tokens - 1) / a.max_tokens;
+    if (parts > most) parts = most;
+    AWEQ_LAUNCH((tree_join_kernel<D, HB>), dim3((unsigned)a.max_tokens * (unsigned)parts), dim3(kTjWarps * 32), 0, stream, a, p, parts,
+                (const unsigned char *)ws);
+    return AWEQ_OK;
 }
 
 template <class D, bool TWO>
@@ -846,9 +875,10 @@ static aweq_status tree_launch(const TreeArgs &a, const TreePlan &p, unsigned ch
 {
     const aweq_status rc = p.two ? tree_units<D, true>(a, p, ws, stream) : tree_units<D, false>(a, p, ws, stream);
     if (rc != AWEQ_OK) return rc;
-    AWEQ_LAUNCH(tree_join_kernel<D>, dim3((unsigned)a.max_tokens * (unsigned)((a.n_heads + kTjHeads - 1) / kTjHeads)), dim3(kTjHeads * 32), 0,
-                stream, a, p, (const unsigned char *)ws);
-    return AWEQ_OK;
+    // heads of one key head together, where their rows lie in one tile
+    if (p.group <= 128 && p.group % 4 == 0) return tree_join<D, 4>(a, p, ws, stream);
+    if (p.group <= 128 && p.group % 2 == 0) return tree_join<D, 2>(a, p, ws, stream);
+    return tree_join<D, 1>(a, p, ws, stream);
 }
 
 aweq_status run_tree_attention(const TreeArgs &a, const aweq_kv_cache *cache, void *ws, cudaStream_t stream)
