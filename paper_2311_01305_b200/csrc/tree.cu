@@ -11,7 +11,7 @@
 // rescaled.  Two such sums are under way in a CTA, so that one's products run under the other's exponentials: two row tiles on
 // the same keys where a sequence has more than 128 rows to a key head, else the same rows on every other unit of keys.
 // A unit is 128 keys (or the whole pages that fit).  The units of all (segment, key head, row tile) items in a row are dealt out evenly
-// to a CTA per SM; where a CTA leaves an item it writes a record (m, sum, O of the keys it has seen) for each row and sum.
+// to a CTA per SM; where a CTA leaves an item it writes a record (m, sum, O of the keys it has seen) for each row.
 // Warps: 0 copies keys and values, 1 issues the products, 2 brings the rows of Q, 3 says which items come, 4-11 and 12-19 the
 // softmax of the two sums.
 #include <type_traits>
@@ -32,7 +32,7 @@ struct TreeShared {
     TreeItem item[kTrItems];
     uint32_t tmem;
     volatile int gave_up[8];             // by sum and TMEM quarter: a softmax warp has
-    float top[2][2][128];                // the halves' maxima, by sum and half; at the end of an item one half's l
+    float top[2][2][128];                // the halves' maxima, by sum and half; at the end of an item the sums' bases and l
 };
 constexpr size_t kTrSmem = kTrQBytes + kTrRing + sizeof(TreeShared);
 static_assert(kTrSmem <= 227 * 1024, "shared memory of a CTA");
@@ -65,13 +65,12 @@ static TreePlan tree_plan(const aweq_kv_cache *c, long long prefix_len, long lon
     p.pre_tiles = (int)((prefix_len + p.unit - 1) / p.unit);
     p.pre_rec = (int)(pre_rows < p.rows ? pre_rows : p.rows);
     p.own_rec = (int)(own_rows < p.rows ? own_rows : p.rows);
-    const int sums = p.two ? 1 : 2;
     const long long pre_items = p.pre_tiles ? (long long)c->n_kv_heads * p.pre_rt : 0;
     // (no more row tiles than every sequence's most, nor than the tokens make)
     long long rt = n_seq * ((own_rows + p.rows - 1) / p.rows);
     if (rt > pre_rows / p.rows + n_seq) rt = pre_rows / p.rows + n_seq;
-    const size_t pre_kept = p.pre_tiles ? (size_t)(pre_items + p.ctas) * p.pre_rec * sums : 0;
-    const size_t own_kept = (size_t)(rt * c->n_kv_heads + p.ctas) * p.own_rec * sums;
+    const size_t pre_kept = p.pre_tiles ? (size_t)(pre_items + p.ctas) * p.pre_rec : 0;
+    const size_t own_kept = (size_t)(rt * c->n_kv_heads + p.ctas) * p.own_rec;
     size_t off = up256(sizeof(TreeTotals) + (size_t)n_seq * sizeof(TreeFirst));
     p.off_seq = off; off += up256((size_t)max_tokens * 4);
     p.off_pre_o = off; off += up256(pre_kept * c->head_dim * 4);
@@ -133,7 +132,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             mbar_init(&sh.s_full[i], 1);
             mbar_init(&sh.p_ready[i], 8);
             mbar_init(&sh.pv_done[i], 1);
-            mbar_init(&sh.o_free[i], 8);
+            mbar_init(&sh.o_free[i], TWO ? 8 : 16);
         }
         for (int i = 0; i < kTrItems; ++i) {
             mbar_init(&sh.item_full[i], 1);
@@ -191,7 +190,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     it.len = w.len;
                     it.rows = w.rows(p);
                     it.t0 = w.t0;
-                    it.rec = (long long)(w.item + cta) * (TWO ? rec : 2 * rec);
+                    it.rec = (long long)(w.item + cta) * rec;
                     left -= it.count;
                     it.stop = left == 0;
                 }
@@ -493,6 +492,10 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             named_bar_sync(1 + pair, 64);
             return !sh.gave_up[pair];
         };
+        auto meet4 = [&] {                                      // the four that have the same rows (one tile to an item)
+            named_bar_sync(9 + q4, 128);
+            return !sh.gave_up[q4] && !sh.gave_up[4 + q4];
+        };
         TreeItems items;
         // The first pass, on a unit that there is not, keeps nothing: it brings the code in while the first keys are under way (the
         // products wait for its P).  cnt: passes; the products of the first do not exist.
@@ -606,45 +609,89 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             }
             done += it.count;
             if (mine <= 0 || it.count == 0) continue;
-            const long long rec = it.rec + (TWO ? sum * p.part : sum * (it.own ? p.own_rec : p.pre_rec)) + r;       // (its number among all rows)
+            // The CTA's record of the item.  (Eight dims of every row side by side, so that a warp's stores lie together.)
+            const long long rec = it.rec + (TWO ? sum * p.part : 0) + r;        // the row's number among all records'
             float2 *const ml = reinterpret_cast<float2 *>(ws + (it.own ? p.off_own_ml : p.off_pre_ml));
-            if (fresh) {
-                if (r < mine && !half) ml[rec] = make_float2(-CUDART_INF_F, 0.0f);      // the item had no unit for this sum
-                continue;
-            }
-            if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.pv_done[sum], cnt & 1)))) break;                      // (pass cnt - 1)
+            float *const dst = reinterpret_cast<float *>(ws + (it.own ? p.off_own_o : p.off_pre_o)) + tree_record(p, it.own, rec, 0, hd);
+            const int step = (it.own ? p.own_rec : p.pre_rec) * 8;
+            const float base = m == -CUDART_INF_F ? m : __fmul_rn(m, scale) - kShift;
+            if (!fresh && !(ok = __all_sync(0xffffffffu, mbar_wait(&sh.pv_done[sum], cnt & 1)))) break;            // (pass cnt - 1)
             tc_fence_after();
-            if (live) {
+            if (TWO) {
+                if (live) {
+                    if (half) sh.top[sum][1][r] = l;
+                    if (!(ok = meet())) break;
+                    if (r < mine && !half) ml[rec] = make_float2(base, l + sh.top[sum][1][r]);
+#pragma unroll 1
+                    for (int c = half * 64; c < min(hd, half * 64 + 64); c += 32) {
+                        uint32_t o[32];
+                        __syncwarp();
+                        tc_ld32(acc + c, o);
+                        tc_wait_ld();
+                        if (r < mine)
+#pragma unroll
+                            for (int j = 0; j < 32; j += 8)
+                                if (c + j < hd) {
+                                    uint4 *const to = reinterpret_cast<uint4 *>(dst + ((c + j) >> 3) * step);
+                                    to[0] = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                                    to[1] = make_uint4(o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
+                                }
+                    }
+                }
+            } else if (live) {
+                // The two sums of the same rows become one: the four threads of a row exchange bases and sums, each takes 32 dims of both.
+                // (Of a sum that had no unit O may be anything.)
                 if (half) sh.top[sum][1][r] = l;
                 if (!(ok = meet())) break;
-                if (r < mine && !half) ml[rec] = make_float2(m == -CUDART_INF_F ? m : __fmul_rn(m, scale) - kShift, l + sh.top[sum][1][r]);
-                // (eight dims of every row side by side, so that a warp's stores lie together)
-                float *const dst = reinterpret_cast<float *>(ws + (it.own ? p.off_own_o : p.off_pre_o)) + tree_record(p, it.own, rec, 0, hd);
-                const int step = (it.own ? p.own_rec : p.pre_rec) * 8;
-#pragma unroll 1
-                for (int c = half * 64; c < min(hd, half * 64 + 64); c += 32) {
-                    uint32_t o[32];
-                    __syncwarp();
-                    tc_ld32(acc + c, o);
+                if (!half) {
+                    sh.top[sum][0][r] = fresh ? -CUDART_INF_F : base;
+                    sh.top[sum][1][r] = fresh ? 0.0f : l + sh.top[sum][1][r];
+                }
+                tc_fence_before();
+                if (!(ok = meet4())) break;
+                tc_fence_after();
+                const float b0 = sh.top[0][0][r], b1 = sh.top[1][0][r], l0 = sh.top[0][1][r], l1 = sh.top[1][1][r];
+                const float to = fmaxf(b0, b1), from = to == -CUDART_INF_F ? 0.0f : to, f0 = exp2_fast(b0 - from), f1 = exp2_fast(b1 - from);
+                const bool only0 = it.count < 2 && ((done - it.count) & 1) == 0, only1 = it.count < 2 && !only0;
+                if (r < mine && sum == 0 && !half) ml[rec] = make_float2(to, only0 ? l0 : only1 ? l1 : l0 * f0 + l1 * f1);
+                const int c = (sum * 2 + half) * 32;
+                if (c < hd) {
+                    uint32_t x[32], y[32];
+                    tc_ld32(acc - sum * 128 + c, x);
+                    tc_ld32(acc - sum * 128 + 128 + c, y);
                     tc_wait_ld();
                     if (r < mine)
 #pragma unroll
                         for (int j = 0; j < 32; j += 8)
                             if (c + j < hd) {
-                                uint4 *const to = reinterpret_cast<uint4 *>(dst + ((c + j) >> 3) * step);
-                                to[0] = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-                                to[1] = make_uint4(o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
+                                float v[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    const float p0 = __uint_as_float(x[j + i]), p1 = __uint_as_float(y[j + i]);
+                                    v[i] = only0 ? p0 : only1 ? p1 : p0 * f0 + p1 * f1;
+                                }
+                                float4 *const at8 = reinterpret_cast<float4 *>(dst + ((c + j) >> 3) * step);
+                                at8[0] = make_float4(v[0], v[1], v[2], v[3]);
+                                at8[1] = make_float4(v[4], v[5], v[6], v[7]);
                             }
                 }
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.o_free[sum]);
+            if (lane == 0) {
+                if (TWO) mbar_arrive(&sh.o_free[sum]);
+                else {
+                    // (both sums' O have been read; a sum without a unit has no products to wait)
+                    if (it.count > 1 || ((done - it.count) & 1) == 0) mbar_arrive(&sh.o_free[0]);
+                    if (it.count > 1 || ((done - it.count) & 1) == 1) mbar_arrive(&sh.o_free[1]);
+                }
+            }
         } while (!it.stop);
         if (!ok) {
             if (lane == 0) sh.gave_up[pair] = 1;
             __syncwarp();
             named_bar_arrive(1 + pair, 64);
+            if (!TWO) named_bar_arrive(9 + q4, 128);
         }
     }
     if (!ok && lane == 0 && a.st) atomicAdd(&a.st->wait_timeout, 1ull);
@@ -708,7 +755,6 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, int parts, const unsigned c
     if (sees) place[before + __popc(seen & ((1u << lane) - 1))] = at;
     __syncthreads();
     const float scale = a.scale * 1.4426950408889634f;
-    const int sums = p.two ? 1 : 2;
     const bool none = nodes == 0 && s.base <= 0 && a.prefix_len == 0;
     for (int block = part * kTjWarps + warp; block < blocks; block += parts * kTjWarps) {
         const int h = block * HB, kh = h / G, g = h - kh * G;
@@ -796,9 +842,9 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, int parts, const unsigned c
         deal.more = totals.more;
         const bool there = lane & 2 ? s.base > 0 : p.pre_tiles > 0;
         const int c = there ? deal.cta_of(u) : lane & 1 ? -1 : 0;
-        const int c0 = __shfl_sync(0xffffffffu, c, 0), n0 = (__shfl_sync(0xffffffffu, c, 1) - c0 + 1) * sums;
-        const int c2 = __shfl_sync(0xffffffffu, c, 2), n1 = (__shfl_sync(0xffffffffu, c, 3) - c2 + 1) * sums;
-        const long long rec0 = (item0 + c0) * sums, rec1 = (long long)(s.item + within + c2) * sums - n0;
+        const int c0 = __shfl_sync(0xffffffffu, c, 0), n0 = __shfl_sync(0xffffffffu, c, 1) - c0 + 1;
+        const int c2 = __shfl_sync(0xffffffffu, c, 2), n1 = __shfl_sync(0xffffffffu, c, 3) - c2 + 1;
+        const long long rec0 = item0 + c0, rec1 = (long long)(s.item + within + c2) - n0;
         const int in0 = (int)(in_all - rt0 * (unsigned)p.rows), in1 = (int)(in_seq - rt1 * (unsigned)p.rows);
         for (int k = half; k < n0 + n1; k += 2) {
             const bool own = k >= n0;
