@@ -4,14 +4,14 @@
 namespace aweq {
 
 // eight binary32 values as eight e2m1 elements (round to nearest even, saturating at 6)
-__device__ __forceinline__ uint32_t e2m1_encode8(const float *v)
+__device__ __forceinline__ uint32_t e2m1_encode8(const float2 *v)
 {
     uint32_t r;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
         "mov.b32 %0, {a, b, c, d};\n\t}"
-        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+        : "=r"(r) : "f"(v[0].x), "f"(v[0].y), "f"(v[1].x), "f"(v[1].y), "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y));
     return r;
 }
 __device__ __forceinline__ void e2m1_decode8(uint32_t codes, float *v)
@@ -60,44 +60,61 @@ __device__ __forceinline__ Mx4Chunk mx4_load(const Mx4QuantArgs &a, long long ro
     }
     return c;
 }
-// the elements times the columns' factors
-template <class D>
-__device__ __forceinline__ void mx4_values(const Mx4Chunk &c, const float *scale, int chunk, bool in, float (&v)[16])
+// the elements times the columns' factors, two at a time
+struct Mx4Scale { float2 f[8]; };
+__device__ __forceinline__ Mx4Scale mx4_scale(const float *scale, int chunk, bool in)
 {
-    widen8<D>(c.a, *reinterpret_cast<float (*)[8]>(v));
-    widen8<D>(c.b, *reinterpret_cast<float (*)[8]>(v + 8));
-    if (scale && in)
+    Mx4Scale m;
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const float4 s = *reinterpret_cast<const float4 *>(scale + chunk * 16 + i);
-            v[i] *= s.x; v[i + 1] *= s.y; v[i + 2] *= s.z; v[i + 3] *= s.w;
-        }
+    for (int i = 0; i < 8; i += 2) {
+        const float4 s = scale && in ? *reinterpret_cast<const float4 *>(scale + chunk * 16 + 2 * i) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+        m.f[i] = make_float2(s.x, s.y);
+        m.f[i + 1] = make_float2(s.z, s.w);
+    }
+    return m;
 }
-__device__ __forceinline__ uint32_t mx4_top(const float (&v)[16])      // largest magnitude, as bits (infinite and NaN on top)
+template <class D>
+__device__ __forceinline__ void mx4_values(const Mx4Chunk &c, const Mx4Scale &m, float2 (&v)[8])
 {
-    uint32_t top = 0;
+    const uint32_t w[8] = {c.a.x, c.a.y, c.a.z, c.a.w, c.b.x, c.b.y, c.b.z, c.b.w};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-    return top;
+    for (int i = 0; i < 8; ++i) v[i] = __fmul2_rn(D::to_float2(D::from_bits(w[i])), m.f[i]);
+}
+// largest magnitude, as bits (infinities and NaN on top)
+__device__ __forceinline__ uint32_t mx4_top(const float2 (&v)[8])
+{
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(top) : "f"(top), "f"(v[i].x), "f"(v[i].y));
+    return __float_as_uint(top) & 0x7fffffffu;
 }
 
 // A CTA takes a row, a thread V chunks of 16 columns; rows go round-robin over the grid with the next row's loads in flight.
+// The factors of a thread's columns stay in registers where it has one chunk; its values do between their maximum and their codes.
 template <class D, int FMT, int V, bool EPS>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(V == 1 ? 512 : 1024)
 mx4_quant_kernel(const Mx4QuantArgs a)
 {
     __shared__ uint32_t sh_top[2][32];
     __shared__ float sh_eps[2][32];
     pdl_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    Mx4Scale kept;
+    if (V == 1) kept = mx4_scale(a.scale, threadIdx.x, (int)threadIdx.x < a.chunks);
+    auto factors = [&](int chunk) { return V == 1 ? kept : mx4_scale(a.scale, chunk, chunk < a.chunks); };
+    constexpr bool kAhead = V <= 2;                             // (the registers hold the next row of up to 32768 columns too)
     Mx4Chunk x[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = mx4_load(a, blockIdx.x, threadIdx.x + i * blockDim.x);
+    for (int i = 0; i < V; ++i)
+        if (kAhead) x[i] = mx4_load(a, blockIdx.x, threadIdx.x + i * blockDim.x);
     int turn = 0;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         Mx4Chunk next[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) next[i] = mx4_load(a, row + gridDim.x, threadIdx.x + i * blockDim.x);
+        for (int i = 0; i < V; ++i) {
+            if (kAhead) next[i] = mx4_load(a, row + gridDim.x, threadIdx.x + i * blockDim.x);
+            else x[i] = mx4_load(a, row, threadIdx.x + i * blockDim.x);
+        }
         float row_step = 1.0f;
         bool row_bad = false;
         if (FMT == AWEQ_MX4_E4M3) {
@@ -105,8 +122,8 @@ mx4_quant_kernel(const Mx4QuantArgs a)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int chunk = threadIdx.x + i * blockDim.x;
-                float v[16];
-                mx4_values<D>(x[i], a.scale, chunk, chunk < a.chunks, v);
+                float2 v[8];
+                mx4_values<D>(x[i], factors(chunk), v);
                 top = max(top, mx4_top(v));
             }
             top = __reduce_max_sync(0xffffffffu, top);
@@ -125,8 +142,8 @@ mx4_quant_kernel(const Mx4QuantArgs a)
         for (int i = 0; i < V; ++i) {
             const int chunk = threadIdx.x + i * blockDim.x;
             const bool in = chunk < a.chunks;
-            float v[16];
-            mx4_values<D>(x[i], a.scale, chunk, in, v);
+            float2 v[8];
+            mx4_values<D>(x[i], factors(chunk), v);
             uint32_t top = mx4_top(v), byte;
             float step, inv;
             bool zero;
@@ -150,10 +167,13 @@ mx4_quant_kernel(const Mx4QuantArgs a)
                 if (zero) byte = 0u;
                 inv = zero ? 0.0f : __frcp_rn(step);
             }
-            float y[16];
+            // (inv is zero where the block becomes zeros; zero times an infinity or a NaN is none, but then every code is cleared)
+            const float2 inv2 = make_float2(inv, inv);
+            float2 y[8];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) y[j] = zero ? 0.0f : __fmul_rn(v[j], inv);
-            const uint2 codes = make_uint2(e2m1_encode8(y), e2m1_encode8(y + 8));
+            for (int j = 0; j < 8; ++j) y[j] = __fmul2_rn(v[j], inv2);
+            uint2 codes = make_uint2(e2m1_encode8(y), e2m1_encode8(y + 4));
+            if (zero) codes = make_uint2(0u, 0u);
             if (in) *reinterpret_cast<uint2 *>(a.codes + row * (a.cols / 2) + chunk * 8) = codes;
             // four blocks' scales to a word
             uint32_t word;
@@ -177,10 +197,11 @@ mx4_quant_kernel(const Mx4QuantArgs a)
 #pragma unroll
                 for (int j = 0; j < 16; j += 4) {
                     const float4 m = *reinterpret_cast<const float4 *>(a.mu + chunk * 16 + j);
-                    eps = __fmaf_rn(__fmaf_rn(q[j], step, -v[j]), m.x, eps);
-                    eps = __fmaf_rn(__fmaf_rn(q[j + 1], step, -v[j + 1]), m.y, eps);
-                    eps = __fmaf_rn(__fmaf_rn(q[j + 2], step, -v[j + 2]), m.z, eps);
-                    eps = __fmaf_rn(__fmaf_rn(q[j + 3], step, -v[j + 3]), m.w, eps);
+                    const float2 v0 = v[j / 2], v1 = v[j / 2 + 1];
+                    eps = __fmaf_rn(__fmaf_rn(q[j], step, -v0.x), m.x, eps);
+                    eps = __fmaf_rn(__fmaf_rn(q[j + 1], step, -v0.y), m.y, eps);
+                    eps = __fmaf_rn(__fmaf_rn(q[j + 2], step, -v1.x), m.z, eps);
+                    eps = __fmaf_rn(__fmaf_rn(q[j + 3], step, -v1.y), m.w, eps);
                 }
             }
         }
@@ -194,7 +215,8 @@ mx4_quant_kernel(const Mx4QuantArgs a)
             }
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = next[i];
+        for (int i = 0; i < V; ++i)
+            if (kAhead) x[i] = next[i];
     }
 }
 
@@ -212,7 +234,7 @@ static aweq_status quant_launch(const Mx4QuantArgs &a, unsigned threads, cudaStr
 template <class D, int FMT>
 static aweq_status quant_width(const Mx4QuantArgs &a, cudaStream_t stream)
 {
-    int v = 1;
+    int v = a.padded <= 512 ? 1 : 2;
     while (a.padded > 1024 * v) ++v;
     const unsigned threads = (unsigned)((a.padded + 32 * v - 1) / (32 * v) * 32);
     switch (v) {
@@ -243,7 +265,7 @@ mx4_dequant_kernel(const unsigned char *codes, const unsigned char *scales, cons
     pdl_begin();
     const long long total = rows * chunks;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long row = i / chunks;
+        const long long row = i >> 32 ? i / chunks : (long long)((uint32_t)i / (uint32_t)chunks);
         const int chunk = (int)(i - row * chunks);
         const uint2 c = *reinterpret_cast<const uint2 *>(codes + i * 8);
         const uint32_t byte = scales[mx4_scale_at(row, FMT == AWEQ_MX4_E8M0 ? chunk >> 1 : chunk, row_tiles)];

@@ -97,49 +97,79 @@ __device__ __forceinline__ PlanTotals plan_sequences(const KvPlanArgs &a, long l
     return {(int)tokens, taken + min(more_before, free), given + min(less_before, a.n_pages - free)};
 }
 
+// Where the ring's next free page lies, and where the next one given back goes.
+struct PlanEnds { int take, give, free; };
+__device__ __forceinline__ PlanEnds plan_ends(const KvPlanArgs &a, long long taken, long long given)
+{
+    return {(int)(taken % a.n_pages), (int)(given % a.n_pages), (int)(given - taken)};
+}
+// (offsets are at most n_pages, ends below it)
+__device__ __forceinline__ int plan_at(const KvPlanArgs &a, int end, int offset)
+{
+    const int i = end + offset, n = (int)a.n_pages;
+    return i < n ? i : i - n;
+}
 // A page of the ring for a sequence's p'th page, -1 where there is none.
-__device__ __forceinline__ int plan_ring(const KvPlanArgs &a, long long taken, const PlanSeq &s, int p)
+__device__ __forceinline__ int plan_ring(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq &s, int p)
 {
     const int i = p - s.have;
     if (i >= s.granted) return -1;
-    const int page = a.ring[(taken + s.take + i) % a.n_pages];
+    const int page = a.ring[plan_at(a, e.take, s.take + i)];
     return page < 0 || page >= a.n_pages ? -1 : page;
 }
 
-// Page moves (a warp per sequence) and tokens (four a thread), shared out over the grid.
-__device__ __forceinline__ void plan_fill(const KvPlanArgs &a, long long taken, long long given, const PlanSeq *seqs, int total)
+// the last sequence that starts at or before token t (of several with the same start, the last: the others are empty)
+__device__ __forceinline__ int plan_find(const PlanSeq *seqs, int n_seq, int t)
 {
-    const int n_seq = (int)a.n_seq, lane = threadIdx.x & 31;
-    const long long free = given - taken;
-    for (int b = blockIdx.x * (kPlanThreads / 32) + (threadIdx.x >> 5); b < n_seq; b += gridDim.x * (kPlanThreads / 32)) {
+    int b = 0;
+    for (int n = n_seq; n > 1;) {
+        const int half = n >> 1;
+        if (seqs[b + half].start <= t) b += half;
+        n -= half;
+    }
+    return b;
+}
+
+// Page moves, a warp per sequence.
+__device__ __forceinline__ void plan_pages_move(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq *seqs)
+{
+    const int lane = threadIdx.x & 31;
+    for (int b = blockIdx.x * (kPlanThreads / 32) + (threadIdx.x >> 5); b < (int)a.n_seq; b += gridDim.x * (kPlanThreads / 32)) {
         const PlanSeq s = seqs[b];
         int *const row = a.page_table + (long long)b * a.ld_table;
         for (int p = s.have + lane; p < s.want; p += 32) {
-            const int page = plan_ring(a, taken, s, p);
+            const int page = plan_ring(a, e, s, p);
             row[p] = page;
             if (page < 0 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
         }
         for (int p = s.want + lane; p < s.have; p += 32) {
-            const long long at = s.give + (p - s.want);
-            if (at < a.n_pages - free) a.ring[(given + at) % a.n_pages] = row[p];
+            const long long at = (long long)s.give + (p - s.want);
+            if (at < a.n_pages - e.free) a.ring[plan_at(a, e.give, (int)at)] = row[p];
             row[p] = -1;
         }
     }
-    const int quads = (int)((a.max_tokens + 3) / 4);
+}
+// The slot of a sequence's key; `p`, `page`: the page looked up last.
+__device__ __forceinline__ long long plan_slot(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq &s, int b, int key, int &p, int &page)
+{
+    if (key >= s.after) return -1;
+    const int q = (int)((unsigned)key / (unsigned)a.page_size), r = key - q * a.page_size;
+    if (q != p) {
+        p = q;
+        page = q < s.have ? a.page_table[(long long)b * a.ld_table + q] : plan_ring(a, e, s, q);
+    }
+    return page >= 0 && page < a.n_pages ? (long long)page * a.page_size + r : -1;
+}
+
+// Tokens in a row, four to a thread.
+__device__ __forceinline__ void plan_tokens(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq *seqs, int total)
+{
+    const int n_seq = (int)a.n_seq, quads = (int)((a.max_tokens + 3) / 4);
     for (int i = blockIdx.x * kPlanThreads + threadIdx.x; i < quads; i += gridDim.x * kPlanThreads) {
         const int t0 = i * 4;
         int seq[4], pos[4];
         long long slot[4];
-        // the last sequence that starts at or before t0 (of several with the same start, the last: the others are empty)
-        int b = 0;
-        if (t0 < total) {
-            int n = n_seq;
-            while (n > 1) {
-                const int half = n >> 1;
-                if (seqs[b + half].start <= t0) b += half;
-                n -= half;
-            }
-        }
+        int b = t0 < total ? plan_find(seqs, n_seq, t0) : 0, p = -1, page = -1;
         PlanSeq s = seqs[b];
         int end = b + 1 < n_seq ? seqs[b + 1].start : total;
 #pragma unroll
@@ -147,46 +177,16 @@ __device__ __forceinline__ void plan_fill(const KvPlanArgs &a, long long taken, 
             const int t = t0 + j;
             seq[j] = pos[j] = -1;
             slot[j] = -1;
-            if (t >= total) {
-                if (a.mask && t < a.max_tokens)
-                    for (int w = 0; w < a.words; ++w) a.mask[(long long)t * a.words + w] = 0;
-                continue;
-            }
+            if (t >= total) continue;
             while (t >= end) {
                 s = seqs[++b];
                 end = b + 1 < n_seq ? seqs[b + 1].start : total;
+                p = -1;
             }
-            const int node = t - s.start, key = s.held + node;
-            int depth = node;
-            if (a.mask) {
-                // the node and those above it; a parent is a node before its child
-                unsigned long long bits[kPlanMaxWords] = {};
-                int at = node;
-                depth = 0;
-                if (node >> 6 >= a.words) {
-                    if (a.st) atomicAdd(&a.st->out_of_range, 1ull);
-                } else for (;;) {
-#pragma unroll
-                    for (int w = 0; w < kPlanMaxWords; ++w)
-                        if (at >> 6 == w) bits[w] |= 1ull << (at & 63);
-                    const int up = a.parent[s.start + at];
-                    const bool bad = up < -1 || up >= at;
-                    if (bad && at == node && a.st) atomicAdd(&a.st->out_of_range, 1ull);
-                    if (bad || up < 0) break;
-                    at = up;
-                    ++depth;
-                }
-#pragma unroll
-                for (int w = 0; w < kPlanMaxWords; ++w)
-                    if (w < a.words) a.mask[(long long)t * a.words + w] = (long long)bits[w];
-            }
+            const int key = s.held + t - s.start;
             seq[j] = b;
-            pos[j] = (int)(a.first + s.held + depth);
-            if (key < s.after) {
-                const int p = (int)((unsigned)key / (unsigned)a.page_size), r = key - p * a.page_size;
-                const int page = p < s.have ? a.page_table[(long long)b * a.ld_table + p] : plan_ring(a, taken, s, p);
-                if (page >= 0 && page < a.n_pages) slot[j] = (long long)page * a.page_size + r;
-            }
+            pos[j] = (int)(a.first + key);
+            slot[j] = plan_slot(a, e, s, b, key, p, page);
         }
         if (t0 + 4 <= a.max_tokens) {
             *reinterpret_cast<int4 *>(a.seq + t0) = make_int4(seq[0], seq[1], seq[2], seq[3]);
@@ -202,17 +202,76 @@ __device__ __forceinline__ void plan_fill(const KvPlanArgs &a, long long taken, 
     }
 }
 
+// Nodes of trees, a thread each.  A node's way up is a chain of look-ups, so the parents of a CTA's nodes and of the nodes before them
+// that a tree can reach lie in shared memory.
+__device__ __forceinline__ void plan_nodes(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq *seqs, int total, int *parents)
+{
+    constexpr int kBack = 64 * kPlanMaxWords;
+    const int n_seq = (int)a.n_seq;
+    for (long long t00 = (long long)blockIdx.x * kPlanThreads; t00 < a.max_tokens; t00 += (long long)gridDim.x * kPlanThreads) {
+        const int t0 = (int)t00, t = t0 + (int)threadIdx.x;
+        __syncthreads();
+        for (int i = threadIdx.x; i < kBack + kPlanThreads; i += kPlanThreads) {
+            const int from = t0 - kBack + i;
+            parents[i] = from >= 0 && from < total ? a.parent[from] : -1;
+        }
+        __syncthreads();
+        if (t >= a.max_tokens) continue;
+        int seq = -1, pos = -1;
+        long long slot = -1;
+        unsigned long long bits[kPlanMaxWords] = {};
+        if (t < total) {
+            const int b = plan_find(seqs, n_seq, t);
+            const PlanSeq s = seqs[b];
+            const int node = t - s.start, *const mine = parents + kBack - node + (int)threadIdx.x;      // parents of the sequence's nodes
+            int depth = 0, p = -1, page = -1;
+            if (node >> 6 < a.words) {
+                // the node and those above it; a parent is a node before its child
+                for (int at = node;;) {
+#pragma unroll
+                    for (int w = 0; w < kPlanMaxWords; ++w)
+                        if (at >> 6 == w) bits[w] |= 1ull << (at & 63);
+                    const int up = mine[at];
+                    const bool bad = up < -1 || up >= at;
+                    if (bad && at == node && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+                    if (bad || up < 0) break;
+                    at = up;
+                    ++depth;
+                }
+            } else if (a.st) atomicAdd(&a.st->out_of_range, 1ull);
+            seq = b;
+            pos = (int)(a.first + s.held + depth);
+            slot = plan_slot(a, e, s, b, s.held + node, p, page);
+        }
+        a.seq[t] = seq;
+        a.pos[t] = pos;
+        a.slot[t] = slot;
+#pragma unroll
+        for (int w = 0; w < kPlanMaxWords; ++w)
+            if (w < a.words) a.mask[(long long)t * a.words + w] = (long long)bits[w];
+    }
+}
+
+__device__ __forceinline__ void plan_fill(const KvPlanArgs &a, const PlanRing &ring, const PlanSeq *seqs, int total, int *parents)
+{
+    const PlanEnds e = plan_ends(a, ring.taken, ring.given);
+    plan_pages_move(a, e, seqs);
+    if (a.mask) plan_nodes(a, e, seqs, total, parents);
+    else plan_tokens(a, e, seqs, total);
+}
+
 // Up to kPlanShared sequences: every CTA works out the sequences for itself and fills its share, in one launch.  The ring's counters
 // are set by the CTA that ends last, when all have read them.
 __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlanArgs a, unsigned *ticket)
 {
     __shared__ PlanSeq seqs[kPlanShared];
+    __shared__ int parents[64 * kPlanMaxWords + kPlanThreads];
     __shared__ long long sh[kPlanThreads / 32];
     pdl_begin();
     const PlanRing ring = plan_state(a);
     const PlanTotals all = plan_sequences(a, ring.taken, ring.given, seqs, sh, blockIdx.x == 0);
     __syncthreads();
-    plan_fill(a, ring.taken, ring.given, seqs, all.tokens);
+    plan_fill(a, ring, seqs, all.tokens, parents);
     if (threadIdx.x == 0) {
         // (this CTA's threads read the counters before the barriers above)
         __threadfence();
@@ -243,18 +302,22 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_sequences_kernel(const K
 }
 __global__ void __launch_bounds__(kPlanThreads) kv_plan_fill_kernel(const KvPlanArgs a, const PlanHead *head, const PlanSeq *seqs)
 {
+    __shared__ int parents[64 * kPlanMaxWords + kPlanThreads];
     pdl_begin();
-    plan_fill(a, head->taken, head->given, seqs, head->tokens);
+    plan_fill(a, {head->taken, head->given, false}, seqs, head->tokens, parents);
 }
 
 size_t kv_plan_ws_bytes(long long n_seq) { return n_seq <= kPlanShared ? 256 : 256 + (size_t)n_seq * sizeof(PlanSeq); }
 
 aweq_status run_kv_plan(const KvPlanArgs &a, void *ws, cudaStream_t stream)
 {
-    long long ctas = (a.max_tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
-    const long long by_seq = (a.n_seq + 31) / 32;                              // (page moves: four sequences to a warp at least)
+    // every CTA works out the sequences for itself, so no more of them than the tokens (four to a thread, nodes one) and the page moves
+    // (a sequence to a warp) keep busy
+    const int per = kPlanThreads * (a.mask ? 1 : 4);
+    long long ctas = (a.max_tokens + per - 1) / per;
+    const long long by_seq = (a.n_seq + kPlanThreads / 32 - 1) / (kPlanThreads / 32);
     if (ctas < by_seq) ctas = by_seq;
-    if (ctas > kSmCount * 4) ctas = kSmCount * 4;
+    if (ctas > kSmCount * 2) ctas = kSmCount * 2;
     unsigned char *const w = reinterpret_cast<unsigned char *>(ws);
     if (a.n_seq <= kPlanShared) {
         AWEQ_LAUNCH(kv_plan_kernel, dim3((unsigned)ctas), dim3(kPlanThreads), 0, stream, a, reinterpret_cast<unsigned *>(w));
@@ -268,14 +331,17 @@ aweq_status run_kv_plan(const KvPlanArgs &a, void *ws, cudaStream_t stream)
 }
 
 // ------------------------------------------------------------------ accept
-// A thread moves one 16-byte piece of every row of a sequence's path, in the path's order.  Paths ascend, so a place is read before
-// it is written (key path[j] = i is read for place j < i), whatever the piece: no thread needs another.
-__global__ void __launch_bounds__(128) kv_accept_kernel(const KvAcceptArgs a, int pieces, int blocks)
+// A CTA takes 128 16-byte pieces of a sequence's rows, a thread one piece of every row of the path, in the path's order.  Where the rows
+// lie is looked up first, a thread per row.  Paths ascend, so a place is read before it is written (key path[j] = i is read for place
+// j < i), whatever the piece: no thread needs another.  Bound by the chain of path, page, row.
+constexpr int kAcceptThreads = 128;
+__global__ void __launch_bounds__(kAcceptThreads) kv_accept_kernel(const KvAcceptArgs a, int pieces, int blocks)
 {
+    __shared__ long long from[kAcceptThreads], to[kAcceptThreads];
+    __shared__ int first_bad, nodes[kAcceptThreads + 1];
     pdl_begin();
-    const int b = blockIdx.x / blocks, i = (blockIdx.x - b * blocks) * 128 + threadIdx.x;
+    const int tid = threadIdx.x, b = blockIdx.x / blocks, i = (blockIdx.x - b * blocks) * kAcceptThreads + tid;
     const bool lead = i == 0;
-    if (i >= 2 * pieces) return;
     const long long base = a.base[b], cap = a.pages_per_seq * a.page_size;
     const int asked = a.n_path[b];
     int n = min(max(asked, 0), a.max_path);
@@ -289,47 +355,54 @@ __global__ void __launch_bounds__(128) kv_accept_kernel(const KvAcceptArgs a, in
     const int *const path = a.path + (long long)b * a.ld_path, *const row = a.page_table + (long long)b * a.ld_table;
     // element of the pool of a key, -1: nowhere
     auto place = [&](long long key) -> long long {
-        if (key >= cap) return -1;
-        const unsigned p = (unsigned)((unsigned long long)key / (unsigned)a.page_size);
+        if (key < 0 || key >= cap) return -1;
+        const unsigned p = (unsigned)key / (unsigned)a.page_size;
         const int page = row[p];
         return page < 0 || page >= a.n_pages ? -1 : page * a.page_stride + (key - (long long)p * a.page_size) * a.token_stride;
     };
-    constexpr int U = 8;
-    int last = -1;
-    bool on = true;
-    for (int i0 = 0; i0 < n && on; i0 += U) {
-        uint4 x[U];
-        long long to[U];
-        int node[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j) node[j] = i0 + j < n ? path[i0 + j] : -1;
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-            to[j] = -1;
-            if (i0 + j >= n) continue;
-            if (node[j] <= last) on = false;                    // (what follows a node that is out of order stays where it is)
-            last = node[j];
-            const long long from = on ? place(base + node[j]) : -1;
-            if (on) to[j] = place(base + i0 + j);
-            if (from < 0 || to[j] < 0) {
-                on = false;
-                to[j] = -1;
-            }
-            if (node[j] == i0 + j) to[j] = -1;
-            if (to[j] >= 0) x[j] = *reinterpret_cast<const uint4 *>(pool + from);
+    if (tid == 0) nodes[0] = -1;
+    for (int i0 = 0; i0 < n; i0 += kAcceptThreads) {
+        const int count = min(n - i0, kAcceptThreads);
+        if (tid == 0) first_bad = count;
+        const int node = tid < count ? path[i0 + tid] : 0;
+        if (tid < count) nodes[tid + 1] = node;
+        __syncthreads();
+        if (tid < count) {
+            const long long x = place(base + node), y = place(base + i0 + tid);
+            if (node <= nodes[tid] || x < 0 || y < 0) atomicMin(&first_bad, tid);
+            from[tid] = x;
+            to[tid] = node == i0 + tid ? -1 : y;
         }
+        __syncthreads();
+        // what comes before the first node that is out of order or nowhere
+        const int good = first_bad;
+        constexpr int U = 8;
+        if (i < 2 * pieces)
+            for (int j0 = 0; j0 < good; j0 += U) {
+                uint4 x[U];
 #pragma unroll
-        for (int j = 0; j < U; ++j)
-            if (to[j] >= 0) *reinterpret_cast<uint4 *>(pool + to[j]) = x[j];
+                for (int j = 0; j < U; ++j)
+                    if (j0 + j < good && to[j0 + j] >= 0) x[j] = *reinterpret_cast<const uint4 *>(pool + from[j0 + j]);
+#pragma unroll
+                for (int j = 0; j < U; ++j)
+                    if (j0 + j < good && to[j0 + j] >= 0) *reinterpret_cast<uint4 *>(pool + to[j0 + j]) = x[j];
+            }
+        if (good < count) {
+            bad = true;
+            break;
+        }
+        const int last = nodes[count];
+        __syncthreads();
+        if (tid == 0) nodes[0] = last;
     }
-    if (lead && (bad || !on) && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+    if (lead && bad && a.st) atomicAdd(&a.st->out_of_range, 1ull);
 }
 
 aweq_status run_kv_accept(const KvAcceptArgs &a, cudaStream_t stream)
 {
     const int pieces = a.n_kv * (a.head_dim / 8);
-    const int blocks = (2 * pieces + 127) / 128;
-    AWEQ_LAUNCH(kv_accept_kernel, dim3((unsigned)(a.n_seq * blocks)), dim3(128), 0, stream, a, pieces, blocks);
+    const int blocks = (2 * pieces + kAcceptThreads - 1) / kAcceptThreads;
+    AWEQ_LAUNCH(kv_accept_kernel, dim3((unsigned)(a.n_seq * blocks)), dim3(kAcceptThreads), 0, stream, a, pieces, blocks);
     return AWEQ_OK;
 }
 
