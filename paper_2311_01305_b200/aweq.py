@@ -584,22 +584,29 @@ class MX4:
 
     def quantise(self, X, scale=None, mu=None, epsmu=None, st=None):
         """Codes of X times ``scale`` (float32 per column); ``epsmu`` gets the row sums of (value - X scale) mu."""
-        shape, (ld, one) = X.shape, X.stride()
-        if shape != (self.rows, self.cols) or one != 1 or not X.is_cuda:
-            raise ValueError("X must be a 16-bit device matrix [%d x %d] with contiguous rows" % (self.rows, self.cols))
-        for t, n, what in ((scale, self.cols, "scale"), (mu, self.cols, "mu"), (epsmu, self.rows, "epsmu")):
-            _want(t, torch.float32, n, what)
-        rc = _lib.aweq_quant_mx4(X.data_ptr(), dtype_tag(X), self.rows, self.cols, ld if self.rows > 1 else self.cols, _ptr(scale), self.tag,
-                                 *self.args, _ptr(mu), _ptr(epsmu), _ptr(st), _stream())
+        ld, one = X.stride()
+        # (every check a few tenths of a microsecond, as in LinearW8A8)
+        if (X.shape != (self.rows, self.cols) or one != 1 or not X.is_cuda
+                or scale is not None and (scale.dtype is not torch.float32 or scale.shape != (self.cols,) or not scale.is_contiguous() or not scale.is_cuda)):
+            raise ValueError("X must be a 16-bit device matrix [%d x %d] with contiguous rows, scale float32 [%d]" % (self.rows, self.cols, self.cols))
+        _want(mu, torch.float32, self.cols, "mu")
+        _want(epsmu, torch.float32, self.rows, "epsmu")
+        rc = _lib.aweq_quant_mx4(X.data_ptr(), dtype_tag(X), self.rows, self.cols, ld if self.rows > 1 else self.cols,
+                                 None if scale is None else scale.data_ptr(), self.tag, *self.args, _ptr(mu), _ptr(epsmu), _ptr(st), _stream())
         if rc:
             raise AweqError(rc)
         return self
 
     def values(self, out=None, dtype=torch.bfloat16):
         out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.codes.device) if out is None else out
-        if out.shape != (self.rows, self.cols):
-            raise ValueError("out must be [%d x %d]" % (self.rows, self.cols))
-        return aweq_dequant_mx4(self.codes, self.scales, self.row_step, self.fmt, out)
+        ldo, one = out.stride()
+        if out.shape != (self.rows, self.cols) or one != 1 or not out.is_cuda:
+            raise ValueError("out must be a 16-bit device matrix [%d x %d] with contiguous rows" % (self.rows, self.cols))
+        rc = _lib.aweq_dequant_mx4(*self.args, self.tag, self.rows, self.cols, out.data_ptr(), dtype_tag(out), ldo if self.rows > 1 else self.cols,
+                                   _stream())
+        if rc:
+            raise AweqError(rc)
+        return out
 
 
 class LinearMX4:
@@ -786,12 +793,14 @@ class StepPlan:
 
     def __init__(self, n_seq, max_tokens, max_nodes=0, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)
-        self.n_seq, self.max_tokens = n_seq, max_tokens
+        self.n_seq, self.max_tokens, self.words = n_seq, max_tokens, -(-max_nodes // 64)
         self.own_len, self.start = torch.empty(n_seq, **i32), torch.empty(n_seq + 1, **i32)
         self.seq, self.pos = torch.empty(max_tokens, **i32), torch.empty(max_tokens, **i32)
         self.slot = torch.empty(max_tokens, dtype=torch.int64, device=device)
-        self.mask = torch.empty((max_tokens, -(-max_nodes // 64)), dtype=torch.int64, device=device) if max_nodes else None
+        self.mask = torch.empty((max_tokens, self.words), dtype=torch.int64, device=device) if max_nodes else None
         self.ws = workspace(aweq_kv_plan_workspace_bytes(n_seq), device).zero_()
+        self._out = (self.own_len.data_ptr(), self.start.data_ptr(), *((t.data_ptr() for t in (self.seq, self.pos, self.slot)) if max_tokens else (None,) * 3))
+        self._ws = (self.ws.data_ptr(), self.ws.numel())
 
 
 class PagePool:
@@ -802,16 +811,27 @@ class PagePool:
         self.n_pages, self.page_size = n_pages, page_size
         self.ring = torch.arange(n_pages, dtype=torch.int32, device=device) if ring is None else ring
         self.state = torch.tensor([0, n_pages], dtype=torch.int64, device=device) if state is None else state
-        if self.ring.numel() != n_pages:
-            raise ValueError("ring has a place for every page")
+        if self.state.dtype is not torch.int64 or self.state.numel() != 2 or not self.state.is_contiguous() or not self.state.is_cuda:
+            raise ValueError("state must be a contiguous int64 device tensor of two elements")
+        self._ring = (_int32_rows(self.ring, n_pages, "ring"), self.state.data_ptr(), n_pages)
 
     def plan(self, page_table, held, change, into, first=0, parent=None, st=None):
         """Sequence b of ``page_table`` holds ``held[b]`` keys and gets ``change[b]`` new tokens (below zero: gives up that many): its
-        pages come from or go to the ring, lengths, slots and positions are written into the ``StepPlan`` ``into``."""
-        if parent is not None and into.mask is None:
-            raise ValueError("trees need a StepPlan with max_nodes")
-        aweq_kv_plan(page_table, self.page_size, self.ring, self.state, held, change, into.own_len, into.start, into.ws, into.max_tokens,
-                     into.seq, into.pos, into.slot, first, parent, into.mask, st)
+        pages come from or go to the ring, lengths, slots and positions are written into the ``StepPlan`` ``into``.  ``parent``: for
+        drafted trees, the number within its sequence of the node above each new token (-1: none)."""
+        pages, n_seq, per_seq, ld_table = _int32_table(page_table, "page_table")
+        if n_seq != into.n_seq:
+            raise ValueError("page_table has a row for each of the %d sequences of the StepPlan" % into.n_seq)
+        up = bits = None
+        if parent is not None and into.max_tokens:
+            if into.mask is None:
+                raise ValueError("trees need a StepPlan with max_nodes")
+            up, bits = _int32_rows(parent, into.max_tokens, "parent"), into.mask.data_ptr()
+        rc = _lib.aweq_kv_plan(pages, n_seq, per_seq, ld_table, self.page_size, *self._ring, _int32_rows(held, n_seq, "held"),
+                               _int32_rows(change, n_seq, "change"), first, into.max_tokens, *into._out, up, bits, into.words, *into._ws, _ptr(st),
+                               _stream())
+        if rc:
+            raise AweqError(rc)
         return into
 
 

@@ -263,28 +263,42 @@ mx4_dequant_kernel(const unsigned char *codes, const unsigned char *scales, cons
                    long long row_tiles, uint16_t *out, long long ldo)
 {
     pdl_begin();
-    const long long total = rows * chunks;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const long long row = i >> 32 ? i / chunks : (long long)((uint32_t)i / (uint32_t)chunks);
-        const int chunk = (int)(i - row * chunks);
-        const uint2 c = *reinterpret_cast<const uint2 *>(codes + i * 8);
-        const uint32_t byte = scales[mx4_scale_at(row, FMT == AWEQ_MX4_E8M0 ? chunk >> 1 : chunk, row_tiles)];
-        float v[16], s, r = 1.0f;
-        if (FMT == AWEQ_MX4_E8M0) s = byte == 0xffu ? __uint_as_float(0x7fffffffu) : byte ? __uint_as_float(byte << 23) : 5.877471754111438e-39f;
-        else {
-            s = e4m3_decode(byte);
-            r = row_step[row];
-        }
-        e2m1_decode8(c.x, v);
-        e2m1_decode8(c.y, v + 8);
-        uint32_t o[8];
+    const long long total = rows * chunks, step = (long long)gridDim.x * 256;
+    constexpr int U = 4;                                        // chunks of 16 columns under way
+    for (long long i0 = (long long)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += U * step) {
+        uint2 c[U];
+        uint32_t byte[U];
+        float r[U];
+        uint16_t *dst[U];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            o[j] = FMT == AWEQ_MX4_E8M0 ? D::encode2(v[2 * j] * s, v[2 * j + 1] * s)
-                                        : D::encode2(__fmul_rn(__fmul_rn(v[2 * j], s), r), __fmul_rn(__fmul_rn(v[2 * j + 1], s), r));
-        uint4 *dst = reinterpret_cast<uint4 *>(out + row * ldo + chunk * 16);
-        dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-        dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+        for (int k = 0; k < U; ++k) {
+            const long long i = i0 + k * step;
+            dst[k] = nullptr;
+            if (i >= total) continue;
+            const long long row = i >> 32 ? i / chunks : (long long)((uint32_t)i / (uint32_t)chunks);
+            const int chunk = (int)(i - row * chunks);
+            c[k] = *reinterpret_cast<const uint2 *>(codes + i * 8);
+            byte[k] = scales[mx4_scale_at(row, FMT == AWEQ_MX4_E8M0 ? chunk >> 1 : chunk, row_tiles)];
+            r[k] = FMT == AWEQ_MX4_E8M0 ? 1.0f : row_step[row];
+            dst[k] = out + row * ldo + chunk * 16;
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (!dst[k]) continue;
+            float v[16], s;
+            if (FMT == AWEQ_MX4_E8M0) s = byte[k] == 0xffu ? __uint_as_float(0x7fffffffu) : byte[k] ? __uint_as_float(byte[k] << 23) : 5.877471754111438e-39f;
+            else s = e4m3_decode(byte[k]);
+            e2m1_decode8(c[k].x, v);
+            e2m1_decode8(c[k].y, v + 8);
+            uint32_t o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                o[j] = FMT == AWEQ_MX4_E8M0 ? D::encode2(v[2 * j] * s, v[2 * j + 1] * s)
+                                            : D::encode2(__fmul_rn(__fmul_rn(v[2 * j], s), r[k]), __fmul_rn(__fmul_rn(v[2 * j + 1], s), r[k]));
+            uint4 *const to = reinterpret_cast<uint4 *>(dst[k]);
+            to[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            to[1] = make_uint4(o[4], o[5], o[6], o[7]);
+        }
     }
 }
 

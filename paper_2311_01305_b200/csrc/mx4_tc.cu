@@ -26,11 +26,11 @@ __device__ __forceinline__ Mx4Col mx4_col(const Mx4LinearArgs &p, long long o)
 // weights, its tokens' scales and all of the channels' scales.  Persistent: a pair takes every (pairs)-th tile.
 //
 // TMEM: 512 columns do not hold two accumulators of 256 and the scales.  The two overlap by 96 columns, which the epilogue takes
-// out first: then the next tile's products may start.  Scales have two buffers of 48 columns, since a copy into TMEM is not in
-// order with the products before it: the buffer's last products are waited for (two stages back, so the pipe stays fed).
+// out first: then the next tile's products may start.  Scales have 96 columns, two buffers (E4M3) or four, since a copy into TMEM is
+// not in order with the products before it: the buffer's last products are waited for (that many stages back, so the pipe stays fed).
 // Warps: 0 copies, 1 issues the products (in the pair's even CTA), 4-11 write the output, two to a quarter of the TMEM lanes.
-constexpr int kM4BigStages = 5, kM4BigThreads = 384, kM4Overlap = 96, kM4ScaleCols = 48;
-constexpr int kM4SecondAcc = 256 - kM4Overlap, kM4Scales = 512 - 2 * kM4ScaleCols;
+constexpr int kM4BigStages = 5, kM4BigThreads = 384, kM4Overlap = 96, kM4ScaleCols = 96;
+constexpr int kM4SecondAcc = 256 - kM4Overlap, kM4Scales = 512 - kM4ScaleCols;
 constexpr int kM4OutPitch = 80;                // bytes of a staged output row: 32 columns and 16 bytes against bank conflicts
 static_assert(kM4SecondAcc + 256 <= kM4Scales, "columns of TMEM");
 __host__ __device__ constexpr int m4_big_stage(int fmt) { return 2 * 128 * kM4Block + 3 * mx4_group_tiles(fmt) * kMx4Tile; }
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kM4BigThreads, 1)
 mx4_big_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW,
                const __grid_constant__ CUtensorMap mapSx, const __grid_constant__ CUtensorMap mapSw, int mt, int nt, int vec_out)
 {
-    constexpr int T = mx4_group_tiles(FMT), kStage = m4_big_stage(FMT), kScaleAt = 2 * 128 * kM4Block;
+    constexpr int T = mx4_group_tiles(FMT), kStage = m4_big_stage(FMT), kScaleAt = 2 * 128 * kM4Block, kBufs = kM4ScaleCols / (12 * T);
     constexpr bool E8M0 = FMT == AWEQ_MX4_E8M0;
     extern __shared__ unsigned char raw[];
     unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -118,7 +118,7 @@ mx4_big_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX, 
     } else if (warp == 1) {
         if (rank == 0) {
             const bool lead = tc_elect();
-            int s = 0, back = kM4BigStages - 2, it = 0;
+            int s = 0, back = kM4BigStages - kBufs, it = 0;
             uint32_t ph = 0, back_ph = 1, buf = 0;
             const uint32_t idesc = tc_idesc_mx4(E8M0, 256, 256);
             for (long long t = blockIdx.x / 2; ok && t < tiles; t += step, ++it) {
@@ -126,10 +126,10 @@ mx4_big_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX, 
                 if (it > 0 && !mbar_wait_cluster(&sh.acc_free, (it - 1) & 1)) { ok = false; break; }
                 tc_fence_after();
                 for (int kb = 0; kb < nkb; ++kb) {
-                    // the products that read this buffer of scales, two stages ago (at the start: a phase that counts as over)
+                    // the products that read this buffer of scales (at the start: a phase that counts as over)
                     if (!mbar_wait_cluster(&sh.full[s], ph) || !mbar_wait_cluster(&sh.empty[back], back_ph)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t a = smem_u32(stages + s * kStage), sf = tmem + kM4Scales + buf * kM4ScaleCols;
+                    const uint32_t a = smem_u32(stages + s * kStage), sf = tmem + kM4Scales + buf * (12 * T);
                     const uint32_t da = tc_desc(a), db = tc_desc(a + 128 * kM4Block);
 #pragma unroll
                     for (int i = 0; i < T; ++i) {
@@ -146,7 +146,7 @@ mx4_big_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX, 
                     tc_commit<2>(&sh.empty[s], lead);
                     if (++s == kM4BigStages) { s = 0; ph ^= 1; }
                     if (++back == kM4BigStages) { back = 0; back_ph ^= 1; }
-                    buf ^= 1;
+                    buf = (buf + 1) % kBufs;
                 }
                 if (ok) tc_commit<2>(&sh.acc_full[it & 1], lead);
             }
@@ -414,7 +414,7 @@ mx4_split_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX
 constexpr int kM4SplitMaxSmem = 216 * 1024;
 
 template <class D, int FMT>
-static aweq_status m4_split_launch(const Mx4LinearArgs &a, int slices, int per_sm, cudaStream_t stream)
+static aweq_status m4_split_launch(const Mx4LinearArgs &a, int slices, cudaStream_t stream)
 {
     constexpr int T = mx4_group_tiles(FMT);
     M4SplitPlan s;
@@ -426,9 +426,11 @@ static aweq_status m4_split_launch(const Mx4LinearArgs &a, int slices, int per_s
     s.scale_cols = T * 4 * (1 + x_tiles);
     s.cols = 32;
     while (s.cols < s.bn + 2 * s.scale_cols) s.cols *= 2;
-    const int out_bytes = s.bn * 132 * 4, room = kM4SplitMaxSmem / per_sm;
-    s.stages = room / s.stage_bytes;
+    // (no more stages than a slice has blocks: 16 x 4096 x 4096 in four slices 5.0 us, with eight stages 5.5)
+    const int out_bytes = s.bn * 132 * 4, blocks = ((a.K + 255) / 256 + slices - 1) / slices;
+    s.stages = kM4SplitMaxSmem / s.stage_bytes;
     if (s.stages > kM4SplitMaxStages) s.stages = kM4SplitMaxStages;
+    if (s.stages > blocks) s.stages = blocks;
     if (s.stages < 3) s.stages = 3;
     int smem = s.stages * s.stage_bytes;
     if (smem < out_bytes) smem = out_bytes;
@@ -446,16 +448,23 @@ static aweq_status m4_split_launch(const Mx4LinearArgs &a, int slices, int per_s
     return e == cudaSuccess ? AWEQ_OK : cuda_failed(e);
 }
 
+// Which kernel, and into how many slices of K.  Measured on the device, in microseconds (weights in the L2):
+//   16 x 4096 x 4096   1 to 4 slices 7.2, 5.5, 5.1, 5.0 (32 to 128 CTAs), 5 and 8 slices 8.2, 9.7 (more CTAs than SMs); pairs 9.7
+//   16 x 13824 x 5120  1 to 4 slices 19.3, 12.3, 11.0, 18.1 (40 to 160 CTAs); pairs 24.1
+//   24 x 4096 x 12288  1 slice 8.6 (96 CTAs), 2 slices 12.0; pairs 13.8         1 x 768 x 768  1 to 3 slices 2.9, 3.4, 3.4; pairs 5.6
+//   64 x 5120 x 13824  1 slice 11.5; pairs 13.7        128 x 4096 x 4096  4 slices 8.5; pairs 11.1
+//   128 x 5120 x 13824 1 slice 16.8; pairs 15.1        256 x 4096 x 4096  4 slices 13.0; pairs 11.2
+// So: as many slices as leave every CTA an SM of its own and two blocks of K; pairs beyond 128 tokens, and beyond 64 where the channels
+// alone fill the SMs.
 template <class D, int FMT>
 static aweq_status m4_choose(const Mx4LinearArgs &a, cudaStream_t stream)
 {
     const int nkb = (a.K + 255) / 256;
-    const long long ct = (a.O + 127) / 128;
-    if (a.N > 256 || ct > 65535) return m4_big_launch<D, FMT>(a, stream);
-    // slices of K until the device is full twice
+    const long long ct = (a.O + 127) / 128;                      // (channels lie on the grid's second dimension)
+    if (a.N > 128 || (a.N > 64 && 2 * ct > kSmCount) || ct > 65535) return m4_big_launch<D, FMT>(a, stream);
     int slices = 1;
-    while (slices < 8 && slices * 2 <= nkb && ct * slices * 2 <= 2 * kSmCount) slices *= 2;
-    return m4_split_launch<D, FMT>(a, slices, a.N <= 64 ? 2 : 1, stream);
+    while (slices < 4 && 2 * (slices + 1) <= nkb && ct * (slices + 1) <= kSmCount) ++slices;
+    return m4_split_launch<D, FMT>(a, slices, stream);
 }
 
 aweq_status run_linear_mx4(const Mx4LinearArgs &a, aweq_dtype dt, cudaStream_t stream)

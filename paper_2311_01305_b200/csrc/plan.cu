@@ -53,41 +53,62 @@ __device__ __forceinline__ PlanTotals plan_sequences(const KvPlanArgs &a, long l
     const long long cap = min(a.pages_per_seq * a.page_size, 0x7fffffffll);
     const long long free = given - taken;
     long long tokens = 0, more_before = 0, less_before = 0;
-    for (int b0 = 0; b0 < (int)a.n_seq; b0 += kPlanThreads) {
-        const int b = b0 + (int)threadIdx.x;
-        const bool in = b < (int)a.n_seq;
-        const int asked_held = in ? a.held[b] : 0, asked = in ? a.change[b] : 0;
-        const int held = (int)(asked_held < 0 ? 0 : min((long long)asked_held, cap));
-        int fresh = asked > 0 ? (int)min((long long)asked, cap - held) : 0;
-        const int drop = asked < 0 ? (int)min(-(long long)asked, (long long)held) : 0;
-        bool bad = held != asked_held || (asked > 0 ? fresh != asked : (long long)drop != -(long long)asked);
-        // the tokens' places end where the rows do
-        const PlanSums t = plan_scan(fresh, sh);
-        const long long start = min(tokens + t.before, a.max_tokens);
-        const int kept = (int)min((long long)fresh, a.max_tokens - start);
-        bad |= kept != fresh;
-        fresh = kept;
-        const int have = plan_pages(held, a.page_size);
-        int after = held + fresh - drop, want = plan_pages(after, a.page_size);
-        const int more = max(want - have, 0), less = max(have - want, 0);
-        // (no sequence asks for or has more than the pool: both sums in one, 32 bits each)
-        const PlanSums m = plan_scan((long long)min((long long)more, a.n_pages) << 32 | min((long long)less, a.n_pages), sh);
-        const long long take = more_before + (m.before >> 32), give = less_before + (m.before & 0xffffffffll);
-        const int granted = (int)min((long long)more, max(free - take, 0ll));
-        if (granted < more) {
-            bad = true;
-            want = have + granted;
-            after = (int)min((long long)after, (long long)want * a.page_size);
+    constexpr int M = 4;                       // sequences of a thread, so that two scans serve a thousand
+    for (int b0 = 0; b0 < (int)a.n_seq; b0 += M * kPlanThreads) {
+        const int b1 = b0 + M * (int)threadIdx.x;
+        int held[M], fresh[M], drop[M];
+        bool bad[M];
+        long long sum = 0;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const bool in = b1 + i < (int)a.n_seq;
+            const int asked_held = in ? a.held[b1 + i] : 0, asked = in ? a.change[b1 + i] : 0;
+            held[i] = (int)(asked_held < 0 ? 0 : min((long long)asked_held, cap));
+            fresh[i] = asked > 0 ? (int)min((long long)asked, cap - held[i]) : 0;
+            drop[i] = asked < 0 ? (int)min(-(long long)asked, (long long)held[i]) : 0;
+            bad[i] = held[i] != asked_held || (asked > 0 ? fresh[i] != asked : (long long)drop[i] != -(long long)asked);
+            sum += fresh[i];
         }
-        // pages given back beyond what the ring holds are lost, and counted
-        bad |= less > 0 && give + less > a.n_pages - free;
-        if (in) {
-            into[b] = {(int)start, held, have, want, granted, (int)min(take, a.n_pages), (int)min(give, a.n_pages), after};
-            if (lead) {
-                a.own_len[b] = after;
-                a.start[b] = (int)start;
-                if (bad && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+        // the tokens' places end where the rows do
+        const PlanSums t = plan_scan(sum, sh);
+        long long at = tokens + t.before, pages = 0;
+        int start[M], have[M], want[M], after[M];
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const long long from = min(at, a.max_tokens);
+            const int kept = (int)min((long long)fresh[i], a.max_tokens - from);
+            at += fresh[i];
+            start[i] = (int)from;
+            bad[i] |= kept != fresh[i];
+            have[i] = plan_pages(held[i], a.page_size);
+            after[i] = held[i] + kept - drop[i];
+            want[i] = plan_pages(after[i], a.page_size);
+            // (no sequence asks for or has more than the pool: both sums in one, 32 bits each)
+            pages += (long long)min((long long)max(want[i] - have[i], 0), a.n_pages) << 32 | min((long long)max(have[i] - want[i], 0), a.n_pages);
+        }
+        const PlanSums m = plan_scan(pages, sh);
+        long long take = more_before + (m.before >> 32), give = less_before + (m.before & 0xffffffffll);
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const int more = max(want[i] - have[i], 0), less = max(have[i] - want[i], 0);
+            const int granted = (int)min((long long)more, max(free - take, 0ll));
+            if (granted < more) {
+                bad[i] = true;
+                want[i] = have[i] + granted;
+                after[i] = (int)min((long long)after[i], (long long)want[i] * a.page_size);
             }
+            // pages given back beyond what the ring holds are lost, and counted
+            bad[i] |= less > 0 && give + less > a.n_pages - free;
+            if (b1 + i < (int)a.n_seq) {
+                into[b1 + i] = {start[i], held[i], have[i], want[i], granted, (int)min(take, a.n_pages), (int)min(give, a.n_pages), after[i]};
+                if (lead) {
+                    a.own_len[b1 + i] = after[i];
+                    a.start[b1 + i] = start[i];
+                    if (bad[i] && a.st) atomicAdd(&a.st->out_of_range, 1ull);
+                }
+            }
+            take += min((long long)more, a.n_pages);
+            give += min((long long)less, a.n_pages);
         }
         tokens = min(tokens + t.all, a.max_tokens);
         more_before += m.all >> 32;
@@ -149,56 +170,76 @@ __device__ __forceinline__ void plan_pages_move(const KvPlanArgs &a, const PlanE
         }
     }
 }
-// The slot of a sequence's key; `p`, `page`: the page looked up last.
-__device__ __forceinline__ long long plan_slot(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq &s, int b, int key, int &p, int &page)
+// The page of a sequence's p'th, -1 where there is none.
+__device__ __forceinline__ int plan_page(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq &s, int b, int p)
 {
-    if (key >= s.after) return -1;
-    const int q = (int)((unsigned)key / (unsigned)a.page_size), r = key - q * a.page_size;
-    if (q != p) {
-        p = q;
-        page = q < s.have ? a.page_table[(long long)b * a.ld_table + q] : plan_ring(a, e, s, q);
-    }
-    return page >= 0 && page < a.n_pages ? (long long)page * a.page_size + r : -1;
+    const int page = p < s.have ? a.page_table[(long long)b * a.ld_table + p] : plan_ring(a, e, s, p);
+    return page >= 0 && page < a.n_pages ? page : -1;
 }
 
-// Tokens in a row, four to a thread.
+// Tokens in a row, four to a thread (so that a warp's stores lie together: with eight the sectors came in halves, 22.5 us in the place
+// of 16.5 for 1.5 million tokens): one search, one division, and a look-up for each page they touch.
 __device__ __forceinline__ void plan_tokens(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq *seqs, int total)
 {
-    const int n_seq = (int)a.n_seq, quads = (int)((a.max_tokens + 3) / 4);
-    for (int i = blockIdx.x * kPlanThreads + threadIdx.x; i < quads; i += gridDim.x * kPlanThreads) {
-        const int t0 = i * 4;
-        int seq[4], pos[4];
-        long long slot[4];
-        int b = t0 < total ? plan_find(seqs, n_seq, t0) : 0, p = -1, page = -1;
-        PlanSeq s = seqs[b];
-        int end = b + 1 < n_seq ? seqs[b + 1].start : total;
+    constexpr int M = 4;
+    const bool wide = (reinterpret_cast<uintptr_t>(a.slot) & 31) == 0;
+    const int n_seq = (int)a.n_seq, runs = (int)((a.max_tokens + M - 1) / M);
+    for (int i = blockIdx.x * kPlanThreads + threadIdx.x; i < runs; i += gridDim.x * kPlanThreads) {
+        const int t0 = i * M;
+        int seq[M], pos[M];
+        long long slot[M];
+        int b = 0, key = 0, end = 0, p = 0, row = 0, page = -1;
+        PlanSeq s = {};
+        auto enter = [&](int t) {
+            s = seqs[b];
+            end = b + 1 < n_seq ? seqs[b + 1].start : total;
+            key = s.held + t - s.start;
+            p = (int)((unsigned)key / (unsigned)a.page_size);
+            row = key - p * a.page_size;
+            page = key < s.after ? plan_page(a, e, s, b, p) : -1;
+        };
+        if (t0 < total) {
+            b = plan_find(seqs, n_seq, t0);
+            enter(t0);
+        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < M; ++j) {
             const int t = t0 + j;
             seq[j] = pos[j] = -1;
             slot[j] = -1;
             if (t >= total) continue;
-            while (t >= end) {
-                s = seqs[++b];
-                end = b + 1 < n_seq ? seqs[b + 1].start : total;
-                p = -1;
+            if (t >= end) {
+                do ++b;                        // (sequences without tokens lie between)
+                while (b + 1 < n_seq && seqs[b + 1].start <= t);
+                enter(t);
             }
-            const int key = s.held + t - s.start;
             seq[j] = b;
             pos[j] = (int)(a.first + key);
-            slot[j] = plan_slot(a, e, s, b, key, p, page);
+            if (page >= 0 && key < s.after) slot[j] = (long long)page * a.page_size + row;
+            ++key;
+            if (++row == a.page_size) {
+                row = 0;
+                ++p;
+                page = j + 1 < M && key < s.after && t + 1 < end ? plan_page(a, e, s, b, p) : -1;
+            }
         }
-        if (t0 + 4 <= a.max_tokens) {
+        if (t0 + M <= a.max_tokens) {
             *reinterpret_cast<int4 *>(a.seq + t0) = make_int4(seq[0], seq[1], seq[2], seq[3]);
             *reinterpret_cast<int4 *>(a.pos + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-            *reinterpret_cast<longlong2 *>(a.slot + t0) = make_longlong2(slot[0], slot[1]);
-            *reinterpret_cast<longlong2 *>(a.slot + t0 + 2) = make_longlong2(slot[2], slot[3]);
-        } else
-            for (int j = 0; j < 4 && t0 + j < a.max_tokens; ++j) {
-                a.seq[t0 + j] = seq[j];
-                a.pos[t0 + j] = pos[j];
-                a.slot[t0 + j] = slot[j];
+            if (wide)
+                asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(a.slot + t0), "l"(slot[0]), "l"(slot[1]), "l"(slot[2]), "l"(slot[3]) : "memory");
+            else {
+                *reinterpret_cast<longlong2 *>(a.slot + t0) = make_longlong2(slot[0], slot[1]);
+                *reinterpret_cast<longlong2 *>(a.slot + t0 + 2) = make_longlong2(slot[2], slot[3]);
             }
+        } else
+#pragma unroll
+            for (int j = 0; j < M; ++j)
+                if (t0 + j < a.max_tokens) {
+                    a.seq[t0 + j] = seq[j];
+                    a.pos[t0 + j] = pos[j];
+                    a.slot[t0 + j] = slot[j];
+                }
     }
 }
 
@@ -224,7 +265,7 @@ __device__ __forceinline__ void plan_nodes(const KvPlanArgs &a, const PlanEnds &
             const int b = plan_find(seqs, n_seq, t);
             const PlanSeq s = seqs[b];
             const int node = t - s.start, *const mine = parents + kBack - node + (int)threadIdx.x;      // parents of the sequence's nodes
-            int depth = 0, p = -1, page = -1;
+            int depth = 0;
             if (node >> 6 < a.words) {
                 // the node and those above it; a parent is a node before its child
                 for (int at = node;;) {
@@ -241,7 +282,9 @@ __device__ __forceinline__ void plan_nodes(const KvPlanArgs &a, const PlanEnds &
             } else if (a.st) atomicAdd(&a.st->out_of_range, 1ull);
             seq = b;
             pos = (int)(a.first + s.held + depth);
-            slot = plan_slot(a, e, s, b, s.held + node, p, page);
+            const int key = s.held + node, p = (int)((unsigned)key / (unsigned)a.page_size);
+            const int page = key < s.after ? plan_page(a, e, s, b, p) : -1;
+            if (page >= 0) slot = (long long)page * a.page_size + (key - p * a.page_size);
         }
         a.seq[t] = seq;
         a.pos[t] = pos;
@@ -311,9 +354,9 @@ size_t kv_plan_ws_bytes(long long n_seq) { return n_seq <= kPlanShared ? 256 : 2
 
 aweq_status run_kv_plan(const KvPlanArgs &a, void *ws, cudaStream_t stream)
 {
-    // every CTA works out the sequences for itself, so no more of them than the tokens (four to a thread, nodes one) and the page moves
+    // every CTA works out the sequences for itself, so no more of them than the tokens (eight to a thread in two turns, nodes one) and the page moves
     // (a sequence to a warp) keep busy
-    const int per = kPlanThreads * (a.mask ? 1 : 4);
+    const int per = kPlanThreads * (a.mask ? 1 : 8);
     long long ctas = (a.max_tokens + per - 1) / per;
     const long long by_seq = (a.n_seq + kPlanThreads / 32 - 1) / (kPlanThreads / 32);
     if (ctas < by_seq) ctas = by_seq;

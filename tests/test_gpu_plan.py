@@ -253,14 +253,14 @@ def test_plan_refusals_of_the_binding(kw):
     table, held = dev([[0, -1]]), dev([1])
     pool, into = aweq.PagePool(4, 4), aweq.StepPlan(1, 4)
     if "own" in kw:
-        into.own_len = held
-    if "state" in kw:
-        pool.state = pool.state.to(torch.int32)
+        held = into.own_len                    # lengths are not rewritten in place
     if "table" in kw:
         table = table.to(torch.int64)
     with pytest.raises((ValueError, aweq.AweqError)):
         if "ring" in kw:
             aweq.PagePool(5, 4, ring=dev([1, 2]))
+        if "state" in kw:
+            aweq.PagePool(4, 4, state=dev([0, 4]))
         pool.plan(table, held.float() if "dtype" in kw else held, dev([1, 2]) if "short" in kw else dev([1]), into, parent=dev([-1] * 4) if "parent" in kw else None)
 
 
