@@ -12,10 +12,9 @@
 // the same keys where a sequence has more than 128 rows to a key head, else the same rows on every other unit of keys.
 // A unit is 128 keys (or the whole pages that fit).  The units of all (segment, key head, row tile) items in a row are dealt out evenly
 // to a CTA per SM; where a CTA leaves an item it writes a record (m, sum, O of the keys it has seen) for each row.
-// Warps: 0 copies keys and values, 1 issues the products, 2 brings the rows of Q, 3 says which items come, 4-11 and 12-19 the
-// softmax of the two sums.
-#include <type_traits>
-
+// Warps: 0 copies keys and values, 1 issues the products (1 and 2 those of a sum each where the sums take units in turn: one warp for
+// both took longer to issue them than the softmax took; two tiles on the same keys have to go in step, and two warps that wait for one
+// another's keys were slower, 250 us to 190), 3 says which items come and brings their rows of Q, 4-11 and 12-19 the softmax.
 #include "tree.cuh"
 #include "tensorcore.cuh"
 
@@ -110,6 +109,38 @@ struct TreeItems {
     }
 };
 
+// The rows of Q of an item's tiles, into buffer `buf`; by a warp.
+template <bool TWO>
+__device__ __forceinline__ void tree_bring(const TreeArgs &a, const TreePlan &p, const TreeItem &it, TreeShared &sh, unsigned char *qs, int buf,
+                                           const CUtensorMap &mapQ)
+{
+    const int lane = threadIdx.x & 31, hd = a.head_dim, halves = hd > 64 ? 2 : 1, parts = TWO && it.rows > p.part ? 2 : 1;
+    if (p.group <= 128) {
+        if (lane == 0) {
+            mbar_arrive_expect_tx(&sh.q_ready[buf], (uint32_t)(parts * halves * p.part * 128));
+            const int tok = it.t0 + it.rt * (p.rows / p.group);
+            for (int i = 0; i < parts; ++i)
+                for (int h = 0; h < halves; ++h)
+                    tma_load3(smem_u32(qs + (TWO ? i : buf) * 32768 + h * 16384), &mapQ, h * 64, it.kh * p.group, tok + i * (p.part / p.group),
+                              smem_u32(&sh.q_ready[buf]));
+        }
+    } else {
+        // more heads to a key head than a tile has rows: row by row
+        for (int i = lane; i < it.rows * halves * 8; i += 32) {
+            const int r = i / (halves * 8), c = i % (halves * 8);
+            const unsigned row = (unsigned)(it.rt * p.rows + r);
+            const uint16_t *src = a.q + (long long)(it.t0 + (int)(row / (unsigned)p.group)) * a.ldq +
+                                  (long long)(it.kh * p.group + (int)(row % (unsigned)p.group)) * hd;
+            *reinterpret_cast<uint4 *>(qs + (TWO ? r >> 7 : buf) * 32768 + (c >> 3) * 16384 + (r & 127) * 128 + (((c ^ r) & 7) << 4)) =
+                c * 8 < hd ? *reinterpret_cast<const uint4 *>(src + c * 8) : make_uint4(0, 0, 0, 0);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_ready[buf]);
+    }
+    __syncwarp();
+}
+
 template <class D, bool TWO>
 __global__ void __launch_bounds__(kTrThreads, 1)
 tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
@@ -128,7 +159,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.q_ready[i], 1);
-            mbar_init(&sh.q_free[i], 1);
+            mbar_init(&sh.q_free[i], TWO ? 1 : 2);
             mbar_init(&sh.s_full[i], 1);
             mbar_init(&sh.p_ready[i], 8);
             mbar_init(&sh.pv_done[i], 1);
@@ -136,7 +167,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
         }
         for (int i = 0; i < kTrItems; ++i) {
             mbar_init(&sh.item_full[i], 1);
-            mbar_init(&sh.item_empty[i], 19);
+            mbar_init(&sh.item_empty[i], TWO ? 18 : 19);
         }
         for (int i = 0; i < 8; ++i) sh.gave_up[i] = 0;
         mbar_init_fence();
@@ -157,7 +188,8 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTrOtherRegs));
         asm volatile("griddepcontrol.wait;" ::: "memory");
         if (warp == 3) {
-            // ---------------------------------------------------------- the CTA's items, a few ahead of those who work on them
+            // ---------------------------------------------------------- the CTA's items, a few ahead of those who work on them, and the rows
+            // of Q: one buffer for two tiles, or two for one each
             asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
             TreeSeq s0 = {};
             TreeScan c0 = {};
@@ -175,35 +207,59 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                 left = (int)(deal.first(cta + 1) - u0);
                 w.begin(a, p, totals, u0, s0, c0);
             }
-            for (int n = 0;; ++n) {
-                const int i = n & (kTrItems - 1);
-                TreeItem it = {};
+            TreeItem it = {};
+            auto make = [&] {
                 it.stop = 1;
-                if (left) {
-                    const int rec = w.own ? p.own_rec : p.pre_rec;
-                    it.own = w.own;
-                    it.b = w.b;
-                    it.kh = w.kh;
-                    it.rt = w.rt;
-                    it.tile = w.tile;
-                    it.count = min(w.tiles - w.tile, left);
-                    it.len = w.len;
-                    it.rows = w.rows(p);
-                    it.t0 = w.t0;
-                    it.rec = (long long)(w.item + cta) * rec;
-                    left -= it.count;
-                    it.stop = left == 0;
+                if (left == 0) return;
+                const int rec = w.own ? p.own_rec : p.pre_rec;
+                it.own = w.own;
+                it.b = w.b;
+                it.kh = w.kh;
+                it.rt = w.rt;
+                it.tile = w.tile;
+                it.count = min(w.tiles - w.tile, left);
+                it.len = w.len;
+                it.rows = w.rows(p);
+                it.t0 = w.t0;
+                it.rec = (long long)(w.item + cta) * rec;
+                left -= it.count;
+                it.stop = left == 0;
+            };
+            make();
+            constexpr int kBufs = TWO ? 1 : 2;
+            int told = 0, brought = 0;                          // items said, items whose rows of Q are there or under way
+            bool all = false;
+            unsigned long long t0 = global_ns();
+            while (!all || brought < told) {
+                bool moved = false;
+                const int i = told & (kTrItems - 1), buf = brought % kBufs;
+                if (!all && told < brought + kTrItems && __all_sync(0xffffffffu, mbar_test(&sh.item_empty[i], ((told / kTrItems) & 1) ^ 1))) {
+                    if (lane == 0) {
+                        sh.item[i] = it;
+                        mbar_arrive(&sh.item_full[i]);
+                    }
+                    __syncwarp();
+                    ++told;
+                    all = it.stop;
+                    moved = true;
+                    if (!all) {
+                        w.next_item(a, p);
+                        make();
+                    }
                 }
-                ok = __all_sync(0xffffffffu, mbar_wait(&sh.item_empty[i], ((n / kTrItems) & 1) ^ 1));
-                if (!ok) break;
-                if (lane == 0) {
-                    sh.item[i] = it;
-                    mbar_arrive(&sh.item_full[i]);
+                if (brought < told && (brought < kBufs || __all_sync(0xffffffffu, mbar_test(&sh.q_free[buf], (brought / kBufs - 1) & 1)))) {
+                    const TreeItem x = sh.item[brought & (kTrItems - 1)];
+                    if (x.count) tree_bring<TWO>(a, p, x, sh, qs, buf, mapQ);
+                    ++brought;
+                    moved = true;
                 }
-                __syncwarp();
-                if (it.stop) break;
-                w.next_item(a, p);
+                if (moved) t0 = global_ns();
+                else if (global_ns() - t0 > kWaitLimitNs) { ok = false; break; }
+                else __nanosleep(40);
             }
+            // (gave up: let what is under way land, bounded, before the memory goes)
+            if (!ok && p.group <= 128)
+                for (int i = 0; i < kBufs; ++i) mbar_wait(&sh.q_ready[i], 0);
             tree_leave(a, p, ws, cta);
         } else if (warp == 0) {
             // ---------------------------------------------------------- copies: a unit's keys, then its values
@@ -307,175 +363,117 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             }
             if (!ok)                                            // gave up: let what is under way land (bounded) before the memory goes
                 for (int i = 0; i < n_tiles; ++i) mbar_wait(&sh.full[i], ph ^ (i >= s ? 1u : 0u));
-        } else if (warp == 2) {
-            // ---------------------------------------------------------- the rows of Q: one buffer for two tiles, or two for one each
-            TreeItems items;
-            TreeItem it;
-            constexpr int kBufs = TWO ? 1 : 2;
-            for (int n = 0;; ++n) {
-                if (!(ok = items.next(sh, it)) || it.count == 0) break;
-                const int buf = n % kBufs;
-                if (n >= kBufs && !(ok = __all_sync(0xffffffffu, mbar_wait(&sh.q_free[buf], (n / kBufs - 1) & 1)))) break;
-                const int parts = TWO && it.rows > p.part ? 2 : 1;
-                if (p.group <= 128) {
-                    if (lane == 0) {
-                        mbar_arrive_expect_tx(&sh.q_ready[buf], (uint32_t)(parts * halves * p.part * 128));
-                        const int tok = it.t0 + it.rt * (p.rows / p.group);
-                        for (int i = 0; i < parts; ++i)
-                            for (int h = 0; h < halves; ++h)
-                                tma_load3(smem_u32(qs + (TWO ? i : buf) * 32768 + h * 16384), &mapQ, h * 64, it.kh * p.group, tok + i * (p.part / p.group),
-                                          smem_u32(&sh.q_ready[buf]));
-                    }
-                } else {
-                    // more heads to a key head than a tile has rows: row by row
-                    for (int i = lane; i < it.rows * halves * 8; i += 32) {
-                        const int r = i / (halves * 8), c = i % (halves * 8);
-                        const unsigned row = (unsigned)(it.rt * p.rows + r);
-                        const uint16_t *src = a.q + (long long)(it.t0 + (int)(row / (unsigned)p.group)) * a.ldq +
-                                              (long long)(it.kh * p.group + (int)(row % (unsigned)p.group)) * hd;
-                        *reinterpret_cast<uint4 *>(qs + (TWO ? r >> 7 : buf) * 32768 + (c >> 3) * 16384 + (r & 127) * 128 + (((c ^ r) & 7) << 4)) =
-                            c * 8 < hd ? *reinterpret_cast<const uint4 *>(src + c * 8) : make_uint4(0, 0, 0, 0);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.q_ready[buf]);
-                }
-                __syncwarp();
-                if (it.stop) break;
-            }
-            if (!ok && p.group <= 128)                          // (copies of Q that are under way)
-                for (int i = 0; i < kBufs; ++i) mbar_wait(&sh.q_ready[i], 0);
-        } else {
-            // ---------------------------------------------------------- products
+        } else if (!TWO || warp == 1) {
+            // ---------------------------------------------------------- products: a warp for both sums of two tiles, else one for each
             const bool lead = tc_elect();
             const uint32_t idesc_s = tc_idesc_f16(D::kBf16, 128, 128, false), idesc_o = tc_idesc_f16(D::kBf16, 128, (hd + 15) / 16 * 16, true);
-            const int ksteps = (hd + 15) / 16;
+            const int ksteps = (hd + 15) / 16, mine = TWO ? 0 : warp - 1;
             const uint32_t q0 = tc_desc(smem_u32(qs)), kv0 = tc_desc(smem_u32(tiles)), v0 = tc_desc_mn(smem_u32(tiles), 16384);
             TreeItems items;
             TreeItem it;
-            // the units as the scores meet them: those left of the item, keys from the current one on, number of the item, units of it so far
-            int left = 0, rest = 0, n_item = -1, of = 0, stop = 0, rows = 0;
-            // the stages of the next K and V tiles (every other one)
-            int ks = 0, vs = 1;
+            // The warp's units: all of them, or every other one.  left: those of the item, rest: keys from the next one's first on, n_item: the
+            // item's number, done: all units of the items before
+            constexpr int kEach = TWO ? 1 : 2;
+            int left = 0, rest = 0, n_item = -1, of = 0, stop = 0, both = 0, done = 0;
+            // the stages of the next K and V tiles
+            int ks = 2 * mine, vs = ks + 1;
             uint32_t kph = 0, vph = 0;
-            struct Unit { int live1, fresh, steps, last; } nu;
+            struct Unit { int both, fresh, steps, last, buf; };
             auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+            auto there = [](uint64_t *bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_wait(bar, parity)); };
             // the next unit: 1, none left: 0, gave up: -1
-            auto next_unit = [&]() -> int {
-                if (left == 0) {
+            auto next_unit = [&](Unit &u) -> int {
+                while (left == 0) {
                     if (stop) return 0;
                     if (!items.next(sh, it)) return -1;
-                    left = uniform(it.count);
+                    const int count = uniform(it.count), first = TWO || (done & 1) == mine ? 0 : 1;
                     stop = uniform(it.stop);
-                    rows = uniform(it.rows);
-                    rest = uniform(it.len - it.tile * p.unit);
+                    if (count == 0) return 0;
+                    left = count > first ? (count - first + kEach - 1) / kEach : 0;
+                    rest = uniform(it.len - (it.tile + first) * p.unit);
+                    both = TWO && uniform(it.rows) > p.part;
+                    done += count;
                     of = 0;
                     ++n_item;
-                    if (left == 0) return 0;
+                    const int buf = TWO ? 0 : n_item & 1;
+                    if (!there(&sh.q_ready[buf], (TWO ? n_item : n_item >> 1) & 1)) return -1;
+                    if (left == 0) tc_commit<1>(&sh.q_free[buf], lead);     // (nothing of this item is this sum's)
                 }
-                nu.live1 = rows > p.part;
-                nu.fresh = TWO ? of == 0 : of < 2;
-                nu.steps = (min(p.unit, rest) + 15) >> 4;
-                nu.last = left == 1;
-                rest -= p.unit;
+                u.both = both;
+                u.fresh = of == 0;
+                u.steps = (min(p.unit, rest) + 15) >> 4;
+                u.last = left == 1;
+                u.buf = TWO ? 0 : n_item & 1;
+                rest -= kEach * p.unit;
                 --left;
                 ++of;
                 return 1;
             };
-            auto scores = [&](auto S) {                         // S = Q K^T into sum S
-                constexpr int s = decltype(S)::value;
-                const uint32_t q = q0 + (TWO ? s : n_item & 1) * 2048, k = kv0 + ks * (tile_bytes >> 4);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < ksteps) tc_mma_f16_ss(tmem + s * 128, q + (i >> 2) * 1024 + 2 * (i & 3), k + (i >> 2) * 1024 + 2 * (i & 3), idesc_s, i > 0, lead);
-                tc_commit<1>(&sh.s_full[s], lead);
-            };
-            auto keys_done = [&] {
-                tc_commit<1>(&sh.empty[ks], lead);
-                if (nu.last) tc_commit<1>(&sh.q_free[TWO ? 0 : n_item & 1], lead);
-                ks += 2;
-                if (ks >= n_tiles) { ks -= n_tiles; kph ^= 1; }
+            auto step = [&](int &stage, uint32_t &phase) {
+                stage += 2 * kEach;
+                if (stage >= n_tiles) { stage -= n_tiles; phase ^= 1; }
             };
             auto keys_there = [&] {
-                if (of == 1 && !__all_sync(0xffffffffu, mbar_wait(&sh.q_ready[TWO ? 0 : n_item & 1], (TWO ? n_item : n_item >> 1) & 1))) return false;
-                const bool r = __all_sync(0xffffffffu, mbar_wait(&sh.full[ks], kph));
+                const bool r = there(&sh.full[ks], kph);
                 tc_fence_after();
                 return r;
             };
-            // O += P V of sum S; cnt: its products so far, outs: its items
-            auto values = [&](auto S, const Unit &u, uint32_t &cnt, uint32_t &outs, bool wait_v) {
-                constexpr int s = decltype(S)::value;
-                if (wait_v && !__all_sync(0xffffffffu, mbar_wait(&sh.full[vs], vph))) return false;
-                if (!__all_sync(0xffffffffu, mbar_wait(&sh.p_ready[s], cnt & 1))) return false;
-                ++cnt;
+            auto scores = [&](int sum, const Unit &u) {         // S = Q K^T
+                const uint32_t q = q0 + (TWO ? sum : u.buf) * 2048, k = kv0 + ks * (tile_bytes >> 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < ksteps) tc_mma_f16_ss(tmem + sum * 128, q + (i >> 2) * 1024 + 2 * (i & 3), k + (i >> 2) * 1024 + 2 * (i & 3), idesc_s, i > 0, lead);
+                tc_commit<1>(&sh.s_full[sum], lead);
+            };
+            auto keys_done = [&](const Unit &u) {
+                tc_commit<1>(&sh.empty[ks], lead);
+                if (u.last) tc_commit<1>(&sh.q_free[u.buf], lead);
+                step(ks, kph);
+            };
+            struct Passes { uint32_t softmax, items; } pass0 = {1, 0}, pass1 = {1, 0};
+            auto values = [&](int sum, const Unit &u, Passes &n) {          // O += P V
+                if (!there(&sh.p_ready[sum], n.softmax & 1)) return false;
+                ++n.softmax;
                 if (u.fresh) {
-                    if (outs > 0 && !__all_sync(0xffffffffu, mbar_wait(&sh.o_free[s], (outs - 1) & 1))) return false;
-                    ++outs;
+                    if (n.items > 0 && !there(&sh.o_free[sum], (n.items - 1) & 1)) return false;
+                    ++n.items;
                 }
                 tc_fence_after();
                 const uint32_t v = v0 + vs * (tile_bytes >> 4);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (i < u.steps) tc_mma_f16_ta(tmem + 256 + s * 128, tmem + s * 128 + i * 8, v + i * 128, idesc_o, !u.fresh || i > 0, lead);
-                tc_commit<1>(&sh.pv_done[s], lead);
+                    if (i < u.steps) tc_mma_f16_ta(tmem + 256 + sum * 128, tmem + sum * 128 + i * 8, v + i * 128, idesc_o, !u.fresh || i > 0, lead);
+                tc_commit<1>(&sh.pv_done[sum], lead);
                 return true;
             };
             auto values_done = [&] {
                 tc_commit<1>(&sh.empty[vs], lead);
-                vs += 2;
-                if (vs >= n_tiles) { vs -= n_tiles; vph ^= 1; }
+                step(vs, vph);
             };
-            constexpr std::integral_constant<int, 0> S0{};
-            constexpr std::integral_constant<int, 1> S1{};
-            uint32_t cnt0 = 1, cnt1 = 1, outs0 = 0, outs1 = 0;
-            int more = next_unit();
+            Unit u, next = {};
+            int more = next_unit(u);
             // (the softmax's first pass writes where S will be)
-            if (more > 0 && !(__all_sync(0xffffffffu, mbar_wait(&sh.p_ready[0], 0)) && __all_sync(0xffffffffu, mbar_wait(&sh.p_ready[1], 0)))) more = -1;
-            tc_fence_after();
-            if (TWO) {
-                // both sums on a unit: each's scores of the next unit behind its values of this one
-                if (more > 0 && (ok = keys_there())) {
-                    scores(S0);
-                    if (nu.live1) scores(S1);
-                    keys_done();
-                    for (;;) {
-                        const Unit u = nu;
-                        more = next_unit();
-                        if (more < 0 || !(ok = values(S0, u, cnt0, outs0, true))) break;
-                        if (more) {
-                            if (!(ok = keys_there())) break;
-                            scores(S0);
-                        }
-                        if (u.live1 && !(ok = values(S1, u, cnt1, outs1, false))) break;
-                        values_done();
-                        if (!more) break;
-                        if (nu.live1) scores(S1);
-                        keys_done();
-                    }
+            if (more > 0 && (ok = there(&sh.p_ready[mine], 0) && (!TWO || there(&sh.p_ready[1], 0)) && keys_there())) {
+                scores(mine, u);
+                if (TWO && u.both) scores(1, u);
+                keys_done(u);
+            }
+            // each sum's scores of its next unit behind its values of this one
+            while (ok && more > 0) {
+                more = next_unit(next);
+                if (!(ok = more >= 0 && there(&sh.full[vs], vph) && values(mine, u, pass0))) break;
+                if (!TWO) values_done();
+                if (more) {
+                    if (!(ok = keys_there())) break;
+                    scores(mine, next);
                 }
-            } else {
-                // units in turn: each sum's scores of the unit after next behind its values of this one
-                Unit u0 = {}, u1 = {};
-                bool on0 = false, on1 = false;
-                auto ahead = [&](auto S, Unit &u, bool &on) {
-                    on = more > 0;
-                    if (!on) return true;
-                    u = nu;
-                    if (!keys_there()) return false;
-                    scores(S);
-                    keys_done();
-                    more = next_unit();
-                    return more >= 0;
-                };
-                ok = ahead(S0, u0, on0) && ahead(S1, u1, on1);
-                while (ok) {
-                    if (!on0 || !(ok = values(S0, u0, cnt0, outs0, true))) break;
+                if (TWO) {
+                    if (u.both && !(ok = values(1, u, pass1))) break;
                     values_done();
-                    if (!(ok = ahead(S0, u0, on0))) break;
-                    if (!on1 || !(ok = values(S1, u1, cnt1, outs1, true))) break;
-                    values_done();
-                    if (!(ok = ahead(S1, u1, on1))) break;
+                    if (more && next.both) scores(1, next);
                 }
+                if (more) keys_done(next);
+                u = next;
             }
             ok = ok && more >= 0;
         }
@@ -518,7 +516,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     // values past the last key, up to the product's step of 16: zero, because a zero probability times whatever lay
                     // there (NaN, say) would not be
                     const int zeros = (keys + 15) / 16 * 16 - keys;
-                    if (zeros && (!TWO || sum == 0) && !warm) {
+                    if (zeros && !warm) {                       // (both sums do it: neither's product waits for the other's rows)
                         const int t = 2 * (done + u) + 1, stage = t % n_tiles;
                         if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.full[stage], (t / n_tiles) & 1)))) break;
                         unsigned char *const vt = tiles + stage * tile_bytes;
