@@ -232,7 +232,8 @@ def read_status(st: torch.Tensor) -> dict:
 
 def read_out_of_range(st: torch.Tensor) -> int:
     """The fourth counter of a status block: positions, lengths, sequence or page numbers that
-    pointed outside their table or pool (``aweq_kv_append``, ``aweq_prefix_attention``)."""
+    pointed outside their table or pool (``aweq_kv_append``, ``aweq_prefix_attention``, and the calls on
+    plans, accepted paths and drafted trees)."""
     return int(st[3])
 
 
@@ -581,6 +582,17 @@ class MX4:
         self.row_step = torch.empty(rows, dtype=torch.float32, device=device) if fmt == "e4m3" else None
         self.args = (_ptr(self.codes), _ptr(self.scales), _ptr(self.row_step))
         self.tag = MX4_FORMATS[fmt]
+
+    def first(self, rows):
+        """An ``MX4`` of up to as many rows, in this one's buffers."""
+        if not 0 <= rows <= self.rows:
+            raise ValueError("there are %d rows" % self.rows)
+        part = object.__new__(MX4)
+        part.rows, part.cols, part.fmt, part.tag = rows, self.cols, self.fmt, self.tag
+        part.codes, part.scales = self.codes[:rows], self.scales[:aweq_mx4_scale_bytes(rows, self.cols, self.fmt)]
+        part.row_step = None if self.row_step is None else self.row_step[:rows]
+        part.args = self.args
+        return part
 
     def quantise(self, X, scale=None, mu=None, epsmu=None, st=None):
         """Codes of X times ``scale`` (float32 per column); ``epsmu`` gets the row sums of (value - X scale) mu."""

@@ -1,4 +1,4 @@
-"""Attention of drafted trees against its definition in binary64, and a whole step of drafting as a server drives it.
+"""Attention of drafted trees against its definition in binary64.
 
 Tolerance, with u = 2^-11 (fp16) or 2^-8 (bf16): a probability is off by its score's error (head_dim products added in binary32,
 2^-23 each at worst), a few 2^-22 of the exponential and the rescalings, and by u where it is rounded for the product with v; the
