@@ -215,7 +215,7 @@ def main(n_seq: int = 16, prefix: int = 500, steps: int = 8) -> float:
     return worst
 
 
-def drafting(n_seq: int = 16, prefix: int = 500, steps: int = 8, nodes: int = 24, fmt: str = "e8m0") -> float:
+def drafting(n_seq: int = 16, prefix: int = 500, steps: int = 8, nodes: int = 24, fmt: str = "e4m3") -> float:
     wl = synth.workloads(1.0 / 128)["opt125m_model_w8a8"]
     X, W = synth.generate(wl, "cuda")
     cal = calibrate.LayerCalibrator(wl, 8, X, W)
