@@ -642,7 +642,7 @@ attention_units_kernel(const AttentionArgs a, const AttentionPlan p, const __gri
 // cut, then (m, l) and the outputs, which fly together (1024 rows 5-6 us; 8 by itself, its start included, which nothing hides).
 template <class D, int WARPS>
 __global__ void __launch_bounds__(128)
-attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsigned char *__restrict__ ws)
+attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsigned char *ws)
 {
     __shared__ float part[4][128], part_l[4];
     pdl_begin();
