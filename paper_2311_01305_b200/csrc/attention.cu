@@ -735,14 +735,14 @@ attention_join_kernel(const AttentionArgs a, const AttentionPlan p, const unsign
     }
     if (in) {
         // no key at all: zeros (keys whose scores are all minus infinity: 0 / 0, as the softmax of them is)
-        const bool none = l == 0.0f && a.prefix_len == 0 && own_length(a, b) < a.n_q - (int)(tok % (unsigned)a.n_q);
+        const bool none = l == 0.0f && a.prefix_len == 0 && clamp_length(a, a.own_len[b], false) < a.n_q - (int)(tok % (unsigned)a.n_q);
         const float inv = none ? 0.0f : 1.0f / l;
         *reinterpret_cast<uint2 *>(a.out + (long long)tok * a.ldo + (long long)h * hd + lane * 4) =
             make_uint2(D::encode2(o.x * inv, o.y * inv), D::encode2(o.z * inv, o.w * inv));
     }
     // without own keys no other kernel looks at the lengths
     if (!p.ctas && blockIdx.x == 0 && threadIdx.x < 32)
-        for (int i = lane; i < (int)a.n_seq; i += 32) clamp_length(a, __ldg(a.own_len + i), true);
+        for (int i = lane; i < (int)a.n_seq; i += 32) clamp_length(a, a.own_len[i], true);
 }
 
 // Keys of a tiled copy: a box lies in one page, on a row of the stage that keeps the swizzle's phase (a multiple of eight).

@@ -40,7 +40,9 @@ __device__ __forceinline__ float exp2_fast(float x)
 constexpr float kProbabilityShift = 7.0f;
 template <class D>
 __device__ __forceinline__ float probability_base(float m) { return D::kBf16 ? m : m - kProbabilityShift; }
-// An own length, clamped.  `count`: the one caller that reports it.
+// An own length, clamped.  `count`: the one caller that reports it.  (Lengths may come from a launch of this library that is still
+// running when a kernel starts: its first look at them is a plain load, which stays behind the wait; an invariant one need not.  A later
+// look, at a place that hangs on lengths already read, may be one.)
 __device__ __forceinline__ int clamp_length(const AttentionArgs &a, int len, bool count)
 {
     const int most = (int)min(a.max_own, a.pages_per_seq * a.page_size);
@@ -111,10 +113,11 @@ struct AttentionWalk {
     }
 };
 
+__device__ __forceinline__ int given_length(const AttentionArgs &a, int b) { return b < (int)a.n_seq ? a.own_len[b] : 0; }
 // Tiles of 32 sequences: the lane's own length and tiles, and the tiles before it.
-__device__ __forceinline__ long long scan_tiles(const AttentionArgs &a, const AttentionPlan &p, int b, bool count, int *len, int *n)
+__device__ __forceinline__ long long scan_tiles(const AttentionArgs &a, const AttentionPlan &p, int given, bool count, int *len, int *n)
 {
-    *len = clamp_length(a, b < (int)a.n_seq ? __ldg(a.own_len + b) : 0, count);
+    *len = clamp_length(a, given, count);
     *n = tiles_of(*len, p.unit);
     int sum = *n;                                               // 32 lengths of at most 2^31 keys: below 2^31 tiles
 #pragma unroll
@@ -130,9 +133,12 @@ __device__ __forceinline__ long long own_units(const AttentionArgs &a, const Att
 {
     const int lane = threadIdx.x & 31, n_seq = (int)a.n_seq, per_seq = a.n_kv * p.own_rt;
     long long total = 0;
+    int given = given_length(a, lane);
     for (int b0 = 0; b0 < n_seq; b0 += 32) {
+        const int now = given;
+        given = given_length(a, b0 + 32 + lane);                // (under way while this one is taken)
         int len, n;
-        const long long before = scan_tiles(a, p, b0 + lane, lead, &len, &n);
+        const long long before = scan_tiles(a, p, now, lead, &len, &n);
         if (lead && b0 + lane < n_seq) start[b0 + lane] = (total + before) * per_seq;
         total += __shfl_sync(0xffffffffu, before + n, 31);
     }
@@ -167,9 +173,12 @@ __device__ __forceinline__ int attention_begin(const AttentionArgs &a, const Att
     }
     const int lane = threadIdx.x & 31, n_seq = (int)a.n_seq, per_seq = a.n_kv * p.own_rt;
     long long passed = 0;
+    int given = given_length(a, lane);
     for (int b0 = 0;; b0 += 32) {
+        const int now = given;
+        given = given_length(a, b0 + 32 + lane);
         int len, n;
-        const long long mine = passed + scan_tiles(a, p, b0 + lane, false, &len, &n) * per_seq;
+        const long long mine = passed + scan_tiles(a, p, now, false, &len, &n) * per_seq;
         const uint32_t here = __ballot_sync(0xffffffffu, u0 >= mine && u0 < mine + (long long)n * per_seq);
         if (here) {
             const int src = __ffs(here) - 1, within = (int)(u0 - __shfl_sync(0xffffffffu, mine, src));

@@ -55,7 +55,7 @@ struct AppendPlace {
 __device__ __forceinline__ AppendPlace append_place(const KvAppendArgs &a, long long t, bool count)
 {
     AppendPlace w;
-    w.pos = __ldg(a.pos + t);
+    w.pos = a.pos[t];
     w.turn_ok = !a.rope || (w.pos >= 0 && w.pos < a.n_pos);
     w.at = -1;
     if (a.slot) {
@@ -72,13 +72,13 @@ __device__ __forceinline__ AppendPlace append_place(const KvAppendArgs &a, long 
         }
         return w;
     }
-    const long long s = a.seq ? __ldg(a.seq + t) : t, c = (long long)w.pos - a.first;
+    const long long s = a.seq ? a.seq[t] : t, c = (long long)w.pos - a.first;
     bool bad = !w.turn_ok || s < 0 || s >= a.n_seq;
     if (!bad && c >= 0) {
         const unsigned in_seq = (unsigned)c / (unsigned)a.page_size, row = (unsigned)c % (unsigned)a.page_size;
         bad = in_seq >= a.pages_per_seq;
         if (!bad) {
-            const long long page = __ldg(a.page_table + s * a.ld_table + in_seq);
+            const long long page = a.page_table[s * a.ld_table + in_seq];
             bad = page < 0 || page >= a.n_pages;
             if (!bad) w.at = page * a.page_stride + (long long)row * a.token_stride;
         }
