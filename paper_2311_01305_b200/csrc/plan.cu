@@ -10,7 +10,7 @@ struct PlanSeq {
     int start, held, have, want;               // first token, keys before, pages before and after
     int granted, take, give, after;            // new pages it gets, their and the returned pages' offsets in the ring, keys after
 };
-constexpr int kPlanThreads = 256, kPlanShared = 1024;      // sequences whose PlanSeq fit a CTA's shared memory
+constexpr int kPlanThreads = 512, kPlanShared = 1024;      // sequences whose PlanSeq fit a CTA's shared memory
 
 __device__ __forceinline__ int plan_pages(int keys, int page_size) { return (int)(((unsigned)keys + (unsigned)page_size - 1) / (unsigned)page_size); }
 
@@ -53,7 +53,7 @@ __device__ __forceinline__ PlanTotals plan_sequences(const KvPlanArgs &a, long l
     const long long cap = min(a.pages_per_seq * a.page_size, 0x7fffffffll);
     const long long free = given - taken;
     long long tokens = 0, more_before = 0, less_before = 0;
-    constexpr int M = 4;                       // sequences of a thread, so that two scans serve a thousand
+    constexpr int M = 2;                       // sequences of a thread, so that two scans serve a thousand
     for (int b0 = 0; b0 < (int)a.n_seq; b0 += M * kPlanThreads) {
         const int b1 = b0 + M * (int)threadIdx.x;
         int held[M], fresh[M], drop[M];
@@ -304,7 +304,7 @@ __device__ __forceinline__ void plan_fill(const KvPlanArgs &a, const PlanRing &r
 }
 
 // Up to kPlanShared sequences: every CTA works out the sequences for itself and fills its share, in one launch.  The ring's counters
-// are set by the CTA that ends last, when all have read them.
+// are set by the CTA that comes last, when all have read them.
 __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlanArgs a, unsigned *ticket)
 {
     __shared__ PlanSeq seqs[kPlanShared];
@@ -314,9 +314,8 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlanArgs 
     const PlanRing ring = plan_state(a);
     const PlanTotals all = plan_sequences(a, ring.taken, ring.given, seqs, sh, blockIdx.x == 0);
     __syncthreads();
-    plan_fill(a, ring, seqs, all.tokens, parents);
+    // (this CTA's threads have read the counters; not at the end, where the fence would wait for the stores)
     if (threadIdx.x == 0) {
-        // (this CTA's threads read the counters before the barriers above)
         __threadfence();
         if (gridDim.x == 1 || atomicAdd(ticket, 1u) == gridDim.x - 1) {
             a.state[0] = all.taken;
@@ -325,6 +324,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlanArgs 
             *ticket = 0;
         }
     }
+    plan_fill(a, ring, seqs, all.tokens, parents);
 }
 
 // More sequences: one CTA works them out, a second launch fills.
