@@ -25,8 +25,9 @@ constexpr int kTrThreads = 640, kTrQBytes = 64 * 1024, kTrRing = 160 * 1024, kTr
 constexpr int kTrSoftRegs = 104, kTrOtherRegs = 64;
 constexpr float kTrSlack = 8.0f;
 
+constexpr int kTrLanding = 8;                // tiles of a sum on which it may have an eye (at most three units are under way)
 struct TreeShared {
-    uint64_t full[kTrMaxTiles], empty[kTrMaxTiles], q_ready[2], q_free[2], s_full[2], p_ready[2], pv_done[2], o_free[2];
+    uint64_t full[2][kTrMaxTiles], empty[kTrMaxTiles], q_ready[2], q_free[2], s_full[2], p_ready[2], pv_done[2], issued[2], o_free[2];
     uint64_t item_full[kTrItems], item_empty[kTrItems];
     TreeItem item[kTrItems];
     uint32_t tmem;
@@ -104,11 +105,19 @@ struct TreeItems {
         if (ok) it = sh.item[i];
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.item_empty[i]);
+        __syncwarp();
         ++n;
         return ok;
     }
 };
 
+// eight dims of a record, a whole sector
+__device__ __forceinline__ void store32(float *to, const float (&v)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])),
+                 "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+                 "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])) : "memory");
+}
 // The rows of Q of an item's tiles, into buffer `buf`; by a warp.
 template <bool TWO>
 __device__ __forceinline__ void tree_bring(const TreeArgs &a, const TreePlan &p, const TreeItem &it, TreeShared &sh, unsigned char *qs, int buf,
@@ -153,8 +162,9 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), cta = blockIdx.x, hd = a.head_dim;
     const int halves = hd > 64 ? 2 : 1, tile_bytes = halves * 16384, n_tiles = kTrRing / tile_bytes;
     if (tid == 0) {
-        for (int i = 0; i < n_tiles; ++i) {
-            mbar_init(&sh.full[i], 1);
+        for (int i = 0; i < kTrMaxTiles; ++i) {
+            mbar_init(&sh.full[0][i], 1);
+            mbar_init(&sh.full[1][i], 1);
             mbar_init(&sh.empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -163,6 +173,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             mbar_init(&sh.s_full[i], 1);
             mbar_init(&sh.p_ready[i], 8);
             mbar_init(&sh.pv_done[i], 1);
+            mbar_init(&sh.issued[i], 1);
             mbar_init(&sh.o_free[i], TWO ? 8 : 16);
         }
         for (int i = 0; i < kTrItems; ++i) {
@@ -182,6 +193,14 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
+    // Where tile v (0: keys, 1: values) of unit g says that it has landed.  A barrier may be looked at one phase ahead and no further, so it
+    // has to have one warp that waits for all its phases: those of the ring's stages have that with two tiles, where one warp takes all
+    // units; else each sum has barriers of its own, by the number of its tiles.
+    auto landing = [&](int g, int v, uint32_t *parity) -> uint64_t * {
+        const int t = 2 * g + v, mine = (g & ~1) + v;           // tile of all, of the sum
+        *parity = TWO ? t / n_tiles & 1 : mine / kTrLanding & 1;
+        return TWO ? &sh.full[0][t % n_tiles] : &sh.full[g & 1][mine % kTrLanding];
+    };
 
     bool ok = true;
     if (warp < 4) {
@@ -206,6 +225,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                 u0 = deal.first(cta);
                 left = (int)(deal.first(cta + 1) - u0);
                 w.begin(a, p, totals, u0, s0, c0);
+                left = max(left - w.ahead, 0);
             }
             TreeItem it = {};
             auto make = [&] {
@@ -223,7 +243,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                 it.t0 = w.t0;
                 it.rec = (long long)(w.item + cta) * rec;
                 left -= it.count;
-                it.stop = left == 0;
+                it.stop = left <= totals.change;
             };
             make();
             constexpr int kBufs = TWO ? 1 : 2;
@@ -244,6 +264,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     moved = true;
                     if (!all) {
                         w.next_item(a, p);
+                        left -= totals.change;
                         make();
                     }
                 }
@@ -260,14 +281,14 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             // (gave up: let what is under way land, bounded, before the memory goes)
             if (!ok && p.group <= 128)
                 for (int i = 0; i < kBufs; ++i) mbar_wait(&sh.q_ready[i], 0);
-            tree_leave(a, p, ws, cta);
+            tree_leave(a, p, ws, cta, totals.change);
         } else if (warp == 0) {
             // ---------------------------------------------------------- copies: a unit's keys, then its values
             TreeItems items;
             TreeItem it, next;
             ok = items.next(sh, it);
-            int s = 0, tile = it.tile, left = it.count;
-            uint32_t ph = 0;
+            int s = 0, tile = it.tile, left = it.count, g = 0, told = 0;    // g: the unit, told: tiles of it that are under way
+            uint32_t ph = 0, unused;
             auto entry = [&](const TreeItem &x, int t, int r) {     // entry of the page list for the unit's r'th key, if there is such a key
                 const int key = t * p.unit + r;
                 if (key >= x.len) return 0;
@@ -294,22 +315,28 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     for (int v = 0; v < 2; ++v) {
                         ok = __all_sync(0xffffffffu, mbar_wait(&sh.empty[s], ph ^ 1));
                         if (!ok) break;
-                        if (lane == 0) mbar_arrive_expect_tx(&sh.full[s], (uint32_t)(n * p.box * 128 * halves));
+                        uint64_t *const full = landing(g, v, &unused);
+                        if (lane == 0) mbar_arrive_expect_tx(full, (uint32_t)(n * p.box * 128 * halves));
                         __syncwarp();
                         if (there)
                             for (int h = 0; h < halves; ++h)
-                                tma_load4(smem_u32(tiles + s * tile_bytes + h * 16384) + at * 128, v ? &mapV : &mapK, h * 64, kh, row, pid, smem_u32(&sh.full[s]));
+                                tma_load4(smem_u32(tiles + s * tile_bytes + h * 16384) + at * 128, v ? &mapV : &mapK, h * 64, kh, row, pid, smem_u32(full));
                         if (++s == n_tiles) { s = 0; ph ^= 1; }
+                        told = v + 1;
                     }
+                    if (!ok) break;
+                    ++g;
+                    told = 0;
                 }
             } else {
                 // pages and strides that tiled copies do not serve: 16 bytes at a time, a tile's under way while the one before lands
                 const int per = hd / 8;
-                int pending = -1;
-                auto landed = [&](int stage) {
+                uint64_t *pending = nullptr;
+                auto landed = [&](uint64_t *full) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.full[stage]);
+                    if (lane == 0) mbar_arrive(full);
+                    __syncwarp();
                 };
                 while (ok && left > 0) {
                     const int keys = min(p.unit, it.len - tile * p.unit);
@@ -332,10 +359,10 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     }
 #pragma unroll 1
                     for (int v = 0; v < 2; ++v) {
-                        if (pending >= 0 && !__all_sync(0xffffffffu, mbar_try_wait(&sh.empty[s], ph ^ 1))) {
+                        if (pending && !__all_sync(0xffffffffu, mbar_try_wait(&sh.empty[s], ph ^ 1))) {
                             asm volatile("cp.async.wait_group 0;" ::: "memory");
                             landed(pending);
-                            pending = -1;
+                            pending = nullptr;
                         }
                         ok = __all_sync(0xffffffffu, mbar_wait(&sh.empty[s], ph ^ 1));
                         if (!ok) break;
@@ -350,19 +377,25 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                                              "l"(pool + (in ? off[i] + c * 8 : 0)), "r"(in ? 16 : 0) : "memory");
                             }
                         asm volatile("cp.async.commit_group;" ::: "memory");
-                        if (pending >= 0) {
+                        if (pending) {
                             asm volatile("cp.async.wait_group 1;" ::: "memory");
                             landed(pending);
                         }
-                        pending = s;
+                        pending = landing(g, v, &unused);
                         if (++s == n_tiles) { s = 0; ph ^= 1; }
                     }
+                    if (!ok) break;
+                    ++g;
                 }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
-                if (pending >= 0) landed(pending);
+                if (pending) landed(pending);
             }
-            if (!ok)                                            // gave up: let what is under way land (bounded) before the memory goes
-                for (int i = 0; i < n_tiles; ++i) mbar_wait(&sh.full[i], ph ^ (i >= s ? 1u : 0u));
+            if (!ok && p.box)                                   // gave up: let what is under way land (bounded) before the memory goes
+                for (int t = max(2 * g + told - n_tiles, 0); t < 2 * g + told; ++t) {
+                    uint32_t parity;
+                    uint64_t *const full = landing(t >> 1, t & 1, &parity);
+                    mbar_wait(full, parity);
+                }
         } else if (!TWO || warp == 1) {
             // ---------------------------------------------------------- products: a warp for both sums of two tiles, else one for each
             const bool lead = tc_elect();
@@ -376,8 +409,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             constexpr int kEach = TWO ? 1 : 2;
             int left = 0, rest = 0, n_item = -1, of = 0, stop = 0, both = 0, done = 0;
             // the stages of the next K and V tiles
-            int ks = 2 * mine, vs = ks + 1;
-            uint32_t kph = 0, vph = 0;
+            int ks = 2 * mine, vs = ks + 1, kg = mine, vg = mine;           // and their units
             struct Unit { int both, fresh, steps, last, buf; };
             auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
             auto there = [](uint64_t *bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, mbar_wait(bar, parity)); };
@@ -409,12 +441,15 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                 ++of;
                 return 1;
             };
-            auto step = [&](int &stage, uint32_t &phase) {
+            auto step = [&](int &stage, int &g) {
                 stage += 2 * kEach;
-                if (stage >= n_tiles) { stage -= n_tiles; phase ^= 1; }
+                if (stage >= n_tiles) stage -= n_tiles;
+                g += kEach;
             };
-            auto keys_there = [&] {
-                const bool r = there(&sh.full[ks], kph);
+            auto tile_there = [&](int g, int v) {
+                uint32_t parity;
+                uint64_t *const full = landing(g, v, &parity);
+                const bool r = there(full, parity);
                 tc_fence_after();
                 return r;
             };
@@ -428,7 +463,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             auto keys_done = [&](const Unit &u) {
                 tc_commit<1>(&sh.empty[ks], lead);
                 if (u.last) tc_commit<1>(&sh.q_free[u.buf], lead);
-                step(ks, kph);
+                step(ks, kg);
             };
             struct Passes { uint32_t softmax, items; } pass0 = {1, 0}, pass1 = {1, 0};
             auto values = [&](int sum, const Unit &u, Passes &n) {          // O += P V
@@ -448,12 +483,12 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             };
             auto values_done = [&] {
                 tc_commit<1>(&sh.empty[vs], lead);
-                step(vs, vph);
+                step(vs, vg);
             };
             Unit u, next = {};
             int more = next_unit(u);
             // (the softmax's first pass writes where S will be)
-            if (more > 0 && (ok = there(&sh.p_ready[mine], 0) && (!TWO || there(&sh.p_ready[1], 0)) && keys_there())) {
+            if (more > 0 && (ok = there(&sh.p_ready[mine], 0) && (!TWO || there(&sh.p_ready[1], 0)) && tile_there(kg, 0))) {
                 scores(mine, u);
                 if (TWO && u.both) scores(1, u);
                 keys_done(u);
@@ -461,10 +496,10 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             // each sum's scores of its next unit behind its values of this one
             while (ok && more > 0) {
                 more = next_unit(next);
-                if (!(ok = more >= 0 && there(&sh.full[vs], vph) && values(mine, u, pass0))) break;
+                if (!(ok = more >= 0 && tile_there(vg, 1) && values(mine, u, pass0))) break;
                 if (!TWO) values_done();
                 if (more) {
-                    if (!(ok = keys_there())) break;
+                    if (!(ok = tile_there(kg, 0))) break;
                     scores(mine, next);
                 }
                 if (TWO) {
@@ -476,6 +511,9 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                 u = next;
             }
             ok = ok && more >= 0;
+            // (no arrival of these products may be under way when the CTA ends)
+            tc_commit<1>(&sh.issued[mine], lead);
+            ok = there(&sh.issued[mine], 0) && ok;
         }
     } else {
         // -------------------------------------------------------------- softmax: two threads to a row, half of a unit's keys each
@@ -517,9 +555,10 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     // there (NaN, say) would not be
                     const int zeros = (keys + 15) / 16 * 16 - keys;
                     if (zeros && !warm) {                       // (both sums do it: neither's product waits for the other's rows)
-                        const int t = 2 * (done + u) + 1, stage = t % n_tiles;
-                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&sh.full[stage], (t / n_tiles) & 1)))) break;
-                        unsigned char *const vt = tiles + stage * tile_bytes;
+                        uint32_t parity;
+                        uint64_t *const full = landing(done + u, 1, &parity);
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(full, parity)))) break;
+                        unsigned char *const vt = tiles + (2 * (done + u) + 1) % n_tiles * tile_bytes;
                         for (int i = half * 128 + r; i < zeros * halves * 8; i += 256) {
                             const int piece = i % (halves * 8);
                             *reinterpret_cast<uint4 *>(vt + (piece >> 3) * 16384 + (keys + i / (halves * 8)) * 128 + ((piece & 7) << 4)) = make_uint4(0, 0, 0, 0);
@@ -596,6 +635,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.p_ready[sum]);
+                    __syncwarp();
                     ++cnt;
                     fresh = false;
                 }
@@ -630,9 +670,10 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
 #pragma unroll
                             for (int j = 0; j < 32; j += 8)
                                 if (c + j < hd) {
-                                    uint4 *const to = reinterpret_cast<uint4 *>(dst + ((c + j) >> 3) * step);
-                                    to[0] = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-                                    to[1] = make_uint4(o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
+                                    float v[8];
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(o[j + i]);
+                                    store32(dst + ((c + j) >> 3) * step, v);
                                 }
                     }
                 }
@@ -652,6 +693,8 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                 const float to = fmaxf(b0, b1), from = to == -CUDART_INF_F ? 0.0f : to, f0 = exp2_fast(b0 - from), f1 = exp2_fast(b1 - from);
                 const bool only0 = it.count < 2 && ((done - it.count) & 1) == 0, only1 = it.count < 2 && !only0;
                 if (r < mine && sum == 0 && !half) ml[rec] = make_float2(to, only0 ? l0 : only1 ? l1 : l0 * f0 + l1 * f1);
+                __syncwarp();
+                if (!(ok = meet4())) break;                     // (all have read what the next pass overwrites)
                 const int c = (sum * 2 + half) * 32;
                 if (c < hd) {
                     uint32_t x[32], y[32];
@@ -668,9 +711,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                                     const float p0 = __uint_as_float(x[j + i]), p1 = __uint_as_float(y[j + i]);
                                     v[i] = only0 ? p0 : only1 ? p1 : p0 * f0 + p1 * f1;
                                 }
-                                float4 *const at8 = reinterpret_cast<float4 *>(dst + ((c + j) >> 3) * step);
-                                at8[0] = make_float4(v[0], v[1], v[2], v[3]);
-                                at8[1] = make_float4(v[4], v[5], v[6], v[7]);
+                                store32(dst + ((c + j) >> 3) * step, v);
                             }
                 }
             }
@@ -684,6 +725,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     if (it.count > 1 || ((done - it.count) & 1) == 1) mbar_arrive(&sh.o_free[1]);
                 }
             }
+            __syncwarp();
         } while (!it.stop);
         if (!ok) {
             if (lane == 0) sh.gave_up[pair] = 1;
@@ -833,8 +875,9 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, int parts, const unsigned c
         const unsigned in_all = (unsigned)(tok * G + g), in_seq = (unsigned)(node * G + g), rt0 = in_all / (unsigned)p.rows, rt1 = in_seq / (unsigned)p.rows;
         const long long item0 = (long long)kh * totals.pre_rt + rt0;
         const int within = kh * s.n_rt + (int)rt1;
-        const long long u = lane & 2 ? totals.pre + s.unit + (long long)within * s.tiles + (lane & 1 ? s.tiles - 1 : 0)
-                                     : item0 * p.pre_tiles + (lane & 1 ? p.pre_tiles - 1 : 0);
+        const int tiles = lane & 2 ? s.tiles : p.pre_tiles;
+        const long long u = (lane & 2 ? totals.pre + s.unit : 0) + ((lane & 2) ? (long long)within : item0) * (tiles + totals.change) + totals.change +
+                            (lane & 1 ? tiles - 1 : 0);
         AttentionDeal deal(0, 1);
         deal.each = totals.each;
         deal.more = totals.more;

@@ -18,7 +18,11 @@ struct TreePlan {
     size_t off_seq, off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
 };
 struct alignas(16) TreeFirst { long long unit; int item, tiles, t0, nodes, base, n_rt; };
-struct alignas(16) TreeTotals { long long pre, own, each, more; int tokens, pre_rt, ctas; };     // each, more, ctas: how the units are dealt
+// How the units are dealt: evenly, an item counting `change` units more than it has, ahead of its own (the record that a CTA writes when
+// it leaves an item takes as long as two or three units: 16 trees of 24 after 512 + 2100 keys @@ us without, @@ with two).
+// pre, own: units of both kinds so counted; each, more: units of a CTA, CTAs with one more.
+struct alignas(16) TreeTotals { long long pre, own, each, more; int tokens, pre_rt, ctas, change; };
+constexpr int kTrChange = 2, kTrChangeFrom = 4;     // with as many units to a CTA or more
 
 // A sequence's new tokens and the keys before them, clamped.
 struct TreeSeq { int t0, t1, nodes, ctx, base; bool bad; };  // base: key of node 0
@@ -42,22 +46,34 @@ __device__ __forceinline__ TreeSeq tree_load(const TreeArgs &a, int b)
 __device__ __forceinline__ int tree_tokens(const TreeArgs &a) { return min(max(a.start[a.n_seq], 0), a.max_tokens); }
 __device__ __forceinline__ int tree_tiles(int n, int of) { return (int)(((unsigned)n + (unsigned)of - 1) / (unsigned)of); }
 
-// own units and items of 32 sequences: the lane's, and those before it
-struct TreeScan { long long units, unit0; int items, item0; };
+// own units and items of 32 sequences, and the items that have units: the lane's, and those before it
+struct TreeScan {
+    long long units, unit0;
+    int items, item0, busy, busy0;
+    __device__ __forceinline__ TreeScan counted(int change) const           // units as they are dealt
+    {
+        TreeScan r = *this;
+        r.units += (long long)change * busy;
+        r.unit0 += (long long)change * busy0;
+        return r;
+    }
+};
 __device__ __forceinline__ TreeScan tree_scan(const TreeArgs &a, const TreePlan &p, const TreeSeq &s)
 {
     const int lane = threadIdx.x & 31;
     TreeScan r;
     r.items = a.n_kv * tree_tiles(s.nodes * p.group, p.rows);
     r.units = (long long)r.items * tree_tiles(s.ctx, p.unit);
+    r.busy = s.ctx > 0 ? r.items : 0;
     long long u = r.units;
-    int i = r.items;
+    int i = r.items, k = r.busy;
 #pragma unroll 1
     for (int x = 1; x < 32; x <<= 1) {
         const long long v = __shfl_up_sync(0xffffffffu, u, x);
-        const int w = __shfl_up_sync(0xffffffffu, i, x);
-        if (lane >= x) { u += v; i += w; }
+        const int w = __shfl_up_sync(0xffffffffu, i, x), y = __shfl_up_sync(0xffffffffu, k, x);
+        if (lane >= x) { u += v; i += w; k += y; }
     }
+    r.busy0 = k - r.busy;
     r.unit0 = u - r.units;
     r.item0 = i - r.items;
     return r;
@@ -68,6 +84,7 @@ __device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreeP
     TreeTotals t;
     t.tokens = tree_tokens(a);
     t.own = 0;
+    long long busy = 0;
     for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
         const TreeSeq s = tree_load(a, b0 + (int)(threadIdx.x & 31));
         const TreeScan c = tree_scan(a, p, s);
@@ -76,14 +93,19 @@ __device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreeP
             c0 = c;
         }
         t.own += __shfl_sync(0xffffffffu, c.unit0 + c.units, 31);
+        busy += __shfl_sync(0xffffffffu, c.busy0 + c.busy, 31);
     }
     t.pre_rt = tree_tiles(t.tokens * p.group, p.rows);
-    t.pre = (long long)a.n_kv * t.pre_rt * p.pre_tiles;
+    const long long items = p.pre_tiles ? (long long)a.n_kv * t.pre_rt : 0;
+    t.change = t.own + items * p.pre_tiles >= (long long)kTrChangeFrom * p.ctas ? kTrChange : 0;
+    t.own += busy * t.change;
+    t.pre = items * (p.pre_tiles + t.change);
+    c0 = c0.counted(t.change);
     return t;
 }
 // What the join needs, in scratch: every ctas'th sequence's first unit and item, and the sequence of its tokens.  Lengths and starts out
 // of range are counted here, once.
-__device__ __forceinline__ void tree_leave(const TreeArgs &a, const TreePlan &p, unsigned char *ws, int cta)
+__device__ __forceinline__ void tree_leave(const TreeArgs &a, const TreePlan &p, unsigned char *ws, int cta, int change)
 {
     const int lane = threadIdx.x & 31;
     TreeFirst *const first = reinterpret_cast<TreeFirst *>(ws + sizeof(TreeTotals));
@@ -92,7 +114,7 @@ __device__ __forceinline__ void tree_leave(const TreeArgs &a, const TreePlan &p,
     int items = 0;
     for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
         const TreeSeq s = tree_load(a, b0 + lane);
-        const TreeScan c = tree_scan(a, p, s);
+        const TreeScan c = tree_scan(a, p, s).counted(change);
         const bool mine = b0 + lane < a.n_seq && (unsigned)(b0 + lane) % (unsigned)p.ctas == (unsigned)cta;
         if (mine) {
             first[b0 + lane] = {units + c.unit0, items + c.item0, tree_tiles(s.ctx, p.unit), s.t0, s.nodes, s.base, tree_tiles(s.nodes * p.group, p.rows)};
@@ -121,6 +143,7 @@ struct alignas(16) TreeItem {
 // key heads.
 struct TreeWalk {
     int own, b, kh, rt, tile, tiles, n_rt, len, t0, n_tok, item;     // t0, n_tok: the tokens whose rows they are
+    int ahead;                                                       // counted units before the first
     __device__ __forceinline__ void take(const TreePlan &p, const TreeSeq &s, int src)
     {
         t0 = __shfl_sync(0xffffffffu, s.t0, src);
@@ -146,17 +169,22 @@ struct TreeWalk {
             item += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
         }
     }
+    __device__ __forceinline__ void place(int counted, int change)
+    {
+        tile = max(counted - change, 0);
+        ahead = max(change - counted, 0);
+    }
     __device__ __forceinline__ void begin(const TreeArgs &a, const TreePlan &p, const TreeTotals &t, long long u0, const TreeSeq &s0, const TreeScan &c0)
     {
-        own = b = kh = rt = tile = tiles = n_rt = len = t0 = n_tok = item = 0;
+        own = b = kh = rt = tile = tiles = n_rt = len = t0 = n_tok = item = ahead = 0;
         const int lane = threadIdx.x & 31;
         if (u0 < t.pre) {
             tiles = p.pre_tiles;
             len = (int)a.prefix_len;
             n_tok = t.tokens;
             n_rt = tree_tiles(n_tok * p.group, p.rows);
-            item = (int)div_units(u0, tiles);
-            tile = (int)(u0 - (long long)item * tiles);
+            item = (int)div_units(u0, tiles + t.change);
+            place((int)(u0 - (long long)item * (tiles + t.change)), t.change);
             kh = item / n_rt;
             rt = item - kh * n_rt;
             return;
@@ -166,7 +194,7 @@ struct TreeWalk {
         int items = 0;
         for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
             const TreeSeq s = b0 ? tree_load(a, b0 + lane) : s0;
-            const TreeScan c = b0 ? tree_scan(a, p, s) : c0;
+            const TreeScan c = b0 ? tree_scan(a, p, s).counted(t.change) : c0;
             const uint32_t here = __ballot_sync(0xffffffffu, u >= passed + c.unit0 && u < passed + c.unit0 + c.units);
             if (here) {
                 const int src = __ffs(here) - 1;
@@ -174,8 +202,8 @@ struct TreeWalk {
                 b = b0 + src;
                 const long long within = u - passed - __shfl_sync(0xffffffffu, c.unit0, src);
                 take(p, s, src);
-                const int i = (int)div_units(within, tiles);
-                tile = (int)(within - (long long)i * tiles);
+                const int i = (int)div_units(within, tiles + t.change);
+                place((int)(within - (long long)i * (tiles + t.change)), t.change);
                 kh = i / n_rt;
                 rt = i - kh * n_rt;
                 item = items + __shfl_sync(0xffffffffu, c.item0, src) + i;
