@@ -178,6 +178,19 @@ def test_many_sequences_and_a_long_context():
     Case([40], [30000], 8, 2, 128, 5000, 16, torch.bfloat16).check()
 
 
+@pytest.mark.parametrize("nodes,d,ctx", [(16, 128, 6000), (16, 64, 6000), (64, 128, 2500)])
+def test_first_calls_over_a_big_pool(nodes, d, ctx):
+    """Pages all over a pool that nothing has looked at yet: tiles land in any order."""
+    Case([nodes] * 32, [(i * 977) % ctx + ctx // 4 for i in range(32)], 32, 8, d, 0, 64, torch.bfloat16, stale=False).check()
+
+
+@pytest.mark.parametrize("most,prefix", [(130, 0), (400, 130), (1100, 600)])
+def test_many_short_items(most, prefix):
+    """Several items to a CTA and units enough that an item counts for more than its own: cuts everywhere."""
+    Case([1 + i % 5 for i in range(150)], [(i * 131) % most for i in range(150)], 16, 8, 64, prefix, 16, torch.float16).check()
+    Case([1 + i % 40 for i in range(90)], [(i * 173) % most for i in range(90)], 32, 8, 128, prefix, 32, torch.bfloat16).check()
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.1, 1e-3, 3.0])
 def test_scales(scale):
     Case([5, 40], [200, 333], 8, 2, 64, 100, 16, torch.float16, spread=1.0).check(scale=scale)
