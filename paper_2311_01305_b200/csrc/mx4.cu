@@ -264,6 +264,7 @@ mx4_dequant_kernel(const unsigned char *codes, const unsigned char *scales, cons
 {
     pdl_begin();
     const long long total = rows * chunks, step = (long long)gridDim.x * 256;
+    const bool wide = ldo % 16 == 0 && (reinterpret_cast<uintptr_t>(out) & 31) == 0;       // a chunk is a sector
     constexpr int U = 4;                                        // chunks of 16 columns under way
     for (long long i0 = (long long)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += U * step) {
         uint2 c[U];
@@ -295,9 +296,14 @@ mx4_dequant_kernel(const unsigned char *codes, const unsigned char *scales, cons
             for (int j = 0; j < 8; ++j)
                 o[j] = FMT == AWEQ_MX4_E8M0 ? D::encode2(v[2 * j] * s, v[2 * j + 1] * s)
                                             : D::encode2(__fmul_rn(__fmul_rn(v[2 * j], s), r[k]), __fmul_rn(__fmul_rn(v[2 * j + 1], s), r[k]));
-            uint4 *const to = reinterpret_cast<uint4 *>(dst[k]);
-            to[0] = make_uint4(o[0], o[1], o[2], o[3]);
-            to[1] = make_uint4(o[4], o[5], o[6], o[7]);
+            if (wide)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst[k]), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]),
+                             "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+            else {
+                uint4 *const to = reinterpret_cast<uint4 *>(dst[k]);
+                to[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                to[1] = make_uint4(o[4], o[5], o[6], o[7]);
+            }
         }
     }
 }
