@@ -19,7 +19,8 @@ struct TreePlan {
 };
 struct alignas(16) TreeFirst { long long unit; int item, tiles, t0, nodes, base, n_rt; };
 // How the units are dealt: evenly, an item counting `change` units more than it has, ahead of its own (the record that a CTA writes when
-// it leaves an item takes as long as two or three units: 16 trees of 24 after 512 + 2100 keys @@ us without, @@ with two).
+// it leaves an item takes as long as two or three units: 16 trees of 24 nodes after 512 + 2100 keys 56 us without, 50 with two; one and
+// three are within 2 % of two over seven shapes, but for 128 short items, where one would be 4 % faster).
 // pre, own: units of both kinds so counted; each, more: units of a CTA, CTAs with one more.
 struct alignas(16) TreeTotals { long long pre, own, each, more; int tokens, pre_rt, ctas, change; };
 constexpr int kTrChange = 2, kTrChangeFrom = 4;     // with as many units to a CTA or more
