@@ -555,9 +555,10 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     if (!TWO && !warm && ((done + u) & 1) != sum) continue;
                     const int keys = min(p.unit, it.len - (it.tile + u) * p.unit);
                     // values past the last key, up to the product's step of 16: zero, because a zero probability times whatever lay
-                    // there (NaN, say) would not be
+                    // there (NaN, say) would not be.  (Of two tiles the first sum does it, whose product comes first; the second may have skipped
+                    // items and would look at the tile's barrier phases ahead.)
                     const int zeros = (keys + 15) / 16 * 16 - keys;
-                    if (zeros && !warm) {                       // (both sums do it: neither's product waits for the other's rows)
+                    if (zeros && (!TWO || sum == 0) && !warm) {
                         uint32_t parity;
                         uint64_t *const full = landing(done + u, 1, &parity);
                         if (!(ok = __all_sync(0xffffffffu, mbar_wait(full, parity)))) break;
@@ -663,6 +664,8 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     if (half) sh.top[sum][1][r] = l;
                     if (!(ok = meet())) break;
                     if (r < mine && !half) ml[rec] = make_float2(base, l + sh.top[sum][1][r]);
+                    __syncwarp();
+                    if (!(ok = meet())) break;                  // (read before the next pass overwrites it)
 #pragma unroll 1
                     for (int c = half * 64; c < min(hd, half * 64 + 64); c += 32) {
                         uint32_t o[32];

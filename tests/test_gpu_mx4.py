@@ -263,6 +263,21 @@ def test_inputs_with_a_pitch_and_scales_left_alone():
     assert (left == 0xAB).all()
 
 
+@pytest.mark.parametrize("ldo,offset", [(104, 0), (112, 8), (112, 16), (96, 8)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_values_into_a_pitch(fmt, ldo, offset):
+    """Rows that start on a sector, and such as only start on 16 bytes: the same values, and nothing around them."""
+    x, s = activations(37, 96, torch.bfloat16, 61)
+    q = quantised(x, s, fmt)
+    buf = torch.full((38 * ldo + offset,), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[offset:].as_strided((37, 96), (ldo, 1))
+    want = q.values()
+    q.values(out)
+    assert torch.equal(out, want)
+    out.fill_(7.0)
+    assert (buf == 7).all()
+
+
 def test_no_tokens():
     layer = aweq.LinearMX4(torch.ones((8, 32), dtype=torch.float16, device="cuda"), "e8m0")
     assert layer(aweq.MX4(0, 32, "e8m0")).shape == (0, 8)

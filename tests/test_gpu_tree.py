@@ -191,6 +191,16 @@ def test_many_short_items(most, prefix):
     Case([1 + i % 40 for i in range(90)], [(i * 173) % most for i in range(90)], 32, 8, 128, prefix, 32, torch.bfloat16).check()
 
 
+@pytest.mark.parametrize("most_nodes,h", [(40, 32), (30, 32), (5, 16)])
+def test_the_same_answer_every_time(most_nodes, h):
+    """Items of one and of two row tiles in turn, so that the sums of a CTA skip some of them; every run's output bit by bit."""
+    case = Case([1 + i % most_nodes for i in range(90)], [(i * 173) % 1100 for i in range(90)], h, 8, 128, 600, 32, torch.bfloat16)
+    want = case.check()
+    attend, total = case.attend(), sum(case.counts)
+    for _ in range(30):
+        assert torch.equal(attend(case.q, case.table, case.own_len, case.start, case.mask)[:total], want[:total])
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.1, 1e-3, 3.0])
 def test_scales(scale):
     Case([5, 40], [200, 333], 8, 2, 64, 100, 16, torch.float16, spread=1.0).check(scale=scale)
