@@ -29,8 +29,8 @@ __device__ __forceinline__ Mx4Col mx4_col(const Mx4LinearArgs &p, long long o)
 // out first: then the next tile's products may start.  Scales have 96 columns, two buffers (E4M3) or four, since a copy into TMEM is
 // not in order with the products before it: the buffer's last products are waited for (that many stages back, so the pipe stays fed).
 // Warps: 0 copies, 1 issues the products (in the pair's even CTA), 4-11 write the output, two to a quarter of the TMEM lanes.
-// 4099 x 5120 x 13824 in blocks of 32: 110 us by itself, 5.3 PFLOP/s (3.4 of the measured bf16 rates; nominal is 4), 120 us in a row at
-// the power cap.  A stage of 256 columns takes 880 cycles for 512 of products: the tensor pipe is 65 % busy, the L2 sends every SM 53
+// 4099 x 5120 x 13824 in blocks of 32: 110-120 us by itself, 4.8-5.3 PFLOP/s (3.1 to 3.4 of the measured bf16
+// rates; nominal is 4), 130 in a row at the power cap.  A stage of 256 columns takes 880 cycles for 512 of products: the tensor pipe is 65 to 70 % busy, the L2 sends every SM 53
 // bytes a cycle, near its limit; larger tiles do not fit TMEM beside the scales.  Scales' copies by a warp of their own: 127 us.
 constexpr int kM4BigStages = 5, kM4BigThreads = 384, kM4Overlap = 96, kM4ScaleCols = 96;
 constexpr int kM4SecondAcc = 256 - kM4Overlap, kM4Scales = 512 - kM4ScaleCols;

@@ -15,8 +15,8 @@
 // Warps: 0 copies keys and values, 1 issues the products (1 and 2 those of a sum each where the sums take units in turn: one warp for
 // both took longer to issue them than the softmax took; two tiles on the same keys have to go in step, and two warps that wait for one
 // another's keys were slower, 250 us to 190), 3 says which items come and brings their rows of Q, 4-11 and 12-19 the softmax.
-// Measured on the device, by itself: 16 trees of 24 nodes after 512 + 2100 keys, 32 / 8 heads of 128, 32-35 us (and the join 18), 32 of 64 after
-// 8192 keys 172-188 us (and 51): 3.7 TB/s of keys and values, 690 TFLOP/s.  Bound by the chain of a unit's steps (scores, maxima,
+// Measured on the device, by itself: 16 trees of 24 nodes after 512 + 2100 keys, 32 / 8 heads of 128, 33-36 us (and the join 18), 32 of 64 after
+// up to 8192 keys 180-210 us (and 51): 3.6 TB/s of keys and values, 660 TFLOP/s, tensor pipe 46 %.  Bound by the chain of a unit's steps (scores, maxima,
 // exponentials, products: 3000 cycles, two under way) and, for short items, by start (7 us) and records (6000 cycles an item).
 #include "tree.cuh"
 #include "tensorcore.cuh"
