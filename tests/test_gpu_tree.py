@@ -157,6 +157,12 @@ def test_pages_and_layouts(page, layout):
     Case([3, 30, 8, 1], [3, 300, 511, 129], 8, 4, 128, 200, page, torch.bfloat16, layout).check()
 
 
+@pytest.mark.parametrize("layout", ["tokens", "heads", "joint"])
+@pytest.mark.parametrize("page", [7, 24, 64, 100, 256])
+def test_pages_and_layouts_with_two_tiles(page, layout):
+    Case([70, 3, 90, 64], [511, 129, 300, 40], 8, 4, 128, 200, page, torch.float16, layout).check()
+
+
 @pytest.mark.parametrize("ctx", [0, 1, 2, 15, 16, 17, 120, 127, 128, 129, 143, 144, 255, 256, 257, 640, 3000])
 def test_contexts(ctx):
     """One tile of rows, whose units alternate, and two on the same keys."""
