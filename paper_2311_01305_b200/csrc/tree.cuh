@@ -27,22 +27,33 @@ constexpr int kTrChange = 2, kTrChangeFrom = 4;     // with as many units to a C
 
 // A sequence's new tokens and the keys before them, clamped.
 struct TreeSeq { int t0, t1, nodes, ctx, base; bool bad; };  // base: key of node 0
-__device__ __forceinline__ TreeSeq tree_seq(const TreeArgs &a, int s0, int s1, int len)
+// Of 32 sequences, a lane each (b: the lane's).  A start below one before it counts as that one, so that no token belongs to two
+// sequences and the rows of all are no more than the tokens', which the scratch is made for.  top: where the sequences before these end.
+__device__ __forceinline__ TreeSeq tree_load(const TreeArgs &a, int b, int top)
 {
+    const bool in = b < a.n_seq;
+    const int s0 = in ? a.start[b] : 0, s1 = in ? a.start[b + 1] : 0, len = in ? a.own_len[b] : 0;
     const int cap = (int)min(a.max_own, a.pages_per_seq * a.page_size);
     TreeSeq s;
     s.t0 = min(max(s0, 0), a.max_tokens);
-    s.t1 = min(max(s1, s.t0), a.max_tokens);
+    s.t1 = min(max(s1, 0), a.max_tokens);
+    if (__any_sync(0xffffffffu, in && (s.t0 < top || s.t1 < s.t0))) {
+        s.t0 = max(s.t0, top);
+#pragma unroll 1
+        for (int x = 1; x < 32; x <<= 1) s.t0 = max(s.t0, __shfl_up_sync(0xffffffffu, s.t0, x));      // (the lowest lanes get their own)
+        s.t1 = max(s.t0, s.t1);
+    }
     const int l = min(max(len, 0), cap);
     s.nodes = min(s.t1 - s.t0, a.max_nodes);
     s.base = l - s.nodes;
     s.ctx = max(s.base, 0);
     s.bad = s.t0 != s0 || s.t1 != s1 || s.nodes != s.t1 - s.t0 || l != len || l < s.nodes;
-    return s;
+    return in ? s : TreeSeq{0, 0, 0, 0, 0, false};
 }
-__device__ __forceinline__ TreeSeq tree_load(const TreeArgs &a, int b)
+// Where the 32 sequences from b0 on end.
+__device__ __forceinline__ int tree_end(const TreeArgs &a, const TreeSeq &s, int b0, int top)
 {
-    return b < a.n_seq ? tree_seq(a, a.start[b], a.start[b + 1], a.own_len[b]) : TreeSeq{0, 0, 0, 0, 0, false};
+    return max(top, __shfl_sync(0xffffffffu, s.t1, min(31, max(a.n_seq - 1 - b0, 0))));
 }
 __device__ __forceinline__ int tree_tokens(const TreeArgs &a) { return min(max(a.start[a.n_seq], 0), a.max_tokens); }
 __device__ __forceinline__ int tree_tiles(int n, int of) { return (int)(((unsigned)n + (unsigned)of - 1) / (unsigned)of); }
@@ -86,8 +97,10 @@ __device__ __forceinline__ TreeTotals tree_totals(const TreeArgs &a, const TreeP
     t.tokens = tree_tokens(a);
     t.own = 0;
     long long busy = 0;
+    int top = 0;
     for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
-        const TreeSeq s = tree_load(a, b0 + (int)(threadIdx.x & 31));
+        const TreeSeq s = tree_load(a, b0 + (int)(threadIdx.x & 31), top);
+        top = tree_end(a, s, b0, top);
         const TreeScan c = tree_scan(a, p, s);
         if (b0 == 0) {
             s0 = s;
@@ -112,9 +125,10 @@ __device__ __forceinline__ void tree_leave(const TreeArgs &a, const TreePlan &p,
     TreeFirst *const first = reinterpret_cast<TreeFirst *>(ws + sizeof(TreeTotals));
     int *const seq_of = reinterpret_cast<int *>(ws + p.off_seq);
     long long units = 0;
-    int items = 0;
+    int items = 0, top = 0;
     for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
-        const TreeSeq s = tree_load(a, b0 + lane);
+        const TreeSeq s = tree_load(a, b0 + lane, top);
+        top = tree_end(a, s, b0, top);
         const TreeScan c = tree_scan(a, p, s).counted(change);
         const bool mine = b0 + lane < a.n_seq && (unsigned)(b0 + lane) % (unsigned)p.ctas == (unsigned)cta;
         if (mine) {
@@ -144,10 +158,11 @@ struct alignas(16) TreeItem {
 // key heads.
 struct TreeWalk {
     int own, b, kh, rt, tile, tiles, n_rt, len, t0, n_tok, item;     // t0, n_tok: the tokens whose rows they are
-    int ahead;                                                       // counted units before the first
+    int ahead, top;                                                  // counted units before the first; where the sequences so far end
     __device__ __forceinline__ void take(const TreePlan &p, const TreeSeq &s, int src)
     {
         t0 = __shfl_sync(0xffffffffu, s.t0, src);
+        top = __shfl_sync(0xffffffffu, s.t1, src);
         n_tok = __shfl_sync(0xffffffffu, s.nodes, src);
         len = __shfl_sync(0xffffffffu, s.ctx, src);
         tiles = tree_tiles(len, p.unit);
@@ -157,7 +172,7 @@ struct TreeWalk {
     {
         own = 1;
         for (int b0 = to;; b0 += 32) {
-            const TreeSeq s = tree_load(a, b0 + (int)(threadIdx.x & 31));
+            const TreeSeq s = tree_load(a, b0 + (int)(threadIdx.x & 31), top);
             const TreeScan c = tree_scan(a, p, s);
             const uint32_t here = __ballot_sync(0xffffffffu, c.units > 0);
             if (here || b0 + 32 >= a.n_seq) {
@@ -168,6 +183,7 @@ struct TreeWalk {
                 return;
             }
             item += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
+            top = tree_end(a, s, b0, top);
         }
     }
     __device__ __forceinline__ void place(int counted, int change)
@@ -177,7 +193,7 @@ struct TreeWalk {
     }
     __device__ __forceinline__ void begin(const TreeArgs &a, const TreePlan &p, const TreeTotals &t, long long u0, const TreeSeq &s0, const TreeScan &c0)
     {
-        own = b = kh = rt = tile = tiles = n_rt = len = t0 = n_tok = item = ahead = 0;
+        own = b = kh = rt = tile = tiles = n_rt = len = t0 = n_tok = item = ahead = top = 0;
         const int lane = threadIdx.x & 31;
         if (u0 < t.pre) {
             tiles = p.pre_tiles;
@@ -194,7 +210,7 @@ struct TreeWalk {
         long long passed = 0;
         int items = 0;
         for (int b0 = 0; b0 < a.n_seq; b0 += 32) {
-            const TreeSeq s = b0 ? tree_load(a, b0 + lane) : s0;
+            const TreeSeq s = b0 ? tree_load(a, b0 + lane, top) : s0;
             const TreeScan c = b0 ? tree_scan(a, p, s).counted(t.change) : c0;
             const uint32_t here = __ballot_sync(0xffffffffu, u >= passed + c.unit0 && u < passed + c.unit0 + c.units);
             if (here) {
@@ -212,6 +228,7 @@ struct TreeWalk {
             }
             passed += __shfl_sync(0xffffffffu, c.unit0 + c.units, 31);
             items += __shfl_sync(0xffffffffu, c.item0 + c.items, 31);
+            top = tree_end(a, s, b0, top);
         }
     }
     __device__ __forceinline__ void next_item(const TreeArgs &a, const TreePlan &p)

@@ -1,0 +1,79 @@
+"""Attention of drafted trees on starts, lengths and trees that are not as they should be: what is out of range is counted, what is
+well formed keeps its outputs, and nothing is written outside the buffers."""
+import pytest
+import torch
+
+from paper_2311_01305_b200 import aweq
+
+from .test_gpu_tree import Case, i32
+
+pytestmark = pytest.mark.gpu
+
+
+def guarded(case, starts, max_nodes=None):
+    """The outputs for other starts, with scratch and output inside larger buffers that have to stay as they were; what was counted."""
+    c, h, d = case, case.q.shape[1], case.q.shape[2]
+    nodes, n_seq = max_nodes or c.max_nodes, len(c.counts)
+    size = -(-aweq.aweq_tree_attention_workspace_bytes(c.cache, c.prefix, 2 ** 31 - 1, n_seq, c.rows, nodes, h) // 256) * 256
+    ws, out = torch.full((size + (64 << 20),), 0xA5, dtype=torch.uint8, device="cuda"), torch.full((c.rows + 64, h, d), 9.0, dtype=c.dtype, device="cuda")
+    assert ws.data_ptr() % 256 == 0
+    st = aweq.new_status()
+    aweq.aweq_tree_attention(c.q, c.cache, c.prefix_pages, c.prefix, c.table, c.own_len, starts, c.mask, 2 ** 31 - 1, nodes, d ** -0.5, out[:c.rows], ws[:size], st)
+    assert (ws[size:] == 0xA5).all(), "write behind the scratch"
+    assert (out[c.rows:] == 9).all() and aweq.read_status(st)["wait_timeout"] == 0
+    return out[:c.rows], aweq.read_out_of_range(st)
+
+
+def sequences(case, starts, max_nodes):
+    """Each sequence's number of tokens, a start counting as the largest up to it, and those that have a start or length out of range."""
+    starts, length = starts.cpu(), case.own_len.cpu()
+    up = torch.cummax(starts.clamp(0, case.rows), 0).values
+    nodes = up[1:] - up[:-1]
+    cap = case.table.shape[1] * case.cache.page_size
+    return nodes, (up[:-1] != starts[:-1]) | (up[1:] != starts[1:]) | (nodes > max_nodes) | (length > cap) | (length < nodes.clamp(max=max_nodes))
+
+
+@pytest.mark.parametrize("h,kv", [(32, 8), (8, 1), (4, 4)])
+@pytest.mark.parametrize("n_seq", [2, 16, 33, 64, 100])
+@pytest.mark.parametrize("prefix", [0, 40])
+def test_starts_that_go_up_and_down(n_seq, h, kv, prefix):
+    """Every second sequence would have all rows: only the first has them, and its outputs are as they should be."""
+    rows = 256
+    case = Case([rows] + [0] * (n_seq - 1), [40 + 3 * b for b in range(n_seq)], h, kv, 64, prefix, 16, torch.float16)
+    want = case.check()
+    starts = i32(([0, rows] * (n_seq // 2 + 1))[:n_seq] + [rows])
+    out, counted = guarded(case, starts)
+    nodes, bad = sequences(case, starts, rows)
+    assert nodes.tolist() == [rows] + [0] * (n_seq - 1) and torch.equal(out, want) and counted == int(bad.sum())
+
+
+def test_one_start_below_the_one_before():
+    counts, ctx = [5, 6, 7, 8], [30, 300, 50, 200]
+    for seen_to in (3, 4, 0, -7):
+        case = Case(counts, ctx, 8, 2, 64, 33, 16, torch.bfloat16, stale=False)
+        want = case.check()
+        starts = case.start.clone()
+        starts[1] = 5
+        starts[2] = seen_to                                     # ends the second before it starts
+        out, counted = guarded(case, starts)
+        # the second has no tokens, the third has the second's too: more than a tree may have
+        assert counted == 2
+        assert torch.equal(out[:5], want[:5]) and torch.equal(out[18:], want[18:])
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_starts_of_any_kind(seed):
+    g = torch.Generator().manual_seed(seed)
+    n_seq, rows = (3, 31, 32, 33, 64, 65)[seed % 6], 300
+    ctx = torch.randint(0, 400, (n_seq,), generator=g).tolist()
+    case = Case([rows // n_seq] * n_seq, ctx, 16, 4, 64, 70 * (seed % 2), 16, torch.float16, stale=False, extra=rows - rows // n_seq * n_seq, max_nodes=(256, 40)[seed % 2])
+    starts = torch.randint(-50, rows + 100, (n_seq + 1,), generator=g)
+    if seed % 3 == 0:
+        starts[:] = torch.tensor([0, 256] * n_seq)[:n_seq + 1]
+    if seed % 3 == 1:
+        starts = starts.sort(descending=True).values
+    case.own_len += torch.randint(0, 200, (n_seq,), generator=g).cuda().int() * (seed % 2)
+    case.table.clamp_(min=0)
+    _, bad = sequences(case, starts, case.max_nodes)
+    _, counted = guarded(case, starts.int().cuda())
+    assert counted == int(bad.sum())
