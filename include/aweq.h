@@ -605,7 +605,8 @@ aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_ca
  * start[n_seq] on stay as they were.  start: device int[n_seq + 1], ascending from 0; mask: device [max_tokens x words] 64-bit words,
  * words >= ceil(max_nodes / 64).  max_nodes (to 256), max_own: HOST bounds on a sequence's nodes and own keys.
  * Lengths and starts out of range are clamped (a start below one before it counts as that one, so that no token has two
- * sequences), nodes beyond max_nodes are not computed, a page outside the pool is replaced by page 0; st->out_of_range counts each sequence with such a length or start, and each such entry of prefix_pages and page_table that holds
+ * sequences), nodes beyond max_nodes are not computed (the last keys are still those of all nodes, and a key beyond max_own or the table is
+ * no node's and nobody's), a page outside the pool is replaced by page 0; st->out_of_range counts each sequence with such a length or start, and each such entry of prefix_pages and page_table that holds
  * keys, once.  max_tokens * n_heads at most 2^31 - 1.
  * ws: aweq_tree_attention_workspace_bytes(...) bytes, 256-byte aligned. */
 size_t aweq_tree_attention_workspace_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq,

@@ -778,11 +778,11 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, int parts, const unsigned c
     if (node < 0 || node >= s.nodes) return;                    // (more nodes than there may be: counted, not computed)
     // the nodes that this one sees; a thread per bit, a warp per half word (a length below the number of nodes: the first have no key)
     const int key = s.base + tid;
-    const bool sees = (bits >> (tid & 63) & 1) && tid < s.nodes && key >= 0;
+    const bool placed = tid < s.placed && key >= 0, sees = (bits >> (tid & 63) & 1) && placed;
     const uint32_t seen = __ballot_sync(0xffffffffu, sees);
     if (lane == 0) counts[warp] = __popc(seen);
     long long at = 0;
-    if (sees || (tid == node && key >= 0)) {
+    if (sees || (tid == node && placed)) {
         const unsigned pg = (unsigned)key / (unsigned)a.page_size, row = (unsigned)key - pg * (unsigned)a.page_size;
         int page = a.page_table[(long long)b * a.ld_table + pg];
         const bool bad = page < 0 || page >= a.n_pages;

@@ -17,7 +17,7 @@ struct TreePlan {
     // scratch: the totals, per sequence its first own unit and item (TreeFirst[n_seq]), every token's sequence; records
     size_t off_seq, off_pre_o, off_pre_ml, off_own_o, off_own_ml, total;
 };
-struct alignas(16) TreeFirst { long long unit; int item, tiles, t0, nodes, base, n_rt; };
+struct alignas(16) TreeFirst { long long unit; int item, tiles, t0; short nodes, placed; int base, n_rt; };
 // How the units are dealt: evenly, an item counting `change` units more than it has, ahead of its own (the record that a CTA writes when
 // it leaves an item takes as long as two or three units: 16 trees of 24 nodes after 512 + 2100 keys 56 us without, 50 with two; one and
 // three are within 2 % of two over seven shapes, but for 128 short items, where one would be 4 % faster).
@@ -26,7 +26,8 @@ struct alignas(16) TreeTotals { long long pre, own, each, more; int tokens, pre_
 constexpr int kTrChange = 2, kTrChangeFrom = 4;     // with as many units to a CTA or more
 
 // A sequence's new tokens and the keys before them, clamped.
-struct TreeSeq { int t0, t1, nodes, ctx, base; bool bad; };  // base: key of node 0
+// base: key of node 0 (below zero: the first nodes have none); placed: the nodes before the first one behind the last key; ctx: keys before them
+struct TreeSeq { int t0, t1, nodes, placed, ctx, base; bool bad; };
 // Of 32 sequences, a lane each (b: the lane's).  A start below one before it counts as that one, so that no token belongs to two
 // sequences and the rows of all are no more than the tokens', which the scratch is made for.  top: where the sequences before these end.
 __device__ __forceinline__ TreeSeq tree_load(const TreeArgs &a, int b, int top)
@@ -45,10 +46,13 @@ __device__ __forceinline__ TreeSeq tree_load(const TreeArgs &a, int b, int top)
     }
     const int l = min(max(len, 0), cap);
     s.nodes = min(s.t1 - s.t0, a.max_nodes);
-    s.base = l - s.nodes;
+    // the last keys are those of all the sequence's tokens, also where some are not computed or some keys are beyond what there may be
+    const int base = max(len, 0) - (s.t1 - s.t0);
+    s.base = min(max(base, -64 * kPlanMaxWords), l);
+    s.placed = min(s.nodes, l - s.base);
     s.ctx = max(s.base, 0);
-    s.bad = s.t0 != s0 || s.t1 != s1 || s.nodes != s.t1 - s.t0 || l != len || l < s.nodes;
-    return in ? s : TreeSeq{0, 0, 0, 0, 0, false};
+    s.bad = s.t0 != s0 || s.t1 != s1 || s.nodes != s.t1 - s.t0 || l != len || base < 0;
+    return in ? s : TreeSeq{0, 0, 0, 0, 0, 0, false};
 }
 // Where the 32 sequences from b0 on end.
 __device__ __forceinline__ int tree_end(const TreeArgs &a, const TreeSeq &s, int b0, int top)
@@ -132,7 +136,8 @@ __device__ __forceinline__ void tree_leave(const TreeArgs &a, const TreePlan &p,
         const TreeScan c = tree_scan(a, p, s).counted(change);
         const bool mine = b0 + lane < a.n_seq && (unsigned)(b0 + lane) % (unsigned)p.ctas == (unsigned)cta;
         if (mine) {
-            first[b0 + lane] = {units + c.unit0, items + c.item0, tree_tiles(s.ctx, p.unit), s.t0, s.nodes, s.base, tree_tiles(s.nodes * p.group, p.rows)};
+            first[b0 + lane] = {units + c.unit0, items + c.item0, tree_tiles(s.ctx, p.unit), s.t0, (short)s.nodes, (short)s.placed, s.base,
+                               tree_tiles(s.nodes * p.group, p.rows)};
             if (s.bad && a.st) atomicAdd(&a.st->out_of_range, 1ull);
         }
         for (uint32_t left = __ballot_sync(0xffffffffu, mine); left; left &= left - 1) {

@@ -5,7 +5,7 @@ import torch
 
 from paper_2311_01305_b200 import aweq
 
-from .test_gpu_tree import Case, i32
+from .test_gpu_tree import TINY, U16, Case, i32, words
 
 pytestmark = pytest.mark.gpu
 
@@ -77,3 +77,47 @@ def test_starts_of_any_kind(seed):
     _, bad = sequences(case, starts, case.max_nodes)
     _, counted = guarded(case, starts.int().cuda())
     assert counted == int(bad.sum())
+
+
+def close(case, out, rows):
+    """Rows of an output against the definition, with the tolerance of the tests of well-formed calls."""
+    want, mag, reach = (x[rows] for x in case.reference())
+    d, keys = case.q.shape[2], case.prefix + max(case.ctx) + max(case.counts)
+    off = (reach * d * 2.0 ** -23 + 2.0 ** -20 + (keys / 16 + 64) * 2.0 ** -23)[..., None]
+    u = U16[case.dtype]
+    return bool(((out[rows].double() - want).abs() <= u * 1.001 * want.abs() + (u + 2 * off) * 1.01 * mag + TINY[case.dtype]).all())
+
+
+@pytest.mark.parametrize("counts,most", [([9, 4, 12], 4), ([70, 3, 64], 64), ([200, 256, 130], 128), ([300, 2], 256), ([3000], 256)])
+def test_the_first_nodes_of_trees_that_are_too_large(counts, most):
+    """What they see is the keys before the tree and the nodes above them, which lie where the whole tree's keys begin."""
+    g = torch.Generator().manual_seed(1)
+    seen = torch.rand((sum(counts), max(256, *counts)), generator=g) < 0.1
+    seen[:, most:] = False                                      # (what lies behind is beyond the mask's words)
+    case = Case(counts, [100, 37, 0][:len(counts)], 8, 2, 64, 20, 16, torch.float16, stale=False, seen=seen.cuda(), max_nodes=max(counts))
+    case.mask, case.max_nodes = words(case.seen[:, :256], 4), most
+    out = torch.full_like(case.q, 9.0)
+    st = aweq.new_status()
+    case.attend()(case.q, case.table, case.own_len, case.start, case.mask, out, st=st)
+    t = 0
+    for n in counts:
+        assert close(case, out, slice(t, t + min(n, most))) and (out[t + most:t + n] == 9).all()
+        t += n
+    assert aweq.read_out_of_range(st) == sum(n > most for n in counts)
+
+
+@pytest.mark.parametrize("max_own", [0, 30, 41, 45, 60])
+def test_keys_beyond_what_there_may_be(max_own):
+    """Keys are what they are by their number: those from max_own on are nobody's, the others keep their part."""
+    counts, ctx = [5, 6, 7], [40, 36, 20]
+    case = Case(counts, ctx, 8, 2, 64, 33, 16, torch.float16, stale=False)
+    st = aweq.new_status()
+    out = case.attend(max_own)(case.q, case.table, case.own_len, case.start, case.mask, st=st)
+    assert aweq.read_out_of_range(st) == sum(c + n > max_own for c, n in zip(ctx, counts))
+    t = 0
+    for b, n in enumerate(counts):
+        case.seen[t:t + n, max(0, max_own - ctx[b]):] = False
+        t += n
+    case.ctx = [min(c, max_own) for c in ctx]
+    # (the definition takes the nodes' keys from behind the context: where that is cut no node has a key)
+    assert close(case, out, slice(0, t))
