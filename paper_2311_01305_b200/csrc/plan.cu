@@ -365,7 +365,10 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_fill_kernel(const KvPlan
     plan_fill(a, {head->taken, head->given, false}, seqs, head->tokens, parents);
 }
 
-size_t kv_plan_ws_bytes(long long n_seq) { return n_seq <= kPlanShared ? 256 : 256 + (size_t)n_seq * sizeof(PlanSeq); }
+// Scratch: the ticket, zero between calls; behind it, for more sequences than one launch serves, the head and the sequences.  (A word of its
+// own, so that calls of both kinds may take turns.)
+constexpr size_t kPlanHeadAt = 64, kPlanSeqsAt = 256;
+size_t kv_plan_ws_bytes(long long n_seq) { return n_seq <= kPlanShared ? kPlanSeqsAt : kPlanSeqsAt + (size_t)n_seq * sizeof(PlanSeq); }
 
 aweq_status run_kv_plan(const KvPlanArgs &a, void *ws, cudaStream_t stream)
 {
@@ -381,8 +384,8 @@ aweq_status run_kv_plan(const KvPlanArgs &a, void *ws, cudaStream_t stream)
         AWEQ_LAUNCH(kv_plan_kernel, dim3((unsigned)ctas), dim3(kPlanThreads), 0, stream, a, reinterpret_cast<unsigned *>(w));
         return AWEQ_OK;
     }
-    PlanHead *const head = reinterpret_cast<PlanHead *>(w);
-    PlanSeq *const seqs = reinterpret_cast<PlanSeq *>(w + 256);
+    PlanHead *const head = reinterpret_cast<PlanHead *>(w + kPlanHeadAt);
+    PlanSeq *const seqs = reinterpret_cast<PlanSeq *>(w + kPlanSeqsAt);
     AWEQ_LAUNCH(kv_plan_sequences_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, head, seqs);
     AWEQ_LAUNCH(kv_plan_fill_kernel, dim3((unsigned)ctas), dim3(kPlanThreads), 0, stream, a, (const PlanHead *)head, (const PlanSeq *)seqs);
     return AWEQ_OK;
