@@ -548,7 +548,8 @@ aweq_status aweq_kv_append_slots(const aweq_kv_cache *cache, const long long *sl
  * pages put back go to the other (this call takes none of those that it puts back).  n_pages at most 2^22.
  * Where something does not fit, it is counted in st->out_of_range, once for each sequence: a length or change beyond 0 ..
  * pages_per_seq * page_size or the max_tokens rows is clamped, a sequence that finds no free pages keeps own_len within what it
- * has, and its tokens without a page get slot -1, pages put back beyond n_pages are lost.  Also counted: each page number outside
+ * has, and its tokens without a page get slot -1 (start still counts them, and own_len no longer says where the sequence's tokens begin:
+ * attention of such trees is aweq_tree_attention_planned's, and what is given up next goes by own_len), pages put back beyond n_pages are lost.  Also counted: each page number outside
  * 0 .. n_pages in the ring that is taken, each parent that is none of the nodes before (the node then has none), each node
  * beyond 64 * words (mask 0, depth 0), and a state that cannot be, which is taken as an empty ring.
  * own_len must not be held or change.  seq, pos, slot, mask and ws 16-byte aligned (not read for max_tokens = 0).
@@ -594,7 +595,7 @@ aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_ca
 
 /* Attention of drafted trees over the prefix the sequences share, each sequence's own keys and the trees themselves.  Sequence b
  * brings the tokens (nodes) t = start[b] .. start[b+1] - 1; own_len[b] own keys lie where row b of page_table says, the last of
- * which are the nodes' (appended before this call), as aweq_kv_plan and aweq_kv_append_slots leave them.
+ * which are the nodes' (appended before this call), as aweq_kv_plan and aweq_kv_append_slots leave them where all tokens found a page.
  *   out[t, h] = sum_j p_j v_j,  p = softmax_j(scale q . k_j)
  * over all prefix keys, all own keys before the nodes', and the key of the sequence's node j where bit j % 64 of
  * mask[t, j / 64] is set (its own only if its bit is); head h reads key head h / (n_heads / n_kv_heads).  A key or value that a token does not
@@ -616,6 +617,16 @@ aweq_status aweq_tree_attention(const void *q, long long ldq, const aweq_kv_cach
                                 const int *own_len, const int *start, const long long *mask, int words, long long max_own,
                                 long long n_seq, long long max_tokens, int max_nodes, int n_heads, float scale, void *out,
                                 long long ldo, void *ws, size_t ws_bytes, aweq_dev_status *st, void *stream);
+/* The same on a step as aweq_kv_plan left it, also where it found no pages for all: pos are its positions, first as it was given there,
+ * and node i of sequence b has the key pos[start[b]] - first + i (what the sequence held, and i) wherever own_len[b] ends.  Nodes from
+ * own_len[b] on have no key, so nobody sees them; their own rows get what they see of the others.  Such a sequence is counted in
+ * st->out_of_range here as well. */
+aweq_status aweq_tree_attention_planned(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages,
+                                        long long prefix_len, const int *page_table, long long pages_per_seq, long long ld_table,
+                                        const int *own_len, const int *start, const int *pos, long long first,
+                                        const long long *mask, int words, long long max_own, long long n_seq, long long max_tokens,
+                                        int max_nodes, int n_heads, float scale, void *out, long long ldo, void *ws, size_t ws_bytes,
+                                        aweq_dev_status *st, void *stream);
 
 #ifdef __cplusplus
 }

@@ -147,6 +147,9 @@ _lib.aweq_tree_attention_workspace_bytes.restype = _sz
 _lib.aweq_tree_attention.argtypes = [_vp, _ll, ctypes.POINTER(KvCacheArgs), _vp, _ll, _vp, _ll, _ll, _vp, _vp, _vp, _i, _ll, _ll, _ll, _i,
                                      _i, ctypes.c_float, _vp, _ll, _vp, _sz, _vp, _vp]
 _lib.aweq_tree_attention.restype = _i
+_lib.aweq_tree_attention_planned.argtypes = [_vp, _ll, ctypes.POINTER(KvCacheArgs), _vp, _ll, _vp, _ll, _ll, _vp, _vp, _vp, _ll, _vp, _i, _ll, _ll,
+                                             _ll, _i, _i, ctypes.c_float, _vp, _ll, _vp, _sz, _vp, _vp]
+_lib.aweq_tree_attention_planned.restype = _i
 for _f in ("aweq_stats", "aweq_wrange", "aweq_factors", "aweq_equalize_quantize", "aweq_bias_correct",
            "aweq_quant_act", "aweq_layer_pass", "aweq_forward_check"):
     getattr(_lib, _f).restype = _i
@@ -801,7 +804,8 @@ def aweq_kv_plan(page_table, page_size, ring, state, held, change, own_len, star
 
 class StepPlan:
     """What ``PagePool.plan`` writes for ``n_seq`` sequences and up to ``max_tokens`` new tokens: ``own_len``, ``start``, ``seq``,
-    ``pos``, ``slot`` and, for drafted trees of up to ``max_nodes`` nodes a sequence, ``mask``.  Serves one stream at a time."""
+    ``pos``, ``slot`` and, for drafted trees of up to ``max_nodes`` nodes a sequence, ``mask``; ``first``: as it was given.  Serves one
+    stream at a time."""
 
     def __init__(self, n_seq, max_tokens, max_nodes=0, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)
@@ -813,6 +817,7 @@ class StepPlan:
         self.ws = workspace(aweq_kv_plan_workspace_bytes(n_seq), device).zero_()
         self._out = (self.own_len.data_ptr(), self.start.data_ptr(), *((t.data_ptr() for t in (self.seq, self.pos, self.slot)) if max_tokens else (None,) * 3))
         self._ws = (self.ws.data_ptr(), self.ws.numel())
+        self.first = None                      # of the plan it has
 
 
 class PagePool:
@@ -844,6 +849,7 @@ class PagePool:
                                _stream())
         if rc:
             raise AweqError(rc)
+        into.first = first
         return into
 
 
@@ -926,6 +932,14 @@ def aweq_tree_attention(q, cache, prefix_pages, prefix_len, page_table, own_len,
                                q.shape[1] if q.dim() == 3 else q.shape[1] // cache.head_dim, max_own, scale, ws, st)
 
 
+def aweq_tree_attention_planned(q, cache, prefix_pages, prefix_len, page_table, own_len, start, pos, first, mask, max_own, max_nodes, scale, out, ws,
+                                st=None):
+    """``aweq_tree_attention`` on a plan that may have found too few pages: node 0 of a sequence has the key of its position less
+    ``first`` (argument marshalling only; see ``include/aweq.h``)."""
+    return TreeAttention._call(q, page_table, own_len, start, mask, out, cache, prefix_pages, prefix_len, own_len.numel(), q.shape[0], max_nodes,
+                               q.shape[1] if q.dim() == 3 else q.shape[1] // cache.head_dim, max_own, scale, ws, st, pos, first)
+
+
 class TreeAttention:
     """``aweq_tree_attention`` for one batch shape: up to ``max_nodes`` tokens of each of ``n_seq`` sequences, ``max_tokens`` rows in
     all.  Holds the prefix's page list and the scratch; one object serves one stream at a time (its calls share the scratch)."""
@@ -941,7 +955,8 @@ class TreeAttention:
                             cache.k.device)
 
     @staticmethod
-    def _call(q, page_table, own_len, start, mask, out, cache, prefix_pages, prefix_len, n_seq, n, max_nodes, h, max_own, scale, ws, st):
+    def _call(q, page_table, own_len, start, mask, out, cache, prefix_pages, prefix_len, n_seq, n, max_nodes, h, max_own, scale, ws, st, pos=None,
+              first=0):
         ldq, ldo = _heads(q, n, h, cache.head_dim, cache.dtype, "q"), _heads(out, n, h, cache.head_dim, cache.dtype, "out")
         pages, rows, per_seq, ld_table = _int32_table(page_table, "page_table")
         if rows != n_seq:
@@ -950,17 +965,22 @@ class TreeAttention:
             raise ValueError("mask must be a contiguous int64 device matrix with a row for each of %d tokens" % n)
         if prefix_len:
             _want(prefix_pages, torch.int32, -(-prefix_len // cache.page_size), "prefix_pages")
-        rc = _lib.aweq_tree_attention(q.data_ptr(), ldq, cache.ref, _ptr(prefix_pages) if prefix_len else None, prefix_len, pages, per_seq, ld_table,
-                                      _int32_rows(own_len, n_seq, "own_len"), _int32_rows(start, n_seq + 1, "start"), mask.data_ptr(),
-                                      mask.shape[1], max_own, n_seq, n, max_nodes, h, scale, out.data_ptr(), ldo, ws.data_ptr(), ws.numel(),
-                                      _ptr(st), _stream())
+        keys = (q.data_ptr(), ldq, cache.ref, _ptr(prefix_pages) if prefix_len else None, prefix_len, pages, per_seq, ld_table,
+                _int32_rows(own_len, n_seq, "own_len"), _int32_rows(start, n_seq + 1, "start"))
+        rest = (mask.data_ptr(), mask.shape[1], max_own, n_seq, n, max_nodes, h, scale, out.data_ptr(), ldo, ws.data_ptr(), ws.numel(), _ptr(st),
+                _stream())
+        if pos is None:
+            rc = _lib.aweq_tree_attention(*keys, *rest)
+        else:
+            rc = _lib.aweq_tree_attention_planned(*keys, _int32_rows(pos, n, "pos"), first, *rest)
         if rc:
             raise AweqError(rc)
         return out
 
-    def __call__(self, q, page_table, own_len, start, mask, out=None, st=None):
+    def __call__(self, q, page_table, own_len, start, mask, out=None, st=None, pos=None, first=0):
         """``q``, ``out``: [max_tokens, n_heads, head_dim]; ``start``: the sequences' first rows and the number of all; ``mask``: a
-        row of 64-bit words for every token, bit j for its sequence's node j."""
+        row of 64-bit words for every token, bit j for its sequence's node j.  ``pos``, ``first``: the positions of the ``StepPlan`` and
+        what it was filled with; without them all tokens have to have found a page."""
         out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         return self._call(q, page_table, own_len, start, mask, out, self.cache, self.prefix_pages, self.prefix_len, self.n_seq, self.max_tokens,
-                          self.max_nodes, self.n_heads, self.max_own, self.scale, self.ws, st)
+                          self.max_nodes, self.n_heads, self.max_own, self.scale, self.ws, st, pos, first)

@@ -829,11 +829,11 @@ size_t aweq_tree_attention_workspace_bytes(const aweq_kv_cache *cache, long long
     return tree_attention_ws_bytes(cache, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads);
 }
 
-aweq_status aweq_tree_attention(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages, long long prefix_len,
-                                const int *page_table, long long pages_per_seq, long long ld_table, const int *own_len, const int *start,
-                                const long long *mask, int words, long long max_own, long long n_seq, long long max_tokens, int max_nodes,
-                                int n_heads, float scale, void *out, long long ldo, void *ws, size_t ws_bytes, aweq_dev_status *st,
-                                void *stream)
+static aweq_status tree_attention(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages, long long prefix_len,
+                                  const int *page_table, long long pages_per_seq, long long ld_table, const int *own_len, const int *start,
+                                  const int *pos, long long first, const long long *mask, int words, long long max_own, long long n_seq,
+                                  long long max_tokens, int max_nodes, int n_heads, float scale, void *out, long long ldo, void *ws,
+                                  size_t ws_bytes, aweq_dev_status *st, void *stream)
 {
     aweq_status rc = check_tree(cache, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads);
     if (rc != AWEQ_OK) return rc;
@@ -842,7 +842,7 @@ aweq_status aweq_tree_attention(const void *q, long long ldq, const aweq_kv_cach
     if (!q || !out || !own_len || !start || !mask || !page_table || (prefix_len && !prefix_pages)) return AWEQ_ERR_NULL;
     const long long row = (long long)n_heads * cache->head_dim;
     if (!aligned(q, 16) || !aligned(out, 16) || ldq < row || ldo < row || ldq % 8 || ldo % 8 || ld_table < pages_per_seq ||
-        !aligned(prefix_pages, 4) || !aligned(page_table, 4) || !aligned(own_len, 4) || !aligned(start, 4) || !aligned(mask, 8))
+        !aligned(prefix_pages, 4) || !aligned(page_table, 4) || !aligned(own_len, 4) || !aligned(start, 4) || !aligned(pos, 4) || !aligned(mask, 8))
         return AWEQ_ERR_ALIGN;
     rc = check_ws(ws, ws_bytes, tree_attention_ws_bytes(cache, prefix_len, max_own, n_seq, max_tokens, max_nodes, n_heads));
     if (rc != AWEQ_OK) return rc;
@@ -855,9 +855,31 @@ aweq_status aweq_tree_attention(const void *q, long long ldq, const aweq_kv_cach
     a.token_stride = cache->token_stride; a.head_stride = cache->head_stride; a.page_size = cache->page_size;
     a.n_kv = cache->n_kv_heads; a.head_dim = cache->head_dim; a.n_heads = n_heads; a.words = words; a.max_nodes = max_nodes;
     a.max_tokens = (int)max_tokens; a.n_seq = (int)n_seq; a.prefix_pages = prefix_pages; a.page_table = page_table;
-    a.own_len = own_len; a.start = start; a.mask = mask; a.prefix_len = prefix_len; a.pages_per_seq = pages_per_seq;
+    a.own_len = own_len; a.start = start; a.pos = pos; a.first = first; a.mask = mask; a.prefix_len = prefix_len; a.pages_per_seq = pages_per_seq;
     a.ld_table = ld_table; a.max_own = max_own; a.scale = scale; a.st = st;
     return run_tree_attention(a, cache, ws, (cudaStream_t)stream);
+}
+
+aweq_status aweq_tree_attention(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages, long long prefix_len,
+                                const int *page_table, long long pages_per_seq, long long ld_table, const int *own_len, const int *start,
+                                const long long *mask, int words, long long max_own, long long n_seq, long long max_tokens, int max_nodes,
+                                int n_heads, float scale, void *out, long long ldo, void *ws, size_t ws_bytes, aweq_dev_status *st,
+                                void *stream)
+{
+    return tree_attention(q, ldq, cache, prefix_pages, prefix_len, page_table, pages_per_seq, ld_table, own_len, start, nullptr, 0, mask, words,
+                          max_own, n_seq, max_tokens, max_nodes, n_heads, scale, out, ldo, ws, ws_bytes, st, stream);
+}
+
+aweq_status aweq_tree_attention_planned(const void *q, long long ldq, const aweq_kv_cache *cache, const int *prefix_pages, long long prefix_len,
+                                        const int *page_table, long long pages_per_seq, long long ld_table, const int *own_len,
+                                        const int *start, const int *pos, long long first, const long long *mask, int words, long long max_own,
+                                        long long n_seq, long long max_tokens, int max_nodes, int n_heads, float scale, void *out,
+                                        long long ldo, void *ws, size_t ws_bytes, aweq_dev_status *st, void *stream)
+{
+    if (first < 0 || first > 0x7fffffffll) return AWEQ_ERR_SHAPE;
+    if (!pos && max_tokens > 0) return AWEQ_ERR_NULL;
+    return tree_attention(q, ldq, cache, prefix_pages, prefix_len, page_table, pages_per_seq, ld_table, own_len, start, pos, first, mask, words,
+                          max_own, n_seq, max_tokens, max_nodes, n_heads, scale, out, ldo, ws, ws_bytes, st, stream);
 }
 
 }  // extern "C"

@@ -157,9 +157,9 @@ struct TreeArgs {
     uint16_t *out;
     long long ldq, ldo, n_pages, page_stride, token_stride, head_stride;
     int page_size, n_kv, head_dim, n_heads, words, max_nodes, max_tokens, n_seq;
-    const int *prefix_pages, *page_table, *own_len, *start;
+    const int *prefix_pages, *page_table, *own_len, *start, *pos;       // pos: NULL, or node 0's key is pos[start] - first
     const long long *mask;
-    long long prefix_len, pages_per_seq, ld_table, max_own;
+    long long first, prefix_len, pages_per_seq, ld_table, max_own;
     float scale;
     aweq_dev_status *st;
 };

@@ -46,12 +46,14 @@ __device__ __forceinline__ TreeSeq tree_load(const TreeArgs &a, int b, int top)
     }
     const int l = min(max(len, 0), cap);
     s.nodes = min(s.t1 - s.t0, a.max_nodes);
-    // the last keys are those of all the sequence's tokens, also where some are not computed or some keys are beyond what there may be
-    const int base = max(len, 0) - (s.t1 - s.t0);
-    s.base = min(max(base, -64 * kPlanMaxWords), l);
+    // the last keys are those of all the sequence's tokens, also where some are not computed or some keys are beyond what there may be;
+    // or the tokens' positions say where theirs begin (a length short of them then leaves the last without a key)
+    const int tokens = s.t1 - s.t0;
+    const long long base = a.pos ? (in && tokens ? a.pos[s.t0] - a.first : l) : (long long)max(len, 0) - tokens;
+    s.base = (int)min(max(base, -64ll * kPlanMaxWords), (long long)l);
     s.placed = min(s.nodes, l - s.base);
     s.ctx = max(s.base, 0);
-    s.bad = s.t0 != s0 || s.t1 != s1 || s.nodes != s.t1 - s.t0 || l != len || base < 0;
+    s.bad = s.t0 != s0 || s.t1 != s1 || s.nodes != s.t1 - s.t0 || l != len || base < 0 || (tokens && base + tokens > l);
     return in ? s : TreeSeq{0, 0, 0, 0, 0, 0, false};
 }
 // Where the 32 sequences from b0 on end.

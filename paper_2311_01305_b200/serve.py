@@ -125,8 +125,9 @@ class AttentionBlock:
     def verify(self, x: torch.Tensor, attend: aweq.TreeAttention, page_table: torch.Tensor, plan: aweq.StepPlan,
                st: Optional[torch.Tensor] = None) -> torch.Tensor:
         """``x`` [max_tokens, C_in], the block's input of the nodes in the order of ``plan``, which ``PagePool.plan`` has filled with
-        the trees and with ``first`` = the prefix's length; the rows behind the last node are padding, their outputs anything.  A path of
-        nodes is then kept with ``aweq.aweq_kv_accept``, and the rest given back with a plan whose changes are below zero."""
+        the trees and with ``first`` = the prefix's length; the rows behind the last node are padding, their outputs anything, as are those of
+        nodes that found no page (slot below zero; counted in ``st``).  A path of nodes is then kept with ``aweq.aweq_kv_accept``, and the
+        rest given back with a plan whose changes are below zero (what is held less what is kept: ``plan.own_len`` says what is held)."""
         if (not isinstance(attend, aweq.TreeAttention) or attend.cache is not self.cache or plan.mask is None or plan.n_seq != attend.n_seq
                 or plan.max_tokens != attend.max_tokens or x.dim() != 2 or x.shape != (plan.max_tokens, self.qkv.C_in)):
             raise ValueError("x must be [%d x %d], with a plan of trees and an attention of this block for as many rows and sequences" % (
@@ -135,7 +136,9 @@ class AttentionBlock:
         def step(q, k, v, q_turned, attended):
             aweq.aweq_kv_append_slots(self.cache, plan.slot, k, v, plan.pos, table=self.rope, interleaved=self.interleaved, q=q, q_out=q_turned,
                                       st=st)
-            attend(q_turned, page_table, plan.own_len, plan.start, plan.mask, attended, st=st)
+            # (node 0's key by its position: own_len ends before the last node where the pool ran out)
+            where = {} if plan.first is None else dict(pos=plan.pos, first=plan.first)
+            attend(q_turned, page_table, plan.own_len, plan.start, plan.mask, attended, st=st, **where)
         return self._run(x, step, st)
 
     def _run(self, x: torch.Tensor, step, st: Optional[torch.Tensor]) -> torch.Tensor:

@@ -121,3 +121,39 @@ def test_keys_beyond_what_there_may_be(max_own):
     case.ctx = [min(c, max_own) for c in ctx]
     # (the definition takes the nodes' keys from behind the context: where that is cut no node has a key)
     assert close(case, out, slice(0, t))
+
+
+@pytest.mark.parametrize("counts,ctx,short", [([5, 24, 7], [40, 100, 20], [0, 12, 0]), ([5, 24, 7], [40, 100, 20], [5, 24, 1]), ([70, 3, 128], [0, 0, 300], [69, 3, 20]),
+                                              ([40, 0, 40], [10, 90, 130], [0, 0, 60])])
+def test_own_keys_that_end_before_the_last_node(counts, ctx, short):
+    """With positions the nodes' keys begin where the sequence's held ones end, and those beyond its length are nobody's."""
+    case = Case(counts, ctx, 8, 2, 64, 33, 16, torch.bfloat16, stale=False, extra=3)
+    node = [i for n in counts for i in range(n)]
+    base = [c for c, n in zip(ctx, counts) for _ in range(n)]
+    pos = i32([1000 + b + (i * 7) % (i + 1) for b, i in zip(base, node)] + [-1] * 3)       # (depths: only a first node's is known, zero)
+    attend, st = case.attend(), aweq.new_status()
+    whole = attend(case.q, case.table, case.own_len, case.start, case.mask)
+    total = sum(counts)
+    assert torch.equal(attend(case.q, case.table, case.own_len, case.start, case.mask, st=st, pos=pos, first=1000)[:total], whole[:total])
+    assert aweq.read_out_of_range(st) == 0
+    case.own_len -= i32(short)
+    out = attend(case.q, case.table, case.own_len, case.start, case.mask, st=st, pos=pos, first=1000)
+    assert aweq.read_out_of_range(st) == sum(s > 0 and n > 0 for s, n in zip(short, counts))
+    t = 0
+    for b, n in enumerate(counts):
+        case.seen[t:t + n, max(n - short[b], 0):] = False
+        case.ctx[b] -= max(short[b] - n, 0)
+        t += n
+    assert close(case, out, slice(0, total))
+
+
+@pytest.mark.parametrize("pos0,counted", [(-5, 1), (2 ** 31 - 1, 1), (-2 ** 31, 1), (900, 1), (1000 + 40, 0)])
+def test_positions_out_of_range(pos0, counted):
+    """Counted, and the other sequences' outputs are what they were."""
+    case = Case([5, 6, 7], [30, 40, 20], 8, 2, 64, 33, 16, torch.float16, stale=False)
+    pos = i32([1030] * 5 + [1040] * 6 + [1020] * 7)
+    attend, st = case.attend(), aweq.new_status()
+    want = attend(case.q, case.table, case.own_len, case.start, case.mask)
+    pos[5] = pos0
+    out = attend(case.q, case.table, case.own_len, case.start, case.mask, st=st, pos=pos, first=1000)
+    assert aweq.read_out_of_range(st) == counted and torch.equal(out[:5], want[:5]) and torch.equal(out[11:], want[11:])
