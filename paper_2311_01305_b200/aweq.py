@@ -804,8 +804,8 @@ def aweq_kv_plan(page_table, page_size, ring, state, held, change, own_len, star
 
 class StepPlan:
     """What ``PagePool.plan`` writes for ``n_seq`` sequences and up to ``max_tokens`` new tokens: ``own_len``, ``start``, ``seq``,
-    ``pos``, ``slot`` and, for drafted trees of up to ``max_nodes`` nodes a sequence, ``mask``; ``first``: as it was given.  Serves one
-    stream at a time."""
+    ``pos``, ``slot`` and, for drafted trees of up to ``max_nodes`` nodes a sequence, ``mask``; ``first``: as it was given; ``trees``: whether there
+    were parents, without which ``mask`` stays as it was.  Serves one stream at a time."""
 
     def __init__(self, n_seq, max_tokens, max_nodes=0, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)
@@ -817,7 +817,8 @@ class StepPlan:
         self.ws = workspace(aweq_kv_plan_workspace_bytes(n_seq), device).zero_()
         self._out = (self.own_len.data_ptr(), self.start.data_ptr(), *((t.data_ptr() for t in (self.seq, self.pos, self.slot)) if max_tokens else (None,) * 3))
         self._ws = (self.ws.data_ptr(), self.ws.numel())
-        self.first = None                      # of the plan it has
+        # of the plan it has, once PagePool.plan has filled it: whether the masks belong to it
+        self.first = self.trees = None
 
 
 class PagePool:
@@ -849,7 +850,7 @@ class PagePool:
                                _stream())
         if rc:
             raise AweqError(rc)
-        into.first = first
+        into.first, into.trees = first, up is not None
         return into
 
 

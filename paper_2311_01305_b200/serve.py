@@ -128,9 +128,9 @@ class AttentionBlock:
         the trees and with ``first`` = the prefix's length; the rows behind the last node are padding, their outputs anything, as are those of
         nodes that found no page (slot below zero; counted in ``st``).  A path of nodes is then kept with ``aweq.aweq_kv_accept``, and the
         rest given back with a plan whose changes are below zero (what is held less what is kept: ``plan.own_len`` says what is held)."""
-        if (not isinstance(attend, aweq.TreeAttention) or attend.cache is not self.cache or plan.mask is None or plan.n_seq != attend.n_seq
-                or plan.max_tokens != attend.max_tokens or x.dim() != 2 or x.shape != (plan.max_tokens, self.qkv.C_in)):
-            raise ValueError("x must be [%d x %d], with a plan of trees and an attention of this block for as many rows and sequences" % (
+        if (not isinstance(attend, aweq.TreeAttention) or attend.cache is not self.cache or plan.mask is None or plan.trees is False
+                or plan.n_seq != attend.n_seq or plan.max_tokens != attend.max_tokens or x.dim() != 2 or x.shape != (plan.max_tokens, self.qkv.C_in)):
+            raise ValueError("x must be [%d x %d], with a plan filled with trees and an attention of this block for as many rows and sequences" % (
                 plan.max_tokens, self.qkv.C_in))
 
         def step(q, k, v, q_turned, attended):

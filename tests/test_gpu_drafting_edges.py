@@ -51,3 +51,22 @@ def test_a_pool_that_runs_out(layer, fmt, prefix, pages):  # noqa: F811
         server.pool.plan(server.table, server.grown.own_len, i32(back), server.kept)
         assert server.kept.own_len.tolist() == [k.shape[0] - prefix for k in kept]
     assert short_once and aweq.read_status(server.st)["wait_timeout"] == 0
+
+
+def test_masks_of_another_step_are_refused(layer):  # noqa: F811
+    """A plan that was last filled without parents has the masks of the step before, or none yet; with parents it serves again."""
+    block = make_block(layer, "e8m0", 8)
+    pool, table, held = aweq.PagePool(8, PAGE), i32([[-1] * 2, [-1] * 2]), i32([0, 0])
+    plan, attend = aweq.StepPlan(2, 8, 4), block.drafts(2, 8, 4, max_own=32)
+    x = layer[1][:8].contiguous()
+    for _ in range(2):
+        pool.plan(table, held, i32([3, 2]), plan)
+        before = block.cache.k.clone()
+        with pytest.raises(ValueError):
+            block.verify(x, attend, table, plan)
+        assert torch.equal(block.cache.k, before), "refused, but stored"
+        pool.plan(table, plan.own_len, i32([-3, -2]), aweq.StepPlan(2, 0))
+        pool.plan(table, held, i32([3, 2]), plan, parent=i32([-1, 0, 1, -1, 0, -1, -1, -1]))
+        chain = block.verify(x, attend, table, plan)
+        assert torch.isfinite(chain[:5]).all() and plan.mask[:5, 0].tolist() == [1, 3, 7, 1, 3]
+        pool.plan(table, plan.own_len, i32([-3, -2]), aweq.StepPlan(2, 0))
