@@ -129,7 +129,8 @@ class AttentionBlock:
         nodes that found no page (slot below zero; counted in ``st``).  A path of nodes is then kept with ``aweq.aweq_kv_accept``, and the
         rest given back with a plan whose changes are below zero (what is held less what is kept: ``plan.own_len`` says what is held)."""
         if (not isinstance(attend, aweq.TreeAttention) or attend.cache is not self.cache or plan.mask is None or plan.trees is False
-                or plan.n_seq != attend.n_seq or plan.max_tokens != attend.max_tokens or x.dim() != 2 or x.shape != (plan.max_tokens, self.qkv.C_in)):
+                or plan.n_seq != attend.n_seq or plan.max_tokens != attend.max_tokens or 64 * plan.words < attend.max_nodes
+                or page_table.shape[0] != plan.n_seq or x.dim() != 2 or x.shape != (plan.max_tokens, self.qkv.C_in)):
             raise ValueError("x must be [%d x %d], with a plan filled with trees and an attention of this block for as many rows and sequences" % (
                 plan.max_tokens, self.qkv.C_in))
 

@@ -70,3 +70,15 @@ def test_masks_of_another_step_are_refused(layer):  # noqa: F811
         chain = block.verify(x, attend, table, plan)
         assert torch.isfinite(chain[:5]).all() and plan.mask[:5, 0].tolist() == [1, 3, 7, 1, 3]
         pool.plan(table, plan.own_len, i32([-3, -2]), aweq.StepPlan(2, 0))
+
+
+@pytest.mark.parametrize("wrong", ["masks", "table"])
+def test_what_is_refused_stores_nothing(layer, wrong):  # noqa: F811
+    """Masks too narrow for the attention's trees, a table of other sequences: known before the first launch."""
+    block = make_block(layer, "e8m0", 8)
+    pool, table = aweq.PagePool(8, PAGE), i32([[-1] * 2, [-1] * 2])
+    plan, attend = aweq.StepPlan(2, 8, 4), block.drafts(2, 8, 100 if wrong == "masks" else 4, max_own=32)
+    pool.plan(table, i32([0, 0]), i32([3, 2]), plan, parent=i32([-1, 0, 1, -1, 0, -1, -1, -1]))
+    with pytest.raises(ValueError):
+        block.verify(layer[1][:8].contiguous(), attend, table[:1] if wrong == "table" else table, plan)
+    assert not block.cache.k.any()
