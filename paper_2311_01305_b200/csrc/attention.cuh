@@ -106,10 +106,11 @@ struct AttentionWalk {
     }
     __device__ __forceinline__ bool has(const AttentionPlan &p, int r) const { return at.tile * (OWN ? p.unit : p.pre_unit) + r < at.len; }
     // entry of the page list for the unit's r'th key, if there is such a key; not looked at here, so that the load can fly
+    // (a prefix' page list lies where the launch knows it: a plain load)
     __device__ __forceinline__ int entry(const AttentionArgs &a, const AttentionPlan &p, int r) const
     {
-        const int *pages = OWN ? a.page_table + (long long)at.b * a.ld_table : a.prefix_pages;
-        return has(p, r) ? __ldg(pages + (unsigned)(at.tile * (OWN ? p.unit : p.pre_unit) + r) / (unsigned)a.page_size) : 0;
+        const int *pages = (OWN ? a.page_table + (long long)at.b * a.ld_table : a.prefix_pages) + (unsigned)(at.tile * (OWN ? p.unit : p.pre_unit) + r) / (unsigned)a.page_size;
+        return has(p, r) ? OWN ? __ldg(pages) : *pages : 0;
     }
 };
 

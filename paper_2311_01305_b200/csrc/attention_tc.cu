@@ -100,7 +100,7 @@ attention_tc_kernel(const AttentionArgs a, const AttentionPlan p, const __grid_c
             const int boxes = p.pre_unit / p.box;
             auto has = [&](int tile) { return lane < boxes && (long long)tile * p.pre_unit + lane * p.box < a.prefix_len; };
             auto look_up = [&](int tile) {                                  // entry of the lane's box (not looked at here: the load flies)
-                return has(tile) ? __ldg(a.prefix_pages + (unsigned)(tile * p.pre_unit + lane * p.box) / (unsigned)a.page_size) : 0;
+                return has(tile) ? a.prefix_pages[(unsigned)(tile * p.pre_unit + lane * p.box) / (unsigned)a.page_size] : 0;
             };
             int tile = tile0, kh = item0 / p.pre_rt, rt = item0 % p.pre_rt, page = look_up(tile), s = 0, items = 0;
             uint32_t ph = 0;

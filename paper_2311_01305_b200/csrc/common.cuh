@@ -96,8 +96,9 @@ inline cudaError_t allow_smem(void (*kern)(KArgs...), size_t bytes, std::atomic<
     if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_release);
     return e;
 }
-// (What an earlier launch may have written is not read through __ldg or a const __restrict__ pointer behind a wait that other
-// loads stand before: such loads count as invariant, and nothing keeps them behind it.)
+// (In the calls of a step of serving, which follow one another without a gap, what an earlier launch may have written is not read through
+// an invariant load, __ldg's or a const __restrict__ pointer's, at an address that is known at the launch: nothing keeps such a load behind
+// the wait.  One whose address hangs on a plain load behind the wait stays there too.)
 __device__ __forceinline__ void pdl_begin()
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -176,6 +177,13 @@ __device__ __forceinline__ uint4 ldg_stream(const void *p)   // read-once data: 
     uint4 v;
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+// the same for what the launch before may have written
+__device__ __forceinline__ uint4 ld_stream(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 __device__ __forceinline__ float4 ldg_f4(const float *p) { return __ldg(reinterpret_cast<const float4 *>(p)); }

@@ -4,8 +4,7 @@
 namespace aweq {
 
 // Row sums of the codes, once per layer: one warp per row, a read of the codes.
-__global__ void __launch_bounds__(256) code_sums_kernel(const unsigned char *__restrict__ Q, long long rows, long long cols,
-                                                        long long ld, int *__restrict__ out)
+__global__ void __launch_bounds__(256) code_sums_kernel(const unsigned char *Q, long long rows, long long cols, long long ld, int *out)
 {
     pdl_begin();
     const int lane = threadIdx.x & 31;
@@ -14,7 +13,7 @@ __global__ void __launch_bounds__(256) code_sums_kernel(const unsigned char *__r
     const uint4 *p = reinterpret_cast<const uint4 *>(Q + row * ld);
     uint32_t acc = 0;
     for (long long i = lane; i < cols / 16; i += 32) {
-        const uint4 v = ldg_stream(p + i);
+        const uint4 v = ld_stream(p + i);
         acc = __dp4a(v.x, 0x01010101u, acc);
         acc = __dp4a(v.y, 0x01010101u, acc);
         acc = __dp4a(v.z, 0x01010101u, acc);
@@ -70,10 +69,10 @@ __global__ void __launch_bounds__(256) linear8_stream_kernel(const Linear8Args p
             const int k = (s0 + u * kWarps) * 64;
             const bool in = k + t * 16 < p.K;              // K is a multiple of 16: a quarter is all in or all out
             const uint4 zero = make_uint4(0, 0, 0, 0);
-            a[u] = in ? ldg_stream(wa + k) : zero;
-            b[u] = in ? ldg_stream(wb + k) : zero;
+            a[u] = in ? ld_stream(wa + k) : zero;
+            b[u] = in ? ld_stream(wb + k) : zero;
 #pragma unroll
-            for (int i = 0; i < NT; ++i) x[u][i] = in ? __ldg(reinterpret_cast<const uint4 *>(xt[i] + k)) : zero;
+            for (int i = 0; i < NT; ++i) x[u][i] = in ? *reinterpret_cast<const uint4 *>(xt[i] + k) : zero;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)

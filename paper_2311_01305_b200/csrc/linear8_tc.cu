@@ -33,10 +33,10 @@ __device__ __forceinline__ Linear8Col linear8_col(const Linear8Args &p, long lon
 {
     Linear8Col c = {0.0f, 0.0f, 0, 0u};
     if (o < p.O) {
-        c.step = __ldg(p.w_step + o * p.w_inc);
-        c.zp = __ldg(p.w_zp + o * p.w_inc);
-        c.sum = (uint32_t)__ldg(p.w_sum + o);
-        if (p.bias) c.bias = __ldg(p.bias + o);
+        c.step = p.w_step[o * p.w_inc];
+        c.zp = p.w_zp[o * p.w_inc];
+        c.sum = (uint32_t)p.w_sum[o];
+        if (p.bias) c.bias = p.bias[o];
     }
     return c;
 }
@@ -177,8 +177,8 @@ linear8_big_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap mapX
             float reach = redux_max(linear8_reach(mine.zp), 0xffffffffu);
             if (lane == 0) sh.reach[warp - 4] = reach;
             const bool live = row < p.N;
-            const int zx = live ? __ldg(p.x_zp + row * p.x_inc) : 0;
-            const float sx = live ? __ldg(p.x_step + row * p.x_inc) : 0.0f;
+            const int zx = live ? p.x_zp[row * p.x_inc] : 0;
+            const float sx = live ? p.x_step[row * p.x_inc] : 0.0f;
             named_bar_sync(1, 256);
 #pragma unroll
             for (int i = 0; i < 8; ++i) reach = fmaxf(reach, sh.reach[i]);
@@ -391,8 +391,8 @@ linear8_split_kernel(const Linear8Args p, const __grid_constant__ CUtensorMap ma
         // the pairs of channels and tokens, while the first copies are under way
         for (int i = threadIdx.x - 64; i < bn; i += 192) sh.col[i] = linear8_col(p, o0 + i);
         for (int i = threadIdx.x - 64; i < rows; i += 192) {
-            const int z = __ldg(p.x_zp + (row0 + i) * p.x_inc);
-            sh.row[i] = {__ldg(p.x_step + (row0 + i) * p.x_inc), linear8_reach(z) * (float)p.K, z, 0u};
+            const int z = p.x_zp[(row0 + i) * p.x_inc];
+            sh.row[i] = {p.x_step[(row0 + i) * p.x_inc], linear8_reach(z) * (float)p.K, z, 0u};
         }
         const int groups = min(plan.rx_groups, 6), group = (warp - 2) % groups, set = (warp - 2) / groups;
         if (set < plan.rx_sets) {
