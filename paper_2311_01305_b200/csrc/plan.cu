@@ -83,11 +83,13 @@ __device__ __forceinline__ PlanTotals plan_sequences(const KvPlanArgs &a, long l
             have[i] = plan_pages(held[i], a.page_size);
             after[i] = held[i] + kept - drop[i];
             want[i] = plan_pages(after[i], a.page_size);
-            // (no sequence asks for or has more than the pool: both sums in one, 32 bits each)
-            pages += (long long)min((long long)max(want[i] - have[i], 0), a.n_pages) << 32 | min((long long)max(have[i] - want[i], 0), a.n_pages);
+            // (both sums in one: pages taken are no more than the tokens, 31 bits; a thousand sequences' pages put back, of 2^22 each, 33)
+            pages += (long long)((unsigned long long)min((long long)max(want[i] - have[i], 0), a.n_pages) << 33) + min((long long)max(have[i] - want[i], 0), a.n_pages);
         }
         const PlanSums m = plan_scan(pages, sh);
-        long long take = more_before + (m.before >> 32), give = less_before + (m.before & 0xffffffffll);
+        auto taken_of = [](long long sums) { return (long long)((unsigned long long)sums >> 33); };
+        auto given_of = [](long long sums) { return sums & 0x1ffffffffll; };
+        long long take = more_before + taken_of(m.before), give = less_before + given_of(m.before);
 #pragma unroll
         for (int i = 0; i < M; ++i) {
             const int more = max(want[i] - have[i], 0), less = max(have[i] - want[i], 0);
@@ -111,8 +113,8 @@ __device__ __forceinline__ PlanTotals plan_sequences(const KvPlanArgs &a, long l
             give += min((long long)less, a.n_pages);
         }
         tokens = min(tokens + t.all, a.max_tokens);
-        more_before += m.all >> 32;
-        less_before += m.all & 0xffffffffll;
+        more_before += taken_of(m.all);
+        less_before += given_of(m.all);
     }
     if (lead && threadIdx.x == 0) a.start[a.n_seq] = (int)tokens;
     return {(int)tokens, taken + min(more_before, free), given + min(less_before, a.n_pages - free)};
