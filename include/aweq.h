@@ -545,7 +545,7 @@ aweq_status aweq_kv_append_slots(const aweq_kv_cache *cache, const long long *sl
  * none (drafted trees): then pos[t] = first + held[b] + its depth, and mask[t] (words 64-bit words, node j in bit j % 64 of word
  * j / 64) has the bits of the node itself and of those above it.  At most 64 * words nodes to a sequence; words 1 to 4.
  * ring: int[n_pages], state: {taken, given}: the free pages are ring[i % n_pages], taken <= i < given; taken pages come from the one end,
- * pages put back go to the other (this call takes none of those that it puts back).  n_pages at most 2^22.
+ * pages put back go to the other (this call takes none of those that it puts back).  n_pages at most 2^22, n_seq 2^30.
  * Where something does not fit, it is counted in st->out_of_range, once for each sequence: a length or change beyond 0 ..
  * pages_per_seq * page_size or the max_tokens rows is clamped, a sequence that finds no free pages keeps own_len within what it
  * has, and its tokens without a page get slot -1 (start still counts them, and own_len no longer says where the sequence's tokens begin:

@@ -706,11 +706,11 @@ aweq_status aweq_kv_append_slots(const aweq_kv_cache *cache, const long long *sl
     return run_kv_append(a, cache->dt, (cudaStream_t)stream);
 }
 
-constexpr long long kMostPages = 1ll << 22;
+constexpr long long kMostPages = 1ll << 22, kMostPlanned = 1ll << 30;        // (32-bit loops over the sequences step beyond the last)
 
 size_t aweq_kv_plan_workspace_bytes(long long n_seq)
 {
-    return n_seq < 0 || n_seq > 0x7fffffffll ? 0 : kv_plan_ws_bytes(n_seq);
+    return n_seq < 0 || n_seq > kMostPlanned ? 0 : kv_plan_ws_bytes(n_seq);
 }
 
 aweq_status aweq_kv_plan(int *page_table, long long n_seq, long long pages_per_seq, long long ld_table, int page_size, int *ring,
@@ -718,7 +718,7 @@ aweq_status aweq_kv_plan(int *page_table, long long n_seq, long long pages_per_s
                          long long max_tokens, int *own_len, int *start, int *seq, int *pos, long long *slot, const int *parent,
                          long long *mask, int words, void *ws, size_t ws_bytes, aweq_dev_status *st, void *stream)
 {
-    if (n_seq <= 0 || n_seq > 0x7fffffffll || pages_per_seq <= 0 || pages_per_seq > 0x7fffffffll || page_size <= 0 || page_size > (1 << 20) ||
+    if (n_seq <= 0 || n_seq > kMostPlanned || pages_per_seq <= 0 || pages_per_seq > 0x7fffffffll || page_size <= 0 || page_size > (1 << 20) ||
         n_pages <= 0 || n_pages > kMostPages || max_tokens < 0 || max_tokens > 0x7fffffffll - 2048 || first < 0)
         return AWEQ_ERR_SHAPE;
     if (first + (double)pages_per_seq * page_size > 2147483647.0) return AWEQ_ERR_SHAPE;

@@ -1,9 +1,10 @@
-"""What the attention of drafted trees on a plan refuses: host-side validation, no CUDA call (the addresses are never dereferenced)."""
+"""What the attention of drafted trees on a plan refuses, and a plan beyond what its loops count: host-side validation, no CUDA call (the
+addresses are never dereferenced)."""
 import pytest
 
 from paper_2311_01305_b200 import aweq
 
-from .test_drafting_refusals import ALIGN, CACHES, NULL, OK, P, SHAPE, WORKSPACE, cache
+from .test_drafting_refusals import ALIGN, CACHES, NULL, OK, P, SHAPE, WORKSPACE, cache, plan
 
 
 def planned(c=None, **kw):
@@ -25,3 +26,8 @@ def test_refuses_caches(kw, code):
     (dict(n_seq=0), OK), (dict(rows=0), OK), (dict(rows=0, q=None, out=None, pos=None), OK)])
 def test_refusals(kw, code):
     assert planned(**kw) == code
+
+
+@pytest.mark.parametrize("n_seq,code", [((1 << 30) + 1, SHAPE), ((1 << 31) - 1, SHAPE)])
+def test_a_plan_of_more_sequences_than_its_loops_count(n_seq, code):
+    assert plan(n_seq=n_seq) == code and aweq.aweq_kv_plan_workspace_bytes(n_seq) == 0
