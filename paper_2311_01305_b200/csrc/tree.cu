@@ -293,15 +293,15 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             int s = 0, tile = it.tile, left = it.count, g = 0, told = 0;    // g: the unit, told: tiles of it that are under way
             uint32_t ph = 0, unused;
             auto entry = [&](const TreeItem &x, int t, int r) {     // entry of the page list for the unit's r'th key, if there is such a key
+                if (r >= x.len - t * p.unit) return 0;              // (the sum may be beyond 2^31)
                 const int key = t * p.unit + r;
-                if (key >= x.len) return 0;
                 return (x.own ? a.page_table + (long long)x.b * a.ld_table : a.prefix_pages)[(unsigned)key / (unsigned)a.page_size];
             };
             if (p.box) {
                 const int boxes = p.unit / p.box, at = lane * p.box;
                 int page = ok && left && lane < boxes ? entry(it, tile, at) : 0;
                 while (ok && left > 0) {
-                    const int keys = min(p.unit, it.len - tile * p.unit), kh = it.kh, row = (unsigned)(tile * p.unit + at) % (unsigned)a.page_size;
+                    const int keys = min(p.unit, it.len - tile * p.unit), kh = it.kh, row = ((unsigned)(tile * p.unit) + (unsigned)at) % (unsigned)a.page_size;
                     const bool there = lane < boxes && at < keys, bad = there && (page < 0 || page >= a.n_pages);
                     const int pid = bad ? 0 : page, n = __popc(__ballot_sync(0xffffffffu, there));
                     if (bad && (kh | it.rt | row) == 0 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
@@ -348,7 +348,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     for (int i = 0; i < 4; ++i) {
                         const int r = i * 32 + lane;
                         const int page = entry(it, tile, r);
-                        const unsigned row = (unsigned)(tile * p.unit + r) % (unsigned)a.page_size;
+                        const unsigned row = ((unsigned)(tile * p.unit) + (unsigned)r) % (unsigned)a.page_size;
                         const bool bad = r < keys && (page < 0 || page >= a.n_pages);
                         if (bad && (it.kh | it.rt) == 0 && row == 0 && a.st) atomicAdd(&a.st->out_of_range, 1ull);
                         off[i] = r < keys ? (long long)(bad ? 0 : page) * a.page_stride + (long long)row * a.token_stride + it.kh * a.head_stride : -1;
@@ -777,7 +777,7 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, int parts, const unsigned c
     const int node = tok - s.t0;
     if (node < 0 || node >= s.nodes) return;                    // (more nodes than there may be: counted, not computed)
     // the nodes that this one sees; a thread per bit, a warp per half word (a length below the number of nodes: the first have no key)
-    const int key = s.base + tid;
+    const int key = (int)((unsigned)s.base + (unsigned)tid);     // (looked at below 2^31 only: where the node has a place)
     const bool placed = tid < s.placed && key >= 0, sees = (bits >> (tid & 63) & 1) && placed;
     const uint32_t seen = __ballot_sync(0xffffffffu, sees);
     if (lane == 0) counts[warp] = __popc(seen);

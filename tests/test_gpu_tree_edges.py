@@ -157,3 +157,19 @@ def test_positions_out_of_range(pos0, counted):
     pos[5] = pos0
     out = attend(case.q, case.table, case.own_len, case.start, case.mask, st=st, pos=pos, first=1000)
     assert aweq.read_out_of_range(st) == counted and torch.equal(out[:5], want[:5]) and torch.equal(out[11:], want[11:])
+
+
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("page", [128, 50])
+def test_two_thousand_million_keys(page, own):
+    """Key numbers up to 2^31 - 2, pages over and over.  Queries of zeros and values of one: every sum of a thread block is a whole number of
+    units below 2^24 of them, so exact, and a mean over some hundred parts is off by 2^-16 at most: one."""
+    n = 2 ** 31 - 1
+    k = torch.randn((4, page, 1, 8), device="cuda").half()
+    cache = aweq.KVCache(k, torch.ones_like(k))
+    pages = (torch.arange(-(-n // page), device="cuda") % 4).to(torch.int32)
+    q, mask, st = torch.zeros((1, 1, 8), dtype=torch.float16, device="cuda"), torch.ones((1, 1), dtype=torch.int64, device="cuda"), aweq.new_status()
+    table = pages.view(1, -1) if own else i32([[1]])
+    attend = aweq.TreeAttention(cache, None if own else pages, 0 if own else n, 1, 1, 1, 1)
+    out = attend(q, table, i32([n if own else 1]), i32([0, 1]), mask, st=st)
+    assert (out == 1).all() and not st.any()
