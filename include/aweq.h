@@ -601,7 +601,9 @@ aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_ca
  * mask[t, j / 64] is set (its own only if its bit is); head h reads key head h / (n_heads / n_kv_heads).  A key or value that a token does not
  * see has no part in its output, whatever it is.  A row without keys gives zeros, one whose scores are all minus infinity NaN.
  * Scores, running maximum, sum and output are binary32; the probabilities of prefix and own keys before the nodes' are rounded to the 16-bit
- * type for the product with v, as in aweq_prefix_attention; one rounding at the end.
+ * type for the product with v, as in aweq_prefix_attention; one rounding at the end.  (The tensor cores drop what a product has below
+ * a sum's last bit.  With equal weights 2^17 keys added up by one thread block leave a mean 1.3e-4 too small, 2^18 4.6e-4, 2^20 2.7e-3 in fp16, and 2^20
+ * 1e-3 in bf16; a call's keys lie on up to 148 of them.)
  * q, out: 16-bit [max_tokens x n_heads * head_dim], row pitches ldq, ldo elements, 16-byte aligned, pitches multiples of 8; rows of out from
  * start[n_seq] on stay as they were.  start: device int[n_seq + 1], ascending from 0; mask: device [max_tokens x words] 64-bit words,
  * words >= ceil(max_nodes / 64).  max_nodes (to 256), max_own: HOST bounds on a sequence's nodes and own keys.

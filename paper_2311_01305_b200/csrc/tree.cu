@@ -252,7 +252,8 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             constexpr int kBufs = TWO ? 1 : 2;
             int told = 0, brought = 0;                          // items said, items whose rows of Q are there or under way
             bool all = false;
-            unsigned long long t0 = global_ns();
+            // It moves when an item ends, which is as long away as the longest under way takes (a unit 1.5 us, here 20).
+            unsigned long long t0 = global_ns(), longest = 0;
             while (!all || brought < told) {
                 bool moved = false;
                 const int i = told & (kTrItems - 1), buf = brought % kBufs;
@@ -262,6 +263,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                         mbar_arrive(&sh.item_full[i]);
                     }
                     __syncwarp();
+                    longest = max(longest, (unsigned long long)it.count);
                     ++told;
                     all = it.stop;
                     moved = true;
@@ -278,7 +280,7 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
                     moved = true;
                 }
                 if (moved) t0 = global_ns();
-                else if (global_ns() - t0 > kWaitLimitNs) { ok = false; break; }
+                else if (global_ns() - t0 > kWaitLimitNs + longest * 20000) { ok = false; break; }
                 else __nanosleep(40);
             }
             // (gave up: let what is under way land, bounded, before the memory goes)

@@ -173,3 +173,17 @@ def test_two_thousand_million_keys(page, own):
     attend = aweq.TreeAttention(cache, None if own else pages, 0 if own else n, 1, 1, 1, 1)
     out = attend(q, table, i32([n if own else 1]), i32([0, 1]), mask, st=st)
     assert (out == 1).all() and not st.any()
+
+
+def test_items_that_take_longer_than_a_wait_may():
+    """16 key heads over 2^31 - 1 keys, more than a tile of rows: a thread block that has the end of one item and the start of the next is at the
+    first for seconds, and does not give up.  Nothing is said of the values: with ten million keys and more in a sum it is 2^31, 2^8 to its last bit,
+    where a product is 2^7 (the header says how far sums go)."""
+    n, page, rows = 2 ** 31 - 1, 128, 130
+    k = torch.randn((4, page, 16, 8), device="cuda").half()
+    cache, st = aweq.KVCache(k, torch.ones_like(k)), aweq.new_status()
+    pages = (torch.arange(-(-n // page), device="cuda") % 4).to(torch.int32)
+    attend = aweq.TreeAttention(cache, pages, n, 16, 1, rows, rows)
+    out = attend(torch.zeros((rows, 16, 8), dtype=torch.float16, device="cuda"), i32([[1, 2]]), i32([rows]), i32([0, rows]),
+                 torch.ones((rows, 3), dtype=torch.int64, device="cuda"), st=st)
+    assert not st.any() and torch.isfinite(out).all()
