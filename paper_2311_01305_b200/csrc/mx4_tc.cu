@@ -30,8 +30,8 @@ __device__ __forceinline__ Mx4Col mx4_col(const Mx4LinearArgs &p, long long o)
 // not in order with the products before it: the buffer's last products are waited for (that many stages back, so the pipe stays fed).
 // Warps: 0 copies, 1 issues the products (in the pair's even CTA), 4-11 write the output, two to a quarter of the TMEM lanes.
 // 4099 x 5120 x 13824 in blocks of 32: 110-120 us by itself, 4.8-5.3 PFLOP/s (3.1 to 3.4 of the measured bf16
-// rates; nominal is 4), 130 in a row at the power cap.  A stage of 256 columns takes 880 cycles for 512 of products: the tensor pipe is 65 to 70 % busy, the L2 sends every SM 53
-// bytes a cycle, near its limit; larger tiles do not fit TMEM beside the scales.  Scales' copies by a warp of their own: 127 us.
+// rates; nominal is 4), 130 in a row at the power cap.  A stage of 256 columns takes some 690 cycles for 512 of products: the tensor pipe is 70 % busy, the L2
+// sends every SM some 55 bytes a cycle, near its limit; larger tiles do not fit TMEM beside the scales.  Scales' copies by a warp of their own: 127 us.
 constexpr int kM4BigStages = 5, kM4BigThreads = 384, kM4Overlap = 96, kM4ScaleCols = 96;
 constexpr int kM4SecondAcc = 256 - kM4Overlap, kM4Scales = 512 - kM4ScaleCols;
 constexpr int kM4OutPitch = 80;                // bytes of a staged output row: 32 columns and 16 bytes against bank conflicts
@@ -252,15 +252,15 @@ static aweq_status m4_big_launch(const Mx4LinearArgs &a, cudaStream_t stream)
 }
 
 // ------------------------------------------------------------------ few tokens
-// The layer is bound by the weights here.  The weights are the 128-row operand and the tokens, up to 256, the other: a product costs
+// The layer is bound by the weights here.  The weights are the 128-row operand and the tokens, up to 128, the other: a product costs
 // what the tokens there are ask for, and reads nothing that is not there.  Where few channels leave SMs idle, K is cut over the
-// CTAs of a cluster, whose sums are added through distributed shared memory in the order of the slices.  Two or three CTAs
-// share an SM, so that one's start and end lie under another's copies.  Warps: 0 copies, 1 issues the products; all write the output.
+// CTAs of a cluster, whose sums are added through distributed shared memory in the order of the slices.  A CTA's ring takes as much of an SM
+// as its blocks of K fill: with few of them two or three CTAs share one.  Warps: 0 copies, 1 issues the products; all write the output.
 // 24 x 4096 x 12288 in blocks of 16, weights from memory: 11.3 us, 2.5 TB/s (a copy of as many bytes 4.4 us and a launch's start and end);
 // with the weights in the L2 8.6.  1 x 768 x 768: 5.7 us from memory, 2.9 from the L2: latency.
 constexpr int kM4SplitMaxStages = 8;
 struct M4SplitPlan {
-    int bn, slices, stages;                    // tokens of a tile (a multiple of 16), slices of K, ring
+    int bn, slices, stages;                    // tokens, as a multiple of 16 up to 128, slices of K, ring
     int stage_bytes, scale_cols, cols;         // TMEM: a buffer of scales, all
 };
 struct M4SplitShared {
@@ -280,12 +280,11 @@ mx4_split_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX
     unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     float *part = reinterpret_cast<float *>(stages);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int bn = plan.bn, x_tiles = bn > 128 ? 2 : 1, x_at = 128 * kM4Block, sf_at = x_at + bn * kM4Block;
+    const int bn = plan.bn, x_at = 128 * kM4Block, sf_at = x_at + bn * kM4Block;
     const int slices = plan.slices, slice = blockIdx.x;
     const int nkb = (p.K + 255) / 256;
     const int kb0 = (int)((long long)nkb * slice / slices), kb1 = (int)((long long)nkb * (slice + 1) / slices);
-    const long long row0 = (long long)blockIdx.z * bn;
-    const int rows = (int)min((long long)bn, p.N - row0);
+    const int rows = (int)p.N;
     const int o0 = blockIdx.y * 128;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
@@ -310,12 +309,9 @@ mx4_split_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX
         if (lane == 0) {
             int s = 0;
             uint32_t ph = 0;
-            // tokens' scales: the 128-row blocks that this tile of tokens lies in (bn is 128 or 256 where there are several tiles)
-            const long long per_row = mx4_row_tiles(p.K, FMT);
-            const unsigned char *sw = p.w_scales + ((long long)blockIdx.y * per_row + (long long)kb0 * T) * kMx4Tile;
-            const unsigned char *sx = p.x_scales + ((row0 >> 7) * per_row + (long long)kb0 * T) * kMx4Tile;
-            const bool second = x_tiles == 2 && row0 + 128 < p.N;
-            const uint32_t bytes = 128 * kM4Block + bn * kM4Block + (2 + second) * T * kMx4Tile;
+            const unsigned char *sw = p.w_scales + ((long long)blockIdx.y * mx4_row_tiles(p.K, FMT) + (long long)kb0 * T) * kMx4Tile;
+            const unsigned char *sx = p.x_scales + (long long)kb0 * T * kMx4Tile;
+            const uint32_t bytes = 128 * kM4Block + bn * kM4Block + 2 * T * kMx4Tile;
             for (int kb = kb0; kb < kb1; ++kb, sw += T * kMx4Tile, sx += T * kMx4Tile) {
                 if (!mbar_wait(&sh.empty[s], ph ^ 1)) { ok = false; break; }
                 unsigned char *const st = stages + s * plan.stage_bytes;
@@ -323,9 +319,8 @@ mx4_split_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX
                 mbar_arrive_expect_tx(&sh.full[s], bytes);
                 tma_load2<1>(dst, &mapW, kb * kM4Block, o0, bar);
                 bulk_g2s(st + sf_at, sw, T * kMx4Tile, &sh.full[s]);
-                tma_load2<1>(dst + x_at, &mapX, kb * kM4Block, (int)row0, bar);
+                tma_load2<1>(dst + x_at, &mapX, kb * kM4Block, 0, bar);
                 bulk_g2s(st + sf_at + T * kMx4Tile, sx, T * kMx4Tile, &sh.full[s]);
-                if (second) bulk_g2s(st + sf_at + 2 * T * kMx4Tile, sx + per_row * kMx4Tile, T * kMx4Tile, &sh.full[s]);
                 if (++s == plan.stages) { s = 0; ph ^= 1; }
             }
             if (!ok)                           // gave up: let what is under way land (bounded) before the memory goes
@@ -344,14 +339,13 @@ mx4_split_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX
 #pragma unroll
             for (int i = 0; i < T; ++i) {
                 tc_copy_scales<1>(sf + i * 4, a + sf_at + i * kMx4Tile, lead);
-                tc_copy_scales<1>(xs + i * 4 * x_tiles, a + sf_at + (T + i) * kMx4Tile, lead);
-                if (x_tiles == 2) tc_copy_scales<1>(xs + i * 8 + 4, a + sf_at + (2 * T + i) * kMx4Tile, lead);
+                tc_copy_scales<1>(xs + i * 4, a + sf_at + (T + i) * kMx4Tile, lead);
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int i = E8M0 ? k >> 1 : k;
                 tc_mma_mx4<1, E8M0>(tmem, da + 2 * k, db + 2 * k, E8M0 ? tc_idesc_mx4_half(idesc, k & 1) : idesc, sf + i * 4,
-                                    xs + i * 4 * x_tiles, kb > kb0 || k > 0, lead);
+                                    xs + i * 4, kb > kb0 || k > 0, lead);
             }
             tc_commit<1>(&sh.empty[s], lead);
             if (++s == plan.stages) { s = 0; ph ^= 1; }
@@ -402,10 +396,10 @@ mx4_split_kernel(const Mx4LinearArgs p, const __grid_constant__ CUtensorMap mapX
                              : "r"(cluster_map(part + r * pitch + c, k)) : "memory");
             v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
         }
-        const float sx = p.x_step ? p.x_step[row0 + r] : 1.0f;
+        const float sx = p.x_step ? p.x_step[r] : 1.0f;
         const float y[4] = {__fmaf_rn(v.x * sx, col[0].step, col[0].bias), __fmaf_rn(v.y * sx, col[1].step, col[1].bias),
                             __fmaf_rn(v.z * sx, col[2].step, col[2].bias), __fmaf_rn(v.w * sx, col[3].step, col[3].bias)};
-        uint16_t *dst = p.out + (row0 + r) * p.ldo + o0 + c;
+        uint16_t *dst = p.out + r * p.ldo + o0 + c;
         if (vec_out && o0 + c + 4 <= p.O)
             *reinterpret_cast<uint2 *>(dst) = make_uint2(D::encode2(y[0], y[1]), D::encode2(y[2], y[3]));
         else
@@ -423,12 +417,11 @@ static aweq_status m4_split_launch(const Mx4LinearArgs &a, int slices, cudaStrea
 {
     constexpr int T = mx4_group_tiles(FMT);
     M4SplitPlan s;
-    s.bn = a.N >= 256 ? 256 : (int)((a.N + 15) / 16 * 16);
+    s.bn = (int)((a.N + 15) / 16 * 16);
     s.slices = slices;
-    const int x_tiles = s.bn > 128 ? 2 : 1;
-    s.stage_bytes = (128 + s.bn) * kM4Block + (1 + x_tiles) * T * kMx4Tile;
+    s.stage_bytes = (128 + s.bn) * kM4Block + 2 * T * kMx4Tile;
     s.stage_bytes = (s.stage_bytes + 1023) / 1024 * 1024;
-    s.scale_cols = T * 4 * (1 + x_tiles);
+    s.scale_cols = T * 8;
     s.cols = 32;
     while (s.cols < s.bn + 2 * s.scale_cols) s.cols *= 2;
     // (no more stages than a slice has blocks: 16 x 4096 x 4096 in four slices 5.0 us, with eight stages 5.5)
@@ -446,7 +439,7 @@ static aweq_status m4_split_launch(const Mx4LinearArgs &a, int slices, cudaStrea
     if (rc != AWEQ_OK) return rc;
     static std::atomic<unsigned long long> allowed{0};
     AWEQ_CUDA_OK(allow_smem(mx4_split_kernel<D, FMT>, 226 * 1024, allowed));
-    const dim3 grid((unsigned)slices, (unsigned)((a.O + 127) / 128), (unsigned)((a.N + s.bn - 1) / s.bn));
+    const dim3 grid((unsigned)slices, (unsigned)((a.O + 127) / 128));
     const int vec = (a.ldo % 4 == 0) && ((reinterpret_cast<uintptr_t>(a.out) & 7) == 0);
     const cudaError_t e = launch_pdl_cluster(mx4_split_kernel<D, FMT>, grid, dim3(256), (size_t)smem, stream, (unsigned)slices, a, mx, mw, s, vec);
     note_launch();
