@@ -658,7 +658,8 @@ tree_units_kernel(const TreeArgs a, const TreePlan p, const __grid_constant__ CU
             float2 *const ml = reinterpret_cast<float2 *>(ws + (it.own ? p.off_own_ml : p.off_pre_ml));
             float *const dst = reinterpret_cast<float *>(ws + (it.own ? p.off_own_o : p.off_pre_o)) + tree_record(p, it.own, rec, 0, hd);
             const int step = (it.own ? p.own_rec : p.pre_rec) * 8;
-            const float base = m == -CUDART_INF_F ? m : __fmul_rn(m, scale) - kShift;
+            // (the shift of the probabilities is the join's to take out: behind a score of 2^24 and more it would be lost in the rounding here)
+            const float base = m == -CUDART_INF_F ? m : __fmul_rn(m, scale);
             if (!fresh && !(ok = __all_sync(0xffffffffu, mbar_wait(&sh.pv_done[sum], cnt & 1)))) break;            // (pass cnt - 1)
             tc_fence_after();
             if (TWO) {
@@ -803,6 +804,7 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, int parts, const unsigned c
     if (sees) place[before + __popc(seen & ((1u << lane) - 1))] = at;
     __syncthreads();
     const float scale = a.scale * 1.4426950408889634f;
+    constexpr float kRecord = D::kBf16 ? 1.0f : 1.0f / 128.0f;  // 2^-kProbabilityShift: what a record has is as much larger
     const bool none = nodes == 0 && s.base <= 0 && a.prefix_len == 0;
     for (int block = part * kTjWarps + warp; block < blocks; block += parts * kTjWarps) {
         const int h = block * HB, kh = h / G, g = h - kh * G;
@@ -912,7 +914,7 @@ tree_join_kernel(const TreeArgs a, const TreePlan p, int parts, const unsigned c
 #pragma unroll
             for (int i = 0; i < HB; ++i) {
                 if (y[i].x == -CUDART_INF_F && y[i].y == 0.0f) continue;        // (its output may be anything)
-                const float to = fmaxf(m[i], y[i].x), f = m[i] == -CUDART_INF_F ? 0.0f : exp2_fast(m[i] - to), e = exp2_fast(y[i].x - to);
+                const float to = fmaxf(m[i], y[i].x), f = m[i] == -CUDART_INF_F ? 0.0f : exp2_fast(m[i] - to), e = exp2_fast(y[i].x - to) * kRecord;
                 l[i] = l[i] * f + y[i].y * e;                   // (a sum that is no number stays one)
                 m[i] = to;
                 const float w[8] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w, v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};

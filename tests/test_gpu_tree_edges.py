@@ -187,3 +187,44 @@ def test_items_that_take_longer_than_a_wait_may():
     out = attend(torch.zeros((rows, 16, 8), dtype=torch.float16, device="cuda"), i32([[1, 2]]), i32([rows]), i32([0, rows]),
                  torch.ones((rows, 3), dtype=torch.int64, device="cuda"), st=st)
     assert not st.any() and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("counts,h", [([5, 3], 4), ([90, 70], 4)])
+@pytest.mark.parametrize("dtype,log2_size", [(torch.float16, e) for e in (4, 8, 9, 12, 13, 15)] + [(torch.bfloat16, e) for e in (8, 13, 16, 20, 24)])
+def test_scores_far_beyond_the_exponents_resolution(counts, h, dtype, log2_size):
+    """Queries and keys of plus and minus 2^e: scores are exact, and a few keys lead by so much that the softmax has nothing else (another
+    key is 2 2^(2e) / 8 below, 64 at least).  Where several lead, in the prefix, before the tree and the node itself, the output is the mean
+    of their values: a third is off by 2^-23, their sum by 2 2^-23, and it is rounded once."""
+    ctx, d = [300, 41], 64
+    case = Case(counts, ctx, h, h, d, 100, 16, dtype, stale=False, max_nodes=max(counts))
+    g = torch.Generator(device="cuda").manual_seed(5)
+    sign = lambda *s: torch.randint(0, 2, s, generator=g, device="cuda").mul_(2).sub_(1).to(dtype) * 2.0 ** log2_size  # noqa: E731
+    case.cache.k.copy_(sign(*case.cache.k.shape))
+    case.q.copy_(sign(1, h, d).expand(case.rows, h, d))
+    mask = torch.zeros_like(case.mask)
+    t = 0
+    leads = []
+    for b, n in enumerate(counts):
+        for i in range(n):
+            mask[t + i, i // 64] = (1 << i % 64) - (2 ** 64 if i % 64 == 63 else 0)
+        leads.append([(case.prefix_pages[37 // 16], 37 % 16), (case.table[b, 29 // 16], 29 % 16)])
+        t += n
+    places = lambda b, n: [(case.table[b, (ctx[b] + i) // 16], (ctx[b] + i) % 16) for i in range(n)]  # noqa: E731
+    k, v = case.cache.k, case.cache.v
+    attend = case.attend()
+    for which in range(1, 8):
+        kept = k.clone()
+        t, want = 0, []
+        for b, n in enumerate(counts):
+            here = [leads[b][j] for j in range(2) if which >> j & 1]
+            for page, row in here:
+                k[page.long(), row] = case.q[0]
+            for page, row in places(b, n):
+                k[page.long(), row] = case.q[0] if which & 4 else -case.q[0]
+                parts = [v[p.long(), r].double() for p, r in here] + ([v[page.long(), row].double()] if which & 4 else [])
+                want.append(sum(parts) / len(parts))
+        out = attend(case.q, case.table, case.own_len, case.start, mask)
+        want = torch.stack(want)
+        worst = v.double().abs().max()
+        assert ((out.double() - want).abs() <= U16[dtype] * want.abs() + 4 * 2.0 ** -23 * worst + TINY[dtype]).all(), which
+        k.copy_(kept)
