@@ -850,7 +850,7 @@ class PagePool:
                                _stream())
         if rc:
             raise AweqError(rc)
-        into.first, into.trees = first, up is not None
+        into.first, into.trees = first, parent is not None or not into.max_tokens
         return into
 
 

@@ -82,3 +82,13 @@ def test_what_is_refused_stores_nothing(layer, wrong):  # noqa: F811
     with pytest.raises(ValueError):
         block.verify(layer[1][:8].contiguous(), attend, table[:1] if wrong == "table" else table, plan)
     assert not block.cache.k.any()
+
+
+def test_no_rows_at_all(layer):  # noqa: F811
+    """A plan without rows has no masks to be stale: nothing is answered, nothing stored."""
+    block = make_block(layer, "e4m3", 8)
+    plan, attend, table = aweq.StepPlan(2, 0, 4), block.drafts(2, 0, 4, max_own=32), i32([[-1] * 2, [-1] * 2])
+    for parent in (None, i32([])):
+        aweq.PagePool(8, PAGE).plan(table, i32([0, 0]), i32([0, 0]), plan, parent=parent)
+        assert block.verify(layer[1][:0], attend, table, plan).shape == (0, block.o.C_out)
+    assert not block.cache.k.any()
