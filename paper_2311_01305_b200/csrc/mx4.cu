@@ -94,7 +94,7 @@ __device__ __forceinline__ uint32_t mx4_top(const float2 (&v)[8])
 // A CTA takes a row, a thread V chunks of 16 columns; rows go round-robin over the grid with the next row's loads in flight.
 // The factors of a thread's columns stay in registers where it has one chunk; its values do between their maximum and their codes.
 // The steps are binary32, the one rounding is the element's (and, E4M3, the scale's).  Bound by memory, and close behind by its
-// instructions (58 % of the SMs' peak): 11008 x 4096 to blocks of 16 in 26.5 us, 4.4 TB/s; 16 x 5120 3.2 us, all latency.  Loads of 32
+// instructions (70 % of the issue slots): 11008 x 4096 to blocks of 16 in 26.5 us, 4.4 TB/s; 16 x 5120 3.2 us, all latency.  Loads of 32
 // bytes in the place of two of 16 were slower (30 us: the registers wait for the later half).
 template <class D, int FMT, int V, bool EPS>
 __global__ void __launch_bounds__(V == 1 ? 512 : 1024)

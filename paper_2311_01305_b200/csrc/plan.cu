@@ -181,7 +181,7 @@ __device__ __forceinline__ int plan_page(const KvPlanArgs &a, const PlanEnds &e,
 
 // Tokens in a row, four to a thread (so that a warp's stores lie together: with eight the sectors came in halves, 22.5 us in the place
 // of 16.5 for 1.6 million tokens): one search, one division, and a look-up for each page they touch; runs within a sequence, which nearly
-// all are, without a test for every token (15 to 14 us: 61 % of the issue slots before).
+// all are, without a test for every token (15 to 14 us; 60 % of the issue slots).
 __device__ __forceinline__ void plan_tokens(const KvPlanArgs &a, const PlanEnds &e, const PlanSeq *seqs, int total)
 {
     constexpr int M = 4;
