@@ -548,10 +548,11 @@ aweq_status aweq_kv_append_slots(const aweq_kv_cache *cache, const long long *sl
  * pages put back go to the other (this call takes none of those that it puts back).  n_pages at most 2^22, n_seq 2^30.
  * Where something does not fit, it is counted in st->out_of_range, once for each sequence: a length or change beyond 0 ..
  * pages_per_seq * page_size or the max_tokens rows is clamped, a sequence that finds no free pages keeps own_len within what it
- * has, and its tokens without a page get slot -1 (start still counts them, and own_len no longer says where the sequence's tokens begin:
- * attention of such trees is aweq_tree_attention_planned's, and what is given up next goes by own_len), pages put back beyond n_pages are lost.  Also counted: each page number outside
- * 0 .. n_pages in the ring that is taken, each parent that is none of the nodes before (the node then has none), each node
- * beyond 64 * words (mask 0, depth 0), and a state that cannot be, which is taken as an empty ring.
+ * has, and its tokens without a page get slot -1 (start still counts them, and own_len no longer says where the sequence's new
+ * tokens begin: attention of such trees is aweq_tree_attention_planned's, and what is given up next goes by own_len), pages put
+ * back beyond n_pages are lost.  Also counted: each page number outside 0 .. n_pages in the ring that is taken, each parent that is
+ * none of the nodes before (the node then has none), each node beyond 64 * words (mask 0, depth 0), and a state that cannot be,
+ * which is taken as an empty ring.
  * own_len must not be held or change.  seq, pos, slot, mask and ws 16-byte aligned (not read for max_tokens = 0).
  * ws: aweq_kv_plan_workspace_bytes(n_seq) bytes, 256-byte aligned, zero before its first call, for one stream at a time. */
 size_t aweq_kv_plan_workspace_bytes(long long n_seq);
@@ -608,9 +609,9 @@ aweq_status aweq_prefix_attention(const void *q, long long ldq, const aweq_kv_ca
  * start[n_seq] on stay as they were.  start: device int[n_seq + 1], ascending from 0; mask: device [max_tokens x words] 64-bit words,
  * words >= ceil(max_nodes / 64).  max_nodes (to 256), max_own: HOST bounds on a sequence's nodes and own keys.
  * Lengths and starts out of range are clamped (a start below one before it counts as that one, so that no token has two
- * sequences), nodes beyond max_nodes are not computed (the last keys are still those of all nodes, and a key beyond max_own or the table is
- * no node's and nobody's), a page outside the pool is replaced by page 0; st->out_of_range counts each sequence with such a length or start, and each such entry of prefix_pages and page_table that holds
- * keys, once.  max_tokens * n_heads at most 2^31 - 1.
+ * sequences), nodes beyond max_nodes are not computed (the last keys are still those of all nodes), a key beyond max_own or the table
+ * is nobody's, a page outside the pool is replaced by page 0; st->out_of_range counts each sequence with such a length or start, and
+ * each such entry of prefix_pages and page_table that holds keys, once.  max_tokens * n_heads at most 2^31 - 1.
  * ws: aweq_tree_attention_workspace_bytes(...) bytes, 256-byte aligned. */
 size_t aweq_tree_attention_workspace_bytes(const aweq_kv_cache *cache, long long prefix_len, long long max_own, long long n_seq,
                                            long long max_tokens, int max_nodes, int n_heads);
